@@ -218,7 +218,8 @@ enum triroute_op {
   TRIROUTE_OP_LAYER_DECODE = 7,
   TRIROUTE_OP_STACK_DECODE = 8,
   TRIROUTE_OP_ROUTER_RELAXED = 9,
-  TRIROUTE_OP_ROUTER_RELAXED_BACKWARD = 10
+  TRIROUTE_OP_ROUTER_RELAXED_BACKWARD = 10,
+  TRIROUTE_OP_MOE_BACKWARD = 11
 };
 
 /* ---- configuration, errors, sizes ---------------------------------------- */
@@ -540,6 +541,95 @@ int triroute_router_relaxed_backward(const triroute_cfg *cfg, int B, int T, cons
                                      const float *egate, const triroute_relax_grad_in *gin,
                                      const triroute_relax_grad_out *gout, void *ws,
                                      size_t ws_bytes, triroute_stream_t stream);
+
+/* ---- backward pass of the experts ------------------------------------------ */
+
+/* Gradients of triroute_moe (device, overwritten).
+ *   dxt     act [N, d]: of xt, the residual's share included
+ *   dWgate, dWup [E, d_ff, d], dWdown [E, d, d_ff] act: all three, or all three
+ *           NULL (frozen experts: their products are not computed); zeros for
+ *           an expert without tokens
+ *   dg2     act [d], or NULL
+ *   g_gate  f32 [N, k], or NULL: of egate (0 for null slots), which is the g_gate that
+ *           triroute_router_relaxed_backward takes
+ * dxt may be dx_out itself (the same pointer); otherwise outputs overlap
+ * neither inputs nor each other. */
+typedef struct triroute_moe_grad_out {
+  void *dxt;
+  void *dWgate, *dWup, *dWdown;
+  void *dg2;
+  float *g_gate;
+} triroute_moe_grad_out;
+
+/* Backward pass of triroute_moe for n_tok tokens (Sec. 3.2 (B) expert equation,
+ * Sec. 3.1 second half of the block).  With n = n2 as the forward rounds it,
+ * e = eidx and p = egate of a slot, G = Wgate_e n, U = Wup_e n, s = 1 / (1 + exp(-G)),
+ * q = Wdown_e^T dx_out, per slot with e != 0:
+ *   g_gate = <q, s G U>,  dU = p q s G,  dG = p q U s (1 + G (1 - s)),
+ *   dWdown_e += dx_out (p s G U)^T,  dWgate_e += dG n^T,  dWup_e += dU n^T,
+ *   dn += Wgate_e^T dG + Wup_e^T dU;
+ * then through the norm, r = 1 / sqrt(mean(xt^2) + eps):
+ *   dxt = dx_out + r (dn g2) - r^3 xt <dn g2, xt> / d,  dg2 = sum over tokens of dn r xt.
+ * G, U and the hidden rows are computed again from xt, so the forward keeps
+ * nothing.  bf16: products sum in fp32; dG, dU and p s G U are rounded to bf16
+ * once, as operands of the products that follow; g_gate sees none of these
+ * roundings.  The order of every sum depends on the sizes and the expert lists alone.
+ *   xt, dx_out act [N, d]; eidx, egate, cmp as given to triroute_moe (of cmp the
+ *   expert lists are read); dw: g2 is read;
+ *   ws: triroute_workspace_bytes(cfg, TRIROUTE_OP_MOE_BACKWARD, n_tok, 1) bytes. */
+int triroute_moe_backward(const triroute_cfg *cfg, int n_tok, const void *xt,
+                          const triroute_dense_w *dw, const triroute_moe_w *w,
+                          const int32_t *eidx, const float *egate,
+                          const triroute_compaction *cmp, const void *dx_out,
+                          const triroute_moe_grad_out *out, void *ws, size_t ws_bytes,
+                          triroute_stream_t stream);
+
+/* ---- gradient norm and clipping --------------------------------------------- */
+
+/* One gradient tensor: numel elements (0 or more) of type dtype (enum triroute_dtype) at src, aligned
+ * to its element; dst (the same size and type, aligned alike; NULL if the list is
+ * only measured) takes the clipped values and is src itself or overlaps no tensor's src. */
+typedef struct triroute_grad_tensor {
+  const void *src;
+  void *dst;
+  int64_t numel;
+  int32_t dtype;
+} triroute_grad_tensor;
+
+/* A list of gradient tensors, laid out in the caller's memory by
+ * triroute_grad_list_init; treat the fields as read-only.  It holds addresses, so it serves for as long as
+ * the tensors stay where they are. */
+typedef struct triroute_grad_list {
+  void *base;
+  int64_t n_pieces;
+  int32_t n_tensors;
+  int32_t has_dst; /* every tensor that has elements has a dst */
+} triroute_grad_list;
+
+/* Workspace of triroute_grad_norm and triroute_grad_clip (calls that may overlap need one
+ * each). */
+#define TRIROUTE_GRAD_WS_BYTES ((size_t)16 << 10)
+
+/* Bytes of the list of n tensors (tensors: host array; 1 <= n <= 2^20). */
+int triroute_grad_list_bytes(const triroute_grad_tensor *tensors, int n, size_t *bytes);
+/* Writes the list of n tensors into base (>= list_bytes, 256-byte aligned) on
+ * `stream`; `tensors` is a host array that is not read after the call. */
+int triroute_grad_list_init(triroute_grad_list *list, const triroute_grad_tensor *tensors, int n,
+                            void *base, size_t bytes, triroute_stream_t stream);
+/* *norm (device fp64) = the norm over all elements of all tensors: norm_type 2: the
+ * root of the sum of squares (summed in fp64), infinity: the largest magnitude.  An empty
+ * list has norm 0; a NaN element makes it NaN. */
+int triroute_grad_norm(const triroute_grad_list *list, double norm_type, double *norm, void *ws,
+                       size_t ws_bytes, triroute_stream_t stream);
+/* dst = src * c of every tensor, c = min(1, max_norm / *norm) rounded to fp32, the product
+ * rounded once to the tensor's type (norm: device fp64, such as triroute_grad_norm
+ * leaves, or one joined over ranks).  A NaN norm gives NaN.  max_norm >= 0.  Tensors whose dst is
+ * their src are left as they are when c is 1. */
+int triroute_grad_scale(const triroute_grad_list *list, const double *norm, double max_norm,
+                        triroute_stream_t stream);
+/* triroute_grad_norm and triroute_grad_scale in two launches: the same norm and values. */
+int triroute_grad_clip(const triroute_grad_list *list, double norm_type, double max_norm,
+                       double *norm, void *ws, size_t ws_bytes, triroute_stream_t stream);
 
 /* ---- no-allocation variant ---------------------------------------------- */
 

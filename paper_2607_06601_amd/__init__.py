@@ -20,7 +20,7 @@ F32, BF16 = 0, 1
 SKIP, LOCAL, FULL = 0, 1, 2
 OP_ROUTER, OP_QKV, OP_KV_APPEND, OP_ATTN_PREFILL, OP_ATTN_DECODE, OP_MOE, \
     OP_LAYER_PREFILL, OP_LAYER_DECODE, OP_STACK_DECODE, OP_ROUTER_RELAXED, \
-    OP_ROUTER_RELAXED_BACKWARD = range(11)
+    OP_ROUTER_RELAXED_BACKWARD, OP_MOE_BACKWARD = range(12)
 # fp64 fields of RelaxOut.stats (axes in the order attention, experts, bits)
 RS_LBAL, RS_LZ, RS_LENT, RS_ENTROPY, RS_CBAR, RS_COST, RS_DENSE, RS_REG = 0, 3, 6, 9, 12, 14, 16, 18
 RS_F_ATTN, RS_P_ATTN, RS_F_BITS, RS_P_BITS, RELAX_NSTAT = 19, 22, 25, 29, 33
@@ -109,6 +109,22 @@ class RelaxGradOut(C.Structure):
                  "dg1", "dx", "dpsi", "lm_norm")]
 
 
+class MoeGradOut(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("dxt", "dWgate", "dWup", "dWdown", "dg2", "g_gate")]
+
+
+class GradTensor(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("numel", C.c_int64),
+                ("dtype", C.c_int32)]
+
+
+class GradListDesc(C.Structure):
+    _fields_ = [("base", C.c_void_p), ("n_pieces", C.c_int64), ("n_tensors", C.c_int32),
+                ("has_dst", C.c_int32)]
+
+
+GRAD_WS_BYTES = 16 << 10  # TRIROUTE_GRAD_WS_BYTES
+
 EXPORTS = [
     "triroute_validate", "triroute_status_string", "triroute_last_error",
     "triroute_workspace_bytes", "triroute_kv_cache_bytes", "triroute_kv_cache_init",
@@ -118,6 +134,8 @@ EXPORTS = [
     "triroute_layer_prefill", "triroute_layer_decode", "triroute_layer_decode_noalloc",
     "triroute_stack_decode", "triroute_router_relaxed", "triroute_router_relaxed_backward",
     "triroute_kv_paged_cache_bytes", "triroute_kv_paged_cache_init", "triroute_kv_free_pages",
+    "triroute_moe_backward", "triroute_grad_list_bytes", "triroute_grad_list_init",
+    "triroute_grad_norm", "triroute_grad_scale", "triroute_grad_clip",
 ]
 
 _lib = None
@@ -158,6 +176,12 @@ def lib():
             "triroute_stack_decode": [P, i32, i32, P, P, P, P, P, P, P, sz, P],
             "triroute_router_relaxed": [P, i32, i32, P, P, P, P, P, P, P, P, P, P, P, P, sz, P],
             "triroute_router_relaxed_backward": [P, i32, i32, P, P, P, P, P, P, P, P, P, P, sz, P],
+            "triroute_moe_backward": [P, i32, P, P, P, P, P, P, P, P, P, sz, P],
+            "triroute_grad_list_bytes": [P, i32, C.POINTER(sz)],
+            "triroute_grad_list_init": [P, P, i32, P, sz, P],
+            "triroute_grad_norm": [P, C.c_double, P, P, sz, P],
+            "triroute_grad_scale": [P, P, C.c_double, P],
+            "triroute_grad_clip": [P, C.c_double, C.c_double, P, P, sz, P],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -346,6 +370,14 @@ def moe(cfg, n_tok, xt, dw: DenseW, mw: MoeW, eidx, egate, cmp: Compaction, x_ou
                               _stream(stream)))
 
 
+def moe_backward(cfg, n_tok, xt, dw: DenseW, mw: MoeW, eidx, egate, cmp: Compaction, dx_out,
+                 out: MoeGradOut, ws, stream=None):
+    """Backward pass of the experts (triroute_moe_backward)."""
+    _check(lib().triroute_moe_backward(
+        C.byref(cfg), n_tok, _p(xt), C.byref(dw), C.byref(mw), _p(eidx), _p(egate), C.byref(cmp),
+        _p(dx_out), C.byref(out), _p(ws), ws.numel(), _stream(stream)))
+
+
 def layer_prefill(cfg, B, T, x, psi, rw, dw, mw, cache: KVCache, x_out, ws, taps=None,
                   seq_ids=None, stream=None):
     _check(lib().triroute_layer_prefill(
@@ -379,6 +411,69 @@ def stack_decode(cfg, B, x, psi, layers, caches, x_out, ws, seq_ids=None, stream
     _check(lib().triroute_stack_decode(
         C.byref(cfg), n, B, _p(seq_ids), _p(x), _p(psi), lw, cs, _p(x_out), _p(ws), ws.numel(),
         _stream(stream)))
+
+
+# ------------------------------------------------- gradient norm and clipping
+class GradList:
+    """The device list of gradient tensors (triroute_grad_list_init): ``tensors``
+    are contiguous fp32 or bf16 device tensors of any size and element
+    alignment; ``dst`` (alike; None: the tensors themselves) takes the
+    clipped values.  The tensors are held, so the list stays valid."""
+
+    def __init__(self, tensors, dst=None, stream=None):
+        dst = list(tensors) if dst is None else list(dst)
+        self.tensors, self.dst = list(tensors), dst
+        n = len(self.tensors)
+        if n == 0 or len(dst) != n:
+            raise ValueError("GradList takes one or more tensors and as many destinations")
+        arr = (GradTensor * n)()
+        for i, (a, b) in enumerate(zip(self.tensors, dst)):
+            for t in (a, b):
+                if t.dtype not in (torch.float32, torch.bfloat16) or not t.is_contiguous() \
+                        or t.device != self.tensors[0].device:
+                    raise ValueError(f"tensor {i}: contiguous fp32 or bf16 on one device wanted")
+            if a.dtype != b.dtype or a.numel() != b.numel():
+                raise ValueError(f"tensor {i}: destination of another type or size")
+            arr[i] = GradTensor(a.data_ptr(), b.data_ptr(), a.numel(),
+                                BF16 if a.dtype == torch.bfloat16 else F32)
+        need = C.c_size_t()
+        _check(lib().triroute_grad_list_bytes(arr, n, C.byref(need)))
+        self.buf = torch.empty(need.value, dtype=torch.uint8, device=self.tensors[0].device)
+        self.desc = GradListDesc()
+        _check(lib().triroute_grad_list_init(C.byref(self.desc), arr, n, self.buf.data_ptr(),
+                                             need.value, _stream(stream)))
+
+    @property
+    def ref(self):
+        return C.byref(self.desc)
+
+
+def grad_workspace(device="cuda"):
+    """Workspace of grad_norm and grad_clip."""
+    return torch.empty(GRAD_WS_BYTES, dtype=torch.uint8, device=device)
+
+
+def _norm_p(norm):
+    if norm.dtype != torch.float64 or norm.numel() != 1:
+        raise ValueError("norm: one fp64 element")
+    return norm.data_ptr()
+
+
+def grad_norm(grads: GradList, norm, ws, norm_type=2.0, stream=None):
+    """norm (fp64, one element) = the norm over all tensors of the list."""
+    _check(lib().triroute_grad_norm(grads.ref, norm_type, _norm_p(norm), _p(ws), ws.numel(),
+                                    _stream(stream)))
+
+
+def grad_scale(grads: GradList, norm, max_norm, stream=None):
+    """dst = src * min(1, max_norm / norm) for every tensor of the list."""
+    _check(lib().triroute_grad_scale(grads.ref, _norm_p(norm), max_norm, _stream(stream)))
+
+
+def grad_clip(grads: GradList, max_norm, norm, ws, norm_type=2.0, stream=None):
+    """grad_norm, then grad_scale, in two launches."""
+    _check(lib().triroute_grad_clip(grads.ref, norm_type, max_norm, _norm_p(norm), _p(ws), ws.numel(),
+                                    _stream(stream)))
 
 
 # ------------------------------------------------------ device-side buffers

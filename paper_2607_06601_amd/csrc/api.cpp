@@ -237,6 +237,19 @@ RelaxBwdWs carve_relax_bwd(Carve &cv, const triroute_cfg &c, int N) {
   return w;
 }
 
+void carve_moe_grad(Carve &cv, const triroute_cfg &c, int N, tr::MoeGradJob &j) {
+  const size_t ab = act_bytes(c), rows = size_t(tr::moe_grad_rows(c, N));
+  j.n2 = cv.take<uint8_t>(rows * c.d_model * ab);
+  j.dy = cv.take<uint8_t>(rows * c.d_model * ab);
+  j.dGU = cv.take<uint8_t>(rows * c.d_ff * 2 * ab);
+  j.Hp = cv.take<uint8_t>(rows * c.d_ff * ab);
+  j.Y = cv.take<float>(rows * c.d_model);
+  j.gpart = cv.take<float>(rows * tr::moe_grad_gate_parts(c));
+  j.gate = cv.take<float>(rows);
+  j.row_of = cv.take<int32_t>(size_t(N) * c.top_k);
+  j.part = cv.take<float>(size_t(tr::moe_grad_part_rows(N)) * c.d_model);
+}
+
 size_t op_bytes(const triroute_cfg &c, int op, int B, int T) {
   Carve cv(nullptr);
   const int N = B * T;
@@ -272,6 +285,11 @@ size_t op_bytes(const triroute_cfg &c, int op, int B, int T) {
       carve_relax(cv, c, N);
       carve_relax_bwd(cv, c, N);
       break;
+    case TRIROUTE_OP_MOE_BACKWARD: {
+      tr::MoeGradJob j;
+      carve_moe_grad(cv, c, N, j);
+      break;
+    }
     default: return 0;
   }
   return cv.used;
@@ -354,6 +372,46 @@ int check_cache(const triroute_cfg &c, const triroute_kv_cache *kc, int B, int T
     int r_ = (expr);              \
     if (r_ != TRIROUTE_OK) return r_; \
   } while (0)
+
+// The gradient tensors of a list: a host array, checked before anything is
+// launched; *pieces is what the list holds.
+int check_grads(const triroute_grad_tensor *t, int n, int64_t *pieces) {
+  REQUIRE(n >= 1 && n <= (1 << 20), TRIROUTE_E_INVALID, "n (%d) must be in [1, 2^20]", n);
+  int64_t sum = 0;
+  for (int i = 0; i < n; ++i) {
+    REQUIRE(t[i].dtype == TRIROUTE_F32 || t[i].dtype == TRIROUTE_BF16, TRIROUTE_E_INVALID,
+            "tensor %d: dtype %d", i, t[i].dtype);
+    REQUIRE(t[i].numel >= 0 && t[i].numel <= (int64_t(1) << 40), TRIROUTE_E_INVALID,
+            "tensor %d: numel %lld", i, (long long)t[i].numel);
+    REQUIRE(t[i].numel == 0 || t[i].src, TRIROUTE_E_INVALID, "tensor %d: NULL src", i);
+    const uintptr_t m = t[i].dtype == TRIROUTE_BF16 ? 1 : 3;
+    REQUIRE(t[i].numel == 0 || ((uintptr_t(t[i].src) | uintptr_t(t[i].dst)) & m) == 0,
+            TRIROUTE_E_INVALID, "tensor %d: a pointer is not aligned to its element", i);
+    sum += tr::grad_pieces(t[i]);
+  }
+  *pieces = sum;
+  return TRIROUTE_OK;
+}
+
+int check_grad_call(const triroute_grad_list *l, double norm_type, const double *norm, const void *ws,
+                    size_t ws_bytes) {
+  REQUIRE(l && l->base && norm && ws, TRIROUTE_E_INVALID, "NULL argument");
+  REQUIRE(norm_type == 2.0 || (isinf(norm_type) && norm_type > 0), TRIROUTE_E_UNSUPPORTED,
+          "norm_type %g: 2 or infinity", norm_type);
+  REQUIRE(ws_bytes >= TRIROUTE_GRAD_WS_BYTES, TRIROUTE_E_WORKSPACE, "workspace %zu bytes < %zu needed",
+          ws_bytes, TRIROUTE_GRAD_WS_BYTES);
+  REQUIRE(((uintptr_t(ws) & 255) | (uintptr_t(norm) & 7)) == 0, TRIROUTE_E_INVALID,
+          "workspace must be 256-byte aligned, norm 8-byte");
+  return TRIROUTE_OK;
+}
+
+int check_grad_dst(const triroute_grad_list *l, const double *norm, double max_norm) {
+  REQUIRE(l && l->base && norm, TRIROUTE_E_INVALID, "NULL argument");
+  REQUIRE((uintptr_t(norm) & 7) == 0, TRIROUTE_E_INVALID, "norm must be 8-byte aligned");
+  REQUIRE(l->has_dst, TRIROUTE_E_INVALID, "a tensor of the list has no dst");
+  REQUIRE(max_norm >= 0.0, TRIROUTE_E_INVALID, "max_norm (%g) must be >= 0", max_norm);
+  return TRIROUTE_OK;
+}
 
 void layout_cache(const triroute_cfg &c, int n_seq, int capacity, triroute_kv_cache *kc) {
   memset(kc, 0, sizeof *kc);
@@ -523,7 +581,7 @@ int triroute_workspace_bytes(const triroute_cfg *cfg, int op, int B, int T, size
   TRY(check_cfg(cfg));
   TRY(check_bt(B, T));
   REQUIRE(bytes, TRIROUTE_E_INVALID, "bytes is NULL");
-  REQUIRE(op >= TRIROUTE_OP_ROUTER && op <= TRIROUTE_OP_ROUTER_RELAXED_BACKWARD, TRIROUTE_E_INVALID,
+  REQUIRE(op >= TRIROUTE_OP_ROUTER && op <= TRIROUTE_OP_MOE_BACKWARD, TRIROUTE_E_INVALID,
           "unknown op %d", op);
   *bytes = op_bytes(*cfg, op, B, T);
   return TRIROUTE_OK;
@@ -1099,6 +1157,104 @@ int triroute_stack_decode(const triroute_cfg *cfg, int n_layers, int B, const in
       CHECK_HIP(tr::launch_psi_next(*cfg, B, psi, S.mode, S.bit, S.eidx, S.psi, st), "psi launch");
     xin = xo;
   }
+  return TRIROUTE_OK;
+}
+
+int triroute_moe_backward(const triroute_cfg *cfg, int n_tok, const void *xt,
+                          const triroute_dense_w *dw, const triroute_moe_w *w,
+                          const int32_t *eidx, const float *egate,
+                          const triroute_compaction *cmp, const void *dx_out,
+                          const triroute_moe_grad_out *out, void *ws, size_t ws_bytes,
+                          triroute_stream_t stream) {
+  TRY(check_cfg(cfg));
+  TRY(check_bt(n_tok, 1));
+  REQUIRE(xt && dw && dw->g2 && w && w->Wgate && w->Wup && w->Wdown && eidx && egate && cmp &&
+              cmp->exp_cnt && cmp->exp_off && cmp->exp_rows && dx_out && out && out->dxt,
+          TRIROUTE_E_INVALID, "NULL argument");
+  REQUIRE(!out->dWgate == !out->dWup && !out->dWgate == !out->dWdown, TRIROUTE_E_INVALID,
+          "dWgate, dWup and dWdown must all be given or all be NULL");
+  TRY(check_aligned({xt, dw->g2, w->Wgate, w->Wup, w->Wdown, dx_out, out->dxt, out->dWgate, out->dWup,
+                     out->dWdown, out->dg2}));
+  TRY(check_ws(*cfg, TRIROUTE_OP_MOE_BACKWARD, n_tok, 1, ws, ws_bytes));
+  Carve cv(ws);
+  tr::MoeGradJob j;
+  carve_moe_grad(cv, *cfg, n_tok, j);
+  j.xt = xt; j.dx = dx_out; j.g2 = dw->g2; j.eidx = eidx; j.egate = egate;
+  j.w = *w; j.cmp = *cmp; j.out = *out;
+  CHECK_HIP(tr::launch_moe_backward(*cfg, n_tok, j, (hipStream_t)stream), "moe backward launch");
+  return TRIROUTE_OK;
+}
+
+// ---- gradient norm and clipping ----
+
+int triroute_grad_list_bytes(const triroute_grad_tensor *tensors, int n, size_t *bytes) {
+  REQUIRE(tensors && bytes, TRIROUTE_E_INVALID, "NULL argument");
+  int64_t pieces = 0;
+  TRY(check_grads(tensors, n, &pieces));
+  *bytes = align256(size_t(std::max<int64_t>(pieces, 1)) * sizeof(tr::GradRec));
+  return TRIROUTE_OK;
+}
+
+int triroute_grad_list_init(triroute_grad_list *list, const triroute_grad_tensor *tensors, int n,
+                            void *base, size_t bytes, triroute_stream_t stream) {
+  REQUIRE(list && tensors && base, TRIROUTE_E_INVALID, "NULL argument");
+  int64_t pieces = 0;
+  TRY(check_grads(tensors, n, &pieces));
+  const size_t need = align256(size_t(std::max<int64_t>(pieces, 1)) * sizeof(tr::GradRec));
+  REQUIRE(bytes >= need, TRIROUTE_E_WORKSPACE, "list memory %zu bytes < %zu needed", bytes, need);
+  REQUIRE((uintptr_t(base) & 255) == 0, TRIROUTE_E_INVALID, "list memory must be 256-byte aligned");
+  triroute_grad_list l{};
+  l.base = base;
+  l.n_pieces = pieces;
+  l.n_tensors = n;
+  l.has_dst = 1;
+  int64_t at = 0;
+  for (int i = 0; i < n; i += tr::GRAD_BATCH) {
+    tr::GradBatch b{};
+    const int m = std::min(n - i, tr::GRAD_BATCH);
+    int64_t most = 0;
+    for (int j = 0; j < m; ++j) {
+      const triroute_grad_tensor &t = tensors[i + j];
+      b.t[j] = tr::GradDesc{t.src, t.dst, t.numel, t.dtype};
+      b.first[j] = at;
+      const int64_t p = tr::grad_pieces(t);
+      if (p > 0 && !t.dst) l.has_dst = 0;
+      at += p;
+      most = std::max(most, p);
+    }
+    b.first[m] = at;
+    CHECK_HIP(tr::launch_grad_list(b, m, most, (tr::GradRec *)base, (hipStream_t)stream),
+              "grad list launch");
+  }
+  *list = l;
+  return TRIROUTE_OK;
+}
+
+int triroute_grad_norm(const triroute_grad_list *list, double norm_type, double *norm, void *ws,
+                       size_t ws_bytes, triroute_stream_t stream) {
+  TRY(check_grad_call(list, norm_type, norm, ws, ws_bytes));
+  CHECK_HIP(tr::launch_grad_norm((const tr::GradRec *)list->base, list->n_pieces, isinf(norm_type),
+                                 (double *)ws, norm, (hipStream_t)stream),
+            "grad norm launch");
+  return TRIROUTE_OK;
+}
+
+int triroute_grad_scale(const triroute_grad_list *list, const double *norm, double max_norm,
+                        triroute_stream_t stream) {
+  TRY(check_grad_dst(list, norm, max_norm));
+  CHECK_HIP(tr::launch_grad_scale((const tr::GradRec *)list->base, list->n_pieces, norm, max_norm,
+                                  (hipStream_t)stream),
+            "grad scale launch");
+  return TRIROUTE_OK;
+}
+
+int triroute_grad_clip(const triroute_grad_list *list, double norm_type, double max_norm,
+                       double *norm, void *ws, size_t ws_bytes, triroute_stream_t stream) {
+  TRY(check_grad_call(list, norm_type, norm, ws, ws_bytes));
+  TRY(check_grad_dst(list, norm, max_norm));
+  CHECK_HIP(tr::launch_grad_clip((const tr::GradRec *)list->base, list->n_pieces, isinf(norm_type),
+                                 max_norm, (double *)ws, norm, (hipStream_t)stream),
+            "grad clip launch");
   return TRIROUTE_OK;
 }
 

@@ -21,12 +21,10 @@
 #include <initializer_list>
 #include <type_traits>
 
+#include "gemm_tile.hpp"
 #include "kernels.hpp"
 
 namespace tr {
-
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 struct MTile {
   int m0, n0, mvalid, e, p0;
@@ -580,37 +578,6 @@ struct Moe2M {
 };
 
 // ------------------------------------------------------------------ kernel
-// Tiles of the whole problem are handed out XCD by XCD: blocks are issued to
-// the 8 XCDs round-robin, so block L runs on XCD L % 8, and it takes tile
-// number (its XCD's contiguous share) + L / 8.  Tile t covers row tile t / ny
-// and column tile t % ny, so the blocks resident on one XCD share A rows and
-// a few weight tiles in that XCD's L2.
-__device__ __forceinline__ int xcd_tile(int L, int total) {
-  const int per = total >> 3, extra = total & 7, x = L & 7;
-  return x * per + min(x, extra) + (L >> 3);
-}
-
-// Order of the tiles handed to one XCD.  The 32 CUs of an XCD run 32
-// consecutive tiles of its share at a time and stream their K loops in near
-// lockstep, so what that XCD's L2 must hold per K step is the union of their
-// operand slices.  Walking the tiles in bands of BAND_R row tiles (of one
-// expert, for grouped problems), each band in chunks of BAND_R x BAND_C
-// tiles with the row fastest, makes that union BAND_R A slices and BAND_C B
-// slices instead of one A slice and 32 B slices (the expert weights would
-// otherwise stream past the L2 once per row tile).
-constexpr int BAND_R = 16, BAND_C = 2;
-
-// Tile t of a rows x ny grid walked in bands -> (row tile i, column tile j).
-__device__ __forceinline__ void band_order(int t, int rows, int ny, int &i, int &j) {
-  const int band = t / (BAND_R * ny);
-  const int rem = t - band * BAND_R * ny;
-  const int rb = min(BAND_R, rows - band * BAND_R);  // rows of this band
-  const int chunk = rem / (rb * BAND_C);
-  const int idx = rem - chunk * rb * BAND_C;
-  i = band * BAND_R + idx % rb;
-  j = chunk * BAND_C + idx / rb;
-}
-
 // The same within each expert of a grouped problem: tile t lies in the
 // first expert whose tiles (row tiles x ny, in expert order) reach past it.
 __device__ __forceinline__ void grouped_band_order(int t, int ny, const GroupScan &gs, int &bx,
@@ -621,28 +588,6 @@ __device__ __forceinline__ void grouped_band_order(int t, int ny, const GroupSca
   int i;
   band_order(t - first * ny, nt, ny, i, by);
   bx = first + i;
-}
-
-// LDS chunk (16 bytes) of chunk c of operand row r in a stage whose rows are
-// CPR chunks long: a XOR with the row's position in its 256-byte bank span
-// makes the 16 rows read by one 16-lane phase (same c) hit 16 distinct
-// 16-byte bank groups.
-template <int CPR>
-__device__ __forceinline__ int swz(int r, int c) {
-  if constexpr (CPR == 8)
-    return c ^ ((r >> 1) & 7);  // 2 rows per 256-byte span
-  else
-    return c ^ ((r >> 2) & 3);  // 4 rows per span
-}
-
-// vmcnt(n * N) for the run-time n of stages still allowed in flight, n < S - 1
-template <int N, int S>
-__device__ __forceinline__ void wait_stages(int n) {
-  if constexpr (S > 5) if (n >= 4) { wait_vm<4 * N>(); return; }
-  if constexpr (S > 4) if (n == 3) { wait_vm<3 * N>(); return; }
-  if constexpr (S > 3) if (n == 2) { wait_vm<2 * N>(); return; }
-  if constexpr (S > 2) if (n == 1) { wait_vm<N>(); return; }
-  wait_vm<0>();
 }
 
 // Epilogue register pass: lane holds rows 4 (lane/16) + i of each 16-row tile
@@ -815,37 +760,6 @@ __global__ __launch_bounds__(64 * WM * WN * KW, 1) void gemm_mfma_kernel(P p, in
 // set while the current slice's MFMAs issue, the reads slotted between the
 // MFMAs.  Stages are double-buffered (BK = 64); stage kt + 2 goes into the
 // buffer of stage kt as soon as every wave has read it (schedule below).
-// acc += a b on the accumulator registers (AGPRs).  With 256 accumulators
-// per lane the register allocator, left to itself, parks some of them in
-// VGPRs and copies them around every MFMA; pinning them to AGPRs keeps the
-// loop free of copies.  As a volatile asm statement it also keeps its place
-// relative to the LDS reads and transfers written around it, so the program
-// order below is the issue order.
-__device__ __forceinline__ void mfma_agpr(f32x4_t &acc, const bf16x8_t &a, const bf16x8_t &b) {
-  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
-}
-// acc = a b (the first product of a tile: no zeroing of the accumulators)
-__device__ __forceinline__ void mfma_agpr_first(f32x4_t &acc, const bf16x8_t &a, const bf16x8_t &b) {
-  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=a"(acc) : "v"(a), "v"(b));
-}
-
-// The compiler does not see the MFMAs inside the asm statements, so it does
-// not keep its own accesses of the accumulators clear of their hazards.
-// Each row of accumulators passes through an asm statement that starts with
-// `nops` wait states: accesses after it are ordered after the wait, and
-// writes before it (zeroing) before the wait.
-template <int NI>
-__device__ __forceinline__ void acc_fence_row(f32x4_t (&a)[NI]) {
-  static_assert(NI == 4 || NI == 6 || NI == 8, "accumulator row widths in use");
-  if constexpr (NI == 4)
-    asm volatile("s_nop 4" : "+a"(a[0]), "+a"(a[1]), "+a"(a[2]), "+a"(a[3]));
-  else if constexpr (NI == 8)
-    asm volatile("s_nop 4" : "+a"(a[0]), "+a"(a[1]), "+a"(a[2]), "+a"(a[3]), "+a"(a[4]), "+a"(a[5]),
-                 "+a"(a[6]), "+a"(a[7]));
-  else
-    asm volatile("s_nop 4" : "+a"(a[0]), "+a"(a[1]), "+a"(a[2]), "+a"(a[3]), "+a"(a[4]), "+a"(a[5]));
-}
-
 template <class P, int BM, int BN>
 __global__ __launch_bounds__(256, 1) void gemm_w4_kernel(P p, int K, int ny) {
   constexpr int NW = 4, NT = 256, WN = 2;

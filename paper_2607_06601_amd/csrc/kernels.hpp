@@ -1,6 +1,8 @@
 // Launchers of the device kernels (internal to libtriroute).
 #pragma once
 
+#include <algorithm>
+
 #include "common.hpp"
 
 namespace tr {
@@ -213,4 +215,57 @@ hipError_t launch_relax_backward(const triroute_cfg &cfg, int N, const void *x, 
                                  const triroute_router_w &w, const float *Wf,
                                  const float *white_mu, const float *white_sd, float white_eps,
                                  const RelaxBwdJob &j, hipStream_t st);
+
+// moe_grad.hip: the experts' backward pass
+constexpr int MOE_PAD = 64;  // each expert's rows are padded to a multiple of this
+inline int64_t moe_grad_rows(const triroute_cfg &c, int N) {
+  return int64_t(N) * c.top_k + int64_t(MOE_PAD - 1) * c.n_experts;
+}
+int moe_grad_gate_parts(const triroute_cfg &cfg);
+int moe_grad_part_rows(int N);
+struct MoeGradJob {
+  const void *xt, *dx, *g2;
+  const int32_t *eidx;
+  const float *egate;
+  triroute_moe_w w;
+  triroute_compaction cmp;
+  triroute_moe_grad_out out;
+  // scratch: rows by expert (moe_grad_rows of them)
+  void *n2, *dy;      // [rows][d] act
+  void *dGU, *Hp;     // [rows][2 d_ff], [rows][d_ff] act
+  float *Y, *gpart;   // [rows][d]; [rows][moe_grad_gate_parts]
+  float *gate;        // [rows]
+  int32_t *row_of;    // [N k]
+  float *part;        // [moe_grad_part_rows][d]
+};
+hipError_t launch_moe_backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, hipStream_t st);
+
+// grad.hip: norm and clipping over a list of tensors
+struct GradRec {  // a piece of a tensor
+  const void *src;
+  void *dst;
+  int32_t n, dtype;
+};
+constexpr int GRAD_BATCH = 64;         // descriptors a launch carries
+constexpr int GRAD_MAX_BLOCKS = 2048;  // partial values of a norm
+struct GradDesc {
+  const void *src;
+  void *dst;
+  int64_t numel;
+  int32_t dtype;
+};
+struct GradBatch {
+  GradDesc t[GRAD_BATCH];
+  int64_t first[GRAD_BATCH + 1];  // first piece of each tensor
+};
+int64_t grad_pieces(const triroute_grad_tensor &t);
+// the records of n <= GRAD_BATCH tensors, of at most `most` pieces each
+hipError_t launch_grad_list(const GradBatch &b, int n, int64_t most, GradRec *rec, hipStream_t st);
+// part: GRAD_MAX_BLOCKS doubles; mx: the largest magnitude instead of the root of squares
+hipError_t launch_grad_norm(const GradRec *rec, int64_t pieces, bool mx, double *part, double *norm,
+                            hipStream_t st);
+hipError_t launch_grad_scale(const GradRec *rec, int64_t pieces, const double *norm, double max_norm,
+                             hipStream_t st);
+hipError_t launch_grad_clip(const GradRec *rec, int64_t pieces, bool mx, double max_norm, double *part,
+                            double *norm, hipStream_t st);
 }  // namespace tr

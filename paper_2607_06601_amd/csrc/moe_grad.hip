@@ -1,0 +1,746 @@
+// Backward pass of the experts' gated feed-forward block (paper Sec. 3.2 (B),
+// second half of the Sec. 3.1 block).  Per assignment of a token to expert e
+// with gate p (n the normalised row, dx the gradient of x_out):
+//   G = Wg n, U = Wu n, q = Wd^T dx, s = 1 / (1 + exp(-G))
+//   g_gate = <q, s G U>;  dU = p q s G;  dG = p q U s (1 + G (1 - s))
+//   dWd += dx (p s G U)^T, dWg += dG n^T, dWu += dU n^T
+//   dn += Wg^T dG + Wu^T dU
+// and through the norm to xt and g2.  Three grouped products:
+//   hidden  [G; U; q] of a tile of units and rows, whose sum indices are all d_model,
+//           so that one epilogue holds the three in fp32: G, U and q never
+//           leave the registers, and g_gate is summed from values that were not rounded
+//   input   dn = [dG dU] [Wg; Wu]
+//   weight  dWg, dWu, dWd: sums over the rows of an expert
+// Rows lie by expert, each expert's padded to a multiple of 64 rows with zeros: a
+// padded row adds nothing to the weight gradients, so their K steps are whole.
+// Operands whose sum index is not their contiguous one (Wd in hidden, Wg and
+// Wu in input, both sides of weight) are staged as they lie, K rows of
+// columns, and read as fragments by the transposing LDS load
+// (ds_read_b64_tr_b16), so no transposed copy is made.
+#include "gemm_tile.hpp"
+#include "kernels.hpp"
+
+namespace tr {
+
+// ------------------------------------------------------------------ row maps
+// Lane e - 1 of every wave holds expert e: rows, padded rows, and the sums before it.
+struct PadScan {
+  int c, pc;         // rows, padded rows
+  int list, pad;     // first list entry, first padded row
+  int total;         // all padded rows
+};
+__device__ __forceinline__ PadScan pad_scan(const int32_t *cnt, int E) {
+  const int lane = threadIdx.x & 63;
+  PadScan g;
+  g.c = lane < E ? cnt[lane + 1] : 0;
+  g.pc = (g.c + MOE_PAD - 1) / MOE_PAD * MOE_PAD;
+  int a = g.c, b = g.pc;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int x = __shfl_up(a, d, 64), y = __shfl_up(b, d, 64);
+    if (lane >= d) {
+      a += x;
+      b += y;
+    }
+  }
+  g.list = a - g.c;
+  g.pad = b - g.pc;
+  g.total = __shfl(b, 63, 64);
+  return g;
+}
+
+// Row tile t of BN padded rows: its expert, first padded row and rows (a multiple of 64).
+struct RowTile {
+  int e, p0, rows;
+};
+template <int BN>
+__device__ __forceinline__ bool row_tile(const PadScan &g, int t, RowTile &r, int &total) {
+  const int lane = threadIdx.x & 63;
+  const int nt = (g.pc + BN - 1) / BN;
+  int incl = nt;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int x = __shfl_up(incl, d, 64);
+    if (lane >= d) incl += x;
+  }
+  total = __shfl(incl, 63, 64);
+  const uint64_t m = __ballot(incl > t);
+  if (!m) return false;
+  const int l = __ffsll((unsigned long long)m) - 1;
+  const int i = t - (__shfl(incl, l, 64) - __shfl(nt, l, 64));
+  r.e = __builtin_amdgcn_readfirstlane(l + 1);
+  r.p0 = __builtin_amdgcn_readfirstlane(__shfl(g.pad, l, 64) + i * BN);
+  r.rows = __builtin_amdgcn_readfirstlane(min(BN, __shfl(g.pc, l, 64) - i * BN));
+  return true;
+}
+
+// ------------------------------------------------------------------ rows
+// One wave per padded row: the normalised row (in fp64, rounded once, the
+// forward's arithmetic and so its bits) and the row of dx, its gate, and where its
+// assignment lies; zeros for the padding.
+template <typename T>
+__global__ __launch_bounds__(256) void moe_grad_rows_kernel(
+    const T *__restrict__ x, const T *__restrict__ dx, const T *__restrict__ g,
+    const float *__restrict__ egate, const int32_t *__restrict__ cnt,
+    const int32_t *__restrict__ rows, int E, int k, int d, float eps, T *__restrict__ n2,
+    T *__restrict__ dy, float *__restrict__ gate, int32_t *__restrict__ row_of) {
+  const int pos = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+  const int lane = threadIdx.x & 63;
+  const PadScan ps = pad_scan(cnt, E);
+  if (pos >= ps.total) return;
+  const uint64_t m = __ballot(ps.pad + ps.pc > pos);
+  const int l = __ffsll((unsigned long long)m) - 1;
+  const int i = pos - __shfl(ps.pad, l, 64);
+  T *no = n2 + int64_t(pos) * d, *yo = dy + int64_t(pos) * d;
+  if (i >= __shfl(ps.c, l, 64)) {
+    const float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int c = lane * 8; c < d; c += 512) {
+      store8(no + c, z);
+      store8(yo + c, z);
+    }
+    if (lane == 0) gate[pos] = 0.f;
+    return;
+  }
+  const int a = __builtin_amdgcn_readfirstlane(rows[__shfl(ps.list, l, 64) + i]);
+  const T *xr = x + int64_t(a / k) * d, *yr = dx + int64_t(a / k) * d;
+  double ss = 0.0;
+  for (int c = lane * 8; c < d; c += 512) {
+    float w[8];
+    load8(xr + c, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ss = fma(double(w[j]), double(w[j]), ss);
+  }
+  ss = wave_sum(ss);
+  const double r = 1.0 / sqrt(ss / double(d) + double(eps));
+  for (int c = lane * 8; c < d; c += 512) {
+    float w[8], gv[8], y[8];
+    double o[8];
+    load8(xr + c, w);
+    load8(g + c, gv);
+    load8(yr + c, y);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = (double(w[j]) * r) * double(gv[j]);
+    store8(no + c, o);
+    store8(yo + c, y);
+  }
+  if (lane == 0) {
+    gate[pos] = egate[a];
+    row_of[a] = pos;
+  }
+}
+
+// ------------------------------------------------------------------ bf16 tile
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+
+// Where a stage keeps the 32-byte column block b of K row k of a transposed
+// operand of R columns: the 4 K rows that 16 lanes read at once, and those of the next
+// lane group, lie in different banks.
+template <int R>
+__device__ __forceinline__ int tswz(int k, int b) {
+  if constexpr (R == 64)
+    return b ^ (((k >> 1) & 1) | (((k >> 3) & 1) << 1));  // two K rows a bank span
+  else
+    return b ^ ((k & 3) | (((k >> 3) & 1) << 2));
+}
+
+// acc += A B^T over nk steps of 64, A of MR and B of NR rows, WM x WN waves, S
+// stages in LDS.  AT / BT: the operand lies as K rows of MR / NR columns.  Sources are
+// given as functions (row, 16-byte chunk of its K step) or, transposed, (K row of
+// the step, 16-byte chunk of its columns) -> address at step 0, and the bytes
+// from one step to the next.  SPLIT 2: a wave's rows are taken in halves from
+// the two halves of A (the units' gates and ups).
+template <int MR, int NR, bool AT, bool BT, int SPLIT, int WM, int WN, int S>
+struct TileCore {
+  static constexpr int NW = WM * WN, MI = MR / WM / 16, NI = NR / WN / 16;
+  static constexpr int ABYTES = MR * 128, STAGE = (MR + NR) * 128, IPW = STAGE / 1024 / NW;
+  static_assert(STAGE % (1024 * NW) == 0, "whole transfers");
+
+  template <int R, bool TR>
+  __device__ static __forceinline__ bf16x8_t frag(const uint8_t *base, int row0, int ks, int lane) {
+    if constexpr (!TR) {
+      const int r = row0 + (lane & 15), ch = ks * 4 + (lane >> 4);
+      return *(const bf16x8_t *)(base + r * 128 + (swz<8>(r, ch) << 4));
+    } else {
+      typedef __attribute__((address_space(3))) s16x4_t *P;
+      s16x4_t h[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int k = 32 * ks + 8 * (lane >> 4) + 4 * x + ((lane & 15) >> 2);
+        h[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (P)(base + k * (2 * R) + tswz<R>(k, row0 >> 4) * 32 + (lane & 3) * 8));
+      }
+      typedef short s16x8_t __attribute__((ext_vector_type(8)));
+      const s16x8_t v = __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
+      return __builtin_bit_cast(bf16x8_t, v);
+    }
+  }
+
+  template <class FA, class FB>
+  __device__ static __forceinline__ void run(uint8_t *smem, FA &&fa, FB &&fb, int64_t astep,
+                                             int64_t bstep, int nk, f32x4_t (&acc)[MI][NI]) {
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / WN, wn = wave % WN;
+    const uint8_t *src[IPW];
+#pragma unroll
+    for (int j = 0; j < IPW; ++j) {
+      int p = (wave * IPW + j) * 64 + lane;  // the 16-byte piece of the stage
+      const bool isa = (wave * IPW + j) * 1024 < ABYTES;
+      if (isa) {
+        if constexpr (AT) {
+          const int k = p / (MR / 8), c = p % (MR / 8);
+          src[j] = fa(k, tswz<MR>(k, c >> 1) * 2 + (c & 1));
+        } else {
+          src[j] = fa(p / 8, swz<8>(p / 8, p % 8));
+        }
+      } else {
+        p -= ABYTES / 16;
+        if constexpr (BT) {
+          const int k = p / (NR / 8), c = p % (NR / 8);
+          src[j] = fb(k, tswz<NR>(k, c >> 1) * 2 + (c & 1));
+        } else {
+          src[j] = fb(p / 8, swz<8>(p / 8, p % 8));
+        }
+      }
+    }
+    const uint32_t sbase = lds_addr(smem) + wave * IPW * 1024;
+    auto issue = [&](int kt, int stage) {
+#pragma unroll
+      for (int j = 0; j < IPW; ++j) {
+        const bool isa = (wave * IPW + j) * 1024 < ABYTES;
+        dma16(src[j] + kt * (isa ? astep : bstep), sbase + stage * STAGE + j * 1024);
+      }
+    };
+#pragma unroll
+    for (int s0 = 0; s0 < S - 1; ++s0)
+      if (s0 < nk) issue(s0, s0);
+    for (int kt = 0; kt < nk; ++kt) {
+      wait_stages<IPW, S>(min(S - 2, nk - 1 - kt));
+      __syncthreads();  // every wave's part of stage kt is in; stage kt - 1 is free
+      if (kt + S - 1 < nk) issue(kt + S - 1, (kt + S - 1) % S);
+      const uint8_t *As = smem + (kt % S) * STAGE, *Bs = As + ABYTES;
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        bf16x8_t b[NI];
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni) b[ni] = frag<NR, BT>(Bs, wn * (NR / WN) + ni * 16, ks, lane);
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+          constexpr int H = MI / SPLIT;  // 16-row blocks of a wave in each part of A
+          const int row0 = (mi / H) * (MR / SPLIT) + wm * (MR / SPLIT / WM) + (mi % H) * 16;
+          const bf16x8_t a = frag<MR, AT>(As, row0, ks, lane);
+#pragma unroll
+          for (int ni = 0; ni < NI; ++ni)
+            acc[mi][ni] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[ni], acc[mi][ni], 0, 0, 0);
+        }
+      }
+    }
+    __syncthreads();  // every wave is done with the stages
+  }
+};
+
+template <int MI, int NI>
+__device__ __forceinline__ void zero_acc(f32x4_t (&acc)[MI][NI]) {
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+}
+
+struct MoeGradArgs {
+  const void *Wg, *Wu, *Wd;
+  const void *n2, *dy;  // [rows][d]
+  void *dGU, *Hp;       // [rows][2 d_ff]: dG, then dU; [rows][d_ff]: p s G U (NULL: not wanted)
+  const float *gate;    // [rows]
+  float *Y, *gpart;     // [rows][d]; [rows][GP]
+  void *dWg, *dWu, *dWd;
+  const int32_t *cnt;
+  int E, d, f, GP;
+};
+
+// Gradients of the hidden row's two factors and its gate's share, from fp32
+// G, U, q: h = s G U unscaled.
+struct Hidden {
+  float dg, du, hp, gq;
+};
+template <bool FAST>
+__device__ __forceinline__ Hidden hidden_grad(float G, float U, float q, float p) {
+  const float s = FAST ? __builtin_amdgcn_rcpf(1.0f + __expf(-G)) : 1.0f / (1.0f + expf(-G));
+  const float a = G * s, h = a * U, pq = p * q;
+  Hidden r;
+  r.du = pq * a;
+  r.dg = pq * U * (s * (1.0f + (G - a)));
+  r.hp = p * h;
+  r.gq = q * h;
+  return r;
+}
+
+// ------------------------------------------------------------------ hidden
+constexpr int HID_F = 64, HID_R = 128;  // units and rows of a tile
+template <int>
+__global__ __launch_bounds__(256) void moe_grad_hidden_kernel(MoeGradArgs a, int nf) {
+  using C1 = TileCore<2 * HID_F, HID_R, false, false, 2, 2, 2, 2>;
+  using C2 = TileCore<HID_F, HID_R, true, false, 1, 2, 2, 2>;
+  constexpr int MI = C2::MI, NI = C2::NI;
+  __shared__ __align__(1024) uint8_t smem[2 * C1::STAGE];
+  const PadScan ps = pad_scan(a.cnt, a.E);
+  RowTile t;
+  int nt;
+  row_tile<HID_R>(ps, 0, t, nt);
+  const int total = nt * nf;
+  if (int(blockIdx.x) >= total) return;
+  const int L = xcd_tile(blockIdx.x, total);
+  row_tile<HID_R>(ps, L / nf, t, nt);
+  const int f0 = (L % nf) * HID_F;
+  const int d = a.d, f = a.f;
+  const bf16 *Wg = (const bf16 *)a.Wg + (int64_t(t.e - 1) * f + f0) * d;
+  const bf16 *Wu = (const bf16 *)a.Wu + (int64_t(t.e - 1) * f + f0) * d;
+  const bf16 *Wd = (const bf16 *)a.Wd + int64_t(t.e - 1) * d * f + f0;
+  const bf16 *n2 = (const bf16 *)a.n2 + int64_t(t.p0) * d, *dy = (const bf16 *)a.dy + int64_t(t.p0) * d;
+  f32x4_t gu[2 * MI][NI], q[MI][NI];
+  zero_acc(gu);
+  zero_acc(q);
+  C1::run(
+      smem,
+      [&](int r, int c) {
+        return (const uint8_t *)((r < HID_F ? Wg : Wu) + int64_t(r & (HID_F - 1)) * d) + c * 16;
+      },
+      [&](int r, int c) { return (const uint8_t *)(n2 + int64_t(r < t.rows ? r : 0) * d) + c * 16; },
+      128, 128, d / 64, gu);
+  C2::run(
+      smem, [&](int k, int c) { return (const uint8_t *)(Wd + int64_t(k) * f) + c * 16; },
+      [&](int r, int c) { return (const uint8_t *)(dy + int64_t(r < t.rows ? r : 0) * d) + c * 16; },
+      int64_t(128) * f, 128, d / 64, q);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
+#pragma unroll
+  for (int ni = 0; ni < NI; ++ni) {
+    const int r = wn * (HID_R / 2) + ni * 16 + (lane & 15);
+    const int64_t pos = t.p0 + r;
+    const bool in = r < t.rows;
+    const float p = in ? a.gate[pos] : 0.f;
+    float gs = 0.f;
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+      const int u = f0 + wm * (HID_F / 2) + mi * 16 + 4 * (lane >> 4);
+      Hidden h[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        h[i] = hidden_grad<true>(gu[mi][ni][i], gu[MI + mi][ni][i], q[mi][ni][i], p);
+        gs += h[i].gq;
+      }
+      if (in) {
+        bf16 *o = (bf16 *)a.dGU + pos * (2 * f) + u;
+        *(uint2 *)o = make_uint2(pk_bf16(h[0].dg, h[1].dg), pk_bf16(h[2].dg, h[3].dg));
+        *(uint2 *)(o + f) = make_uint2(pk_bf16(h[0].du, h[1].du), pk_bf16(h[2].du, h[3].du));
+        if (a.Hp)
+          *(uint2 *)((bf16 *)a.Hp + pos * f + u) =
+              make_uint2(pk_bf16(h[0].hp, h[1].hp), pk_bf16(h[2].hp, h[3].hp));
+      }
+    }
+    gs += __shfl_xor(gs, 16, 64);
+    gs += __shfl_xor(gs, 32, 64);
+    if (in && lane < 16) a.gpart[pos * a.GP + (f0 / HID_F) * 2 + wm] = gs;
+  }
+}
+
+// ------------------------------------------------------------------ input
+constexpr int INP_M = 128, INP_R = 128;
+template <int>
+__global__ __launch_bounds__(256) void moe_grad_input_kernel(MoeGradArgs a, int nd) {
+  using C = TileCore<INP_M, INP_R, true, false, 1, 2, 2, 2>;
+  __shared__ __align__(1024) uint8_t smem[2 * C::STAGE];
+  const PadScan ps = pad_scan(a.cnt, a.E);
+  RowTile t;
+  int nt;
+  row_tile<INP_R>(ps, 0, t, nt);
+  const int total = nt * nd;
+  if (int(blockIdx.x) >= total) return;
+  const int L = xcd_tile(blockIdx.x, total);
+  row_tile<INP_R>(ps, L / nd, t, nt);
+  const int m0 = (L % nd) * INP_M, d = a.d, f = a.f;
+  f32x4_t acc[C::MI][C::NI];
+  zero_acc(acc);
+#pragma unroll 1
+  for (int half = 0; half < 2; ++half) {
+    const bf16 *W = (const bf16 *)(half ? a.Wu : a.Wg) + int64_t(t.e - 1) * f * d + m0;
+    const bf16 *g = (const bf16 *)a.dGU + int64_t(t.p0) * (2 * f) + half * f;
+    C::run(
+        smem,
+        [&](int k, int c) {
+          return (const uint8_t *)(W + int64_t(k) * d) + (m0 + c * 8 < d ? c * 16 : 0);
+        },
+        [&](int r, int c) {
+          return (const uint8_t *)(g + int64_t(r < t.rows ? r : 0) * (2 * f)) + c * 16;
+        },
+        int64_t(128) * d, 128, f / 64, acc);
+  }
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
+#pragma unroll
+  for (int ni = 0; ni < C::NI; ++ni) {
+    const int r = wn * (INP_R / 2) + ni * 16 + (lane & 15);
+    if (r >= t.rows) continue;
+#pragma unroll
+    for (int mi = 0; mi < C::MI; ++mi) {
+      const int m = m0 + wm * (INP_M / 2) + mi * 16 + 4 * (lane >> 4);
+      if (m < d) *(f32x4_t *)(a.Y + int64_t(t.p0 + r) * d + m) = acc[mi][ni];
+    }
+  }
+}
+
+// ------------------------------------------------------------------ weight
+constexpr int WGT_M = 128, WGT_N = 128;
+template <int>
+__global__ __launch_bounds__(256) void moe_grad_weight_kernel(MoeGradArgs a) {
+  using C = TileCore<WGT_M, WGT_N, true, true, 1, 2, 2, 2>;
+  __shared__ __align__(1024) uint8_t smem[2 * C::STAGE];
+  const int d = a.d, f = a.f;
+  const int md = (d + WGT_M - 1) / WGT_M, mf = (f + WGT_M - 1) / WGT_M;
+  const int t1 = md * ((2 * f + WGT_N - 1) / WGT_N), t2 = mf * ((d + WGT_N - 1) / WGT_N);
+  int L = xcd_tile(blockIdx.x, gridDim.x);
+  const int e = L / (t1 + t2) + 1;
+  L -= (e - 1) * (t1 + t2);
+  const PadScan ps = pad_scan(a.cnt, a.E);
+  const int p0 = __builtin_amdgcn_readfirstlane(__shfl(ps.pad, e - 1, 64));
+  const int rows = __builtin_amdgcn_readfirstlane(__shfl(ps.pc, e - 1, 64));
+  const bool down = L >= t1;  // dWd[d][f] = dy^T Hp; else [dWg; dWu] = dGU^T n2
+  if (down) L -= t1;
+  const int mt = down ? mf : md, M = down ? f : d, N = down ? d : 2 * f;
+  const int m0 = (L % mt) * WGT_M, n0 = (L / mt) * WGT_N;
+  const bf16 *A = (const bf16 *)(down ? a.Hp : a.n2) + int64_t(p0) * M + m0;
+  const bf16 *B = (const bf16 *)(down ? a.dy : a.dGU) + int64_t(p0) * N + n0;
+  f32x4_t acc[C::MI][C::NI];
+  zero_acc(acc);
+  C::run(
+      smem,
+      [&](int k, int c) { return (const uint8_t *)(A + int64_t(k) * M) + (m0 + c * 8 < M ? c * 16 : 0); },
+      [&](int k, int c) { return (const uint8_t *)(B + int64_t(k) * N) + (n0 + c * 8 < N ? c * 16 : 0); },
+      int64_t(128) * M, int64_t(128) * N, rows / 64, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
+#pragma unroll
+  for (int ni = 0; ni < C::NI; ++ni) {
+    int n = n0 + wn * (WGT_N / 2) + ni * 16 + (lane & 15);
+    if (n >= N) continue;
+    bf16 *o = (bf16 *)(down ? a.dWd : a.dWg);
+    if (!down && n >= f) {
+      o = (bf16 *)a.dWu;
+      n -= f;
+    }
+    o += int64_t(e - 1) * d * f + int64_t(n) * M;
+#pragma unroll
+    for (int mi = 0; mi < C::MI; ++mi) {
+      const int m = m0 + wm * (WGT_M / 2) + mi * 16 + 4 * (lane >> 4);
+      if (m < M)
+        *(uint2 *)(o + m) = make_uint2(pk_bf16(acc[mi][ni][0], acc[mi][ni][1]),
+                                       pk_bf16(acc[mi][ni][2], acc[mi][ni][3]));
+    }
+  }
+}
+
+// ------------------------------------------------------------------ fp32 tile
+// acc += A B^T over K (a multiple of 16), 64 x 64 on 2 x 2 waves, fp32 MFMA
+// (16x16x4).  Stages hold [k][row], rows of 80 floats: the 4 x 16 floats of a fragment
+// lie in different banks.  Sources: (row, k) -> address of 4 consecutive k, or,
+// transposed, (k, row) -> address of 4 consecutive rows.
+constexpr int F32_T = 64, F32_K = 16, F32_LD = 80;
+struct F32Smem {
+  float a[2][F32_K][F32_LD], b[2][F32_K][F32_LD];
+};
+template <bool AT, bool BT, class FA, class FB>
+__device__ __forceinline__ void tile_f32(F32Smem &sm, FA &&fa, FB &&fb, int K, f32x4_t (&acc)[2][2]) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / 2, wn = wave % 2;
+  const int tk = tid >> 4, tr = (tid & 15) * 4;  // transposed: K row, first of 4 rows
+  const int nr = tid >> 2, nk = (tid & 3) * 4;   // else: row, first of 4 k
+  f32x4_t ra, rb;
+  auto fetch = [&](int k0) {
+    if constexpr (AT) ra = *(const f32x4_t *)fa(k0 + tk, tr);
+    else ra = *(const f32x4_t *)fa(nr, k0 + nk);
+    if constexpr (BT) rb = *(const f32x4_t *)fb(k0 + tk, tr);
+    else rb = *(const f32x4_t *)fb(nr, k0 + nk);
+  };
+  auto put = [&](int s) {
+    if constexpr (AT) *(f32x4_t *)&sm.a[s][tk][tr] = ra;
+    else
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sm.a[s][nk + i][nr] = ra[i];
+    if constexpr (BT) *(f32x4_t *)&sm.b[s][tk][tr] = rb;
+    else
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sm.b[s][nk + i][nr] = rb[i];
+  };
+  if (K <= 0) return;
+  fetch(0);
+  put(0);
+  __syncthreads();
+  int s = 0;
+  for (int k0 = 0; k0 < K; k0 += F32_K) {
+    const bool more = k0 + F32_K < K;
+    if (more) fetch(k0 + F32_K);
+#pragma unroll
+    for (int kk = 0; kk < F32_K; kk += 4) {
+      float x[2], y[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        x[i] = sm.a[s][kk + (lane >> 4)][wm * 32 + 16 * i + (lane & 15)];
+        y[i] = sm.b[s][kk + (lane >> 4)][wn * 32 + 16 * i + (lane & 15)];
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[j], acc[i][j], 0, 0, 0);
+    }
+    if (more) put(s ^ 1);
+    __syncthreads();
+    s ^= 1;
+  }
+}
+
+__global__ __launch_bounds__(256) void moe_grad_hidden_f32_kernel(MoeGradArgs a, int nf) {
+  __shared__ __align__(16) F32Smem sm;
+  const PadScan ps = pad_scan(a.cnt, a.E);
+  RowTile t;
+  int nt;
+  if (!row_tile<F32_T>(ps, blockIdx.x / nf, t, nt)) return;
+  const int f0 = (blockIdx.x % nf) * F32_T, d = a.d, f = a.f;
+  const float *Wg = (const float *)a.Wg + (int64_t(t.e - 1) * f + f0) * d;
+  const float *Wu = (const float *)a.Wu + (int64_t(t.e - 1) * f + f0) * d;
+  const float *Wd = (const float *)a.Wd + int64_t(t.e - 1) * d * f + f0;
+  const float *n2 = (const float *)a.n2 + int64_t(t.p0) * d, *dy = (const float *)a.dy + int64_t(t.p0) * d;
+  f32x4_t G[2][2], U[2][2], q[2][2];
+  zero_acc(G);
+  zero_acc(U);
+  zero_acc(q);
+  tile_f32<false, false>(sm, [&](int r, int k) { return Wg + int64_t(r) * d + k; },
+                         [&](int r, int k) { return n2 + int64_t(r) * d + k; }, d, G);
+  tile_f32<false, false>(sm, [&](int r, int k) { return Wu + int64_t(r) * d + k; },
+                         [&](int r, int k) { return n2 + int64_t(r) * d + k; }, d, U);
+  tile_f32<true, false>(sm, [&](int k, int r) { return Wd + int64_t(k) * f + r; },
+                        [&](int r, int k) { return dy + int64_t(r) * d + k; }, d, q);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
+#pragma unroll
+  for (int ni = 0; ni < 2; ++ni) {
+    const int64_t pos = t.p0 + wn * 32 + ni * 16 + (lane & 15);  // tiles are whole: 64 rows
+    const float p = a.gate[pos];
+    float gs = 0.f;
+#pragma unroll
+    for (int mi = 0; mi < 2; ++mi) {
+      const int u = f0 + wm * 32 + mi * 16 + 4 * (lane >> 4);
+      f32x4_t dg, du, hp;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const Hidden h = hidden_grad<false>(G[mi][ni][i], U[mi][ni][i], q[mi][ni][i], p);
+        dg[i] = h.dg;
+        du[i] = h.du;
+        hp[i] = h.hp;
+        gs += h.gq;
+      }
+      float *o = (float *)a.dGU + pos * (2 * f) + u;
+      *(f32x4_t *)o = dg;
+      *(f32x4_t *)(o + f) = du;
+      if (a.Hp) *(f32x4_t *)((float *)a.Hp + pos * f + u) = hp;
+    }
+    gs += __shfl_xor(gs, 16, 64);
+    gs += __shfl_xor(gs, 32, 64);
+    if (lane < 16) a.gpart[pos * a.GP + (f0 / F32_T) * 2 + wm] = gs;
+  }
+}
+
+__global__ __launch_bounds__(256) void moe_grad_input_f32_kernel(MoeGradArgs a, int nd) {
+  __shared__ __align__(16) F32Smem sm;
+  const PadScan ps = pad_scan(a.cnt, a.E);
+  RowTile t;
+  int nt;
+  if (!row_tile<F32_T>(ps, blockIdx.x / nd, t, nt)) return;
+  const int m0 = (blockIdx.x % nd) * F32_T, d = a.d, f = a.f;
+  const float *g = (const float *)a.dGU + int64_t(t.p0) * (2 * f);
+  f32x4_t acc[2][2];
+  zero_acc(acc);
+#pragma unroll 1
+  for (int half = 0; half < 2; ++half) {
+    const float *W = (const float *)(half ? a.Wu : a.Wg) + int64_t(t.e - 1) * f * d + m0;
+    tile_f32<true, false>(sm, [&](int k, int r) { return W + int64_t(k) * d + r; },
+                          [&](int r, int k) { return g + int64_t(r) * (2 * f) + half * f + k; }, f, acc);
+  }
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
+#pragma unroll
+  for (int ni = 0; ni < 2; ++ni)
+#pragma unroll
+    for (int mi = 0; mi < 2; ++mi)
+      *(f32x4_t *)(a.Y + int64_t(t.p0 + wn * 32 + ni * 16 + (lane & 15)) * d + m0 + wm * 32 + mi * 16 +
+                   4 * (lane >> 4)) = acc[mi][ni];
+}
+
+__global__ __launch_bounds__(256) void moe_grad_weight_f32_kernel(MoeGradArgs a) {
+  __shared__ __align__(16) F32Smem sm;
+  const int d = a.d, f = a.f, md = d / F32_T, mf = f / F32_T, t1 = md * 2 * mf, t2 = mf * md;
+  int L = blockIdx.x;
+  const int e = L / (t1 + t2) + 1;
+  L -= (e - 1) * (t1 + t2);
+  const PadScan ps = pad_scan(a.cnt, a.E);
+  const int p0 = __builtin_amdgcn_readfirstlane(__shfl(ps.pad, e - 1, 64));
+  const int rows = __builtin_amdgcn_readfirstlane(__shfl(ps.pc, e - 1, 64));
+  const bool down = L >= t1;
+  if (down) L -= t1;
+  const int mt = down ? mf : md, M = down ? f : d, N = down ? d : 2 * f;
+  const int m0 = (L % mt) * F32_T, n0 = (L / mt) * F32_T;
+  const float *A = (const float *)(down ? a.Hp : a.n2) + int64_t(p0) * M + m0;
+  const float *B = (const float *)(down ? a.dy : a.dGU) + int64_t(p0) * N + n0;
+  f32x4_t acc[2][2];
+  zero_acc(acc);
+  tile_f32<true, true>(sm, [&](int k, int r) { return A + int64_t(k) * M + r; },
+                       [&](int k, int r) { return B + int64_t(k) * N + r; }, rows, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
+  float *o = (float *)(down ? a.dWd : n0 < f ? a.dWg : a.dWu) + int64_t(e - 1) * d * f;
+  const int nb = !down && n0 >= f ? n0 - f : n0;
+#pragma unroll
+  for (int ni = 0; ni < 2; ++ni)
+#pragma unroll
+    for (int mi = 0; mi < 2; ++mi)
+      *(f32x4_t *)(o + int64_t(nb + wn * 32 + ni * 16 + (lane & 15)) * M + m0 + wm * 32 + mi * 16 +
+                   4 * (lane >> 4)) = acc[mi][ni];
+}
+
+// ------------------------------------------------------------------ tokens
+// dn of a token = the sum of its slots' rows of Y; through the norm to dxt; the
+// block's share of dg2 (fp32 over the tokens of a block, joined in fp64);
+// g_gate from the hidden tiles' partial sums.  One wave per token at a time.
+constexpr int TOK_BLOCKS = 512;
+template <typename T>
+__global__ __launch_bounds__(256) void moe_grad_token_kernel(
+    const T *__restrict__ x, const T *dx, const T *__restrict__ g, const float *__restrict__ Y,
+    const int32_t *__restrict__ eidx, const int32_t *__restrict__ row_of,
+    const float *__restrict__ gpart, int GP, int N, int k, int d, float eps, T *dxt,
+    float *__restrict__ g_gate, float *__restrict__ part) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  float *pr = part ? part + (int64_t(blockIdx.x) * 4 + wave) * d : nullptr;
+  bool first = true;
+  for (int i = blockIdx.x * 4 + wave; i < N; i += gridDim.x * 4) {
+    const T *xr = x + int64_t(i) * d;
+    const int32_t *ei = eidx + int64_t(i) * k, *ro = row_of + int64_t(i) * k;
+    auto dn8 = [&](int c, float *dn) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) dn[j] = 0.f;
+      for (int s = 0; s < k; ++s) {
+        if (ei[s] == 0) continue;
+        float y[8];
+        load8(Y + int64_t(ro[s]) * d + c, y);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dn[j] += y[j];
+      }
+    };
+    double ss = 0.0, dot = 0.0;
+    for (int c = lane * 8; c < d; c += 512) {
+      float w[8], gv[8], dn[8];
+      load8(xr + c, w);
+      load8(g + c, gv);
+      dn8(c, dn);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        ss = fma(double(w[j]), double(w[j]), ss);
+        dot = fma(double(dn[j] * gv[j]), double(w[j]), dot);
+      }
+    }
+    ss = wave_sum(ss);
+    dot = wave_sum(dot);
+    const double r = 1.0 / sqrt(ss / double(d) + double(eps));
+    const float rf = float(r), cf = float(r * r * r * dot / double(d));
+    for (int c = lane * 8; c < d; c += 512) {
+      float w[8], gv[8], dn[8], u[8], o[8];
+      load8(xr + c, w);
+      load8(g + c, gv);
+      load8(dx + int64_t(i) * d + c, u);
+      dn8(c, dn);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o[j] = u[j] + fmaf(rf, dn[j] * gv[j], -cf * w[j]);
+      store8(dxt + int64_t(i) * d + c, o);
+      if (pr) {
+        float q[8];
+        if (first) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) q[j] = 0.f;
+        } else {
+          load8(pr + c, q);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[j] = fmaf(dn[j] * rf, w[j], q[j]);
+        store8(pr + c, q);
+      }
+    }
+    first = false;
+    if (g_gate) {
+      for (int s = 0; s < k; ++s) {
+        float v = 0.f;
+        if (ei[s] != 0)
+          for (int j = lane; j < GP; j += 64) v += gpart[int64_t(ro[s]) * GP + j];
+        v = wave_sum(v);
+        if (lane == 0) g_gate[int64_t(i) * k + s] = v;
+      }
+    }
+  }
+  if (pr && first)
+    for (int c = lane; c < d; c += 64) pr[c] = 0.f;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void moe_grad_g2_kernel(const float *__restrict__ part, int rows, int d,
+                                                          T *__restrict__ dg2) {
+  __shared__ double red[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  double v = 0.0;
+  for (int r = wave; r < rows; r += 4) v += double(part[int64_t(r) * d + c]);
+  red[wave][lane] = v;
+  __syncthreads();
+  if (wave == 0)
+    Act<T>::st(dg2, c, float(((red[0][lane] + red[1][lane]) + red[2][lane]) + red[3][lane]));
+}
+
+// ------------------------------------------------------------------ launchers
+int moe_grad_gate_parts(const triroute_cfg &cfg) { return cfg.d_ff / 64 * 2; }
+int moe_grad_part_rows(int N) { return std::min((N + 3) / 4, TOK_BLOCKS) * 4; }
+
+template <typename T>
+static hipError_t backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, hipStream_t st) {
+  const int E = cfg.n_experts, k = cfg.top_k, d = cfg.d_model, f = cfg.d_ff, Nk = N * k;
+  const int64_t rows = moe_grad_rows(cfg, N);
+  MoeGradArgs a;
+  a.Wg = j.w.Wgate; a.Wu = j.w.Wup; a.Wd = j.w.Wdown;
+  a.n2 = j.n2; a.dy = j.dy; a.dGU = j.dGU;
+  a.Hp = j.out.dWgate ? j.Hp : nullptr;
+  a.gate = j.gate; a.Y = j.Y; a.gpart = j.gpart;
+  a.dWg = j.out.dWgate; a.dWu = j.out.dWup; a.dWd = j.out.dWdown;
+  a.cnt = j.cmp.exp_cnt;
+  a.E = E; a.d = d; a.f = f;
+  a.GP = moe_grad_gate_parts(cfg);
+  moe_grad_rows_kernel<T><<<dim3(unsigned((rows + 3) / 4)), 256, 0, st>>>(
+      (const T *)j.xt, (const T *)j.dx, (const T *)j.g2, j.egate, j.cmp.exp_cnt, j.cmp.exp_rows, E, k, d,
+      cfg.rms_eps, (T *)j.n2, (T *)j.dy, j.gate, j.row_of);
+  if constexpr (sizeof(T) == 2) {
+    const int nf = f / HID_F, nd = (d + INP_M - 1) / INP_M;
+    const int rt = Nk / HID_R + E;  // row tiles at most
+    moe_grad_hidden_kernel<0><<<unsigned(rt) * nf, 256, 0, st>>>(a, nf);
+    moe_grad_input_kernel<0><<<unsigned(rt) * nd, 256, 0, st>>>(a, nd);
+    if (a.Hp) {
+      const int t1 = (d + WGT_M - 1) / WGT_M * ((2 * f + WGT_N - 1) / WGT_N);
+      const int t2 = (f + WGT_M - 1) / WGT_M * ((d + WGT_N - 1) / WGT_N);
+      moe_grad_weight_kernel<0><<<unsigned(E) * (t1 + t2), 256, 0, st>>>(a);
+    }
+  } else {
+    const int nf = f / F32_T, nd = d / F32_T, rt = Nk / F32_T + E;
+    moe_grad_hidden_f32_kernel<<<unsigned(rt) * nf, 256, 0, st>>>(a, nf);
+    moe_grad_input_f32_kernel<<<unsigned(rt) * nd, 256, 0, st>>>(a, nd);
+    if (a.Hp) moe_grad_weight_f32_kernel<<<unsigned(E) * nd * nf * 3, 256, 0, st>>>(a);
+  }
+  const int prows = moe_grad_part_rows(N);
+  moe_grad_token_kernel<T><<<prows / 4, 256, 0, st>>>(
+      (const T *)j.xt, (const T *)j.dx, (const T *)j.g2, j.Y, j.eidx, j.row_of, j.gpart, a.GP, N, k, d,
+      cfg.rms_eps, (T *)j.out.dxt, j.out.g_gate, j.out.dg2 ? j.part : nullptr);
+  if (j.out.dg2)
+    moe_grad_g2_kernel<T><<<d / 64, 256, 0, st>>>(j.part, prows, d, (T *)j.out.dg2);
+  return hipGetLastError();
+}
+
+hipError_t launch_moe_backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, hipStream_t st) {
+  return cfg.act == TRIROUTE_BF16 ? backward<bf16>(cfg, N, j, st) : backward<float>(cfg, N, j, st);
+}
+
+}  // namespace tr

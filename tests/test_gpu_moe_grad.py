@@ -1,0 +1,243 @@
+"""Backward pass of the experts (triroute_moe_backward) against the fp64 oracle.
+
+Every element is held to the bound that ``oracle.moe_grad`` derives from the
+roundings of the operator: fp32 sums, operands rounded once to the
+activation type, one rounding of each output."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_06601_amd as tr
+from oracle.moe_grad import moe_backward
+from paper_2607_06601_amd.device import to_dev
+
+from _common import note, npy, torch_act
+from _moe_grad import lists, moe_case
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+OUTS = ("dxt", "dg2", "g_gate", "dWgate", "dWup", "dWdown")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    tr.lib()
+    yield
+    torch.cuda.synchronize()
+
+
+class Call:
+    """Device copies of a case and one call's buffers (filled with NaN first)."""
+
+    def __init__(self, L, xt, dx, eidx, egate, act, want=OUTS, in_place=False):
+        E, f, d = L["Wg"].shape
+        self.N, self.k, self.dt = len(xt), eidx.shape[1], torch_act(act)
+        self.cfg = tr.make_cfg(d, 4, 1, 64, 32, E, self.k, f, 32, act)
+        t = {n: to_dev(L[n], self.dt) for n in ("g2", "Wg", "Wu", "Wd")}
+        t.update(xt=to_dev(xt, self.dt), dx=to_dev(dx, self.dt), eidx=to_dev(eidx, torch.int32),
+                 egate=to_dev(egate, torch.float32))
+        for n, a in zip(("cnt", "off", "rows"), lists(eidx, E)):
+            t[n] = to_dev(a if len(a) else np.zeros(1, np.int32), torch.int32)
+        self.t = t
+        shape = dict(dxt=(self.N, d), dg2=(d,), g_gate=(self.N, self.k), dWgate=(E, f, d),
+                     dWup=(E, f, d), dWdown=(E, d, f))
+        self.out = {n: torch.full(shape[n], float("nan"), device=DEV,
+                                  dtype=torch.float32 if n == "g_gate" else self.dt) for n in want}
+        if in_place:
+            self.out["dxt"] = t["dx"]
+        self.ws = tr.workspace(self.cfg, tr.OP_MOE_BACKWARD, self.N, 1)
+        self.ws.fill_(0xFF)  # NaN in either type
+
+    def __call__(self, stream=None):
+        t = self.t
+        tr.moe_backward(self.cfg, self.N, t["xt"], tr.DenseW(g2=t["g2"].data_ptr()),
+                        tr.MoeW(*(t[n].data_ptr() for n in ("Wg", "Wu", "Wd"))), t["eidx"],
+                        t["egate"], tr.Compaction(exp_cnt=t["cnt"].data_ptr(),
+                                                  exp_off=t["off"].data_ptr(),
+                                                  exp_rows=t["rows"].data_ptr()),
+                        t["dx"], tr.MoeGradOut(**{n: v.data_ptr() for n, v in self.out.items()}),
+                        self.ws, stream=stream)
+        return self
+
+    def result(self):
+        torch.cuda.synchronize()
+        return {n: npy(v).astype(np.float64) for n, v in self.out.items()}
+
+
+def check(got, ref, err, where=""):
+    ratios = {}
+    for n in got:
+        assert np.isfinite(got[n]).all(), (where, n)
+        ratios[n] = float((np.abs(got[n] - ref[n]) / err[n]).max())
+        note(f"{where} {n}", ratios[n])
+    assert max(ratios.values()) <= 1.0, (where, ratios)
+
+
+# (act, N, d, d_ff, E, k, choice): one token; sizes off every tile; rows around the
+# padding and the tiles; every option chosen; no expert chosen; d past the
+# widths that stay in registers; more experts than tokens
+CASES = [
+    ("bf16", 1, 64, 64, 1, 1, [0, 1]),
+    ("f32", 1, 64, 64, 1, 1, [0, 1]),
+    ("bf16", 1, 768, 2048, 8, 2, "random"),
+    ("bf16", 37, 192, 320, 5, 2, "random"),
+    ("f32", 37, 192, 320, 5, 2, "random"),
+    ("bf16", 514, 128, 64, 6, 1, [3, 63, 64, 65, 127, 192]),
+    ("f32", 322, 64, 128, 5, 1, [2, 63, 64, 65, 128]),
+    ("bf16", 771, 320, 448, 4, 1, [0, 129, 0, 257, 385]),
+    ("bf16", 33, 128, 128, 3, 4, "random"),
+    ("bf16", 40, 128, 192, 3, 1, "null"),
+    ("f32", 40, 128, 192, 3, 1, "null"),
+    ("bf16", 21, 2112, 128, 2, 2, "random"),
+    ("f32", 21, 2112, 64, 2, 2, "random"),
+    ("bf16", 5, 128, 64, 63, 3, "random"),
+    ("bf16", 1000, 64, 1088, 2, 2, "random"),
+    ("bf16", 2500, 128, 128, 3, 2, "random"),
+    ("f32", 2500, 64, 64, 3, 3, "random"),
+]
+
+
+@pytest.mark.parametrize("act,N,d,f,E,k,choice", CASES)
+def test_matches_oracle(act, N, d, f, E, k, choice):
+    print(f"moe backward {act} N={N} d={d} f={f} E={E} k={k}", flush=True)
+    case = moe_case(7, act, N, d, f, E, k, choice)
+    L, xt, dx, eidx, egate = case
+    ref, err = moe_backward(xt, L, eidx, egate, dx, act, bounds=True)
+    got = Call(*case, act)().result()
+    check(got, ref, err, f"{act} {N}x{d}x{f}")
+    assert (got["g_gate"][eidx == 0] == 0).all()
+    for e in range(1, E + 1):
+        if not (eidx == e).any():
+            for n in ("dWgate", "dWup", "dWdown"):
+                assert (got[n][e - 1] == 0).all(), (n, e)
+    if choice == "null":
+        np.testing.assert_array_equal(got["dxt"], np.asarray(dx, np.float64))
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+def test_frozen_experts_in_place_and_without_the_rest(act):
+    """dxt over dx_out, no weight gradients, no dg2, no g_gate: the same dxt."""
+    case = moe_case(8, act, 150, 128, 192, 4, 2)
+    full = Call(*case, act)().result()
+    part = Call(*case, act, want=("g_gate",), in_place=True)()
+    np.testing.assert_array_equal(part.result()["dxt"], full["dxt"])
+    np.testing.assert_array_equal(part.result()["g_gate"], full["g_gate"])
+    only = Call(*case, act, want=("dxt",))().result()
+    np.testing.assert_array_equal(only["dxt"], full["dxt"])
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+def test_null_slots_are_not_read(act):
+    """What lies in a null slot (a NaN gate, a huge one) reaches no output; a zero
+    gate on an expert does give that gate a gradient."""
+    case = L, xt, dx, eidx, egate = moe_case(9, act, 90, 128, 128, 3, 2)
+    clean = Call(*case, act)().result()
+    bad = egate.copy()
+    bad[eidx == 0] = np.nan
+    assert np.isnan(bad).any()
+    got = Call(L, xt, dx, eidx, bad, act)().result()
+    for n in OUTS:
+        np.testing.assert_array_equal(got[n], clean[n], err_msg=n)
+    zero = egate * 0
+    ref, err = moe_backward(xt, L, eidx, zero, dx, act, bounds=True)
+    got = Call(L, xt, dx, eidx, zero, act)().result()
+    check(got, ref, err, f"{act} zero gates")
+    assert (got["dWgate"] == 0).all() and (got["dxt"] == np.asarray(dx)).all()
+    assert np.abs(got["g_gate"][eidx != 0]).min() > 0
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+def test_saturated_gates(act):
+    """Pre-activations far outside the range of exp: SiLU and its derivative
+    go to their limits without a NaN."""
+    L, xt, dx, eidx, egate = moe_case(10, act, 64, 128, 128, 2, 1, [0, 40, 24])
+    L["Wg"] = L["Wg"] * np.float32(512)
+    ref, err = moe_backward(xt, L, eidx, egate, dx, act, bounds=True)
+    n = np.asarray(xt, np.float64)
+    assert np.abs(n @ L["Wg"][0].T.astype(np.float64)).max() > 700
+    check(Call(L, xt, dx, eidx, egate, act)().result(), ref, err, f"{act} saturated")
+
+
+@pytest.mark.parametrize("act,N", [("bf16", 300), ("f32", 100), ("bf16", 3)])
+def test_same_bits_every_time_on_any_stream_and_captured(act, N):
+    case = moe_case(11, act, N, 192, 192, 4, 2)
+    first = Call(*case, act)().result()
+    c = Call(*case, act)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    c(stream=s)
+    s.synchronize()
+    for n, v in c.result().items():
+        np.testing.assert_array_equal(v, first[n], err_msg=n)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c()
+    dx = c.t["dx"].clone()
+    for rep in range(3):
+        for v in c.out.values():
+            v.fill_(float("nan"))
+        c.ws.fill_(0xFF)
+        g.replay()
+        for n, v in c.result().items():
+            np.testing.assert_array_equal(v, first[n], err_msg=f"{n} replay {rep}")
+    # new data in the captured buffers
+    c.t["dx"].copy_(dx * 2)
+    g.replay()
+    twice = c.result()
+    for n in ("dWgate", "dWup", "dWdown", "g_gate", "dg2"):  # powers of two scale exactly
+        np.testing.assert_array_equal(twice[n], 2 * first[n], err_msg=n)
+
+
+def test_two_calls_at_once():
+    """Two streams, two workspaces: neither call sees the other."""
+    a, b = (moe_case(s, "bf16", 700, 256, 320, 4, 2) for s in (12, 13))
+    want = [Call(*x, "bf16")().result() for x in (a, b)]
+    calls, streams = [Call(*x, "bf16") for x in (a, b)], [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for c, s in zip(calls, streams):
+            c(stream=s)
+    for c, w in zip(calls, want):
+        for n, v in c.result().items():
+            np.testing.assert_array_equal(v, w[n], err_msg=n)
+
+
+@pytest.mark.parametrize("shape,N", [("160m_bf16_prefill", 3000), ("1p3b_bf16_prefill", 700)])
+def test_layer_shapes_against_fp32_products(shape, N):
+    """The layers' own widths, where the fp64 oracle on the CPU takes too long: fp64
+    products on the GPU in the oracle's order of steps, and its tolerance for
+    whole tensors: operand and output roundings of bf16 add in squares."""
+    import gen
+    m = gen.CONFIGS[shape]
+    case = L, xt, dx, eidx, egate = moe_case(14, "bf16", N, m["d"], m["d_ff"], 4, 2)
+    got = Call(*case, "bf16")()
+    torch.cuda.synchronize()
+    D = {n: got.t[n].double() for n in ("xt", "dx", "g2", "Wg", "Wu", "Wd")}
+    x = D["xt"]
+    r = 1.0 / torch.sqrt((x * x).mean(1, keepdim=True) + 1e-6)
+    n = (x * r * D["g2"]).float().bfloat16().double()
+    dn = torch.zeros_like(x)
+    ref = dict(g_gate=torch.zeros(N, 2, dtype=torch.float64, device=DEV))
+    for name, w in (("dWgate", "Wg"), ("dWup", "Wu"), ("dWdown", "Wd")):
+        ref[name] = torch.zeros_like(D[w])
+    for e in range(1, 5):
+        i, s = torch.nonzero(got.t["eidx"] == e, as_tuple=True)
+        p = got.t["egate"][i, s].double()[:, None]
+        G, U, q = n[i] @ D["Wg"][e - 1].T, n[i] @ D["Wu"][e - 1].T, D["dx"][i] @ D["Wd"][e - 1]
+        sg = torch.sigmoid(G)
+        dG, dU = p * q * U * sg * (1 + G * (1 - sg)), p * q * G * sg
+        ref["g_gate"][i, s] = (q * G * sg * U).sum(1)
+        ref["dWgate"][e - 1], ref["dWup"][e - 1] = dG.T @ n[i], dU.T @ n[i]
+        ref["dWdown"][e - 1] = D["dx"][i].T @ (p * G * sg * U)
+        dn.index_put_((i,), dG @ D["Wg"][e - 1] + dU @ D["Wu"][e - 1], accumulate=True)
+    gx = dn * D["g2"]
+    ref["dxt"] = D["dx"] + r * gx - r ** 3 * x * (gx * x).mean(1, keepdim=True)
+    ref["dg2"] = (dn * x * r).sum(0)
+    for name, want in ref.items():
+        # two roundings of at most 2^-8, each 2^-8 / sqrt(3) in the mean square or
+        # less; fp32 sums of up to 2 d_ff products for g_gate
+        tol = 2.0 ** -7.5 / 3 ** 0.5 if name != "g_gate" else (m["d"] + m["d_ff"]) ** 0.5 * 2.0 ** -24 * 8
+        off = float((got.out[name].double() - want).norm() / want.norm())
+        note(f"{shape} {name}", off / tol)
+        assert off <= tol, (name, off, tol)

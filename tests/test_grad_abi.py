@@ -1,0 +1,125 @@
+"""Host-side refusals of the training operators (no GPU): the expert backward
+pass and the gradient list, norm and clipping."""
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+import paper_2607_06601_amd as tr
+
+FAKE = 1 << 40
+
+
+def cfg160(**over):
+    c = tr.make_cfg(768, 12, 3, 64, 128, 8, 2, 2048, 64, "bf16")
+    for k, v in over.items():
+        setattr(c, k, v)
+    return c
+
+
+def backward(c=None, n=16, ws_bytes=1 << 44, xt=FAKE, dx=FAKE, eidx=FAKE, ws=FAKE, cmp=None, mw=None,
+             **out):
+    c = cfg160() if c is None else c
+    o = tr.MoeGradOut(**{**dict(dxt=FAKE, dWgate=FAKE, dWup=FAKE, dWdown=FAKE, dg2=FAKE, g_gate=FAKE),
+                         **out})
+    dw = tr.DenseW(g2=FAKE)
+    mw = tr.MoeW(FAKE, FAKE, FAKE) if mw is None else mw
+    cmp = tr.Compaction(exp_cnt=FAKE, exp_off=FAKE, exp_rows=FAKE) if cmp is None else cmp
+    return tr.lib().triroute_moe_backward(C.byref(c), n, xt, C.byref(dw), C.byref(mw), eidx, FAKE,
+                                          C.byref(cmp), dx, C.byref(o), ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("over,code,word", [
+    (dict(xt=None), -1, b"NULL"), (dict(dx=None), -1, b"NULL"), (dict(eidx=None), -1, b"NULL"),
+    (dict(dxt=None), -1, b"NULL"), (dict(mw=tr.MoeW(FAKE, None, FAKE)), -1, b"NULL"),
+    (dict(cmp=tr.Compaction(exp_cnt=FAKE, exp_rows=FAKE)), -1, b"NULL"),
+    (dict(dWup=None), -1, b"all"), (dict(dWgate=None), -1, b"all"), (dict(dWdown=None), -1, b"all"),
+    (dict(dxt=FAKE + 8), -1, b"aligned"), (dict(dWup=FAKE + 2), -1, b"aligned"),
+    (dict(xt=FAKE + 4), -1, b"aligned"), (dict(dg2=FAKE + 2), -1, b"aligned"),
+    (dict(n=0), -1, b">= 1"), (dict(n=(1 << 24) + 1), -2, b"tokens"),
+    (dict(ws=None), -1, b"workspace"), (dict(ws=FAKE + 16), -1, b"aligned"),
+    (dict(ws_bytes=1024), -3, b"workspace"), (dict(c=cfg160(d_ff=100)), -2, b"multiples")])
+def test_moe_backward_refuses(over, code, word):
+    assert backward(**over) == code
+    assert word in tr.lib().triroute_last_error()
+
+
+def test_moe_backward_workspace():
+    c = cfg160()
+    need = tr.workspace_bytes(c, tr.OP_MOE_BACKWARD, 16, 1)
+    assert backward(ws_bytes=need - 1) == -3
+    # the rows' four operands, and dn in fp32
+    rows = 16 * 2
+    assert need >= rows * (2 * 768 + 3 * 2048) * 2 + rows * 768 * 4
+    assert tr.workspace_bytes(c, tr.OP_MOE_BACKWARD, 1000, 1) > need
+
+
+def tensor(src=FAKE, dst=FAKE, numel=100, dtype=tr.F32):
+    return tr.GradTensor(src, dst, numel, dtype)
+
+
+def list_bytes(*ts, n=None):
+    arr = (tr.GradTensor * max(1, len(ts)))(*ts)
+    need = C.c_size_t()
+    r = tr.lib().triroute_grad_list_bytes(arr, len(ts) if n is None else n, C.byref(need))
+    return r, need.value
+
+
+@pytest.mark.parametrize("bad,word", [
+    (tensor(dtype=2), b"dtype"), (tensor(numel=-1), b"numel"), (tensor(src=None), b"NULL"),
+    (tensor(src=FAKE + 2), b"aligned"), (tensor(dst=FAKE + 1), b"aligned"),
+    (tensor(src=FAKE + 1, dtype=tr.BF16), b"aligned"), (tensor(numel=1 << 41), b"numel")])
+def test_grad_list_refuses_tensors(bad, word):
+    assert list_bytes(tensor(), bad)[0] == -1
+    assert word in tr.lib().triroute_last_error()
+    arr = (tr.GradTensor * 2)(tensor(), bad)
+    d = tr.GradListDesc()
+    assert tr.lib().triroute_grad_list_init(C.byref(d), arr, 2, FAKE, 1 << 30, None) == -1
+    assert d.base is None
+
+
+def test_grad_list_sizes():
+    assert list_bytes(tensor(), n=0)[0] == -1
+    # pieces of 16 KB, counted from the 16-byte address at or before src
+    assert list_bytes(tensor(numel=0, src=None, dst=None)) == (0, 256)
+    one = list_bytes(tensor(numel=4096))[1]
+    assert one == list_bytes(tensor(numel=1))[1] == 256
+    big = list_bytes(tensor(numel=1 << 30))[1]
+    assert 24 * (1 << 18) <= big < 24 * (1 << 18) + 512
+    d = tr.GradListDesc()
+    arr = (tr.GradTensor * 1)(tensor(numel=1 << 30))
+    f = tr.lib().triroute_grad_list_init
+    assert f(C.byref(d), arr, 1, FAKE, big - 256, None) == -3
+    assert f(C.byref(d), arr, 1, FAKE + 128, big, None) == -1
+    assert f(C.byref(d), None, 1, FAKE, big, None) == -1
+
+
+def test_grad_calls_refuse():
+    lib = tr.lib()
+    d = tr.GradListDesc(FAKE, 1, 1, 1)
+    clip = lambda d=d, t=2.0, m=1.0, norm=FAKE, ws=FAKE, n=tr.GRAD_WS_BYTES: \
+        lib.triroute_grad_clip(C.byref(d), t, m, norm, ws, n, None)  # noqa: E731
+    assert clip(t=1.0) == -2 and b"norm_type" in lib.triroute_last_error()
+    assert clip(t=-math.inf) == -2 and clip(t=math.nan) == -2
+    assert clip(m=-1.0) == -1 and clip(m=math.nan) == -1
+    assert clip(norm=None) == -1 and clip(norm=FAKE + 4) == -1
+    assert clip(ws=None) == -1 and clip(ws=FAKE + 8) == -1 and clip(n=100) == -3
+    assert clip(d=tr.GradListDesc()) == -1
+    measured = tr.GradListDesc(FAKE, 1, 1, 0)
+    assert clip(d=measured) == -1 and b"dst" in lib.triroute_last_error()
+    assert lib.triroute_grad_scale(C.byref(measured), FAKE, 1.0, None) == -1
+    assert lib.triroute_grad_scale(C.byref(d), FAKE, math.nan, None) == -1
+    assert lib.triroute_grad_norm(C.byref(d), 3.0, FAKE, FAKE, tr.GRAD_WS_BYTES, None) == -2
+
+
+def test_binding_refuses():
+    f, h = torch.zeros(4, 4), torch.zeros(4, 4, dtype=torch.bfloat16)
+    for bad in ([], [torch.zeros(3, dtype=torch.float16)], [f.t()[1:]]):
+        with pytest.raises(ValueError):
+            tr.GradList(bad)
+    for dst in ([f], [f, f, f], [f, f]):
+        with pytest.raises(ValueError):
+            tr.GradList([f, h], dst)
+    with pytest.raises(ValueError):
+        tr.GradList([f], [torch.zeros(5)])
