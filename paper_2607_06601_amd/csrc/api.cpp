@@ -247,7 +247,7 @@ void carve_moe_grad(Carve &cv, const triroute_cfg &c, int N, tr::MoeGradJob &j) 
   j.gpart = cv.take<float>(rows * tr::moe_grad_gate_parts(c));
   j.gate = cv.take<float>(rows);
   j.row_of = cv.take<int32_t>(size_t(N) * c.top_k);
-  j.part = cv.take<float>(size_t(tr::moe_grad_part_rows(N)) * c.d_model);
+  j.part = cv.take<float>(size_t(tr::moe_grad_part_rows(c, N)) * c.d_model);
 }
 
 size_t op_bytes(const triroute_cfg &c, int op, int B, int T) {

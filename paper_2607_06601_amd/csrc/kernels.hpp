@@ -222,7 +222,7 @@ inline int64_t moe_grad_rows(const triroute_cfg &c, int N) {
   return int64_t(N) * c.top_k + int64_t(MOE_PAD - 1) * c.n_experts;
 }
 int moe_grad_gate_parts(const triroute_cfg &cfg);
-int moe_grad_part_rows(int N);
+int moe_grad_part_rows(const triroute_cfg &cfg, int N);
 struct MoeGradJob {
   const void *xt, *dx, *g2;
   const int32_t *eidx;

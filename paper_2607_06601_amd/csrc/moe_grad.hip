@@ -17,6 +17,8 @@
 // Wu in input, both sides of weight) are staged as they lie, K rows of
 // columns, and read as fragments by the transposing LDS load
 // (ds_read_b64_tr_b16), so no transposed copy is made.
+#include <type_traits>
+
 #include "gemm_tile.hpp"
 #include "kernels.hpp"
 
@@ -436,6 +438,511 @@ __global__ __launch_bounds__(256) void moe_grad_weight_kernel(MoeGradArgs a) {
   }
 }
 
+// ------------------------------------------------------- four-wave products
+// One block a CU, one wave a SIMD, tiles walked by a resident block: 128 x 128
+// wave tiles of the input and weight products (64 units x 3 and 64 rows in the
+// hidden one), so that a fragment read from LDS feeds eight MFMAs (four).  Stages of 64
+// sum indices, two of them in LDS; the fragments of the next 32 are read
+// while the MFMAs of the present 32 issue.  The transfers run on over the
+// tiles' ends: the producer is two stages ahead in the block's list of (tile, step), whatever
+// the tiles' own numbers of steps.
+struct BigTile {
+  int e, p0, rows, m0, n0, nk, down;
+};
+
+// One operand of a stage: R rows of 64 sum indices (K-contiguous), or 64 rows of R
+// columns (TR).  The 1 KB transfers are dealt to the four waves in turn; the
+// jj-th of a wave covers rows step(jj) .. on, which a scalar offset adds.
+template <int R, bool TR>
+struct Operand {
+  static constexpr int BYTES = R * 128, XF = BYTES / 4096;
+  static constexpr int RPJ = TR ? 2048 / R : 32;  // rows (K rows) of the four waves' transfer jj
+  static constexpr int PAR = TR && R == 256 ? 2 : 1;
+  // the lane's source offset; columns from `valid` on (TR) read the first ones
+  // instead (their products are never stored)
+  __device__ static __forceinline__ uint32_t offset(int wave, int lane, int par, uint32_t ld, int valid) {
+    if constexpr (!TR) {
+      const int r = 8 * wave + (lane >> 3);
+      return uint32_t(r) * ld + swz<8>(r, lane & 7) * 16;
+    } else {
+      constexpr int LPR = R / 8;  // lanes a K row
+      const int k = (64 / LPR) * wave + lane / LPR, c = lane % LPR;
+      int cc = tswz<R>(k + RPJ * par, c >> 1) * 2 + (c & 1);
+      cc = cc * 8 < valid ? cc : 0;
+      return uint32_t(k) * ld + cc * 16;
+    }
+  }
+};
+
+struct Src {  // an operand's source in the producer's tile
+  const uint8_t *base;
+  int64_t step;  // bytes from one stage to the next
+  uint32_t ld;   // row pitch
+  uint32_t off[2];
+  int rows;      // rows to read (K-contiguous; a multiple of 64 or all): the others read the first
+};
+template <int R, bool TR>
+__device__ __forceinline__ void make_src(Src &s, const void *base, int64_t ld_elems, int64_t step, int rows,
+                                         int cols) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  using O = Operand<R, TR>;
+  s.base = (const uint8_t *)base;
+  s.step = step;
+  s.ld = uint32_t(ld_elems * 2);
+  s.rows = rows;
+#pragma unroll
+  for (int p = 0; p < O::PAR; ++p) s.off[p] = O::offset(wave, lane, p, s.ld, cols);
+}
+template <int R, bool TR>
+__device__ __forceinline__ void transfer(const Src &s, const uint8_t *at, int jj, uint32_t lds) {
+  using O = Operand<R, TR>;
+  const int row = O::RPJ * jj;
+  const uint8_t *b = at + (TR || row < s.rows ? uint32_t(row) * s.ld : 0u);
+  dma16_s(b, s.off[O::PAR == 2 ? jj & 1 : 0], lds + jj * 4096);
+}
+
+// Fragment addresses of an operand in a stage: 16 rows of block i from row0 on.
+template <int R, bool TR, int NI>
+struct Frags {
+  const uint8_t *b[TR ? NI : 2];
+  __device__ __forceinline__ void init(const uint8_t *base, int row0, int lane) {
+    if constexpr (!TR) {
+      const int r = row0 + (lane & 15);
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) b[ks] = base + r * 128 + (swz<8>(r, ks * 4 + (lane >> 4)) << 4);
+    } else {
+      const int k = 8 * (lane >> 4) + ((lane & 15) >> 2);
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+        b[i] = base + k * (2 * R) + tswz<R>(k, (row0 >> 4) + i) * 32 + (lane & 3) * 8;
+    }
+  }
+  __device__ __forceinline__ bf16x8_t read(int stage_off, int ks, int i) const {
+    if constexpr (!TR) {
+      return *(const bf16x8_t *)(b[ks] + stage_off + i * 2048);
+    } else {
+      typedef __attribute__((address_space(3))) s16x4_t *P;
+      typedef short s16x8_t __attribute__((ext_vector_type(8)));
+      const uint8_t *a = b[i] + stage_off + ks * (64 * R);
+      const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)a);
+      const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(a + 8 * R));
+      return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  }
+};
+
+// Row tiles of BN rows of every expert (lane e - 1), their inclusive sums.
+struct TileScan {
+  PadScan ps;
+  int nt, incl, total;
+};
+template <int BN>
+__device__ __forceinline__ TileScan tile_scan(const int32_t *cnt, int E) {
+  TileScan g;
+  g.ps = pad_scan(cnt, E);
+  g.nt = (g.ps.pc + BN - 1) / BN;
+  int x = g.nt;
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(x, d, 64);
+    if (lane >= d) x += y;
+  }
+  g.incl = x;
+  g.total = __builtin_amdgcn_readfirstlane(__shfl(x, 63, 64));
+  return g;
+}
+// Tile t of (row tiles x ny columns), in bands within each expert.
+template <int BN>
+__device__ __forceinline__ BigTile row_col_tile(const TileScan &g, int t, int ny, int &col) {
+  const uint64_t m = __ballot(g.incl * ny > t);
+  const int l = __ffsll((unsigned long long)m) - 1;
+  const int nt = __shfl(g.nt, l, 64), first = __shfl(g.incl, l, 64) - nt;
+  int i;
+  band_order(t - first * ny, nt, ny, i, col);
+  BigTile r;
+  r.e = __builtin_amdgcn_readfirstlane(l + 1);
+  r.p0 = __builtin_amdgcn_readfirstlane(__shfl(g.ps.pad, l, 64) + i * BN);
+  r.rows = __builtin_amdgcn_readfirstlane(min(BN, __shfl(g.ps.pc, l, 64) - i * BN));
+  col = __builtin_amdgcn_readfirstlane(col);
+  r.down = 0;
+  return r;
+}
+
+// [G; U; q] of 128 units and 128 rows: A blocks 0..3 gates, 4..7 ups, 8..11 the
+// columns of Wd; B blocks 0..3 n2, 4..7 dy.
+struct HiddenBig {
+  static constexpr bool EMPTY = false;  // a tile without steps
+  static constexpr int F = 128, BN = 128, NO = 5, MI = 12, NI = 4, NA = 12, NB = 8;
+  static constexpr int STAGE = 5 * 16384, IPW = 20, NM = 48;
+  MoeGradArgs a;
+  int ny;
+  Src s[NO];
+  Frags<128, false, 4> fg, fu, fn, fy;
+  Frags<128, true, 4> fd;
+  __device__ __forceinline__ TileScan scan() const { return tile_scan<BN>(a.cnt, a.E); }
+  __device__ __forceinline__ int total(const TileScan &g) const { return g.total * ny; }
+  __device__ __forceinline__ BigTile tile(const TileScan &g, int l, int total) const {
+    int by;
+    BigTile t = row_col_tile<BN>(g, xcd_tile(l, total), ny, by);
+    t.m0 = by * F;
+    t.n0 = 0;
+    t.nk = a.d / 64;
+    return t;
+  }
+  __device__ __forceinline__ void source(const BigTile &t) {
+    const int64_t d = a.d, f = a.f, w = (int64_t(t.e - 1) * f + t.m0) * d;
+    const int uv = min(F, a.f - t.m0);
+    make_src<128, false>(s[0], (const bf16 *)a.Wg + w, d, 128, uv, 0);
+    make_src<128, false>(s[1], (const bf16 *)a.Wu + w, d, 128, uv, 0);
+    make_src<128, true>(s[2], (const bf16 *)a.Wd + int64_t(t.e - 1) * d * f + t.m0, f, 128 * f, 0, uv);
+    make_src<128, false>(s[3], (const bf16 *)a.n2 + int64_t(t.p0) * d, d, 128, t.rows, 0);
+    make_src<128, false>(s[4], (const bf16 *)a.dy + int64_t(t.p0) * d, d, 128, t.rows, 0);
+  }
+  __device__ __forceinline__ const uint8_t *at(int o, int k) const { return s[o].base + k * s[o].step; }
+  __device__ __forceinline__ void dma(int j, const uint8_t *const (&at)[NO], uint32_t lds) const {
+    const int o = j / 4, jj = j % 4;
+    if (o == 2)
+      transfer<128, true>(s[2], at[2], jj, lds + 2 * 16384);
+    else
+      transfer<128, false>(s[o], at[o], jj, lds + o * 16384);
+  }
+  __device__ __forceinline__ void frags(const uint8_t *smem, int wm, int wn, int lane) {
+    fg.init(smem, wm * 64, lane);
+    fu.init(smem + 16384, wm * 64, lane);
+    fd.init(smem + 2 * 16384, wm * 64, lane);
+    fn.init(smem + 3 * 16384, wn * 64, lane);
+    fy.init(smem + 4 * 16384, wn * 64, lane);
+  }
+  // pieces in the order of their first use: A0, the rows, A1 ..
+  __device__ __forceinline__ static constexpr int npieces() { return NA + NB; }
+  __device__ __forceinline__ void read(int q, int off, int ks, bf16x8_t (&fa)[NA], bf16x8_t (&fb)[NB]) const {
+    if (q == 0) fa[0] = fg.read(off, ks, 0);
+    else if (q <= 4) fb[q - 1] = fn.read(off, ks, q - 1);
+    else if (q <= 7) fa[q - 4] = fg.read(off, ks, q - 4);
+    else if (q <= 11) fa[q - 4] = fu.read(off, ks, q - 8);
+    else if (q <= 15) fb[q - 8] = fy.read(off, ks, q - 12);
+    else fa[q - 8] = fd.read(off, ks, q - 16);
+  }
+  __device__ static constexpr int bidx(int mi, int ni) { return mi < 8 ? ni : 4 + ni; }
+  __device__ __forceinline__ void store(const BigTile &t, const f32x4_t (&acc)[MI][NI], int wm, int wn,
+                                        int lane) const {
+    const int u0 = t.m0 + wm * 64, f = a.f;
+    if (u0 >= f) return;
+    float p[NI];
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) {
+      const int r = wn * 64 + ni * 16 + (lane & 15);
+      p[ni] = r < t.rows ? a.gate[t.p0 + r] : 0.f;
+    }
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) {
+      const int r = wn * 64 + ni * 16 + (lane & 15);
+      const int64_t pos = t.p0 + r;
+      const bool in = r < t.rows;
+      float gs = 0.f;
+#pragma unroll
+      for (int mi = 0; mi < 4; ++mi) {
+        const int u = u0 + mi * 16 + 4 * (lane >> 4);
+        Hidden h[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          h[i] = hidden_grad<true>(acc[mi][ni][i], acc[4 + mi][ni][i], acc[8 + mi][ni][i], p[ni]);
+          gs += h[i].gq;
+        }
+        if (in) {
+          bf16 *o = (bf16 *)a.dGU + pos * (2 * f) + u;
+          *(uint2 *)o = make_uint2(pk_bf16(h[0].dg, h[1].dg), pk_bf16(h[2].dg, h[3].dg));
+          *(uint2 *)(o + f) = make_uint2(pk_bf16(h[0].du, h[1].du), pk_bf16(h[2].du, h[3].du));
+          if (a.Hp)
+            *(uint2 *)((bf16 *)a.Hp + pos * f + u) =
+                make_uint2(pk_bf16(h[0].hp, h[1].hp), pk_bf16(h[2].hp, h[3].hp));
+        }
+      }
+      gs += __shfl_xor(gs, 16, 64);
+      gs += __shfl_xor(gs, 32, 64);
+      if (in && lane < 16) a.gpart[pos * a.GP + u0 / 64] = gs;
+    }
+  }
+};
+
+// dn of 256 columns and 256 rows: A the columns of Wg, then of Wu; B the rows
+// of dG, then of dU, which lie behind each other.
+struct InputBig {
+  static constexpr bool EMPTY = false;
+  static constexpr int BN = 256, NO = 2, MI = 8, NI = 8, NA = 8, NB = 8;
+  static constexpr int STAGE = 2 * 32768, IPW = 16, NM = 64;
+  MoeGradArgs a;
+  int ny;
+  Src s[NO];
+  const uint8_t *Wu;  // of the producer's tile
+  Frags<256, true, 8> fa_;
+  Frags<256, false, 8> fb_;
+  __device__ __forceinline__ TileScan scan() const { return tile_scan<BN>(a.cnt, a.E); }
+  __device__ __forceinline__ int total(const TileScan &g) const { return g.total * ny; }
+  __device__ __forceinline__ BigTile tile(const TileScan &g, int l, int total) const {
+    int by;
+    BigTile t = row_col_tile<BN>(g, xcd_tile(l, total), ny, by);
+    t.m0 = by * 256;
+    t.n0 = 0;
+    t.nk = a.f / 32;
+    return t;
+  }
+  __device__ __forceinline__ void source(const BigTile &t) {
+    const int64_t d = a.d, f = a.f, w = int64_t(t.e - 1) * f * d + t.m0;
+    make_src<256, true>(s[0], (const bf16 *)a.Wg + w, d, 128 * d, 0, a.d - t.m0);
+    Wu = (const uint8_t *)((const bf16 *)a.Wu + w);
+    make_src<256, false>(s[1], (const bf16 *)a.dGU + int64_t(t.p0) * (2 * f), 2 * f, 128, t.rows, 0);
+  }
+  __device__ __forceinline__ const uint8_t *at(int o, int k) const {
+    if (o == 1) return s[1].base + k * s[1].step;
+    const int h = a.f / 64;
+    return k < h ? s[0].base + k * s[0].step : Wu + (k - h) * s[0].step;
+  }
+  __device__ __forceinline__ void dma(int j, const uint8_t *const (&at)[NO], uint32_t lds) const {
+    if (j < 8)
+      transfer<256, true>(s[0], at[0], j, lds);
+    else
+      transfer<256, false>(s[1], at[1], j - 8, lds + 32768);
+  }
+  __device__ __forceinline__ void frags(const uint8_t *smem, int wm, int wn, int lane) {
+    fa_.init(smem, wm * 128, lane);
+    fb_.init(smem + 32768, wn * 128, lane);
+  }
+  __device__ __forceinline__ void read(int q, int off, int ks, bf16x8_t (&fa)[NA], bf16x8_t (&fb)[NB]) const {
+    if (q == 0) fa[0] = fa_.read(off, ks, 0);
+    else if (q <= NB) fb[q - 1] = fb_.read(off, ks, q - 1);
+    else fa[q - NB] = fa_.read(off, ks, q - NB);
+  }
+  __device__ static constexpr int bidx(int, int ni) { return ni; }
+  __device__ __forceinline__ void store(const BigTile &t, const f32x4_t (&acc)[MI][NI], int wm, int wn,
+                                        int lane) const {
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) {
+      const int r = wn * 128 + ni * 16 + (lane & 15);
+      if (r >= t.rows) continue;
+      float *y = a.Y + int64_t(t.p0 + r) * a.d;
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi) {
+        const int m = t.m0 + wm * 128 + mi * 16 + 4 * (lane >> 4);
+        if (m < a.d) *(f32x4_t *)(y + m) = acc[mi][ni];
+      }
+    }
+  }
+};
+
+// 256 x 256 of an expert's weight gradients: [dWg; dWu] (columns d of n2
+// against units of [dG dU]) or, down, dWd (units of p s G U against columns d of
+// dy); the sum runs over the expert's rows.  The tiles of an expert are dealt to all
+// XCDs, so that experts with many rows load them alike.
+struct WeightBig {
+  static constexpr bool EMPTY = true;
+  static constexpr int NO = 2, MI = 8, NI = 8, NA = 8, NB = 8;
+  static constexpr int STAGE = 2 * 32768, IPW = 16, NM = 64;
+  MoeGradArgs a;
+  int md, mf, t1, t2;  // column tiles of d and d_ff; tiles of the two problems
+  Src s[NO];
+  Frags<256, true, 8> fa_, fb_;
+  __device__ __forceinline__ TileScan scan() const {
+    TileScan g;
+    g.ps = pad_scan(a.cnt, a.E);
+    return g;
+  }
+  // row n of the tile's matrix: a unit's row of dWg or dWu, or a column's of dWd
+  __device__ __forceinline__ bf16 *out_row(const BigTile &t, int n) const {
+    const int64_t e = int64_t(t.e - 1) * a.d * a.f;
+    if (t.down) return (bf16 *)a.dWd + e + int64_t(n) * a.f;
+    return n < a.f ? (bf16 *)a.dWg + e + int64_t(n) * a.d : (bf16 *)a.dWu + e + int64_t(n - a.f) * a.d;
+  }
+  __device__ __forceinline__ void store_zero(const BigTile &t) const {
+    const int M = t.down ? a.f : a.d, N = t.down ? a.d : 2 * a.f;
+    const int m = t.m0 + (threadIdx.x & 31) * 8;
+    for (int r = threadIdx.x >> 5; r < 256; r += 8)
+      if (t.n0 + r < N && m < M) *(uint4 *)(out_row(t, t.n0 + r) + m) = make_uint4(0u, 0u, 0u, 0u);
+  }
+  __device__ __forceinline__ int total(const TileScan &) const { return a.E * (t1 + t2); }
+  __device__ __forceinline__ BigTile tile(const TileScan &g, int l, int) const {
+    BigTile t;
+    const int e = l / (t1 + t2);
+    int x = xcd_tile(l - e * (t1 + t2), t1 + t2), i, j;
+    t.down = x >= t1;
+    if (t.down) {
+      x -= t1;
+      band_order(x, md, mf, j, i);
+    } else {
+      band_order(x, t1 / md, md, j, i);
+    }
+    t.e = e + 1;
+    t.p0 = __builtin_amdgcn_readfirstlane(__shfl(g.ps.pad, e, 64));
+    t.rows = __builtin_amdgcn_readfirstlane(__shfl(g.ps.pc, e, 64));
+    t.nk = t.rows / 64;
+    t.m0 = i * 256;
+    t.n0 = j * 256;
+    return t;
+  }
+  __device__ __forceinline__ void source(const BigTile &t) {
+    const int64_t M = t.down ? a.f : a.d, N = t.down ? a.d : 2 * a.f;
+    make_src<256, true>(s[0], (const bf16 *)(t.down ? a.Hp : a.n2) + t.p0 * M + t.m0, M, 128 * M, 0,
+                        int(M) - t.m0);
+    make_src<256, true>(s[1], (const bf16 *)(t.down ? a.dy : a.dGU) + t.p0 * N + t.n0, N, 128 * N, 0,
+                        int(N) - t.n0);
+  }
+  __device__ __forceinline__ const uint8_t *at(int o, int k) const { return s[o].base + k * s[o].step; }
+  __device__ __forceinline__ void dma(int j, const uint8_t *const (&at)[NO], uint32_t lds) const {
+    transfer<256, true>(s[j / 8], at[j / 8], j % 8, lds + (j / 8) * 32768);
+  }
+  __device__ __forceinline__ void frags(const uint8_t *smem, int wm, int wn, int lane) {
+    fa_.init(smem, wm * 128, lane);
+    fb_.init(smem + 32768, wn * 128, lane);
+  }
+  __device__ __forceinline__ void read(int q, int off, int ks, bf16x8_t (&fa)[NA], bf16x8_t (&fb)[NB]) const {
+    if (q == 0) fa[0] = fa_.read(off, ks, 0);
+    else if (q <= NB) fb[q - 1] = fb_.read(off, ks, q - 1);
+    else fa[q - NB] = fa_.read(off, ks, q - NB);
+  }
+  __device__ static constexpr int bidx(int, int ni) { return ni; }
+  __device__ __forceinline__ void store(const BigTile &t, const f32x4_t (&acc)[MI][NI], int wm, int wn,
+                                        int lane) const {
+    const int M = t.down ? a.f : a.d, N = t.down ? a.d : 2 * a.f;
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) {
+      const int n = t.n0 + wn * 128 + ni * 16 + (lane & 15);
+      if (n >= N) continue;
+      bf16 *o = out_row(t, n);
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi) {
+        const int m = t.m0 + wm * 128 + mi * 16 + 4 * (lane >> 4);
+        if (m < M)
+          *(uint2 *)(o + m) = make_uint2(pk_bf16(acc[mi][ni][0], acc[mi][ni][1]),
+                                         pk_bf16(acc[mi][ni][2], acc[mi][ni][3]));
+      }
+    }
+  }
+};
+
+template <class P>
+__global__ __launch_bounds__(256, 1) void moe_grad_big_kernel(P p) {
+  constexpr int NM = P::NM, NF = P::NA + P::NB, IPW = P::IPW, STAGE = P::STAGE;
+  constexpr int MI = P::MI, NI = P::NI;
+  // The schedule of a step, in MFMAs of its two slices of 32: reads of slice 1 beside
+  // the first NF of slice 0; a barrier once they are in (after B1J), which frees the
+  // stage for the transfers of the stage after the next; before MFMA RS of slice 1 the
+  // barrier that publishes the next stage, whose slice 0 is read from there on.
+  constexpr int RS = NM - NF < 48 ? NM - NF : 48;
+  constexpr int B1J = NF + 2;
+  constexpr int NSLOT = (NM - 1 - B1J) + RS;
+  constexpr int GAP = NSLOT / IPW < 5 ? NSLOT / IPW : 5;
+  static_assert(B1J < NM && RS + NF <= NM && GAP >= 1 && GAP * (IPW - 1) < NSLOT, "room for the transfers");
+  __shared__ __align__(1024) uint8_t smem[2 * STAGE];
+  const TileScan gs = p.scan();
+  const int total = __builtin_amdgcn_readfirstlane(p.total(gs));
+  if (int(blockIdx.x) >= total) return;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
+  const uint32_t sbase = lds_addr(smem) + wave * 1024;
+  p.frags(smem, wm, wn, lane);
+
+  // the producer: tile Lp, stage pk of it; behind the last stage the same one again, unused
+  int Lp = int(blockIdx.x) - int(gridDim.x), pk = 0, pnk = 0;
+  bool pdone = false;
+  auto advance = [&]() {
+    if (++pk < pnk) return;
+    BigTile t;
+    int l = Lp;
+    do {
+      l += int(gridDim.x);
+      if (l >= total) {
+        pdone = true;
+        pk = max(pnk - 1, 0);
+        return;
+      }
+      t = p.tile(gs, l, total);
+    } while (t.nk == 0);
+    Lp = l;
+    pk = 0;
+    pnk = t.nk;
+    p.source(t);
+  };
+  const uint8_t *src[P::NO];
+  auto locate = [&]() {
+#pragma unroll
+    for (int o = 0; o < P::NO; ++o) src[o] = p.at(o, pk);
+  };
+  bf16x8_t fa[2][P::NA], fb[2][P::NB];
+  f32x4_t acc[MI][NI];
+  advance();
+  if (!P::EMPTY || pnk > 0) {  // the block has a product
+#pragma unroll 1
+    for (int st = 0; st < 2; ++st) {
+      locate();
+#pragma unroll
+      for (int j = 0; j < IPW; ++j) p.dma(j, src, sbase + st * STAGE);
+      if (!pdone) advance();
+    }
+    wait_vm<IPW>();
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < NF; ++q) p.read(q, 0, 0, fa[0], fb[0]);
+  }
+  int cur = 0;  // byte offset of the stage in use
+  auto kstep = [&](auto first) {
+    constexpr bool FIRST = decltype(first)::value;
+    locate();
+    const uint32_t dst = sbase + cur;
+    auto slot = [&](int pos) {
+      if (pos >= 0 && pos % GAP == 0 && pos / GAP < IPW) p.dma(pos / GAP, src, dst);
+    };
+#pragma unroll
+    for (int j = 0; j < NM; ++j) {
+      const int mi = j / NI, ni = j % NI;
+      if constexpr (FIRST)
+        mfma_agpr_first(acc[mi][ni], fa[0][mi], fb[0][P::bidx(mi, ni)]);
+      else
+        mfma_agpr(acc[mi][ni], fa[0][mi], fb[0][P::bidx(mi, ni)]);
+      if (j < NF) p.read(j, cur, 1, fa[1], fb[1]);
+      if (j == B1J) __syncthreads();  // every wave's reads of the stage are in
+      if (j > B1J) slot(j - B1J - 1);
+    }
+#pragma unroll
+    for (int j = 0; j < NM; ++j) {
+      const int mi = j / NI, ni = j % NI;
+      if (j == RS) {
+        wait_vm<IPW>();  // the next stage is in: only the one after it may be out
+        __syncthreads();
+      }
+      mfma_agpr(acc[mi][ni], fa[1][mi], fb[1][P::bidx(mi, ni)]);
+      if (j < RS) slot(NM - 1 - B1J + j);
+      if (j >= RS && j - RS < NF) p.read(j - RS, (STAGE - cur), 0, fa[0], fb[0]);
+    }
+    cur = STAGE - cur;
+    if (!pdone) advance();
+  };
+  for (int L = blockIdx.x; L < total; L += int(gridDim.x)) {
+    const BigTile t = p.tile(gs, L, total);
+    if constexpr (P::EMPTY) {
+      if (t.nk == 0) {  // an expert without rows
+        p.store_zero(t);
+        continue;
+      }
+    }
+    kstep(std::true_type{});
+    for (int k = 1; k < t.nk; ++k) kstep(std::false_type{});
+    asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < MI; ++i) acc_fence_row<NI>(acc[i]);
+    // (an opaque copy of the lane: address terms hoisted out of the tile loop would hold
+    // registers through the products)
+    int ln = lane;
+    asm volatile("" : "+v"(ln));
+    p.store(t, acc, wm, wn, ln);
+    // the next stage's slice 0 again: its registers served the results
+#pragma unroll
+    for (int q = 0; q < NF; ++q) p.read(q, cur, 0, fa[0], fb[0]);
+  }
+  wait_vm<0>();  // (the unused stages)
+}
+
 // ------------------------------------------------------------------ fp32 tile
 // acc += A B^T over K (a multiple of 16), 64 x 64 on 2 x 2 waves, fp32 MFMA
 // (16x16x4).  Stages hold [k][row], rows of 80 floats: the 4 x 16 floats of a fragment
@@ -603,17 +1110,28 @@ __global__ __launch_bounds__(256) void moe_grad_weight_f32_kernel(MoeGradArgs a)
 // ------------------------------------------------------------------ tokens
 // dn of a token = the sum of its slots' rows of Y; through the norm to dxt; the
 // block's share of dg2 (fp32 over the tokens of a block, joined in fp64);
-// g_gate from the hidden tiles' partial sums.  One wave per token at a time.
+// g_gate from the hidden tiles' partial sums.  One wave per token at a time;
+// rows of up to 512 RR elements are read once and stay in registers (RR 0: any
+// width, read twice).  Bound by HBM.
 constexpr int TOK_BLOCKS = 512;
-template <typename T>
+template <typename T, int RR>
 __global__ __launch_bounds__(256) void moe_grad_token_kernel(
     const T *__restrict__ x, const T *dx, const T *__restrict__ g, const float *__restrict__ Y,
     const int32_t *__restrict__ eidx, const int32_t *__restrict__ row_of,
     const float *__restrict__ gpart, int GP, int N, int k, int d, float eps, T *dxt,
     float *__restrict__ g_gate, float *__restrict__ part) {
+  constexpr int RN = RR > 0 ? RR : 1;
+  __shared__ __align__(16) float red[RR > 0 ? 4 : 1][RR > 0 ? 512 * RR : 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  float *pr = part ? part + (int64_t(blockIdx.x) * 4 + wave) * d : nullptr;
-  bool first = true;
+  float sum[RN][8];  // the wave's share of dg2
+#pragma unroll
+  for (int q = 0; q < RN; ++q)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum[q][j] = 0.f;
+  // (RR 0: every wave has a row of part and adds to it)
+  float *pr = RR == 0 && part ? part + (int64_t(blockIdx.x) * 4 + wave) * d : nullptr;
+  if (RR == 0 && pr)
+    for (int c = lane * 8; c < d; c += 512) store8(pr + c, &sum[0][0]);
   for (int i = blockIdx.x * 4 + wave; i < N; i += gridDim.x * 4) {
     const T *xr = x + int64_t(i) * d;
     const int32_t *ei = eidx + int64_t(i) * k, *ro = row_of + int64_t(i) * k;
@@ -628,45 +1146,57 @@ __global__ __launch_bounds__(256) void moe_grad_token_kernel(
         for (int j = 0; j < 8; ++j) dn[j] += y[j];
       }
     };
+    float w[RN][8], dn[RN][8];
     double ss = 0.0, dot = 0.0;
-    for (int c = lane * 8; c < d; c += 512) {
-      float w[8], gv[8], dn[8];
-      load8(xr + c, w);
+    auto take = [&](int c, float *wv, float *dv) {  // the sums over a row
+      float gv[8];
+      load8(xr + c, wv);
       load8(g + c, gv);
-      dn8(c, dn);
+      dn8(c, dv);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        ss = fma(double(w[j]), double(w[j]), ss);
-        dot = fma(double(dn[j] * gv[j]), double(w[j]), dot);
+        ss = fma(double(wv[j]), double(wv[j]), ss);
+        dot = fma(double(dv[j] * gv[j]), double(wv[j]), dot);
       }
+    };
+    if constexpr (RR > 0) {
+#pragma unroll
+      for (int q = 0; q < RN; ++q)
+        if (lane * 8 + 512 * q < d) take(lane * 8 + 512 * q, w[q], dn[q]);
+    } else {
+      for (int c = lane * 8; c < d; c += 512) take(c, w[0], dn[0]);
     }
     ss = wave_sum(ss);
     dot = wave_sum(dot);
     const double r = 1.0 / sqrt(ss / double(d) + double(eps));
     const float rf = float(r), cf = float(r * r * r * dot / double(d));
-    for (int c = lane * 8; c < d; c += 512) {
-      float w[8], gv[8], dn[8], u[8], o[8];
-      load8(xr + c, w);
+    auto give = [&](int c, const float *wv, const float *dv, float *q) {
+      float gv[8], u[8], o[8];
       load8(g + c, gv);
       load8(dx + int64_t(i) * d + c, u);
-      dn8(c, dn);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) o[j] = u[j] + fmaf(rf, dn[j] * gv[j], -cf * w[j]);
+      for (int j = 0; j < 8; ++j) {
+        o[j] = u[j] + fmaf(rf, dv[j] * gv[j], -cf * wv[j]);
+        q[j] = fmaf(dv[j] * rf, wv[j], q[j]);
+      }
       store8(dxt + int64_t(i) * d + c, o);
-      if (pr) {
+    };
+    if constexpr (RR > 0) {
+#pragma unroll
+      for (int q = 0; q < RN; ++q)
+        if (lane * 8 + 512 * q < d) give(lane * 8 + 512 * q, w[q], dn[q], sum[q]);
+    } else {
+      for (int c = lane * 8; c < d; c += 512) {
         float q[8];
-        if (first) {
+        load8(xr + c, w[0]);
+        dn8(c, dn[0]);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) q[j] = 0.f;
-        } else {
-          load8(pr + c, q);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = fmaf(dn[j] * rf, w[j], q[j]);
-        store8(pr + c, q);
+        for (int j = 0; j < 8; ++j) q[j] = 0.f;
+        if (pr) load8(pr + c, q);
+        give(c, w[0], dn[0], q);
+        if (pr) store8(pr + c, q);
       }
     }
-    first = false;
     if (g_gate) {
       for (int s = 0; s < k; ++s) {
         float v = 0.f;
@@ -677,26 +1207,65 @@ __global__ __launch_bounds__(256) void moe_grad_token_kernel(
       }
     }
   }
-  if (pr && first)
-    for (int c = lane; c < d; c += 64) pr[c] = 0.f;
+  if constexpr (RR > 0) {
+    if (!part) return;
+#pragma unroll
+    for (int q = 0; q < RN; ++q) store8(&red[wave][512 * q + lane * 8], sum[q]);
+    __syncthreads();
+    for (int c = threadIdx.x; c < d; c += 256)
+      part[int64_t(blockIdx.x) * d + c] = ((red[0][c] + red[1][c]) + red[2][c]) + red[3][c];
+  }
 }
 
+// dg2 from the token blocks' rows of partial sums: 16 columns a block, 64 threads a
+// column over the rows, joined in fp64 in a fixed order.
 template <typename T>
-__global__ __launch_bounds__(256) void moe_grad_g2_kernel(const float *__restrict__ part, int rows, int d,
-                                                          T *__restrict__ dg2) {
-  __shared__ double red[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+__global__ __launch_bounds__(1024) void moe_grad_g2_kernel(const float *__restrict__ part, int rows, int d,
+                                                           T *__restrict__ dg2) {
+  __shared__ double red[64][17];
+  const int col = threadIdx.x & 15, at = threadIdx.x >> 4, c = blockIdx.x * 16 + col;
+  constexpr int U = 8;
   double v = 0.0;
-  for (int r = wave; r < rows; r += 4) v += double(part[int64_t(r) * d + c]);
-  red[wave][lane] = v;
+  for (int r0 = at; r0 < rows; r0 += 64 * U) {
+    float t[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) t[u] = r0 + 64 * u < rows ? part[int64_t(r0 + 64 * u) * d + c] : 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) v += double(t[u]);
+  }
+  red[at][col] = v;
   __syncthreads();
-  if (wave == 0)
-    Act<T>::st(dg2, c, float(((red[0][lane] + red[1][lane]) + red[2][lane]) + red[3][lane]));
+  if (at < 8) {
+    v = red[at][col];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) v += red[at + 8 * j][col];
+    red[at][col] = v;
+  }
+  __syncthreads();
+  if (at == 0) {
+#pragma unroll
+    for (int j = 1; j < 8; ++j) v += red[j][col];
+    Act<T>::st(dg2, c, float(v));
+  }
 }
 
 // ------------------------------------------------------------------ launchers
+static int cu_count() {
+  static const int n = [] {
+    int dev = 0, v = 0;
+    return hipGetDevice(&dev) == hipSuccess &&
+                   hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && v > 0
+               ? v
+               : 256;
+  }();
+  return n;
+}
+
 int moe_grad_gate_parts(const triroute_cfg &cfg) { return cfg.d_ff / 64 * 2; }
-int moe_grad_part_rows(int N) { return std::min((N + 3) / 4, TOK_BLOCKS) * 4; }
+static int token_blocks(int N) { return std::min((N + 3) / 4, TOK_BLOCKS); }
+int moe_grad_part_rows(const triroute_cfg &cfg, int N) {
+  return token_blocks(N) * (cfg.d_model <= 2048 ? 1 : 4);
+}
 
 template <typename T>
 static hipError_t backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, hipStream_t st) {
@@ -715,14 +1284,37 @@ static hipError_t backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, 
       (const T *)j.xt, (const T *)j.dx, (const T *)j.g2, j.egate, j.cmp.exp_cnt, j.cmp.exp_rows, E, k, d,
       cfg.rms_eps, (T *)j.n2, (T *)j.dy, j.gate, j.row_of);
   if constexpr (sizeof(T) == 2) {
-    const int nf = f / HID_F, nd = (d + INP_M - 1) / INP_M;
-    const int rt = Nk / HID_R + E;  // row tiles at most
-    moe_grad_hidden_kernel<0><<<unsigned(rt) * nf, 256, 0, st>>>(a, nf);
-    moe_grad_input_kernel<0><<<unsigned(rt) * nd, 256, 0, st>>>(a, nd);
-    if (a.Hp) {
-      const int t1 = (d + WGT_M - 1) / WGT_M * ((2 * f + WGT_N - 1) / WGT_N);
-      const int t2 = (f + WGT_M - 1) / WGT_M * ((d + WGT_N - 1) / WGT_N);
-      moe_grad_weight_kernel<0><<<unsigned(E) * (t1 + t2), 256, 0, st>>>(a);
+    const int r = Nk / (E + 1);  // rows of an expert when the router spreads its options evenly
+    if (r >= 128) {
+      const int cu = cu_count();
+      a.GP = f / 64;
+      HiddenBig h;
+      h.a = a;
+      h.ny = (f + 127) / 128;
+      moe_grad_big_kernel<<<std::min((Nk / 128 + E) * h.ny, cu), 256, 0, st>>>(h);
+      InputBig i;
+      i.a = a;
+      i.ny = (d + 255) / 256;
+      moe_grad_big_kernel<<<std::min((Nk / 256 + E) * i.ny, cu), 256, 0, st>>>(i);
+      if (a.Hp) {
+        WeightBig w;
+        w.a = a;
+        w.md = (d + 255) / 256;
+        w.mf = (f + 255) / 256;
+        w.t1 = w.md * ((2 * f + 255) / 256);
+        w.t2 = w.md * w.mf;
+        moe_grad_big_kernel<<<std::min(E * (w.t1 + w.t2), cu), 256, 0, st>>>(w);
+      }
+    } else {
+      const int nf = f / HID_F, nd = (d + INP_M - 1) / INP_M;
+      const int rt = Nk / HID_R + E;  // row tiles at most
+      moe_grad_hidden_kernel<0><<<unsigned(rt) * nf, 256, 0, st>>>(a, nf);
+      moe_grad_input_kernel<0><<<unsigned(rt) * nd, 256, 0, st>>>(a, nd);
+      if (a.Hp) {
+        const int t1 = (d + WGT_M - 1) / WGT_M * ((2 * f + WGT_N - 1) / WGT_N);
+        const int t2 = (f + WGT_M - 1) / WGT_M * ((d + WGT_N - 1) / WGT_N);
+        moe_grad_weight_kernel<0><<<unsigned(E) * (t1 + t2), 256, 0, st>>>(a);
+      }
     }
   } else {
     const int nf = f / F32_T, nd = d / F32_T, rt = Nk / F32_T + E;
@@ -730,12 +1322,18 @@ static hipError_t backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, 
     moe_grad_input_f32_kernel<<<unsigned(rt) * nd, 256, 0, st>>>(a, nd);
     if (a.Hp) moe_grad_weight_f32_kernel<<<unsigned(E) * nd * nf * 3, 256, 0, st>>>(a);
   }
-  const int prows = moe_grad_part_rows(N);
-  moe_grad_token_kernel<T><<<prows / 4, 256, 0, st>>>(
-      (const T *)j.xt, (const T *)j.dx, (const T *)j.g2, j.Y, j.eidx, j.row_of, j.gpart, a.GP, N, k, d,
-      cfg.rms_eps, (T *)j.out.dxt, j.out.g_gate, j.out.dg2 ? j.part : nullptr);
+  const int prows = moe_grad_part_rows(cfg, N);
+  auto token = [&](auto rr) {
+    moe_grad_token_kernel<T, decltype(rr)::value><<<token_blocks(N), 256, 0, st>>>(
+        (const T *)j.xt, (const T *)j.dx, (const T *)j.g2, j.Y, j.eidx, j.row_of, j.gpart, a.GP, N, k, d,
+        cfg.rms_eps, (T *)j.out.dxt, j.out.g_gate, j.out.dg2 ? j.part : nullptr);
+  };
+  if (d <= 512) token(std::integral_constant<int, 1>{});
+  else if (d <= 1024) token(std::integral_constant<int, 2>{});
+  else if (d <= 2048) token(std::integral_constant<int, 4>{});
+  else token(std::integral_constant<int, 0>{});
   if (j.out.dg2)
-    moe_grad_g2_kernel<T><<<d / 64, 256, 0, st>>>(j.part, prows, d, (T *)j.out.dg2);
+    moe_grad_g2_kernel<T><<<d / 16, 1024, 0, st>>>(j.part, prows, d, (T *)j.out.dg2);
   return hipGetLastError();
 }
 
