@@ -31,14 +31,15 @@ __device__ __forceinline__ int xcd_tile(int L, int total) {
 constexpr int BAND_R = 16, BAND_C = 2;
 
 // Tile t of a rows x ny grid walked in bands -> (row tile i, column tile j).
+template <int BR = BAND_R, int BC = BAND_C>
 __device__ __forceinline__ void band_order(int t, int rows, int ny, int &i, int &j) {
-  const int band = t / (BAND_R * ny);
-  const int rem = t - band * BAND_R * ny;
-  const int rb = min(BAND_R, rows - band * BAND_R);  // rows of this band
-  const int chunk = rem / (rb * BAND_C);
-  const int idx = rem - chunk * rb * BAND_C;
-  i = band * BAND_R + idx % rb;
-  j = chunk * BAND_C + idx / rb;
+  const int band = t / (BR * ny);
+  const int rem = t - band * BR * ny;
+  const int rb = min(BR, rows - band * BR);  // rows of this band
+  const int chunk = rem / (rb * BC);
+  const int idx = rem - chunk * rb * BC;
+  i = band * BR + idx % rb;
+  j = chunk * BC + idx / rb;
 }
 
 // LDS chunk (16 bytes) of chunk c of operand row r in a stage whose rows are

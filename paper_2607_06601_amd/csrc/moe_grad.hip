@@ -18,6 +18,7 @@
 // columns, and read as fragments by the transposing LDS load
 // (ds_read_b64_tr_b16), so no transposed copy is made.
 #include <type_traits>
+#include <utility>
 
 #include "gemm_tile.hpp"
 #include "kernels.hpp"
@@ -136,13 +137,24 @@ typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
 // Where a stage keeps the 32-byte column block b of K row k of a transposed
 // operand of R columns: the 4 K rows that 16 lanes read at once, and those of the next
-// lane group, lie in different banks.
-template <int R>
+// lane group, lie in different banks.  PAIR: the lanes read 8-byte pieces over 64
+// bytes of a K row (see Frags).
+template <int R, bool PAIR = false>
 __device__ __forceinline__ int tswz(int k, int b) {
   if constexpr (R == 64)
     return b ^ (((k >> 1) & 1) | (((k >> 3) & 1) << 1));  // two K rows a bank span
+  else if constexpr (PAIR)
+    return b ^ (((k & 3) << 1) | ((k >> 3) & 1));
   else
     return b ^ ((k & 3) | (((k >> 3) & 1) << 2));
+}
+// The same for 16-byte chunk c of row r of a K-contiguous operand (rows of 128 bytes).
+template <bool PAIR>
+__device__ __forceinline__ int rswz(int r, int c) {
+  if constexpr (PAIR)
+    return c ^ ((((r >> 3) & 3) << 1) | ((r >> 1) & 1));
+  else
+    return swz<8>(r, c);
 }
 
 // acc += A B^T over nk steps of 64, A of MR and B of NR rows, WM x WN waves, S
@@ -252,7 +264,9 @@ __device__ __forceinline__ void zero_acc(f32x4_t (&acc)[MI][NI]) {
 struct MoeGradArgs {
   const void *Wg, *Wu, *Wd;
   const void *n2, *dy;  // [rows][d]
-  void *dGU, *Hp;       // [rows][2 d_ff]: dG, then dU; [rows][d_ff]: p s G U (NULL: not wanted)
+  // dGU [rows][2 d_ff]: bf16: 64 dG, the same units' dU, the next 64 dG, ..; fp32: all dG,
+  // then all dU.  Hp [rows][d_ff]: p s G U (NULL: not wanted)
+  void *dGU, *Hp;
   const float *gate;    // [rows]
   float *Y, *gpart;     // [rows][d]; [rows][GP]
   void *dWg, *dWu, *dWd;
@@ -331,9 +345,9 @@ __global__ __launch_bounds__(256) void moe_grad_hidden_kernel(MoeGradArgs a, int
         gs += h[i].gq;
       }
       if (in) {
-        bf16 *o = (bf16 *)a.dGU + pos * (2 * f) + u;
+        bf16 *o = (bf16 *)a.dGU + pos * (2 * f) + f0 + u;  // (f0: a multiple of 64)
         *(uint2 *)o = make_uint2(pk_bf16(h[0].dg, h[1].dg), pk_bf16(h[2].dg, h[3].dg));
-        *(uint2 *)(o + f) = make_uint2(pk_bf16(h[0].du, h[1].du), pk_bf16(h[2].du, h[3].du));
+        *(uint2 *)(o + 64) = make_uint2(pk_bf16(h[0].du, h[1].du), pk_bf16(h[2].du, h[3].du));
         if (a.Hp)
           *(uint2 *)((bf16 *)a.Hp + pos * f + u) =
               make_uint2(pk_bf16(h[0].hp, h[1].hp), pk_bf16(h[2].hp, h[3].hp));
@@ -363,9 +377,9 @@ __global__ __launch_bounds__(256) void moe_grad_input_kernel(MoeGradArgs a, int 
   f32x4_t acc[C::MI][C::NI];
   zero_acc(acc);
 #pragma unroll 1
-  for (int half = 0; half < 2; ++half) {
+  for (int half = 0; half < 2; ++half) {  // the steps of 64 gates, then those of 64 ups
     const bf16 *W = (const bf16 *)(half ? a.Wu : a.Wg) + int64_t(t.e - 1) * f * d + m0;
-    const bf16 *g = (const bf16 *)a.dGU + int64_t(t.p0) * (2 * f) + half * f;
+    const bf16 *g = (const bf16 *)a.dGU + int64_t(t.p0) * (2 * f) + half * 64;
     C::run(
         smem,
         [&](int k, int c) {
@@ -374,7 +388,7 @@ __global__ __launch_bounds__(256) void moe_grad_input_kernel(MoeGradArgs a, int 
         [&](int r, int c) {
           return (const uint8_t *)(g + int64_t(r < t.rows ? r : 0) * (2 * f)) + c * 16;
         },
-        int64_t(128) * d, 128, f / 64, acc);
+        int64_t(128) * d, 256, f / 64, acc);
   }
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
 #pragma unroll
@@ -420,14 +434,10 @@ __global__ __launch_bounds__(256) void moe_grad_weight_kernel(MoeGradArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
 #pragma unroll
   for (int ni = 0; ni < C::NI; ++ni) {
-    int n = n0 + wn * (WGT_N / 2) + ni * 16 + (lane & 15);
+    const int n = n0 + wn * (WGT_N / 2) + ni * 16 + (lane & 15);
     if (n >= N) continue;
-    bf16 *o = (bf16 *)(down ? a.dWd : a.dWg);
-    if (!down && n >= f) {
-      o = (bf16 *)a.dWu;
-      n -= f;
-    }
-    o += int64_t(e - 1) * d * f + int64_t(n) * M;
+    bf16 *o = (bf16 *)(down ? a.dWd : (n & 64) ? a.dWu : a.dWg) + int64_t(e - 1) * d * f +
+              int64_t(down ? n : (n >> 7) * 64 + (n & 63)) * M;
 #pragma unroll
     for (int mi = 0; mi < C::MI; ++mi) {
       const int m = m0 + wm * (WGT_M / 2) + mi * 16 + 4 * (lane >> 4);
@@ -449,82 +459,130 @@ __global__ __launch_bounds__(256) void moe_grad_weight_kernel(MoeGradArgs a) {
 struct BigTile {
   int e, p0, rows, m0, n0, nk, down;
 };
+// Column tiles of a product over row tiles (ny), or the weight product's: column tiles of d
+// and d_ff, tiles of its two problems.
+struct BigShape {
+  int ny, md, mf, t1, t2;
+};
 
 // One operand of a stage: R rows of 64 sum indices (K-contiguous), or 64 rows of R
 // columns (TR).  The 1 KB transfers are dealt to the four waves in turn; the
-// jj-th of a wave covers rows step(jj) .. on, which a scalar offset adds.
-template <int R, bool TR>
+// jj-th of a wave covers K rows (rows) RPJ jj on.
+template <int R, bool TR, bool PAIR>
 struct Operand {
   static constexpr int BYTES = R * 128, XF = BYTES / 4096;
-  static constexpr int RPJ = TR ? 2048 / R : 32;  // rows (K rows) of the four waves' transfer jj
+  static constexpr int RPJ = TR ? 2048 / R : 32;
   static constexpr int PAR = TR && R == 256 ? 2 : 1;
   // the lane's source offset; columns from `valid` on (TR) read the first ones
   // instead (their products are never stored)
   __device__ static __forceinline__ uint32_t offset(int wave, int lane, int par, uint32_t ld, int valid) {
     if constexpr (!TR) {
       const int r = 8 * wave + (lane >> 3);
-      return uint32_t(r) * ld + swz<8>(r, lane & 7) * 16;
+      return uint32_t(r) * ld + rswz<PAIR>(r, lane & 7) * 16;
     } else {
       constexpr int LPR = R / 8;  // lanes a K row
       const int k = (64 / LPR) * wave + lane / LPR, c = lane % LPR;
-      int cc = tswz<R>(k + RPJ * par, c >> 1) * 2 + (c & 1);
+      int cc = tswz<R, PAIR>(k + RPJ * par, c >> 1) * 2 + (c & 1);
       cc = cc * 8 < valid ? cc : 0;
       return uint32_t(k) * ld + cc * 16;
     }
   }
 };
 
-struct Src {  // an operand's source in the producer's tile
-  const uint8_t *base;
-  int64_t step;  // bytes from one stage to the next
-  uint32_t ld;   // row pitch
-  uint32_t off[2];
-  int rows;      // rows to read (K-contiguous; a multiple of 64 or all): the others read the first
-};
-template <int R, bool TR>
-__device__ __forceinline__ void make_src(Src &s, const void *base, int64_t ld_elems, int64_t step, int rows,
-                                         int cols) {
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  using O = Operand<R, TR>;
-  s.base = (const uint8_t *)base;
-  s.step = step;
-  s.ld = uint32_t(ld_elems * 2);
-  s.rows = rows;
-#pragma unroll
-  for (int p = 0; p < O::PAR; ++p) s.off[p] = O::offset(wave, lane, p, s.ld, cols);
-}
-template <int R, bool TR>
-__device__ __forceinline__ void transfer(const Src &s, const uint8_t *at, int jj, uint32_t lds) {
-  using O = Operand<R, TR>;
-  const int row = O::RPJ * jj;
-  const uint8_t *b = at + (TR || row < s.rows ? uint32_t(row) * s.ld : 0u);
-  dma16_s(b, s.off[O::PAR == 2 ? jj & 1 : 0], lds + jj * 4096);
+// A wave-uniform pointer that the compiler would otherwise keep in vector registers.
+__device__ __forceinline__ const uint8_t *uniform(const void *p) {
+  const uint64_t u = uint64_t(uintptr_t(p));
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(u)), hi = __builtin_amdgcn_readfirstlane(uint32_t(u >> 32));
+  return (const uint8_t *)uintptr_t(lo | (uint64_t(hi) << 32));
 }
 
-// Fragment addresses of an operand in a stage: 16 rows of block i from row0 on.
-template <int R, bool TR, int NI>
-struct Frags {
-  const uint8_t *b[TR ? NI : 2];
-  __device__ __forceinline__ void init(const uint8_t *base, int row0, int lane) {
-    if constexpr (!TR) {
-      const int r = row0 + (lane & 15);
+// The producer's view of an operand: the base of its present stage (scalar) and the
+// lane's byte offset of each of the wave's transfers from it.
+template <int R, bool TR, bool PAIR = false>
+struct Src {
+  using O = Operand<R, TR, PAIR>;
+  const uint8_t *cur;
+  int64_t step;  // bytes from one stage to the next
+  uint32_t off[O::XF];
+  // rows: rows to read (K-contiguous; a multiple of 64 or all of them): the others read the first;
+  // cols: columns to read (TR)
+  __device__ __forceinline__ void init(const void *base, int64_t ld_elems, int64_t step_, int rows, int cols) {
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    cur = uniform(base);
+    step = step_;
+    const uint32_t ld = uint32_t(ld_elems * 2);
+    uint32_t o[O::PAR];
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) b[ks] = base + r * 128 + (swz<8>(r, ks * 4 + (lane >> 4)) << 4);
-    } else {
-      const int k = 8 * (lane >> 4) + ((lane & 15) >> 2);
+    for (int p = 0; p < O::PAR; ++p) o[p] = O::offset(wave, lane, p, ld, cols);
 #pragma unroll
-      for (int i = 0; i < NI; ++i)
-        b[i] = base + k * (2 * R) + tswz<R>(k, (row0 >> 4) + i) * 32 + (lane & 3) * 8;
+    for (int j = 0; j < O::XF; ++j) {
+      const int row = O::RPJ * j;
+      off[j] = o[O::PAR == 2 ? j & 1 : 0] + (TR || row < rows ? uint32_t(row) * ld : 0u);
     }
   }
-  __device__ __forceinline__ bf16x8_t read(int stage_off, int ks, int i) const {
+};
+
+// One transfer (dma16_s) to LDS address lds + OFF beside one MFMA, which also is the
+// wait state between the write of m0 and its use: two more instructions in the
+// shadow of the product, where an address of its own would cost five.
+template <bool FIRST, int OFF>
+__device__ __forceinline__ void mfma_dma(f32x4_t &acc, const bf16x8_t &a, const bf16x8_t &b, const void *base,
+                                         uint32_t voff, uint32_t lds) {
+  if constexpr (FIRST)
+    asm volatile(
+        "s_add_u32 m0, %4, %6\n\t"
+        "v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0\n\t"
+        "global_load_lds_dwordx4 %3, %5"
+        : "=a"(acc)
+        : "v"(a), "v"(b), "v"(voff), "s"(lds), "s"(base), "i"(OFF)
+        : "memory", "m0", "scc");
+  else
+    asm volatile(
+        "s_add_u32 m0, %4, %6\n\t"
+        "v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0\n\t"
+        "global_load_lds_dwordx4 %3, %5"
+        : "+a"(acc)
+        : "v"(a), "v"(b), "v"(voff), "s"(lds), "s"(base), "i"(OFF)
+        : "memory", "m0", "scc");
+}
+
+// Fragment addresses (LDS) of an operand in the present stage: 16 rows of block i
+// from row0 on.  What differs by block or slice is an immediate offset, and the
+// switch to the other stage (flip) one addition an address and step.
+// PAIR: row 4 q + t of blocks 2 j and 2 j + 1 is operand row 32 j + 8 q + t and
+// 32 j + 8 q + 4 + t, so that a lane's results of the two blocks are 8 consecutive ones: one
+// 16-byte store in bf16, four lanes a 64-byte run.
+template <int R, bool TR, bool PAIR, int NI>
+struct Frags {
+  static constexpr int NB = TR ? NI : 2;
+  uint32_t b[NB];
+  __device__ __forceinline__ void init(uint32_t base, int row0, int lane) {
+    const int n = lane & 15;
     if constexpr (!TR) {
-      return *(const bf16x8_t *)(b[ks] + stage_off + i * 2048);
+      const int r = row0 + (PAIR ? (n >> 2) * 8 + (n & 3) : n);
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) b[ks] = base + r * 128 + (rswz<PAIR>(r, ks * 4 + (lane >> 4)) << 4);
+    } else {
+      const int k = 8 * (lane >> 4) + (n >> 2), q = lane & 3;
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int col = row0 + (PAIR ? (i >> 1) * 32 + q * 8 + (i & 1) * 4 : i * 16 + q * 4);
+        b[i] = base + k * (2 * R) + tswz<R, PAIR>(k, col >> 4) * 32 + (col & 15) * 2;
+      }
+    }
+  }
+  __device__ __forceinline__ void flip(int delta) {
+#pragma unroll
+    for (int i = 0; i < NB; ++i) b[i] += delta;
+  }
+  __device__ __forceinline__ bf16x8_t read(int ks, int i) const {
+    if constexpr (!TR) {
+      typedef const __attribute__((address_space(3))) bf16x8_t *P;
+      return *(P)(b[ks] + (PAIR ? (i >> 1) * 4096 + (i & 1) * 512 : i * 2048));
     } else {
       typedef __attribute__((address_space(3))) s16x4_t *P;
-      typedef short s16x8_t __attribute__((ext_vector_type(8)));
-      const uint8_t *a = b[i] + stage_off + ks * (64 * R);
+      const uint32_t a = b[i] + ks * (64 * R);
       const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)a);
       const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(a + 8 * R));
       return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -570,164 +628,191 @@ __device__ __forceinline__ BigTile row_col_tile(const TileScan &g, int t, int ny
   return r;
 }
 
-// [G; U; q] of 128 units and 128 rows: A blocks 0..3 gates, 4..7 ups, 8..11 the
-// columns of Wd; B blocks 0..3 n2, 4..7 dy.
-struct HiddenBig {
-  static constexpr bool EMPTY = false;  // a tile without steps
-  static constexpr int F = 128, BN = 128, NO = 5, MI = 12, NI = 4, NA = 12, NB = 8;
-  static constexpr int STAGE = 5 * 16384, IPW = 20, NM = 48;
-  MoeGradArgs a;
-  int ny;
-  Src s[NO];
-  Frags<128, false, 4> fg, fu, fn, fy;
-  Frags<128, true, 4> fd;
+// Shared by the products over row tiles of 256: out [rows][..] of A's 256 rows (columns of a
+// weight) against the rows of a tile.
+struct RowsBase {
+  static constexpr bool EMPTY = false;  // a tile may have no steps
+  static constexpr int BN = 256, MI = 8, NI = 8, NA = 8, NB = 8;
+  static constexpr int STAGE = 2 * 32768, IPW = 16, NM = 64;
+  const MoeGradArgs &a;  // the kernel's own argument, which is not written
+  const int ny;
+  __device__ __forceinline__ RowsBase(const MoeGradArgs &a_, const BigShape &s) : a(a_), ny(s.ny) {}
   __device__ __forceinline__ TileScan scan() const { return tile_scan<BN>(a.cnt, a.E); }
   __device__ __forceinline__ int total(const TileScan &g) const { return g.total * ny; }
-  __device__ __forceinline__ BigTile tile(const TileScan &g, int l, int total) const {
-    int by;
-    BigTile t = row_col_tile<BN>(g, xcd_tile(l, total), ny, by);
-    t.m0 = by * F;
-    t.n0 = 0;
-    t.nk = a.d / 64;
-    return t;
-  }
-  __device__ __forceinline__ void source(const BigTile &t) {
-    const int64_t d = a.d, f = a.f, w = (int64_t(t.e - 1) * f + t.m0) * d;
-    const int uv = min(F, a.f - t.m0);
-    make_src<128, false>(s[0], (const bf16 *)a.Wg + w, d, 128, uv, 0);
-    make_src<128, false>(s[1], (const bf16 *)a.Wu + w, d, 128, uv, 0);
-    make_src<128, true>(s[2], (const bf16 *)a.Wd + int64_t(t.e - 1) * d * f + t.m0, f, 128 * f, 0, uv);
-    make_src<128, false>(s[3], (const bf16 *)a.n2 + int64_t(t.p0) * d, d, 128, t.rows, 0);
-    make_src<128, false>(s[4], (const bf16 *)a.dy + int64_t(t.p0) * d, d, 128, t.rows, 0);
-  }
-  __device__ __forceinline__ const uint8_t *at(int o, int k) const { return s[o].base + k * s[o].step; }
-  __device__ __forceinline__ void dma(int j, const uint8_t *const (&at)[NO], uint32_t lds) const {
-    const int o = j / 4, jj = j % 4;
-    if (o == 2)
-      transfer<128, true>(s[2], at[2], jj, lds + 2 * 16384);
-    else
-      transfer<128, false>(s[o], at[o], jj, lds + o * 16384);
-  }
-  __device__ __forceinline__ void frags(const uint8_t *smem, int wm, int wn, int lane) {
-    fg.init(smem, wm * 64, lane);
-    fu.init(smem + 16384, wm * 64, lane);
-    fd.init(smem + 2 * 16384, wm * 64, lane);
-    fn.init(smem + 3 * 16384, wn * 64, lane);
-    fy.init(smem + 4 * 16384, wn * 64, lane);
-  }
-  // pieces in the order of their first use: A0, the rows, A1 ..
-  __device__ __forceinline__ static constexpr int npieces() { return NA + NB; }
-  __device__ __forceinline__ void read(int q, int off, int ks, bf16x8_t (&fa)[NA], bf16x8_t (&fb)[NB]) const {
-    if (q == 0) fa[0] = fg.read(off, ks, 0);
-    else if (q <= 4) fb[q - 1] = fn.read(off, ks, q - 1);
-    else if (q <= 7) fa[q - 4] = fg.read(off, ks, q - 4);
-    else if (q <= 11) fa[q - 4] = fu.read(off, ks, q - 8);
-    else if (q <= 15) fb[q - 8] = fy.read(off, ks, q - 12);
-    else fa[q - 8] = fd.read(off, ks, q - 16);
-  }
-  __device__ static constexpr int bidx(int mi, int ni) { return mi < 8 ? ni : 4 + ni; }
-  __device__ __forceinline__ void store(const BigTile &t, const f32x4_t (&acc)[MI][NI], int wm, int wn,
-                                        int lane) const {
-    const int u0 = t.m0 + wm * 64, f = a.f;
-    if (u0 >= f) return;
-    float p[NI];
-#pragma unroll
-    for (int ni = 0; ni < NI; ++ni) {
-      const int r = wn * 64 + ni * 16 + (lane & 15);
-      p[ni] = r < t.rows ? a.gate[t.p0 + r] : 0.f;
-    }
-#pragma unroll
-    for (int ni = 0; ni < NI; ++ni) {
-      const int r = wn * 64 + ni * 16 + (lane & 15);
-      const int64_t pos = t.p0 + r;
-      const bool in = r < t.rows;
-      float gs = 0.f;
-#pragma unroll
-      for (int mi = 0; mi < 4; ++mi) {
-        const int u = u0 + mi * 16 + 4 * (lane >> 4);
-        Hidden h[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          h[i] = hidden_grad<true>(acc[mi][ni][i], acc[4 + mi][ni][i], acc[8 + mi][ni][i], p[ni]);
-          gs += h[i].gq;
-        }
-        if (in) {
-          bf16 *o = (bf16 *)a.dGU + pos * (2 * f) + u;
-          *(uint2 *)o = make_uint2(pk_bf16(h[0].dg, h[1].dg), pk_bf16(h[2].dg, h[3].dg));
-          *(uint2 *)(o + f) = make_uint2(pk_bf16(h[0].du, h[1].du), pk_bf16(h[2].du, h[3].du));
-          if (a.Hp)
-            *(uint2 *)((bf16 *)a.Hp + pos * f + u) =
-                make_uint2(pk_bf16(h[0].hp, h[1].hp), pk_bf16(h[2].hp, h[3].hp));
-        }
-      }
-      gs += __shfl_xor(gs, 16, 64);
-      gs += __shfl_xor(gs, 32, 64);
-      if (in && lane < 16) a.gpart[pos * a.GP + u0 / 64] = gs;
-    }
-  }
+  static constexpr int lds_off(int j) { return j * 4096; }
 };
 
-// dn of 256 columns and 256 rows: A the columns of Wg, then of Wu; B the rows
-// of dG, then of dU, which lie behind each other.
-struct InputBig {
-  static constexpr bool EMPTY = false;
-  static constexpr int BN = 256, NO = 2, MI = 8, NI = 8, NA = 8, NB = 8;
-  static constexpr int STAGE = 2 * 32768, IPW = 16, NM = 64;
-  MoeGradArgs a;
-  int ny;
-  Src s[NO];
-  const uint8_t *Wu;  // of the producer's tile
-  Frags<256, true, 8> fa_;
-  Frags<256, false, 8> fb_;
-  __device__ __forceinline__ TileScan scan() const { return tile_scan<BN>(a.cnt, a.E); }
-  __device__ __forceinline__ int total(const TileScan &g) const { return g.total * ny; }
+// fp32 out = W^T rows, 256 columns of W (whose rows are the sum index) and 256 rows.
+// TWO: dn = Wg^T dG + Wu^T dU; else q = Wd^T dx.
+template <bool TWO>
+struct RowsBig : RowsBase {
+  using RowsBase::RowsBase;
+  Src<256, true> sw;
+  Src<256, false> sr;
+  const uint8_t *other;  // the next stage of the matrix whose turn it is not
+  Frags<256, true, false, 8> fa_;
+  Frags<256, false, false, 8> fb_;
   __device__ __forceinline__ BigTile tile(const TileScan &g, int l, int total) const {
     int by;
     BigTile t = row_col_tile<BN>(g, xcd_tile(l, total), ny, by);
     t.m0 = by * 256;
     t.n0 = 0;
-    t.nk = a.f / 32;
+    t.nk = TWO ? a.f / 32 : a.d / 64;
     return t;
   }
   __device__ __forceinline__ void source(const BigTile &t) {
     const int64_t d = a.d, f = a.f, w = int64_t(t.e - 1) * f * d + t.m0;
-    make_src<256, true>(s[0], (const bf16 *)a.Wg + w, d, 128 * d, 0, a.d - t.m0);
-    Wu = (const uint8_t *)((const bf16 *)a.Wu + w);
-    make_src<256, false>(s[1], (const bf16 *)a.dGU + int64_t(t.p0) * (2 * f), 2 * f, 128, t.rows, 0);
+    if constexpr (TWO) {
+      sw.init((const bf16 *)a.Wg + w, d, 128 * d, 0, a.d - t.m0);
+      other = uniform((const bf16 *)a.Wu + w);
+      sr.init((const bf16 *)a.dGU + int64_t(t.p0) * (2 * f), 2 * f, 128, t.rows, 0);
+    } else {
+      sw.init((const bf16 *)a.Wd + w, f, 128 * f, 0, a.f - t.m0);
+      sr.init((const bf16 *)a.dy + int64_t(t.p0) * d, d, 128, t.rows, 0);
+    }
   }
-  __device__ __forceinline__ const uint8_t *at(int o, int k) const {
-    if (o == 1) return s[1].base + k * s[1].step;
-    const int h = a.f / 64;
-    return k < h ? s[0].base + k * s[0].step : Wu + (k - h) * s[0].step;
+  __device__ __forceinline__ void next(int) {
+    if constexpr (TWO) {  // 64 gates, then the same 64 ups
+      const uint8_t *n = sw.cur + sw.step;
+      sw.cur = other;
+      other = n;
+    } else {
+      sw.cur += sw.step;
+    }
+    sr.cur += sr.step;
   }
-  __device__ __forceinline__ void dma(int j, const uint8_t *const (&at)[NO], uint32_t lds) const {
-    if (j < 8)
-      transfer<256, true>(s[0], at[0], j, lds);
-    else
-      transfer<256, false>(s[1], at[1], j - 8, lds + 32768);
-  }
-  __device__ __forceinline__ void frags(const uint8_t *smem, int wm, int wn, int lane) {
+  __device__ __forceinline__ const uint8_t *base(int j) const { return j < 8 ? sw.cur : sr.cur; }
+  __device__ __forceinline__ uint32_t off(int j) const { return j < 8 ? sw.off[j & 7] : sr.off[j & 7]; }
+  __device__ __forceinline__ void frags(uint32_t smem, int wm, int wn, int lane) {
     fa_.init(smem, wm * 128, lane);
     fb_.init(smem + 32768, wn * 128, lane);
   }
-  __device__ __forceinline__ void read(int q, int off, int ks, bf16x8_t (&fa)[NA], bf16x8_t (&fb)[NB]) const {
-    if (q == 0) fa[0] = fa_.read(off, ks, 0);
-    else if (q <= NB) fb[q - 1] = fb_.read(off, ks, q - 1);
-    else fa[q - NB] = fa_.read(off, ks, q - NB);
+  __device__ __forceinline__ void flip(int delta) {
+    fa_.flip(delta);
+    fb_.flip(delta);
   }
-  __device__ static constexpr int bidx(int, int ni) { return ni; }
+  // piece q of slice ks, in the order of their first use: A0, the rows, A1 ..
+  __device__ __forceinline__ void read(int q, int ks, bf16x8_t (&fa)[NA], bf16x8_t (&fb)[NB]) const {
+    if (q == 0) fa[0] = fa_.read(ks, 0);
+    else if (q <= NB) fb[q - 1] = fb_.read(ks, q - 1);
+    else fa[q - NB] = fa_.read(ks, q - NB);
+  }
   __device__ __forceinline__ void store(const BigTile &t, const f32x4_t (&acc)[MI][NI], int wm, int wn,
                                         int lane) const {
+    const int M = TWO ? a.d : a.f;
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni) {
       const int r = wn * 128 + ni * 16 + (lane & 15);
       if (r >= t.rows) continue;
-      float *y = a.Y + int64_t(t.p0 + r) * a.d;
+      float *y = (TWO ? a.Y : (float *)a.dGU) + int64_t(t.p0 + r) * M;
 #pragma unroll
       for (int mi = 0; mi < MI; ++mi) {
         const int m = t.m0 + wm * 128 + mi * 16 + 4 * (lane >> 4);
-        if (m < a.d) *(f32x4_t *)(y + m) = acc[mi][ni];
+        if (m < M) *(f32x4_t *)(y + m) = acc[mi][ni];
       }
+    }
+  }
+};
+
+// G and U of 128 units and 256 rows, and with q (in fp32, where dG and dU go) the
+// hidden gradients: A blocks 0..3 are a wave's gates, 4..7 its ups.
+struct GateUpBig : RowsBase {
+  using RowsBase::RowsBase;
+  Src<128, false, true> sg, su;
+  Src<256, false> sr;
+  Frags<128, false, true, 4> fg, fu;
+  Frags<256, false, false, 8> fb_;
+  __device__ __forceinline__ BigTile tile(const TileScan &g, int l, int total) const {
+    int by;
+    BigTile t = row_col_tile<BN>(g, xcd_tile(l, total), ny, by);
+    t.m0 = by * 128;
+    t.n0 = 0;
+    t.nk = a.d / 64;
+    return t;
+  }
+  __device__ __forceinline__ void source(const BigTile &t) {
+    const int64_t d = a.d, w = (int64_t(t.e - 1) * a.f + t.m0) * d;
+    const int uv = min(128, a.f - t.m0);
+    sg.init((const bf16 *)a.Wg + w, d, 128, uv, 0);
+    su.init((const bf16 *)a.Wu + w, d, 128, uv, 0);
+    sr.init((const bf16 *)a.n2 + int64_t(t.p0) * d, d, 128, t.rows, 0);
+  }
+  __device__ __forceinline__ void next(int) {
+    sg.cur += sg.step;
+    su.cur += su.step;
+    sr.cur += sr.step;
+  }
+  __device__ __forceinline__ const uint8_t *base(int j) const { return j < 4 ? sg.cur : j < 8 ? su.cur : sr.cur; }
+  __device__ __forceinline__ uint32_t off(int j) const {
+    return j < 4 ? sg.off[j & 3] : j < 8 ? su.off[j & 3] : sr.off[j & 7];
+  }
+  __device__ __forceinline__ void frags(uint32_t smem, int wm, int wn, int lane) {
+    fg.init(smem, wm * 64, lane);
+    fu.init(smem + 16384, wm * 64, lane);
+    fb_.init(smem + 32768, wn * 128, lane);
+  }
+  __device__ __forceinline__ void flip(int delta) {
+    fg.flip(delta);
+    fu.flip(delta);
+    fb_.flip(delta);
+  }
+  __device__ __forceinline__ void read(int q, int ks, bf16x8_t (&fa)[NA], bf16x8_t (&fb)[NB]) const {
+    if (q == 0) fa[0] = fg.read(ks, 0);
+    else if (q <= NB) fb[q - 1] = fb_.read(ks, q - 1);
+    else if (q - NB < 4) fa[q - NB] = fg.read(ks, q - NB);
+    else fa[q - NB] = fu.read(ks, q - NB - 4);
+  }
+  __device__ __forceinline__ void store(const BigTile &t, const f32x4_t (&acc)[MI][NI], int wm, int wn,
+                                        int lane) const {
+    const int u0 = t.m0 + wm * 64, f = a.f;
+    if (u0 >= f) return;
+#pragma unroll
+    for (int ni = 0; ni < NI; ++ni) {
+      const int r = wn * 128 + ni * 16 + (lane & 15);
+      const int64_t pos = t.p0 + r;
+      const bool in = r < t.rows;
+      const float p = in ? a.gate[pos] : 0.f;
+      float gs = 0.f;
+      // the lane's 8 units of each half of the wave's 64, whose 64 q are read before dG
+      // and dU take their place: no other wave or lane touches these rows' 256 bytes
+      // but the row's other three lanes, which read them in the same instructions
+      f32x4_t q[2][2];
+      const int u = 8 * (lane >> 4);
+      bf16 *o = (bf16 *)a.dGU + pos * (2 * f) + 2 * u0;
+      if (in) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) q[j][h] = *(const f32x4_t *)((const float *)o + 32 * j + u + 4 * h);
+      }
+      if (in) {
+        uint4 wg[2], wu[2], wh[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          Hidden h[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int mi = 2 * j + (i >> 2);
+            h[i] = hidden_grad<true>(acc[mi][ni][i & 3], acc[4 + mi][ni][i & 3], q[j][i >> 2][i & 3], p);
+            gs += h[i].gq;
+          }
+          wg[j] = make_uint4(pk_bf16(h[0].dg, h[1].dg), pk_bf16(h[2].dg, h[3].dg),
+                             pk_bf16(h[4].dg, h[5].dg), pk_bf16(h[6].dg, h[7].dg));
+          wu[j] = make_uint4(pk_bf16(h[0].du, h[1].du), pk_bf16(h[2].du, h[3].du),
+                             pk_bf16(h[4].du, h[5].du), pk_bf16(h[6].du, h[7].du));
+          wh[j] = make_uint4(pk_bf16(h[0].hp, h[1].hp), pk_bf16(h[2].hp, h[3].hp),
+                             pk_bf16(h[4].hp, h[5].hp), pk_bf16(h[6].hp, h[7].hp));
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          *(uint4 *)(o + 32 * j + u) = wg[j];
+          *(uint4 *)(o + 64 + 32 * j + u) = wu[j];
+          if (a.Hp) *(uint4 *)((bf16 *)a.Hp + pos * f + u0 + 32 * j + u) = wh[j];
+        }
+      }
+      gs += __shfl_xor(gs, 16, 64);
+      gs += __shfl_xor(gs, 32, 64);
+      if (in && lane < 16) a.gpart[pos * a.GP + u0 / 64] = gs;
     }
   }
 };
@@ -738,12 +823,16 @@ struct InputBig {
 // XCDs, so that experts with many rows load them alike.
 struct WeightBig {
   static constexpr bool EMPTY = true;
-  static constexpr int NO = 2, MI = 8, NI = 8, NA = 8, NB = 8;
+  static constexpr int MI = 8, NI = 8, NA = 8, NB = 8;
   static constexpr int STAGE = 2 * 32768, IPW = 16, NM = 64;
-  MoeGradArgs a;
-  int md, mf, t1, t2;  // column tiles of d and d_ff; tiles of the two problems
-  Src s[NO];
-  Frags<256, true, 8> fa_, fb_;
+  const MoeGradArgs &a;
+  const int md, mf, t1, t2;
+  __device__ __forceinline__ WeightBig(const MoeGradArgs &a_, const BigShape &s)
+      : a(a_), md(s.md), mf(s.mf), t1(s.t1), t2(s.t2) {}
+  Src<256, true, true> sm;
+  Src<256, true> sn;
+  Frags<256, true, true, 8> fa_;
+  Frags<256, true, false, 8> fb_;
   __device__ __forceinline__ TileScan scan() const {
     TileScan g;
     g.ps = pad_scan(a.cnt, a.E);
@@ -753,7 +842,8 @@ struct WeightBig {
   __device__ __forceinline__ bf16 *out_row(const BigTile &t, int n) const {
     const int64_t e = int64_t(t.e - 1) * a.d * a.f;
     if (t.down) return (bf16 *)a.dWd + e + int64_t(n) * a.f;
-    return n < a.f ? (bf16 *)a.dWg + e + int64_t(n) * a.d : (bf16 *)a.dWu + e + int64_t(n - a.f) * a.d;
+    const int u = (n >> 7) * 64 + (n & 63);  // 64 gates, then the same 64 ups
+    return (bf16 *)((n & 64) ? a.dWu : a.dWg) + e + int64_t(u) * a.d;
   }
   __device__ __forceinline__ void store_zero(const BigTile &t) const {
     const int M = t.down ? a.f : a.d, N = t.down ? a.d : 2 * a.f;
@@ -783,46 +873,63 @@ struct WeightBig {
   }
   __device__ __forceinline__ void source(const BigTile &t) {
     const int64_t M = t.down ? a.f : a.d, N = t.down ? a.d : 2 * a.f;
-    make_src<256, true>(s[0], (const bf16 *)(t.down ? a.Hp : a.n2) + t.p0 * M + t.m0, M, 128 * M, 0,
-                        int(M) - t.m0);
-    make_src<256, true>(s[1], (const bf16 *)(t.down ? a.dy : a.dGU) + t.p0 * N + t.n0, N, 128 * N, 0,
-                        int(N) - t.n0);
+    sm.init((const bf16 *)(t.down ? a.Hp : a.n2) + t.p0 * M + t.m0, M, 128 * M, 0, int(M) - t.m0);
+    sn.init((const bf16 *)(t.down ? a.dy : a.dGU) + t.p0 * N + t.n0, N, 128 * N, 0, int(N) - t.n0);
   }
-  __device__ __forceinline__ const uint8_t *at(int o, int k) const { return s[o].base + k * s[o].step; }
-  __device__ __forceinline__ void dma(int j, const uint8_t *const (&at)[NO], uint32_t lds) const {
-    transfer<256, true>(s[j / 8], at[j / 8], j % 8, lds + (j / 8) * 32768);
+  __device__ __forceinline__ void next(int) {
+    sm.cur += sm.step;
+    sn.cur += sn.step;
   }
-  __device__ __forceinline__ void frags(const uint8_t *smem, int wm, int wn, int lane) {
+  static constexpr int lds_off(int j) { return j * 4096; }
+  __device__ __forceinline__ const uint8_t *base(int j) const { return j < 8 ? sm.cur : sn.cur; }
+  __device__ __forceinline__ uint32_t off(int j) const { return j < 8 ? sm.off[j & 7] : sn.off[j & 7]; }
+  __device__ __forceinline__ void frags(uint32_t smem, int wm, int wn, int lane) {
     fa_.init(smem, wm * 128, lane);
     fb_.init(smem + 32768, wn * 128, lane);
   }
-  __device__ __forceinline__ void read(int q, int off, int ks, bf16x8_t (&fa)[NA], bf16x8_t (&fb)[NB]) const {
-    if (q == 0) fa[0] = fa_.read(off, ks, 0);
-    else if (q <= NB) fb[q - 1] = fb_.read(off, ks, q - 1);
-    else fa[q - NB] = fa_.read(off, ks, q - NB);
+  __device__ __forceinline__ void flip(int delta) {
+    fa_.flip(delta);
+    fb_.flip(delta);
   }
-  __device__ static constexpr int bidx(int, int ni) { return ni; }
+  __device__ __forceinline__ void read(int q, int ks, bf16x8_t (&fa)[NA], bf16x8_t (&fb)[NB]) const {
+    if (q == 0) fa[0] = fa_.read(ks, 0);
+    else if (q <= NB) fb[q - 1] = fb_.read(ks, q - 1);
+    else fa[q - NB] = fa_.read(ks, q - NB);
+  }
   __device__ __forceinline__ void store(const BigTile &t, const f32x4_t (&acc)[MI][NI], int wm, int wn,
                                         int lane) const {
     const int M = t.down ? a.f : a.d, N = t.down ? a.d : 2 * a.f;
 #pragma unroll
     for (int ni = 0; ni < NI; ++ni) {
-      const int n = t.n0 + wn * 128 + ni * 16 + (lane & 15);
-      if (n >= N) continue;
-      bf16 *o = out_row(t, n);
+      const int n0 = t.n0 + wn * 128 + ni * 16;  // (M and N are multiples of 64: blocks are in or out whole)
+      if (n0 >= N) continue;
+      bf16 *o = out_row(t, n0 + (lane & 15)) + 8 * (lane >> 4);
 #pragma unroll
-      for (int mi = 0; mi < MI; ++mi) {
-        const int m = t.m0 + wm * 128 + mi * 16 + 4 * (lane >> 4);
-        if (m < M)
-          *(uint2 *)(o + m) = make_uint2(pk_bf16(acc[mi][ni][0], acc[mi][ni][1]),
-                                         pk_bf16(acc[mi][ni][2], acc[mi][ni][3]));
+      for (int j = 0; j < MI / 2; ++j) {
+        const int m = t.m0 + wm * 128 + j * 32;
+        if (m >= M) continue;
+        const f32x4_t x = acc[2 * j][ni], y = acc[2 * j + 1][ni];
+        *(uint4 *)(o + m) = make_uint4(pk_bf16(x[0], x[1]), pk_bf16(x[2], x[3]), pk_bf16(y[0], y[1]),
+                                       pk_bf16(y[2], y[3]));
       }
+      __builtin_amdgcn_sched_barrier(0);  // (a block's results at a time, not all 256 in registers)
     }
   }
 };
 
+// f(0), f(1), .. f(N - 1) with compile-time arguments
+template <int N, class F, int... I>
+__device__ __forceinline__ void unroll_(F &&f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void unroll(F &&f) {
+  unroll_<N>(f, std::make_integer_sequence<int, N>{});
+}
+
 template <class P>
-__global__ __launch_bounds__(256, 1) void moe_grad_big_kernel(P p) {
+__global__ __launch_bounds__(256, 1) void moe_grad_big_kernel(MoeGradArgs a, BigShape shape) {
+  P p(a, shape);
   constexpr int NM = P::NM, NF = P::NA + P::NB, IPW = P::IPW, STAGE = P::STAGE;
   constexpr int MI = P::MI, NI = P::NI;
   // The schedule of a step, in MFMAs of its two slices of 32: reads of slice 1 beside
@@ -840,23 +947,22 @@ __global__ __launch_bounds__(256, 1) void moe_grad_big_kernel(P p) {
   if (int(blockIdx.x) >= total) return;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
-  const uint32_t sbase = lds_addr(smem) + wave * 1024;
-  p.frags(smem, wm, wn, lane);
+  uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(smem) + wave * 1024);  // the wave's part of the present stage
+  int delta = STAGE;                                                             // to the other one
+  p.frags(lds_addr(smem), wm, wn, lane);
 
-  // the producer: tile Lp, stage pk of it; behind the last stage the same one again, unused
+  // the producer: stage pk of tile Lp; behind the block's last stage the same one again, unused
   int Lp = int(blockIdx.x) - int(gridDim.x), pk = 0, pnk = 0;
-  bool pdone = false;
-  auto advance = [&]() {
-    if (++pk < pnk) return;
+  auto advance = [&]() __attribute__((always_inline)) {
+    if (pk + 1 < pnk) {
+      p.next(++pk);
+      return;
+    }
     BigTile t;
     int l = Lp;
     do {
       l += int(gridDim.x);
-      if (l >= total) {
-        pdone = true;
-        pk = max(pnk - 1, 0);
-        return;
-      }
+      if (l >= total) return;
       t = p.tile(gs, l, total);
     } while (t.nk == 0);
     Lp = l;
@@ -864,59 +970,52 @@ __global__ __launch_bounds__(256, 1) void moe_grad_big_kernel(P p) {
     pnk = t.nk;
     p.source(t);
   };
-  const uint8_t *src[P::NO];
-  auto locate = [&]() {
-#pragma unroll
-    for (int o = 0; o < P::NO; ++o) src[o] = p.at(o, pk);
-  };
   bf16x8_t fa[2][P::NA], fb[2][P::NB];
   f32x4_t acc[MI][NI];
   advance();
   if (!P::EMPTY || pnk > 0) {  // the block has a product
-#pragma unroll 1
-    for (int st = 0; st < 2; ++st) {
-      locate();
 #pragma unroll
-      for (int j = 0; j < IPW; ++j) p.dma(j, src, sbase + st * STAGE);
-      if (!pdone) advance();
-    }
+    for (int j = 0; j < IPW; ++j) dma16_s(p.base(j), p.off(j), dst + P::lds_off(j));
+    advance();
+#pragma unroll
+    for (int j = 0; j < IPW; ++j) dma16_s(p.base(j), p.off(j), dst + STAGE + P::lds_off(j));
+    advance();
     wait_vm<IPW>();
     __syncthreads();
 #pragma unroll
-    for (int q = 0; q < NF; ++q) p.read(q, 0, 0, fa[0], fb[0]);
+    for (int q = 0; q < NF; ++q) p.read(q, 0, fa[0], fb[0]);
   }
-  int cur = 0;  // byte offset of the stage in use
-  auto kstep = [&](auto first) {
+  auto step = [&](auto first) __attribute__((always_inline)) {
     constexpr bool FIRST = decltype(first)::value;
-    locate();
-    const uint32_t dst = sbase + cur;
-    auto slot = [&](int pos) {
-      if (pos >= 0 && pos % GAP == 0 && pos / GAP < IPW) p.dma(pos / GAP, src, dst);
-    };
-#pragma unroll
-    for (int j = 0; j < NM; ++j) {
-      const int mi = j / NI, ni = j % NI;
-      if constexpr (FIRST)
-        mfma_agpr_first(acc[mi][ni], fa[0][mi], fb[0][P::bidx(mi, ni)]);
+    unroll<NM>([&](auto J) __attribute__((always_inline)) {
+      constexpr int j = decltype(J)::value, mi = j / NI, ni = j % NI, pos = j - B1J - 1;
+      if constexpr (pos >= 0 && pos % GAP == 0 && pos / GAP < IPW)
+        mfma_dma<FIRST, P::lds_off(pos / GAP)>(acc[mi][ni], fa[0][mi], fb[0][ni],
+                                               p.base(pos / GAP), p.off(pos / GAP), dst);
+      else if constexpr (FIRST)
+        mfma_agpr_first(acc[mi][ni], fa[0][mi], fb[0][ni]);
       else
-        mfma_agpr(acc[mi][ni], fa[0][mi], fb[0][P::bidx(mi, ni)]);
-      if (j < NF) p.read(j, cur, 1, fa[1], fb[1]);
-      if (j == B1J) __syncthreads();  // every wave's reads of the stage are in
-      if (j > B1J) slot(j - B1J - 1);
-    }
-#pragma unroll
-    for (int j = 0; j < NM; ++j) {
-      const int mi = j / NI, ni = j % NI;
-      if (j == RS) {
+        mfma_agpr(acc[mi][ni], fa[0][mi], fb[0][ni]);
+      if constexpr (j < NF) p.read(j, 1, fa[1], fb[1]);
+      if constexpr (j == B1J) __syncthreads();  // every wave's reads of the stage are in
+    });
+    p.flip(delta);
+    unroll<NM>([&](auto J) __attribute__((always_inline)) {
+      constexpr int j = decltype(J)::value, mi = j / NI, ni = j % NI, pos = NM - 1 - B1J + j;
+      if constexpr (j == RS) {
         wait_vm<IPW>();  // the next stage is in: only the one after it may be out
         __syncthreads();
       }
-      mfma_agpr(acc[mi][ni], fa[1][mi], fb[1][P::bidx(mi, ni)]);
-      if (j < RS) slot(NM - 1 - B1J + j);
-      if (j >= RS && j - RS < NF) p.read(j - RS, (STAGE - cur), 0, fa[0], fb[0]);
-    }
-    cur = STAGE - cur;
-    if (!pdone) advance();
+      if constexpr (j < RS && pos % GAP == 0 && pos / GAP < IPW)
+        mfma_dma<false, P::lds_off(pos / GAP)>(acc[mi][ni], fa[1][mi], fb[1][ni],
+                                               p.base(pos / GAP), p.off(pos / GAP), dst);
+      else
+        mfma_agpr(acc[mi][ni], fa[1][mi], fb[1][ni]);
+      if constexpr (j >= RS && j - RS < NF) p.read(j - RS, 0, fa[0], fb[0]);
+    });
+    dst += delta;
+    delta = -delta;
+    advance();
   };
   for (int L = blockIdx.x; L < total; L += int(gridDim.x)) {
     const BigTile t = p.tile(gs, L, total);
@@ -926,8 +1025,8 @@ __global__ __launch_bounds__(256, 1) void moe_grad_big_kernel(P p) {
         continue;
       }
     }
-    kstep(std::true_type{});
-    for (int k = 1; k < t.nk; ++k) kstep(std::false_type{});
+    step(std::true_type{});
+    for (int k = 1; k < t.nk; ++k) step(std::false_type{});
     asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory");
 #pragma unroll
     for (int i = 0; i < MI; ++i) acc_fence_row<NI>(acc[i]);
@@ -938,7 +1037,7 @@ __global__ __launch_bounds__(256, 1) void moe_grad_big_kernel(P p) {
     p.store(t, acc, wm, wn, ln);
     // the next stage's slice 0 again: its registers served the results
 #pragma unroll
-    for (int q = 0; q < NF; ++q) p.read(q, cur, 0, fa[0], fb[0]);
+    for (int q = 0; q < NF; ++q) p.read(q, 0, fa[0], fb[0]);
   }
   wait_vm<0>();  // (the unused stages)
 }
@@ -1288,23 +1387,21 @@ static hipError_t backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, 
     if (r >= 128) {
       const int cu = cu_count();
       a.GP = f / 64;
-      HiddenBig h;
-      h.a = a;
-      h.ny = (f + 127) / 128;
-      moe_grad_big_kernel<<<std::min((Nk / 128 + E) * h.ny, cu), 256, 0, st>>>(h);
-      InputBig i;
-      i.a = a;
-      i.ny = (d + 255) / 256;
-      moe_grad_big_kernel<<<std::min((Nk / 256 + E) * i.ny, cu), 256, 0, st>>>(i);
-      if (a.Hp) {
-        WeightBig w;
-        w.a = a;
-        w.md = (d + 255) / 256;
-        w.mf = (f + 255) / 256;
-        w.t1 = w.md * ((2 * f + 255) / 256);
-        w.t2 = w.md * w.mf;
-        moe_grad_big_kernel<<<std::min(E * (w.t1 + w.t2), cu), 256, 0, st>>>(w);
-      }
+      BigShape sh{};
+      sh.md = (d + 255) / 256;
+      sh.mf = (f + 255) / 256;
+      sh.t1 = sh.md * ((2 * f + 255) / 256);
+      sh.t2 = sh.md * sh.mf;
+      auto blocks = [&](int ny) { return unsigned(std::min<int64_t>((int64_t(Nk) / 256 + E) * ny, cu)); };
+      sh.ny = sh.mf;
+      moe_grad_big_kernel<RowsBig<false>><<<blocks(sh.ny), 256, 0, st>>>(a, sh);
+      sh.ny = (f + 127) / 128;
+      moe_grad_big_kernel<GateUpBig><<<blocks(sh.ny), 256, 0, st>>>(a, sh);
+      sh.ny = sh.md;
+      moe_grad_big_kernel<RowsBig<true>><<<blocks(sh.ny), 256, 0, st>>>(a, sh);
+      if (a.Hp)
+        moe_grad_big_kernel<WeightBig><<<unsigned(std::min<int64_t>(int64_t(E) * (sh.t1 + sh.t2), cu)), 256, 0, st>>>(
+            a, sh);
     } else {
       const int nf = f / HID_F, nd = (d + INP_M - 1) / INP_M;
       const int rt = Nk / HID_R + E;  // row tiles at most
