@@ -137,14 +137,11 @@ typedef short s16x4_t __attribute__((ext_vector_type(4)));
 
 // Where a stage keeps the 32-byte column block b of K row k of a transposed
 // operand of R columns: the 4 K rows that 16 lanes read at once, and those of the next
-// lane group, lie in different banks.  PAIR: the lanes read 8-byte pieces over 64
-// bytes of a K row (see Frags).
-template <int R, bool PAIR = false>
+// lane group, lie in different banks.
+template <int R>
 __device__ __forceinline__ int tswz(int k, int b) {
   if constexpr (R == 64)
     return b ^ (((k >> 1) & 1) | (((k >> 3) & 1) << 1));  // two K rows a bank span
-  else if constexpr (PAIR)
-    return b ^ (((k & 3) << 1) | ((k >> 3) & 1));
   else
     return b ^ ((k & 3) | (((k >> 3) & 1) << 2));
 }
@@ -482,7 +479,7 @@ struct Operand {
     } else {
       constexpr int LPR = R / 8;  // lanes a K row
       const int k = (64 / LPR) * wave + lane / LPR, c = lane % LPR;
-      int cc = tswz<R, PAIR>(k + RPJ * par, c >> 1) * 2 + (c & 1);
+      int cc = tswz<R>(k + RPJ * par, c >> 1) * 2 + (c & 1);
       cc = cc * 8 < valid ? cc : 0;
       return uint32_t(k) * ld + cc * 16;
     }
@@ -550,11 +547,13 @@ __device__ __forceinline__ void mfma_dma(f32x4_t &acc, const bf16x8_t &a, const 
 // Fragment addresses (LDS) of an operand in the present stage: 16 rows of block i
 // from row0 on.  What differs by block or slice is an immediate offset, and the
 // switch to the other stage (flip) one addition an address and step.
-// PAIR: row 4 q + t of blocks 2 j and 2 j + 1 is operand row 32 j + 8 q + t and
+// PAIR (K-contiguous): row 4 q + t of blocks 2 j and 2 j + 1 is operand row 32 j + 8 q + t and
 // 32 j + 8 q + 4 + t, so that a lane's results of the two blocks are 8 consecutive ones: one
-// 16-byte store in bf16, four lanes a 64-byte run.
+// 16-byte store in bf16, four lanes a 64-byte run.  (The transposing load would read 8
+// bytes of every 16 then, and half the banks: see pair_rows.)
 template <int R, bool TR, bool PAIR, int NI>
 struct Frags {
+  static_assert(!(TR && PAIR), "K-contiguous operands");
   static constexpr int NB = TR ? NI : 2;
   uint32_t b[NB];
   __device__ __forceinline__ void init(uint32_t base, int row0, int lane) {
@@ -567,8 +566,8 @@ struct Frags {
       const int k = 8 * (lane >> 4) + (n >> 2), q = lane & 3;
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int col = row0 + (PAIR ? (i >> 1) * 32 + q * 8 + (i & 1) * 4 : i * 16 + q * 4);
-        b[i] = base + k * (2 * R) + tswz<R, PAIR>(k, col >> 4) * 32 + (col & 15) * 2;
+        const int col = row0 + i * 16 + q * 4;
+        b[i] = base + k * (2 * R) + tswz<R>(k, col >> 4) * 32 + (col & 15) * 2;
       }
     }
   }
@@ -766,26 +765,32 @@ struct GateUpBig : RowsBase {
                                         int lane) const {
     const int u0 = t.m0 + wm * 64, f = a.f;
     if (u0 >= f) return;
+    // Four row blocks at a time, their q in flight together.  The lane's 8 units of each half
+    // of the wave's 64: their q (256 bytes a row) are read before dG and dU take their place;
+    // nothing but the row's other three lanes touches those bytes, in the same instructions.
+    const int u = 8 * (lane >> 4);
+    constexpr int NQ = 4;
 #pragma unroll
-    for (int ni = 0; ni < NI; ++ni) {
-      const int r = wn * 128 + ni * 16 + (lane & 15);
-      const int64_t pos = t.p0 + r;
-      const bool in = r < t.rows;
-      const float p = in ? a.gate[pos] : 0.f;
-      float gs = 0.f;
-      // the lane's 8 units of each half of the wave's 64, whose 64 q are read before dG
-      // and dU take their place: no other wave or lane touches these rows' 256 bytes
-      // but the row's other three lanes, which read them in the same instructions
-      f32x4_t q[2][2];
-      const int u = 8 * (lane >> 4);
-      bf16 *o = (bf16 *)a.dGU + pos * (2 * f) + 2 * u0;
-      if (in) {
+    for (int n0 = 0; n0 < NI; n0 += NQ) {
+      f32x4_t q[NQ][2][2];
+      float p[NQ];
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        const int r = wn * 128 + (n0 + n) * 16 + (lane & 15);
+        const int64_t pos = t.p0 + (r < t.rows ? r : 0);  // (the first row's are read, and not used)
+        const float *qr = (const float *)a.dGU + pos * f + u0 + u;
+        p[n] = a.gate[pos];
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) q[j][h] = *(const f32x4_t *)((const float *)o + 32 * j + u + 4 * h);
+          for (int h = 0; h < 2; ++h) q[n][j][h] = *(const f32x4_t *)(qr + 32 * j + 4 * h);
       }
-      if (in) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) {
+        const int ni = n0 + n, r = wn * 128 + ni * 16 + (lane & 15);
+        const int64_t pos = t.p0 + r;
+        const bool in = r < t.rows;
+        float gs = 0.f;
         uint4 wg[2], wu[2], wh[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -793,7 +798,7 @@ struct GateUpBig : RowsBase {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int mi = 2 * j + (i >> 2);
-            h[i] = hidden_grad<true>(acc[mi][ni][i & 3], acc[4 + mi][ni][i & 3], q[j][i >> 2][i & 3], p);
+            h[i] = hidden_grad<true>(acc[mi][ni][i & 3], acc[4 + mi][ni][i & 3], q[n][j][i >> 2][i & 3], p[n]);
             gs += h[i].gq;
           }
           wg[j] = make_uint4(pk_bf16(h[0].dg, h[1].dg), pk_bf16(h[2].dg, h[3].dg),
@@ -803,19 +808,31 @@ struct GateUpBig : RowsBase {
           wh[j] = make_uint4(pk_bf16(h[0].hp, h[1].hp), pk_bf16(h[2].hp, h[3].hp),
                              pk_bf16(h[4].hp, h[5].hp), pk_bf16(h[6].hp, h[7].hp));
         }
+        if (in) {
+          bf16 *o = (bf16 *)a.dGU + pos * (2 * f) + 2 * u0 + u;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          *(uint4 *)(o + 32 * j + u) = wg[j];
-          *(uint4 *)(o + 64 + 32 * j + u) = wu[j];
-          if (a.Hp) *(uint4 *)((bf16 *)a.Hp + pos * f + u0 + 32 * j + u) = wh[j];
+          for (int j = 0; j < 2; ++j) {
+            *(uint4 *)(o + 32 * j) = wg[j];
+            *(uint4 *)(o + 64 + 32 * j) = wu[j];
+            if (a.Hp) *(uint4 *)((bf16 *)a.Hp + pos * f + u0 + 32 * j + u) = wh[j];
+          }
         }
+        gs += __shfl_xor(gs, 16, 64);
+        gs += __shfl_xor(gs, 32, 64);
+        if (in && lane < 16) a.gpart[pos * a.GP + u0 / 64] = gs;
       }
-      gs += __shfl_xor(gs, 16, 64);
-      gs += __shfl_xor(gs, 32, 64);
-      if (in && lane < 16) a.gpart[pos * a.GP + u0 / 64] = gs;
     }
   }
 };
+
+// Rows 4 g .. 4 g + 3 (g = lane / 16) of two 16-row blocks a and b, packed, to 8
+// consecutive rows a lane: lane groups 0 and 2 get rows 0 .. 7 and 8 .. 15 of a, 1 and 3
+// those of b (the odd groups' words of a change places with the even groups' of b).
+__device__ __forceinline__ uint4 pair_rows(uint2 a, uint2 b) {
+  const auto x = __builtin_amdgcn_permlane16_swap(a.x, b.x, false, false);
+  const auto y = __builtin_amdgcn_permlane16_swap(a.y, b.y, false, false);
+  return make_uint4(x[0], y[0], x[1], y[1]);
+}
 
 // 256 x 256 of an expert's weight gradients: [dWg; dWu] (columns d of n2
 // against units of [dG dU]) or, down, dWd (units of p s G U against columns d of
@@ -829,10 +846,8 @@ struct WeightBig {
   const int md, mf, t1, t2;
   __device__ __forceinline__ WeightBig(const MoeGradArgs &a_, const BigShape &s)
       : a(a_), md(s.md), mf(s.mf), t1(s.t1), t2(s.t2) {}
-  Src<256, true, true> sm;
-  Src<256, true> sn;
-  Frags<256, true, true, 8> fa_;
-  Frags<256, true, false, 8> fb_;
+  Src<256, true> sm, sn;
+  Frags<256, true, false, 8> fa_, fb_;
   __device__ __forceinline__ TileScan scan() const {
     TileScan g;
     g.ps = pad_scan(a.cnt, a.E);
@@ -903,14 +918,14 @@ struct WeightBig {
     for (int ni = 0; ni < NI; ++ni) {
       const int n0 = t.n0 + wn * 128 + ni * 16;  // (M and N are multiples of 64: blocks are in or out whole)
       if (n0 >= N) continue;
-      bf16 *o = out_row(t, n0 + (lane & 15)) + 8 * (lane >> 4);
+      bf16 *o = out_row(t, n0 + (lane & 15)) + 16 * ((lane >> 4) & 1) + 8 * (lane >> 5);
 #pragma unroll
       for (int j = 0; j < MI / 2; ++j) {
         const int m = t.m0 + wm * 128 + j * 32;
         if (m >= M) continue;
         const f32x4_t x = acc[2 * j][ni], y = acc[2 * j + 1][ni];
-        *(uint4 *)(o + m) = make_uint4(pk_bf16(x[0], x[1]), pk_bf16(x[2], x[3]), pk_bf16(y[0], y[1]),
-                                       pk_bf16(y[2], y[3]));
+        *(uint4 *)(o + m) = pair_rows(make_uint2(pk_bf16(x[0], x[1]), pk_bf16(x[2], x[3])),
+                                      make_uint2(pk_bf16(y[0], y[1]), pk_bf16(y[2], y[3])));
       }
       __builtin_amdgcn_sched_barrier(0);  // (a block's results at a time, not all 256 in registers)
     }
