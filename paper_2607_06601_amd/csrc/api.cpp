@@ -243,10 +243,11 @@ void carve_moe_grad(Carve &cv, const triroute_cfg &c, int N, tr::MoeGradJob &j) 
   j.dy = cv.take<uint8_t>(rows * c.d_model * ab);
   j.dGU = cv.take<uint8_t>(rows * c.d_ff * 2 * ab);
   j.Hp = cv.take<uint8_t>(rows * c.d_ff * ab);
-  j.Y = cv.take<float>(rows * c.d_model);
+  j.Y = cv.take<float>(std::max(rows, size_t(N) * c.top_k * tr::moe_grad_splits(c, N)) * c.d_model);
   j.gpart = cv.take<float>(rows * tr::moe_grad_gate_parts(c));
   j.gate = cv.take<float>(rows);
   j.row_of = cv.take<int32_t>(size_t(N) * c.top_k);
+  j.list_of = cv.take<int32_t>(size_t(N) * c.top_k);
   j.part = cv.take<float>(size_t(tr::moe_grad_part_rows(c, N)) * c.d_model);
 }
 

@@ -222,6 +222,7 @@ inline int64_t moe_grad_rows(const triroute_cfg &c, int N) {
   return int64_t(N) * c.top_k + int64_t(MOE_PAD - 1) * c.n_experts;
 }
 int moe_grad_gate_parts(const triroute_cfg &cfg);
+int moe_grad_splits(const triroute_cfg &cfg, int N);  // planes of Y
 int moe_grad_part_rows(const triroute_cfg &cfg, int N);
 struct MoeGradJob {
   const void *xt, *dx, *g2;
@@ -233,9 +234,9 @@ struct MoeGradJob {
   // scratch: rows by expert (moe_grad_rows of them)
   void *n2, *dy;      // [rows][d] act
   void *dGU, *Hp;     // [rows][2 d_ff], [rows][d_ff] act
-  float *Y, *gpart;   // [rows][d]; [rows][moe_grad_gate_parts]
+  float *Y, *gpart;   // [rows][d], or (split sums) planes of [N k][d]; [rows][moe_grad_gate_parts]
   float *gate;        // [rows]
-  int32_t *row_of;    // [N k]
+  int32_t *row_of, *list_of;  // [N k]: the assignment's padded row and list entry
   float *part;        // [moe_grad_part_rows][d]
 };
 hipError_t launch_moe_backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, hipStream_t st);

@@ -55,6 +55,7 @@ __device__ __forceinline__ PadScan pad_scan(const int32_t *cnt, int E) {
 // Row tile t of BN padded rows: its expert, first padded row and rows (a multiple of 64).
 struct RowTile {
   int e, p0, rows;
+  int l0, valid;  // first list entry, rows that are not padding
 };
 template <int BN>
 __device__ __forceinline__ bool row_tile(const PadScan &g, int t, RowTile &r, int &total) {
@@ -74,6 +75,8 @@ __device__ __forceinline__ bool row_tile(const PadScan &g, int t, RowTile &r, in
   r.e = __builtin_amdgcn_readfirstlane(l + 1);
   r.p0 = __builtin_amdgcn_readfirstlane(__shfl(g.pad, l, 64) + i * BN);
   r.rows = __builtin_amdgcn_readfirstlane(min(BN, __shfl(g.pc, l, 64) - i * BN));
+  r.l0 = __builtin_amdgcn_readfirstlane(__shfl(g.list, l, 64) + i * BN);
+  r.valid = __builtin_amdgcn_readfirstlane(min(BN, __shfl(g.c, l, 64) - i * BN));
   return true;
 }
 
@@ -86,7 +89,8 @@ __global__ __launch_bounds__(256) void moe_grad_rows_kernel(
     const T *__restrict__ x, const T *__restrict__ dx, const T *__restrict__ g,
     const float *__restrict__ egate, const int32_t *__restrict__ cnt,
     const int32_t *__restrict__ rows, int E, int k, int d, float eps, T *__restrict__ n2,
-    T *__restrict__ dy, float *__restrict__ gate, int32_t *__restrict__ row_of) {
+    T *__restrict__ dy, float *__restrict__ gate, int32_t *__restrict__ row_of,
+    int32_t *__restrict__ list_of) {
   const int pos = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   const int lane = threadIdx.x & 63;
   const PadScan ps = pad_scan(cnt, E);
@@ -104,7 +108,8 @@ __global__ __launch_bounds__(256) void moe_grad_rows_kernel(
     if (lane == 0) gate[pos] = 0.f;
     return;
   }
-  const int a = __builtin_amdgcn_readfirstlane(rows[__shfl(ps.list, l, 64) + i]);
+  const int entry = __shfl(ps.list, l, 64) + i;
+  const int a = __builtin_amdgcn_readfirstlane(rows[entry]);
   const T *xr = x + int64_t(a / k) * d, *yr = dx + int64_t(a / k) * d;
   double ss = 0.0;
   for (int c = lane * 8; c < d; c += 512) {
@@ -129,6 +134,7 @@ __global__ __launch_bounds__(256) void moe_grad_rows_kernel(
   if (lane == 0) {
     gate[pos] = egate[a];
     row_of[a] = pos;
+    list_of[a] = entry;
   }
 }
 
@@ -157,8 +163,8 @@ __device__ __forceinline__ int rswz(int r, int c) {
 // acc += A B^T over nk steps of 64, A of MR and B of NR rows, WM x WN waves, S
 // stages in LDS.  AT / BT: the operand lies as K rows of MR / NR columns.  Sources are
 // given as functions (row, 16-byte chunk of its K step) or, transposed, (K row of
-// the step, 16-byte chunk of its columns) -> address at step 0, and the bytes
-// from one step to the next.  SPLIT 2: a wave's rows are taken in halves from
+// the step, 16-byte chunk of its columns) -> address at step 0, and step -> bytes
+// from there.  SPLIT 2: a wave's rows are taken in halves from
 // the two halves of A (the units' gates and ups).
 template <int MR, int NR, bool AT, bool BT, int SPLIT, int WM, int WN, int S>
 struct TileCore {
@@ -186,9 +192,9 @@ struct TileCore {
     }
   }
 
-  template <class FA, class FB>
-  __device__ static __forceinline__ void run(uint8_t *smem, FA &&fa, FB &&fb, int64_t astep,
-                                             int64_t bstep, int nk, f32x4_t (&acc)[MI][NI]) {
+  template <class FA, class FB, class SA, class SB>
+  __device__ static __forceinline__ void run(uint8_t *smem, FA &&fa, FB &&fb, SA &&astep, SB &&bstep, int nk,
+                                             f32x4_t (&acc)[MI][NI]) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
@@ -216,10 +222,11 @@ struct TileCore {
     }
     const uint32_t sbase = lds_addr(smem) + wave * IPW * 1024;
     auto issue = [&](int kt, int stage) {
+      const int64_t ao = astep(kt), bo = bstep(kt);
 #pragma unroll
       for (int j = 0; j < IPW; ++j) {
         const bool isa = (wave * IPW + j) * 1024 < ABYTES;
-        dma16(src[j] + kt * (isa ? astep : bstep), sbase + stage * STAGE + j * 1024);
+        dma16(src[j] + (isa ? ao : bo), sbase + stage * STAGE + j * 1024);
       }
     };
 #pragma unroll
@@ -288,14 +295,18 @@ __device__ __forceinline__ Hidden hidden_grad(float G, float U, float q, float p
   return r;
 }
 
-// ------------------------------------------------------------------ hidden
-constexpr int HID_F = 64, HID_R = 128;  // units and rows of a tile
-template <int>
+// ------------------------------------------------- few rows: streaming weights
+// With few rows an expert the products read each weight about once and the time
+// is that of the stream: narrow tiles over all CUs, three stages in flight ahead of
+// the one in use.
+
+// [G; U; q] of 64 units and 64 rows.
+constexpr int HID_F = 64, HID_R = 64, HID_S = 4;
 __global__ __launch_bounds__(256) void moe_grad_hidden_kernel(MoeGradArgs a, int nf) {
-  using C1 = TileCore<2 * HID_F, HID_R, false, false, 2, 2, 2, 2>;
-  using C2 = TileCore<HID_F, HID_R, true, false, 1, 2, 2, 2>;
+  using C1 = TileCore<2 * HID_F, HID_R, false, false, 2, 2, 2, HID_S>;
+  using C2 = TileCore<HID_F, HID_R, true, false, 1, 2, 2, HID_S>;
   constexpr int MI = C2::MI, NI = C2::NI;
-  __shared__ __align__(1024) uint8_t smem[2 * C1::STAGE];
+  __shared__ __align__(1024) uint8_t smem[HID_S * C1::STAGE];
   const PadScan ps = pad_scan(a.cnt, a.E);
   RowTile t;
   int nt;
@@ -313,24 +324,22 @@ __global__ __launch_bounds__(256) void moe_grad_hidden_kernel(MoeGradArgs a, int
   f32x4_t gu[2 * MI][NI], q[MI][NI];
   zero_acc(gu);
   zero_acc(q);
+  auto along = [](int kt) { return int64_t(kt) * 128; };
   C1::run(
       smem,
       [&](int r, int c) {
         return (const uint8_t *)((r < HID_F ? Wg : Wu) + int64_t(r & (HID_F - 1)) * d) + c * 16;
       },
-      [&](int r, int c) { return (const uint8_t *)(n2 + int64_t(r < t.rows ? r : 0) * d) + c * 16; },
-      128, 128, d / 64, gu);
+      [&](int r, int c) { return (const uint8_t *)(n2 + int64_t(r) * d) + c * 16; }, along, along, d / 64, gu);
   C2::run(
       smem, [&](int k, int c) { return (const uint8_t *)(Wd + int64_t(k) * f) + c * 16; },
-      [&](int r, int c) { return (const uint8_t *)(dy + int64_t(r < t.rows ? r : 0) * d) + c * 16; },
-      int64_t(128) * f, 128, d / 64, q);
+      [&](int r, int c) { return (const uint8_t *)(dy + int64_t(r) * d) + c * 16; },
+      [&](int kt) { return int64_t(kt) * 128 * f; }, along, d / 64, q);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
 #pragma unroll
   for (int ni = 0; ni < NI; ++ni) {
-    const int r = wn * (HID_R / 2) + ni * 16 + (lane & 15);
-    const int64_t pos = t.p0 + r;
-    const bool in = r < t.rows;
-    const float p = in ? a.gate[pos] : 0.f;
+    const int64_t pos = t.p0 + wn * (HID_R / 2) + ni * 16 + (lane & 15);  // (tiles are whole: 64 rows)
+    const float p = a.gate[pos];
     float gs = 0.f;
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
@@ -341,74 +350,67 @@ __global__ __launch_bounds__(256) void moe_grad_hidden_kernel(MoeGradArgs a, int
         h[i] = hidden_grad<true>(gu[mi][ni][i], gu[MI + mi][ni][i], q[mi][ni][i], p);
         gs += h[i].gq;
       }
-      if (in) {
-        bf16 *o = (bf16 *)a.dGU + pos * (2 * f) + f0 + u;  // (f0: a multiple of 64)
-        *(uint2 *)o = make_uint2(pk_bf16(h[0].dg, h[1].dg), pk_bf16(h[2].dg, h[3].dg));
-        *(uint2 *)(o + 64) = make_uint2(pk_bf16(h[0].du, h[1].du), pk_bf16(h[2].du, h[3].du));
-        if (a.Hp)
-          *(uint2 *)((bf16 *)a.Hp + pos * f + u) =
-              make_uint2(pk_bf16(h[0].hp, h[1].hp), pk_bf16(h[2].hp, h[3].hp));
-      }
+      bf16 *o = (bf16 *)a.dGU + pos * (2 * f) + f0 + u;  // (f0: a multiple of 64)
+      *(uint2 *)o = make_uint2(pk_bf16(h[0].dg, h[1].dg), pk_bf16(h[2].dg, h[3].dg));
+      *(uint2 *)(o + 64) = make_uint2(pk_bf16(h[0].du, h[1].du), pk_bf16(h[2].du, h[3].du));
+      if (a.Hp)
+        *(uint2 *)((bf16 *)a.Hp + pos * f + u) =
+            make_uint2(pk_bf16(h[0].hp, h[1].hp), pk_bf16(h[2].hp, h[3].hp));
     }
     gs += __shfl_xor(gs, 16, 64);
     gs += __shfl_xor(gs, 32, 64);
-    if (in && lane < 16) a.gpart[pos * a.GP + (f0 / HID_F) * 2 + wm] = gs;
+    if (lane < 16) a.gpart[pos * a.GP + (f0 / HID_F) * 2 + wm] = gs;
   }
 }
 
-// ------------------------------------------------------------------ input
-constexpr int INP_M = 128, INP_R = 128;
-template <int>
-__global__ __launch_bounds__(256) void moe_grad_input_kernel(MoeGradArgs a, int nd) {
-  using C = TileCore<INP_M, INP_R, true, false, 1, 2, 2, 2>;
-  __shared__ __align__(1024) uint8_t smem[2 * C::STAGE];
+// dn of 64 columns and 64 rows over one of `splits` parts of the sum, to its plane
+// of Y (list order, nl rows a plane).
+constexpr int INP_M = 64, INP_R = 64, INP_S = 4;
+__global__ __launch_bounds__(256) void moe_grad_input_kernel(MoeGradArgs a, int nd, int splits, int64_t plane) {
+  using C = TileCore<INP_M, INP_R, true, false, 1, 2, 2, INP_S>;
+  __shared__ __align__(1024) uint8_t smem[INP_S * C::STAGE];
   const PadScan ps = pad_scan(a.cnt, a.E);
   RowTile t;
   int nt;
   row_tile<INP_R>(ps, 0, t, nt);
-  const int total = nt * nd;
+  const int total = nt * nd * splits;
   if (int(blockIdx.x) >= total) return;
-  const int L = xcd_tile(blockIdx.x, total);
+  int L = xcd_tile(blockIdx.x, total);
+  const int sp = L % splits;
+  L /= splits;
   row_tile<INP_R>(ps, L / nd, t, nt);
-  const int m0 = (L % nd) * INP_M, d = a.d, f = a.f;
+  const int m0 = (L % nd) * INP_M, d = a.d, f = a.f, steps = f / 64;
+  const int h0 = steps * sp / splits, h1 = steps * (sp + 1) / splits;  // blocks of 64 gates and 64 ups
+  const bf16 *Wg = (const bf16 *)a.Wg + (int64_t(t.e - 1) * f + h0 * 64) * d + m0;
+  const bf16 *g = (const bf16 *)a.dGU + int64_t(t.p0) * (2 * f) + h0 * 128;
+  const int64_t up = (const uint8_t *)a.Wu - (const uint8_t *)a.Wg;
   f32x4_t acc[C::MI][C::NI];
   zero_acc(acc);
-#pragma unroll 1
-  for (int half = 0; half < 2; ++half) {  // the steps of 64 gates, then those of 64 ups
-    const bf16 *W = (const bf16 *)(half ? a.Wu : a.Wg) + int64_t(t.e - 1) * f * d + m0;
-    const bf16 *g = (const bf16 *)a.dGU + int64_t(t.p0) * (2 * f) + half * 64;
-    C::run(
-        smem,
-        [&](int k, int c) {
-          return (const uint8_t *)(W + int64_t(k) * d) + (m0 + c * 8 < d ? c * 16 : 0);
-        },
-        [&](int r, int c) {
-          return (const uint8_t *)(g + int64_t(r < t.rows ? r : 0) * (2 * f)) + c * 16;
-        },
-        int64_t(128) * d, 256, f / 64, acc);
-  }
+  C::run(
+      smem, [&](int k, int c) { return (const uint8_t *)(Wg + int64_t(k) * d) + c * 16; },
+      [&](int r, int c) { return (const uint8_t *)(g + int64_t(r) * (2 * f)) + c * 16; },
+      [&](int kt) { return int64_t(kt >> 1) * 128 * d + (kt & 1) * up; },
+      [](int kt) { return int64_t(kt) * 128; }, 2 * (h1 - h0), acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
 #pragma unroll
   for (int ni = 0; ni < C::NI; ++ni) {
     const int r = wn * (INP_R / 2) + ni * 16 + (lane & 15);
-    if (r >= t.rows) continue;
+    if (r >= t.valid) continue;
+    float *y = a.Y + sp * plane + int64_t(t.l0 + r) * d + m0 + wm * (INP_M / 2) + 4 * (lane >> 4);
 #pragma unroll
-    for (int mi = 0; mi < C::MI; ++mi) {
-      const int m = m0 + wm * (INP_M / 2) + mi * 16 + 4 * (lane >> 4);
-      if (m < d) *(f32x4_t *)(a.Y + int64_t(t.p0 + r) * d + m) = acc[mi][ni];
-    }
+    for (int mi = 0; mi < C::MI; ++mi) *(f32x4_t *)(y + mi * 16) = acc[mi][ni];
   }
 }
 
-// ------------------------------------------------------------------ weight
-constexpr int WGT_M = 128, WGT_N = 128;
-template <int>
+// 128 x 128 of an expert's weight gradients (see WeightBig), written in rows of
+// 256 bytes through LDS: with few rows it is the time of the writes.
+constexpr int WGT_T = 128, WGT_S = 2;
 __global__ __launch_bounds__(256) void moe_grad_weight_kernel(MoeGradArgs a) {
-  using C = TileCore<WGT_M, WGT_N, true, true, 1, 2, 2, 2>;
-  __shared__ __align__(1024) uint8_t smem[2 * C::STAGE];
+  using C = TileCore<WGT_T, WGT_T, true, true, 1, 2, 2, WGT_S>;
+  __shared__ __align__(1024) uint8_t smem[WGT_S * C::STAGE];
   const int d = a.d, f = a.f;
-  const int md = (d + WGT_M - 1) / WGT_M, mf = (f + WGT_M - 1) / WGT_M;
-  const int t1 = md * ((2 * f + WGT_N - 1) / WGT_N), t2 = mf * ((d + WGT_N - 1) / WGT_N);
+  const int md = (d + WGT_T - 1) / WGT_T, mf = (f + WGT_T - 1) / WGT_T;
+  const int t1 = md * (2 * f / WGT_T), t2 = mf * md;  // (2 f is a multiple of 128)
   int L = xcd_tile(blockIdx.x, gridDim.x);
   const int e = L / (t1 + t2) + 1;
   L -= (e - 1) * (t1 + t2);
@@ -418,30 +420,36 @@ __global__ __launch_bounds__(256) void moe_grad_weight_kernel(MoeGradArgs a) {
   const bool down = L >= t1;  // dWd[d][f] = dy^T Hp; else [dWg; dWu] = dGU^T n2
   if (down) L -= t1;
   const int mt = down ? mf : md, M = down ? f : d, N = down ? d : 2 * f;
-  const int m0 = (L % mt) * WGT_M, n0 = (L / mt) * WGT_N;
-  const bf16 *A = (const bf16 *)(down ? a.Hp : a.n2) + int64_t(p0) * M + m0;
-  const bf16 *B = (const bf16 *)(down ? a.dy : a.dGU) + int64_t(p0) * N + n0;
-  f32x4_t acc[C::MI][C::NI];
-  zero_acc(acc);
-  C::run(
-      smem,
-      [&](int k, int c) { return (const uint8_t *)(A + int64_t(k) * M) + (m0 + c * 8 < M ? c * 16 : 0); },
-      [&](int k, int c) { return (const uint8_t *)(B + int64_t(k) * N) + (n0 + c * 8 < N ? c * 16 : 0); },
-      int64_t(128) * M, int64_t(128) * N, rows / 64, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
+  const int m0 = (L % mt) * WGT_T, n0 = (L / mt) * WGT_T;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / 2, wn = wave % 2;
+  if (rows > 0) {
+    const bf16 *A = (const bf16 *)(down ? a.Hp : a.n2) + int64_t(p0) * M + m0;
+    const bf16 *B = (const bf16 *)(down ? a.dy : a.dGU) + int64_t(p0) * N + n0;
+    f32x4_t acc[C::MI][C::NI];
+    zero_acc(acc);
+    C::run(
+        smem, [&](int k, int c) { return (const uint8_t *)(A + int64_t(k) * M) + (m0 + c * 8 < M ? c * 16 : 0); },
+        [&](int k, int c) { return (const uint8_t *)(B + int64_t(k) * N) + (n0 + c * 8 < N ? c * 16 : 0); },
+        [&](int kt) { return int64_t(kt) * 128 * M; }, [&](int kt) { return int64_t(kt) * 128 * N; }, rows / 64, acc);
 #pragma unroll
-  for (int ni = 0; ni < C::NI; ++ni) {
-    const int n = n0 + wn * (WGT_N / 2) + ni * 16 + (lane & 15);
-    if (n >= N) continue;
+    for (int ni = 0; ni < C::NI; ++ni)
+#pragma unroll
+      for (int mi = 0; mi < C::MI; ++mi) {
+        // row n of 256 bytes, its 16-byte chunks turned by the row
+        const int n = wn * 64 + ni * 16 + (lane & 15), c = wm * 8 + mi * 2 + (lane >> 5);
+        *(uint2 *)(smem + n * 256 + ((c ^ (n & 15)) << 4) + ((lane >> 4) & 1) * 8) =
+            make_uint2(pk_bf16(acc[mi][ni][0], acc[mi][ni][1]), pk_bf16(acc[mi][ni][2], acc[mi][ni][3]));
+      }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int x = 0; x < WGT_T / 16; ++x) {
+    const int r = x * 16 + (tid >> 4), c = tid & 15, n = n0 + r;
+    if (n >= N || m0 + c * 8 >= M) continue;
+    const uint4 v = rows > 0 ? *(const uint4 *)(smem + r * 256 + ((c ^ (r & 15)) << 4)) : make_uint4(0u, 0u, 0u, 0u);
     bf16 *o = (bf16 *)(down ? a.dWd : (n & 64) ? a.dWu : a.dWg) + int64_t(e - 1) * d * f +
               int64_t(down ? n : (n >> 7) * 64 + (n & 63)) * M;
-#pragma unroll
-    for (int mi = 0; mi < C::MI; ++mi) {
-      const int m = m0 + wm * (WGT_M / 2) + mi * 16 + 4 * (lane >> 4);
-      if (m < M)
-        *(uint2 *)(o + m) = make_uint2(pk_bf16(acc[mi][ni][0], acc[mi][ni][1]),
-                                       pk_bf16(acc[mi][ni][2], acc[mi][ni][3]));
-    }
+    *(uint4 *)(o + m0 + c * 8) = v;
   }
 }
 
@@ -610,14 +618,17 @@ __device__ __forceinline__ TileScan tile_scan(const int32_t *cnt, int E) {
   g.total = __builtin_amdgcn_readfirstlane(__shfl(x, 63, 64));
   return g;
 }
-// Tile t of (row tiles x ny columns), in bands within each expert.
-template <int BN>
+// Tile t of (row tiles x ny columns), in bands of BR x BC tiles within each expert: the 32
+// blocks of an XCD then read BR + BC operand slices.  (1.3B, 16384 tokens, 16 x 2 / 4 x 8,
+// us: weights 1824 / 1794, dn 1126 / 1116; 160M dn 227 / 206, gates 284 / 278; q, whose tiles are
+// shortest, 723 / 732 and 684 with 6 x 5.)
+template <int BN, int BR, int BC>
 __device__ __forceinline__ BigTile row_col_tile(const TileScan &g, int t, int ny, int &col) {
   const uint64_t m = __ballot(g.incl * ny > t);
   const int l = __ffsll((unsigned long long)m) - 1;
   const int nt = __shfl(g.nt, l, 64), first = __shfl(g.incl, l, 64) - nt;
   int i;
-  band_order(t - first * ny, nt, ny, i, col);
+  band_order<BR, BC>(t - first * ny, nt, ny, i, col);
   BigTile r;
   r.e = __builtin_amdgcn_readfirstlane(l + 1);
   r.p0 = __builtin_amdgcn_readfirstlane(__shfl(g.ps.pad, l, 64) + i * BN);
@@ -646,6 +657,7 @@ struct RowsBase {
 template <bool TWO>
 struct RowsBig : RowsBase {
   using RowsBase::RowsBase;
+  static constexpr int BR = TWO ? 4 : 6, BC = TWO ? 8 : 5;
   Src<256, true> sw;
   Src<256, false> sr;
   const uint8_t *other;  // the next stage of the matrix whose turn it is not
@@ -653,7 +665,7 @@ struct RowsBig : RowsBase {
   Frags<256, false, false, 8> fb_;
   __device__ __forceinline__ BigTile tile(const TileScan &g, int l, int total) const {
     int by;
-    BigTile t = row_col_tile<BN>(g, xcd_tile(l, total), ny, by);
+    BigTile t = row_col_tile<BN, BR, BC>(g, xcd_tile(l, total), ny, by);
     t.m0 = by * 256;
     t.n0 = 0;
     t.nk = TWO ? a.f / 32 : a.d / 64;
@@ -717,13 +729,14 @@ struct RowsBig : RowsBase {
 // hidden gradients: A blocks 0..3 are a wave's gates, 4..7 its ups.
 struct GateUpBig : RowsBase {
   using RowsBase::RowsBase;
+  static constexpr int BR = 4, BC = 8;
   Src<128, false, true> sg, su;
   Src<256, false> sr;
   Frags<128, false, true, 4> fg, fu;
   Frags<256, false, false, 8> fb_;
   __device__ __forceinline__ BigTile tile(const TileScan &g, int l, int total) const {
     int by;
-    BigTile t = row_col_tile<BN>(g, xcd_tile(l, total), ny, by);
+    BigTile t = row_col_tile<BN, BR, BC>(g, xcd_tile(l, total), ny, by);
     t.m0 = by * 128;
     t.n0 = 0;
     t.nk = a.d / 64;
@@ -874,9 +887,9 @@ struct WeightBig {
     t.down = x >= t1;
     if (t.down) {
       x -= t1;
-      band_order(x, md, mf, j, i);
+      band_order<4, 8>(x, md, mf, j, i);
     } else {
-      band_order(x, t1 / md, md, j, i);
+      band_order<4, 8>(x, t1 / md, md, j, i);
     }
     t.e = e + 1;
     t.p0 = __builtin_amdgcn_readfirstlane(__shfl(g.ps.pad, e, 64));
@@ -1232,8 +1245,9 @@ template <typename T, int RR>
 __global__ __launch_bounds__(256) void moe_grad_token_kernel(
     const T *__restrict__ x, const T *dx, const T *__restrict__ g, const float *__restrict__ Y,
     const int32_t *__restrict__ eidx, const int32_t *__restrict__ row_of,
-    const float *__restrict__ gpart, int GP, int N, int k, int d, float eps, T *dxt,
-    float *__restrict__ g_gate, float *__restrict__ part) {
+    const int32_t *__restrict__ yrow_of, int planes, int64_t plane, const float *__restrict__ gpart, int GP,
+    int N, int k, int d, float eps, T *dxt, float *__restrict__ g_gate, float *__restrict__ part,
+    T *__restrict__ dg2) {
   constexpr int RN = RR > 0 ? RR : 1;
   __shared__ __align__(16) float red[RR > 0 ? 4 : 1][RR > 0 ? 512 * RR : 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1248,16 +1262,19 @@ __global__ __launch_bounds__(256) void moe_grad_token_kernel(
     for (int c = lane * 8; c < d; c += 512) store8(pr + c, &sum[0][0]);
   for (int i = blockIdx.x * 4 + wave; i < N; i += gridDim.x * 4) {
     const T *xr = x + int64_t(i) * d;
-    const int32_t *ei = eidx + int64_t(i) * k, *ro = row_of + int64_t(i) * k;
+    const int32_t *ei = eidx + int64_t(i) * k, *ro = row_of + int64_t(i) * k, *yo = yrow_of + int64_t(i) * k;
     auto dn8 = [&](int c, float *dn) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) dn[j] = 0.f;
       for (int s = 0; s < k; ++s) {
         if (ei[s] == 0) continue;
-        float y[8];
-        load8(Y + int64_t(ro[s]) * d + c, y);
+        const float *yr = Y + int64_t(yo[s]) * d + c;
+        for (int p = 0; p < planes; ++p) {  // the parts of a split sum, in order
+          float y[8];
+          load8(yr + p * plane, y);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) dn[j] += y[j];
+          for (int j = 0; j < 8; ++j) dn[j] += y[j];
+        }
       }
     };
     float w[RN][8], dn[RN][8];
@@ -1322,12 +1339,17 @@ __global__ __launch_bounds__(256) void moe_grad_token_kernel(
     }
   }
   if constexpr (RR > 0) {
-    if (!part) return;
+    if (!part && !dg2) return;
 #pragma unroll
     for (int q = 0; q < RN; ++q) store8(&red[wave][512 * q + lane * 8], sum[q]);
     __syncthreads();
-    for (int c = threadIdx.x; c < d; c += 256)
-      part[int64_t(blockIdx.x) * d + c] = ((red[0][c] + red[1][c]) + red[2][c]) + red[3][c];
+    for (int c = threadIdx.x; c < d; c += 256) {
+      const float v = ((red[0][c] + red[1][c]) + red[2][c]) + red[3][c];
+      if (dg2)  // (the only block)
+        Act<T>::st(dg2, c, v);
+      else
+        part[int64_t(blockIdx.x) * d + c] = v;
+    }
   }
 }
 
@@ -1381,6 +1403,19 @@ int moe_grad_part_rows(const triroute_cfg &cfg, int N) {
   return token_blocks(N) * (cfg.d_model <= 2048 ? 1 : 4);
 }
 
+// bf16: whether the experts have rows enough for the 256-row tiles (r: rows of an
+// expert when the router spreads its options evenly).
+static bool big_tiles(const triroute_cfg &cfg, int N) {
+  return cfg.act == TRIROUTE_BF16 && int64_t(N) * cfg.top_k / (cfg.n_experts + 1) >= 128;
+}
+// Parts of the sum of dn for few rows, so that the stream of the weights has about
+// two blocks a CU: each of at least 4 blocks of 64 units.
+int moe_grad_splits(const triroute_cfg &cfg, int N) {
+  if (cfg.act != TRIROUTE_BF16 || big_tiles(cfg, N)) return 1;
+  const int Nk = N * cfg.top_k, tiles = (Nk / INP_R + std::min(cfg.n_experts, Nk)) * (cfg.d_model / INP_M);
+  return std::max(1, std::min({(512 + tiles - 1) / tiles, cfg.d_ff / 64 / 4, 16}));
+}
+
 template <typename T>
 static hipError_t backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, hipStream_t st) {
   const int E = cfg.n_experts, k = cfg.top_k, d = cfg.d_model, f = cfg.d_ff, Nk = N * k;
@@ -1396,10 +1431,12 @@ static hipError_t backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, 
   a.GP = moe_grad_gate_parts(cfg);
   moe_grad_rows_kernel<T><<<dim3(unsigned((rows + 3) / 4)), 256, 0, st>>>(
       (const T *)j.xt, (const T *)j.dx, (const T *)j.g2, j.egate, j.cmp.exp_cnt, j.cmp.exp_rows, E, k, d,
-      cfg.rms_eps, (T *)j.n2, (T *)j.dy, j.gate, j.row_of);
+      cfg.rms_eps, (T *)j.n2, (T *)j.dy, j.gate, j.row_of, j.list_of);
+  const int32_t *yrow_of = j.row_of;
+  int splits = 1;
+  const int64_t plane = int64_t(Nk) * d;
   if constexpr (sizeof(T) == 2) {
-    const int r = Nk / (E + 1);  // rows of an expert when the router spreads its options evenly
-    if (r >= 128) {
+    if (big_tiles(cfg, N)) {
       const int cu = cu_count();
       a.GP = f / 64;
       BigShape sh{};
@@ -1418,33 +1455,35 @@ static hipError_t backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, 
         moe_grad_big_kernel<WeightBig><<<unsigned(std::min<int64_t>(int64_t(E) * (sh.t1 + sh.t2), cu)), 256, 0, st>>>(
             a, sh);
     } else {
-      const int nf = f / HID_F, nd = (d + INP_M - 1) / INP_M;
-      const int rt = Nk / HID_R + E;  // row tiles at most
-      moe_grad_hidden_kernel<0><<<unsigned(rt) * nf, 256, 0, st>>>(a, nf);
-      moe_grad_input_kernel<0><<<unsigned(rt) * nd, 256, 0, st>>>(a, nd);
+      const int nf = f / HID_F, nd = d / INP_M, rt = Nk / 64 + std::min(E, Nk);  // row tiles at most
+      splits = moe_grad_splits(cfg, N);
+      yrow_of = j.list_of;
+      moe_grad_hidden_kernel<<<unsigned(rt) * nf, 256, 0, st>>>(a, nf);
+      moe_grad_input_kernel<<<unsigned(rt) * nd * splits, 256, 0, st>>>(a, nd, splits, plane);
       if (a.Hp) {
-        const int t1 = (d + WGT_M - 1) / WGT_M * ((2 * f + WGT_N - 1) / WGT_N);
-        const int t2 = (f + WGT_M - 1) / WGT_M * ((d + WGT_N - 1) / WGT_N);
-        moe_grad_weight_kernel<0><<<unsigned(E) * (t1 + t2), 256, 0, st>>>(a);
+        const int md = (d + WGT_T - 1) / WGT_T, mf = (f + WGT_T - 1) / WGT_T;
+        moe_grad_weight_kernel<<<unsigned(E) * (md * (2 * f / WGT_T) + mf * md), 256, 0, st>>>(a);
       }
     }
   } else {
-    const int nf = f / F32_T, nd = d / F32_T, rt = Nk / F32_T + E;
+    const int nf = f / F32_T, nd = d / F32_T, rt = Nk / F32_T + std::min(E, Nk);
     moe_grad_hidden_f32_kernel<<<unsigned(rt) * nf, 256, 0, st>>>(a, nf);
     moe_grad_input_f32_kernel<<<unsigned(rt) * nd, 256, 0, st>>>(a, nd);
     if (a.Hp) moe_grad_weight_f32_kernel<<<unsigned(E) * nd * nf * 3, 256, 0, st>>>(a);
   }
   const int prows = moe_grad_part_rows(cfg, N);
+  const bool direct = token_blocks(N) == 1 && d <= 2048;  // one block: its dg2 is the sum
   auto token = [&](auto rr) {
     moe_grad_token_kernel<T, decltype(rr)::value><<<token_blocks(N), 256, 0, st>>>(
-        (const T *)j.xt, (const T *)j.dx, (const T *)j.g2, j.Y, j.eidx, j.row_of, j.gpart, a.GP, N, k, d,
-        cfg.rms_eps, (T *)j.out.dxt, j.out.g_gate, j.out.dg2 ? j.part : nullptr);
+        (const T *)j.xt, (const T *)j.dx, (const T *)j.g2, j.Y, j.eidx, j.row_of, yrow_of, splits, plane, j.gpart,
+        a.GP, N, k, d, cfg.rms_eps, (T *)j.out.dxt, j.out.g_gate, j.out.dg2 && !direct ? j.part : nullptr,
+        direct ? (T *)j.out.dg2 : nullptr);
   };
   if (d <= 512) token(std::integral_constant<int, 1>{});
   else if (d <= 1024) token(std::integral_constant<int, 2>{});
   else if (d <= 2048) token(std::integral_constant<int, 4>{});
   else token(std::integral_constant<int, 0>{});
-  if (j.out.dg2)
+  if (j.out.dg2 && !direct)
     moe_grad_g2_kernel<T><<<d / 16, 1024, 0, st>>>(j.part, prows, d, (T *)j.out.dg2);
   return hipGetLastError();
 }
