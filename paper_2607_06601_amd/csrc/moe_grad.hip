@@ -160,29 +160,51 @@ __device__ __forceinline__ int rswz(int r, int c) {
     return swz<8>(r, c);
 }
 
-// acc += A B^T over nk steps of 64, A of MR and B of NR rows, WM x WN waves, S
-// stages in LDS.  AT / BT: the operand lies as K rows of MR / NR columns.  Sources are
-// given as functions (row, 16-byte chunk of its K step) or, transposed, (K row of
-// the step, 16-byte chunk of its columns) -> address at step 0, and step -> bytes
-// from there.  SPLIT 2: a wave's rows are taken in halves from
-// the two halves of A (the units' gates and ups).
-template <int MR, int NR, bool AT, bool BT, int SPLIT, int WM, int WN, int S>
+// acc += A B^T over nk steps of 128 bytes of the sum (64 bf16 or 32 fp32), A of MR
+// and B of NR rows, WM x WN waves (of which this is number `wave`; nk + 1 barriers of the
+// block, for S 1 2 nk), S stages in LDS.  AT / BT: the operand lies as K rows of MR / NR columns.
+// Sources are given as functions (row, 16-byte chunk of its K step) or,
+// transposed, (K row of the step, 16-byte chunk of its columns) -> address at
+// step 0, and step -> bytes from there.  SPLIT 2: a wave's rows are taken in
+// halves from the two halves of A (the units' gates and ups).
+// fp32: of 16 sum indices lane group g holds 4 g .. 4 g + 3, and MFMA i (16x16x4) takes
+// component i of both operands.
+template <typename T, int MR, int NR, bool AT, bool BT, int SPLIT, int WM, int WN, int S>
 struct TileCore {
+  static constexpr bool F = sizeof(T) == 4;
+  static constexpr int KB = 128 / int(sizeof(T));  // sum indices of a step
   static constexpr int NW = WM * WN, MI = MR / WM / 16, NI = NR / WN / 16;
   static constexpr int ABYTES = MR * 128, STAGE = (MR + NR) * 128, IPW = STAGE / 1024 / NW;
   static_assert(STAGE % (1024 * NW) == 0, "whole transfers");
+  using Frag = typename std::conditional<F, f32x4_t, bf16x8_t>::type;  // 16 rows x 32 (fp32: 16) indices
+
+  // Source chunk of 16-byte chunk c of K row k in a stage of a transposed operand of R columns.
+  template <int R>
+  __device__ static __forceinline__ int tchunk(int k, int c) {
+    if constexpr (F)
+      return c ^ (((k >> 2) & 3) << 2);  // the lane groups' K rows 4 g + i in different banks
+    else
+      return tswz<R>(k, c >> 1) * 2 + (c & 1);
+  }
 
   template <int R, bool TR>
-  __device__ static __forceinline__ bf16x8_t frag(const uint8_t *base, int row0, int ks, int lane) {
+  __device__ static __forceinline__ Frag frag(const uint8_t *base, int row0, int ks, int lane) {
+    const int n = lane & 15, g = lane >> 4;
     if constexpr (!TR) {
-      const int r = row0 + (lane & 15), ch = ks * 4 + (lane >> 4);
-      return *(const bf16x8_t *)(base + r * 128 + (swz<8>(r, ch) << 4));
+      const int r = row0 + n;
+      return *(const Frag *)(base + r * 128 + (swz<8>(r, ks * 4 + g) << 4));
+    } else if constexpr (F) {
+      f32x4_t v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        v[i] = *(const float *)(base + (16 * ks + 4 * g + i) * (4 * R) + (((row0 >> 4) ^ g) * 16 + n) * 4);
+      return v;
     } else {
       typedef __attribute__((address_space(3))) s16x4_t *P;
       s16x4_t h[2];
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const int k = 32 * ks + 8 * (lane >> 4) + 4 * x + ((lane & 15) >> 2);
+        const int k = 32 * ks + 8 * g + 4 * x + (n >> 2);
         h[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
             (P)(base + k * (2 * R) + tswz<R>(k, row0 >> 4) * 32 + (lane & 3) * 8));
       }
@@ -193,10 +215,9 @@ struct TileCore {
   }
 
   template <class FA, class FB, class SA, class SB>
-  __device__ static __forceinline__ void run(uint8_t *smem, FA &&fa, FB &&fb, SA &&astep, SB &&bstep, int nk,
-                                             f32x4_t (&acc)[MI][NI]) {
+  __device__ static __forceinline__ void run(uint8_t *smem, int wave, FA &&fa, FB &&fb, SA &&astep, SB &&bstep,
+                                             int nk, f32x4_t (&acc)[MI][NI]) {
     const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / WN, wn = wave % WN;
     const uint8_t *src[IPW];
 #pragma unroll
@@ -205,16 +226,16 @@ struct TileCore {
       const bool isa = (wave * IPW + j) * 1024 < ABYTES;
       if (isa) {
         if constexpr (AT) {
-          const int k = p / (MR / 8), c = p % (MR / 8);
-          src[j] = fa(k, tswz<MR>(k, c >> 1) * 2 + (c & 1));
+          constexpr int CR = MR * int(sizeof(T)) / 16;  // chunks a K row
+          src[j] = fa(p / CR, tchunk<MR>(p / CR, p % CR));
         } else {
           src[j] = fa(p / 8, swz<8>(p / 8, p % 8));
         }
       } else {
         p -= ABYTES / 16;
         if constexpr (BT) {
-          const int k = p / (NR / 8), c = p % (NR / 8);
-          src[j] = fb(k, tswz<NR>(k, c >> 1) * 2 + (c & 1));
+          constexpr int CR = NR * int(sizeof(T)) / 16;
+          src[j] = fb(p / CR, tchunk<NR>(p / CR, p % CR));
         } else {
           src[j] = fb(p / 8, swz<8>(p / 8, p % 8));
         }
@@ -233,29 +254,52 @@ struct TileCore {
     for (int s0 = 0; s0 < S - 1; ++s0)
       if (s0 < nk) issue(s0, s0);
     for (int kt = 0; kt < nk; ++kt) {
-      wait_stages<IPW, S>(min(S - 2, nk - 1 - kt));
-      __syncthreads();  // every wave's part of stage kt is in; stage kt - 1 is free
-      if (kt + S - 1 < nk) issue(kt + S - 1, (kt + S - 1) % S);
+      if constexpr (S == 1) {
+        issue(kt, 0);
+        wait_vm<0>();
+        __syncthreads();
+      } else {
+        wait_stages<IPW, S>(min(S - 2, nk - 1 - kt));
+        __syncthreads();  // every wave's part of stage kt is in; stage kt - 1 is free
+        if (kt + S - 1 < nk) issue(kt + S - 1, (kt + S - 1) % S);
+      }
       const uint8_t *As = smem + (kt % S) * STAGE, *Bs = As + ABYTES;
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
-        bf16x8_t b[NI];
+        Frag b[NI];
 #pragma unroll
         for (int ni = 0; ni < NI; ++ni) b[ni] = frag<NR, BT>(Bs, wn * (NR / WN) + ni * 16, ks, lane);
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi) {
           constexpr int H = MI / SPLIT;  // 16-row blocks of a wave in each part of A
           const int row0 = (mi / H) * (MR / SPLIT) + wm * (MR / SPLIT / WM) + (mi % H) * 16;
-          const bf16x8_t a = frag<MR, AT>(As, row0, ks, lane);
+          const Frag a = frag<MR, AT>(As, row0, ks, lane);
+          if constexpr (F) {
 #pragma unroll
-          for (int ni = 0; ni < NI; ++ni)
-            acc[mi][ni] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[ni], acc[mi][ni], 0, 0, 0);
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int ni = 0; ni < NI; ++ni)
+                acc[mi][ni] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[ni][i], acc[mi][ni], 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int ni = 0; ni < NI; ++ni)
+              acc[mi][ni] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[ni], acc[mi][ni], 0, 0, 0);
+          }
         }
       }
+      if (S == 1 && kt + 1 < nk) __syncthreads();
     }
     __syncthreads();  // every wave is done with the stages
   }
 };
+
+// 4 consecutive results to memory in the tensor's type.
+__device__ __forceinline__ void put4(bf16 *o, float x, float y, float z, float w) {
+  *(uint2 *)o = make_uint2(pk_bf16(x, y), pk_bf16(z, w));
+}
+__device__ __forceinline__ void put4(float *o, float x, float y, float z, float w) {
+  *(f32x4_t *)o = f32x4_t{x, y, z, w};
+}
 
 template <int MI, int NI>
 __device__ __forceinline__ void zero_acc(f32x4_t (&acc)[MI][NI]) {
@@ -268,8 +312,8 @@ __device__ __forceinline__ void zero_acc(f32x4_t (&acc)[MI][NI]) {
 struct MoeGradArgs {
   const void *Wg, *Wu, *Wd;
   const void *n2, *dy;  // [rows][d]
-  // dGU [rows][2 d_ff]: bf16: 64 dG, the same units' dU, the next 64 dG, ..; fp32: all dG,
-  // then all dU.  Hp [rows][d_ff]: p s G U (NULL: not wanted)
+  // dGU [rows][2 d_ff]: 64 dG, the same units' dU, the next 64 dG, ..; Hp [rows][d_ff]:
+  // p s G U (NULL: not wanted)
   void *dGU, *Hp;
   const float *gate;    // [rows]
   float *Y, *gpart;     // [rows][d]; [rows][GP]
@@ -295,18 +339,23 @@ __device__ __forceinline__ Hidden hidden_grad(float G, float U, float q, float p
   return r;
 }
 
-// ------------------------------------------------- few rows: streaming weights
+// ------------------------------------------ few rows, and fp32: small tiles
 // With few rows an expert the products read each weight about once and the time
-// is that of the stream: narrow tiles over all CUs, three stages in flight ahead of
-// the one in use.
+// is that of the stream: narrow tiles over all CUs, stages in flight ahead of the one
+// in use.  The fp32 products, bound by the fp32 MFMA rate, run on the same tiles,
+// several blocks a CU.
 
-// [G; U; q] of 64 units and 64 rows.
-constexpr int HID_F = 64, HID_R = 64, HID_S = 4;
-__global__ __launch_bounds__(256) void moe_grad_hidden_kernel(MoeGradArgs a, int nf) {
-  using C1 = TileCore<2 * HID_F, HID_R, false, false, 2, 2, 2, HID_S>;
-  using C2 = TileCore<HID_F, HID_R, true, false, 1, 2, 2, HID_S>;
-  constexpr int MI = C2::MI, NI = C2::NI;
-  __shared__ __align__(1024) uint8_t smem[HID_S * C1::STAGE];
+// [G; U; q] of 64 units and 64 rows: four waves make G and U while four make q, over
+// the same number of steps (and barriers), and hand it over in LDS.
+// (160M, 1 token, 64 tiles: two stages 14.2 us, three 12.0; 410M, 333 tokens, 704 tiles, two
+// blocks a CU with two stages 46 us, one with three 50.)
+constexpr int HID_F = 64, HID_R = 64;
+template <typename T, int HID_S>
+__global__ __launch_bounds__(512) void moe_grad_hidden_kernel(MoeGradArgs a, int nf) {
+  using C1 = TileCore<T, 2 * HID_F, HID_R, false, false, 2, 2, 2, HID_S>;
+  using C2 = TileCore<T, HID_F, HID_R, true, false, 1, 2, 2, HID_S>;
+  constexpr int MI = C2::MI, NI = C2::NI, ES = sizeof(T);
+  __shared__ __align__(1024) uint8_t smem[HID_S * (C1::STAGE + C2::STAGE)];
   const PadScan ps = pad_scan(a.cnt, a.E);
   RowTile t;
   int nt;
@@ -316,26 +365,34 @@ __global__ __launch_bounds__(256) void moe_grad_hidden_kernel(MoeGradArgs a, int
   const int L = xcd_tile(blockIdx.x, total);
   row_tile<HID_R>(ps, L / nf, t, nt);
   const int f0 = (L % nf) * HID_F;
-  const int d = a.d, f = a.f;
-  const bf16 *Wg = (const bf16 *)a.Wg + (int64_t(t.e - 1) * f + f0) * d;
-  const bf16 *Wu = (const bf16 *)a.Wu + (int64_t(t.e - 1) * f + f0) * d;
-  const bf16 *Wd = (const bf16 *)a.Wd + int64_t(t.e - 1) * d * f + f0;
-  const bf16 *n2 = (const bf16 *)a.n2 + int64_t(t.p0) * d, *dy = (const bf16 *)a.dy + int64_t(t.p0) * d;
-  f32x4_t gu[2 * MI][NI], q[MI][NI];
-  zero_acc(gu);
-  zero_acc(q);
+  const int d = a.d, f = a.f, steps = d / C1::KB;
+  const int lane = threadIdx.x & 63, w8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = w8 & 3, wm = wave / 2, wn = wave % 2;
   auto along = [](int kt) { return int64_t(kt) * 128; };
+  f32x4_t(*qs)[64] = (f32x4_t(*)[64])(smem + HID_S * C1::STAGE) + wave * MI * NI;  // [block][lane]
+  if (w8 >= 4) {
+    const T *Wd = (const T *)a.Wd + int64_t(t.e - 1) * d * f + f0, *dy = (const T *)a.dy + int64_t(t.p0) * d;
+    f32x4_t q[MI][NI];
+    zero_acc(q);
+    C2::run(
+        smem + HID_S * C1::STAGE, wave, [&](int k, int c) { return (const uint8_t *)(Wd + int64_t(k) * f) + c * 16; },
+        [&](int r, int c) { return (const uint8_t *)(dy + int64_t(r) * d) + c * 16; },
+        [&](int kt) { return int64_t(kt) * (C2::KB * ES) * f; }, along, steps, q);
+#pragma unroll
+    for (int i = 0; i < MI * NI; ++i) qs[i][lane] = q[i / NI][i % NI];
+    __syncthreads();
+    return;
+  }
+  const uint8_t *Wg = (const uint8_t *)((const T *)a.Wg + (int64_t(t.e - 1) * f + f0) * d);
+  const int64_t up = (const uint8_t *)a.Wu - (const uint8_t *)a.Wg;
+  const T *n2 = (const T *)a.n2 + int64_t(t.p0) * d;
+  f32x4_t gu[2 * MI][NI];
+  zero_acc(gu);
   C1::run(
-      smem,
-      [&](int r, int c) {
-        return (const uint8_t *)((r < HID_F ? Wg : Wu) + int64_t(r & (HID_F - 1)) * d) + c * 16;
-      },
-      [&](int r, int c) { return (const uint8_t *)(n2 + int64_t(r) * d) + c * 16; }, along, along, d / 64, gu);
-  C2::run(
-      smem, [&](int k, int c) { return (const uint8_t *)(Wd + int64_t(k) * f) + c * 16; },
-      [&](int r, int c) { return (const uint8_t *)(dy + int64_t(r) * d) + c * 16; },
-      [&](int kt) { return int64_t(kt) * 128 * f; }, along, d / 64, q);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
+      smem, wave,
+      [&](int r, int c) { return Wg + (r / HID_F) * up + int64_t(r % HID_F) * ES * d + c * 16; },
+      [&](int r, int c) { return (const uint8_t *)(n2 + int64_t(r) * d) + c * 16; }, along, along, steps, gu);
+  __syncthreads();  // q is there
 #pragma unroll
   for (int ni = 0; ni < NI; ++ni) {
     const int64_t pos = t.p0 + wn * (HID_R / 2) + ni * 16 + (lane & 15);  // (tiles are whole: 64 rows)
@@ -344,18 +401,17 @@ __global__ __launch_bounds__(256) void moe_grad_hidden_kernel(MoeGradArgs a, int
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
       const int u = f0 + wm * (HID_F / 2) + mi * 16 + 4 * (lane >> 4);
+      const f32x4_t q = qs[mi * NI + ni][lane];
       Hidden h[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        h[i] = hidden_grad<true>(gu[mi][ni][i], gu[MI + mi][ni][i], q[mi][ni][i], p);
+        h[i] = hidden_grad<ES == 2>(gu[mi][ni][i], gu[MI + mi][ni][i], q[i], p);
         gs += h[i].gq;
       }
-      bf16 *o = (bf16 *)a.dGU + pos * (2 * f) + f0 + u;  // (f0: a multiple of 64)
-      *(uint2 *)o = make_uint2(pk_bf16(h[0].dg, h[1].dg), pk_bf16(h[2].dg, h[3].dg));
-      *(uint2 *)(o + 64) = make_uint2(pk_bf16(h[0].du, h[1].du), pk_bf16(h[2].du, h[3].du));
-      if (a.Hp)
-        *(uint2 *)((bf16 *)a.Hp + pos * f + u) =
-            make_uint2(pk_bf16(h[0].hp, h[1].hp), pk_bf16(h[2].hp, h[3].hp));
+      T *o = (T *)a.dGU + pos * (2 * f) + f0 + u;  // (f0: a multiple of 64)
+      put4(o, h[0].dg, h[1].dg, h[2].dg, h[3].dg);
+      put4(o + 64, h[0].du, h[1].du, h[2].du, h[3].du);
+      if (a.Hp) put4((T *)a.Hp + pos * f + u, h[0].hp, h[1].hp, h[2].hp, h[3].hp);
     }
     gs += __shfl_xor(gs, 16, 64);
     gs += __shfl_xor(gs, 32, 64);
@@ -364,10 +420,12 @@ __global__ __launch_bounds__(256) void moe_grad_hidden_kernel(MoeGradArgs a, int
 }
 
 // dn of 64 columns and 64 rows over one of `splits` parts of the sum, to its plane
-// of Y (list order, nl rows a plane).
-constexpr int INP_M = 64, INP_R = 64, INP_S = 4;
+// of Y (list order).
+constexpr int INP_M = 64, INP_R = 64;
+template <typename T, int INP_S>
 __global__ __launch_bounds__(256) void moe_grad_input_kernel(MoeGradArgs a, int nd, int splits, int64_t plane) {
-  using C = TileCore<INP_M, INP_R, true, false, 1, 2, 2, INP_S>;
+  using C = TileCore<T, INP_M, INP_R, true, false, 1, 2, 2, INP_S>;
+  constexpr int ES = sizeof(T), SPB = 64 / C::KB;  // steps of 64 gates (ups)
   __shared__ __align__(1024) uint8_t smem[INP_S * C::STAGE];
   const PadScan ps = pad_scan(a.cnt, a.E);
   RowTile t;
@@ -379,19 +437,23 @@ __global__ __launch_bounds__(256) void moe_grad_input_kernel(MoeGradArgs a, int 
   const int sp = L % splits;
   L /= splits;
   row_tile<INP_R>(ps, L / nd, t, nt);
-  const int m0 = (L % nd) * INP_M, d = a.d, f = a.f, steps = f / 64;
-  const int h0 = steps * sp / splits, h1 = steps * (sp + 1) / splits;  // blocks of 64 gates and 64 ups
-  const bf16 *Wg = (const bf16 *)a.Wg + (int64_t(t.e - 1) * f + h0 * 64) * d + m0;
-  const bf16 *g = (const bf16 *)a.dGU + int64_t(t.p0) * (2 * f) + h0 * 128;
+  const int m0 = (L % nd) * INP_M, d = a.d, f = a.f, blocks = f / 64;
+  const int h0 = int(int64_t(blocks) * sp / splits), h1 = int(int64_t(blocks) * (sp + 1) / splits);
+  const T *Wg = (const T *)a.Wg + (int64_t(t.e - 1) * f + h0 * 64) * d + m0;
+  const T *g = (const T *)a.dGU + int64_t(t.p0) * (2 * f) + h0 * 128;
   const int64_t up = (const uint8_t *)a.Wu - (const uint8_t *)a.Wg;
   f32x4_t acc[C::MI][C::NI];
   zero_acc(acc);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / 2, wn = wave % 2;
   C::run(
-      smem, [&](int k, int c) { return (const uint8_t *)(Wg + int64_t(k) * d) + c * 16; },
+      smem, wave, [&](int k, int c) { return (const uint8_t *)(Wg + int64_t(k) * d) + c * 16; },
       [&](int r, int c) { return (const uint8_t *)(g + int64_t(r) * (2 * f)) + c * 16; },
-      [&](int kt) { return int64_t(kt >> 1) * 128 * d + (kt & 1) * up; },
-      [](int kt) { return int64_t(kt) * 128; }, 2 * (h1 - h0), acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
+      [&](int kt) {  // 64 rows of Wg, the same of Wu, the next of Wg ..
+        const int x = kt / SPB;
+        return int64_t((x >> 1) * 64 + (kt % SPB) * C::KB) * ES * d + (x & 1) * up;
+      },
+      [](int kt) { return int64_t(kt) * 128; }, 2 * SPB * (h1 - h0), acc);
 #pragma unroll
   for (int ni = 0; ni < C::NI; ++ni) {
     const int r = wn * (INP_R / 2) + ni * 16 + (lane & 15);
@@ -402,11 +464,14 @@ __global__ __launch_bounds__(256) void moe_grad_input_kernel(MoeGradArgs a, int 
   }
 }
 
-// 128 x 128 of an expert's weight gradients (see WeightBig), written in rows of
-// 256 bytes through LDS: with few rows it is the time of the writes.
-constexpr int WGT_T = 128, WGT_S = 2;
-__global__ __launch_bounds__(256) void moe_grad_weight_kernel(MoeGradArgs a) {
-  using C = TileCore<WGT_T, WGT_T, true, true, 1, 2, 2, WGT_S>;
+// 128 x 128 of an expert's weight gradients (see WeightBig).  bf16: written in rows of
+// 256 bytes through LDS (with few rows it is the time of the writes; one stage and four
+// blocks a CU: 160M, 1 token 17.4 us, three blocks 20.4; 410M, 333 tokens 39.5, 45.0).
+constexpr int WGT_T = 128;
+template <typename T, int WGT_S>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) void moe_grad_weight_kernel(MoeGradArgs a) {
+  using C = TileCore<T, WGT_T, WGT_T, true, true, 1, 2, 2, WGT_S>;
+  constexpr int ES = sizeof(T), EC = 16 / ES;  // elements of a chunk
   __shared__ __align__(1024) uint8_t smem[WGT_S * C::STAGE];
   const int d = a.d, f = a.f;
   const int md = (d + WGT_T - 1) / WGT_T, mf = (f + WGT_T - 1) / WGT_T;
@@ -421,35 +486,47 @@ __global__ __launch_bounds__(256) void moe_grad_weight_kernel(MoeGradArgs a) {
   if (down) L -= t1;
   const int mt = down ? mf : md, M = down ? f : d, N = down ? d : 2 * f;
   const int m0 = (L % mt) * WGT_T, n0 = (L / mt) * WGT_T;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / 2, wn = wave % 2;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / 2, wn = wave % 2;
+  // row n of the tile's matrix: of dWd, or 64 units of dWg, the same of dWu, ..
+  auto out_row = [&](int n) {
+    T *o = (T *)(down ? a.dWd : (n & 64) ? a.dWu : a.dWg) + int64_t(e - 1) * d * f;
+    return o + int64_t(down ? n : (n >> 7) * 64 + (n & 63)) * M + m0;
+  };
   if (rows > 0) {
-    const bf16 *A = (const bf16 *)(down ? a.Hp : a.n2) + int64_t(p0) * M + m0;
-    const bf16 *B = (const bf16 *)(down ? a.dy : a.dGU) + int64_t(p0) * N + n0;
+    const T *A = (const T *)(down ? a.Hp : a.n2) + int64_t(p0) * M + m0;
+    const T *B = (const T *)(down ? a.dy : a.dGU) + int64_t(p0) * N + n0;
     f32x4_t acc[C::MI][C::NI];
     zero_acc(acc);
     C::run(
-        smem, [&](int k, int c) { return (const uint8_t *)(A + int64_t(k) * M) + (m0 + c * 8 < M ? c * 16 : 0); },
-        [&](int k, int c) { return (const uint8_t *)(B + int64_t(k) * N) + (n0 + c * 8 < N ? c * 16 : 0); },
-        [&](int kt) { return int64_t(kt) * 128 * M; }, [&](int kt) { return int64_t(kt) * 128 * N; }, rows / 64, acc);
+        smem, wave, [&](int k, int c) { return (const uint8_t *)(A + int64_t(k) * M) + (m0 + c * EC < M ? c * 16 : 0); },
+        [&](int k, int c) { return (const uint8_t *)(B + int64_t(k) * N) + (n0 + c * EC < N ? c * 16 : 0); },
+        [&](int kt) { return int64_t(kt) * 128 * M; }, [&](int kt) { return int64_t(kt) * 128 * N; }, rows / C::KB,
+        acc);
 #pragma unroll
     for (int ni = 0; ni < C::NI; ++ni)
 #pragma unroll
       for (int mi = 0; mi < C::MI; ++mi) {
-        // row n of 256 bytes, its 16-byte chunks turned by the row
-        const int n = wn * 64 + ni * 16 + (lane & 15), c = wm * 8 + mi * 2 + (lane >> 5);
-        *(uint2 *)(smem + n * 256 + ((c ^ (n & 15)) << 4) + ((lane >> 4) & 1) * 8) =
-            make_uint2(pk_bf16(acc[mi][ni][0], acc[mi][ni][1]), pk_bf16(acc[mi][ni][2], acc[mi][ni][3]));
+        const int n = wn * 64 + ni * 16 + (lane & 15), m = wm * 64 + mi * 16 + 4 * (lane >> 4);
+        const f32x4_t v = acc[mi][ni];
+        if constexpr (ES == 4) {
+          if (n0 + n < N && m0 + m < M) put4(out_row(n0 + n) + m, v[0], v[1], v[2], v[3]);
+        } else {
+          // row n of 256 bytes, its 16-byte chunks turned by the row
+          put4((T *)(smem + n * 256 + (((m >> 3) ^ (n & 15)) << 4) + (m & 4) * 2), v[0], v[1], v[2], v[3]);
+        }
       }
+    if constexpr (ES == 4) return;
     __syncthreads();
   }
 #pragma unroll
-  for (int x = 0; x < WGT_T / 16; ++x) {
-    const int r = x * 16 + (tid >> 4), c = tid & 15, n = n0 + r;
-    if (n >= N || m0 + c * 8 >= M) continue;
-    const uint4 v = rows > 0 ? *(const uint4 *)(smem + r * 256 + ((c ^ (r & 15)) << 4)) : make_uint4(0u, 0u, 0u, 0u);
-    bf16 *o = (bf16 *)(down ? a.dWd : (n & 64) ? a.dWu : a.dWg) + int64_t(e - 1) * d * f +
-              int64_t(down ? n : (n >> 7) * 64 + (n & 63)) * M;
-    *(uint4 *)(o + m0 + c * 8) = v;
+  for (int x = 0; x < WGT_T * (WGT_T / EC) / 256; ++x) {
+    constexpr int CR = WGT_T / EC;  // chunks a row
+    const int r = x * (256 / CR) + tid / CR, c = tid % CR;
+    if (n0 + r >= N || m0 + c * EC >= M) continue;
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (ES == 2 && rows > 0) v = *(const uint4 *)(smem + r * 256 + ((c ^ (r & 15)) << 4));
+    *(uint4 *)(out_row(n0 + r) + c * EC) = v;
   }
 }
 
@@ -1070,170 +1147,6 @@ __global__ __launch_bounds__(256, 1) void moe_grad_big_kernel(MoeGradArgs a, Big
   wait_vm<0>();  // (the unused stages)
 }
 
-// ------------------------------------------------------------------ fp32 tile
-// acc += A B^T over K (a multiple of 16), 64 x 64 on 2 x 2 waves, fp32 MFMA
-// (16x16x4).  Stages hold [k][row], rows of 80 floats: the 4 x 16 floats of a fragment
-// lie in different banks.  Sources: (row, k) -> address of 4 consecutive k, or,
-// transposed, (k, row) -> address of 4 consecutive rows.
-constexpr int F32_T = 64, F32_K = 16, F32_LD = 80;
-struct F32Smem {
-  float a[2][F32_K][F32_LD], b[2][F32_K][F32_LD];
-};
-template <bool AT, bool BT, class FA, class FB>
-__device__ __forceinline__ void tile_f32(F32Smem &sm, FA &&fa, FB &&fb, int K, f32x4_t (&acc)[2][2]) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / 2, wn = wave % 2;
-  const int tk = tid >> 4, tr = (tid & 15) * 4;  // transposed: K row, first of 4 rows
-  const int nr = tid >> 2, nk = (tid & 3) * 4;   // else: row, first of 4 k
-  f32x4_t ra, rb;
-  auto fetch = [&](int k0) {
-    if constexpr (AT) ra = *(const f32x4_t *)fa(k0 + tk, tr);
-    else ra = *(const f32x4_t *)fa(nr, k0 + nk);
-    if constexpr (BT) rb = *(const f32x4_t *)fb(k0 + tk, tr);
-    else rb = *(const f32x4_t *)fb(nr, k0 + nk);
-  };
-  auto put = [&](int s) {
-    if constexpr (AT) *(f32x4_t *)&sm.a[s][tk][tr] = ra;
-    else
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sm.a[s][nk + i][nr] = ra[i];
-    if constexpr (BT) *(f32x4_t *)&sm.b[s][tk][tr] = rb;
-    else
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sm.b[s][nk + i][nr] = rb[i];
-  };
-  if (K <= 0) return;
-  fetch(0);
-  put(0);
-  __syncthreads();
-  int s = 0;
-  for (int k0 = 0; k0 < K; k0 += F32_K) {
-    const bool more = k0 + F32_K < K;
-    if (more) fetch(k0 + F32_K);
-#pragma unroll
-    for (int kk = 0; kk < F32_K; kk += 4) {
-      float x[2], y[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        x[i] = sm.a[s][kk + (lane >> 4)][wm * 32 + 16 * i + (lane & 15)];
-        y[i] = sm.b[s][kk + (lane >> 4)][wn * 32 + 16 * i + (lane & 15)];
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[j], acc[i][j], 0, 0, 0);
-    }
-    if (more) put(s ^ 1);
-    __syncthreads();
-    s ^= 1;
-  }
-}
-
-__global__ __launch_bounds__(256) void moe_grad_hidden_f32_kernel(MoeGradArgs a, int nf) {
-  __shared__ __align__(16) F32Smem sm;
-  const PadScan ps = pad_scan(a.cnt, a.E);
-  RowTile t;
-  int nt;
-  if (!row_tile<F32_T>(ps, blockIdx.x / nf, t, nt)) return;
-  const int f0 = (blockIdx.x % nf) * F32_T, d = a.d, f = a.f;
-  const float *Wg = (const float *)a.Wg + (int64_t(t.e - 1) * f + f0) * d;
-  const float *Wu = (const float *)a.Wu + (int64_t(t.e - 1) * f + f0) * d;
-  const float *Wd = (const float *)a.Wd + int64_t(t.e - 1) * d * f + f0;
-  const float *n2 = (const float *)a.n2 + int64_t(t.p0) * d, *dy = (const float *)a.dy + int64_t(t.p0) * d;
-  f32x4_t G[2][2], U[2][2], q[2][2];
-  zero_acc(G);
-  zero_acc(U);
-  zero_acc(q);
-  tile_f32<false, false>(sm, [&](int r, int k) { return Wg + int64_t(r) * d + k; },
-                         [&](int r, int k) { return n2 + int64_t(r) * d + k; }, d, G);
-  tile_f32<false, false>(sm, [&](int r, int k) { return Wu + int64_t(r) * d + k; },
-                         [&](int r, int k) { return n2 + int64_t(r) * d + k; }, d, U);
-  tile_f32<true, false>(sm, [&](int k, int r) { return Wd + int64_t(k) * f + r; },
-                        [&](int r, int k) { return dy + int64_t(r) * d + k; }, d, q);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
-#pragma unroll
-  for (int ni = 0; ni < 2; ++ni) {
-    const int64_t pos = t.p0 + wn * 32 + ni * 16 + (lane & 15);  // tiles are whole: 64 rows
-    const float p = a.gate[pos];
-    float gs = 0.f;
-#pragma unroll
-    for (int mi = 0; mi < 2; ++mi) {
-      const int u = f0 + wm * 32 + mi * 16 + 4 * (lane >> 4);
-      f32x4_t dg, du, hp;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const Hidden h = hidden_grad<false>(G[mi][ni][i], U[mi][ni][i], q[mi][ni][i], p);
-        dg[i] = h.dg;
-        du[i] = h.du;
-        hp[i] = h.hp;
-        gs += h.gq;
-      }
-      float *o = (float *)a.dGU + pos * (2 * f) + u;
-      *(f32x4_t *)o = dg;
-      *(f32x4_t *)(o + f) = du;
-      if (a.Hp) *(f32x4_t *)((float *)a.Hp + pos * f + u) = hp;
-    }
-    gs += __shfl_xor(gs, 16, 64);
-    gs += __shfl_xor(gs, 32, 64);
-    if (lane < 16) a.gpart[pos * a.GP + (f0 / F32_T) * 2 + wm] = gs;
-  }
-}
-
-__global__ __launch_bounds__(256) void moe_grad_input_f32_kernel(MoeGradArgs a, int nd) {
-  __shared__ __align__(16) F32Smem sm;
-  const PadScan ps = pad_scan(a.cnt, a.E);
-  RowTile t;
-  int nt;
-  if (!row_tile<F32_T>(ps, blockIdx.x / nd, t, nt)) return;
-  const int m0 = (blockIdx.x % nd) * F32_T, d = a.d, f = a.f;
-  const float *g = (const float *)a.dGU + int64_t(t.p0) * (2 * f);
-  f32x4_t acc[2][2];
-  zero_acc(acc);
-#pragma unroll 1
-  for (int half = 0; half < 2; ++half) {
-    const float *W = (const float *)(half ? a.Wu : a.Wg) + int64_t(t.e - 1) * f * d + m0;
-    tile_f32<true, false>(sm, [&](int k, int r) { return W + int64_t(k) * d + r; },
-                          [&](int r, int k) { return g + int64_t(r) * (2 * f) + half * f + k; }, f, acc);
-  }
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
-#pragma unroll
-  for (int ni = 0; ni < 2; ++ni)
-#pragma unroll
-    for (int mi = 0; mi < 2; ++mi)
-      *(f32x4_t *)(a.Y + int64_t(t.p0 + wn * 32 + ni * 16 + (lane & 15)) * d + m0 + wm * 32 + mi * 16 +
-                   4 * (lane >> 4)) = acc[mi][ni];
-}
-
-__global__ __launch_bounds__(256) void moe_grad_weight_f32_kernel(MoeGradArgs a) {
-  __shared__ __align__(16) F32Smem sm;
-  const int d = a.d, f = a.f, md = d / F32_T, mf = f / F32_T, t1 = md * 2 * mf, t2 = mf * md;
-  int L = blockIdx.x;
-  const int e = L / (t1 + t2) + 1;
-  L -= (e - 1) * (t1 + t2);
-  const PadScan ps = pad_scan(a.cnt, a.E);
-  const int p0 = __builtin_amdgcn_readfirstlane(__shfl(ps.pad, e - 1, 64));
-  const int rows = __builtin_amdgcn_readfirstlane(__shfl(ps.pc, e - 1, 64));
-  const bool down = L >= t1;
-  if (down) L -= t1;
-  const int mt = down ? mf : md, M = down ? f : d, N = down ? d : 2 * f;
-  const int m0 = (L % mt) * F32_T, n0 = (L / mt) * F32_T;
-  const float *A = (const float *)(down ? a.Hp : a.n2) + int64_t(p0) * M + m0;
-  const float *B = (const float *)(down ? a.dy : a.dGU) + int64_t(p0) * N + n0;
-  f32x4_t acc[2][2];
-  zero_acc(acc);
-  tile_f32<true, true>(sm, [&](int k, int r) { return A + int64_t(k) * M + r; },
-                       [&](int k, int r) { return B + int64_t(k) * N + r; }, rows, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / 2, wn = wave % 2;
-  float *o = (float *)(down ? a.dWd : n0 < f ? a.dWg : a.dWu) + int64_t(e - 1) * d * f;
-  const int nb = !down && n0 >= f ? n0 - f : n0;
-#pragma unroll
-  for (int ni = 0; ni < 2; ++ni)
-#pragma unroll
-    for (int mi = 0; mi < 2; ++mi)
-      *(f32x4_t *)(o + int64_t(nb + wn * 32 + ni * 16 + (lane & 15)) * M + m0 + wm * 32 + mi * 16 +
-                   4 * (lane >> 4)) = acc[mi][ni];
-}
-
 // ------------------------------------------------------------------ tokens
 // dn of a token = the sum of its slots' rows of Y; through the norm to dxt; the
 // block's share of dg2 (fp32 over the tokens of a block, joined in fp64);
@@ -1248,7 +1161,7 @@ __global__ __launch_bounds__(256) void moe_grad_token_kernel(
     const int32_t *__restrict__ yrow_of, int planes, int64_t plane, const float *__restrict__ gpart, int GP,
     int N, int k, int d, float eps, T *dxt, float *__restrict__ g_gate, float *__restrict__ part,
     T *__restrict__ dg2) {
-  constexpr int RN = RR > 0 ? RR : 1;
+  constexpr int RN = RR > 0 ? RR : 1, PU = 8;
   __shared__ __align__(16) float red[RR > 0 ? 4 : 1][RR > 0 ? 512 * RR : 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   float sum[RN][8];  // the wave's share of dg2
@@ -1269,11 +1182,18 @@ __global__ __launch_bounds__(256) void moe_grad_token_kernel(
       for (int s = 0; s < k; ++s) {
         if (ei[s] == 0) continue;
         const float *yr = Y + int64_t(yo[s]) * d + c;
-        for (int p = 0; p < planes; ++p) {  // the parts of a split sum, in order
-          float y[8];
-          load8(yr + p * plane, y);
+        // the parts of a split sum, in order, eight loads in flight
+        for (int p0 = 0; p0 < planes; p0 += PU) {
+          float y[PU][8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) dn[j] += y[j];
+          for (int p = 0; p < PU; ++p)
+            if (p == 0 || p0 + p < planes) load8(yr + (p0 + p) * plane, y[p]);
+#pragma unroll
+          for (int p = 0; p < PU; ++p)
+            if (p == 0 || p0 + p < planes) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) dn[j] += y[p][j];
+            }
         }
       }
     };
@@ -1411,9 +1331,10 @@ static bool big_tiles(const triroute_cfg &cfg, int N) {
 // Parts of the sum of dn for few rows, so that the stream of the weights has about
 // two blocks a CU: each of at least 4 blocks of 64 units.
 int moe_grad_splits(const triroute_cfg &cfg, int N) {
-  if (cfg.act != TRIROUTE_BF16 || big_tiles(cfg, N)) return 1;
-  const int Nk = N * cfg.top_k, tiles = (Nk / INP_R + std::min(cfg.n_experts, Nk)) * (cfg.d_model / INP_M);
-  return std::max(1, std::min({(512 + tiles - 1) / tiles, cfg.d_ff / 64 / 4, 16}));
+  if (big_tiles(cfg, N)) return 1;
+  const int Nk = N * cfg.top_k;
+  const int64_t tiles = int64_t(Nk / INP_R + std::min(cfg.n_experts, Nk)) * (cfg.d_model / INP_M);
+  return std::max(1, std::min({int((512 + tiles - 1) / tiles), cfg.d_ff / 64 / 4, 16}));
 }
 
 template <typename T>
@@ -1434,6 +1355,7 @@ static hipError_t backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, 
       cfg.rms_eps, (T *)j.n2, (T *)j.dy, j.gate, j.row_of, j.list_of);
   const int32_t *yrow_of = j.row_of;
   int splits = 1;
+  bool done = false;
   const int64_t plane = int64_t(Nk) * d;
   if constexpr (sizeof(T) == 2) {
     if (big_tiles(cfg, N)) {
@@ -1454,22 +1376,29 @@ static hipError_t backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, 
       if (a.Hp)
         moe_grad_big_kernel<WeightBig><<<unsigned(std::min<int64_t>(int64_t(E) * (sh.t1 + sh.t2), cu)), 256, 0, st>>>(
             a, sh);
-    } else {
-      const int nf = f / HID_F, nd = d / INP_M, rt = Nk / 64 + std::min(E, Nk);  // row tiles at most
-      splits = moe_grad_splits(cfg, N);
-      yrow_of = j.list_of;
-      moe_grad_hidden_kernel<<<unsigned(rt) * nf, 256, 0, st>>>(a, nf);
-      moe_grad_input_kernel<<<unsigned(rt) * nd * splits, 256, 0, st>>>(a, nd, splits, plane);
-      if (a.Hp) {
-        const int md = (d + WGT_T - 1) / WGT_T, mf = (f + WGT_T - 1) / WGT_T;
-        moe_grad_weight_kernel<<<unsigned(E) * (md * (2 * f / WGT_T) + mf * md), 256, 0, st>>>(a);
-      }
+      done = true;
     }
-  } else {
-    const int nf = f / F32_T, nd = d / F32_T, rt = Nk / F32_T + std::min(E, Nk);
-    moe_grad_hidden_f32_kernel<<<unsigned(rt) * nf, 256, 0, st>>>(a, nf);
-    moe_grad_input_f32_kernel<<<unsigned(rt) * nd, 256, 0, st>>>(a, nd);
-    if (a.Hp) moe_grad_weight_f32_kernel<<<unsigned(E) * nd * nf * 3, 256, 0, st>>>(a);
+  }
+  if (!done) {
+    const int nf = f / HID_F, nd = d / INP_M, rt = Nk / 64 + std::min(E, Nk);  // row tiles at most
+    splits = moe_grad_splits(cfg, N);
+    yrow_of = j.list_of;
+    if (int64_t(rt) * nf <= cu_count())
+      moe_grad_hidden_kernel<T, 3><<<unsigned(rt) * nf, 512, 0, st>>>(a, nf);
+    else
+      moe_grad_hidden_kernel<T, 2><<<unsigned(rt) * nf, 512, 0, st>>>(a, nf);
+    if (int64_t(rt) * nd * splits <= 2 * cu_count())
+      moe_grad_input_kernel<T, 4><<<unsigned(rt) * nd * splits, 256, 0, st>>>(a, nd, splits, plane);
+    else
+      moe_grad_input_kernel<T, 2><<<unsigned(rt) * nd * splits, 256, 0, st>>>(a, nd, splits, plane);
+    if (a.Hp) {
+      const int md = (d + WGT_T - 1) / WGT_T, mf = (f + WGT_T - 1) / WGT_T;
+      const unsigned tiles = unsigned(E) * (md * (2 * f / WGT_T) + mf * md);
+      if (Nk / (E + 1) < 128)
+        moe_grad_weight_kernel<T, 1><<<tiles, 256, 0, st>>>(a);
+      else
+        moe_grad_weight_kernel<T, 2><<<tiles, 256, 0, st>>>(a);
+    }
   }
   const int prows = moe_grad_part_rows(cfg, N);
   const bool direct = token_blocks(N) == 1 && d <= 2048;  // one block: its dg2 is the sum
