@@ -7,8 +7,9 @@
 //   dn += Wg^T dG + Wu^T dU
 // and through the norm to xt and g2.  Three grouped products:
 //   hidden  [G; U; q] of a tile of units and rows, whose sum indices are all d_model,
-//           so that one epilogue holds the three in fp32: G, U and q never
-//           leave the registers, and g_gate is summed from values that were not rounded
+//           so that one epilogue holds the three in fp32 and g_gate is summed from
+//           values that were not rounded (many rows: q comes from a product of its own,
+//           in fp32, and the epilogue of G and U reads it)
 //   input   dn = [dG dU] [Wg; Wu]
 //   weight  dWg, dWu, dWd: sums over the rows of an expert
 // Rows lie by expert, each expert's padded to a multiple of 64 rows with zeros: a
@@ -423,17 +424,19 @@ __global__ __launch_bounds__(512) void moe_grad_hidden_kernel(MoeGradArgs a, int
 // of Y (list order).
 constexpr int INP_M = 64, INP_R = 64;
 template <typename T, int INP_S>
-__global__ __launch_bounds__(256) void moe_grad_input_kernel(MoeGradArgs a, int nd, int splits, int64_t plane) {
-  using C = TileCore<T, INP_M, INP_R, true, false, 1, 2, 2, INP_S>;
+using InputCore = TileCore<T, INP_M, INP_R, true, false, 1, 2, 2, INP_S>;
+template <typename T, int INP_S>
+__device__ __forceinline__ void input_tile(const MoeGradArgs &a, uint8_t *smem, int block, int nd, int splits,
+                                           int64_t plane) {
+  using C = InputCore<T, INP_S>;
   constexpr int ES = sizeof(T), SPB = 64 / C::KB;  // steps of 64 gates (ups)
-  __shared__ __align__(1024) uint8_t smem[INP_S * C::STAGE];
   const PadScan ps = pad_scan(a.cnt, a.E);
   RowTile t;
   int nt;
   row_tile<INP_R>(ps, 0, t, nt);
   const int total = nt * nd * splits;
-  if (int(blockIdx.x) >= total) return;
-  int L = xcd_tile(blockIdx.x, total);
+  if (block >= total) return;
+  int L = xcd_tile(block, total);
   const int sp = L % splits;
   L /= splits;
   row_tile<INP_R>(ps, L / nd, t, nt);
@@ -469,14 +472,15 @@ __global__ __launch_bounds__(256) void moe_grad_input_kernel(MoeGradArgs a, int 
 // blocks a CU: 160M, 1 token 17.4 us, three blocks 20.4; 410M, 333 tokens 39.5, 45.0).
 constexpr int WGT_T = 128;
 template <typename T, int WGT_S>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) void moe_grad_weight_kernel(MoeGradArgs a) {
-  using C = TileCore<T, WGT_T, WGT_T, true, true, 1, 2, 2, WGT_S>;
+using WeightCore = TileCore<T, WGT_T, WGT_T, true, true, 1, 2, 2, WGT_S>;
+template <typename T, int WGT_S>
+__device__ __forceinline__ void weight_tile(const MoeGradArgs &a, uint8_t *smem, int block, int tiles) {
+  using C = WeightCore<T, WGT_S>;
   constexpr int ES = sizeof(T), EC = 16 / ES;  // elements of a chunk
-  __shared__ __align__(1024) uint8_t smem[WGT_S * C::STAGE];
   const int d = a.d, f = a.f;
   const int md = (d + WGT_T - 1) / WGT_T, mf = (f + WGT_T - 1) / WGT_T;
   const int t1 = md * (2 * f / WGT_T), t2 = mf * md;  // (2 f is a multiple of 128)
-  int L = xcd_tile(blockIdx.x, gridDim.x);
+  int L = xcd_tile(block, tiles);
   const int e = L / (t1 + t2) + 1;
   L -= (e - 1) * (t1 + t2);
   const PadScan ps = pad_scan(a.cnt, a.E);
@@ -528,6 +532,24 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) void moe_grad_weight_k
     if (ES == 2 && rows > 0) v = *(const uint4 *)(smem + r * 256 + ((c ^ (r & 15)) << 4));
     *(uint4 *)(out_row(n0 + r) + c * EC) = v;
   }
+}
+
+// dn alone (frozen experts), or dn's tiles (the first nin blocks) beside the weight
+// gradients', which do not wait for each other.
+template <typename T, int S>
+__global__ __launch_bounds__(256) void moe_grad_input_kernel(MoeGradArgs a, int nd, int splits, int64_t plane) {
+  __shared__ __align__(1024) uint8_t smem[S * InputCore<T, S>::STAGE];
+  input_tile<T, S>(a, smem, blockIdx.x, nd, splits, plane);
+}
+template <typename T, int WS>
+__global__ __launch_bounds__(256, sizeof(T) == 2 && WS == 1 ? 4 : 2) void moe_grad_input_weight_kernel(
+    MoeGradArgs a, int nin, int nd, int splits, int64_t plane) {
+  constexpr int BI = 2 * InputCore<T, 2>::STAGE, BW = WS * WeightCore<T, WS>::STAGE;
+  __shared__ __align__(1024) uint8_t smem[BI > BW ? BI : BW];
+  if (int(blockIdx.x) < nin)
+    input_tile<T, 2>(a, smem, blockIdx.x, nd, splits, plane);
+  else
+    weight_tile<T, WS>(a, smem, int(blockIdx.x) - nin, int(gridDim.x) - nin);
 }
 
 // ------------------------------------------------------- four-wave products
@@ -1032,8 +1054,9 @@ __device__ __forceinline__ void unroll(F &&f) {
   unroll_<N>(f, std::make_integer_sequence<int, N>{});
 }
 
+// The block's tiles first, first + gridDim.x, .. of problem P; returns P's number of tiles.
 template <class P>
-__global__ __launch_bounds__(256, 1) void moe_grad_big_kernel(MoeGradArgs a, BigShape shape) {
+__device__ __forceinline__ int big_tiles_run(const MoeGradArgs &a, const BigShape &shape, uint8_t *smem, int first) {
   P p(a, shape);
   constexpr int NM = P::NM, NF = P::NA + P::NB, IPW = P::IPW, STAGE = P::STAGE;
   constexpr int MI = P::MI, NI = P::NI;
@@ -1046,10 +1069,9 @@ __global__ __launch_bounds__(256, 1) void moe_grad_big_kernel(MoeGradArgs a, Big
   constexpr int NSLOT = (NM - 1 - B1J) + RS;
   constexpr int GAP = NSLOT / IPW < 5 ? NSLOT / IPW : 5;
   static_assert(B1J < NM && RS + NF <= NM && GAP >= 1 && GAP * (IPW - 1) < NSLOT, "room for the transfers");
-  __shared__ __align__(1024) uint8_t smem[2 * STAGE];
   const TileScan gs = p.scan();
   const int total = __builtin_amdgcn_readfirstlane(p.total(gs));
-  if (int(blockIdx.x) >= total) return;
+  if (first >= total) return total;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
   uint32_t dst = __builtin_amdgcn_readfirstlane(lds_addr(smem) + wave * 1024);  // the wave's part of the present stage
@@ -1057,7 +1079,7 @@ __global__ __launch_bounds__(256, 1) void moe_grad_big_kernel(MoeGradArgs a, Big
   p.frags(lds_addr(smem), wm, wn, lane);
 
   // the producer: stage pk of tile Lp; behind the block's last stage the same one again, unused
-  int Lp = int(blockIdx.x) - int(gridDim.x), pk = 0, pnk = 0;
+  int Lp = first - int(gridDim.x), pk = 0, pnk = 0;
   auto advance = [&]() __attribute__((always_inline)) {
     if (pk + 1 < pnk) {
       p.next(++pk);
@@ -1122,7 +1144,7 @@ __global__ __launch_bounds__(256, 1) void moe_grad_big_kernel(MoeGradArgs a, Big
     delta = -delta;
     advance();
   };
-  for (int L = blockIdx.x; L < total; L += int(gridDim.x)) {
+  for (int L = first; L < total; L += int(gridDim.x)) {
     const BigTile t = p.tile(gs, L, total);
     if constexpr (P::EMPTY) {
       if (t.nk == 0) {  // an expert without rows
@@ -1145,6 +1167,22 @@ __global__ __launch_bounds__(256, 1) void moe_grad_big_kernel(MoeGradArgs a, Big
     for (int q = 0; q < NF; ++q) p.read(q, 0, fa[0], fb[0]);
   }
   wait_vm<0>();  // (the unused stages)
+  return total;
+}
+
+// P's tiles, then Q's (which wait for none of P's): the blocks that P leaves a tile short begin Q's
+// list, so that the two lose one last round together (160M, 16384 tokens: dn 1.4 rounds and weights
+// 2.3: 488 us one after the other, 409 together; 410M, 4000 tokens, skewed: 286 and 238).
+template <class P, class Q = void>
+__global__ __launch_bounds__(256, 1) void moe_grad_big_kernel(MoeGradArgs a, BigShape shape) {
+  __shared__ __align__(1024) uint8_t smem[2 * P::STAGE];
+  const int n = big_tiles_run<P>(a, shape, smem, blockIdx.x);
+  if constexpr (!std::is_void<Q>::value) {
+    static_assert(P::STAGE == Q::STAGE, "one array of stages");
+    __syncthreads();
+    const int g = int(gridDim.x), r = (int(blockIdx.x) - n % g + g) % g;
+    big_tiles_run<Q>(a, shape, smem, r);
+  }
 }
 
 // ------------------------------------------------------------------ tokens
@@ -1329,12 +1367,15 @@ static bool big_tiles(const triroute_cfg &cfg, int N) {
   return cfg.act == TRIROUTE_BF16 && int64_t(N) * cfg.top_k / (cfg.n_experts + 1) >= 128;
 }
 // Parts of the sum of dn for few rows, so that the stream of the weights has about
-// two blocks a CU: each of at least 4 blocks of 64 units.
+// two blocks a CU: at most 8 (a token's partial rows are loaded together), each of at least 4 blocks of 64 units
+// (fp32, whose steps are half as long: 2; the small layer, 128 tokens: dn 14.6 -> 8.9 us with
+// four parts instead of two; 160M, 1 token, bf16: 16 parts of 2 blocks gain nothing there and cost the
+// tokens 3 us).
 int moe_grad_splits(const triroute_cfg &cfg, int N) {
   if (big_tiles(cfg, N)) return 1;
   const int Nk = N * cfg.top_k;
   const int64_t tiles = int64_t(Nk / INP_R + std::min(cfg.n_experts, Nk)) * (cfg.d_model / INP_M);
-  return std::max(1, std::min({int((512 + tiles - 1) / tiles), cfg.d_ff / 64 / 4, 16}));
+  return std::max(1, std::min({int((512 + tiles - 1) / tiles), cfg.d_ff / 64 / (cfg.act == TRIROUTE_BF16 ? 4 : 2), 8}));
 }
 
 template <typename T>
@@ -1372,10 +1413,10 @@ static hipError_t backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, 
       sh.ny = (f + 127) / 128;
       moe_grad_big_kernel<GateUpBig><<<blocks(sh.ny), 256, 0, st>>>(a, sh);
       sh.ny = sh.md;
-      moe_grad_big_kernel<RowsBig<true>><<<blocks(sh.ny), 256, 0, st>>>(a, sh);
       if (a.Hp)
-        moe_grad_big_kernel<WeightBig><<<unsigned(std::min<int64_t>(int64_t(E) * (sh.t1 + sh.t2), cu)), 256, 0, st>>>(
-            a, sh);
+        moe_grad_big_kernel<RowsBig<true>, WeightBig><<<cu, 256, 0, st>>>(a, sh);
+      else
+        moe_grad_big_kernel<RowsBig<true>><<<blocks(sh.ny), 256, 0, st>>>(a, sh);
       done = true;
     }
   }
@@ -1387,17 +1428,21 @@ static hipError_t backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, 
       moe_grad_hidden_kernel<T, 3><<<unsigned(rt) * nf, 512, 0, st>>>(a, nf);
     else
       moe_grad_hidden_kernel<T, 2><<<unsigned(rt) * nf, 512, 0, st>>>(a, nf);
-    if (int64_t(rt) * nd * splits <= 2 * cu_count())
-      moe_grad_input_kernel<T, 4><<<unsigned(rt) * nd * splits, 256, 0, st>>>(a, nd, splits, plane);
-    else
-      moe_grad_input_kernel<T, 2><<<unsigned(rt) * nd * splits, 256, 0, st>>>(a, nd, splits, plane);
+    const unsigned nin = unsigned(rt) * nd * splits;
     if (a.Hp) {
       const int md = (d + WGT_T - 1) / WGT_T, mf = (f + WGT_T - 1) / WGT_T;
       const unsigned tiles = unsigned(E) * (md * (2 * f / WGT_T) + mf * md);
-      if (Nk / (E + 1) < 128)
-        moe_grad_weight_kernel<T, 1><<<tiles, 256, 0, st>>>(a);
+      // (bf16 with more rows than these has gone to the large tiles)
+      if constexpr (sizeof(T) == 2)
+        moe_grad_input_weight_kernel<T, 1><<<nin + tiles, 256, 0, st>>>(a, int(nin), nd, splits, plane);
+      else if (Nk / (E + 1) < 128)
+        moe_grad_input_weight_kernel<T, 1><<<nin + tiles, 256, 0, st>>>(a, int(nin), nd, splits, plane);
       else
-        moe_grad_weight_kernel<T, 2><<<tiles, 256, 0, st>>>(a);
+        moe_grad_input_weight_kernel<T, 2><<<nin + tiles, 256, 0, st>>>(a, int(nin), nd, splits, plane);
+    } else if (nin <= unsigned(2 * cu_count())) {
+      moe_grad_input_kernel<T, 4><<<nin, 256, 0, st>>>(a, nd, splits, plane);
+    } else {
+      moe_grad_input_kernel<T, 2><<<nin, 256, 0, st>>>(a, nd, splits, plane);
     }
   }
   const int prows = moe_grad_part_rows(cfg, N);
