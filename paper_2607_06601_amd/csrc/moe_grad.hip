@@ -1361,10 +1361,17 @@ int moe_grad_part_rows(const triroute_cfg &cfg, int N) {
   return token_blocks(N) * (cfg.d_model <= 2048 ? 1 : 4);
 }
 
-// bf16: whether the experts have rows enough for the 256-row tiles (r: rows of an
-// expert when the router spreads its options evenly).
+// bf16: whether the experts have rows enough for the 256-row tiles: r >= 64 of them (those of an
+// expert when the router spreads its options evenly), and units and sum indices enough that the tiles
+// fill the card, counted as rows x d x d_ff >= 1e10.  Us, small tiles / large ones: 160M, r 455
+// 191 / 209, r 568 249 / 254, r 777 298 / 265, r 910 332 / 275; 410M, r 311 240 / 297, r 455
+// 331 / 331, r 577 414 / 389, r 777 541 / 434; 1.3B, r 32 754 / 862, r 56 804 / 900, r 64
+// 1026 / 939, r 96 1187 / 987, r 256 2228 / 1240; 63 experts of 2048 x 5632, r 32 2706 / 2849,
+// r 64 3638 / 3093; one expert of 256 x 512, 16384 rows: 140 / 151.
 static bool big_tiles(const triroute_cfg &cfg, int N) {
-  return cfg.act == TRIROUTE_BF16 && int64_t(N) * cfg.top_k / (cfg.n_experts + 1) >= 128;
+  const int64_t r = int64_t(N) * cfg.top_k / (cfg.n_experts + 1);
+  return cfg.act == TRIROUTE_BF16 && r >= 64 &&
+         double(r * cfg.n_experts) * cfg.d_model * cfg.d_ff >= 1e10;
 }
 // Parts of the sum of dn for few rows, so that the stream of the weights has about
 // two blocks a CU: at most 8 (a token's partial rows are loaded together), each of at least 4 blocks of 64 units

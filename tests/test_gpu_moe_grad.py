@@ -241,3 +241,50 @@ def test_layer_shapes_against_fp32_products(shape, N):
         off = float((got.out[name].double() - want).norm() / want.norm())
         note(f"{shape} {name}", off / tol)
         assert off <= tol, (name, off, tol)
+
+
+# Rows and widths enough for the large tiles (rows an expert >= 64, rows x d x d_ff >= 1e10):
+# rows around the tiles, an expert without any; widths off every tile, both ways; d past
+# the widths that the tokens' part holds in registers; many experts
+MANY = [
+    ("bf16", 10500, 960, 1216, 6, 1, [517, 1, 0, 255, 257, 4000, 5470]),
+    ("bf16", 8200, 320, 2880, 2, 2, "random"),
+    ("bf16", 15600, 2240, 192, 3, 2, "random"),
+    ("bf16", 1088, 1984, 2496, 16, 2, "random"),
+]
+
+
+@pytest.mark.parametrize("act,N,d,f,E,k,choice", MANY)
+def test_many_rows(act, N, d, f, E, k, choice):
+    assert N * k // (E + 1) >= 64 and N * k // (E + 1) * E * d * f >= 1e10
+    test_matches_oracle(act, N, d, f, E, k, choice)
+
+
+def test_many_rows_streams_graphs_and_frozen_experts():
+    """Two calls at once, a replayed graph beside an eager call and frozen experts give the
+    first call's bits."""
+    case = moe_case(15, "bf16", 6301, 1024, 1024, 4, 2)
+    first = Call(*case, "bf16")().result()
+    only = Call(*case, "bf16", want=("dxt", "g_gate"), in_place=True)().result()
+    for n, v in only.items():
+        np.testing.assert_array_equal(v, first[n], err_msg=n)
+    calls, streams = [Call(*case, "bf16") for _ in range(2)], [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for c, s in zip(calls, streams):
+        c(stream=s)
+    for c in calls:
+        for n, v in c.result().items():
+            np.testing.assert_array_equal(v, first[n], err_msg=n)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        calls[0]()
+    for rep in range(3):
+        for v in calls[0].out.values():
+            v.fill_(float("nan"))
+        calls[0].ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        g.replay()
+        calls[1](stream=streams[0])
+        for c in calls:
+            for n, v in c.result().items():
+                np.testing.assert_array_equal(v, first[n], err_msg=f"{n} replay {rep}")
