@@ -147,7 +147,9 @@ typedef short s16x4_t __attribute__((ext_vector_type(4)));
 // lane group, lie in different banks.
 template <int R>
 __device__ __forceinline__ int tswz(int k, int b) {
-  if constexpr (R == 64)
+  if constexpr (R == 32)
+    return b ^ ((k >> 3) & 1);  // four K rows a bank span
+  else if constexpr (R == 64)
     return b ^ (((k >> 1) & 1) | (((k >> 3) & 1) << 1));  // two K rows a bank span
   else
     return b ^ ((k & 3) | (((k >> 3) & 1) << 2));
@@ -179,11 +181,12 @@ struct TileCore {
   static_assert(STAGE % (1024 * NW) == 0, "whole transfers");
   using Frag = typename std::conditional<F, f32x4_t, bf16x8_t>::type;  // 16 rows x 32 (fp32: 16) indices
 
+  static constexpr int fmask(int R) { return R >= 64 ? 3 : R / 16 - 1; }
   // Source chunk of 16-byte chunk c of K row k in a stage of a transposed operand of R columns.
   template <int R>
   __device__ static __forceinline__ int tchunk(int k, int c) {
     if constexpr (F)
-      return c ^ (((k >> 2) & 3) << 2);  // the lane groups' K rows 4 g + i in different banks
+      return c ^ (((k >> 2) & fmask(R)) << 2);  // the lane groups' K rows 4 g + i in different banks (R 32: halves)
     else
       return tswz<R>(k, c >> 1) * 2 + (c & 1);
   }
@@ -198,7 +201,8 @@ struct TileCore {
       f32x4_t v;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        v[i] = *(const float *)(base + (16 * ks + 4 * g + i) * (4 * R) + (((row0 >> 4) ^ g) * 16 + n) * 4);
+        v[i] = *(const float *)(base + (16 * ks + 4 * g + i) * (4 * R) +
+                                (((row0 >> 4) ^ (g & fmask(R))) * 16 + n) * 4);
       return v;
     } else {
       typedef __attribute__((address_space(3))) s16x4_t *P;
@@ -346,15 +350,19 @@ __device__ __forceinline__ Hidden hidden_grad(float G, float U, float q, float p
 // in use.  The fp32 products, bound by the fp32 MFMA rate, run on the same tiles,
 // several blocks a CU.
 
-// [G; U; q] of 64 units and 64 rows: four waves make G and U while four make q, over
+// [G; U; q] of HID_F units and 64 rows: four waves make G and U while four make q, over
 // the same number of steps (and barriers), and hand it over in LDS.
-// (160M, 1 token, 64 tiles: two stages 14.2 us, three 12.0; 410M, 333 tokens, 704 tiles, two
+// HID_F 32, with four stages, where the tiles then still are no more than the CUs: twice the
+// CUs share the stream of the weights and, in fp32, the products.
+// (160M, 1 token, 64 tiles: two stages 14.2 us, three 12.0, 128 tiles of 32 units 9.7; 256 x 512 in
+// fp32, 128 tokens, 48 tiles: 19.2, 96 of 32 units 12.9; 410M, 333 tokens, 704 tiles, two
 // blocks a CU with two stages 46 us, one with three 50.)
-constexpr int HID_F = 64, HID_R = 64;
-template <typename T, int HID_S>
+constexpr int HID_R = 64;
+template <typename T, int HID_F, int HID_S>
 __global__ __launch_bounds__(512) void moe_grad_hidden_kernel(MoeGradArgs a, int nf) {
-  using C1 = TileCore<T, 2 * HID_F, HID_R, false, false, 2, 2, 2, HID_S>;
-  using C2 = TileCore<T, HID_F, HID_R, true, false, 1, 2, 2, HID_S>;
+  constexpr int WM = HID_F / 32, WN = 4 / WM;  // waves of 32 units
+  using C1 = TileCore<T, 2 * HID_F, HID_R, false, false, 2, WM, WN, HID_S>;
+  using C2 = TileCore<T, HID_F, HID_R, true, false, 1, WM, WN, HID_S>;
   constexpr int MI = C2::MI, NI = C2::NI, ES = sizeof(T);
   __shared__ __align__(1024) uint8_t smem[HID_S * (C1::STAGE + C2::STAGE)];
   const PadScan ps = pad_scan(a.cnt, a.E);
@@ -368,7 +376,7 @@ __global__ __launch_bounds__(512) void moe_grad_hidden_kernel(MoeGradArgs a, int
   const int f0 = (L % nf) * HID_F;
   const int d = a.d, f = a.f, steps = d / C1::KB;
   const int lane = threadIdx.x & 63, w8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wave = w8 & 3, wm = wave / 2, wn = wave % 2;
+  const int wave = w8 & 3, wm = wave / WN, wn = wave % WN;
   auto along = [](int kt) { return int64_t(kt) * 128; };
   f32x4_t(*qs)[64] = (f32x4_t(*)[64])(smem + HID_S * C1::STAGE) + wave * MI * NI;  // [block][lane]
   if (w8 >= 4) {
@@ -396,12 +404,12 @@ __global__ __launch_bounds__(512) void moe_grad_hidden_kernel(MoeGradArgs a, int
   __syncthreads();  // q is there
 #pragma unroll
   for (int ni = 0; ni < NI; ++ni) {
-    const int64_t pos = t.p0 + wn * (HID_R / 2) + ni * 16 + (lane & 15);  // (tiles are whole: 64 rows)
+    const int64_t pos = t.p0 + wn * (HID_R / WN) + ni * 16 + (lane & 15);  // (tiles are whole: 64 rows)
     const float p = a.gate[pos];
     float gs = 0.f;
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
-      const int u = f0 + wm * (HID_F / 2) + mi * 16 + 4 * (lane >> 4);
+      const int u = f0 + wm * 32 + mi * 16 + 4 * (lane >> 4);
       const f32x4_t q = qs[mi * NI + ni][lane];
       Hidden h[4];
 #pragma unroll
@@ -409,14 +417,14 @@ __global__ __launch_bounds__(512) void moe_grad_hidden_kernel(MoeGradArgs a, int
         h[i] = hidden_grad<ES == 2>(gu[mi][ni][i], gu[MI + mi][ni][i], q[i], p);
         gs += h[i].gq;
       }
-      T *o = (T *)a.dGU + pos * (2 * f) + f0 + u;  // (f0: a multiple of 64)
+      T *o = (T *)a.dGU + pos * (2 * f) + (u & ~63) + u;
       put4(o, h[0].dg, h[1].dg, h[2].dg, h[3].dg);
       put4(o + 64, h[0].du, h[1].du, h[2].du, h[3].du);
       if (a.Hp) put4((T *)a.Hp + pos * f + u, h[0].hp, h[1].hp, h[2].hp, h[3].hp);
     }
     gs += __shfl_xor(gs, 16, 64);
     gs += __shfl_xor(gs, 32, 64);
-    if (lane < 16) a.gpart[pos * a.GP + (f0 / HID_F) * 2 + wm] = gs;
+    if (lane < 16) a.gpart[pos * a.GP + f0 / 32 + wm] = gs;
   }
 }
 
@@ -1188,20 +1196,34 @@ __global__ __launch_bounds__(256, 1) void moe_grad_big_kernel(MoeGradArgs a, Big
 // ------------------------------------------------------------------ tokens
 // dn of a token = the sum of its slots' rows of Y; through the norm to dxt; the
 // block's share of dg2 (fp32 over the tokens of a block, joined in fp64);
-// g_gate from the hidden tiles' partial sums.  One wave per token at a time;
+// beside them, in blocks of their own, g_gate from the hidden tiles' partial sums (160M, 1 token:
+// 8.1 us after the token's own work, 6.4 beside it).  One wave per token at a time;
 // rows of up to 512 RR elements are read once and stay in registers (RR 0: any
-// width, read twice).  Bound by HBM.
+// width, read twice).  ONE: dn's sum is not split; without the registers of the parts'
+// loads two more waves a SIMD (160M, 16384 tokens 66 us, 50).  Bound by HBM: 1.3B, 16384
+// tokens, 453 MB, 127 us (1024 blocks 132; a slot's whole row in flight 135).
 constexpr int TOK_BLOCKS = 512;
-template <typename T, int RR>
+template <typename T, int RR, bool ONE>
 __global__ __launch_bounds__(256) void moe_grad_token_kernel(
     const T *__restrict__ x, const T *dx, const T *__restrict__ g, const float *__restrict__ Y,
     const int32_t *__restrict__ eidx, const int32_t *__restrict__ row_of,
     const int32_t *__restrict__ yrow_of, int planes, int64_t plane, const float *__restrict__ gpart, int GP,
     int N, int k, int d, float eps, T *dxt, float *__restrict__ g_gate, float *__restrict__ part,
-    T *__restrict__ dg2) {
-  constexpr int RN = RR > 0 ? RR : 1, PU = 8;
+    T *__restrict__ dg2, int tb) {
+  constexpr int RN = RR > 0 ? RR : 1, PU = ONE ? 1 : 8;
   __shared__ __align__(16) float red[RR > 0 ? 4 : 1][RR > 0 ? 512 * RR : 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (int(blockIdx.x) >= tb) {  // the gates' blocks: one wave per assignment
+    const int stride = (int(gridDim.x) - tb) * 4;
+    for (int64_t i = (int(blockIdx.x) - tb) * 4 + wave; i < int64_t(N) * k; i += stride) {
+      float v = 0.f;
+      if (eidx[i] != 0)
+        for (int j = lane; j < GP; j += 64) v += gpart[int64_t(row_of[i]) * GP + j];
+      v = wave_sum(v);
+      if (lane == 0) g_gate[i] = v;
+    }
+    return;
+  }
   float sum[RN][8];  // the wave's share of dg2
 #pragma unroll
   for (int q = 0; q < RN; ++q)
@@ -1211,9 +1233,9 @@ __global__ __launch_bounds__(256) void moe_grad_token_kernel(
   float *pr = RR == 0 && part ? part + (int64_t(blockIdx.x) * 4 + wave) * d : nullptr;
   if (RR == 0 && pr)
     for (int c = lane * 8; c < d; c += 512) store8(pr + c, &sum[0][0]);
-  for (int i = blockIdx.x * 4 + wave; i < N; i += gridDim.x * 4) {
+  for (int i = blockIdx.x * 4 + wave; i < N; i += tb * 4) {
     const T *xr = x + int64_t(i) * d;
-    const int32_t *ei = eidx + int64_t(i) * k, *ro = row_of + int64_t(i) * k, *yo = yrow_of + int64_t(i) * k;
+    const int32_t *ei = eidx + int64_t(i) * k, *yo = yrow_of + int64_t(i) * k;
     auto dn8 = [&](int c, float *dn) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) dn[j] = 0.f;
@@ -1221,7 +1243,7 @@ __global__ __launch_bounds__(256) void moe_grad_token_kernel(
         if (ei[s] == 0) continue;
         const float *yr = Y + int64_t(yo[s]) * d + c;
         // the parts of a split sum, in order, eight loads in flight
-        for (int p0 = 0; p0 < planes; p0 += PU) {
+        for (int p0 = 0; p0 < (ONE ? 1 : planes); p0 += PU) {
           float y[PU][8];
 #pragma unroll
           for (int p = 0; p < PU; ++p)
@@ -1235,12 +1257,13 @@ __global__ __launch_bounds__(256) void moe_grad_token_kernel(
         }
       }
     };
-    float w[RN][8], dn[RN][8];
+    float w[RN][8], dn[RN][8], up[RN][8];
     double ss = 0.0, dot = 0.0;
-    auto take = [&](int c, float *wv, float *dv) {  // the sums over a row
+    auto take = [&](int c, float *wv, float *dv, float *uv) {  // the sums over a row
       float gv[8];
       load8(xr + c, wv);
       load8(g + c, gv);
+      if constexpr (RR > 0) load8(dx + int64_t(i) * d + c, uv);
       dn8(c, dv);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -1251,18 +1274,17 @@ __global__ __launch_bounds__(256) void moe_grad_token_kernel(
     if constexpr (RR > 0) {
 #pragma unroll
       for (int q = 0; q < RN; ++q)
-        if (lane * 8 + 512 * q < d) take(lane * 8 + 512 * q, w[q], dn[q]);
+        if (lane * 8 + 512 * q < d) take(lane * 8 + 512 * q, w[q], dn[q], up[q]);
     } else {
-      for (int c = lane * 8; c < d; c += 512) take(c, w[0], dn[0]);
+      for (int c = lane * 8; c < d; c += 512) take(c, w[0], dn[0], up[0]);
     }
     ss = wave_sum(ss);
     dot = wave_sum(dot);
     const double r = 1.0 / sqrt(ss / double(d) + double(eps));
     const float rf = float(r), cf = float(r * r * r * dot / double(d));
-    auto give = [&](int c, const float *wv, const float *dv, float *q) {
-      float gv[8], u[8], o[8];
+    auto give = [&](int c, const float *wv, const float *dv, const float *u, float *q) {
+      float gv[8], o[8];
       load8(g + c, gv);
-      load8(dx + int64_t(i) * d + c, u);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         o[j] = u[j] + fmaf(rf, dv[j] * gv[j], -cf * wv[j]);
@@ -1273,26 +1295,18 @@ __global__ __launch_bounds__(256) void moe_grad_token_kernel(
     if constexpr (RR > 0) {
 #pragma unroll
       for (int q = 0; q < RN; ++q)
-        if (lane * 8 + 512 * q < d) give(lane * 8 + 512 * q, w[q], dn[q], sum[q]);
+        if (lane * 8 + 512 * q < d) give(lane * 8 + 512 * q, w[q], dn[q], up[q], sum[q]);
     } else {
       for (int c = lane * 8; c < d; c += 512) {
         float q[8];
         load8(xr + c, w[0]);
+        load8(dx + int64_t(i) * d + c, up[0]);
         dn8(c, dn[0]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) q[j] = 0.f;
         if (pr) load8(pr + c, q);
-        give(c, w[0], dn[0], q);
+        give(c, w[0], dn[0], up[0], q);
         if (pr) store8(pr + c, q);
-      }
-    }
-    if (g_gate) {
-      for (int s = 0; s < k; ++s) {
-        float v = 0.f;
-        if (ei[s] != 0)
-          for (int j = lane; j < GP; j += 64) v += gpart[int64_t(ro[s]) * GP + j];
-        v = wave_sum(v);
-        if (lane == 0) g_gate[int64_t(i) * k + s] = v;
       }
     }
   }
@@ -1428,13 +1442,15 @@ static hipError_t backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, 
     }
   }
   if (!done) {
-    const int nf = f / HID_F, nd = d / INP_M, rt = Nk / 64 + std::min(E, Nk);  // row tiles at most
+    const int nf = f / 64, nd = d / INP_M, rt = Nk / 64 + std::min(E, Nk);  // row tiles at most
     splits = moe_grad_splits(cfg, N);
     yrow_of = j.list_of;
-    if (int64_t(rt) * nf <= cu_count())
-      moe_grad_hidden_kernel<T, 3><<<unsigned(rt) * nf, 512, 0, st>>>(a, nf);
+    if (int64_t(rt) * nf * 2 <= cu_count())
+      moe_grad_hidden_kernel<T, 32, 4><<<unsigned(rt) * nf * 2, 512, 0, st>>>(a, nf * 2);
+    else if (int64_t(rt) * nf <= cu_count())
+      moe_grad_hidden_kernel<T, 64, 3><<<unsigned(rt) * nf, 512, 0, st>>>(a, nf);
     else
-      moe_grad_hidden_kernel<T, 2><<<unsigned(rt) * nf, 512, 0, st>>>(a, nf);
+      moe_grad_hidden_kernel<T, 64, 2><<<unsigned(rt) * nf, 512, 0, st>>>(a, nf);
     const unsigned nin = unsigned(rt) * nd * splits;
     if (a.Hp) {
       const int md = (d + WGT_T - 1) / WGT_T, mf = (f + WGT_T - 1) / WGT_T;
@@ -1452,13 +1468,18 @@ static hipError_t backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, 
       moe_grad_input_kernel<T, 2><<<nin, 256, 0, st>>>(a, nd, splits, plane);
     }
   }
-  const int prows = moe_grad_part_rows(cfg, N);
-  const bool direct = token_blocks(N) == 1 && d <= 2048;  // one block: its dg2 is the sum
-  auto token = [&](auto rr) {
-    moe_grad_token_kernel<T, decltype(rr)::value><<<token_blocks(N), 256, 0, st>>>(
+  const int prows = moe_grad_part_rows(cfg, N), tb = token_blocks(N);
+  const bool direct = tb == 1 && d <= 2048;  // one block: its dg2 is the sum
+  const unsigned blocks = tb + (j.out.g_gate ? std::min((Nk + 3) / 4, TOK_BLOCKS) : 0);
+  auto launch = [&](auto rr, auto one) {
+    moe_grad_token_kernel<T, decltype(rr)::value, decltype(one)::value><<<blocks, 256, 0, st>>>(
         (const T *)j.xt, (const T *)j.dx, (const T *)j.g2, j.Y, j.eidx, j.row_of, yrow_of, splits, plane, j.gpart,
         a.GP, N, k, d, cfg.rms_eps, (T *)j.out.dxt, j.out.g_gate, j.out.dg2 && !direct ? j.part : nullptr,
-        direct ? (T *)j.out.dg2 : nullptr);
+        direct ? (T *)j.out.dg2 : nullptr, tb);
+  };
+  auto token = [&](auto rr) {
+    if (splits == 1) launch(rr, std::true_type{});
+    else launch(rr, std::false_type{});
   };
   if (d <= 512) token(std::integral_constant<int, 1>{});
   else if (d <= 1024) token(std::integral_constant<int, 2>{});
