@@ -745,6 +745,17 @@ __device__ __forceinline__ BigTile row_col_tile(const TileScan &g, int t, int ny
   return r;
 }
 
+// An accumulator's values, read where they are used: left to itself the compiler copies
+// all of them to vector registers at once, and spills.
+__device__ __forceinline__ f32x4_t acc_get(const f32x4_t &a) {
+  f32x4_t v;
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[0]) : "a"(a[0]));
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[1]) : "a"(a[1]));
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[2]) : "a"(a[2]));
+  asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[3]) : "a"(a[3]));
+  return v;
+}
+
 // Shared by the products over row tiles of 256: out [rows][..] of A's 256 rows (columns of a
 // weight) against the rows of a tile.
 struct RowsBase {
@@ -885,62 +896,66 @@ struct GateUpBig : RowsBase {
                                         int lane) const {
     const int u0 = t.m0 + wm * 64, f = a.f;
     if (u0 >= f) return;
-    // Four row blocks at a time, their q in flight together.  The lane's 8 units of each half
-    // of the wave's 64: their q (256 bytes a row) are read before dG and dU take their place;
-    // nothing but the row's other three lanes touches those bytes, in the same instructions.
+    // The lane's 8 units of each half of the wave's 64: their q (256 bytes a row) are read before
+    // dG and dU take their place; nothing but the row's other three lanes touches
+    // those bytes, in the same instructions.  The q of NQ row blocks are in flight, asked for before the
+    // stores of the block NQ before them: loads and stores are waited for in their order.
     const int u = 8 * (lane >> 4);
     constexpr int NQ = 4;
+    f32x4_t q[NQ][2][2];
+    float p[NQ];
+    auto load = [&](int ni) __attribute__((always_inline)) {
+      const int r = wn * 128 + ni * 16 + (lane & 15);
+      const int64_t pos = t.p0 + (r < t.rows ? r : 0);  // (the first row's are read, and not used)
+      const float *qr = (const float *)a.dGU + pos * f + u0 + u;
+      p[ni % NQ] = a.gate[pos];
 #pragma unroll
-    for (int n0 = 0; n0 < NI; n0 += NQ) {
-      f32x4_t q[NQ][2][2];
-      float p[NQ];
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        const int r = wn * 128 + (n0 + n) * 16 + (lane & 15);
-        const int64_t pos = t.p0 + (r < t.rows ? r : 0);  // (the first row's are read, and not used)
-        const float *qr = (const float *)a.dGU + pos * f + u0 + u;
-        p[n] = a.gate[pos];
+        for (int h = 0; h < 2; ++h) q[ni % NQ][j][h] = *(const f32x4_t *)(qr + 32 * j + 4 * h);
+    };
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+    for (int ni = 0; ni < NQ; ++ni) load(ni);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) q[n][j][h] = *(const f32x4_t *)(qr + 32 * j + 4 * h);
+    for (int ni = 0; ni < NI; ++ni) {
+      const int r = wn * 128 + ni * 16 + (lane & 15), n = ni % NQ;
+      const int64_t pos = t.p0 + r;
+      const bool in = r < t.rows;
+      float gs = 0.f;
+      uint4 wg[2], wu[2], wh[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        Hidden h[8];
+        const f32x4_t G[2] = {acc_get(acc[2 * j][ni]), acc_get(acc[2 * j + 1][ni])};
+        const f32x4_t U[2] = {acc_get(acc[4 + 2 * j][ni]), acc_get(acc[5 + 2 * j][ni])};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          h[i] = hidden_grad<true>(G[i >> 2][i & 3], U[i >> 2][i & 3], q[n][j][i >> 2][i & 3], p[n]);
+          gs += h[i].gq;
+        }
+        wg[j] = make_uint4(pk_bf16(h[0].dg, h[1].dg), pk_bf16(h[2].dg, h[3].dg),
+                           pk_bf16(h[4].dg, h[5].dg), pk_bf16(h[6].dg, h[7].dg));
+        wu[j] = make_uint4(pk_bf16(h[0].du, h[1].du), pk_bf16(h[2].du, h[3].du),
+                           pk_bf16(h[4].du, h[5].du), pk_bf16(h[6].du, h[7].du));
+        wh[j] = make_uint4(pk_bf16(h[0].hp, h[1].hp), pk_bf16(h[2].hp, h[3].hp),
+                           pk_bf16(h[4].hp, h[5].hp), pk_bf16(h[6].hp, h[7].hp));
       }
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        const int ni = n0 + n, r = wn * 128 + ni * 16 + (lane & 15);
-        const int64_t pos = t.p0 + r;
-        const bool in = r < t.rows;
-        float gs = 0.f;
-        uint4 wg[2], wu[2], wh[2];
+      __builtin_amdgcn_sched_barrier(0);
+      if (ni + NQ < NI) load(ni + NQ);
+      __builtin_amdgcn_sched_barrier(0);
+      gs += __shfl_xor(gs, 16, 64);
+      gs += __shfl_xor(gs, 32, 64);
+      if (in) {
+        bf16 *o = (bf16 *)a.dGU + pos * (2 * f) + 2 * u0 + u;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          Hidden h[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int mi = 2 * j + (i >> 2);
-            h[i] = hidden_grad<true>(acc[mi][ni][i & 3], acc[4 + mi][ni][i & 3], q[n][j][i >> 2][i & 3], p[n]);
-            gs += h[i].gq;
-          }
-          wg[j] = make_uint4(pk_bf16(h[0].dg, h[1].dg), pk_bf16(h[2].dg, h[3].dg),
-                             pk_bf16(h[4].dg, h[5].dg), pk_bf16(h[6].dg, h[7].dg));
-          wu[j] = make_uint4(pk_bf16(h[0].du, h[1].du), pk_bf16(h[2].du, h[3].du),
-                             pk_bf16(h[4].du, h[5].du), pk_bf16(h[6].du, h[7].du));
-          wh[j] = make_uint4(pk_bf16(h[0].hp, h[1].hp), pk_bf16(h[2].hp, h[3].hp),
-                             pk_bf16(h[4].hp, h[5].hp), pk_bf16(h[6].hp, h[7].hp));
+          *(uint4 *)(o + 32 * j) = wg[j];
+          *(uint4 *)(o + 64 + 32 * j) = wu[j];
+          if (a.Hp) *(uint4 *)((bf16 *)a.Hp + pos * f + u0 + 32 * j + u) = wh[j];
         }
-        if (in) {
-          bf16 *o = (bf16 *)a.dGU + pos * (2 * f) + 2 * u0 + u;
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            *(uint4 *)(o + 32 * j) = wg[j];
-            *(uint4 *)(o + 64 + 32 * j) = wu[j];
-            if (a.Hp) *(uint4 *)((bf16 *)a.Hp + pos * f + u0 + 32 * j + u) = wh[j];
-          }
-        }
-        gs += __shfl_xor(gs, 16, 64);
-        gs += __shfl_xor(gs, 32, 64);
-        if (in && lane < 16) a.gpart[pos * a.GP + u0 / 64] = gs;
+        if (lane < 16) a.gpart[pos * a.GP + u0 / 64] = gs;
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 };
@@ -1043,7 +1058,7 @@ struct WeightBig {
       for (int j = 0; j < MI / 2; ++j) {
         const int m = t.m0 + wm * 128 + j * 32;
         if (m >= M) continue;
-        const f32x4_t x = acc[2 * j][ni], y = acc[2 * j + 1][ni];
+        const f32x4_t x = acc_get(acc[2 * j][ni]), y = acc_get(acc[2 * j + 1][ni]);
         *(uint4 *)(o + m) = pair_rows(make_uint2(pk_bf16(x[0], x[1]), pk_bf16(x[2], x[3])),
                                       make_uint2(pk_bf16(y[0], y[1]), pk_bf16(y[2], y[3])));
       }
