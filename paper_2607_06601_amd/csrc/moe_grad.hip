@@ -53,32 +53,38 @@ __device__ __forceinline__ PadScan pad_scan(const int32_t *cnt, int E) {
   return g;
 }
 
-// Row tile t of BN padded rows: its expert, first padded row and rows (a multiple of 64).
+// Tile L of (row tiles of BN padded rows) x n columns: within an expert the row tiles of a
+// column are neighbours, so that they read its weights at the same time (160M, 1152 tokens: all
+// columns of a row tile in a row 126 us, so 116; 1.3B, 500 tokens 901, 835).
 struct RowTile {
-  int e, p0, rows;
+  int e, p0, col;
   int l0, valid;  // first list entry, rows that are not padding
 };
 template <int BN>
-__device__ __forceinline__ bool row_tile(const PadScan &g, int t, RowTile &r, int &total) {
+__device__ __forceinline__ int row_tiles(const PadScan &g, int n, int &incl) {
   const int lane = threadIdx.x & 63;
-  const int nt = (g.pc + BN - 1) / BN;
-  int incl = nt;
+  incl = (g.pc + BN - 1) / BN;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const int x = __shfl_up(incl, d, 64);
     if (lane >= d) incl += x;
   }
-  total = __shfl(incl, 63, 64);
-  const uint64_t m = __ballot(incl > t);
-  if (!m) return false;
+  return __builtin_amdgcn_readfirstlane(__shfl(incl, 63, 64)) * n;
+}
+template <int BN>
+__device__ __forceinline__ RowTile row_tile(const PadScan &g, int incl, int n, int L) {
+  const int nt = (g.pc + BN - 1) / BN;
+  const uint64_t m = __ballot(incl * n > L);
   const int l = __ffsll((unsigned long long)m) - 1;
-  const int i = t - (__shfl(incl, l, 64) - __shfl(nt, l, 64));
+  const int nte = __builtin_amdgcn_readfirstlane(__shfl(nt, l, 64));
+  const int x = __builtin_amdgcn_readfirstlane(L - (__shfl(incl, l, 64) - nte) * n), i = x % nte;
+  RowTile r;
   r.e = __builtin_amdgcn_readfirstlane(l + 1);
+  r.col = x / nte;
   r.p0 = __builtin_amdgcn_readfirstlane(__shfl(g.pad, l, 64) + i * BN);
-  r.rows = __builtin_amdgcn_readfirstlane(min(BN, __shfl(g.pc, l, 64) - i * BN));
   r.l0 = __builtin_amdgcn_readfirstlane(__shfl(g.list, l, 64) + i * BN);
   r.valid = __builtin_amdgcn_readfirstlane(min(BN, __shfl(g.c, l, 64) - i * BN));
-  return true;
+  return r;
 }
 
 // ------------------------------------------------------------------ rows
@@ -356,7 +362,8 @@ __device__ __forceinline__ Hidden hidden_grad(float G, float U, float q, float p
 // CUs share the stream of the weights and, in fp32, the products.
 // (160M, 1 token, 64 tiles: two stages 14.2 us, three 12.0, 128 tiles of 32 units 9.7; 256 x 512 in
 // fp32, 128 tokens, 48 tiles: 19.2, 96 of 32 units 12.9; 410M, 333 tokens, 704 tiles, two
-// blocks a CU with two stages 46 us, one with three 50.)
+// blocks a CU with two stages 46 us, one with three 50.  Tiles of 128 rows, one block a CU: 1.0 to 1.2
+// times the time at 30 to 400 rows an expert.)
 constexpr int HID_R = 64;
 template <typename T, int HID_F, int HID_S>
 __global__ __launch_bounds__(512) void moe_grad_hidden_kernel(MoeGradArgs a, int nf) {
@@ -366,18 +373,17 @@ __global__ __launch_bounds__(512) void moe_grad_hidden_kernel(MoeGradArgs a, int
   constexpr int MI = C2::MI, NI = C2::NI, ES = sizeof(T);
   __shared__ __align__(1024) uint8_t smem[HID_S * (C1::STAGE + C2::STAGE)];
   const PadScan ps = pad_scan(a.cnt, a.E);
-  RowTile t;
-  int nt;
-  row_tile<HID_R>(ps, 0, t, nt);
-  const int total = nt * nf;
+  int incl;
+  const int total = row_tiles<HID_R>(ps, nf, incl);
   if (int(blockIdx.x) >= total) return;
-  const int L = xcd_tile(blockIdx.x, total);
-  row_tile<HID_R>(ps, L / nf, t, nt);
-  const int f0 = (L % nf) * HID_F;
+  const RowTile t = row_tile<HID_R>(ps, incl, nf, xcd_tile(blockIdx.x, total));
+  const int f0 = t.col * HID_F;
   const int d = a.d, f = a.f, steps = d / C1::KB;
   const int lane = threadIdx.x & 63, w8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wave = w8 & 3, wm = wave / WN, wn = wave % WN;
   auto along = [](int kt) { return int64_t(kt) * 128; };
+  // (padding: one line, read again, instead of rows of zeros; 1.3B, 100 tokens 746 us, 729)
+  auto row = [&](int r) { return r < t.valid ? r : 0; };
   f32x4_t(*qs)[64] = (f32x4_t(*)[64])(smem + HID_S * C1::STAGE) + wave * MI * NI;  // [block][lane]
   if (w8 >= 4) {
     const T *Wd = (const T *)a.Wd + int64_t(t.e - 1) * d * f + f0, *dy = (const T *)a.dy + int64_t(t.p0) * d;
@@ -385,7 +391,7 @@ __global__ __launch_bounds__(512) void moe_grad_hidden_kernel(MoeGradArgs a, int
     zero_acc(q);
     C2::run(
         smem + HID_S * C1::STAGE, wave, [&](int k, int c) { return (const uint8_t *)(Wd + int64_t(k) * f) + c * 16; },
-        [&](int r, int c) { return (const uint8_t *)(dy + int64_t(r) * d) + c * 16; },
+        [&](int r, int c) { return (const uint8_t *)(dy + int64_t(row(r)) * d) + c * 16; },
         [&](int kt) { return int64_t(kt) * (C2::KB * ES) * f; }, along, steps, q);
 #pragma unroll
     for (int i = 0; i < MI * NI; ++i) qs[i][lane] = q[i / NI][i % NI];
@@ -400,11 +406,13 @@ __global__ __launch_bounds__(512) void moe_grad_hidden_kernel(MoeGradArgs a, int
   C1::run(
       smem, wave,
       [&](int r, int c) { return Wg + (r / HID_F) * up + int64_t(r % HID_F) * ES * d + c * 16; },
-      [&](int r, int c) { return (const uint8_t *)(n2 + int64_t(r) * d) + c * 16; }, along, along, steps, gu);
+      [&](int r, int c) { return (const uint8_t *)(n2 + int64_t(row(r)) * d) + c * 16; }, along, along, steps, gu);
   __syncthreads();  // q is there
 #pragma unroll
   for (int ni = 0; ni < NI; ++ni) {
-    const int64_t pos = t.p0 + wn * (HID_R / WN) + ni * 16 + (lane & 15);  // (tiles are whole: 64 rows)
+    const int r = wn * (HID_R / WN) + ni * 16 + (lane & 15);
+    const int64_t pos = t.p0 + r;
+    const bool live = r < t.valid;  // the padding's are zeros
     const float p = a.gate[pos];
     float gs = 0.f;
 #pragma unroll
@@ -414,7 +422,8 @@ __global__ __launch_bounds__(512) void moe_grad_hidden_kernel(MoeGradArgs a, int
       Hidden h[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        h[i] = hidden_grad<ES == 2>(gu[mi][ni][i], gu[MI + mi][ni][i], q[i], p);
+        h[i] = hidden_grad<ES == 2>(live ? gu[mi][ni][i] : 0.f, live ? gu[MI + mi][ni][i] : 0.f,
+                                    live ? q[i] : 0.f, p);
         gs += h[i].gq;
       }
       T *o = (T *)a.dGU + pos * (2 * f) + (u & ~63) + u;
@@ -439,16 +448,12 @@ __device__ __forceinline__ void input_tile(const MoeGradArgs &a, uint8_t *smem, 
   using C = InputCore<T, INP_S>;
   constexpr int ES = sizeof(T), SPB = 64 / C::KB;  // steps of 64 gates (ups)
   const PadScan ps = pad_scan(a.cnt, a.E);
-  RowTile t;
-  int nt;
-  row_tile<INP_R>(ps, 0, t, nt);
-  const int total = nt * nd * splits;
+  int incl;
+  const int total = row_tiles<INP_R>(ps, nd * splits, incl);
   if (block >= total) return;
-  int L = xcd_tile(block, total);
-  const int sp = L % splits;
-  L /= splits;
-  row_tile<INP_R>(ps, L / nd, t, nt);
-  const int m0 = (L % nd) * INP_M, d = a.d, f = a.f, blocks = f / 64;
+  const RowTile t = row_tile<INP_R>(ps, incl, nd * splits, xcd_tile(block, total));
+  const int sp = t.col % splits;
+  const int m0 = (t.col / splits) * INP_M, d = a.d, f = a.f, blocks = f / 64;
   const int h0 = int(int64_t(blocks) * sp / splits), h1 = int(int64_t(blocks) * (sp + 1) / splits);
   const T *Wg = (const T *)a.Wg + (int64_t(t.e - 1) * f + h0 * 64) * d + m0;
   const T *g = (const T *)a.dGU + int64_t(t.p0) * (2 * f) + h0 * 128;
