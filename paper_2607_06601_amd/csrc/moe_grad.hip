@@ -91,6 +91,7 @@ __device__ __forceinline__ RowTile row_tile(const PadScan &g, int incl, int n, i
 // One wave per padded row: the normalised row (in fp64, rounded once, the
 // forward's arithmetic and so its bits) and the row of dx, its gate, and where its
 // assignment lies; zeros for the padding.
+constexpr int ROW_BLOCKS = 4096;  // (of 8 a CU at once; a launch is limited to 2^32 threads, the rows are not)
 template <typename T>
 __global__ __launch_bounds__(256) void moe_grad_rows_kernel(
     const T *__restrict__ x, const T *__restrict__ dx, const T *__restrict__ g,
@@ -98,50 +99,51 @@ __global__ __launch_bounds__(256) void moe_grad_rows_kernel(
     const int32_t *__restrict__ rows, int E, int k, int d, float eps, T *__restrict__ n2,
     T *__restrict__ dy, float *__restrict__ gate, int32_t *__restrict__ row_of,
     int32_t *__restrict__ list_of) {
-  const int pos = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   const int lane = threadIdx.x & 63;
   const PadScan ps = pad_scan(cnt, E);
-  if (pos >= ps.total) return;
-  const uint64_t m = __ballot(ps.pad + ps.pc > pos);
-  const int l = __ffsll((unsigned long long)m) - 1;
-  const int i = pos - __shfl(ps.pad, l, 64);
-  T *no = n2 + int64_t(pos) * d, *yo = dy + int64_t(pos) * d;
-  if (i >= __shfl(ps.c, l, 64)) {
-    const float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int c = lane * 8; c < d; c += 512) {
-      store8(no + c, z);
-      store8(yo + c, z);
+  for (int pos = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)); pos < ps.total;
+       pos += gridDim.x * 4) {
+    const uint64_t m = __ballot(ps.pad + ps.pc > pos);
+    const int l = __ffsll((unsigned long long)m) - 1;
+    const int i = pos - __shfl(ps.pad, l, 64);
+    T *no = n2 + int64_t(pos) * d, *yo = dy + int64_t(pos) * d;
+    if (i >= __shfl(ps.c, l, 64)) {
+      const float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      for (int c = lane * 8; c < d; c += 512) {
+        store8(no + c, z);
+        store8(yo + c, z);
+      }
+      if (lane == 0) gate[pos] = 0.f;
+      continue;
     }
-    if (lane == 0) gate[pos] = 0.f;
-    return;
-  }
-  const int entry = __shfl(ps.list, l, 64) + i;
-  const int a = __builtin_amdgcn_readfirstlane(rows[entry]);
-  const T *xr = x + int64_t(a / k) * d, *yr = dx + int64_t(a / k) * d;
-  double ss = 0.0;
-  for (int c = lane * 8; c < d; c += 512) {
-    float w[8];
-    load8(xr + c, w);
+    const int entry = __shfl(ps.list, l, 64) + i;
+    const int a = __builtin_amdgcn_readfirstlane(rows[entry]);
+    const T *xr = x + int64_t(a / k) * d, *yr = dx + int64_t(a / k) * d;
+    double ss = 0.0;
+    for (int c = lane * 8; c < d; c += 512) {
+      float w[8];
+      load8(xr + c, w);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) ss = fma(double(w[j]), double(w[j]), ss);
-  }
-  ss = wave_sum(ss);
-  const double r = 1.0 / sqrt(ss / double(d) + double(eps));
-  for (int c = lane * 8; c < d; c += 512) {
-    float w[8], gv[8], y[8];
-    double o[8];
-    load8(xr + c, w);
-    load8(g + c, gv);
-    load8(yr + c, y);
+      for (int j = 0; j < 8; ++j) ss = fma(double(w[j]), double(w[j]), ss);
+    }
+    ss = wave_sum(ss);
+    const double r = 1.0 / sqrt(ss / double(d) + double(eps));
+    for (int c = lane * 8; c < d; c += 512) {
+      float w[8], gv[8], y[8];
+      double o[8];
+      load8(xr + c, w);
+      load8(g + c, gv);
+      load8(yr + c, y);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = (double(w[j]) * r) * double(gv[j]);
-    store8(no + c, o);
-    store8(yo + c, y);
-  }
-  if (lane == 0) {
-    gate[pos] = egate[a];
-    row_of[a] = pos;
-    list_of[a] = entry;
+      for (int j = 0; j < 8; ++j) o[j] = (double(w[j]) * r) * double(gv[j]);
+      store8(no + c, o);
+      store8(yo + c, y);
+    }
+    if (lane == 0) {
+      gate[pos] = egate[a];
+      row_of[a] = pos;
+      list_of[a] = entry;
+    }
   }
 }
 
@@ -1432,7 +1434,7 @@ static hipError_t backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, 
   a.cnt = j.cmp.exp_cnt;
   a.E = E; a.d = d; a.f = f;
   a.GP = moe_grad_gate_parts(cfg);
-  moe_grad_rows_kernel<T><<<dim3(unsigned((rows + 3) / 4)), 256, 0, st>>>(
+  moe_grad_rows_kernel<T><<<unsigned(std::min<int64_t>((rows + 3) / 4, ROW_BLOCKS)), 256, 0, st>>>(
       (const T *)j.xt, (const T *)j.dx, (const T *)j.g2, j.egate, j.cmp.exp_cnt, j.cmp.exp_rows, E, k, d,
       cfg.rms_eps, (T *)j.n2, (T *)j.dy, j.gate, j.row_of, j.list_of);
   const int32_t *yrow_of = j.row_of;
