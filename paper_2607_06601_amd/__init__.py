@@ -10,6 +10,8 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from bisect import bisect_left, bisect_right
+from contextlib import nullcontext
 
 import torch
 
@@ -416,9 +418,10 @@ def stack_decode(cfg, B, x, psi, layers, caches, x_out, ws, seq_ids=None, stream
 # ------------------------------------------------- gradient norm and clipping
 class GradList:
     """The device list of gradient tensors (triroute_grad_list_init): ``tensors``
-    are contiguous fp32 or bf16 device tensors of any size and element
+    are contiguous fp32 or bf16 tensors of the current device, of any size and element
     alignment; ``dst`` (alike; None: the tensors themselves) takes the
-    clipped values.  The tensors are held, so the list stays valid."""
+    clipped values.  The tensors are held, so the list stays valid.  It is written on
+    ``stream``: calls on other streams have to wait for that."""
 
     def __init__(self, tensors, dst=None, stream=None):
         dst = list(tensors) if dst is None else list(dst)
@@ -436,9 +439,15 @@ class GradList:
                 raise ValueError(f"tensor {i}: destination of another type or size")
             arr[i] = GradTensor(a.data_ptr(), b.data_ptr(), a.numel(),
                                 BF16 if a.dtype == torch.bfloat16 else F32)
+        _check_overlap(self.tensors, dst)
+        self.device = self.tensors[0].device
+        if self.device.type != "cuda" or self.device.index != torch.cuda.current_device():
+            raise ValueError("GradList takes tensors of the current GPU")
         need = C.c_size_t()
         _check(lib().triroute_grad_list_bytes(arr, n, C.byref(need)))
-        self.buf = torch.empty(need.value, dtype=torch.uint8, device=self.tensors[0].device)
+        # (the memory is the stream's that writes it)
+        with torch.cuda.stream(stream) if stream is not None else nullcontext():
+            self.buf = torch.empty(need.value, dtype=torch.uint8, device=self.device)
         self.desc = GradListDesc()
         _check(lib().triroute_grad_list_init(C.byref(self.desc), arr, n, self.buf.data_ptr(),
                                              need.value, _stream(stream)))
@@ -453,27 +462,49 @@ def grad_workspace(device="cuda"):
     return torch.empty(GRAD_WS_BYTES, dtype=torch.uint8, device=device)
 
 
-def _norm_p(norm):
+def _check_overlap(tensors, dst):
+    """A destination is its own tensor, whole, or touches neither another tensor nor another
+    destination: the pieces are scaled in any order."""
+    def span(t):
+        return t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()
+
+    out = sorted((*span(t), i) for i, t in enumerate(dst) if t.numel())
+    for (_, end, i), (start, _, j) in zip(out, out[1:]):
+        if start < end:
+            raise ValueError(f"tensors {i} and {j}: destinations overlap")
+    starts = [s for s, _, _ in out]
+    for i, t in enumerate(tensors):
+        s, e = span(t)
+        if s == e:
+            continue
+        for o in out[max(0, bisect_right(starts, s) - 1):bisect_left(starts, e)]:
+            if o[1] > s and not (o[2] == i and o[:2] == (s, e)):
+                raise ValueError(f"tensor {i} overlaps the destination of tensor {o[2]}")
+
+
+def _norm_p(grads, norm, *ws):
     if norm.dtype != torch.float64 or norm.numel() != 1:
         raise ValueError("norm: one fp64 element")
+    if any(t.device != grads.device for t in (norm, *ws)):
+        raise ValueError("norm and workspace: on the gradients' device")
     return norm.data_ptr()
 
 
 def grad_norm(grads: GradList, norm, ws, norm_type=2.0, stream=None):
     """norm (fp64, one element) = the norm over all tensors of the list."""
-    _check(lib().triroute_grad_norm(grads.ref, norm_type, _norm_p(norm), _p(ws), ws.numel(),
+    _check(lib().triroute_grad_norm(grads.ref, norm_type, _norm_p(grads, norm, ws), _p(ws), ws.numel(),
                                     _stream(stream)))
 
 
 def grad_scale(grads: GradList, norm, max_norm, stream=None):
     """dst = src * min(1, max_norm / norm) for every tensor of the list."""
-    _check(lib().triroute_grad_scale(grads.ref, _norm_p(norm), max_norm, _stream(stream)))
+    _check(lib().triroute_grad_scale(grads.ref, _norm_p(grads, norm), max_norm, _stream(stream)))
 
 
 def grad_clip(grads: GradList, max_norm, norm, ws, norm_type=2.0, stream=None):
     """grad_norm, then grad_scale, in two launches."""
-    _check(lib().triroute_grad_clip(grads.ref, norm_type, max_norm, _norm_p(norm), _p(ws), ws.numel(),
-                                    _stream(stream)))
+    _check(lib().triroute_grad_clip(grads.ref, norm_type, max_norm, _norm_p(grads, norm, ws), _p(ws),
+                                    ws.numel(), _stream(stream)))
 
 
 # ------------------------------------------------------ device-side buffers

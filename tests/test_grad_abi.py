@@ -123,3 +123,36 @@ def test_binding_refuses():
             tr.GradList([f, h], dst)
     with pytest.raises(ValueError):
         tr.GradList([f], [torch.zeros(5)])
+
+
+def test_binding_refuses_overlaps_and_host_tensors():
+    """A destination that is another tensor, or another destination, in part or whole: its
+    pieces would be scaled twice or under a reader.  Tensors in host memory: no kernel may
+    be given their addresses."""
+    flat, other = torch.zeros(100), torch.zeros(100)
+    a, b, c = flat[:40], flat[40:80], flat[30:60]
+    for src, dst in (([a, a], None), ([a, c], None), ([a, b], [other[:40], other[20:60]]),
+                     ([a, b], [b, other[:40]]), ([a, b], [other[:40], a]), ([a], [flat[1:41]]),
+                     ([flat, b], [other, b])):
+        with pytest.raises(ValueError, match="overlap"):
+            tr.GradList(src, dst)
+    # none of these overlap; they are refused only for where they lie
+    empty = flat[50:50]
+    for src, dst in (([a, b], None), ([a, a], [other[:40], other[40:80]]), ([a, empty, b], None),
+                     ([a, b], [other[40:80], other[:40]]), ([flat], [other])):
+        with pytest.raises(ValueError, match="current GPU"):
+            tr.GradList(src, dst)
+
+
+def test_norm_must_lie_with_the_gradients():
+    class L:
+        ref = None
+        device = torch.device("cuda", 0)
+    norm, ws = torch.zeros(1, dtype=torch.float64), torch.zeros(tr.GRAD_WS_BYTES, dtype=torch.uint8)
+    for call in (lambda: tr.grad_norm(L, norm, ws), lambda: tr.grad_scale(L, norm, 1.0),
+                 lambda: tr.grad_clip(L, 1.0, norm, ws)):
+        with pytest.raises(ValueError, match="device"):
+            call()
+    L.device = torch.device("cpu")
+    with pytest.raises(ValueError, match="fp64"):
+        tr.grad_norm(L, norm.float(), ws)
