@@ -442,12 +442,12 @@ __global__ __launch_bounds__(512) void moe_grad_hidden_kernel(MoeGradArgs a, int
 // dn of 64 columns and 64 rows over one of `splits` parts of the sum, to its plane
 // of Y (list order).
 constexpr int INP_M = 64, INP_R = 64;
-template <typename T, int INP_S>
-using InputCore = TileCore<T, INP_M, INP_R, true, false, 1, 2, 2, INP_S>;
-template <typename T, int INP_S>
+template <typename T>
+using InputCore = TileCore<T, INP_M, INP_R, true, false, 1, 2, 2, 2>;
+template <typename T>
 __device__ __forceinline__ void input_tile(const MoeGradArgs &a, uint8_t *smem, int block, int nd, int splits,
                                            int64_t plane) {
-  using C = InputCore<T, INP_S>;
+  using C = InputCore<T>;
   constexpr int ES = sizeof(T), SPB = 64 / C::KB;  // steps of 64 gates (ups)
   const PadScan ps = pad_scan(a.cnt, a.E);
   int incl;
@@ -484,13 +484,15 @@ __device__ __forceinline__ void input_tile(const MoeGradArgs &a, uint8_t *smem, 
 
 // 128 x 128 of an expert's weight gradients (see WeightBig).  bf16: written in rows of
 // 256 bytes through LDS (with few rows it is the time of the writes; one stage and four
-// blocks a CU: 160M, 1 token 17.4 us, three blocks 20.4; 410M, 333 tokens 39.5, 45.0).
+// blocks a CU: 160M, 1 token 17.4 us, three blocks 20.4; 410M, 333 tokens 39.5, 45.0).  Two stages
+// and two blocks a CU instead, the whole pass: 160M, 1 token 43 us, 50; 2000 tokens 169, 186, in fp32
+// 867, 879; only layers of few tiles with many rows gain (256 x 512, 4 experts, 8000 tokens 81, 68).
 constexpr int WGT_T = 128;
-template <typename T, int WGT_S>
-using WeightCore = TileCore<T, WGT_T, WGT_T, true, true, 1, 2, 2, WGT_S>;
-template <typename T, int WGT_S>
+template <typename T>
+using WeightCore = TileCore<T, WGT_T, WGT_T, true, true, 1, 2, 2, 1>;
+template <typename T>
 __device__ __forceinline__ void weight_tile(const MoeGradArgs &a, uint8_t *smem, int block, int tiles) {
-  using C = WeightCore<T, WGT_S>;
+  using C = WeightCore<T>;
   constexpr int ES = sizeof(T), EC = 16 / ES;  // elements of a chunk
   const int d = a.d, f = a.f;
   const int md = (d + WGT_T - 1) / WGT_T, mf = (f + WGT_T - 1) / WGT_T;
@@ -551,20 +553,20 @@ __device__ __forceinline__ void weight_tile(const MoeGradArgs &a, uint8_t *smem,
 
 // dn alone (frozen experts), or dn's tiles (the first nin blocks) beside the weight
 // gradients', which do not wait for each other.
-template <typename T, int S>
+template <typename T>
 __global__ __launch_bounds__(256) void moe_grad_input_kernel(MoeGradArgs a, int nd, int splits, int64_t plane) {
-  __shared__ __align__(1024) uint8_t smem[S * InputCore<T, S>::STAGE];
-  input_tile<T, S>(a, smem, blockIdx.x, nd, splits, plane);
+  __shared__ __align__(1024) uint8_t smem[2 * InputCore<T>::STAGE];
+  input_tile<T>(a, smem, blockIdx.x, nd, splits, plane);
 }
-template <typename T, int WS>
-__global__ __launch_bounds__(256, sizeof(T) == 2 && WS == 1 ? 4 : 2) void moe_grad_input_weight_kernel(
+template <typename T>
+__global__ __launch_bounds__(256, 4) void moe_grad_input_weight_kernel(
     MoeGradArgs a, int nin, int nd, int splits, int64_t plane) {
-  constexpr int BI = 2 * InputCore<T, 2>::STAGE, BW = WS * WeightCore<T, WS>::STAGE;
+  constexpr int BI = 2 * InputCore<T>::STAGE, BW = WeightCore<T>::STAGE;
   __shared__ __align__(1024) uint8_t smem[BI > BW ? BI : BW];
   if (int(blockIdx.x) < nin)
-    input_tile<T, 2>(a, smem, blockIdx.x, nd, splits, plane);
+    input_tile<T>(a, smem, blockIdx.x, nd, splits, plane);
   else
-    weight_tile<T, WS>(a, smem, int(blockIdx.x) - nin, int(gridDim.x) - nin);
+    weight_tile<T>(a, smem, int(blockIdx.x) - nin, int(gridDim.x) - nin);
 }
 
 // ------------------------------------------------------- four-wave products
@@ -1477,17 +1479,9 @@ static hipError_t backward(const triroute_cfg &cfg, int N, const MoeGradJob &j, 
     if (a.Hp) {
       const int md = (d + WGT_T - 1) / WGT_T, mf = (f + WGT_T - 1) / WGT_T;
       const unsigned tiles = unsigned(E) * (md * (2 * f / WGT_T) + mf * md);
-      // (bf16 with more rows than these has gone to the large tiles)
-      if constexpr (sizeof(T) == 2)
-        moe_grad_input_weight_kernel<T, 1><<<nin + tiles, 256, 0, st>>>(a, int(nin), nd, splits, plane);
-      else if (Nk / (E + 1) < 128)
-        moe_grad_input_weight_kernel<T, 1><<<nin + tiles, 256, 0, st>>>(a, int(nin), nd, splits, plane);
-      else
-        moe_grad_input_weight_kernel<T, 2><<<nin + tiles, 256, 0, st>>>(a, int(nin), nd, splits, plane);
-    } else if (nin <= unsigned(2 * cu_count())) {
-      moe_grad_input_kernel<T, 4><<<nin, 256, 0, st>>>(a, nd, splits, plane);
+      moe_grad_input_weight_kernel<T><<<nin + tiles, 256, 0, st>>>(a, int(nin), nd, splits, plane);
     } else {
-      moe_grad_input_kernel<T, 2><<<nin, 256, 0, st>>>(a, nd, splits, plane);
+      moe_grad_input_kernel<T><<<nin, 256, 0, st>>>(a, nd, splits, plane);
     }
   }
   const int prows = moe_grad_part_rows(cfg, N), tb = token_blocks(N);
