@@ -356,7 +356,8 @@ __device__ __forceinline__ Hidden hidden_grad(float G, float U, float q, float p
 // With few rows an expert the products read each weight about once and the time
 // is that of the stream: narrow tiles over all CUs, stages in flight ahead of the one
 // in use.  The fp32 products, bound by the fp32 MFMA rate, run on the same tiles,
-// several blocks a CU.
+// several blocks a CU (160M, 2000 tokens: 96 TFLOP/s of the 154 of a large product; MFMA 69 %
+// busy, 79 while the CU has a block).
 
 // [G; U; q] of HID_F units and 64 rows: four waves make G and U while four make q, over
 // the same number of steps (and barriers), and hand it over in LDS.
@@ -570,9 +571,11 @@ __global__ __launch_bounds__(256, 4) void moe_grad_input_weight_kernel(
 }
 
 // ------------------------------------------------------- four-wave products
-// One block a CU, one wave a SIMD, tiles walked by a resident block: 128 x 128
-// wave tiles of the input and weight products (64 units x 3 and 64 rows in the
-// hidden one), so that a fragment read from LDS feeds eight MFMAs (four).  Stages of 64
+// One block a CU, one wave a SIMD, 256 x 256 tiles walked by a resident block: 128 x 128 to a
+// wave, so that a fragment read from LDS feeds eight MFMAs.  1.3B, 16384 tokens: q 700 us, gates and ups
+// 1362, dn and the weights 2890 (1020, 1045 and 1230 TFLOP/s; MFMA 53, 53 and 64 % busy at the 1.8 GHz
+// that the chip's power leaves).  The loops alone run at 1260-1450, a large library product's
+// rate; the rest is what an epilogue reads, computes and writes, 0.2 to 0.3 MB a tile.  Stages of 64
 // sum indices, two of them in LDS; the fragments of the next 32 are read
 // while the MFMAs of the present 32 issue.  The transfers run on over the
 // tiles' ends: the producer is two stages ahead in the block's list of (tile, step), whatever
@@ -1399,17 +1402,18 @@ int moe_grad_part_rows(const triroute_cfg &cfg, int N) {
   return token_blocks(N) * (cfg.d_model <= 2048 ? 1 : 4);
 }
 
-// bf16: whether the experts have rows enough for the 256-row tiles: r >= 64 of them (those of an
-// expert when the router spreads its options evenly), and units and sum indices enough that the tiles
-// fill the card, counted as rows x d x d_ff >= 1e10.  Us, small tiles / large ones: 160M, r 455
-// 191 / 209, r 568 249 / 254, r 777 298 / 265, r 910 332 / 275; 410M, r 311 240 / 297, r 455
-// 331 / 331, r 577 414 / 389, r 777 541 / 434; 1.3B, r 32 754 / 862, r 56 804 / 900, r 64
-// 1026 / 939, r 96 1187 / 987, r 256 2228 / 1240; 63 experts of 2048 x 5632, r 32 2706 / 2849,
-// r 64 3638 / 3093; one expert of 256 x 512, 16384 rows: 140 / 151.
+// bf16: whether the 256 x 256 tiles serve: where an expert has r >= 96 rows (when the router
+// spreads its options evenly), so that a tile is not mostly padding, and q's tiles, the fewest, give
+// each of the 256 CUs one.  Us, small tiles / large ones.  By tiles, T: 160M, T 192 225 / 249 and
+// 247 / 249, T 256 281 / 261 and 319 / 275; 410M, T 176 312 / 339, T 264 382 / 399, T 352
+// 490 / 437; 2048 x 5632, one expert, T 88 276 / 410, four, T 176 545 / 609; 256 x 512, four, T 104
+// 137 / 146, T 416 572 / 498; 512 x 1024, eight, T 256 240 / 208.  By r: 1.3B (T 352), r 32
+// 740 / 859, r 64 910 / 940, r 96 970 / 993, r 256 1582 / 1221; 63 experts of 768 x 2048, r 64
+// 509 / 504, r 128 653 / 580; of 2048 x 5632, r 32 2680 / 2850, r 64 3241 / 3084.
 static bool big_tiles(const triroute_cfg &cfg, int N) {
   const int64_t r = int64_t(N) * cfg.top_k / (cfg.n_experts + 1);
-  return cfg.act == TRIROUTE_BF16 && r >= 64 &&
-         double(r * cfg.n_experts) * cfg.d_model * cfg.d_ff >= 1e10;
+  return cfg.act == TRIROUTE_BF16 && r >= 96 &&
+         cfg.n_experts * ((r + 255) / 256) * ((cfg.d_ff + 255) / 256) >= 256;
 }
 // Parts of the sum of dn for few rows, so that the stream of the weights has about
 // two blocks a CU: at most 8 (a token's partial rows are loaded together), each of at least 4 blocks of 64 units
