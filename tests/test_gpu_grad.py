@@ -200,3 +200,23 @@ def test_stream_graph_and_same_bits():
     g.replay()
     torch.cuda.synchronize()
     assert norm.item() == 2 * wn
+
+
+def test_list_written_on_a_stream_of_its_own():
+    """The list is written, and its memory taken, on the stream given: what the current
+    stream still does with memory that it has freed does not reach it."""
+    src = [torch.randn(5000 + i, device=DEV) for i in range(20)]
+    want = math.sqrt(sum(float((t.double() ** 2).sum()) for t in src))
+    ws, s = tr.grad_workspace(), torch.cuda.Stream()
+    norm = torch.zeros(1, dtype=torch.float64, device=DEV)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        junk = [torch.empty(4096, dtype=torch.uint8, device=DEV) for _ in range(64)]
+        big = torch.empty(1 << 28, device=DEV).fill_(1.0)  # (the current stream is busy)
+        for t in junk:
+            t.fill_(0xFF)
+        del junk, big
+        gl = tr.GradList(src, stream=s)
+        tr.grad_norm(gl, norm, ws, stream=s)
+        torch.cuda.synchronize()
+        assert abs(norm.item() - want) <= 1e-12 * want

@@ -247,12 +247,15 @@ def test_layer_shapes_against_fp32_products(shape, N):
 # Rows and units enough for the large tiles (rows an expert >= 96, a 256 x 256 tile of rows and
 # units for each of 256 CUs): rows around the tiles, an expert without any; widths off
 # every tile, both ways; d past the widths that the tokens' part holds in registers;
-# many experts
+# many experts; sums of one and two steps
 MANY = [
     ("bf16", 14530, 704, 1216, 6, 1, [517, 1, 0, 255, 257, 4000, 9500]),
     ("bf16", 8200, 320, 2880, 2, 2, "random"),
     ("bf16", 2600, 2240, 1856, 16, 2, "random"),
     ("bf16", 1700, 640, 1984, 32, 2, "random"),
+    ("bf16", 8200, 64, 2880, 2, 2, "random"),
+    ("bf16", 8200, 128, 2880, 2, 2, "random"),
+    ("bf16", 49200, 64, 64, 2, 2, "random"),
 ]
 
 
@@ -291,3 +294,13 @@ def test_many_rows_streams_graphs_and_frozen_experts():
         for c in calls:
             for n, v in c.result().items():
                 np.testing.assert_array_equal(v, first[n], err_msg=f"{n} replay {rep}")
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+def test_one_expert_in_both_slots(act):
+    """A token whose slots name the same expert: two rows, whose gradients add."""
+    L, xt, dx, eidx, egate = moe_case(16, act, 70, 128, 192, 3, 2)
+    eidx = np.repeat(eidx[:, :1], 2, axis=1).astype(np.int32)
+    assert (eidx != 0).any()
+    ref, err = moe_backward(xt, L, eidx, egate, dx, act, bounds=True)
+    check(Call(L, xt, dx, eidx, egate, act)().result(), ref, err, f"{act} twice")
