@@ -421,7 +421,9 @@ class GradList:
     are contiguous fp32 or bf16 tensors of the current device, of any size and element
     alignment; ``dst`` (alike; None: the tensors themselves) takes the
     clipped values.  The tensors are held, so the list stays valid.  It is written on
-    ``stream``: calls on other streams have to wait for that."""
+    ``stream``: calls on other streams have to wait for that.  A list may be dropped while
+    its calls are queued, on any stream; it has to outlive the replays of a graph that holds
+    one of them."""
 
     def __init__(self, tensors, dst=None, stream=None):
         dst = list(tensors) if dst is None else list(dst)
@@ -448,6 +450,8 @@ class GradList:
         # (the memory is the stream's that writes it)
         with torch.cuda.stream(stream) if stream is not None else nullcontext():
             self.buf = torch.empty(need.value, dtype=torch.uint8, device=self.device)
+        # the streams on which the memory and the tensors are in use, as the allocator knows
+        self._known = set() if stream is not None else {torch.cuda.current_stream().cuda_stream}
         self.desc = GradListDesc()
         _check(lib().triroute_grad_list_init(C.byref(self.desc), arr, n, self.buf.data_ptr(),
                                              need.value, _stream(stream)))
@@ -455,6 +459,14 @@ class GradList:
     @property
     def ref(self):
         return C.byref(self.desc)
+
+    def used_on(self, stream):
+        """A call of ``stream`` reads the list and its tensors: where that is another stream
+        than theirs, their memory goes to no other tensor before the call is done."""
+        if stream.cuda_stream not in self._known:
+            self._known.add(stream.cuda_stream)
+            for t in (self.buf, *self.tensors, *self.dst):
+                t.record_stream(stream)
 
 
 def grad_workspace(device="cuda"):
@@ -490,21 +502,27 @@ def _norm_p(grads, norm, *ws):
     return norm.data_ptr()
 
 
+def _grad_stream(grads, stream):
+    stream = torch.cuda.current_stream() if stream is None else stream
+    grads.used_on(stream)
+    return _stream(stream)
+
+
 def grad_norm(grads: GradList, norm, ws, norm_type=2.0, stream=None):
     """norm (fp64, one element) = the norm over all tensors of the list."""
     _check(lib().triroute_grad_norm(grads.ref, norm_type, _norm_p(grads, norm, ws), _p(ws), ws.numel(),
-                                    _stream(stream)))
+                                    _grad_stream(grads, stream)))
 
 
 def grad_scale(grads: GradList, norm, max_norm, stream=None):
     """dst = src * min(1, max_norm / norm) for every tensor of the list."""
-    _check(lib().triroute_grad_scale(grads.ref, _norm_p(grads, norm), max_norm, _stream(stream)))
+    _check(lib().triroute_grad_scale(grads.ref, _norm_p(grads, norm), max_norm, _grad_stream(grads, stream)))
 
 
 def grad_clip(grads: GradList, max_norm, norm, ws, norm_type=2.0, stream=None):
     """grad_norm, then grad_scale, in two launches."""
     _check(lib().triroute_grad_clip(grads.ref, norm_type, max_norm, _norm_p(grads, norm, ws), _p(ws),
-                                    ws.numel(), _stream(stream)))
+                                    ws.numel(), _grad_stream(grads, stream)))
 
 
 # ------------------------------------------------------ device-side buffers

@@ -220,3 +220,29 @@ def test_list_written_on_a_stream_of_its_own():
         tr.grad_norm(gl, norm, ws, stream=s)
         torch.cuda.synchronize()
         assert abs(norm.item() - want) <= 1e-12 * want
+
+
+def test_list_dropped_while_a_call_on_another_stream_is_queued():
+    """Its memory, and that of tensors which only the list held, goes to no other tensor
+    before the call is done."""
+    s = torch.cuda.Stream()
+    for n in (1, 40):
+        src = [torch.randn(3000 + i, device=DEV) for i in range(n)]
+        want = math.sqrt(sum(float((t.double() ** 2).sum()) for t in src))
+        norm, ws = torch.zeros(1, dtype=torch.float64, device=DEV), tr.grad_workspace()
+        busy = torch.empty(1 << 29, device=DEV)
+        torch.cuda.synchronize()
+        gl = tr.GradList(src)
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            for i in range(50):
+                busy.fill_(i)
+        tr.grad_clip(gl, 1.0, norm, ws, stream=s)
+        held = {gl.buf.data_ptr()} | {t.data_ptr() for t in src}
+        sizes = [gl.buf.numel()] + [4 * t.numel() for t in src]
+        del gl, src
+        new = [torch.empty(b, dtype=torch.uint8, device=DEV) for b in sizes for _ in range(4)]
+        if not s.query():  # the call is still queued
+            assert not held & {t.data_ptr() for t in new}
+        torch.cuda.synchronize()
+        assert abs(norm.item() - want) <= 1e-12 * want

@@ -156,3 +156,69 @@ def test_norm_must_lie_with_the_gradients():
     L.device = torch.device("cpu")
     with pytest.raises(ValueError, match="fp64"):
         tr.grad_norm(L, norm.float(), ws)
+
+
+class FakeStream:
+    device = torch.device("cuda", 0)
+
+    def __init__(self, handle):
+        self.cuda_stream = handle
+
+
+class FakeTensor:
+    """What the binding asks of a tensor on a GPU."""
+    device, dtype = torch.device("cuda", 0), torch.float64
+
+    def __init__(self, numel=1):
+        self.n, self.streams = numel, []
+
+    def numel(self):
+        return self.n
+
+    def data_ptr(self):
+        return FAKE
+
+    def record_stream(self, stream):
+        self.streams.append(stream.cuda_stream)
+
+
+class FakeLib:
+    """Entry points that launch nothing."""
+
+    def __init__(self):
+        self.streams = []
+
+    def __getattr__(self, name):
+        return lambda *a: self.streams.append(a[-1]) or 0
+
+
+@pytest.fixture
+def fake_list(monkeypatch):
+    """A list of two tensors as its constructor leaves it on stream 7, and the calls'
+    arguments: no GPU is touched."""
+    g = object.__new__(tr.GradList)
+    a, b, c = FakeTensor(), FakeTensor(), FakeTensor()
+    g.tensors, g.dst, g.buf, g.device, g.desc = [a, b], [a, c], FakeTensor(), a.device, tr.GradListDesc()
+    g._known = {7}
+    lib = FakeLib()
+    monkeypatch.setattr(tr, "lib", lambda: lib)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: FakeStream(7))
+    norm, ws = FakeTensor(), FakeTensor(tr.GRAD_WS_BYTES)
+    calls = [lambda **k: tr.grad_norm(g, norm, ws, **k), lambda **k: tr.grad_scale(g, norm, 1.0, **k),
+             lambda **k: tr.grad_clip(g, 1.0, norm, ws, **k)]
+    return g, lib, calls
+
+
+@pytest.mark.parametrize("which", range(3))
+def test_calls_on_other_streams_hold_the_memory_of_list_and_tensors(fake_list, which):
+    """The list's memory holds addresses that kernels read and write: given to another tensor
+    while a call is queued, they would be any."""
+    g, lib, calls = fake_list
+    held = (g.buf, *g.tensors, *g.dst)
+    calls[which]()
+    assert lib.streams == [7] and not any(t.streams for t in held)
+    calls[which](stream=FakeStream(9))
+    assert lib.streams == [7, 9] and all(set(t.streams) == {9} for t in held)
+    calls[which](stream=FakeStream(11))
+    assert lib.streams == [7, 9, 11] and all(set(t.streams) == {9, 11} for t in held)
