@@ -426,8 +426,8 @@ class GradList:
     one of them."""
 
     def __init__(self, tensors, dst=None, stream=None):
-        dst = list(tensors) if dst is None else list(dst)
-        self.tensors, self.dst = list(tensors), dst
+        self.tensors = list(tensors)
+        self.dst = dst = list(self.tensors if dst is None else dst)
         n = len(self.tensors)
         if n == 0 or len(dst) != n:
             raise ValueError("GradList takes one or more tensors and as many destinations")

@@ -222,3 +222,12 @@ def test_calls_on_other_streams_hold_the_memory_of_list_and_tensors(fake_list, w
     assert lib.streams == [7, 9] and all(set(t.streams) == {9} for t in held)
     calls[which](stream=FakeStream(11))
     assert lib.streams == [7, 9, 11] and all(set(t.streams) == {9, 11} for t in held)
+
+
+def test_list_takes_any_iterable():
+    """Such as the gradients of a module's parameters; host tensors are refused only for
+    where they lie."""
+    t = [torch.zeros(4), torch.zeros(5, dtype=torch.bfloat16)]
+    for args in ((iter(t),), (iter(t), iter([x.clone() for x in t])), (tuple(t), None)):
+        with pytest.raises(ValueError, match="current GPU"):
+            tr.GradList(*args)
