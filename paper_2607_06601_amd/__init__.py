@@ -445,6 +445,8 @@ class GradList:
         self.device = self.tensors[0].device
         if self.device.type != "cuda" or self.device.index != torch.cuda.current_device():
             raise ValueError("GradList takes tensors of the current GPU")
+        if stream is not None and stream.device != self.device:
+            raise ValueError("stream: one of the tensors' device")
         need = C.c_size_t()
         _check(lib().triroute_grad_list_bytes(arr, n, C.byref(need)))
         # (the memory is the stream's that writes it)
@@ -503,7 +505,11 @@ def _norm_p(grads, norm, *ws):
 
 
 def _grad_stream(grads, stream):
+    if torch.cuda.current_device() != grads.device.index:
+        raise ValueError("the list's tensors do not lie on the current GPU")
     stream = torch.cuda.current_stream() if stream is None else stream
+    if stream.device != grads.device:
+        raise ValueError("stream: one of the gradients' device")
     grads.used_on(stream)
     return _stream(stream)
 

@@ -231,3 +231,30 @@ def test_list_takes_any_iterable():
     for args in ((iter(t),), (iter(t), iter([x.clone() for x in t])), (tuple(t), None)):
         with pytest.raises(ValueError, match="current GPU"):
             tr.GradList(*args)
+
+
+@pytest.mark.parametrize("which", range(3))
+def test_calls_refuse_another_current_device_and_its_streams(fake_list, which, monkeypatch):
+    """A launch goes to the current device, whose streams do not order the list's memory."""
+    g, lib, calls = fake_list
+    other = FakeStream(9)
+    other.device = torch.device("cuda", 1)
+    with pytest.raises(ValueError, match="device"):
+        calls[which](stream=other)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for kw in ({}, dict(stream=FakeStream(9))):
+        with pytest.raises(ValueError, match="current GPU"):
+            calls[which](**kw)
+    assert lib.streams == []
+
+
+def test_list_refuses_a_stream_of_another_device(monkeypatch):
+    """(host tensors, called the current GPU's)"""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+
+    class OnGpu(torch.Tensor):
+        device = torch.device("cuda", 0)
+    other = FakeStream(9)
+    other.device = torch.device("cuda", 1)
+    with pytest.raises(ValueError, match="stream"):
+        tr.GradList([torch.zeros(4).as_subclass(OnGpu)], stream=other)
