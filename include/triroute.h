@@ -588,7 +588,8 @@ int triroute_moe_backward(const triroute_cfg *cfg, int n_tok, const void *xt,
 
 /* One gradient tensor: numel elements (0 or more) of type dtype (enum triroute_dtype) at src, aligned
  * to its element; dst (the same size and type, aligned alike; NULL if the list is
- * only measured) takes the clipped values and is src itself or overlaps no tensor's src. */
+ * only measured) takes the clipped values and is src itself or overlaps no tensor's src.
+ * Destinations do not overlap each other: a tensor that is scaled in place is listed once. */
 typedef struct triroute_grad_tensor {
   const void *src;
   void *dst;
@@ -613,7 +614,8 @@ typedef struct triroute_grad_list {
 /* Bytes of the list of n tensors (tensors: host array; 1 <= n <= 2^20). */
 int triroute_grad_list_bytes(const triroute_grad_tensor *tensors, int n, size_t *bytes);
 /* Writes the list of n tensors into base (>= list_bytes, 256-byte aligned) on
- * `stream`; `tensors` is a host array that is not read after the call. */
+ * `stream`; `tensors` is a host array that is not read after the call.  Overlapping
+ * destinations are refused with TRIROUTE_E_INVALID. */
 int triroute_grad_list_init(triroute_grad_list *list, const triroute_grad_tensor *tensors, int n,
                             void *base, size_t bytes, triroute_stream_t stream);
 /* *norm (device fp64) = the norm over all elements of all tensors: norm_type 2: the

@@ -6,9 +6,11 @@
 #include <stdio.h>
 
 #include <algorithm>
+#include <memory>
 #include <string.h>
 
 #include <mutex>
+#include <new>
 
 #include <initializer_list>
 
@@ -391,6 +393,38 @@ int check_grads(const triroute_grad_tensor *t, int n, int64_t *pieces) {
     sum += tr::grad_pieces(t[i]);
   }
   *pieces = sum;
+  return TRIROUTE_OK;
+}
+
+// Pieces are scaled in any order: a destination is its own source, whole, or touches neither
+// another destination nor any source.
+int check_grad_overlap(const triroute_grad_tensor *t, int n) {
+  struct Span {
+    uintptr_t from, to;
+    int i;
+  };
+  auto span = [&](const void *p, int i) {
+    return Span{uintptr_t(p), uintptr_t(p) + size_t(t[i].numel) * (t[i].dtype == TRIROUTE_BF16 ? 2 : 4), i};
+  };
+  const std::unique_ptr<Span[]> out(new (std::nothrow) Span[n]);
+  REQUIRE(out, TRIROUTE_E_INVALID, "no host memory to check %d tensors", n);
+  int m = 0;
+  for (int i = 0; i < n; ++i)
+    if (t[i].dst && t[i].numel > 0) out[m++] = span(t[i].dst, i);
+  std::sort(out.get(), out.get() + m, [](const Span &a, const Span &b) { return a.from < b.from; });
+  for (int i = 1; i < m; ++i)
+    REQUIRE(out[i].from >= out[i - 1].to, TRIROUTE_E_INVALID, "destinations of tensors %d and %d overlap",
+            out[i - 1].i, out[i].i);
+  for (int i = 0; i < n; ++i) {
+    if (t[i].numel <= 0) continue;
+    const Span s = span(t[i].src, i);
+    // (they do not overlap, so their ends are in order too)
+    const Span *o = std::upper_bound(out.get(), out.get() + m, s.from,
+                                     [](uintptr_t from, const Span &a) { return from < a.to; });
+    for (; o != out.get() + m && o->from < s.to; ++o)
+      REQUIRE(o->i == i && o->from == s.from, TRIROUTE_E_INVALID,
+              "tensor %d overlaps the destination of tensor %d", i, o->i);
+  }
   return TRIROUTE_OK;
 }
 
@@ -1201,6 +1235,7 @@ int triroute_grad_list_init(triroute_grad_list *list, const triroute_grad_tensor
   REQUIRE(list && tensors && base, TRIROUTE_E_INVALID, "NULL argument");
   int64_t pieces = 0;
   TRY(check_grads(tensors, n, &pieces));
+  TRY(check_grad_overlap(tensors, n));
   const size_t need = align256(size_t(std::max<int64_t>(pieces, 1)) * sizeof(tr::GradRec));
   REQUIRE(bytes >= need, TRIROUTE_E_WORKSPACE, "list memory %zu bytes < %zu needed", bytes, need);
   REQUIRE((uintptr_t(base) & 255) == 0, TRIROUTE_E_INVALID, "list memory must be 256-byte aligned");

@@ -258,3 +258,57 @@ def test_list_refuses_a_stream_of_another_device(monkeypatch):
     other.device = torch.device("cuda", 1)
     with pytest.raises(ValueError, match="stream"):
         tr.GradList([torch.zeros(4).as_subclass(OnGpu)], stream=other)
+
+
+def grad_list_init(*ts):
+    """Into no memory at all: a list that is right is refused only for that, and nothing is
+    launched."""
+    d = tr.GradListDesc()
+    r = tr.lib().triroute_grad_list_init(C.byref(d), (tr.GradTensor * len(ts))(*ts), len(ts), FAKE, 0, None)
+    assert d.base is None
+    return r, tr.lib().triroute_last_error()
+
+
+A, B = FAKE, FAKE + (1 << 20)
+HALF = tr.BF16
+
+
+@pytest.mark.parametrize("ts", [
+    [tensor(A, A), tensor(A, A)],                                   # one tensor twice, in place
+    [tensor(A, A), tensor(A + 396, A + 396)],                       # .. the last element shared
+    [tensor(A, A, dtype=HALF), tensor(A + 198, B, dtype=HALF)],
+    [tensor(A, B), tensor(A + 400, B)],                             # one destination for two
+    [tensor(A, B), tensor(A + 400, B + 4)],
+    [tensor(A, A + 200)],                                           # over a part of its own source
+    [tensor(A + 200, A)],
+    [tensor(A, A + 400), tensor(A + 400, B)],                       # over another's source
+    [tensor(A, B), tensor(B + 396, A + 800)],
+    [tensor(A, B, numel=4000), tensor(B + 16, A + 40000, numel=1)],  # .. one far inside it
+    [tensor(A, A), tensor(A, None, numel=1)],                       # measured while it is scaled
+    [tensor(A, B), tensor(A + 8000, A + 400), tensor(A + 796, A + 4000)],
+])
+def test_grad_list_refuses_overlaps(ts):
+    for order in (ts, ts[::-1]):
+        r, why = grad_list_init(*order)
+        assert r == -1 and b"overlap" in why, (r, why)
+
+
+@pytest.mark.parametrize("ts", [
+    [tensor(A, A)],
+    [tensor(A, A), tensor(A + 400, A + 400)],                       # one behind the other
+    [tensor(A, B), tensor(A, B + 400)],                             # one source for two
+    [tensor(A, None), tensor(A, None), tensor(A + 4, None)],        # only measured
+    [tensor(A, B), tensor(A + 400, A + 800), tensor(B + 400, B + 800)],
+    [tensor(A, A), tensor(A, A, numel=0), tensor(A + 8, A + 12, numel=0)],
+    [tensor(A, A, dtype=HALF), tensor(A + 200, A + 200, dtype=HALF), tensor(A + 400, A + 400)],
+])
+def test_grad_list_takes_neighbours(ts):
+    for order in (ts, ts[::-1]):
+        assert grad_list_init(*order)[0] == -3
+
+
+def test_grad_list_of_many_tensors():
+    ts = [tensor(A + 1000 * i, B * 2 + 1000 * i, numel=250) for i in range(5000)]
+    assert grad_list_init(*ts)[0] == -3
+    ts[4321] = tensor(A + 1000 * 4321, ts[17].dst + 996, numel=250)
+    assert grad_list_init(*ts)[0] == -1
