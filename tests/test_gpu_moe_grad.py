@@ -12,7 +12,7 @@ from oracle.moe_grad import moe_backward
 from paper_2607_06601_amd.device import to_dev
 
 from _common import note, npy, torch_act
-from _moe_grad import lists, moe_case
+from _moe_grad import lists, moe_case, reference, whole_tensor_ratios
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -304,3 +304,16 @@ def test_one_expert_in_both_slots(act):
     assert (eidx != 0).any()
     ref, err = moe_backward(xt, L, eidx, egate, dx, act, bounds=True)
     check(Call(L, xt, dx, eidx, egate, act)().result(), ref, err, f"{act} twice")
+
+
+@pytest.mark.parametrize("act,N,d,f,E,k,choice", [c for c in CASES + MANY if c[1] >= 256])
+def test_whole_tensors(act, N, d, f, E, k, choice):
+    """Lost work that hides within the elements' bounds, which grow with the rows."""
+    print(f"moe backward {act} N={N} d={d} f={f} E={E} k={k}", flush=True)
+    c = Call(*moe_case(17, act, N, d, f, E, k, choice), act)()
+    torch.cuda.synchronize()
+    ratios = whole_tensor_ratios(c.out, reference(c.t), c.t["eidx"], act)
+    assert len(ratios) > 3
+    for key, v in ratios.items():
+        note(f"{act} {N}x{d}x{f} {key}", v)
+    assert max(ratios.values()) <= 1.0, ratios

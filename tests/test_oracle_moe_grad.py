@@ -7,7 +7,7 @@ import torch
 import oracle
 from oracle.moe_grad import moe_backward
 
-from _moe_grad import forward, moe_case
+from _moe_grad import forward, moe_case, reference, whole_tensor_ratios
 
 
 def scalar(L, xt, dx, eidx, egate):
@@ -82,3 +82,40 @@ def test_bounds_cover_a_rounded_run():
         dW[e - 1] = bf(dG.T @ n32)
     ratio = np.abs(dW - g["dWgate"]) / err["dWgate"]
     assert 0.05 < ratio.max() <= 1.0
+
+
+def tensors(L, xt, dx, eidx, egate, dtype):
+    t = {n: torch.tensor(np.asarray(v, np.float32)).to(dtype)
+         for n, v in dict(xt=xt, dx=dx, **{n: L[n] for n in ("g2", "Wg", "Wu", "Wd")}).items()}
+    return dict(t, eidx=torch.tensor(eidx), egate=torch.tensor(egate))
+
+
+@pytest.mark.parametrize("act,dtype", [("bf16", torch.bfloat16), ("f32", torch.float32)])
+def test_torch_reference_equals_the_oracle(act, dtype):
+    case = moe_case(6, act, 300, 64, 128, 4, 2)
+    want = moe_backward(case[1], case[0], case[3], case[4], case[2], act)
+    got = reference(tensors(*case, dtype))
+    for name in want:
+        np.testing.assert_allclose(got[name].numpy(), want[name], rtol=1e-9, atol=1e-11, err_msg=name)
+
+
+@pytest.mark.parametrize("N,d,f", [(49200, 64, 64), (8200, 128, 320)])
+def test_whole_tensors_show_lost_work(N, d, f):
+    """Rounded once they pass; a step of 64 rows that the weight gradients of one expert miss, or
+    a block's tokens that dg2 misses, do not (each element may stay inside its own
+    bound, which grows with the rows while the sum grows with their root)."""
+    case = moe_case(7, "bf16", N, d, f, 2, 2)
+    t = tensors(*case, torch.bfloat16)
+    ref = reference(t)
+
+    def ratios(g):
+        return whole_tensor_ratios({n: v if n == "g_gate" else v.bfloat16() for n, v in g.items()}, ref,
+                                   t["eidx"], "bf16")
+    right = ratios(ref)
+    assert len(right) == 9 and 0 < max(right.values()) <= 1
+    rows = int((t["eidx"] == 2).sum())
+    for lo in (0, rows // 128 * 64):
+        bad = ratios(reference(t, skip_rows=(2, lo, lo + 64)))
+        assert {k for k, v in bad.items() if v > 1} == {(n, 2) for n in ("dWgate", "dWup", "dWdown")}
+    block = torch.arange(N) // 4 % 512 == 77
+    assert {k for k, v in ratios(reference(t, skip_tokens=block)).items() if v > 1} == {"dg2"}
