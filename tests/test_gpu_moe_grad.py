@@ -317,3 +317,31 @@ def test_whole_tensors(act, N, d, f, E, k, choice):
     for key, v in ratios.items():
         note(f"{act} {N}x{d}x{f} {key}", v)
     assert max(ratios.values()) <= 1.0, ratios
+
+
+# The hidden product's tiles, by their number against the 256 CUs: 32 units and four stages while
+# there are no more of those than CUs, then 64 units with three stages, then with two; each in
+# both types, with rows around the tiles, an expert without any, odd widths, a layer's own
+HIDDEN = [
+    ((32, 4), "f32", 60, 192, 832, 3, 2, "random"),
+    ((64, 3), "f32", 1200, 128, 320, 4, 2, "random"),
+    ((64, 3), "f32", 700, 64, 832, 5, 1, [5, 63, 0, 65, 127, 440]),
+    ((64, 3), "f32", 3, 768, 2048, 8, 2, "random"),
+    ((64, 2), "f32", 2000, 192, 832, 3, 2, "random"),
+    ((64, 2), "f32", 1500, 320, 1088, 5, 1, [9, 191, 0, 193, 1, 1106]),
+    ((64, 2), "f32", 300, 768, 2048, 3, 2, "random"),
+    ((32, 4), "bf16", 60, 192, 832, 3, 2, "random"),
+    ((64, 3), "bf16", 700, 64, 832, 5, 1, [5, 63, 0, 65, 127, 440]),
+    ((64, 2), "bf16", 1500, 320, 1088, 5, 1, [9, 191, 0, 193, 1, 1106]),
+]
+
+
+@pytest.mark.parametrize("tile,act,N,d,f,E,k,choice", HIDDEN)
+def test_hidden_tiles(tile, act, N, d, f, E, k, choice):
+    r, rt = N * k // (E + 1), N * k // 64 + min(E, N * k)
+    assert act == "f32" or r < 96 or E * -(-r // 256) * -(-f // 256) < 256
+    tiles = rt * (f // 64)
+    assert tile == ((32, 4) if 2 * tiles <= 256 else (64, 3) if tiles <= 256 else (64, 2))
+    test_matches_oracle(act, N, d, f, E, k, choice)
+    if N >= 256:
+        test_whole_tensors(act, N, d, f, E, k, choice)
