@@ -345,3 +345,40 @@ def test_hidden_tiles(tile, act, N, d, f, E, k, choice):
     test_matches_oracle(act, N, d, f, E, k, choice)
     if N >= 256:
         test_whole_tensors(act, N, d, f, E, k, choice)
+
+
+# top-k 4 in the large tiles: several rows of a token in different experts' lists
+def test_many_rows_of_four_slots():
+    test_many_rows("bf16", 2600, 192, 1856, 8, 4, "random")
+    test_whole_tensors("bf16", 2600, 192, 1856, 8, 4, "random")
+
+
+@pytest.mark.parametrize("act,N,d,f,E", [("bf16", 300, 192, 320, 6), ("f32", 300, 192, 320, 6),
+                                         ("bf16", 14000, 256, 1344, 6)])
+def test_values_that_are_no_numbers_stay_where_they_are(act, N, d, f, E):
+    """A NaN or an infinity in a token, or in its upstream gradient, reaches this token's row
+    and gate, the weights of its own expert and dg2; every other bit stays."""
+    case = L, xt, dx, eidx, egate = moe_case(18, act, N, d, f, E, 1)
+    r = N // (E + 1)
+    assert (N > 1000) == (act == "bf16" and r >= 96 and E * -(-r // 256) * -(-f // 256) >= 256)
+    clean = Call(*case, act)().result()
+    # the last row of an expert's list and the first of another's, next to paddings
+    i = int(np.nonzero(eidx[:, 0] == 2)[0][-1])
+    j = int(np.nonzero(eidx[:, 0] == 4)[0][0])
+    for bad in (np.nan, np.inf):
+        x, g = xt.copy(), dx.copy()
+        x[i, 3] = bad
+        g[j, d - 1] = bad
+        got = Call(L, x, g, eidx, egate, act)().result()
+        rows = np.ones(N, bool)
+        rows[[i, j]] = False
+        for n in ("dxt", "g_gate"):
+            np.testing.assert_array_equal(got[n][rows], clean[n][rows], err_msg=n)
+            assert not np.isfinite(got[n][i]).all() and not np.isfinite(got[n][j]).all(), n
+        for n in ("dWgate", "dWup", "dWdown"):
+            for e in range(1, E + 1):
+                if e in (2, 4):
+                    assert not np.isfinite(got[n][e - 1]).all(), (n, e)
+                else:
+                    np.testing.assert_array_equal(got[n][e - 1], clean[n][e - 1], err_msg=f"{n} {e}")
+        assert not np.isfinite(got["dg2"]).any()
