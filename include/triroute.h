@@ -624,7 +624,7 @@ int triroute_grad_list_init(triroute_grad_list *list, const triroute_grad_tensor
 int triroute_grad_norm(const triroute_grad_list *list, double norm_type, double *norm, void *ws,
                        size_t ws_bytes, triroute_stream_t stream);
 /* dst = src * c of every tensor, c = min(1, max_norm / *norm) rounded to fp32, the product
- * rounded once to the tensor's type (norm: device fp64, such as triroute_grad_norm
+ * formed in fp32 and, for a bf16 tensor, rounded to it (norm: device fp64, such as triroute_grad_norm
  * leaves, or one joined over ranks).  A NaN norm gives NaN.  max_norm >= 0.  Tensors whose dst is
  * their src are left as they are when c is 1. */
 int triroute_grad_scale(const triroute_grad_list *list, const double *norm, double max_norm,

@@ -7,10 +7,14 @@
 // initialisation, so that one launch covers any number of tensors and a block
 // finds its work by one load.  Bound by HBM: the norm reads every element,
 // the scaling reads and writes it.  Squares are summed in fp64 (any finite
-// fp32 element's square is a finite fp64 number, and a sum over 10^9 elements
-// keeps 50 bits), in an order that depends only on the list; the largest
-// magnitude is taken on the bit patterns, whose order puts NaN above
-// infinity.
+// fp32 element's square is a finite fp64 number; each of up to 2^19 threads adds
+// its share one by one, so the sum over n elements is off by at most
+// (n / 2^19 + 30) 2^-53 of it, 2^-42 for 10^9 elements), in an order that
+// depends only on the list; the largest magnitude is taken on the bit
+// patterns, whose order puts NaN above infinity.  Layer of 1.3B, 1.1 GB: norm
+// 220 us, scaling 408 (5.0 and 5.4 TB/s, means); where a destination lies
+// otherwise within 16 bytes than its source, an element a lane, the call takes
+// 982 us for 632.
 #include "kernels.hpp"
 
 namespace tr {
@@ -189,7 +193,7 @@ __global__ __launch_bounds__(GRAD_THREADS) void grad_norm_finish_kernel(const do
   if (threadIdx.x == 0) *norm = v;
 }
 
-// x c in fp32, rounded once to the element's type
+// x c in fp32 (the rounding of an fp32 tensor's value), rounded to bf16 where the tensor is
 template <typename T>
 __device__ __forceinline__ uint4 scale_word(const uint4 &w, float c);
 template <>

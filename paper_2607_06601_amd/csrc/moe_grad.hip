@@ -572,9 +572,9 @@ __global__ __launch_bounds__(256, 4) void moe_grad_input_weight_kernel(
 
 // ------------------------------------------------------- four-wave products
 // One block a CU, one wave a SIMD, 256 x 256 tiles walked by a resident block: 128 x 128 to a
-// wave, so that a fragment read from LDS feeds eight MFMAs.  1.3B, 16384 tokens: q 700 us, gates and ups
-// 1362, dn and the weights 2890 (1020, 1045 and 1230 TFLOP/s; MFMA 53, 53 and 64 % busy at the 1.8 GHz
-// that the chip's power leaves).  The loops alone run at 1260-1450, a large library product's
+// wave, so that a fragment read from LDS feeds eight MFMAs.  1.3B, 16384 tokens, means of ten calls: q
+// 733 us, gates and ups 1414, dn and the weights 3080 (970, 1005 and 1155 TFLOP/s; the fastest of the
+// ten 697, 1362 and 2890; MFMA 53, 53 and 64 % busy at the 1.8 GHz that the chip's power leaves).  The loops alone run at 1260-1450, a large library product's
 // rate; the rest is what an epilogue reads, computes and writes, 0.2 to 0.3 MB a tile.  Stages of 64
 // sum indices, two of them in LDS; the fragments of the next 32 are read
 // while the MFMAs of the present 32 issue.  The transfers run on over the
@@ -1207,7 +1207,8 @@ __device__ __forceinline__ int big_tiles_run(const MoeGradArgs &a, const BigShap
 
 // P's tiles, then Q's (which wait for none of P's): the blocks that P leaves a tile short begin Q's
 // list, so that the two lose one last round together (160M, 16384 tokens: dn 1.4 rounds and weights
-// 2.3: 488 us one after the other, 409 together; 410M, 4000 tokens, skewed: 286 and 238).
+// 2.3: 488 us one after the other, 409 together; 410M, 4000 tokens, skewed: 286 and 238; the fastest of
+// ten calls each, of which the means together are 465 and 253).
 template <class P, class Q = void>
 __global__ __launch_bounds__(256, 1) void moe_grad_big_kernel(MoeGradArgs a, BigShape shape) {
   __shared__ __align__(1024) uint8_t smem[2 * P::STAGE];
