@@ -382,3 +382,15 @@ def test_values_that_are_no_numbers_stay_where_they_are(act, N, d, f, E):
                 else:
                     np.testing.assert_array_equal(got[n][e - 1], clean[n][e - 1], err_msg=f"{n} {e}")
         assert not np.isfinite(got["dg2"]).any()
+
+
+@pytest.mark.parametrize("act,N,d,f,E,k", [("bf16", 21, 2112, 128, 2, 2), ("f32", 21, 2112, 64, 2, 2),
+                                           ("bf16", 3, 192, 128, 3, 2), ("bf16", 2600, 2240, 1856, 16, 2)])
+def test_frozen_experts_in_place_with_the_norms_gradient(act, N, d, f, E, k):
+    """dxt over dx_out where a row passes the registers, and dg2 (of one block of tokens, or
+    joined over many) without the weight gradients: the full call's bits."""
+    case = moe_case(19, act, N, d, f, E, k)
+    full = Call(*case, act)().result()
+    part = Call(*case, act, want=("dxt", "dg2", "g_gate"), in_place=True)().result()
+    for n, v in part.items():
+        np.testing.assert_array_equal(v, full[n], err_msg=n)
