@@ -1,4 +1,4 @@
-// Pieces that the bf16 MFMA products share (gfx950): operand types, the order in
+// Pieces that the MFMA products share (gfx950): operand types, the order in
 // which tiles are handed to the XCDs, the LDS swizzle of K-contiguous stages and
 // products on the accumulator registers.
 #pragma once
@@ -9,6 +9,7 @@ namespace tr {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
 
 // Tiles of the whole problem are handed out XCD by XCD: blocks are issued to
 // the 8 XCDs round-robin, so block L runs on XCD L % 8, and it takes tile
@@ -78,13 +79,45 @@ __device__ __forceinline__ void mfma_agpr_first(f32x4_t &acc, const bf16x8_t &a,
   asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=a"(acc) : "v"(a), "v"(b));
 }
 
+// The same with 8-bit integer operands: 16 codes a lane where bf16 has 8 elements, at the
+// same cycles, and sums in int32 (exact).
+__device__ __forceinline__ void mfma_agpr(i32x4_t &acc, const i32x4_t &a, const i32x4_t &b) {
+  asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void mfma_agpr_first(i32x4_t &acc, const i32x4_t &a, const i32x4_t &b) {
+  asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, 0" : "=a"(acc) : "v"(a), "v"(b));
+}
+
+// Operand types of a product: stored element, a lane's fragment of a K step, its
+// four sums.
+struct OpBf16 {
+  static constexpr bool INT = false;
+  typedef bf16 elem;
+  typedef bf16x8_t frag;
+  typedef f32x4_t acc;
+  typedef float sum;
+  __device__ static acc mma(const frag &a, const frag &b, const acc &c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+};
+struct OpI8 {
+  static constexpr bool INT = true;
+  typedef int8_t elem;
+  typedef i32x4_t frag;
+  typedef i32x4_t acc;
+  typedef int32_t sum;
+  __device__ static acc mma(const frag &a, const frag &b, const acc &c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
+  }
+};
+
 // The compiler does not see the MFMAs inside the asm statements, so it does
 // not keep its own accesses of the accumulators clear of their hazards.
 // Each row of accumulators passes through an asm statement that starts with
 // `nops` wait states: accesses after it are ordered after the wait, and
 // writes before it (zeroing) before the wait.
-template <int NI>
-__device__ __forceinline__ void acc_fence_row(f32x4_t (&a)[NI]) {
+template <int NI, class A>
+__device__ __forceinline__ void acc_fence_row(A (&a)[NI]) {
   static_assert(NI == 4 || NI == 6 || NI == 8, "accumulator row widths in use");
   if constexpr (NI == 4)
     asm volatile("s_nop 4" : "+a"(a[0]), "+a"(a[1]), "+a"(a[2]), "+a"(a[3]));
