@@ -219,7 +219,11 @@ enum triroute_op {
   TRIROUTE_OP_STACK_DECODE = 8,
   TRIROUTE_OP_ROUTER_RELAXED = 9,
   TRIROUTE_OP_ROUTER_RELAXED_BACKWARD = 10,
-  TRIROUTE_OP_MOE_BACKWARD = 11
+  TRIROUTE_OP_MOE_BACKWARD = 11,
+  TRIROUTE_OP_QKV_I8 = 12,
+  TRIROUTE_OP_MOE_I8 = 13,
+  TRIROUTE_OP_LAYER_PREFILL_I8 = 14,
+  TRIROUTE_OP_LAYER_DECODE_I8 = 15
 };
 
 /* ---- configuration, errors, sizes ---------------------------------------- */
@@ -632,6 +636,89 @@ int triroute_grad_scale(const triroute_grad_list *list, const double *norm, doub
 /* triroute_grad_norm and triroute_grad_scale in two launches: the same norm and values. */
 int triroute_grad_clip(const triroute_grad_list *list, double norm_type, double max_norm,
                        double *norm, void *ws, size_t ws_bytes, triroute_stream_t stream);
+
+/* ---- the layer in 8-bit integers ------------------------------------------- */
+
+/* A matrix [rows, cols] in 8 bits: codes in [-127, 127], row r's at codes + r * pitch with
+ * pitch = TRIROUTE_I8_PITCH(cols) bytes and zeros from cols on, and one fp32 scale a row.
+ * A row x of largest magnitude a has scale = a / 127 (rounded to fp32) and codes
+ * c = 127 x / a rounded half to even (the exact quotient's; a = 0: codes 0, scale 0); the
+ * codes stand for c * scale.  A row that holds a NaN or an infinity has codes 0 and scale NaN.
+ * As a weight, row = output channel (the experts' stacked as in triroute_moe_w).  codes 16-byte
+ * aligned. */
+typedef struct triroute_i8_w {
+  const int8_t *codes;
+  const float *scale;
+} triroute_i8_w;
+
+#define TRIROUTE_I8_PITCH(cols) (((int64_t)(cols) + 127) / 128 * 128)
+/* Longest row of a product: its sum of products of codes is held in 32 bits. */
+#define TRIROUTE_I8_MAX_COLS 131072
+
+/* Quantises x (act, an enum triroute_dtype; row r at x + r * ldx elements, aligned to its
+ * element, ldx >= cols) to codes and scales as above. */
+int triroute_i8_quantize(int act, int64_t rows, int cols, const void *x, int64_t ldx, int8_t *codes,
+                         float *scale, triroute_stream_t stream);
+
+/* Workspace bytes of triroute_linear_i8. */
+int triroute_linear_i8_workspace_bytes(int n_tok, int in, size_t *bytes);
+/* y = x W^T (+ residual) in 8-bit integers, for n_tok tokens, `in` input and `out` output channels:
+ * the tokens are quantised as triroute_i8_quantize does, the products of codes are summed
+ * exactly, and y[i, j] = sum * s_i * t_j (fp32, the token's scale, then the channel's) plus
+ * residual[i, j] is rounded once to act.  The O-projection is this with residual = x.  A result does
+ * not depend on the other tokens of the call; a token that holds a NaN or an infinity has a
+ * row of NaN.
+ *   x, residual (or NULL), y: act, rows ldx, ldr, ldy elements apart, aligned to their element;
+ *   y may be residual (with ldr == ldy), else overlaps neither input; W [out, in]; 1 <= in <=
+ *   TRIROUTE_I8_MAX_COLS, 1 <= out <= 2^24. */
+int triroute_linear_i8(int act, int n_tok, int in, int out, const void *x, int64_t ldx,
+                       const triroute_i8_w *w, const void *residual, int64_t ldr, void *y,
+                       int64_t ldy, void *ws, size_t ws_bytes, triroute_stream_t stream);
+
+/* Attention projections in 8 bits (of which triroute_qkv_i8 reads Wq, Wk, Wv and the layer
+ * calls all) and the second norm gain (act; read by triroute_moe_i8). */
+typedef struct triroute_dense_i8_w {
+  triroute_i8_w Wq, Wk, Wv, Wo;
+  const void *g2;
+} triroute_dense_i8_w;
+
+/* Experts in 8 bits: Wgate, Wup [E * d_ff, d], Wdown [E * d, d_ff]. */
+typedef struct triroute_moe_i8_w {
+  triroute_i8_w Wgate, Wup, Wdown;
+} triroute_moe_i8_w;
+
+/* triroute_qkv with 8-bit weights: n1's tokens quantised, the products as in triroute_linear_i8,
+ * q and k rotated in fp32 before the rounding to act.  A token's q, k and v do not depend on the
+ * other tokens of the call.
+ * ws: triroute_workspace_bytes(cfg, TRIROUTE_OP_QKV_I8, B, T) bytes. */
+int triroute_qkv_i8(const triroute_cfg *cfg, int B, int T, const void *n1,
+                    const triroute_dense_i8_w *w, const int32_t *pos0, void *q, void *k, void *v,
+                    void *ws, size_t ws_bytes, triroute_stream_t stream);
+
+/* triroute_moe with 8-bit weights.  The normalised token (computed in fp64, rounded once to fp32)
+ * and the hidden row h = silu(G) U (fp32) are quantised, each with one scale; products as in
+ * triroute_linear_i8, gates and the sum over slots as in triroute_moe (fp32).
+ * ws: triroute_workspace_bytes(cfg, TRIROUTE_OP_MOE_I8, n_tok, 1) bytes. */
+int triroute_moe_i8(const triroute_cfg *cfg, int n_tok, const void *xt,
+                    const triroute_dense_i8_w *dw, const triroute_moe_i8_w *w, const int32_t *eidx,
+                    const float *egate, const triroute_compaction *cmp, void *x_out, void *ws,
+                    size_t ws_bytes, triroute_stream_t stream);
+
+/* triroute_layer_prefill and triroute_layer_decode with 8-bit weights (the router's stay fp32, the
+ * cache as it is): triroute_qkv_i8, triroute_linear_i8 for the O-projection, triroute_moe_i8.
+ * ws: TRIROUTE_OP_LAYER_PREFILL_I8 / TRIROUTE_OP_LAYER_DECODE_I8. */
+int triroute_layer_prefill_i8(const triroute_cfg *cfg, int B, int T, const int32_t *seq_ids,
+                              const void *x, const float *psi, const triroute_router_w *rw,
+                              const triroute_dense_i8_w *dw, const triroute_moe_i8_w *mw,
+                              const triroute_kv_cache *cache, void *x_out,
+                              const triroute_layer_taps *taps, void *ws, size_t ws_bytes,
+                              triroute_stream_t stream);
+int triroute_layer_decode_i8(const triroute_cfg *cfg, int B, const int32_t *seq_ids,
+                             const void *x, const float *psi, const triroute_router_w *rw,
+                             const triroute_dense_i8_w *dw, const triroute_moe_i8_w *mw,
+                             const triroute_kv_cache *cache, void *x_out,
+                             const triroute_layer_taps *taps, void *ws, size_t ws_bytes,
+                             triroute_stream_t stream);
 
 /* ---- no-allocation variant ---------------------------------------------- */
 

@@ -22,7 +22,8 @@ F32, BF16 = 0, 1
 SKIP, LOCAL, FULL = 0, 1, 2
 OP_ROUTER, OP_QKV, OP_KV_APPEND, OP_ATTN_PREFILL, OP_ATTN_DECODE, OP_MOE, \
     OP_LAYER_PREFILL, OP_LAYER_DECODE, OP_STACK_DECODE, OP_ROUTER_RELAXED, \
-    OP_ROUTER_RELAXED_BACKWARD, OP_MOE_BACKWARD = range(12)
+    OP_ROUTER_RELAXED_BACKWARD, OP_MOE_BACKWARD, OP_QKV_I8, OP_MOE_I8, OP_LAYER_PREFILL_I8, \
+    OP_LAYER_DECODE_I8 = range(16)
 # fp64 fields of RelaxOut.stats (axes in the order attention, experts, bits)
 RS_LBAL, RS_LZ, RS_LENT, RS_ENTROPY, RS_CBAR, RS_COST, RS_DENSE, RS_REG = 0, 3, 6, 9, 12, 14, 16, 18
 RS_F_ATTN, RS_P_ATTN, RS_F_BITS, RS_P_BITS, RELAX_NSTAT = 19, 22, 25, 29, 33
@@ -57,6 +58,18 @@ class DenseW(C.Structure):
 
 class MoeW(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("Wgate", "Wup", "Wdown")]
+
+
+class I8W(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scale", C.c_void_p)]
+
+
+class DenseI8W(C.Structure):
+    _fields_ = [(n, I8W) for n in ("Wq", "Wk", "Wv", "Wo")] + [("g2", C.c_void_p)]
+
+
+class MoeI8W(C.Structure):
+    _fields_ = [(n, I8W) for n in ("Wgate", "Wup", "Wdown")]
 
 
 class LayerW(C.Structure):
@@ -138,6 +151,8 @@ EXPORTS = [
     "triroute_kv_paged_cache_bytes", "triroute_kv_paged_cache_init", "triroute_kv_free_pages",
     "triroute_moe_backward", "triroute_grad_list_bytes", "triroute_grad_list_init",
     "triroute_grad_norm", "triroute_grad_scale", "triroute_grad_clip",
+    "triroute_i8_quantize", "triroute_linear_i8_workspace_bytes", "triroute_linear_i8",
+    "triroute_qkv_i8", "triroute_moe_i8", "triroute_layer_prefill_i8", "triroute_layer_decode_i8",
 ]
 
 _lib = None
@@ -152,7 +167,7 @@ def lib():
                                "`python -m paper_2607_06601_amd._build`")
         L = C.CDLL(LIB_PATH)
         P = C.c_void_p
-        i32, sz = C.c_int, C.c_size_t
+        i32, i64, sz = C.c_int, C.c_int64, C.c_size_t
         sig = {
             "triroute_validate": [P],
             "triroute_workspace_bytes": [P, i32, i32, i32, C.POINTER(sz)],
@@ -184,6 +199,13 @@ def lib():
             "triroute_grad_norm": [P, C.c_double, P, P, sz, P],
             "triroute_grad_scale": [P, P, C.c_double, P],
             "triroute_grad_clip": [P, C.c_double, C.c_double, P, P, sz, P],
+            "triroute_i8_quantize": [i32, i64, i32, P, i64, P, P, P],
+            "triroute_linear_i8_workspace_bytes": [i32, i32, C.POINTER(sz)],
+            "triroute_linear_i8": [i32, i32, i32, i32, P, i64, P, P, i64, P, i64, P, sz, P],
+            "triroute_qkv_i8": [P, i32, i32, P, P, P, P, P, P, P, sz, P],
+            "triroute_moe_i8": [P, i32, P, P, P, P, P, P, P, P, sz, P],
+            "triroute_layer_prefill_i8": [P, i32, i32, P, P, P, P, P, P, P, P, P, P, sz, P],
+            "triroute_layer_decode_i8": [P, i32, P, P, P, P, P, P, P, P, P, P, sz, P],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -412,6 +434,123 @@ def stack_decode(cfg, B, x, psi, layers, caches, x_out, ws, seq_ids=None, stream
     cs = (type(caches[0].desc) * n)(*[c.desc for c in caches])
     _check(lib().triroute_stack_decode(
         C.byref(cfg), n, B, _p(seq_ids), _p(x), _p(psi), lw, cs, _p(x_out), _p(ws), ws.numel(),
+        _stream(stream)))
+
+
+# ------------------------------------------------- the layer in 8-bit integers
+def i8_pitch(cols: int) -> int:
+    """Bytes of a row of codes (TRIROUTE_I8_PITCH)."""
+    return (cols + 127) // 128 * 128
+
+
+class I8Matrix:
+    """A matrix [rows, cols] in 8 bits: ``codes`` int8 [rows, i8_pitch(cols)], zeros from cols
+    on, and ``scale`` fp32 [rows]; ``w`` is its I8W, valid while the matrix lives.  Made of
+    these two, or by ``I8Matrix.quantize`` of a matrix (experts' weights [E, rows, cols] are
+    stacked)."""
+
+    def __init__(self, codes, scale, cols):
+        if codes.dtype != torch.int8 or codes.dim() != 2 or not codes.is_contiguous() \
+                or codes.shape[1] != i8_pitch(cols):
+            raise ValueError(f"codes: contiguous int8 rows of {i8_pitch(cols)} for {cols} columns")
+        if scale.dtype != torch.float32 or scale.shape != (codes.shape[0],) \
+                or not scale.is_contiguous() or scale.device != codes.device:
+            raise ValueError("scale: one fp32 value a row, on the codes' device")
+        self.codes, self.scale, self.cols = codes, scale, cols
+        self.w = I8W(codes.data_ptr(), scale.data_ptr())
+
+    @property
+    def rows(self):
+        return self.codes.shape[0]
+
+    @classmethod
+    def quantize(cls, x, stream=None):
+        x = x.reshape(-1, x.shape[-1])
+        with torch.cuda.stream(stream) if stream is not None else nullcontext():
+            codes = torch.empty(x.shape[0], i8_pitch(x.shape[1]), dtype=torch.int8, device=x.device)
+            scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+        i8_quantize(x, codes, scale, stream)
+        return cls(codes, scale, x.shape[1])
+
+    def dequantize(self):
+        """The fp32 values that the codes stand for."""
+        return self.codes[:, :self.cols].float() * self.scale[:, None]
+
+
+def _i8_rows(name, t):
+    """dtype, row stride of a [rows, cols] tensor whose rows are contiguous."""
+    if t.dim() != 2 or t.dtype not in (torch.float32, torch.bfloat16) \
+            or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: fp32 or bf16 rows of contiguous elements wanted")
+    # (of a single row the stride does not matter)
+    return BF16 if t.dtype == torch.bfloat16 else F32, \
+        t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def i8_quantize(x, codes, scale, stream=None):
+    """Codes int8 [rows, i8_pitch(cols)] and scales fp32 [rows] of the rows of x."""
+    act, ldx = _i8_rows("x", x)
+    if codes.dtype != torch.int8 or codes.shape != (x.shape[0], i8_pitch(x.shape[1])) \
+            or not codes.is_contiguous():
+        raise ValueError("codes: contiguous int8 [rows, i8_pitch(cols)]")
+    if scale.dtype != torch.float32 or scale.shape != (x.shape[0],) or not scale.is_contiguous():
+        raise ValueError("scale: fp32 [rows]")
+    _check(lib().triroute_i8_quantize(act, x.shape[0], x.shape[1], _p(x), ldx, _p(codes),
+                                      _p(scale), _stream(stream)))
+
+
+def linear_i8_workspace(n_tok: int, cols: int, device="cuda"):
+    """Workspace of linear_i8 for n_tok tokens of cols channels."""
+    n = C.c_size_t()
+    _check(lib().triroute_linear_i8_workspace_bytes(n_tok, cols, C.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device=device)
+
+
+def linear_i8(x, w: I8Matrix, y, ws, residual=None, stream=None):
+    """y = x w^T (+ residual) in 8-bit integers (triroute_linear_i8); x, y and residual are
+    [tokens, channels] of one type, of any row stride."""
+    act, ldx = _i8_rows("x", x)
+    tens = [("y", y)] + ([] if residual is None else [("residual", residual)])
+    for name, t in tens:
+        if _i8_rows(name, t)[0] != act or t.shape != (x.shape[0], w.rows):
+            raise ValueError(f"{name}: [{x.shape[0]}, {w.rows}] of x's type wanted")
+    if x.shape[1] != w.cols:
+        raise ValueError(f"x has {x.shape[1]} channels, the weight {w.cols}")
+    _check(lib().triroute_linear_i8(
+        act, x.shape[0], x.shape[1], w.rows, _p(x), ldx, C.byref(w.w), _p(residual),
+        0 if residual is None else _i8_rows("residual", residual)[1], _p(y), _i8_rows("y", y)[1],
+        _p(ws), ws.numel(), _stream(stream)))
+
+
+def qkv_i8(cfg, B, T, n1, dw: DenseI8W, q, k, v, ws, pos0=None, stream=None):
+    """triroute_qkv_i8: qkv with 8-bit weights."""
+    _check(lib().triroute_qkv_i8(C.byref(cfg), B, T, _p(n1), C.byref(dw), _p(pos0), _p(q), _p(k),
+                                 _p(v), _p(ws), ws.numel(), _stream(stream)))
+
+
+def moe_i8(cfg, n_tok, xt, dw: DenseI8W, mw: MoeI8W, eidx, egate, cmp: Compaction, x_out, ws,
+           stream=None):
+    """triroute_moe_i8: moe with 8-bit weights."""
+    _check(lib().triroute_moe_i8(C.byref(cfg), n_tok, _p(xt), C.byref(dw), C.byref(mw), _p(eidx),
+                                 _p(egate), C.byref(cmp), _p(x_out), _p(ws), ws.numel(),
+                                 _stream(stream)))
+
+
+def layer_prefill_i8(cfg, B, T, x, psi, rw, dw: DenseI8W, mw: MoeI8W, cache: KVCache, x_out, ws,
+                     taps=None, seq_ids=None, stream=None):
+    """triroute_layer_prefill_i8: layer_prefill with 8-bit weights."""
+    _check(lib().triroute_layer_prefill_i8(
+        C.byref(cfg), B, T, _p(seq_ids), _p(x), _p(psi), C.byref(rw), C.byref(dw), C.byref(mw),
+        cache.ref, _p(x_out), C.byref(taps) if taps is not None else None, _p(ws), ws.numel(),
+        _stream(stream)))
+
+
+def layer_decode_i8(cfg, B, x, psi, rw, dw: DenseI8W, mw: MoeI8W, cache: KVCache, x_out, ws,
+                    taps=None, seq_ids=None, stream=None):
+    """triroute_layer_decode_i8: layer_decode with 8-bit weights."""
+    _check(lib().triroute_layer_decode_i8(
+        C.byref(cfg), B, _p(seq_ids), _p(x), _p(psi), C.byref(rw), C.byref(dw), C.byref(mw),
+        cache.ref, _p(x_out), C.byref(taps) if taps is not None else None, _p(ws), ws.numel(),
         _stream(stream)))
 
 

@@ -11,6 +11,7 @@
 
 #include <mutex>
 #include <new>
+#include <type_traits>
 
 #include <initializer_list>
 
@@ -253,6 +254,31 @@ void carve_moe_grad(Carve &cv, const triroute_cfg &c, int N, tr::MoeGradJob &j) 
   j.part = cv.take<float>(size_t(tr::moe_grad_part_rows(c, N)) * c.d_model);
 }
 
+// Codes and scales of the tokens of an 8-bit product.
+struct I8Rows {
+  int8_t *codes;
+  float *scale;
+};
+I8Rows carve_i8_rows(Carve &cv, int N, int cols) {
+  I8Rows r;
+  r.codes = cv.take<int8_t>(size_t(N) * tr::i8_pitch(cols));
+  r.scale = cv.take<float>(N);
+  return r;
+}
+tr::MoeI8Ws carve_moe_i8(Carve &cv, const triroute_cfg &c, int N) {
+  const size_t rows = size_t(N) * c.top_k;
+  tr::MoeI8Ws w;
+  w.n2 = cv.take<int8_t>(rows * tr::i8_pitch(c.d_model));
+  w.hq = cv.take<int8_t>(rows * tr::i8_pitch(c.d_ff));
+  w.s_n2 = cv.take<float>(rows);
+  w.s_h = cv.take<float>(rows);
+  w.h = cv.take<float>(rows * c.d_ff);
+  w.Y = cv.take<float>(rows * c.d_model);
+  w.part = cv.take<uint32_t>(rows * tr::i8_hidden_parts(c));
+  w.slot_of = cv.take<int32_t>(rows);
+  return w;
+}
+
 size_t op_bytes(const triroute_cfg &c, int op, int B, int T) {
   Carve cv(nullptr);
   const int N = B * T;
@@ -274,6 +300,27 @@ size_t op_bytes(const triroute_cfg &c, int op, int B, int T) {
                                                                  : TRIROUTE_OP_ATTN_PREFILL,
                                B, T));
       s = std::max(s, op_bytes(c, TRIROUTE_OP_MOE, B, T));
+      return cv.used + s;
+    }
+    case TRIROUTE_OP_QKV_I8:
+      carve_qkv(cv, c, N);
+      carve_i8_rows(cv, N, c.d_model);
+      break;
+    case TRIROUTE_OP_MOE_I8: carve_moe_i8(cv, c, N); break;
+    case TRIROUTE_OP_LAYER_PREFILL_I8:
+    case TRIROUTE_OP_LAYER_DECODE_I8: {
+      carve_layer(cv, c, B, T);
+      size_t s = 0;
+      // router scratch, rotation table and the tokens' codes together
+      s = std::max(s, op_bytes(c, TRIROUTE_OP_ROUTER, B, T) + op_bytes(c, TRIROUTE_OP_QKV_I8, B, T));
+      s = std::max(s, op_bytes(c, TRIROUTE_OP_KV_APPEND, B, T));
+      s = std::max(s, op_bytes(c, op == TRIROUTE_OP_LAYER_DECODE_I8 ? TRIROUTE_OP_ATTN_DECODE
+                                                                    : TRIROUTE_OP_ATTN_PREFILL,
+                               B, T));
+      Carve oc(nullptr);
+      carve_i8_rows(oc, N, c.n_heads * c.head_dim);
+      s = std::max(s, oc.used);
+      s = std::max(s, op_bytes(c, TRIROUTE_OP_MOE_I8, B, T));
       return cv.used + s;
     }
     case TRIROUTE_OP_STACK_DECODE:
@@ -616,7 +663,7 @@ int triroute_workspace_bytes(const triroute_cfg *cfg, int op, int B, int T, size
   TRY(check_cfg(cfg));
   TRY(check_bt(B, T));
   REQUIRE(bytes, TRIROUTE_E_INVALID, "bytes is NULL");
-  REQUIRE(op >= TRIROUTE_OP_ROUTER && op <= TRIROUTE_OP_MOE_BACKWARD, TRIROUTE_E_INVALID,
+  REQUIRE(op >= TRIROUTE_OP_ROUTER && op <= TRIROUTE_OP_LAYER_DECODE_I8, TRIROUTE_E_INVALID,
           "unknown op %d", op);
   *bytes = op_bytes(*cfg, op, B, T);
   return TRIROUTE_OK;
@@ -1012,7 +1059,7 @@ static int moe_impl(const triroute_cfg *cfg, int n_tok, const void *xt, const tr
   CHECK_HIP(tr::launch_moe_norm_rows(*cfg, n_tok, xt, dw->g2, *cmp, eidx, m.n2, m.slot_of, st),
             "moe_norm_rows launch");
   CHECK_HIP(tr::launch_moe_gemms(*cfg, n_tok, m.n2, *w, *cmp, m.Hm, m.Y, st), "moe gemm launch");
-  CHECK_HIP(tr::launch_moe_combine(*cfg, n_tok, xt, m.Y, m.slot_of, eidx, egate, x_out, st),
+  CHECK_HIP(tr::launch_moe_combine(*cfg, n_tok, xt, m.Y, tr::moe_ysplit(*cfg, n_tok), m.slot_of, eidx, egate, x_out, st),
             "combine launch");
   return TRIROUTE_OK;
 }
@@ -1032,20 +1079,192 @@ int triroute_moe(const triroute_cfg *cfg, int n_tok, const void *xt, const triro
   return moe_impl(cfg, n_tok, xt, dw, w, eidx, egate, cmp, x_out, cv, (hipStream_t)stream);
 }
 
+// ---- 8-bit integer products ----
+
+extern "C++" {
+
+static int check_i8_w(std::initializer_list<triroute_i8_w> ws) {
+  for (const triroute_i8_w &w : ws) {
+    REQUIRE(w.codes && w.scale, TRIROUTE_E_INVALID, "NULL codes or scale of an 8-bit weight");
+    REQUIRE((uintptr_t(w.scale) & 3) == 0, TRIROUTE_E_INVALID, "scales must be 4-byte aligned");
+    TRY(check_aligned({w.codes}));
+  }
+  return TRIROUTE_OK;
+}
+static int check_i8_cols(int cols) {
+  REQUIRE(cols >= 1, TRIROUTE_E_INVALID, "rows of %d channels", cols);
+  REQUIRE(cols <= TRIROUTE_I8_MAX_COLS, TRIROUTE_E_UNSUPPORTED,
+          "rows of %d channels: at most %d fit a 32-bit sum", cols, TRIROUTE_I8_MAX_COLS);
+  return TRIROUTE_OK;
+}
+static int check_qkv_i8_w(const triroute_cfg &c, const triroute_dense_i8_w *w) {
+  TRY(check_i8_cols(c.d_model));
+  return check_i8_w({w->Wq, w->Wk, w->Wv});
+}
+static int check_moe_i8_w(const triroute_cfg &c, const triroute_dense_i8_w *dw,
+                          const triroute_moe_i8_w *w) {
+  TRY(check_i8_cols(c.d_model));
+  TRY(check_i8_cols(c.d_ff));
+  REQUIRE(dw->g2, TRIROUTE_E_INVALID, "g2 is NULL");
+  TRY(check_aligned({dw->g2}));
+  return check_i8_w({w->Wgate, w->Wup, w->Wdown});
+}
+// Rows of a strided tensor: aligned to its element, rows that do not overlap.
+static int check_rows(int act, const char *name, const void *p, int64_t ld, int cols) {
+  REQUIRE((uintptr_t(p) & (act == TRIROUTE_BF16 ? 1 : 3)) == 0, TRIROUTE_E_INVALID,
+          "%s is not aligned to its element", name);
+  REQUIRE(ld >= cols && ld <= (int64_t(1) << 40), TRIROUTE_E_INVALID,
+          "%s: row stride %lld, rows of %d", name, (long long)ld, cols);
+  return TRIROUTE_OK;
+}
+static int check_act(int act) {
+  REQUIRE(act == TRIROUTE_F32 || act == TRIROUTE_BF16, TRIROUTE_E_INVALID,
+          "act must be TRIROUTE_F32 or TRIROUTE_BF16 (got %d)", act);
+  return TRIROUTE_OK;
+}
+
+static hipError_t run_linear_i8(int act, int N, int in, int out, const void *x, int64_t ldx,
+                                const triroute_i8_w &w, const void *res, int64_t ldr, void *y,
+                                int64_t ldy, const I8Rows &rows, hipStream_t st) {
+  const hipError_t e = tr::launch_i8_rows(act, N, in, x, ldx, rows.codes, rows.scale, st);
+  return e != hipSuccess ? e : tr::i8_linear(act, N, out, in, rows.codes, rows.scale, w, res, ldr, y, ldy, st);
+}
+static hipError_t run_qkv_i8(const triroute_cfg &c, int N, const void *n1, const triroute_dense_i8_w &w,
+                             const I8Rows &rows, const float *rope, void *q, void *k, void *v,
+                             hipStream_t st) {
+  const hipError_t e = tr::launch_i8_rows(c.act, N, c.d_model, n1, c.d_model, rows.codes, rows.scale, st);
+  return e != hipSuccess ? e : tr::i8_qkv(c, N, rows.codes, rows.scale, w, rope, q, k, v, st);
+}
+
+}  // extern "C++"
+
+int triroute_i8_quantize(int act, int64_t rows, int cols, const void *x, int64_t ldx, int8_t *codes,
+                         float *scale, triroute_stream_t stream) {
+  TRY(check_act(act));
+  REQUIRE(x && codes && scale, TRIROUTE_E_INVALID, "NULL argument");
+  REQUIRE(rows >= 1 && rows <= (int64_t(1) << 40), TRIROUTE_E_INVALID, "rows (%lld) outside [1, 2^40]",
+          (long long)rows);
+  TRY(check_i8_cols(cols));
+  TRY(check_rows(act, "x", x, ldx, cols));
+  TRY(check_i8_w({triroute_i8_w{codes, scale}}));
+  CHECK_HIP(tr::launch_i8_rows(act, rows, cols, x, ldx, codes, scale, (hipStream_t)stream),
+            "quantisation launch");
+  return TRIROUTE_OK;
+}
+
+int triroute_linear_i8_workspace_bytes(int n_tok, int in, size_t *bytes) {
+  TRY(check_bt(n_tok, 1));
+  TRY(check_i8_cols(in));
+  REQUIRE(bytes, TRIROUTE_E_INVALID, "bytes is NULL");
+  Carve cv(nullptr);
+  carve_i8_rows(cv, n_tok, in);
+  *bytes = cv.used;
+  return TRIROUTE_OK;
+}
+
+int triroute_linear_i8(int act, int n_tok, int in, int out, const void *x, int64_t ldx,
+                       const triroute_i8_w *w, const void *residual, int64_t ldr, void *y,
+                       int64_t ldy, void *ws, size_t ws_bytes, triroute_stream_t stream) {
+  TRY(check_act(act));
+  size_t need = 0;
+  TRY(triroute_linear_i8_workspace_bytes(n_tok, in, &need));
+  REQUIRE(out >= 1 && out <= (1 << 24), TRIROUTE_E_INVALID, "out (%d) outside [1, 2^24]", out);
+  REQUIRE(x && w && y && ws, TRIROUTE_E_INVALID, "NULL argument");
+  TRY(check_rows(act, "x", x, ldx, in));
+  TRY(check_rows(act, "y", y, ldy, out));
+  if (residual) TRY(check_rows(act, "residual", residual, ldr, out));
+  REQUIRE(residual != y || ldr == ldy, TRIROUTE_E_INVALID,
+          "a residual in y's place needs y's row stride");
+  TRY(check_i8_w({*w}));
+  REQUIRE(ws_bytes >= need, TRIROUTE_E_WORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, need);
+  REQUIRE((uintptr_t(ws) & 255) == 0, TRIROUTE_E_INVALID, "workspace must be 256-byte aligned");
+  Carve cv(ws);
+  const I8Rows rows = carve_i8_rows(cv, n_tok, in);
+  CHECK_HIP(run_linear_i8(act, n_tok, in, out, x, ldx, *w, residual, ldr, y, ldy, rows,
+                          (hipStream_t)stream),
+            "linear_i8 launch");
+  return TRIROUTE_OK;
+}
+
+int triroute_qkv_i8(const triroute_cfg *cfg, int B, int T, const void *n1,
+                    const triroute_dense_i8_w *w, const int32_t *pos0, void *q, void *k, void *v,
+                    void *ws, size_t ws_bytes, triroute_stream_t stream) {
+  TRY(check_cfg(cfg));
+  TRY(check_bt(B, T));
+  REQUIRE(n1 && w && q && k && v, TRIROUTE_E_INVALID, "NULL argument");
+  TRY(check_aligned({n1, q, k, v}));
+  TRY(check_qkv_i8_w(*cfg, w));
+  TRY(check_ws(*cfg, TRIROUTE_OP_QKV_I8, B, T, ws, ws_bytes));
+  Carve cv(ws);
+  float *rope = carve_qkv(cv, *cfg, B * T);
+  const I8Rows rows = carve_i8_rows(cv, B * T, cfg->d_model);
+  hipStream_t st = (hipStream_t)stream;
+  CHECK_HIP(tr::launch_rope_table(*cfg, B * T, T, pos0, nullptr, B, rope, st), "rotation table launch");
+  CHECK_HIP(run_qkv_i8(*cfg, B * T, n1, *w, rows, rope, q, k, v, st), "qkv_i8 launch");
+  return TRIROUTE_OK;
+}
+
+extern "C++" {
+static int moe_impl(const triroute_cfg *cfg, int n_tok, const void *xt, const triroute_dense_i8_w *dw,
+                    const triroute_moe_i8_w *w, const int32_t *eidx, const float *egate,
+                    const triroute_compaction *cmp, void *x_out, Carve &cv, hipStream_t st) {
+  const tr::MoeI8Ws m = carve_moe_i8(cv, *cfg, n_tok);
+  CHECK_HIP(tr::launch_i8_norm(*cfg, n_tok, xt, dw->g2, *cmp, eidx, m.n2, m.s_n2, m.slot_of, st),
+            "moe_i8 norm launch");
+  CHECK_HIP(tr::i8_moe(*cfg, n_tok, *w, *cmp, m, st), "moe_i8 product launch");
+  CHECK_HIP(tr::launch_moe_combine(*cfg, n_tok, xt, m.Y, 1, m.slot_of, eidx, egate, x_out, st),
+            "combine launch");
+  return TRIROUTE_OK;
+}
+}  // extern "C++"
+
+int triroute_moe_i8(const triroute_cfg *cfg, int n_tok, const void *xt,
+                    const triroute_dense_i8_w *dw, const triroute_moe_i8_w *w, const int32_t *eidx,
+                    const float *egate, const triroute_compaction *cmp, void *x_out, void *ws,
+                    size_t ws_bytes, triroute_stream_t stream) {
+  TRY(check_cfg(cfg));
+  TRY(check_bt(n_tok, 1));
+  REQUIRE(xt && dw && w && eidx && egate && cmp && cmp->exp_cnt && cmp->exp_off && cmp->exp_rows &&
+              x_out,
+          TRIROUTE_E_INVALID, "NULL argument");
+  TRY(check_aligned({xt, x_out}));
+  TRY(check_moe_i8_w(*cfg, dw, w));
+  TRY(check_ws(*cfg, TRIROUTE_OP_MOE_I8, n_tok, 1, ws, ws_bytes));
+  Carve cv(ws);
+  return moe_impl(cfg, n_tok, xt, dw, w, eidx, egate, cmp, x_out, cv, (hipStream_t)stream);
+}
+
+extern "C++" {
+
+static int check_layer_w(const triroute_cfg &, const triroute_dense_w *dw, const triroute_moe_w *mw) {
+  return check_aligned({dw->Wq, dw->Wk, dw->Wv, dw->Wo, dw->g2, mw->Wgate, mw->Wup, mw->Wdown});
+}
+static int check_layer_w(const triroute_cfg &c, const triroute_dense_i8_w *dw,
+                         const triroute_moe_i8_w *mw) {
+  TRY(check_i8_cols(c.n_heads * c.head_dim));
+  TRY(check_qkv_i8_w(c, dw));
+  TRY(check_i8_w({dw->Wo}));
+  return check_moe_i8_w(c, dw, mw);
+}
+
+// dw, mw: the layer's weights in the activation dtype, or (I8) in 8 bits
+template <class DenseW, class MoeW>
 static int layer_impl(const triroute_cfg *cfg, int B, int T, bool decode, const int32_t *seq_ids,
                       const void *x, const float *psi, const triroute_router_w *rw,
-                      const triroute_dense_w *dw, const triroute_moe_w *mw,
+                      const DenseW *dw, const MoeW *mw,
                       const triroute_kv_cache *cache, void *x_out, const triroute_layer_taps *taps,
                       void *ws, size_t ws_bytes, triroute_stream_t stream) {
+  constexpr bool I8 = std::is_same<DenseW, triroute_dense_i8_w>::value;
   TRY(check_cfg(cfg));
   TRY(check_bt(B, T));
   TRY(check_cache(*cfg, cache, B, T));
   REQUIRE(x && (psi || cfg->d_psi == 0) && rw && dw && mw && x_out, TRIROUTE_E_INVALID,
           "NULL argument");
-  TRY(check_aligned({x, x_out, rw->g1, rw->W1, rw->W2, rw->Wa, rw->We, rw->Wb, dw->Wq, dw->Wk,
-                     dw->Wv, dw->Wo, dw->g2, mw->Wgate, mw->Wup, mw->Wdown}));
+  TRY(check_aligned({x, x_out, rw->g1, rw->W1, rw->W2, rw->Wa, rw->We, rw->Wb}));
+  TRY(check_layer_w(*cfg, dw, mw));
   if (taps) TRY(check_aligned({taps->n1, taps->q, taps->k, taps->v, taps->o, taps->xt}));
-  const int op = decode ? TRIROUTE_OP_LAYER_DECODE : TRIROUTE_OP_LAYER_PREFILL;
+  const int op = I8 ? (decode ? TRIROUTE_OP_LAYER_DECODE_I8 : TRIROUTE_OP_LAYER_PREFILL_I8)
+                    : (decode ? TRIROUTE_OP_LAYER_DECODE : TRIROUTE_OP_LAYER_PREFILL);
   TRY(check_ws(*cfg, op, B, T, ws, ws_bytes));
   TRY(prepare_once());
   hipStream_t st = (hipStream_t)stream;
@@ -1074,6 +1293,8 @@ static int layer_impl(const triroute_cfg *cfg, int B, int T, bool decode, const 
     sc.used = scratch_at;
     RouterWs r = carve_router(sc, *cfg, N);
     float *rope = carve_qkv(sc, *cfg, N);
+    I8Rows n1q{};
+    if constexpr (I8) n1q = carve_i8_rows(sc, N, cfg->d_model);
     const tr::RopeJob job = tr::make_rope_job(*cfg, T, seq_len, seq_ids, cache->n_seq, rope);
     CHECK_HIP(tr::launch_router(*cfg, N, x, psi, *rw, L.n1, L.mode, L.bit, L.eidx, L.egate, r.rinv,
                                 r.u, &job, st),
@@ -1096,9 +1317,12 @@ static int layer_impl(const triroute_cfg *cfg, int B, int T, bool decode, const 
                                  decode ? nullptr : L.o, st),
                 "list launch");
     if (T == 1 && !one) CHECK_HIP(tr::launch_scatter(lists, st), "list launch");
-    CHECK_HIP(tr::launch_qkv(*cfg, B, T, L.n1, *dw, seq_len, seq_ids, cache->n_seq, L.q, L.k, L.v,
-                             rope, true, st),
-              "qkv launch");
+    if constexpr (I8)
+      CHECK_HIP(run_qkv_i8(*cfg, N, L.n1, *dw, n1q, rope, L.q, L.k, L.v, st), "qkv launch");
+    else
+      CHECK_HIP(tr::launch_qkv(*cfg, B, T, L.n1, *dw, seq_len, seq_ids, cache->n_seq, L.q, L.k, L.v,
+                               rope, true, st),
+                "qkv launch");
     CHECK_HIP(tr::launch_kv_append(*cfg, app.cv, B, T, seq_ids, L.k, L.v, L.bit, kw, st, T > 1,
                                    T > 1 || one ? &lists : nullptr),
               "kv_append launch");
@@ -1113,10 +1337,19 @@ static int layer_impl(const triroute_cfg *cfg, int B, int T, bool decode, const 
     // the scratch the expert block uses later holds the attention's partials
     CHECK_HIP(run_attn_prefill(*cfg, *cache, B, T, seq_ids, L.q, L.mode, L.cmp, L.o,
                                (float *)((uint8_t *)ws + scratch_at),
-                               op_bytes(*cfg, TRIROUTE_OP_MOE, B, T), true, st),
+                               op_bytes(*cfg, I8 ? TRIROUTE_OP_MOE_I8 : TRIROUTE_OP_MOE, B, T), true,
+                               st),
               "attn_prefill launch");
   }
-  CHECK_HIP(tr::launch_oproj(*cfg, N, x, L.o, *dw, L.xt, st), "oproj launch");
+  if constexpr (I8) {
+    Carve sc(ws);
+    sc.used = scratch_at;
+    const int hd = cfg->n_heads * cfg->head_dim, d = cfg->d_model;
+    const I8Rows oq = carve_i8_rows(sc, N, hd);
+    CHECK_HIP(run_linear_i8(cfg->act, N, hd, d, L.o, hd, dw->Wo, x, d, L.xt, d, oq, st), "oproj launch");
+  } else {
+    CHECK_HIP(tr::launch_oproj(*cfg, N, x, L.o, *dw, L.xt, st), "oproj launch");
+  }
   {
     Carve sc(ws);
     sc.used = scratch_at;
@@ -1125,6 +1358,8 @@ static int layer_impl(const triroute_cfg *cfg, int B, int T, bool decode, const 
   return TRIROUTE_OK;
 }
 
+}  // extern "C++"
+
 int triroute_layer_prefill(const triroute_cfg *cfg, int B, int T, const int32_t *seq_ids,
                            const void *x, const float *psi, const triroute_router_w *rw,
                            const triroute_dense_w *dw, const triroute_moe_w *mw,
@@ -1132,6 +1367,26 @@ int triroute_layer_prefill(const triroute_cfg *cfg, int B, int T, const int32_t 
                            const triroute_layer_taps *taps, void *ws, size_t ws_bytes,
                            triroute_stream_t stream) {
   return layer_impl(cfg, B, T, false, seq_ids, x, psi, rw, dw, mw, cache, x_out, taps, ws, ws_bytes,
+                    stream);
+}
+
+int triroute_layer_prefill_i8(const triroute_cfg *cfg, int B, int T, const int32_t *seq_ids,
+                              const void *x, const float *psi, const triroute_router_w *rw,
+                              const triroute_dense_i8_w *dw, const triroute_moe_i8_w *mw,
+                              const triroute_kv_cache *cache, void *x_out,
+                              const triroute_layer_taps *taps, void *ws, size_t ws_bytes,
+                              triroute_stream_t stream) {
+  return layer_impl(cfg, B, T, false, seq_ids, x, psi, rw, dw, mw, cache, x_out, taps, ws, ws_bytes,
+                    stream);
+}
+
+int triroute_layer_decode_i8(const triroute_cfg *cfg, int B, const int32_t *seq_ids,
+                             const void *x, const float *psi, const triroute_router_w *rw,
+                             const triroute_dense_i8_w *dw, const triroute_moe_i8_w *mw,
+                             const triroute_kv_cache *cache, void *x_out,
+                             const triroute_layer_taps *taps, void *ws, size_t ws_bytes,
+                             triroute_stream_t stream) {
+  return layer_impl(cfg, B, 1, true, seq_ids, x, psi, rw, dw, mw, cache, x_out, taps, ws, ws_bytes,
                     stream);
 }
 

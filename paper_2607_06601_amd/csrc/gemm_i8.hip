@@ -1,0 +1,443 @@
+// Products of 8-bit codes on gfx950 MFMA (v_mfma_i32_16x16x64_i8) on the kernels of
+// gemm_kernels.hpp: both operands are rows of codes, K-contiguous, of i8_pitch(K) bytes with
+// zeros at the end, and the sums are exact in int32 (K <= 2^17), so a result does not depend on
+// the tile, the order or the split of its sum.  A sum becomes
+//   sum * (row's scale) * (column's scale)
+// in fp32, in that order, in every kernel: the same token gives the same value in any batch.
+//
+//   linear: y = x W^T (+ residual), any sizes and row strides
+//   QKV   : [n1] x [Wq;Wk;Wv]^T, rotate-half RoPE on q and k
+//   MoE-1 : h = silu(G) U per expert, fp32, and each tile's largest |h| of a row
+//   MoE-2 : Y = h Wdown_e^T
+#include "gemm_kernels.hpp"
+
+namespace tr {
+
+__device__ __forceinline__ float dequant(int32_t v, float row, float col) {
+  return float(v) * row * col;
+}
+
+// Sums of a wave's tile to the staged fp32 tile C, as store_acc does for bf16; lane
+// column and row mapping as there.
+template <class P, int MI, int NI, int TM, int TN, int LDC>
+__device__ __forceinline__ void stage_i8(const P &p, const MTile &t, float *C,
+                                         const i32x4_t (&acc)[MI][NI], int wm, int wn, int lane) {
+  float sc[NI];
+#pragma unroll
+  for (int ni = 0; ni < NI; ++ni) sc[ni] = p.col_scale(t, wn * TN + ni * 16 + (lane & 15));
+#pragma unroll
+  for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = wm * TM + mi * 16 + 4 * (lane >> 4) + i;
+      const float sr = p.row_scale(t, r < t.mvalid ? r : 0);
+#pragma unroll
+      for (int ni = 0; ni < NI; ++ni) {
+        if constexpr (P::EPI == EPI_PLAIN) {
+          C[r * LDC + wn * TN + ni * 16 + (lane & 15)] = dequant(acc[mi][ni][i], sr, sc[ni]);
+        } else {
+          if ((ni & 3) >= 2) continue;
+          int Pp, half;
+          col_pair(wn * TN + ni * 16 + (lane & 15), Pp, half);
+          if constexpr (P::EPI == EPI_SWIGLU) {
+            C[r * LDC + Pp] = p.hidden(acc[mi][ni][i], acc[mi][ni + 2][i], sr, sc[ni], sc[ni + 2]);
+          } else {
+            C[r * LDC + p.ccol(Pp, 0)] = dequant(acc[mi][ni][i], sr, sc[ni]);
+            C[r * LDC + p.ccol(Pp, 1)] = dequant(acc[mi][ni + 2][i], sr, sc[ni + 2]);
+          }
+        }
+      }
+    }
+}
+
+// ---------------------------------------------------------------- problems
+template <typename T>
+struct LinearI8 {
+  typedef OpI8 Op;
+  static constexpr int EPI = EPI_PLAIN;
+  static constexpr bool GROUPED = false;
+  const int8_t *a, *w;
+  const float *sa, *sw;
+  T *y;
+  const T *res;
+  int64_t ldy, ldr;
+  int N, m, pitch;
+  bool vec;  // whole 16-byte pieces of y and residual
+  static constexpr int out_cols(int BN) { return BN; }
+  __device__ int tiles(int BM, int ny, const GroupScan &) const { return (N + BM - 1) / BM * ny; }
+  __device__ bool map(int bx, int by, int BM, int BN, MTile &t, const GroupScan &) const {
+    t.m0 = bx * BM;
+    t.n0 = by * BN;
+    t.mvalid = min(BM, N - t.m0);
+    t.e = t.p0 = 0;
+    return t.mvalid > 0;
+  }
+  __device__ const int8_t *a_row(const MTile &t, int r) const { return a + int64_t(t.m0 + r) * pitch; }
+  __device__ const int8_t *b_row(const MTile &t, int n) const {
+    return t.n0 + n < m ? w + int64_t(t.n0 + n) * pitch : nullptr;
+  }
+  __device__ float row_scale(const MTile &t, int r) const { return sa[t.m0 + r]; }
+  __device__ float col_scale(const MTile &t, int n) const { return t.n0 + n < m ? sw[t.n0 + n] : 0.f; }
+  template <int MI, int NI, int TM, int TN, int LDC>
+  __device__ void stage(const MTile &t, float *C, const i32x4_t (&acc)[MI][NI], int wm, int wn,
+                        int lane) const {
+    stage_i8<LinearI8, MI, NI, TM, TN, LDC>(*this, t, C, acc, wm, wn, lane);
+  }
+  // item = 8 columns of one row
+  template <int BM, int NC, int LDC, int NT>
+  __device__ void epilogue(const MTile &t, const float *C, int tid) const {
+    constexpr int CC = NC / 8;
+    for (int it = tid; it < BM * CC; it += NT) {
+      const int r = it / CC, c8 = (it % CC) * 8, c = t.n0 + c8;
+      if (r >= t.mvalid || c >= m) continue;
+      const int64_t row = t.m0 + r;
+      const float *cr = C + r * LDC + c8;
+      if (vec) {
+        float v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = cr[u];
+        if (res) {
+          float x[8];
+          load8(res + row * ldr + c, x);
+#pragma unroll
+          for (int u = 0; u < 8; ++u) v[u] += x[u];
+        }
+        store8(y + row * ldy + c, v);
+      } else {
+        for (int u = 0; u < 8 && c + u < m; ++u)
+          Act<T>::st(y, row * ldy + c + u, res ? Act<T>::ld(res, row * ldr + c + u) + cr[u] : cr[u]);
+      }
+    }
+  }
+};
+
+template <typename T>
+struct QkvI8 {
+  typedef OpI8 Op;
+  static constexpr int EPI = EPI_ROPE;
+  static constexpr bool GROUPED = false;
+  const int8_t *a, *Wq, *Wk, *Wv;
+  const float *sa, *sq, *sk, *sv;
+  T *q, *k, *v;
+  const float2 *rope;  // (cos, sin) of token row, pair j at row * dh / 2 + j
+  int N, pitch, Hd, Kd, dh, Ncols;
+  static constexpr int out_cols(int BN) { return BN; }
+  __device__ int tiles(int BM, int ny, const GroupScan &) const { return (N + BM - 1) / BM * ny; }
+  __device__ bool map(int bx, int by, int BM, int BN, MTile &t, const GroupScan &) const {
+    t.m0 = bx * BM;
+    t.n0 = by * BN;
+    t.mvalid = min(BM, N - t.m0);
+    t.e = t.p0 = 0;
+    return t.mvalid > 0;
+  }
+  // logical column (within the tile) of half `half` of pair P
+  __device__ int ccol(int P, int half) const {
+    const int hd = dh >> 1;
+    return (P / hd) * dh + (P % hd) + half * hd;
+  }
+  // column of [Wq; Wk; Wv] of physical tile column n
+  __device__ int col(const MTile &t, int n) const {
+    int P, half;
+    col_pair(n, P, half);
+    return t.n0 + ccol(P, half);
+  }
+  __device__ const int8_t *a_row(const MTile &t, int r) const { return a + int64_t(t.m0 + r) * pitch; }
+  __device__ const int8_t *b_row(const MTile &t, int n) const {
+    const int gc = col(t, n);
+    if (gc >= Ncols) return nullptr;
+    if (gc < Hd) return Wq + int64_t(gc) * pitch;
+    if (gc < Hd + Kd) return Wk + int64_t(gc - Hd) * pitch;
+    return Wv + int64_t(gc - Hd - Kd) * pitch;
+  }
+  __device__ float row_scale(const MTile &t, int r) const { return sa[t.m0 + r]; }
+  __device__ float col_scale(const MTile &t, int n) const {
+    const int gc = col(t, n);
+    if (gc >= Ncols) return 0.f;
+    return gc < Hd ? sq[gc] : gc < Hd + Kd ? sk[gc - Hd] : sv[gc - Hd - Kd];
+  }
+  template <int MI, int NI, int TM, int TN, int LDC>
+  __device__ void stage(const MTile &t, float *C, const i32x4_t (&acc)[MI][NI], int wm, int wn,
+                        int lane) const {
+    stage_i8<QkvI8, MI, NI, TM, TN, LDC>(*this, t, C, acc, wm, wn, lane);
+  }
+  // item = (row, 8 consecutive pairs of one head)
+  template <int BM, int NC, int LDC, int NT>
+  __device__ void epilogue(const MTile &t, const float *C, int tid) const {
+    constexpr int PC = NC / 16;  // 8-pair chunks per row
+    const int hd = dh >> 1;
+    for (int it = tid; it < BM * PC; it += NT) {
+      const int r = it / PC, P0 = (it % PC) * 8;
+      const int lc1 = (P0 / hd) * dh + (P0 % hd);
+      const int c1 = t.n0 + lc1;
+      if (r >= t.mvalid || c1 >= Ncols) continue;
+      const int row = t.m0 + r;
+      T *out;
+      int ld, col;
+      bool rot = true;
+      if (c1 < Hd) {
+        out = q; ld = Hd; col = c1;
+      } else if (c1 < Hd + Kd) {
+        out = k; ld = Kd; col = c1 - Hd;
+      } else {
+        out = v; ld = Kd; col = c1 - Hd - Kd; rot = false;
+      }
+      float y1[8], y2[8];
+      const float *x1 = C + r * LDC + lc1, *x2 = x1 + hd;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        y1[u] = x1[u];
+        y2[u] = x2[u];
+      }
+      if (rot) {
+        const float2 *tb = rope + int64_t(row) * hd + col % hd;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const float cs = tb[u].x, sn = tb[u].y, a1 = y1[u], a2 = y2[u];
+          y1[u] = a1 * cs - a2 * sn;
+          y2[u] = a1 * sn + a2 * cs;
+        }
+      }
+      T *o = out + int64_t(row) * ld + col;
+      store8(o, y1);
+      store8(o + hd, y2);
+    }
+  }
+};
+
+// F64: h of fp32 activations is computed in fp64 and rounded once: the codes of h then
+// do not hang on the last bits of an fp32 exponential (a code one step off would move the output by
+// far more than an fp32 rounding does; against bf16's rounding it does not count).
+template <bool F64>
+struct Moe1I8 {
+  typedef OpI8 Op;
+  static constexpr int EPI = EPI_SWIGLU;
+  static constexpr bool GROUPED = true;
+  const int8_t *a, *Wg, *Wu;  // a: rows in list order
+  const float *sa, *sg, *su;
+  float *h;
+  uint32_t *part;  // [list rows][nparts]: bits of the largest |h| of a row in a column tile
+  const int32_t *cnt;
+  int E, dff, pitch, nparts;
+  static constexpr int out_cols(int BN) { return BN / 2; }
+  __device__ int tiles(int BM, int ny, const GroupScan &gs) const { return gs.total * ny; }
+  __device__ bool map(int bx, int by, int BM, int BN, MTile &t, const GroupScan &gs) const {
+    if (!mmap_grouped(bx, BM, gs, t)) return false;
+    t.n0 = by * (BN / 2);  // BN/2 expert units per tile (gate + up columns)
+    return true;
+  }
+  __device__ const int8_t *a_row(const MTile &t, int r) const { return a + int64_t(t.p0 + r) * pitch; }
+  __device__ const int8_t *b_row(const MTile &t, int n) const {
+    int P, half;
+    col_pair(n, P, half);
+    const int f = t.n0 + P;
+    if (f >= dff) return nullptr;
+    return (half ? Wu : Wg) + (int64_t(t.e - 1) * dff + f) * pitch;
+  }
+  __device__ float row_scale(const MTile &t, int r) const { return sa[t.p0 + r]; }
+  __device__ float col_scale(const MTile &t, int n) const {
+    int P, half;
+    col_pair(n, P, half);
+    const int f = t.n0 + P;
+    return f < dff ? (half ? su : sg)[int64_t(t.e - 1) * dff + f] : 0.f;
+  }
+  __device__ float hidden(int32_t ag, int32_t au, float sr, float cg, float cu) const {
+    if constexpr (F64) {
+      const double g = double(ag) * double(sr) * double(cg), u = double(au) * double(sr) * double(cu);
+      return float(g / (1.0 + exp(-g)) * u);
+    } else {
+      const float g = dequant(ag, sr, cg), u = dequant(au, sr, cu);
+      return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u;
+    }
+  }
+  template <int MI, int NI, int TM, int TN, int LDC>
+  __device__ void stage(const MTile &t, float *C, const i32x4_t (&acc)[MI][NI], int wm, int wn,
+                        int lane) const {
+    stage_i8<Moe1I8, MI, NI, TM, TN, LDC>(*this, t, C, acc, wm, wn, lane);
+  }
+  // item = 8 expert units of one row; the CC items of a row lie in CC lanes side by side
+  template <int BM, int NC, int LDC, int NT>
+  __device__ void epilogue(const MTile &t, const float *C, int tid) const {
+    constexpr int CC = NC / 8;
+    static_assert(NT % CC == 0 && 64 % CC == 0, "a row's items in one wave");
+    for (int it = tid; it < BM * CC; it += NT) {
+      const int r = it / CC, c8 = (it % CC) * 8;
+      const bool on = r < t.mvalid && t.n0 + c8 < dff;  // d_ff is a multiple of 8
+      const float *cr = C + r * LDC + c8;
+      uint32_t m = 0;
+      if (on) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) m = max(m, __float_as_uint(cr[u]) & 0x7FFFFFFFu);
+        store8(h + int64_t(t.p0 + r) * dff + t.n0 + c8, cr);
+      }
+#pragma unroll
+      for (int s = 1; s < CC; s <<= 1) m = max(m, uint32_t(__shfl_xor(int(m), s, 64)));
+      if (r < t.mvalid && c8 == 0) part[int64_t(t.p0 + r) * nparts + t.n0 / NC] = m;
+    }
+  }
+};
+
+struct Moe2I8 {
+  typedef OpI8 Op;
+  static constexpr int EPI = EPI_PLAIN;
+  static constexpr bool GROUPED = true;
+  const int8_t *a, *Wd;
+  const float *sa, *sd;
+  float *Y;  // rows in list order
+  const int32_t *cnt;
+  int E, d, pitch;
+  static constexpr int out_cols(int BN) { return BN; }
+  __device__ int tiles(int BM, int ny, const GroupScan &gs) const { return gs.total * ny; }
+  __device__ bool map(int bx, int by, int BM, int BN, MTile &t, const GroupScan &gs) const {
+    if (!mmap_grouped(bx, BM, gs, t)) return false;
+    t.n0 = by * BN;
+    return true;
+  }
+  __device__ const int8_t *a_row(const MTile &t, int r) const { return a + int64_t(t.p0 + r) * pitch; }
+  __device__ const int8_t *b_row(const MTile &t, int n) const {
+    return t.n0 + n < d ? Wd + (int64_t(t.e - 1) * d + t.n0 + n) * pitch : nullptr;
+  }
+  __device__ float row_scale(const MTile &t, int r) const { return sa[t.p0 + r]; }
+  __device__ float col_scale(const MTile &t, int n) const {
+    return t.n0 + n < d ? sd[int64_t(t.e - 1) * d + t.n0 + n] : 0.f;
+  }
+  template <int MI, int NI, int TM, int TN, int LDC>
+  __device__ void stage(const MTile &t, float *C, const i32x4_t (&acc)[MI][NI], int wm, int wn,
+                        int lane) const {
+    stage_i8<Moe2I8, MI, NI, TM, TN, LDC>(*this, t, C, acc, wm, wn, lane);
+  }
+  // item = 8 output features of one list row
+  template <int BM, int NC, int LDC, int NT>
+  __device__ void epilogue(const MTile &t, const float *C, int tid) const {
+    constexpr int CC = NC / 8;
+    for (int it = tid; it < BM * CC; it += NT) {
+      const int r = it / CC, c8 = (it % CC) * 8;
+      if (r >= t.mvalid || t.n0 + c8 >= d) continue;
+      store8(Y + int64_t(t.p0 + r) * d + t.n0 + c8, C + r * LDC + c8);
+    }
+  }
+};
+
+// ------------------------------------------------------------------ launchers
+// Rows a launch may take: its blocks stay far below the limits of a grid.
+static int rows_a_launch(int c64) { return std::max(1, (1 << 22) / c64) * 32; }
+
+template <typename T>
+static hipError_t linear_rows(const LinearI8<T> &all, hipStream_t st) {
+  const int K2 = all.pitch / 2, c64 = (all.m + 63) / 64, most = rows_a_launch(c64);
+  for (int at = 0; at < all.N; at += most) {
+    LinearI8<T> p = all;
+    p.N = std::min(most, all.N - at);
+    p.a += int64_t(at) * p.pitch;
+    p.sa += at;
+    p.y += at * p.ldy;
+    if (p.res) p.res += at * p.ldr;
+    const hipError_t e = launch<LinearI8<T>, 32, 64, 2, 1, 64, 4>(p, K2, (p.N + 31) / 32, c64, st);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t i8_linear(int act, int N, int m, int k, const int8_t *a, const float *sa,
+                     const triroute_i8_w &w, const void *res, int64_t ldr, void *y, int64_t ldy,
+                     hipStream_t st) {
+  auto run = [&](auto tag) {
+    using T = decltype(tag);
+    LinearI8<T> p;
+    p.a = a;
+    p.sa = sa;
+    p.w = (const int8_t *)w.codes;
+    p.sw = w.scale;
+    p.y = (T *)y;
+    p.res = (const T *)res;
+    p.ldy = ldy;
+    p.ldr = ldr;
+    p.N = N;
+    p.m = m;
+    p.pitch = i8_pitch(k);
+    p.vec = m % 8 == 0 && ((uintptr_t(y) | uintptr_t(ldy * int64_t(sizeof(T)))) & 15) == 0 &&
+            (!res || ((uintptr_t(res) | uintptr_t(ldr * int64_t(sizeof(T)))) & 15) == 0);
+    return linear_rows(p, st);
+  };
+  return act == TRIROUTE_BF16 ? run(bf16{}) : run(float{});
+}
+
+hipError_t i8_qkv(const triroute_cfg &cfg, int N, const int8_t *a, const float *sa,
+                  const triroute_dense_i8_w &w, const float *rope, void *q, void *k, void *v,
+                  hipStream_t st) {
+  auto run = [&](auto tag) {
+    using T = decltype(tag);
+    QkvI8<T> all;
+    all.Wq = (const int8_t *)w.Wq.codes;
+    all.Wk = (const int8_t *)w.Wk.codes;
+    all.Wv = (const int8_t *)w.Wv.codes;
+    all.sq = w.Wq.scale;
+    all.sk = w.Wk.scale;
+    all.sv = w.Wv.scale;
+    all.pitch = i8_pitch(cfg.d_model);
+    all.dh = cfg.head_dim;
+    all.Hd = cfg.n_heads * cfg.head_dim;
+    all.Kd = cfg.n_kv_heads * cfg.head_dim;
+    all.Ncols = all.Hd + 2 * all.Kd;
+    const int c64 = (all.Ncols + 63) / 64, most = rows_a_launch(c64), K2 = all.pitch / 2;
+    for (int at = 0; at < N; at += most) {
+      QkvI8<T> p = all;
+      p.N = std::min(most, N - at);
+      p.a = a + int64_t(at) * p.pitch;
+      p.sa = sa + at;
+      p.rope = (const float2 *)rope + int64_t(at) * (p.dh / 2);
+      p.q = (T *)q + int64_t(at) * p.Hd;
+      p.k = (T *)k + int64_t(at) * p.Kd;
+      p.v = (T *)v + int64_t(at) * p.Kd;
+      hipError_t e;
+      if (p.dh == 64)
+        e = launch<QkvI8<T>, 32, 64, 2, 1, 64, 4>(p, K2, (p.N + 31) / 32, c64, st);
+      else
+        e = launch<QkvI8<T>, 32, 128, 2, 2, 64, 4>(p, K2, (p.N + 31) / 32, c64 / 2, st);
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  };
+  return cfg.act == TRIROUTE_BF16 ? run(bf16{}) : run(float{});
+}
+
+int i8_hidden_parts(const triroute_cfg &cfg) { return (cfg.d_ff + 31) / 32; }
+
+hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
+                  const triroute_compaction &c, const MoeI8Ws &ws, hipStream_t st) {
+  const int E = cfg.n_experts, Nk = N * cfg.top_k, d = cfg.d_model, dff = cfg.d_ff;
+  auto up = [&](auto f64) {
+    typedef Moe1I8<decltype(f64)::value> P;
+    P p;
+    p.a = ws.n2;
+    p.sa = ws.s_n2;
+    p.Wg = (const int8_t *)w.Wgate.codes;
+    p.Wu = (const int8_t *)w.Wup.codes;
+    p.sg = w.Wgate.scale;
+    p.su = w.Wup.scale;
+    p.h = ws.h;
+    p.part = ws.part;
+    p.cnt = c.exp_cnt;
+    p.E = E;
+    p.dff = dff;
+    p.pitch = i8_pitch(d);
+    p.nparts = (dff + 31) / 32;
+    const hipError_t e = launch<P, 32, 64, 2, 1, 64, 4>(p, p.pitch / 2, Nk / 32 + E, p.nparts, st);
+    if (e != hipSuccess) return e;
+    return launch_i8_hidden(cfg, Nk, ws.h, ws.part, p.nparts, c.exp_off, ws.hq, ws.s_h, st);
+  };
+  const hipError_t e = cfg.act == TRIROUTE_BF16 ? up(std::false_type{}) : up(std::true_type{});
+  if (e != hipSuccess) return e;
+  Moe2I8 p;
+  p.a = ws.hq;
+  p.sa = ws.s_h;
+  p.Wd = (const int8_t *)w.Wdown.codes;
+  p.sd = w.Wdown.scale;
+  p.Y = ws.Y;
+  p.cnt = c.exp_cnt;
+  p.E = E;
+  p.d = d;
+  p.pitch = i8_pitch(dff);
+  return launch<Moe2I8, 32, 64, 2, 1, 64, 4>(p, p.pitch / 2, Nk / 32 + E, (d + 63) / 64, st);
+}
+
+}  // namespace tr

@@ -110,6 +110,8 @@ hipError_t launch_kv_export(const triroute_cfg &cfg, const CacheView &cv, int se
 // position of token (b, t) as in RopeJob (pos_base has n_base entries);
 // rope: scratch of qkv_rope_floats(cfg, B * Tq) floats (the rotation table)
 size_t qkv_rope_floats(const triroute_cfg &cfg, int N);
+hipError_t launch_rope_table(const triroute_cfg &cfg, int N, int Tq, const int32_t *pos_base,
+                             const int32_t *pos_idx, int n_base, float *rope, hipStream_t st);
 hipError_t launch_qkv(const triroute_cfg &cfg, int B, int Tq, const void *n1,
                       const triroute_dense_w &w, const int32_t *pos_base, const int32_t *pos_idx,
                       int n_base, void *q, void *k, void *v, float *rope, bool rope_ready,
@@ -162,9 +164,41 @@ hipError_t launch_attn_zero_rows(const triroute_cfg &cfg, int B, int T, const ui
                                  const int32_t *seq_ids, int n_seq, void *o, hipStream_t st);
 hipError_t launch_psi_next(const triroute_cfg &cfg, int N, const float *psi, const uint8_t *mode,
                            const uint8_t *bit, const int32_t *eidx, float *out, hipStream_t st);
+// Y in `planes` planes (moe_ysplit) of N k rows
 hipError_t launch_moe_combine(const triroute_cfg &cfg, int N, const void *xt, const float *Y,
-                              const int32_t *slot_of, const int32_t *eidx, const float *egate,
-                              void *xout, hipStream_t st);
+                              int planes, const int32_t *slot_of, const int32_t *eidx,
+                              const float *egate, void *xout, hipStream_t st);
+// slot_of[a] = entry of the expert lists that holds assignment a (real ones)
+hipError_t launch_moe_slot_of(const triroute_compaction &c, int E, int Nk, int32_t *slot_of,
+                              hipStream_t st);
+
+// i8.hip, gemm_i8.hip: 8-bit codes with a scale for each row, and products of them
+inline int i8_pitch(int cols) { return (cols + 127) / 128 * 128; }  // bytes of a row of codes
+hipError_t launch_i8_rows(int act, int64_t rows, int cols, const void *x, int64_t ldx, int8_t *codes,
+                          float *scale, hipStream_t st);
+hipError_t i8_linear(int act, int N, int m, int k, const int8_t *a, const float *sa,
+                     const triroute_i8_w &w, const void *res, int64_t ldr, void *y, int64_t ldy,
+                     hipStream_t st);
+hipError_t i8_qkv(const triroute_cfg &cfg, int N, const int8_t *a, const float *sa,
+                  const triroute_dense_i8_w &w, const float *rope, void *q, void *k, void *v,
+                  hipStream_t st);
+int i8_hidden_parts(const triroute_cfg &cfg);
+struct MoeI8Ws {  // one row per expert-list entry
+  int8_t *n2, *hq;
+  float *s_n2, *s_h, *h, *Y;
+  uint32_t *part;    // [rows][i8_hidden_parts]: bits of the largest |h| in a part of a row
+  int32_t *slot_of;  // list entry of each assignment
+};
+// RMSNorm(x; g), quantised, to the list rows of every real assignment; slot_of
+hipError_t launch_i8_norm(const triroute_cfg &cfg, int N, const void *x, const void *g,
+                          const triroute_compaction &c, const int32_t *eidx, int8_t *codes,
+                          float *scale, int32_t *slot_of, hipStream_t st);
+hipError_t launch_i8_hidden(const triroute_cfg &cfg, int Nk, const float *h, const uint32_t *part,
+                            int nparts, const int32_t *off, int8_t *codes, float *scale,
+                            hipStream_t st);
+// gate/up, the hidden rows' codes, down: ws.n2 -> ws.Y
+hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
+                  const triroute_compaction &c, const MoeI8Ws &ws, hipStream_t st);
 
 // relax.hip: the relaxed controller forward around the router kernels
 struct RelaxJob {

@@ -196,6 +196,12 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(const T *__restrict__ 
   }
 }
 
+hipError_t launch_moe_slot_of(const triroute_compaction &c, int E, int Nk, int32_t *slot_of,
+                              hipStream_t st) {
+  moe_slot_of_kernel<<<(Nk + 255) / 256, 256, 0, st>>>(c.exp_rows, c.exp_off, E, Nk, slot_of);
+  return hipGetLastError();
+}
+
 hipError_t launch_moe_norm_rows(const triroute_cfg &cfg, int N, const void *x, const void *g,
                                 const triroute_compaction &c, const int32_t *eidx, void *out,
                                 int32_t *slot_of, hipStream_t st) {
@@ -213,7 +219,8 @@ hipError_t launch_moe_norm_rows(const triroute_cfg &cfg, int N, const void *x, c
                                                       (float *)out, slot_of, d, cfg.rms_eps);
     return hipGetLastError();
   }
-  moe_slot_of_kernel<<<(Nk + 255) / 256, 256, 0, st>>>(c.exp_rows, c.exp_off, E, Nk, slot_of);
+  const hipError_t e = launch_moe_slot_of(c, E, Nk, slot_of, st);
+  if (e != hipSuccess) return e;
   const dim3 grid((N + 3) / 4);
   auto run = [&](auto tag, auto rr) {
     using T = decltype(tag);
@@ -232,17 +239,17 @@ hipError_t launch_moe_norm_rows(const triroute_cfg &cfg, int N, const void *x, c
 }
 
 hipError_t launch_moe_combine(const triroute_cfg &cfg, int N, const void *xt, const float *Y,
-                              const int32_t *slot_of, const int32_t *eidx, const float *egate, void *xout,
-                              hipStream_t st) {
+                              int planes, const int32_t *slot_of, const int32_t *eidx,
+                              const float *egate, void *xout, hipStream_t st) {
   int64_t total = int64_t(N) * (cfg.d_model / 8);
   int64_t blocks = (total + 255) / 256;
   if (blocks > 8192) blocks = 8192;
   if (cfg.act == TRIROUTE_BF16)
     moe_combine_kernel<bf16><<<dim3(unsigned(blocks)), 256, 0, st>>>(
-        (const bf16 *)xt, Y, slot_of, moe_ysplit(cfg, N), int64_t(N) * cfg.top_k * cfg.d_model, eidx, egate, (bf16 *)xout, N, cfg.d_model, cfg.top_k);
+        (const bf16 *)xt, Y, slot_of, planes, int64_t(N) * cfg.top_k * cfg.d_model, eidx, egate, (bf16 *)xout, N, cfg.d_model, cfg.top_k);
   else
     moe_combine_kernel<float><<<dim3(unsigned(blocks)), 256, 0, st>>>(
-        (const float *)xt, Y, slot_of, moe_ysplit(cfg, N), int64_t(N) * cfg.top_k * cfg.d_model, eidx, egate, (float *)xout, N, cfg.d_model, cfg.top_k);
+        (const float *)xt, Y, slot_of, planes, int64_t(N) * cfg.top_k * cfg.d_model, eidx, egate, (float *)xout, N, cfg.d_model, cfg.top_k);
   return hipGetLastError();
 }
 

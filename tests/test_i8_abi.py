@@ -1,0 +1,151 @@
+"""Host-side refusals of the 8-bit operators (no GPU)."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2607_06601_amd as tr
+
+FAKE = 1 << 40
+
+
+def cfg160(**over):
+    c = tr.make_cfg(768, 12, 3, 64, 128, 8, 2, 2048, 64, "bf16")
+    for k, v in over.items():
+        setattr(c, k, v)
+    return c
+
+
+def w(codes=FAKE, scale=FAKE):
+    return tr.I8W(codes, scale)
+
+
+def quantize(act=tr.BF16, rows=4, cols=100, x=FAKE, ldx=100, codes=FAKE, scale=FAKE):
+    return tr.lib().triroute_i8_quantize(act, rows, cols, x, ldx, codes, scale, None)
+
+
+@pytest.mark.parametrize("over,code,word", [
+    (dict(act=2), -1, b"act"), (dict(x=None), -1, b"NULL"), (dict(codes=None), -1, b"NULL"),
+    (dict(scale=None), -1, b"NULL"), (dict(rows=0), -1, b"rows"), (dict(rows=-3), -1, b"rows"),
+    (dict(cols=0), -1, b"channels"), (dict(cols=131073, ldx=131073), -2, b"32-bit"),
+    (dict(ldx=99), -1, b"stride"), (dict(x=FAKE + 1), -1, b"aligned"),
+    (dict(act=tr.F32, x=FAKE + 2), -1, b"aligned"), (dict(codes=FAKE + 8), -1, b"aligned"),
+    (dict(scale=FAKE + 2), -1, b"aligned")])
+def test_quantize_refuses(over, code, word):
+    assert quantize(**over) == code
+    assert word in tr.lib().triroute_last_error()
+
+
+def linear(act=tr.BF16, n=16, k=100, m=50, x=FAKE, ldx=100, wt=None, res=None, ldr=50, y=FAKE, ldy=50,
+           ws=FAKE, ws_bytes=1 << 40):
+    wt = w() if wt is None else wt
+    return tr.lib().triroute_linear_i8(act, n, k, m, x, ldx, C.byref(wt), res, ldr, y, ldy, ws,
+                                       ws_bytes, None)
+
+
+@pytest.mark.parametrize("over,code,word", [
+    (dict(act=-1), -1, b"act"), (dict(n=0), -1, b">= 1"), (dict(n=(1 << 24) + 1), -2, b"tokens"),
+    (dict(k=0), -1, b"channels"), (dict(k=131073, ldx=131073), -2, b"32-bit"),
+    (dict(m=0), -1, b"out"), (dict(m=(1 << 24) + 1, ldy=1 << 25), -1, b"out"),
+    (dict(x=None), -1, b"NULL"), (dict(y=None), -1, b"NULL"), (dict(ws=None), -1, b"NULL"),
+    (dict(wt=w(codes=None)), -1, b"codes"), (dict(wt=w(scale=None)), -1, b"codes"),
+    (dict(wt=w(codes=FAKE + 4)), -1, b"aligned"), (dict(ldx=99), -1, b"x: row stride"),
+    (dict(ldy=49), -1, b"y: row stride"), (dict(res=FAKE, ldr=49), -1, b"residual: row stride"),
+    (dict(res=FAKE + 1), -1, b"aligned"), (dict(res=FAKE, ldr=60), -1, b"y's row stride"),
+    (dict(ws=FAKE + 16), -1, b"aligned"), (dict(ws_bytes=2047), -3, b"workspace")])
+def test_linear_refuses(over, code, word):
+    assert linear(**over) == code
+    assert word in tr.lib().triroute_last_error()
+
+
+def test_linear_workspace():
+    n = C.c_size_t()
+    assert tr.lib().triroute_linear_i8_workspace_bytes(16, 100, C.byref(n)) == 0
+    assert n.value == 16 * 128 + 256      # codes, scales (rounded to 256 B)
+    assert tr.lib().triroute_linear_i8_workspace_bytes(16, 100, None) == -1
+    assert tr.lib().triroute_linear_i8_workspace_bytes(0, 100, C.byref(n)) == -1
+
+
+def qkv(c=None, B=2, T=8, n1=FAKE, q=FAKE, ws=FAKE, ws_bytes=1 << 44, **over):
+    c = cfg160() if c is None else c
+    dw = tr.DenseI8W(**{**dict(Wq=w(), Wk=w(), Wv=w()), **over})
+    return tr.lib().triroute_qkv_i8(C.byref(c), B, T, n1, C.byref(dw), None, q, FAKE, FAKE, ws,
+                                    ws_bytes, None)
+
+
+@pytest.mark.parametrize("over,code,word", [
+    (dict(n1=None), -1, b"NULL"), (dict(q=None), -1, b"NULL"), (dict(Wk=w(codes=None)), -1, b"codes"),
+    (dict(Wv=w(scale=None)), -1, b"codes"), (dict(Wq=w(codes=FAKE + 8)), -1, b"aligned"),
+    (dict(n1=FAKE + 8), -1, b"aligned"), (dict(B=0), -1, b">= 1"), (dict(ws=None), -1, b"workspace"),
+    (dict(ws_bytes=64), -3, b"workspace"), (dict(c=cfg160(head_dim=96)), -2, b"head_dim"),
+    (dict(c=cfg160(d_model=131136)), -2, b"32-bit")])
+def test_qkv_refuses(over, code, word):
+    assert qkv(**over) == code
+    assert word in tr.lib().triroute_last_error()
+
+
+def moe(c=None, n=16, xt=FAKE, xo=FAKE, g2=FAKE, eidx=FAKE, cmp=None, ws=FAKE, ws_bytes=1 << 44, **over):
+    c = cfg160() if c is None else c
+    dw = tr.DenseI8W(g2=g2)
+    mw = tr.MoeI8W(**{**dict(Wgate=w(), Wup=w(), Wdown=w()), **over})
+    cmp = tr.Compaction(exp_cnt=FAKE, exp_off=FAKE, exp_rows=FAKE) if cmp is None else cmp
+    return tr.lib().triroute_moe_i8(C.byref(c), n, xt, C.byref(dw), C.byref(mw), eidx, FAKE,
+                                    C.byref(cmp), xo, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("over,code,word", [
+    (dict(xt=None), -1, b"NULL"), (dict(xo=None), -1, b"NULL"), (dict(g2=None), -1, b"g2"),
+    (dict(eidx=None), -1, b"NULL"), (dict(Wgate=w(codes=None)), -1, b"codes"),
+    (dict(Wdown=w(scale=None)), -1, b"codes"), (dict(Wup=w(codes=FAKE + 1)), -1, b"aligned"),
+    (dict(cmp=tr.Compaction(exp_cnt=FAKE, exp_rows=FAKE)), -1, b"NULL"),
+    (dict(g2=FAKE + 2), -1, b"aligned"), (dict(xo=FAKE + 4), -1, b"aligned"),
+    (dict(n=0), -1, b">= 1"), (dict(ws=FAKE + 16), -1, b"aligned"), (dict(ws_bytes=64), -3, b"workspace"),
+    (dict(c=cfg160(d_ff=131136)), -2, b"32-bit"), (dict(c=cfg160(d_ff=100)), -2, b"multiples")])
+def test_moe_refuses(over, code, word):
+    assert moe(**over) == code
+    assert word in tr.lib().triroute_last_error()
+
+
+def test_layer_refuses_missing_weights():
+    c, lib = cfg160(), tr.lib()
+    cache = tr.KVCacheDesc(base=FAKE, n_seq=4, capacity=64, tile_slots=64, n_tiles=1)
+    rw = tr.RouterW(*[FAKE] * 12)
+    mw = tr.MoeI8W(w(), w(), w())
+
+    def call(decode, **over):
+        dw = tr.DenseI8W(**{**dict(Wq=w(), Wk=w(), Wv=w(), Wo=w(), g2=FAKE), **over})
+        a = (C.byref(c), 2) + (() if decode else (8,)) + (None, FAKE, FAKE, C.byref(rw), C.byref(dw),
+                                                         C.byref(mw), C.byref(cache), FAKE, None, FAKE, 64, None)
+        return (lib.triroute_layer_decode_i8 if decode else lib.triroute_layer_prefill_i8)(*a)
+
+    for decode in (False, True):
+        assert call(decode, Wo=w(codes=None)) == -1 and b"codes" in lib.triroute_last_error()
+        assert call(decode, Wq=w(scale=None)) == -1
+        assert call(decode, g2=None) == -1 and b"g2" in lib.triroute_last_error()
+        assert call(decode) == -3
+        op = tr.OP_LAYER_DECODE_I8 if decode else tr.OP_LAYER_PREFILL_I8
+        assert tr.workspace_bytes(c, op, 2, 1) > tr.workspace_bytes(c, tr.OP_MOE_I8, 2, 1)
+
+
+def test_matrix_takes_whole_rows_of_codes():
+    codes, scale = torch.zeros(5, 128, dtype=torch.int8), torch.zeros(5)
+    m = tr.I8Matrix(codes, scale, 100)
+    assert m.rows == 5 and m.w.codes == codes.data_ptr() and m.w.scale == scale.data_ptr()
+    for bad in ((codes, scale, 129), (codes[:, :100], scale, 100), (codes.float(), scale, 100),
+                (codes, scale[:4], 100), (codes, scale.double(), 100)):
+        with pytest.raises(ValueError):
+            tr.I8Matrix(*bad)
+
+
+def test_tensors_of_other_shapes_are_refused():
+    m = tr.I8Matrix(torch.zeros(5, 128, dtype=torch.int8), torch.zeros(5), 100)
+    x, y, ws = torch.zeros(3, 100), torch.zeros(3, 5), torch.zeros(4096, dtype=torch.uint8)
+    for bad in (dict(x=x[:, :99]), dict(y=y[:2]), dict(y=y.bfloat16()), dict(residual=y[:, :4]),
+                dict(x=x.double()), dict(x=torch.zeros(100, 3).T), dict(residual=y.bfloat16())):
+        a = {**dict(x=x, y=y, residual=None), **bad}
+        with pytest.raises(ValueError):
+            tr.linear_i8(a["x"], m, a["y"], ws, residual=a["residual"])
+    with pytest.raises(ValueError):
+        tr.i8_quantize(x, torch.zeros(3, 100, dtype=torch.int8), torch.zeros(3))
+    with pytest.raises(ValueError):
+        tr.i8_quantize(x, torch.zeros(3, 128, dtype=torch.int8), torch.zeros(2))
