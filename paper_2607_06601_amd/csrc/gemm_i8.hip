@@ -11,6 +11,10 @@
 //   MoE-2 : Y = h Wdown_e^T
 #include "gemm_kernels.hpp"
 
+// (no product fused into a sum behind it, which the compiler would do in one kernel and not in
+// another)
+#pragma clang fp contract(off)
+
 namespace tr {
 
 __device__ __forceinline__ float dequant(int32_t v, float row, float col) {
@@ -50,10 +54,35 @@ __device__ __forceinline__ void stage_i8(const P &p, const MTile &t, float *C,
     }
 }
 
+// Largest of 16 lanes side by side, as whole numbers.
+__device__ __forceinline__ uint32_t row16_umax(uint32_t v) {
+#define TR_ROR(n) uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x120 + (n), 0xF, 0xF, false))
+  v = max(v, TR_ROR(1));
+  v = max(v, TR_ROR(2));
+  v = max(v, TR_ROR(4));
+  v = max(v, TR_ROR(8));
+#undef TR_ROR
+  return v;
+}
+
+// Four-wave kernel: a lane's columns' scales, and the scales of the rows of its row block mi.
+template <class P, int NI>
+__device__ __forceinline__ void w4_col_scales(const P &p, const MTile &t, int wn, int lane,
+                                              float (&sc)[NI]) {
+#pragma unroll
+  for (int ni = 0; ni < NI; ++ni) sc[ni] = p.template col_scale_w4<NI>(t, wn, ni, lane & 15);
+}
+template <class P>
+__device__ __forceinline__ void w4_row_scales(const P &p, const MTile &t, int r0, float (&sr)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sr[i] = p.row_scale(t, r0 + i < t.mvalid ? r0 + i : 0);
+}
+
 // ---------------------------------------------------------------- problems
-template <typename T>
+template <typename T, bool VEC>  // VEC: whole 16-byte pieces of y and residual
 struct LinearI8 {
   typedef OpI8 Op;
+  static constexpr bool WIDE = VEC;  // runs on the four-wave kernel
   static constexpr int EPI = EPI_PLAIN;
   static constexpr bool GROUPED = false;
   const int8_t *a, *w;
@@ -62,7 +91,6 @@ struct LinearI8 {
   const T *res;
   int64_t ldy, ldr;
   int N, m, pitch;
-  bool vec;  // whole 16-byte pieces of y and residual
   static constexpr int out_cols(int BN) { return BN; }
   __device__ int tiles(int BM, int ny, const GroupScan &) const { return (N + BM - 1) / BM * ny; }
   __device__ bool map(int bx, int by, int BM, int BN, MTile &t, const GroupScan &) const {
@@ -78,6 +106,54 @@ struct LinearI8 {
   }
   __device__ float row_scale(const MTile &t, int r) const { return sa[t.m0 + r]; }
   __device__ float col_scale(const MTile &t, int n) const { return t.n0 + n < m ? sw[t.n0 + n] : 0.f; }
+  // Four-wave kernel: in wave column wn, MFMA block ni, lane column c holds
+  // output column NI (16 wn + c) + ni of the tile, so each lane ends with NI
+  // consecutive columns of each of its rows.
+  static constexpr bool DIRECT_W4 = true;
+  __device__ const int8_t *a_base() const { return a; }
+  __device__ const int8_t *b_base() const { return w; }
+  __device__ uint32_t a_off(const MTile &t, int r) const { return uint32_t(t.m0 + r) * uint32_t(pitch); }
+  template <int NI>
+  __device__ uint32_t b_off_w4(const MTile &t, int wn, int ni, int c) const {
+    const int f = t.n0 + NI * (16 * wn + c) + ni;
+    return f < m ? uint32_t(f) * uint32_t(pitch) : 0u;
+  }
+  template <int NI>
+  __device__ float col_scale_w4(const MTile &t, int wn, int ni, int c) const {
+    return col_scale(t, NI * (16 * wn + c) + ni);
+  }
+  template <int MI, int NI>
+  __device__ void store_w4(const MTile &t, const i32x4_t (&acc)[MI][NI], int wm, int wn, int lane) const {
+    static_assert(NI == 8, "whole 8-column pieces");
+    const int f = t.n0 + NI * (16 * wn + (lane & 15));
+    if (f >= m) return;
+    float sc[NI];
+    w4_col_scales(*this, t, wn, lane, sc);
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+      float x[4][8], sr[4];
+      const int r0 = wm * MI * 16 + mi * 16 + 4 * (lane >> 4);
+      w4_row_scales(*this, t, r0, sr);
+      if (res) {  // a block's residual rows first, so that their loads overlap
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          load8(res + (t.m0 + (r0 + i < t.mvalid ? r0 + i : 0)) * ldr + f, x[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (r0 + i >= t.mvalid) continue;
+        const int64_t row = t.m0 + r0 + i;
+        float v[8];
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni) v[ni] = dequant(acc[mi][ni][i], sr[i], sc[ni]);
+        if (res) {
+#pragma unroll
+          for (int ni = 0; ni < NI; ++ni) v[ni] += x[i][ni];
+        }
+        store8(y + row * ldy + f, v);
+      }
+    }
+  }
   template <int MI, int NI, int TM, int TN, int LDC>
   __device__ void stage(const MTile &t, float *C, const i32x4_t (&acc)[MI][NI], int wm, int wn,
                         int lane) const {
@@ -92,7 +168,7 @@ struct LinearI8 {
       if (r >= t.mvalid || c >= m) continue;
       const int64_t row = t.m0 + r;
       const float *cr = C + r * LDC + c8;
-      if (vec) {
+      if constexpr (VEC) {
         float v[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u) v[u] = cr[u];
@@ -154,6 +230,95 @@ struct QkvI8 {
     const int gc = col(t, n);
     if (gc >= Ncols) return 0.f;
     return gc < Hd ? sq[gc] : gc < Hd + Kd ? sk[gc - Hd] : sv[gc - Hd - Kd];
+  }
+  // Four-wave kernel, 256-column tiles: wave column wn holds 128 columns, one head of
+  // d_h 128 or two of 64; lane column c has pairs j .. j + 3 of one head, blocks 2 u and
+  // 2 u + 1 the first and second half of pair j + u.
+  static constexpr bool DIRECT_W4 = true;
+  const int8_t *Wlo;         // the lowest of Wq, Wk, Wv
+  uint32_t wq_o, wk_o, wv_o; // byte offsets of Wq, Wk, Wv from Wlo less their first column's rows
+  __device__ const int8_t *a_base() const { return a; }
+  __device__ const int8_t *b_base() const { return Wlo; }
+  __device__ uint32_t a_off(const MTile &t, int r) const { return uint32_t(t.m0 + r) * uint32_t(pitch); }
+  // first column of the lane's head, and its first pair
+  __device__ void w4_head(const MTile &t, int wn, int c, int &hcol, int &j) const {
+    hcol = t.n0 + 128 * wn + (dh == 64 ? 64 * (c >> 3) : 0);
+    j = 4 * (dh == 64 ? c & 7 : c);
+  }
+  template <int NI>
+  __device__ int w4_col(const MTile &t, int wn, int ni, int c) const {
+    int hcol, j;
+    w4_head(t, wn, c, hcol, j);
+    return hcol + j + (ni >> 1) + (ni & 1) * (dh >> 1);
+  }
+  template <int NI>
+  __device__ uint32_t b_off_w4(const MTile &t, int wn, int ni, int c) const {
+    const int gc = w4_col<NI>(t, wn, ni, c);
+    // (arithmetic on the field values: a select of fields by a lane-varying
+    // condition becomes a per-lane load from the kernel arguments)
+    const uint32_t base = wq_o + uint32_t(gc >= Hd) * (wk_o - wq_o) + uint32_t(gc >= Hd + Kd) * (wv_o - wk_o);
+    return gc < Ncols ? base + uint32_t(gc) * uint32_t(pitch) : 0u;
+  }
+  template <int NI>
+  __device__ float col_scale_w4(const MTile &t, int wn, int ni, int c) const {
+    const int gc = w4_col<NI>(t, wn, ni, c);
+    if (gc >= Ncols) return 0.f;
+    return gc < Hd ? sq[gc] : gc < Hd + Kd ? sk[gc - Hd] : sv[gc - Hd - Kd];
+  }
+  template <int MI, int NI>
+  __device__ void store_w4(const MTile &t, const i32x4_t (&acc)[MI][NI], int wm, int wn, int lane) const {
+    static_assert(NI == 8, "four pairs a lane");
+    int hcol, j;
+    w4_head(t, wn, lane & 15, hcol, j);
+    if (hcol >= Ncols) return;
+    const int hd = dh >> 1;
+    T *out = q;
+    int ld = Hd, col = hcol;
+    bool rot = true;
+    if (hcol >= Hd + Kd) {
+      out = v; ld = Kd; col = hcol - Hd - Kd; rot = false;
+    } else if (hcol >= Hd) {
+      out = k; ld = Kd; col = hcol - Hd;
+    }
+    float sc[NI];
+    w4_col_scales(*this, t, wn, lane, sc);
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+      const int r0 = wm * MI * 16 + mi * 16 + 4 * (lane >> 4);
+      float sr[4];
+      w4_row_scales(*this, t, r0, sr);
+      float4 cs[4][2];
+      if (rot) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float4 *tb = (const float4 *)(rope + int64_t(t.m0 + (r0 + i < t.mvalid ? r0 + i : 0)) * hd + j);
+          cs[i][0] = tb[0];
+          cs[i][1] = tb[1];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float y1[4], y2[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float a1 = dequant(acc[mi][2 * u][i], sr[i], sc[2 * u]);
+          const float a2 = dequant(acc[mi][2 * u + 1][i], sr[i], sc[2 * u + 1]);
+          y1[u] = a1;
+          y2[u] = a2;
+          if (rot) {
+            const float4 c4 = cs[i][u >> 1];  // (cos, sin) of pairs j + 2 (u / 2), + 1
+            const float co = (u & 1) ? c4.z : c4.x, si = (u & 1) ? c4.w : c4.y;
+            y1[u] = a1 * co - a2 * si;
+            y2[u] = a1 * si + a2 * co;
+          }
+        }
+        if (r0 + i < t.mvalid) {
+          T *o = out + int64_t(t.m0 + r0 + i) * ld + col + j;
+          *(uint2 *)o = make_uint2(pk_bf16(y1[0], y1[1]), pk_bf16(y1[2], y1[3]));
+          *(uint2 *)(o + hd) = make_uint2(pk_bf16(y2[0], y2[1]), pk_bf16(y2[2], y2[3]));
+        }
+      }
+    }
   }
   template <int MI, int NI, int TM, int TN, int LDC>
   __device__ void stage(const MTile &t, float *C, const i32x4_t (&acc)[MI][NI], int wm, int wn,
@@ -249,6 +414,59 @@ struct Moe1I8 {
       return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u;
     }
   }
+  // Four-wave kernel: in wave column wn, MFMA block ni, lane column c
+  // holds expert unit (NI / 2) (16 wn + c) + ni / 2 of the tile, gate for
+  // even ni and up for odd, so each lane ends with both halves of NI / 2
+  // consecutive units.  A wave's NI * 8 units are one part of a row's maximum.
+  static constexpr bool DIRECT_W4 = true;
+  const int8_t *Wlo;  // the lower of Wg, Wu
+  __device__ const int8_t *a_base() const { return a; }
+  __device__ const int8_t *b_base() const { return Wlo; }
+  __device__ uint32_t a_off(const MTile &t, int r) const { return uint32_t(t.p0 + r) * uint32_t(pitch); }
+  template <int NI>
+  __device__ uint32_t b_off_w4(const MTile &t, int wn, int ni, int c) const {
+    const int f = t.n0 + (NI / 2) * (16 * wn + c) + (ni >> 1);
+    if (f >= dff) return 0u;
+    const uint32_t off = uint32_t(((ni & 1) ? Wu : Wg) - Wlo);
+    return off + uint32_t((t.e - 1) * dff + f) * uint32_t(pitch);
+  }
+  template <int NI>
+  __device__ float col_scale_w4(const MTile &t, int wn, int ni, int c) const {
+    const int f = t.n0 + (NI / 2) * (16 * wn + c) + (ni >> 1);
+    return f < dff ? ((ni & 1) ? su : sg)[int64_t(t.e - 1) * dff + f] : 0.f;
+  }
+  template <int MI, int NI>
+  __device__ void store_w4(const MTile &t, const i32x4_t (&acc)[MI][NI], int wm, int wn, int lane) const {
+    static_assert(NI == 8 && !F64, "4 units per lane, one 16-byte piece per row");
+    const int f = t.n0 + (NI / 2) * (16 * wn + (lane & 15));
+    const bool on = f < dff;  // d_ff is a multiple of 4: a lane's units are all in or all out
+    float sc[NI];
+    w4_col_scales(*this, t, wn, lane, sc);
+    const int pt = t.n0 / (NI * 8) + wn;  // (d_ff need not fill the wave's units)
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+      const int r0 = wm * MI * 16 + mi * 16 + 4 * (lane >> 4);
+      float sr[4];
+      w4_row_scales(*this, t, r0, sr);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = r0 + i;
+        float v[4];
+        uint32_t m = 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          v[u] = hidden(acc[mi][2 * u][i], acc[mi][2 * u + 1][i], sr[i], sc[2 * u], sc[2 * u + 1]);
+          m = max(m, __float_as_uint(v[u]) & 0x7FFFFFFFu);
+        }
+        m = row16_umax(m);
+        if (r < t.mvalid) {
+          const int64_t row = t.p0 + r;
+          if (on) *(float4 *)(h + row * dff + f) = make_float4(v[0], v[1], v[2], v[3]);
+          if ((lane & 15) == 0 && pt < nparts) part[row * nparts + pt] = m;
+        }
+      }
+    }
+  }
   template <int MI, int NI, int TM, int TN, int LDC>
   __device__ void stage(const MTile &t, float *C, const i32x4_t (&acc)[MI][NI], int wm, int wn,
                         int lane) const {
@@ -300,6 +518,42 @@ struct Moe2I8 {
   __device__ float col_scale(const MTile &t, int n) const {
     return t.n0 + n < d ? sd[int64_t(t.e - 1) * d + t.n0 + n] : 0.f;
   }
+  // Four-wave kernel: columns as in LinearI8.
+  static constexpr bool DIRECT_W4 = true;
+  __device__ const int8_t *a_base() const { return a; }
+  __device__ const int8_t *b_base() const { return Wd; }
+  __device__ uint32_t a_off(const MTile &t, int r) const { return uint32_t(t.p0 + r) * uint32_t(pitch); }
+  template <int NI>
+  __device__ uint32_t b_off_w4(const MTile &t, int wn, int ni, int c) const {
+    const int f = t.n0 + NI * (16 * wn + c) + ni;
+    return f < d ? uint32_t((t.e - 1) * d + f) * uint32_t(pitch) : 0u;
+  }
+  template <int NI>
+  __device__ float col_scale_w4(const MTile &t, int wn, int ni, int c) const {
+    return col_scale(t, NI * (16 * wn + c) + ni);
+  }
+  template <int MI, int NI>
+  __device__ void store_w4(const MTile &t, const i32x4_t (&acc)[MI][NI], int wm, int wn, int lane) const {
+    static_assert(NI == 8, "whole 8-column pieces");
+    const int f = t.n0 + NI * (16 * wn + (lane & 15));
+    if (f >= d) return;  // d is a multiple of NI: a lane's columns are all in or all out
+    float sc[NI];
+    w4_col_scales(*this, t, wn, lane, sc);
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+      const int r0 = wm * MI * 16 + mi * 16 + 4 * (lane >> 4);
+      float sr[4];
+      w4_row_scales(*this, t, r0, sr);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (r0 + i >= t.mvalid) continue;
+        float v[8];
+#pragma unroll
+        for (int ni = 0; ni < NI; ++ni) v[ni] = dequant(acc[mi][ni][i], sr[i], sc[ni]);
+        store8(Y + int64_t(t.p0 + r0 + i) * d + f, v);
+      }
+    }
+  }
   template <int MI, int NI, int TM, int TN, int LDC>
   __device__ void stage(const MTile &t, float *C, const i32x4_t (&acc)[MI][NI], int wm, int wn,
                         int lane) const {
@@ -321,17 +575,33 @@ struct Moe2I8 {
 // Rows a launch may take: its blocks stay far below the limits of a grid.
 static int rows_a_launch(int c64) { return std::max(1, (1 << 22) / c64) * 32; }
 
-template <typename T>
-static hipError_t linear_rows(const LinearI8<T> &all, hipStream_t st) {
-  const int K2 = all.pitch / 2, c64 = (all.m + 63) / 64, most = rows_a_launch(c64);
+template <class P>
+static hipError_t linear_rows(const P &all, hipStream_t st) {
+  const int K2 = all.pitch / 2, c64 = (all.m + 63) / 64, c128 = (all.m + 127) / 128;
+  const int most = rows_a_launch(c64);
   for (int at = 0; at < all.N; at += most) {
-    LinearI8<T> p = all;
+    P p = all;
     p.N = std::min(most, all.N - at);
     p.a += int64_t(at) * p.pitch;
     p.sa += at;
     p.y += at * p.ldy;
     if (p.res) p.res += at * p.ldr;
-    const hipError_t e = launch<LinearI8<T>, 32, 64, 2, 1, 64, 4>(p, K2, (p.N + 31) / 32, c64, st);
+    hipError_t e;
+    bool w4 = false;  // (rows of odd places are written from LDS by the smaller tiles)
+    const int8_t *lo;
+    const int m32 = (p.N + 31) / 32, m256 = (p.N + 255) / 256, c256 = (p.m + 255) / 256;
+    if constexpr (P::WIDE)
+      w4 = K2 >= 128 && span32({{p.a, size_t(p.N) * p.pitch}}, &lo) &&
+           span32({{p.w, size_t(p.m) * p.pitch}}, &lo) &&
+           w4_rounds(p.N, c128, tile_cost(m256 * c256, COST_256X256));
+    if (few_tiles(p.N, c128) && split_k(m32 * c64, K2))
+      e = launch<P, 32, 64, 2, 1, 64, 4, 2>(p, K2, m32, c64, st);
+    else if (few_tiles(p.N, c128))
+      e = launch<P, 32, 64, 2, 1, 64, 4>(p, K2, m32, c64, st);
+    else if (!w4)
+      e = launch_mid(p, K2, p.N, c128, st);
+    else if constexpr (P::WIDE)
+      e = launch_w4<P, 256, 256>(p, K2, m256, c256, st);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -340,9 +610,9 @@ static hipError_t linear_rows(const LinearI8<T> &all, hipStream_t st) {
 hipError_t i8_linear(int act, int N, int m, int k, const int8_t *a, const float *sa,
                      const triroute_i8_w &w, const void *res, int64_t ldr, void *y, int64_t ldy,
                      hipStream_t st) {
-  auto run = [&](auto tag) {
+  auto run = [&](auto tag, auto vec) {
     using T = decltype(tag);
-    LinearI8<T> p;
+    LinearI8<T, decltype(vec)::value> p;
     p.a = a;
     p.sa = sa;
     p.w = (const int8_t *)w.codes;
@@ -354,11 +624,13 @@ hipError_t i8_linear(int act, int N, int m, int k, const int8_t *a, const float 
     p.N = N;
     p.m = m;
     p.pitch = i8_pitch(k);
-    p.vec = m % 8 == 0 && ((uintptr_t(y) | uintptr_t(ldy * int64_t(sizeof(T)))) & 15) == 0 &&
-            (!res || ((uintptr_t(res) | uintptr_t(ldr * int64_t(sizeof(T)))) & 15) == 0);
     return linear_rows(p, st);
   };
-  return act == TRIROUTE_BF16 ? run(bf16{}) : run(float{});
+  const int es = act == TRIROUTE_BF16 ? 2 : 4;
+  const bool vec = m % 8 == 0 && ((uintptr_t(y) | uintptr_t(ldy * es)) & 15) == 0 &&
+                   (!res || ((uintptr_t(res) | uintptr_t(ldr * es)) & 15) == 0);
+  if (act == TRIROUTE_BF16) return vec ? run(bf16{}, std::true_type{}) : run(bf16{}, std::false_type{});
+  return vec ? run(float{}, std::true_type{}) : run(float{}, std::false_type{});
 }
 
 hipError_t i8_qkv(const triroute_cfg &cfg, int N, const int8_t *a, const float *sa,
@@ -389,10 +661,27 @@ hipError_t i8_qkv(const triroute_cfg &cfg, int N, const int8_t *a, const float *
       p.k = (T *)k + int64_t(at) * p.Kd;
       p.v = (T *)v + int64_t(at) * p.Kd;
       hipError_t e;
-      if (p.dh == 64)
-        e = launch<QkvI8<T>, 32, 64, 2, 1, 64, 4>(p, K2, (p.N + 31) / 32, c64, st);
-      else
-        e = launch<QkvI8<T>, 32, 128, 2, 2, 64, 4>(p, K2, (p.N + 31) / 32, c64 / 2, st);
+      const int8_t *lo;
+      const int c128 = (p.Ncols + 127) / 128, m256 = (p.N + 255) / 256, c256 = (p.Ncols + 255) / 256;
+      bool w4 = false;
+      if constexpr (std::is_same<T, bf16>::value)
+        w4 = K2 >= 128 && span32({{p.a, size_t(p.N) * p.pitch}}, &lo) &&
+             span32({{p.Wq, size_t(p.Hd) * p.pitch}, {p.Wk, size_t(p.Kd) * p.pitch},
+                     {p.Wv, size_t(p.Kd) * p.pitch}}, &p.Wlo) &&
+             w4_rounds(p.N, c128, tile_cost(m256 * c256, COST_256X256));
+      if (few_tiles(p.N, c128)) {
+        if (p.dh == 64)
+          e = launch<QkvI8<T>, 32, 64, 2, 1, 64, 4>(p, K2, (p.N + 31) / 32, c64, st);
+        else
+          e = launch<QkvI8<T>, 32, 128, 2, 2, 64, 4>(p, K2, (p.N + 31) / 32, c64 / 2, st);
+      } else if (!w4) {
+        e = launch_mid(p, K2, p.N, c128, st);
+      } else if constexpr (std::is_same<T, bf16>::value) {
+        p.wq_o = uint32_t(p.Wq - p.Wlo);
+        p.wk_o = uint32_t(p.Wk - p.Wlo) - uint32_t(p.Hd) * uint32_t(p.pitch);
+        p.wv_o = uint32_t(p.Wv - p.Wlo) - uint32_t(p.Hd + p.Kd) * uint32_t(p.pitch);
+        e = launch_w4<QkvI8<T>, 256, 256>(p, K2, m256, c256, st);
+      }
       if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -405,6 +694,10 @@ int i8_hidden_parts(const triroute_cfg &cfg) { return (cfg.d_ff + 31) / 32; }
 hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
                   const triroute_compaction &c, const MoeI8Ws &ws, hipStream_t st) {
   const int E = cfg.n_experts, Nk = N * cfg.top_k, d = cfg.d_model, dff = cfg.d_ff;
+  // rows of an expert when the router spreads its options evenly, and the tiles of BM rows that
+  // E such experts make (a few rows more, as the counts vary)
+  const int r = Nk / (E + 1);
+  auto row_tiles = [&](int BM) { return E * ((r + r / 32 + BM) / BM); };
   auto up = [&](auto f64) {
     typedef Moe1I8<decltype(f64)::value> P;
     P p;
@@ -420,8 +713,30 @@ hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
     p.E = E;
     p.dff = dff;
     p.pitch = i8_pitch(d);
-    p.nparts = (dff + 31) / 32;
-    const hipError_t e = launch<P, 32, 64, 2, 1, 64, 4>(p, p.pitch / 2, Nk / 32 + E, p.nparts, st);
+    const int K2 = p.pitch / 2;
+    const size_t wb = size_t(E) * dff * p.pitch;
+    const int8_t *lo;
+    bool w4 = false;
+    if constexpr (!decltype(f64)::value)
+      w4 = r > 64 && K2 >= 128 && span32({{p.Wg, wb}, {p.Wu, wb}}, &p.Wlo) &&
+           span32({{p.a, size_t(Nk) * p.pitch}}, &lo) &&
+           !one_round(row_tiles(128) * ((dff + 63) / 64));
+    const int ny = (dff + 127) / 128;
+    hipError_t e;
+    p.nparts = (dff + 63) / 64;
+    if (r <= 24) {
+      p.nparts = (dff + 31) / 32;
+      e = launch<P, 32, 64, 2, 1, 64, 4>(p, K2, Nk / 32 + E, p.nparts, st);
+    } else if (r <= 64) {
+      e = launch<P, 64, 128, 2, 2, 64, 3>(p, K2, Nk / 64 + E, p.nparts, st);
+    } else if (!w4) {
+      e = launch<P, 128, 128, 4, 2, 64, 3>(p, K2, Nk / 128 + E, p.nparts, st);
+    } else if constexpr (!decltype(f64)::value) {
+      if (tile_cost(row_tiles(128) * ny, 1.f) < tile_cost(row_tiles(256) * ny, 1.77f))
+        e = launch_w4<P, 128, 256>(p, K2, Nk / 128 + E, ny, st);
+      else
+        e = launch_w4<P, 256, 256>(p, K2, Nk / 256 + E, ny, st);
+    }
     if (e != hipSuccess) return e;
     return launch_i8_hidden(cfg, Nk, ws.h, ws.part, p.nparts, c.exp_off, ws.hq, ws.s_h, st);
   };
@@ -437,7 +752,17 @@ hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
   p.E = E;
   p.d = d;
   p.pitch = i8_pitch(dff);
-  return launch<Moe2I8, 32, 64, 2, 1, 64, 4>(p, p.pitch / 2, Nk / 32 + E, (d + 63) / 64, st);
+  const int K2 = p.pitch / 2, c64 = (d + 63) / 64, c128 = (d + 127) / 128, c256 = (d + 255) / 256;
+  const int8_t *lo;
+  if (r <= 64 && row_tiles(64) * c128 < 256)
+    return launch<Moe2I8, 32, 64, 2, 1, 64, 4>(p, K2, Nk / 32 + E, c64, st);
+  if (r <= 64) return launch<Moe2I8, 64, 128, 2, 2, 64, 2>(p, K2, Nk / 64 + E, c128, st);
+  if (K2 < 128 || one_round(row_tiles(128) * c128) || !span32({{p.Wd, size_t(E) * d * p.pitch}}, &lo) ||
+      !span32({{p.a, size_t(Nk) * p.pitch}}, &lo))
+    return launch<Moe2I8, 128, 128, 4, 2, 64, 3>(p, K2, Nk / 128 + E, c128, st);
+  if (row_tiles(256) > E && tile_cost(row_tiles(128) * c256, 1.f) < tile_cost(row_tiles(256) * c256, 1.77f))
+    return launch_w4<Moe2I8, 128, 256>(p, K2, Nk / 128 + E, c256, st);
+  return launch_w4<Moe2I8, 256, 256>(p, K2, Nk / 256 + E, c256, st);
 }
 
 }  // namespace tr

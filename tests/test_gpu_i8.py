@@ -147,6 +147,10 @@ def test_linear_of_many_tokens(N, k, m, act):
             want = y if res is None else y + res.double()
             err = 3.01 * i8.U * y.abs() + (1.01 * i8.U + 1.01 * u) * want.abs() + 1e-38
             assert ((got - want).abs() <= err).all()
+            # the small tiles give the same bits
+            for lo in range(0, N, 499):
+                part = run_linear(xt[lo:lo + 40], W, act, residual=None if res is None else res[lo:lo + 40])
+                assert (torch.from_numpy(part).to(DEV).double() == got[lo:lo + 40]).all()
 
 
 def test_linear_in_place_and_strided():
