@@ -196,6 +196,17 @@ __device__ __forceinline__ void dma16_s(const void *sbase, uint32_t voff, uint32
       : "memory", "m0");
 }
 
+// The same of 4 bytes a lane, to LDS address lds + 4 * lane.
+__device__ __forceinline__ void dma4(const void *src, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %1\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dword %0, off"
+      :
+      : "v"(src), "s"(__builtin_amdgcn_readfirstlane(lds))
+      : "memory", "m0");
+}
+
 // s_waitcnt vmcnt(N) with the other counters left free (gfx9 encoding:
 // vmcnt[3:0] at bits 3:0, vmcnt[5:4] at bits 15:14, expcnt 6:4, lgkmcnt 11:8).
 template <int N>

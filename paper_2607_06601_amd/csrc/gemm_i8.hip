@@ -7,7 +7,7 @@
 //
 //   linear: y = x W^T (+ residual), any sizes and row strides
 //   QKV   : [n1] x [Wq;Wk;Wv]^T, rotate-half RoPE on q and k
-//   MoE-1 : h = silu(G) U per expert, fp32, and each tile's largest |h| of a row
+//   MoE-1 : h = silu(G) U per expert, fp32
 //   MoE-2 : Y = h Wdown_e^T
 #include "gemm_kernels.hpp"
 
@@ -54,28 +54,23 @@ __device__ __forceinline__ void stage_i8(const P &p, const MTile &t, float *C,
     }
 }
 
-// Largest of 16 lanes side by side, as whole numbers.
-__device__ __forceinline__ uint32_t row16_umax(uint32_t v) {
-#define TR_ROR(n) uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x120 + (n), 0xF, 0xF, false))
-  v = max(v, TR_ROR(1));
-  v = max(v, TR_ROR(2));
-  v = max(v, TR_ROR(4));
-  v = max(v, TR_ROR(8));
-#undef TR_ROR
-  return v;
+// Four-wave kernel: the wave's scales in LDS, its TM rows', then its TN columns'; the
+// four rows of a lane in row block mi, and its columns' where it holds NI of them side by side.
+template <int MI>
+__device__ __forceinline__ float4 w4_rows(const float *sc, int mi, int lane) {
+  return *(const float4 *)(sc + mi * 16 + 4 * (lane >> 4));
 }
-
-// Four-wave kernel: a lane's columns' scales, and the scales of the rows of its row block mi.
-template <class P, int NI>
-__device__ __forceinline__ void w4_col_scales(const P &p, const MTile &t, int wn, int lane,
-                                              float (&sc)[NI]) {
+template <int MI, int NI>
+__device__ __forceinline__ void w4_cols(const float *sc, int lane, float (&c)[NI]) {
+  const float4 *p = (const float4 *)(sc + MI * 16 + NI * (lane & 15));
 #pragma unroll
-  for (int ni = 0; ni < NI; ++ni) sc[ni] = p.template col_scale_w4<NI>(t, wn, ni, lane & 15);
+  for (int q = 0; q < NI / 4; ++q) {
+    const float4 v = p[q];
+    c[4 * q] = v.x; c[4 * q + 1] = v.y; c[4 * q + 2] = v.z; c[4 * q + 3] = v.w;
+  }
 }
-template <class P>
-__device__ __forceinline__ void w4_row_scales(const P &p, const MTile &t, int r0, float (&sr)[4]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) sr[i] = p.row_scale(t, r0 + i < t.mvalid ? r0 + i : 0);
+__device__ __forceinline__ float elem(const float4 &v, int i) {
+  return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
 }
 
 // ---------------------------------------------------------------- problems
@@ -118,22 +113,25 @@ struct LinearI8 {
     const int f = t.n0 + NI * (16 * wn + c) + ni;
     return f < m ? uint32_t(f) * uint32_t(pitch) : 0u;
   }
-  template <int NI>
-  __device__ float col_scale_w4(const MTile &t, int wn, int ni, int c) const {
-    return col_scale(t, NI * (16 * wn + c) + ni);
+  __device__ const float *row_scale_at(const MTile &t, int r) const { return sa + t.m0 + r; }
+  // scale n of wave column wn (TN of them)
+  template <int TN>
+  __device__ const float *col_scale_at(const MTile &t, int wn, int n) const {
+    return sw + min(t.n0 + TN * wn + n, m - 1);
   }
   template <int MI, int NI>
-  __device__ void store_w4(const MTile &t, const i32x4_t (&acc)[MI][NI], int wm, int wn, int lane) const {
+  __device__ void store_w4(const MTile &t, const i32x4_t (&acc)[MI][NI], const float *scales, int wm,
+                           int wn, int lane) const {
     static_assert(NI == 8, "whole 8-column pieces");
     const int f = t.n0 + NI * (16 * wn + (lane & 15));
     if (f >= m) return;
     float sc[NI];
-    w4_col_scales(*this, t, wn, lane, sc);
+    w4_cols<MI>(scales, lane, sc);
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
-      float x[4][8], sr[4];
+      float x[4][8];
       const int r0 = wm * MI * 16 + mi * 16 + 4 * (lane >> 4);
-      w4_row_scales(*this, t, r0, sr);
+      const float4 sr = w4_rows<MI>(scales, mi, lane);
       if (res) {  // a block's residual rows first, so that their loads overlap
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -145,7 +143,7 @@ struct LinearI8 {
         const int64_t row = t.m0 + r0 + i;
         float v[8];
 #pragma unroll
-        for (int ni = 0; ni < NI; ++ni) v[ni] = dequant(acc[mi][ni][i], sr[i], sc[ni]);
+        for (int ni = 0; ni < NI; ++ni) v[ni] = dequant(acc[mi][ni][i], elem(sr, i), sc[ni]);
         if (res) {
 #pragma unroll
           for (int ni = 0; ni < NI; ++ni) v[ni] += x[i][ni];
@@ -259,14 +257,15 @@ struct QkvI8 {
     const uint32_t base = wq_o + uint32_t(gc >= Hd) * (wk_o - wq_o) + uint32_t(gc >= Hd + Kd) * (wv_o - wk_o);
     return gc < Ncols ? base + uint32_t(gc) * uint32_t(pitch) : 0u;
   }
-  template <int NI>
-  __device__ float col_scale_w4(const MTile &t, int wn, int ni, int c) const {
-    const int gc = w4_col<NI>(t, wn, ni, c);
-    if (gc >= Ncols) return 0.f;
-    return gc < Hd ? sq[gc] : gc < Hd + Kd ? sk[gc - Hd] : sv[gc - Hd - Kd];
+  __device__ const float *row_scale_at(const MTile &t, int r) const { return sa + t.m0 + r; }
+  template <int TN>
+  __device__ const float *col_scale_at(const MTile &t, int wn, int n) const {
+    const int gc = min(t.n0 + TN * wn + n, Ncols - 1);
+    return gc < Hd ? sq + gc : gc < Hd + Kd ? sk + (gc - Hd) : sv + (gc - Hd - Kd);
   }
   template <int MI, int NI>
-  __device__ void store_w4(const MTile &t, const i32x4_t (&acc)[MI][NI], int wm, int wn, int lane) const {
+  __device__ void store_w4(const MTile &t, const i32x4_t (&acc)[MI][NI], const float *scales, int wm,
+                           int wn, int lane) const {
     static_assert(NI == 8, "four pairs a lane");
     int hcol, j;
     w4_head(t, wn, lane & 15, hcol, j);
@@ -280,13 +279,12 @@ struct QkvI8 {
     } else if (hcol >= Hd) {
       out = k; ld = Kd; col = hcol - Hd;
     }
-    float sc[NI];
-    w4_col_scales(*this, t, wn, lane, sc);
+    const float *cl = scales + MI * 16 + (hcol - t.n0 - 128 * wn) + j;
+    const float4 sc1 = *(const float4 *)cl, sc2 = *(const float4 *)(cl + hd);
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
       const int r0 = wm * MI * 16 + mi * 16 + 4 * (lane >> 4);
-      float sr[4];
-      w4_row_scales(*this, t, r0, sr);
+      const float4 sr = w4_rows<MI>(scales, mi, lane);
       float4 cs[4][2];
       if (rot) {
 #pragma unroll
@@ -301,8 +299,8 @@ struct QkvI8 {
         float y1[4], y2[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const float a1 = dequant(acc[mi][2 * u][i], sr[i], sc[2 * u]);
-          const float a2 = dequant(acc[mi][2 * u + 1][i], sr[i], sc[2 * u + 1]);
+          const float a1 = dequant(acc[mi][2 * u][i], elem(sr, i), elem(sc1, u));
+          const float a2 = dequant(acc[mi][2 * u + 1][i], elem(sr, i), elem(sc2, u));
           y1[u] = a1;
           y2[u] = a2;
           if (rot) {
@@ -380,9 +378,8 @@ struct Moe1I8 {
   const int8_t *a, *Wg, *Wu;  // a: rows in list order
   const float *sa, *sg, *su;
   float *h;
-  uint32_t *part;  // [list rows][nparts]: bits of the largest |h| of a row in a column tile
   const int32_t *cnt;
-  int E, dff, pitch, nparts;
+  int E, dff, pitch;
   static constexpr int out_cols(int BN) { return BN / 2; }
   __device__ int tiles(int BM, int ny, const GroupScan &gs) const { return gs.total * ny; }
   __device__ bool map(int bx, int by, int BM, int BN, MTile &t, const GroupScan &gs) const {
@@ -430,40 +427,34 @@ struct Moe1I8 {
     const uint32_t off = uint32_t(((ni & 1) ? Wu : Wg) - Wlo);
     return off + uint32_t((t.e - 1) * dff + f) * uint32_t(pitch);
   }
-  template <int NI>
-  __device__ float col_scale_w4(const MTile &t, int wn, int ni, int c) const {
-    const int f = t.n0 + (NI / 2) * (16 * wn + c) + (ni >> 1);
-    return f < dff ? ((ni & 1) ? su : sg)[int64_t(t.e - 1) * dff + f] : 0.f;
+  __device__ const float *row_scale_at(const MTile &t, int r) const { return sa + t.p0 + r; }
+  // the wave's TN / 2 gate scales, then its up scales
+  template <int TN>
+  __device__ const float *col_scale_at(const MTile &t, int wn, int n) const {
+    const int u = n < TN / 2 ? n : n - TN / 2;
+    return (n < TN / 2 ? sg : su) + (int64_t(t.e - 1) * dff + min(t.n0 + TN / 2 * wn + u, dff - 1));
   }
   template <int MI, int NI>
-  __device__ void store_w4(const MTile &t, const i32x4_t (&acc)[MI][NI], int wm, int wn, int lane) const {
+  __device__ void store_w4(const MTile &t, const i32x4_t (&acc)[MI][NI], const float *scales, int wm,
+                           int wn, int lane) const {
     static_assert(NI == 8 && !F64, "4 units per lane, one 16-byte piece per row");
     const int f = t.n0 + (NI / 2) * (16 * wn + (lane & 15));
-    const bool on = f < dff;  // d_ff is a multiple of 4: a lane's units are all in or all out
-    float sc[NI];
-    w4_col_scales(*this, t, wn, lane, sc);
-    const int pt = t.n0 / (NI * 8) + wn;  // (d_ff need not fill the wave's units)
+    if (f >= dff) return;  // d_ff is a multiple of 4: a lane's units are all in or all out
+    const float *cl = scales + MI * 16 + (NI / 2) * (lane & 15);
+    const float4 cg = *(const float4 *)cl, cu = *(const float4 *)(cl + NI * 8);
+    float *out = h + int64_t(t.p0) * dff;  // (wave-uniform; a lane's offset fits 32 bits)
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
       const int r0 = wm * MI * 16 + mi * 16 + 4 * (lane >> 4);
-      float sr[4];
-      w4_row_scales(*this, t, r0, sr);
+      const float4 sr = w4_rows<MI>(scales, mi, lane);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int r = r0 + i;
         float v[4];
-        uint32_t m = 0;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          v[u] = hidden(acc[mi][2 * u][i], acc[mi][2 * u + 1][i], sr[i], sc[2 * u], sc[2 * u + 1]);
-          m = max(m, __float_as_uint(v[u]) & 0x7FFFFFFFu);
-        }
-        m = row16_umax(m);
-        if (r < t.mvalid) {
-          const int64_t row = t.p0 + r;
-          if (on) *(float4 *)(h + row * dff + f) = make_float4(v[0], v[1], v[2], v[3]);
-          if ((lane & 15) == 0 && pt < nparts) part[row * nparts + pt] = m;
-        }
+        for (int u = 0; u < 4; ++u)
+          v[u] = hidden(acc[mi][2 * u][i], acc[mi][2 * u + 1][i], elem(sr, i), elem(cg, u), elem(cu, u));
+        if (r0 + i < t.mvalid)
+          *(float4 *)(out + uint32_t((r0 + i) * dff + f)) = make_float4(v[0], v[1], v[2], v[3]);
       }
     }
   }
@@ -472,24 +463,14 @@ struct Moe1I8 {
                         int lane) const {
     stage_i8<Moe1I8, MI, NI, TM, TN, LDC>(*this, t, C, acc, wm, wn, lane);
   }
-  // item = 8 expert units of one row; the CC items of a row lie in CC lanes side by side
+  // item = 8 expert units of one row (C holds silu(g) u)
   template <int BM, int NC, int LDC, int NT>
   __device__ void epilogue(const MTile &t, const float *C, int tid) const {
     constexpr int CC = NC / 8;
-    static_assert(NT % CC == 0 && 64 % CC == 0, "a row's items in one wave");
     for (int it = tid; it < BM * CC; it += NT) {
       const int r = it / CC, c8 = (it % CC) * 8;
-      const bool on = r < t.mvalid && t.n0 + c8 < dff;  // d_ff is a multiple of 8
-      const float *cr = C + r * LDC + c8;
-      uint32_t m = 0;
-      if (on) {
-#pragma unroll
-        for (int u = 0; u < 8; ++u) m = max(m, __float_as_uint(cr[u]) & 0x7FFFFFFFu);
-        store8(h + int64_t(t.p0 + r) * dff + t.n0 + c8, cr);
-      }
-#pragma unroll
-      for (int s = 1; s < CC; s <<= 1) m = max(m, uint32_t(__shfl_xor(int(m), s, 64)));
-      if (r < t.mvalid && c8 == 0) part[int64_t(t.p0 + r) * nparts + t.n0 / NC] = m;
+      if (r >= t.mvalid || t.n0 + c8 >= dff) continue;
+      store8(h + int64_t(t.p0 + r) * dff + t.n0 + c8, C + r * LDC + c8);
     }
   }
 };
@@ -528,29 +509,31 @@ struct Moe2I8 {
     const int f = t.n0 + NI * (16 * wn + c) + ni;
     return f < d ? uint32_t((t.e - 1) * d + f) * uint32_t(pitch) : 0u;
   }
-  template <int NI>
-  __device__ float col_scale_w4(const MTile &t, int wn, int ni, int c) const {
-    return col_scale(t, NI * (16 * wn + c) + ni);
+  __device__ const float *row_scale_at(const MTile &t, int r) const { return sa + t.p0 + r; }
+  template <int TN>
+  __device__ const float *col_scale_at(const MTile &t, int wn, int n) const {
+    return sd + (int64_t(t.e - 1) * d + min(t.n0 + TN * wn + n, d - 1));
   }
   template <int MI, int NI>
-  __device__ void store_w4(const MTile &t, const i32x4_t (&acc)[MI][NI], int wm, int wn, int lane) const {
+  __device__ void store_w4(const MTile &t, const i32x4_t (&acc)[MI][NI], const float *scales, int wm,
+                           int wn, int lane) const {
     static_assert(NI == 8, "whole 8-column pieces");
     const int f = t.n0 + NI * (16 * wn + (lane & 15));
     if (f >= d) return;  // d is a multiple of NI: a lane's columns are all in or all out
     float sc[NI];
-    w4_col_scales(*this, t, wn, lane, sc);
+    w4_cols<MI>(scales, lane, sc);
+    float *out = Y + int64_t(t.p0) * d;  // (wave-uniform; a lane's offset fits 32 bits)
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
       const int r0 = wm * MI * 16 + mi * 16 + 4 * (lane >> 4);
-      float sr[4];
-      w4_row_scales(*this, t, r0, sr);
+      const float4 sr = w4_rows<MI>(scales, mi, lane);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (r0 + i >= t.mvalid) continue;
         float v[8];
 #pragma unroll
-        for (int ni = 0; ni < NI; ++ni) v[ni] = dequant(acc[mi][ni][i], sr[i], sc[ni]);
-        store8(Y + int64_t(t.p0 + r0 + i) * d + f, v);
+        for (int ni = 0; ni < NI; ++ni) v[ni] = dequant(acc[mi][ni][i], elem(sr, i), sc[ni]);
+        store8(out + uint32_t((r0 + i) * d + f), v);
       }
     }
   }
@@ -586,7 +569,7 @@ static hipError_t linear_rows(const P &all, hipStream_t st) {
     p.sa += at;
     p.y += at * p.ldy;
     if (p.res) p.res += at * p.ldr;
-    hipError_t e;
+    hipError_t e = hipErrorInvalidValue;
     bool w4 = false;  // (rows of odd places are written from LDS by the smaller tiles)
     const int8_t *lo;
     const int m32 = (p.N + 31) / 32, m256 = (p.N + 255) / 256, c256 = (p.m + 255) / 256;
@@ -660,7 +643,7 @@ hipError_t i8_qkv(const triroute_cfg &cfg, int N, const int8_t *a, const float *
       p.q = (T *)q + int64_t(at) * p.Hd;
       p.k = (T *)k + int64_t(at) * p.Kd;
       p.v = (T *)v + int64_t(at) * p.Kd;
-      hipError_t e;
+      hipError_t e = hipErrorInvalidValue;
       const int8_t *lo;
       const int c128 = (p.Ncols + 127) / 128, m256 = (p.N + 255) / 256, c256 = (p.Ncols + 255) / 256;
       bool w4 = false;
@@ -689,8 +672,6 @@ hipError_t i8_qkv(const triroute_cfg &cfg, int N, const int8_t *a, const float *
   return cfg.act == TRIROUTE_BF16 ? run(bf16{}) : run(float{});
 }
 
-int i8_hidden_parts(const triroute_cfg &cfg) { return (cfg.d_ff + 31) / 32; }
-
 hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
                   const triroute_compaction &c, const MoeI8Ws &ws, hipStream_t st) {
   const int E = cfg.n_experts, Nk = N * cfg.top_k, d = cfg.d_model, dff = cfg.d_ff;
@@ -708,7 +689,6 @@ hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
     p.sg = w.Wgate.scale;
     p.su = w.Wup.scale;
     p.h = ws.h;
-    p.part = ws.part;
     p.cnt = c.exp_cnt;
     p.E = E;
     p.dff = dff;
@@ -722,15 +702,14 @@ hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
            span32({{p.a, size_t(Nk) * p.pitch}}, &lo) &&
            !one_round(row_tiles(128) * ((dff + 63) / 64));
     const int ny = (dff + 127) / 128;
-    hipError_t e;
-    p.nparts = (dff + 63) / 64;
+    hipError_t e = hipErrorInvalidValue;
+    const int c64 = (dff + 63) / 64;
     if (r <= 24) {
-      p.nparts = (dff + 31) / 32;
-      e = launch<P, 32, 64, 2, 1, 64, 4>(p, K2, Nk / 32 + E, p.nparts, st);
+      e = launch<P, 32, 64, 2, 1, 64, 4>(p, K2, Nk / 32 + E, (dff + 31) / 32, st);
     } else if (r <= 64) {
-      e = launch<P, 64, 128, 2, 2, 64, 3>(p, K2, Nk / 64 + E, p.nparts, st);
+      e = launch<P, 64, 128, 2, 2, 64, 3>(p, K2, Nk / 64 + E, c64, st);
     } else if (!w4) {
-      e = launch<P, 128, 128, 4, 2, 64, 3>(p, K2, Nk / 128 + E, p.nparts, st);
+      e = launch<P, 128, 128, 4, 2, 64, 3>(p, K2, Nk / 128 + E, c64, st);
     } else if constexpr (!decltype(f64)::value) {
       if (tile_cost(row_tiles(128) * ny, 1.f) < tile_cost(row_tiles(256) * ny, 1.77f))
         e = launch_w4<P, 128, 256>(p, K2, Nk / 128 + E, ny, st);
@@ -738,7 +717,7 @@ hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
         e = launch_w4<P, 256, 256>(p, K2, Nk / 256 + E, ny, st);
     }
     if (e != hipSuccess) return e;
-    return launch_i8_hidden(cfg, Nk, ws.h, ws.part, p.nparts, c.exp_off, ws.hq, ws.s_h, st);
+    return launch_i8_hidden(cfg, Nk, ws.h, c.exp_off, ws.hq, ws.s_h, st);
   };
   const hipError_t e = cfg.act == TRIROUTE_BF16 ? up(std::false_type{}) : up(std::true_type{});
   if (e != hipSuccess) return e;

@@ -311,7 +311,12 @@ __global__ __launch_bounds__(256, 1) void gemm_w4_kernel(P p, int K, int ny) {
   static_assert(B1J < NM && RS >= 16 && RS + NF <= NM && GAP >= 1 && GAP * (IPW - 1) < NSLOT,
                 "room for the reads and transfers");
   static_assert(P::DIRECT_W4, "results are written from the accumulators");
-  __shared__ __align__(1024) uint8_t smem[2 * STAGE];
+  // 8-bit products: the scales of each wave's TM rows and TN columns lie behind the stages.  They
+  // come in the tile's first K step, as transfers like the operands' (a load into registers
+  // would be waited for behind the next tile's transfers, at the tile's end) ahead of the next
+  // stage's, so that step's wait covers them.
+  constexpr int NSC = P::Op::INT ? TM + TN : 0;
+  __shared__ __align__(1024) uint8_t smem[2 * STAGE + NW * NSC * 4];
   // Persistent: block b takes tiles b, b + gridDim.x, ... (one block per CU).
   // The operand stream runs on across tiles: the last two K steps of a tile
   // fetch the first two stages of the block's next tile, so its transfers
@@ -404,6 +409,21 @@ __global__ __launch_bounds__(256, 1) void gemm_w4_kernel(P p, int K, int ny) {
     mfma_agpr_first(acc[j / NI][j % NI], fa[set][j / NI], fb[set][j % NI]);
   };
 
+  auto issue_scales = [&](const MTile &t) {
+    if constexpr (P::Op::INT) {
+      const uint32_t at = lds_addr(smem) + 2 * STAGE + wave * NSC * 4;
+      const int ln = pinned_lane();
+#pragma unroll
+      for (int j = 0; j < TM / 64; ++j) {
+        const int r = wm * TM + 64 * j + ln;
+        dma4(p.row_scale_at(t, r < t.mvalid ? r : 0), at + j * 256);
+      }
+#pragma unroll
+      for (int j = 0; j < TN / 64; ++j)
+        dma4(p.template col_scale_at<TN>(t, wn, 64 * j + ln), at + (TM + 64 * j) * 4);
+    }
+  };
+
   const int nk = K / BK;  // >= 2 (host)
 #pragma unroll
   for (int j = 0; j < IPW; ++j) dma16_s(gbase(j), voff[j], sbase + j * 1024);
@@ -467,13 +487,17 @@ __global__ __launch_bounds__(256, 1) void gemm_w4_kernel(P p, int K, int ny) {
         if (j >= RS && j - RS < NF) read_piece(0, buf ^ 1, j - RS);
       }
     };
+    issue_scales(tc);
     kstep(0, std::true_type{});
     for (int kt = 1; kt < nk; ++kt) kstep(kt, std::false_type{});
     // the last MFMAs' results are read below: let them drain first
     asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory");
 #pragma unroll
     for (int i = 0; i < MI; ++i) acc_fence_row<NI>(acc[i]);
-    p.store_w4(tc, acc, wm, wn, pinned_lane());
+    if constexpr (P::Op::INT)
+      p.store_w4(tc, acc, (const float *)(smem + 2 * STAGE) + wave * NSC, wm, wn, pinned_lane());
+    else
+      p.store_w4(tc, acc, wm, wn, pinned_lane());
     if (!more) break;
     ph ^= nk & 1;
     // the next tile's stage 0 is in buffer ph (published by the last step's barrier)

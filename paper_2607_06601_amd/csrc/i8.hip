@@ -78,9 +78,11 @@ __device__ __forceinline__ void row8(const T *row, int c, int cols, float *v) {
 // read again.
 template <typename T, bool VEC, int W, int RR>
 __global__ __launch_bounds__(256) void i8_rows_kernel(const T *__restrict__ x, int64_t ldx,
-                                                      int64_t rows, int cols, int pitch,
-                                                      int8_t *__restrict__ codes,
+                                                      int64_t rows,
+                                                      const int32_t *__restrict__ d_rows, int cols,
+                                                      int pitch, int8_t *__restrict__ codes,
                                                       float *__restrict__ scale) {
+  if (d_rows) rows = min(rows, int64_t(*d_rows));
   constexpr int STEP = 512 * W;
   __shared__ uint32_t part[4];
   const int wave = threadIdx.x >> 6;
@@ -126,8 +128,9 @@ __global__ __launch_bounds__(256) void i8_rows_kernel(const T *__restrict__ x, i
   }
 }
 
-hipError_t launch_i8_rows(int act, int64_t rows, int cols, const void *x, int64_t ldx, int8_t *codes,
-                          float *scale, hipStream_t st) {
+// d_rows (or NULL): a device count that ends the rows earlier
+static hipError_t launch_rows(int act, int64_t rows, const int32_t *d_rows, int cols, const void *x,
+                              int64_t ldx, int8_t *codes, float *scale, hipStream_t st) {
   const int es = act == TRIROUTE_BF16 ? 2 : 4, pitch = i8_pitch(cols);
   const bool vec = cols % 8 == 0 && ((uintptr_t(x) | uintptr_t(ldx * es)) & 15) == 0;
   auto run = [&](auto tag, auto v, auto w) {
@@ -135,7 +138,7 @@ hipError_t launch_i8_rows(int act, int64_t rows, int cols, const void *x, int64_
     constexpr int W = decltype(w)::value;
     const int64_t blocks = std::min<int64_t>((rows * W + 3) / 4, 1 << 20);
     i8_rows_kernel<T, decltype(v)::value, W, 4><<<dim3(unsigned(blocks)), 256, 0, st>>>(
-        (const T *)x, ldx, rows, cols, pitch, codes, scale);
+        (const T *)x, ldx, rows, d_rows, cols, pitch, codes, scale);
   };
   auto by_width = [&](auto tag, auto v) {
     if (cols > 2048) run(tag, v, std::integral_constant<int, 4>{});
@@ -148,6 +151,11 @@ hipError_t launch_i8_rows(int act, int64_t rows, int cols, const void *x, int64_
   if (act == TRIROUTE_BF16) by_vec(bf16{});
   else by_vec(float{});
   return hipGetLastError();
+}
+
+hipError_t launch_i8_rows(int act, int64_t rows, int cols, const void *x, int64_t ldx, int8_t *codes,
+                          float *scale, hipStream_t st) {
+  return launch_rows(act, rows, nullptr, cols, x, ldx, codes, scale, st);
 }
 
 // Second RMSNorm of the experts' rows, quantised: n2 in fp64, rounded once to fp32 (the
@@ -270,45 +278,10 @@ hipError_t launch_i8_norm(const triroute_cfg &cfg, int N, const void *x, const v
   return hipGetLastError();
 }
 
-// Hidden rows (fp32) of the expert lists to codes.  part: the gate/up tiles' largest
-// magnitudes of each row (nparts of them, as bits).
-template <int W>
-__global__ __launch_bounds__(256) void i8_hidden_kernel(const float *__restrict__ h,
-                                                        const uint32_t *__restrict__ part, int nparts,
-                                                        const int32_t *__restrict__ off, int E,
-                                                        int dff, int pitch,
-                                                        int8_t *__restrict__ codes,
-                                                        float *__restrict__ scale) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int at = (W == 4 ? threadIdx.x : lane) * 8;
-  const int total = off[E];
-  for (int64_t row = int64_t(blockIdx.x) * (4 / W) + (W == 4 ? 0 : wave); row < total;
-       row += int64_t(gridDim.x) * (4 / W)) {
-    uint32_t m = 0;
-    for (int j = lane; j < nparts; j += 64) m = max(m, part[row * nparts + j]);
-    const RowCode rc(wave_umax(m));
-    const float *hr = h + row * dff;
-    int8_t *cr = codes + row * pitch;
-    for (int c = at; c < pitch; c += 512 * W) {
-      float v[8];
-      row8<float, true>(hr, c, dff, v);
-      *(uint2 *)(cr + c) = rc.code8(v);
-    }
-    if (at == 0) scale[row] = rc.scale;
-  }
-}
-
-hipError_t launch_i8_hidden(const triroute_cfg &cfg, int Nk, const float *h, const uint32_t *part,
-                            int nparts, const int32_t *off, int8_t *codes, float *scale,
-                            hipStream_t st) {
-  const int E = cfg.n_experts, dff = cfg.d_ff, pitch = i8_pitch(dff);
-  if (Nk <= 2048)  // few rows: four waves on each
-    i8_hidden_kernel<4><<<dim3(unsigned(Nk)), 256, 0, st>>>(h, part, nparts, off, E, dff, pitch,
-                                                            codes, scale);
-  else
-    i8_hidden_kernel<1><<<dim3(unsigned(std::min((Nk + 3) / 4, 1 << 20))), 256, 0, st>>>(
-        h, part, nparts, off, E, dff, pitch, codes, scale);
-  return hipGetLastError();
+// Hidden rows (fp32) of the expert lists to codes; the lists' end is read on the device.
+hipError_t launch_i8_hidden(const triroute_cfg &cfg, int Nk, const float *h, const int32_t *off,
+                            int8_t *codes, float *scale, hipStream_t st) {
+  return launch_rows(TRIROUTE_F32, Nk, off + cfg.n_experts, cfg.d_ff, h, cfg.d_ff, codes, scale, st);
 }
 
 }  // namespace tr
