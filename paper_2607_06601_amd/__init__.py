@@ -457,11 +457,9 @@ class I8Matrix:
                 or not scale.is_contiguous() or scale.device != codes.device:
             raise ValueError("scale: one fp32 value a row, on the codes' device")
         self.codes, self.scale, self.cols = codes, scale, cols
+        self.rows = codes.shape[0]
         self.w = I8W(codes.data_ptr(), scale.data_ptr())
-
-    @property
-    def rows(self):
-        return self.codes.shape[0]
+        self.ref = C.byref(self.w)
 
     @classmethod
     def quantize(cls, x, stream=None):
@@ -477,25 +475,31 @@ class I8Matrix:
         return self.codes[:, :self.cols].float() * self.scale[:, None]
 
 
-def _i8_rows(name, t):
-    """dtype, row stride of a [rows, cols] tensor whose rows are contiguous."""
-    if t.dim() != 2 or t.dtype not in (torch.float32, torch.bfloat16) \
-            or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name}: fp32 or bf16 rows of contiguous elements wanted")
+_ACTS = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _i8_rows(name, t, dtype, shape):
+    """Row stride of a tensor of this type and shape whose rows are contiguous."""
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name}: {list(shape)} of {dtype} wanted")
+    ld, step = t.stride()
+    if step != 1 and shape[1] > 1:
+        raise ValueError(f"{name}: rows of contiguous elements wanted")
     # (of a single row the stride does not matter)
-    return BF16 if t.dtype == torch.bfloat16 else F32, \
-        t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return ld if shape[0] > 1 or ld > shape[1] else shape[1]
 
 
 def i8_quantize(x, codes, scale, stream=None):
     """Codes int8 [rows, i8_pitch(cols)] and scales fp32 [rows] of the rows of x."""
-    act, ldx = _i8_rows("x", x)
+    if x.dim() != 2 or x.dtype not in _ACTS:
+        raise ValueError("x: fp32 or bf16 rows wanted")
+    ldx = _i8_rows("x", x, x.dtype, x.shape)
     if codes.dtype != torch.int8 or codes.shape != (x.shape[0], i8_pitch(x.shape[1])) \
             or not codes.is_contiguous():
         raise ValueError("codes: contiguous int8 [rows, i8_pitch(cols)]")
     if scale.dtype != torch.float32 or scale.shape != (x.shape[0],) or not scale.is_contiguous():
         raise ValueError("scale: fp32 [rows]")
-    _check(lib().triroute_i8_quantize(act, x.shape[0], x.shape[1], _p(x), ldx, _p(codes),
+    _check(lib().triroute_i8_quantize(_ACTS[x.dtype], x.shape[0], x.shape[1], _p(x), ldx, _p(codes),
                                       _p(scale), _stream(stream)))
 
 
@@ -509,17 +513,15 @@ def linear_i8_workspace(n_tok: int, cols: int, device="cuda"):
 def linear_i8(x, w: I8Matrix, y, ws, residual=None, stream=None):
     """y = x w^T (+ residual) in 8-bit integers (triroute_linear_i8); x, y and residual are
     [tokens, channels] of one type, of any row stride."""
-    act, ldx = _i8_rows("x", x)
-    tens = [("y", y)] + ([] if residual is None else [("residual", residual)])
-    for name, t in tens:
-        if _i8_rows(name, t)[0] != act or t.shape != (x.shape[0], w.rows):
-            raise ValueError(f"{name}: [{x.shape[0]}, {w.rows}] of x's type wanted")
-    if x.shape[1] != w.cols:
-        raise ValueError(f"x has {x.shape[1]} channels, the weight {w.cols}")
+    dtype, n, k, m = x.dtype, x.shape[0], w.cols, w.rows
+    act = _ACTS.get(dtype)
+    if act is None:
+        raise ValueError(f"x: fp32 or bf16 wanted, not {dtype}")
     _check(lib().triroute_linear_i8(
-        act, x.shape[0], x.shape[1], w.rows, _p(x), ldx, C.byref(w.w), _p(residual),
-        0 if residual is None else _i8_rows("residual", residual)[1], _p(y), _i8_rows("y", y)[1],
-        _p(ws), ws.numel(), _stream(stream)))
+        act, n, k, m, x.data_ptr(), _i8_rows("x", x, dtype, (n, k)), w.ref,
+        None if residual is None else residual.data_ptr(),
+        0 if residual is None else _i8_rows("residual", residual, dtype, (n, m)), y.data_ptr(),
+        _i8_rows("y", y, dtype, (n, m)), ws.data_ptr(), ws.numel(), _stream(stream)))
 
 
 def qkv_i8(cfg, B, T, n1, dw: DenseI8W, q, k, v, ws, pos0=None, stream=None):

@@ -21,6 +21,12 @@ __device__ __forceinline__ float dequant(int32_t v, float row, float col) {
   return float(v) * row * col;
 }
 
+// 1 and 8 values, rounded to the activation dtype (a NaN stays one).
+__device__ __forceinline__ void put1(float *p, float v) { *p = v; }
+__device__ __forceinline__ void put1(bf16 *p, float v) { *p = bf16(pk_bf16(v, v)); }
+__device__ __forceinline__ void put8(float *p, const float *v) { store8(p, v); }
+__device__ __forceinline__ void put8(bf16 *p, const float *v) { *(u32x4_t *)p = pack8_bf16(v); }
+
 // Sums of a wave's tile to the staged fp32 tile C, as store_acc does for bf16; lane
 // column and row mapping as there.
 template <class P, int MI, int NI, int TM, int TN, int LDC>
@@ -54,6 +60,30 @@ __device__ __forceinline__ void stage_i8(const P &p, const MTile &t, float *C,
     }
 }
 
+__device__ __forceinline__ float elem(const float4 &v, int i) {
+  return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
+}
+
+// v += 8 elements as they lie in memory.
+struct Raw8f {
+  float4 a, b;
+};
+__device__ __forceinline__ void add8(const uint4 &x, float *v) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] += __uint_as_float(w[i] << 16);
+    v[2 * i + 1] += __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void add8(const Raw8f &x, float *v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[i] += elem(x.a, i);
+    v[4 + i] += elem(x.b, i);
+  }
+}
+
 // Four-wave kernel: the wave's scales in LDS, its TM rows', then its TN columns'; the
 // four rows of a lane in row block mi, and its columns' where it holds NI of them side by side.
 template <int MI>
@@ -69,10 +99,6 @@ __device__ __forceinline__ void w4_cols(const float *sc, int lane, float (&c)[NI
     c[4 * q] = v.x; c[4 * q + 1] = v.y; c[4 * q + 2] = v.z; c[4 * q + 3] = v.w;
   }
 }
-__device__ __forceinline__ float elem(const float4 &v, int i) {
-  return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
-}
-
 // ---------------------------------------------------------------- problems
 template <typename T, bool VEC>  // VEC: whole 16-byte pieces of y and residual
 struct LinearI8 {
@@ -106,7 +132,9 @@ struct LinearI8 {
   // consecutive columns of each of its rows.
   static constexpr bool DIRECT_W4 = true;
   __device__ const int8_t *a_base() const { return a; }
-  __device__ const int8_t *b_base() const { return w; }
+  __device__ static int b_pick(int) { return 0; }
+  template <int TN, int K>
+  __device__ const int8_t *b_base_w4(int, int) const { return w; }
   __device__ uint32_t a_off(const MTile &t, int r) const { return uint32_t(t.m0 + r) * uint32_t(pitch); }
   template <int NI>
   __device__ uint32_t b_off_w4(const MTile &t, int wn, int ni, int c) const {
@@ -127,29 +155,40 @@ struct LinearI8 {
     if (f >= m) return;
     float sc[NI];
     w4_cols<MI>(scales, lane, sc);
-#pragma unroll
-    for (int mi = 0; mi < MI; ++mi) {
-      float x[4][8];
-      const int r0 = wm * MI * 16 + mi * 16 + 4 * (lane >> 4);
-      const float4 sr = w4_rows<MI>(scales, mi, lane);
-      if (res) {  // a block's residual rows first, so that their loads overlap
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          load8(res + (t.m0 + (r0 + i < t.mvalid ? r0 + i : 0)) * ldr + f, x[i]);
-      }
+    // Residual rows of AHEAD row blocks in flight, as they lie in memory (64 registers; the
+    // operands' fragments are dead here): a row block that waits for its own loads spends the
+    // memory's latency eight times a tile.
+    constexpr int AHEAD = std::min(MI, sizeof(T) == 2 ? 4 : 2);
+    typedef std::conditional_t<sizeof(T) == 2, uint4, Raw8f> raw;
+    raw x[AHEAD][4];
+    const bool has = res != nullptr;
+    auto row0 = [&](int mi) { return wm * MI * 16 + mi * 16 + 4 * (lane >> 4); };
+    auto fetch = [&](int mi) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (r0 + i >= t.mvalid) continue;
-        const int64_t row = t.m0 + r0 + i;
+        const int r = row0(mi) + i;
+        x[mi % AHEAD][i] = *(const raw *)(res + (t.m0 + (r < t.mvalid ? r : 0)) * ldr + f);
+      }
+    };
+    if (has) {
+#pragma unroll
+      for (int mi = 0; mi < AHEAD; ++mi) fetch(mi);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+      const int r0 = row0(mi);
+      const float4 sr = w4_rows<MI>(scales, mi, lane);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
         float v[8];
 #pragma unroll
         for (int ni = 0; ni < NI; ++ni) v[ni] = dequant(acc[mi][ni][i], elem(sr, i), sc[ni]);
-        if (res) {
-#pragma unroll
-          for (int ni = 0; ni < NI; ++ni) v[ni] += x[i][ni];
-        }
-        store8(y + row * ldy + f, v);
+        if (has) add8(x[mi % AHEAD][i], v);
+        if (r0 + i < t.mvalid) put8(y + (t.m0 + r0 + i) * ldy + f, v);
       }
+      if (has && mi + AHEAD < MI) fetch(mi + AHEAD);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   template <int MI, int NI, int TM, int TN, int LDC>
@@ -176,10 +215,10 @@ struct LinearI8 {
 #pragma unroll
           for (int u = 0; u < 8; ++u) v[u] += x[u];
         }
-        store8(y + row * ldy + c, v);
+        put8(y + row * ldy + c, v);
       } else {
         for (int u = 0; u < 8 && c + u < m; ++u)
-          Act<T>::st(y, row * ldy + c + u, res ? Act<T>::ld(res, row * ldr + c + u) + cr[u] : cr[u]);
+          put1(y + row * ldy + c + u, res ? Act<T>::ld(res, row * ldr + c + u) + cr[u] : cr[u]);
       }
     }
   }
@@ -233,10 +272,16 @@ struct QkvI8 {
   // d_h 128 or two of 64; lane column c has pairs j .. j + 3 of one head, blocks 2 u and
   // 2 u + 1 the first and second half of pair j + u.
   static constexpr bool DIRECT_W4 = true;
-  const int8_t *Wlo;         // the lowest of Wq, Wk, Wv
-  uint32_t wq_o, wk_o, wv_o; // byte offsets of Wq, Wk, Wv from Wlo less their first column's rows
   __device__ const int8_t *a_base() const { return a; }
-  __device__ const int8_t *b_base() const { return Wlo; }
+  // a transfer's 8 B rows are columns of one head, so of one matrix; of the two heads of d_h 64
+  // every other transfer has one
+  __device__ static int b_pick(int j) { return j & 1; }
+  template <int TN, int K>
+  __device__ const int8_t *b_base_w4(int n0, int wn) const {
+    static_assert(TN == 128, "a wave's B rows are one wave column's");
+    const int gc = n0 + TN * wn + (dh == 64 ? 64 * K : 0);
+    return gc < Hd ? Wq : gc < Hd + Kd ? Wk : Wv;
+  }
   __device__ uint32_t a_off(const MTile &t, int r) const { return uint32_t(t.m0 + r) * uint32_t(pitch); }
   // first column of the lane's head, and its first pair
   __device__ void w4_head(const MTile &t, int wn, int c, int &hcol, int &j) const {
@@ -252,10 +297,8 @@ struct QkvI8 {
   template <int NI>
   __device__ uint32_t b_off_w4(const MTile &t, int wn, int ni, int c) const {
     const int gc = w4_col<NI>(t, wn, ni, c);
-    // (arithmetic on the field values: a select of fields by a lane-varying
-    // condition becomes a per-lane load from the kernel arguments)
-    const uint32_t base = wq_o + uint32_t(gc >= Hd) * (wk_o - wq_o) + uint32_t(gc >= Hd + Kd) * (wv_o - wk_o);
-    return gc < Ncols ? base + uint32_t(gc) * uint32_t(pitch) : 0u;
+    const int first = gc < Hd ? 0 : gc < Hd + Kd ? Hd : Hd + Kd;
+    return gc < Ncols ? uint32_t(gc - first) * uint32_t(pitch) : 0u;
   }
   __device__ const float *row_scale_at(const MTile &t, int r) const { return sa + t.m0 + r; }
   template <int TN>
@@ -361,8 +404,8 @@ struct QkvI8 {
         }
       }
       T *o = out + int64_t(row) * ld + col;
-      store8(o, y1);
-      store8(o + hd, y2);
+      put8(o, y1);
+      put8(o + hd, y2);
     }
   }
 };
@@ -416,16 +459,16 @@ struct Moe1I8 {
   // even ni and up for odd, so each lane ends with both halves of NI / 2
   // consecutive units.  A wave's NI * 8 units are one part of a row's maximum.
   static constexpr bool DIRECT_W4 = true;
-  const int8_t *Wlo;  // the lower of Wg, Wu
   __device__ const int8_t *a_base() const { return a; }
-  __device__ const int8_t *b_base() const { return Wlo; }
+  // a transfer has 8 rows of one block ni: two transfers of gate rows, two of up rows, ...
+  __device__ static int b_pick(int j) { return (j >> 1) & 1; }
+  template <int TN, int K>
+  __device__ const int8_t *b_base_w4(int, int) const { return K ? Wu : Wg; }
   __device__ uint32_t a_off(const MTile &t, int r) const { return uint32_t(t.p0 + r) * uint32_t(pitch); }
   template <int NI>
   __device__ uint32_t b_off_w4(const MTile &t, int wn, int ni, int c) const {
     const int f = t.n0 + (NI / 2) * (16 * wn + c) + (ni >> 1);
-    if (f >= dff) return 0u;
-    const uint32_t off = uint32_t(((ni & 1) ? Wu : Wg) - Wlo);
-    return off + uint32_t((t.e - 1) * dff + f) * uint32_t(pitch);
+    return f < dff ? uint32_t((t.e - 1) * dff + f) * uint32_t(pitch) : 0u;
   }
   __device__ const float *row_scale_at(const MTile &t, int r) const { return sa + t.p0 + r; }
   // the wave's TN / 2 gate scales, then its up scales
@@ -502,7 +545,9 @@ struct Moe2I8 {
   // Four-wave kernel: columns as in LinearI8.
   static constexpr bool DIRECT_W4 = true;
   __device__ const int8_t *a_base() const { return a; }
-  __device__ const int8_t *b_base() const { return Wd; }
+  __device__ static int b_pick(int) { return 0; }
+  template <int TN, int K>
+  __device__ const int8_t *b_base_w4(int, int) const { return Wd; }
   __device__ uint32_t a_off(const MTile &t, int r) const { return uint32_t(t.p0 + r) * uint32_t(pitch); }
   template <int NI>
   __device__ uint32_t b_off_w4(const MTile &t, int wn, int ni, int c) const {
@@ -529,11 +574,10 @@ struct Moe2I8 {
       const float4 sr = w4_rows<MI>(scales, mi, lane);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (r0 + i >= t.mvalid) continue;
         float v[8];
 #pragma unroll
         for (int ni = 0; ni < NI; ++ni) v[ni] = dequant(acc[mi][ni][i], elem(sr, i), sc[ni]);
-        store8(out + uint32_t((r0 + i) * d + f), v);
+        if (r0 + i < t.mvalid) store8(out + uint32_t((r0 + i) * d + f), v);
       }
     }
   }
@@ -649,8 +693,7 @@ hipError_t i8_qkv(const triroute_cfg &cfg, int N, const int8_t *a, const float *
       bool w4 = false;
       if constexpr (std::is_same<T, bf16>::value)
         w4 = K2 >= 128 && span32({{p.a, size_t(p.N) * p.pitch}}, &lo) &&
-             span32({{p.Wq, size_t(p.Hd) * p.pitch}, {p.Wk, size_t(p.Kd) * p.pitch},
-                     {p.Wv, size_t(p.Kd) * p.pitch}}, &p.Wlo) &&
+             span32({{p.Wq, size_t(p.Hd) * p.pitch}}, &lo) &&
              w4_rounds(p.N, c128, tile_cost(m256 * c256, COST_256X256));
       if (few_tiles(p.N, c128)) {
         if (p.dh == 64)
@@ -660,9 +703,6 @@ hipError_t i8_qkv(const triroute_cfg &cfg, int N, const int8_t *a, const float *
       } else if (!w4) {
         e = launch_mid(p, K2, p.N, c128, st);
       } else if constexpr (std::is_same<T, bf16>::value) {
-        p.wq_o = uint32_t(p.Wq - p.Wlo);
-        p.wk_o = uint32_t(p.Wk - p.Wlo) - uint32_t(p.Hd) * uint32_t(p.pitch);
-        p.wv_o = uint32_t(p.Wv - p.Wlo) - uint32_t(p.Hd + p.Kd) * uint32_t(p.pitch);
         e = launch_w4<QkvI8<T>, 256, 256>(p, K2, m256, c256, st);
       }
       if (e != hipSuccess) return e;
@@ -698,7 +738,7 @@ hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
     const int8_t *lo;
     bool w4 = false;
     if constexpr (!decltype(f64)::value)
-      w4 = r > 64 && K2 >= 128 && span32({{p.Wg, wb}, {p.Wu, wb}}, &p.Wlo) &&
+      w4 = r > 64 && K2 >= 128 && span32({{p.Wg, wb}}, &lo) &&
            span32({{p.a, size_t(Nk) * p.pitch}}, &lo) &&
            !one_round(row_tiles(128) * ((dff + 63) / 64));
     const int ny = (dff + 127) / 128;

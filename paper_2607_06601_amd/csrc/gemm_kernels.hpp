@@ -342,7 +342,7 @@ __global__ __launch_bounds__(256, 1) void gemm_w4_kernel(P p, int K, int ny) {
     t.p0 = __builtin_amdgcn_readfirstlane(t.p0);
     return t;
   };
-  MTile tc = tile(L);
+  MTile tc = tile(L), tn = tc;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // wave-uniform, in SGPRs
   const int wm = wave / WN, wn = wave % WN;
@@ -355,7 +355,28 @@ __global__ __launch_bounds__(256, 1) void gemm_w4_kernel(P p, int K, int ny) {
   // in accumulators that are never stored.
   static_assert(BM % RPT == 0, "a transfer stays within one operand");
   auto is_a = [&](int j) { return RPT * (wave * IPW + j) < BM; };  // wave-uniform
-  auto gbase = [&](int j) { return (const uint8_t *)(is_a(j) ? p.a_base() : p.b_base()); };
+  // 8-bit problems: matrices may lie far apart, and a transfer's B rows lie in one of two
+  // (P::b_pick of the transfer), whose bases follow the tile: now, and the step to the next tile's.
+  uint64_t bnow[2] = {0, 0}, bstep[2] = {0, 0};
+  auto base_of = [&](const MTile &t, auto k) -> uint64_t {
+    if constexpr (P::Op::INT) {
+      const int n = max(RPT * wave * IPW - BM, 0);  // the wave's first B row
+      return uint64_t(p.template b_base_w4<TN, decltype(k)::value>(t.n0, n / TN));
+    }
+    return 0;
+  };
+  std::integral_constant<int, 0> K0;
+  std::integral_constant<int, 1> K1;
+  bnow[0] = base_of(tc, K0);
+  bnow[1] = base_of(tc, K1);
+  auto gbase = [&](int j, bool next) {
+    if constexpr (P::Op::INT) {
+      const uint64_t b = P::b_pick(j) ? bnow[1] + (next ? bstep[1] : 0) : bnow[0] + (next ? bstep[0] : 0);
+      return is_a(j) ? (const uint8_t *)p.a_base() : (const uint8_t *)b;
+    } else {
+      return (const uint8_t *)(is_a(j) ? p.a_base() : p.b_base());
+    }
+  };
   // (lane-derived terms of the per-tile address arithmetic start from an
   // opaque copy of the lane: hoisted out of the tile loop they would hold
   // registers through the K loop)
@@ -426,15 +447,16 @@ __global__ __launch_bounds__(256, 1) void gemm_w4_kernel(P p, int K, int ny) {
 
   const int nk = K / BK;  // >= 2 (host)
 #pragma unroll
-  for (int j = 0; j < IPW; ++j) dma16_s(gbase(j), voff[j], sbase + j * 1024);
+  for (int j = 0; j < IPW; ++j) dma16_s(gbase(j, false), voff[j], sbase + j * 1024);
 #pragma unroll
-  for (int j = 0; j < IPW; ++j) dma16_s(gbase(j) + RB, voff[j], sbase + STAGE + j * 1024);
+  for (int j = 0; j < IPW; ++j) dma16_s(gbase(j, false) + RB, voff[j], sbase + STAGE + j * 1024);
   // the next tile's offsets while stage 0 lands (needed from step nk - 2 on)
   int Ln = L + int(gridDim.x);
-  MTile tn = tc;
   if (Ln < total) {
     tn = tile(Ln);
     offsets(tn, vnx);
+    bstep[0] = base_of(tn, K0) - bnow[0];
+    bstep[1] = base_of(tn, K1) - bnow[1];
   }
   wait_vm<IPW>();
   __syncthreads();
@@ -456,7 +478,7 @@ __global__ __launch_bounds__(256, 1) void gemm_w4_kernel(P p, int K, int ny) {
       auto dma_slot = [&](int pos) {  // transfer pos / GAP at slot pos
         if (pos >= 0 && pos % GAP == 0 && pos / GAP < IPW) {
           const int j = pos / GAP;
-          dma16_s(gbase(j) + kn * RB, nxt ? vnx[j] : voff[j], sbase + buf * STAGE + j * 1024);
+          dma16_s(gbase(j, nxt) + kn * RB, nxt ? vnx[j] : voff[j], sbase + buf * STAGE + j * 1024);
         }
       };
       // slice 0: MFMAs on set 0, the reads of slice 1 into set 1 after the
@@ -507,10 +529,14 @@ __global__ __launch_bounds__(256, 1) void gemm_w4_kernel(P p, int K, int ny) {
     tc = tn;
 #pragma unroll
     for (int j = 0; j < IPW; ++j) voff[j] = vnx[j];
+    bnow[0] += bstep[0];
+    bnow[1] += bstep[1];
     Ln = L + int(gridDim.x);
     if (Ln < total) {
       tn = tile(Ln);
       offsets(tn, vnx);
+      bstep[0] = base_of(tn, K0) - bnow[0];
+    bstep[1] = base_of(tn, K1) - bnow[1];
     }
   }
 }
