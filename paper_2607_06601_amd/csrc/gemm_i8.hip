@@ -324,19 +324,27 @@ struct QkvI8 {
     }
     const float *cl = scales + MI * 16 + (hcol - t.n0 - 128 * wn) + j;
     const float4 sc1 = *(const float4 *)cl, sc2 = *(const float4 *)(cl + hd);
+    // rotation entries of two row blocks in flight (as the residual rows of LinearI8)
+    float4 cs[2][4][2];
+    auto row0 = [&](int mi) { return wm * MI * 16 + mi * 16 + 4 * (lane >> 4); };
+    auto fetch = [&](int mi) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = row0(mi) + i;
+        const float4 *tb = (const float4 *)(rope + int64_t(t.m0 + (r < t.mvalid ? r : 0)) * hd + j);
+        cs[mi & 1][i][0] = tb[0];
+        cs[mi & 1][i][1] = tb[1];
+      }
+    };
+    if (rot) {
+      fetch(0);
+      fetch(1);
+    }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
-      const int r0 = wm * MI * 16 + mi * 16 + 4 * (lane >> 4);
+      const int r0 = row0(mi);
       const float4 sr = w4_rows<MI>(scales, mi, lane);
-      float4 cs[4][2];
-      if (rot) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float4 *tb = (const float4 *)(rope + int64_t(t.m0 + (r0 + i < t.mvalid ? r0 + i : 0)) * hd + j);
-          cs[i][0] = tb[0];
-          cs[i][1] = tb[1];
-        }
-      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float y1[4], y2[4];
@@ -347,7 +355,7 @@ struct QkvI8 {
           y1[u] = a1;
           y2[u] = a2;
           if (rot) {
-            const float4 c4 = cs[i][u >> 1];  // (cos, sin) of pairs j + 2 (u / 2), + 1
+            const float4 c4 = cs[mi & 1][i][u >> 1];  // (cos, sin) of pairs j + 2 (u / 2), + 1
             const float co = (u & 1) ? c4.z : c4.x, si = (u & 1) ? c4.w : c4.y;
             y1[u] = a1 * co - a2 * si;
             y2[u] = a1 * si + a2 * co;
@@ -359,6 +367,8 @@ struct QkvI8 {
           *(uint2 *)(o + hd) = make_uint2(pk_bf16(y2[0], y2[1]), pk_bf16(y2[2], y2[3]));
         }
       }
+      if (rot && mi + 2 < MI) fetch(mi + 2);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   template <int MI, int NI, int TM, int TN, int LDC>
@@ -715,10 +725,10 @@ hipError_t i8_qkv(const triroute_cfg &cfg, int N, const int8_t *a, const float *
 hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
                   const triroute_compaction &c, const MoeI8Ws &ws, hipStream_t st) {
   const int E = cfg.n_experts, Nk = N * cfg.top_k, d = cfg.d_model, dff = cfg.d_ff;
-  // rows of an expert when the router spreads its options evenly, and the tiles of BM rows that
-  // E such experts make (a few rows more, as the counts vary)
+  // Rows of an expert when the router spreads its options evenly, and the tiles of BM rows that
+  // the experts in use make then (a few rows more, as the counts vary).
   const int r = Nk / (E + 1);
-  auto row_tiles = [&](int BM) { return E * ((r + r / 32 + BM) / BM); };
+  auto row_tiles = [&](int BM) { return std::min(E, Nk) * ((r + r / 32 + BM) / BM); };
   auto up = [&](auto f64) {
     typedef Moe1I8<decltype(f64)::value> P;
     P p;
@@ -744,7 +754,11 @@ hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
     const int ny = (dff + 127) / 128;
     hipError_t e = hipErrorInvalidValue;
     const int c64 = (dff + 63) / 64;
-    if (r <= 24) {
+    // Gate/up: as the bf16 product's rule (times of the two kernels measured alike), but 32-row tiles
+    // with two K groups where they leave CUs without a tile (160M, 1 token: 5.6 -> 5.1 us).
+    if (r <= 24 && split_k(row_tiles(32) * ((dff + 31) / 32), K2)) {
+      e = launch<P, 32, 64, 2, 1, 64, 4, 2>(p, K2, Nk / 32 + E, (dff + 31) / 32, st);
+    } else if (r <= 24) {
       e = launch<P, 32, 64, 2, 1, 64, 4>(p, K2, Nk / 32 + E, (dff + 31) / 32, st);
     } else if (r <= 64) {
       e = launch<P, 64, 128, 2, 2, 64, 3>(p, K2, Nk / 64 + E, c64, st);
@@ -773,10 +787,17 @@ hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
   p.pitch = i8_pitch(dff);
   const int K2 = p.pitch / 2, c64 = (d + 63) / 64, c128 = (d + 127) / 128, c256 = (d + 255) / 256;
   const int8_t *lo;
-  if (r <= 64 && row_tiles(64) * c128 < 256)
-    return launch<Moe2I8, 32, 64, 2, 1, 64, 4>(p, K2, Nk / 32 + E, c64, st);
-  if (r <= 64) return launch<Moe2I8, 64, 128, 2, 2, 64, 2>(p, K2, Nk / 64 + E, c128, st);
-  if (K2 < 128 || one_round(row_tiles(128) * c128) || !span32({{p.Wd, size_t(E) * d * p.pitch}}, &lo) ||
+  // Down.  Few columns and a long K: 32-row tiles up to two a CU, with two K groups up to one
+  // (160M, 1 token 8.0 -> 6.3 us, 410M, 64 tokens 10.2 -> 8.0; 410M, 333 tokens, 384 tiles: 12.4, 64-row
+  // tiles 14.5; 1.3B, 32 tokens, 512: 34, 64-row tiles of two stages 44), then 64-row tiles (410M, 1000
+  // tokens, 256 tiles: 17.1, 32-row 25.1, 128-row 19.4), from about 400 on the four-wave
+  // kernel (1.3B, 1000 tokens, 512 tiles: 60, 64-row 72; 2500 tokens 97 and, of 256 rows, 90, 128-row
+  // tiles 109).
+  const int t32 = row_tiles(32) * c64;
+  if (split_k(t32, K2)) return launch<Moe2I8, 32, 64, 2, 1, 64, 4, 2>(p, K2, Nk / 32 + E, c64, st);
+  if (t32 <= 2 * cu_count()) return launch<Moe2I8, 32, 64, 2, 1, 64, 4>(p, K2, Nk / 32 + E, c64, st);
+  if (row_tiles(64) * c128 <= 400) return launch<Moe2I8, 64, 128, 2, 2, 64, 3>(p, K2, Nk / 64 + E, c128, st);
+  if (K2 < 128 || !span32({{p.Wd, size_t(E) * d * p.pitch}}, &lo) ||
       !span32({{p.a, size_t(Nk) * p.pitch}}, &lo))
     return launch<Moe2I8, 128, 128, 4, 2, 64, 3>(p, K2, Nk / 128 + E, c128, st);
   if (row_tiles(256) > E && tile_cost(row_tiles(128) * c256, 1.f) < tile_cost(row_tiles(256) * c256, 1.77f))

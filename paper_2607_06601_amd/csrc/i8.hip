@@ -17,43 +17,71 @@ __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v
 
 // Largest magnitude of a row, as the bits of |x|: as whole numbers NaN > inf > finite.
 __device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) v = max(v, uint32_t(__shfl_xor(int(v), m, WAVE)));
-  return v;
+#define TR_ROR(n) uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x120 + (n), 0xF, 0xF, false))
+  v = max(v, TR_ROR(1));
+  v = max(v, TR_ROR(2));
+  v = max(v, TR_ROR(4));
+  v = max(v, TR_ROR(8));
+#undef TR_ROR
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(uint32_t(a[0]), uint32_t(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max(uint32_t(b[0]), uint32_t(b[1]));
 }
 
+// Scale of a row and the codes of its elements.  A code is the quotient in fp32, rounded; with
+// one of 8 next to a border (4e-5; the quotient is off by at most 127 * 2^-23), the 8 are
+// compared with their borders instead.  The quotients of a row of tiny values are of values 2^64 times
+// larger (exact), so that 127 / a stays finite.
 struct RowCode {
-  float a, inv, lift;
+  float a, inv;
   float scale;
-  bool bad;
+  bool bad, tiny;
   __device__ __forceinline__ explicit RowCode(uint32_t amax) {
     a = __uint_as_float(amax);
     bad = amax >= INF_BITS;
+    tiny = a < 1e-30f;
     scale = bad ? __uint_as_float(0x7FC00000u) : a / 127.0f;
-    // 127 / a stays finite: rows of tiny values are coded 2^64 times larger (exact)
-    lift = a < 1e-30f ? 18446744073709551616.0f : 1.0f;
-    a *= lift;
+    if (tiny) a *= LIFT;
     inv = a > 0.0f && !bad ? 127.0f / a : 0.0f;
   }
-  __device__ __forceinline__ int code(float x) const {
-    const float v = x * lift, t = v * inv;
-    float r = rintf(t);
-    // (t is off by at most 127 * 2^-22)
-    if (fabsf(fabsf(t - r) - 0.5f) < 1e-4f) {
-      const int k = int(fabsf(t));
-      const double over = 254.0 * fabs(double(v)) - double(2 * k + 1) * double(a);
-      const int c = over > 0.0 ? k + 1 : over < 0.0 ? k : k + (k & 1);
-      r = copysignf(float(c), v);
-    }
-    return bad ? 0 : int(r);
+  static constexpr float LIFT = 18446744073709551616.0f;
+  // the code of v >= 0 whose quotient is about t
+  __device__ __forceinline__ int exact(float v, float t) const {
+    const int k = int(t);
+    if (fabsf(t - (float(k) + 0.5f)) > 1e-3f) return int(rintf(t));
+    const double over = 254.0 * double(v) - double(2 * k + 1) * double(a);
+    return over > 0.0 ? k + 1 : over < 0.0 ? k : k + (k & 1);
   }
-  __device__ __forceinline__ uint2 code8(const float *v) const {
-    uint32_t w[2];
+  __device__ __forceinline__ uint2 code8(const float *x) const {
+    float v[8], r[8], far = 0.0f;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      w[h] = (uint32_t(code(v[4 * h])) & 255u) | (uint32_t(code(v[4 * h + 1])) & 255u) << 8 |
-             (uint32_t(code(v[4 * h + 2])) & 255u) << 16 | uint32_t(code(v[4 * h + 3])) << 24;
-    return make_uint2(w[0], w[1]);
+    for (int i = 0; i < 8; ++i) v[i] = x[i];
+    if (tiny) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] *= LIFT;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float t = v[i] * inv;
+      r[i] = rintf(t);
+      far = fmaxf(far, fabsf(t - r[i]));
+    }
+    if (far > 0.49996f) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r[i] = copysignf(float(exact(fabsf(v[i]), fabsf(v[i]) * inv)), v[i]);
+    }
+    // (the byte of a whole number up to 127 is the lowest of it plus 1.5 * 2^23)
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(r[i] + 12582912.0f);
+    // bytes 0 of two words, then of two pairs
+    uint2 o;
+    o.x = __builtin_amdgcn_perm(__builtin_amdgcn_perm(w[3], w[2], 0x0C0C0400u),
+                                __builtin_amdgcn_perm(w[1], w[0], 0x0C0C0400u), 0x05040100u);
+    o.y = __builtin_amdgcn_perm(__builtin_amdgcn_perm(w[7], w[6], 0x0C0C0400u),
+                                __builtin_amdgcn_perm(w[5], w[4], 0x0C0C0400u), 0x05040100u);
+    return bad ? make_uint2(0u, 0u) : o;
   }
 };
 
@@ -88,8 +116,11 @@ __global__ __launch_bounds__(256) void i8_rows_kernel(const T *__restrict__ x, i
   const int wave = threadIdx.x >> 6;
   const int at = (W == 4 ? threadIdx.x : threadIdx.x & 63) * 8;
   for (int64_t row0 = int64_t(blockIdx.x) * (4 / W); row0 < rows; row0 += int64_t(gridDim.x) * (4 / W)) {
-    const int64_t row = row0 + (W == 4 ? 0 : wave);
+    int64_t row = row0 + (W == 4 ? 0 : wave);
     if (W != 4 && row >= rows) break;
+    // rows of a product just made, its last ones first: they are still in the cache behind the
+    // L2s, and the product that follows begins with the codes written last
+    if (d_rows) row = rows - 1 - row;
     const T *xr = x + row * ldx;
     float v[RR][8];
     uint32_t m = 0;
@@ -161,16 +192,21 @@ hipError_t launch_i8_rows(int act, int64_t rows, int cols, const void *x, int64_
 // Second RMSNorm of the experts' rows, quantised: n2 in fp64, rounded once to fp32 (the
 // values that the codes are of), for the list rows of each token's real assignments.
 // ENTRY: one wave per entry of the expert lists (token rows[pos] / k to row pos, and slot_of),
-// else one wave per token, to the rows slot_of names.  Rows of up to 512 RR elements stay
-// in registers; longer ones are read and normalised again for the codes.
-template <typename T, bool ENTRY, int RR>
+// else one wave per token, to the rows slot_of names.  W waves a row; rows of up to 512 W RR
+// elements stay in registers, longer ones are read and normalised again for the codes.  (Few rows: four
+// waves on each, 1.3B, 32 tokens, 8.4 -> 4.8 us.)
+template <typename T, bool ENTRY, int W, int RR>
 __global__ __launch_bounds__(256) void i8_norm_kernel(
     const T *__restrict__ x, const T *__restrict__ g, const int32_t *__restrict__ rows,
     const int32_t *__restrict__ off, const int32_t *__restrict__ eidx, int32_t *__restrict__ slot_of,
     int E, int k, int n, int d, int pitch, float eps, int8_t *__restrict__ codes,
     float *__restrict__ scale) {
-  const int i = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
-  const int lane = threadIdx.x & 63;
+  constexpr int STEP = 512 * W;
+  __shared__ double part[W];
+  __shared__ uint32_t mpart[W];
+  const int wave = threadIdx.x >> 6;
+  const int i = W == 4 ? int(blockIdx.x) : __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + wave);
+  const int at = (W == 4 ? threadIdx.x : threadIdx.x & 63) * 8;
   if (i >= n || (ENTRY && i >= off[E])) return;  // off[E]: end of the last list
   const int a = ENTRY ? rows[i] : 0;
   const T *xr = x + int64_t(ENTRY ? a / k : i) * d;
@@ -183,16 +219,21 @@ __global__ __launch_bounds__(256) void i8_norm_kernel(
   };
   if constexpr (KEEP) {
 #pragma unroll
-    for (int q = 0; q < RR; ++q) row8<T, true>(xr, lane * 8 + 512 * q, d, v[q]);
+    for (int q = 0; q < RR; ++q) row8<T, true>(xr, at + STEP * q, d, v[q]);
 #pragma unroll
     for (int q = 0; q < RR; ++q) square(v[q]);
   } else {
-    for (int c = lane * 8; c < d; c += 512) {
+    for (int c = at; c < d; c += STEP) {
       load8(xr + c, v[0]);
       square(v[0]);
     }
   }
   ss = wave_sum(ss);
+  if constexpr (W == 4) {
+    if ((threadIdx.x & 63) == 0) part[wave] = ss;
+    __syncthreads();
+    ss = (part[0] + part[1]) + (part[2] + part[3]);
+  }
   const double r = 1.0 / sqrt(ss / double(d) + double(eps));
   uint32_t m = 0;
   auto norm8 = [&](int c, float *w) {
@@ -201,20 +242,29 @@ __global__ __launch_bounds__(256) void i8_norm_kernel(
     load8(g + c, gv);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      w[j] = float((double(w[j]) * r) * double(gv[j]));
+      if constexpr (sizeof(T) == 2)  // (the product of two bf16 numbers is an fp32 number)
+        w[j] = float(double(w[j] * gv[j]) * r);
+      else
+        w[j] = float((double(w[j]) * r) * double(gv[j]));
       m = max(m, abs_bits(w[j]));
     }
   };
   if constexpr (KEEP) {
 #pragma unroll
-    for (int q = 0; q < RR; ++q) norm8(lane * 8 + 512 * q, v[q]);
+    for (int q = 0; q < RR; ++q) norm8(at + STEP * q, v[q]);
   } else {
-    for (int c = lane * 8; c < d; c += 512) {
+    for (int c = at; c < d; c += STEP) {
       load8(xr + c, v[0]);
       norm8(c, v[0]);
     }
   }
-  const RowCode rc(wave_umax(m));
+  m = wave_umax(m);
+  if constexpr (W == 4) {
+    if ((threadIdx.x & 63) == 0) mpart[wave] = m;
+    __syncthreads();
+    m = max(max(mpart[0], mpart[1]), max(mpart[2], mpart[3]));
+  }
+  const RowCode rc(m);
   const int32_t *ei = eidx + int64_t(i) * k, *so = slot_of + int64_t(i) * k;
   auto emit = [&](int c, const uint2 &w) {
     if constexpr (ENTRY) {
@@ -227,22 +277,22 @@ __global__ __launch_bounds__(256) void i8_norm_kernel(
   if constexpr (KEEP) {
 #pragma unroll
     for (int q = 0; q < RR; ++q) {
-      const int c = lane * 8 + 512 * q;
+      const int c = at + STEP * q;
       if (c < pitch) emit(c, rc.code8(v[q]));
     }
   } else {
-    for (int c = lane * 8; c < pitch; c += 512) {
+    for (int c = at; c < pitch; c += STEP) {
       row8<T, true>(xr, c, d, v[0]);
       norm8(c, v[0]);
       emit(c, rc.code8(v[0]));
     }
   }
   if constexpr (ENTRY) {
-    if (lane == 0) {
+    if (at == 0) {
       slot_of[a] = i;
       scale[i] = rc.scale;
     }
-  } else if (lane == 0) {
+  } else if (at == 0) {
     for (int s = 0; s < k; ++s)
       if (ei[s] != 0) scale[so[s]] = rc.scale;
   }
@@ -260,13 +310,16 @@ hipError_t launch_i8_norm(const triroute_cfg &cfg, int N, const void *x, const v
   const int n = entry ? Nk : N;
   auto run = [&](auto tag, auto by_entry, auto rr) {
     using T = decltype(tag);
-    i8_norm_kernel<T, decltype(by_entry)::value, decltype(rr)::value><<<dim3((n + 3) / 4), 256, 0, st>>>(
+    constexpr bool ENTRY = decltype(by_entry)::value;
+    constexpr int W = ENTRY ? 4 : 1;
+    i8_norm_kernel<T, ENTRY, W, decltype(rr)::value><<<dim3((n * W + 3) / 4), 256, 0, st>>>(
         (const T *)x, (const T *)g, c.exp_rows, c.exp_off, eidx, slot_of, E, k, n, d, pitch,
         cfg.rms_eps, codes, scale);
   };
   auto by_width = [&](auto tag, auto by_entry) {
-    if (pitch <= 1024) run(tag, by_entry, std::integral_constant<int, 2>{});
-    else if (pitch <= 2048) run(tag, by_entry, std::integral_constant<int, 4>{});
+    const int w = decltype(by_entry)::value ? 4 : 1;
+    if (pitch <= 1024 * w) run(tag, by_entry, std::integral_constant<int, 2>{});
+    else if (pitch <= 2048 * w) run(tag, by_entry, std::integral_constant<int, 4>{});
     else run(tag, by_entry, std::integral_constant<int, 0>{});
   };
   auto by_mode = [&](auto tag) {
