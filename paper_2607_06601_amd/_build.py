@@ -20,7 +20,8 @@ LIB = os.path.join(PKG, "libtriroute.so")
 
 SOURCES = ["api.cpp", "router.hip", "compact.hip", "kv.hip", "gemm.hip", "gemm_mfma.hip", "attn_f32.hip",
            "attn_mfma.hip", "misc.hip", "relax.hip", "relax_grad.hip", "moe_grad.hip",
-           "grad.hip", "i8.hip", "gemm_i8.hip"]
+           "grad.hip", "i8.hip", "gemm_i8.hip",
+           "gemm_i8_few.hip"]
 
 HIPCC = os.environ.get("HIPCC", shutil.which("hipcc") or "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -1125,13 +1125,18 @@ static int check_act(int act) {
 static hipError_t run_linear_i8(int act, int N, int in, int out, const void *x, int64_t ldx,
                                 const triroute_i8_w &w, const void *res, int64_t ldr, void *y,
                                 int64_t ldy, const I8Rows &rows, hipStream_t st) {
+  if (tr::i8_few_rows(N, in)) return tr::i8_few_linear(act, N, out, in, x, ldx, w, res, ldr, y, ldy, st);
   const hipError_t e = tr::launch_i8_rows(act, N, in, x, ldx, rows.codes, rows.scale, st);
   return e != hipSuccess ? e : tr::i8_linear(act, N, out, in, rows.codes, rows.scale, w, res, ldr, y, ldy, st);
 }
+// made: the rotation table `rope` is there already (else it, or its entries, are made for job)
 static hipError_t run_qkv_i8(const triroute_cfg &c, int N, const void *n1, const triroute_dense_i8_w &w,
-                             const I8Rows &rows, const float *rope, void *q, void *k, void *v,
-                             hipStream_t st) {
-  const hipError_t e = tr::launch_i8_rows(c.act, N, c.d_model, n1, c.d_model, rows.codes, rows.scale, st);
+                             const I8Rows &rows, const tr::RopeJob &job, float *rope, bool made, void *q,
+                             void *k, void *v, hipStream_t st) {
+  if (tr::i8_few_rows(N, c.d_model))
+    return tr::i8_few_qkv(c, N, n1, w, made ? nullptr : &job, made ? rope : nullptr, q, k, v, st);
+  hipError_t e = made ? hipSuccess : tr::launch_rope_table(N, job, st);
+  if (e == hipSuccess) e = tr::launch_i8_rows(c.act, N, c.d_model, n1, c.d_model, rows.codes, rows.scale, st);
   return e != hipSuccess ? e : tr::i8_qkv(c, N, rows.codes, rows.scale, w, rope, q, k, v, st);
 }
 
@@ -1198,8 +1203,8 @@ int triroute_qkv_i8(const triroute_cfg *cfg, int B, int T, const void *n1,
   float *rope = carve_qkv(cv, *cfg, B * T);
   const I8Rows rows = carve_i8_rows(cv, B * T, cfg->d_model);
   hipStream_t st = (hipStream_t)stream;
-  CHECK_HIP(tr::launch_rope_table(*cfg, B * T, T, pos0, nullptr, B, rope, st), "rotation table launch");
-  CHECK_HIP(run_qkv_i8(*cfg, B * T, n1, *w, rows, rope, q, k, v, st), "qkv_i8 launch");
+  const tr::RopeJob job = tr::make_rope_job(*cfg, T, pos0, nullptr, B, rope);
+  CHECK_HIP(run_qkv_i8(*cfg, B * T, n1, *w, rows, job, rope, false, q, k, v, st), "qkv_i8 launch");
   return TRIROUTE_OK;
 }
 
@@ -1208,9 +1213,13 @@ static int moe_impl(const triroute_cfg *cfg, int n_tok, const void *xt, const tr
                     const triroute_moe_i8_w *w, const int32_t *eidx, const float *egate,
                     const triroute_compaction *cmp, void *x_out, Carve &cv, hipStream_t st) {
   const tr::MoeI8Ws m = carve_moe_i8(cv, *cfg, n_tok);
-  CHECK_HIP(tr::launch_i8_norm(*cfg, n_tok, xt, dw->g2, *cmp, eidx, m.n2, m.s_n2, m.slot_of, st),
-            "moe_i8 norm launch");
-  CHECK_HIP(tr::i8_moe(*cfg, n_tok, *w, *cmp, m, st), "moe_i8 product launch");
+  if (tr::i8_few_moe(*cfg, n_tok)) {
+    CHECK_HIP(tr::i8_few_moe_products(*cfg, n_tok, xt, dw->g2, *w, *cmp, m, st), "moe_i8 product launch");
+  } else {
+    CHECK_HIP(tr::launch_i8_norm(*cfg, n_tok, xt, dw->g2, *cmp, eidx, m.n2, m.s_n2, m.slot_of, st),
+              "moe_i8 norm launch");
+    CHECK_HIP(tr::i8_moe(*cfg, n_tok, *w, *cmp, m, st), "moe_i8 product launch");
+  }
   CHECK_HIP(tr::launch_moe_combine(*cfg, n_tok, xt, m.Y, 1, m.slot_of, eidx, egate, x_out, st),
             "combine launch");
   return TRIROUTE_OK;
@@ -1317,7 +1326,7 @@ static int layer_impl(const triroute_cfg *cfg, int B, int T, bool decode, const 
                 "list launch");
     if (T == 1 && !one) CHECK_HIP(tr::launch_scatter(lists, st), "list launch");
     if constexpr (I8)
-      CHECK_HIP(run_qkv_i8(*cfg, N, L.n1, *dw, n1q, rope, L.q, L.k, L.v, st), "qkv launch");
+      CHECK_HIP(run_qkv_i8(*cfg, N, L.n1, *dw, n1q, job, rope, true, L.q, L.k, L.v, st), "qkv launch");
     else
       CHECK_HIP(tr::launch_qkv(*cfg, B, T, L.n1, *dw, seq_len, seq_ids, cache->n_seq, L.q, L.k, L.v,
                                rope, true, st),

@@ -10,20 +10,11 @@
 //   MoE-1 : h = silu(G) U per expert, fp32
 //   MoE-2 : Y = h Wdown_e^T
 #include "gemm_kernels.hpp"
-
-// (no product fused into a sum behind it, which the compiler would do in one kernel and not in
-// another)
-#pragma clang fp contract(off)
+#include "i8_out.hpp"
 
 namespace tr {
 
-__device__ __forceinline__ float dequant(int32_t v, float row, float col) {
-  return float(v) * row * col;
-}
-
-// 1 and 8 values, rounded to the activation dtype (a NaN stays one).
-__device__ __forceinline__ void put1(float *p, float v) { *p = v; }
-__device__ __forceinline__ void put1(bf16 *p, float v) { *p = bf16(pk_bf16(v, v)); }
+// 8 values, rounded to the activation dtype (a NaN stays one).
 __device__ __forceinline__ void put8(float *p, const float *v) { store8(p, v); }
 __device__ __forceinline__ void put8(bf16 *p, const float *v) { *(u32x4_t *)p = pack8_bf16(v); }
 
@@ -350,15 +341,12 @@ struct QkvI8 {
         float y1[4], y2[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const float a1 = dequant(acc[mi][2 * u][i], elem(sr, i), elem(sc1, u));
-          const float a2 = dequant(acc[mi][2 * u + 1][i], elem(sr, i), elem(sc2, u));
-          y1[u] = a1;
-          y2[u] = a2;
+          y1[u] = dequant(acc[mi][2 * u][i], elem(sr, i), elem(sc1, u));
+          y2[u] = dequant(acc[mi][2 * u + 1][i], elem(sr, i), elem(sc2, u));
           if (rot) {
             const float4 c4 = cs[mi & 1][i][u >> 1];  // (cos, sin) of pairs j + 2 (u / 2), + 1
             const float co = (u & 1) ? c4.z : c4.x, si = (u & 1) ? c4.w : c4.y;
-            y1[u] = a1 * co - a2 * si;
-            y2[u] = a1 * si + a2 * co;
+            turn(y1[u], y2[u], co, si);
           }
         }
         if (r0 + i < t.mvalid) {
@@ -408,9 +396,7 @@ struct QkvI8 {
         const float2 *tb = rope + int64_t(row) * hd + col % hd;
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-          const float cs = tb[u].x, sn = tb[u].y, a1 = y1[u], a2 = y2[u];
-          y1[u] = a1 * cs - a2 * sn;
-          y2[u] = a1 * sn + a2 * cs;
+          turn(y1[u], y2[u], tb[u].x, tb[u].y);
         }
       }
       T *o = out + int64_t(row) * ld + col;
@@ -420,9 +406,6 @@ struct QkvI8 {
   }
 };
 
-// F64: h of fp32 activations is computed in fp64 and rounded once: the codes of h then
-// do not hang on the last bits of an fp32 exponential (a code one step off would move the output by
-// far more than an fp32 rounding does; against bf16's rounding it does not count).
 template <bool F64>
 struct Moe1I8 {
   typedef OpI8 Op;
@@ -456,13 +439,7 @@ struct Moe1I8 {
     return f < dff ? (half ? su : sg)[int64_t(t.e - 1) * dff + f] : 0.f;
   }
   __device__ float hidden(int32_t ag, int32_t au, float sr, float cg, float cu) const {
-    if constexpr (F64) {
-      const double g = double(ag) * double(sr) * double(cg), u = double(au) * double(sr) * double(cu);
-      return float(g / (1.0 + exp(-g)) * u);
-    } else {
-      const float g = dequant(ag, sr, cg), u = dequant(au, sr, cu);
-      return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u;
-    }
+    return gated<F64>(ag, au, sr, cg, cu);
   }
   // Four-wave kernel: in wave column wn, MFMA block ni, lane column c
   // holds expert unit (NI / 2) (16 wn + c) + ni / 2 of the tile, gate for

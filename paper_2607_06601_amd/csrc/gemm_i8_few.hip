@@ -1,0 +1,378 @@
+// 8-bit products of a few tokens (at most 16 rows of one matrix), with the quantisation of the rows
+// in the same launch: single tokens and small decode batches, where a launch costs more
+// than the bytes it moves.
+//
+// A block makes 16 columns (16 pairs of columns for rotation and gate/up) of one 16-row MFMA
+// tile.  Its waves share K by 128-byte pieces: each loads its pieces of the weights' rows
+// straight into fragments (a fragment feeds one MFMA, so LDS would be a detour) and adds
+// their products; the waves' sums are added in LDS (whole numbers: any order).  The rows' codes
+// come from the block itself: every block quantises the tile's rows into LDS while its first
+// weights are on the way.  Bound by the latency of that chain, then by the weights' bytes.
+#include "gemm_kernels.hpp"
+#include "i8_rows.hpp"
+#include "i8_out.hpp"
+
+namespace tr {
+
+constexpr int FEW_ROWS = 16;
+constexpr int FEW_PANEL = 48 << 10;  // bytes of codes of a tile's rows
+constexpr int FEW_PAD = 16;          // between rows of codes: 16 rows at one K lie in 16 bank groups
+
+// KS waves; the first WAIT pieces of a wave are asked for ahead of the quantisation.
+template <class P, int KS>
+__global__ __launch_bounds__(64 * KS) void i8_few_kernel(P p, int pitch, int ny) {
+  constexpr int CT = P::CT;
+  constexpr int U = 4;  // pieces of a wave in flight
+  extern __shared__ __align__(16) int8_t panel[];
+  __shared__ i32x4_t part[KS - 1][CT][64];
+  __shared__ float srow[FEW_ROWS];
+  GroupScan gs;
+  if constexpr (P::GROUPED) gs = group_scan(FEW_ROWS, p.cnt, p.E);
+  MTile t;
+  if (!p.map(blockIdx.x / ny, blockIdx.x % ny, FEW_ROWS, 16, t, gs)) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int l15 = lane & 15, kb = 16 * (lane >> 4);
+  // piece i of this wave: bytes 128 (wave + KS i) .. of a row, two fragments
+  const int np = (pitch / 128 - wave + KS - 1) / KS;
+  const int8_t *w[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) w[c] = p.col_row(t, c, l15) + 128 * wave + kb;
+  i32x4_t b[U][CT][2];
+  auto fetch = [&](int i, i32x4_t (&f)[CT][2]) {
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) f[c][h] = *(const i32x4_t *)(w[c] + int64_t(i) * (128 * KS) + 64 * h);
+  };
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (u < np) fetch(u, b[u]);
+  for (int r = wave; r < t.mvalid; r += KS) {
+    const float s = p.quantise(t, r, pitch, lane, panel + r * (pitch + FEW_PAD));
+    if (lane == 0) srow[r] = s;
+  }
+  __syncthreads();
+  i32x4_t acc[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) acc[c] = i32x4_t{0, 0, 0, 0};
+  // (rows past the valid ones read row 0: their sums are not stored)
+  const int8_t *a = panel + (l15 < t.mvalid ? l15 : 0) * (pitch + FEW_PAD) + 128 * wave + kb;
+  for (int i = 0; i < np; i += U) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i + u < np) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const i32x4_t af = *(const i32x4_t *)(a + (i + u) * (128 * KS) + 64 * h);
+#pragma unroll
+          for (int c = 0; c < CT; ++c) acc[c] = OpI8::mma(af, b[u][c][h], acc[c]);
+        }
+        if (i + u + U < np) fetch(i + u + U, b[u]);
+      }
+    }
+  }
+  if (wave > 0) {
+#pragma unroll
+    for (int c = 0; c < CT; ++c) part[wave - 1][c][lane] = acc[c];
+  }
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int k = 0; k < KS - 1; ++k)
+#pragma unroll
+    for (int c = 0; c < CT; ++c) acc[c] += part[k][c][lane];
+  // lane: rows 4 (lane / 16) + i, column (pair) lane % 16
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = 4 * (lane >> 4) + i;
+    if (r < t.mvalid) {
+      if constexpr (CT == 2)
+        p.store(t, r, l15, acc[0][i], acc[1][i], srow[r]);
+      else
+        p.store(t, r, l15, acc[0][i], srow[r]);
+    }
+  }
+}
+
+// ---------------------------------------------------------------- problems
+template <typename T>
+struct RowsIn {  // rows of tokens, of any stride and alignment
+  const T *x;
+  int64_t ldx;
+  int cols;
+  bool vec;
+  __device__ float quantise(int row, int pitch, int lane, int8_t *dst) const {
+    const T *xr = x + row * ldx;
+    if (vec) return wave_row([&](int c, float *v) { row8<T, true>(xr, c, cols, v); }, pitch, lane, dst);
+    return wave_row([&](int c, float *v) { row8<T, false>(xr, c, cols, v); }, pitch, lane, dst);
+  }
+};
+
+template <typename T>
+struct FewLinear {
+  static constexpr int CT = 1;
+  static constexpr bool GROUPED = false;
+  RowsIn<T> in;
+  const int8_t *w;
+  const float *sw;
+  T *y;
+  const T *res;
+  int64_t ldy, ldr;
+  int N, m, pitch;
+  __device__ bool map(int, int by, int, int, MTile &t, const GroupScan &) const {
+    t.m0 = t.e = t.p0 = 0;
+    t.n0 = by * 16;
+    t.mvalid = N;
+    return true;
+  }
+  __device__ const int8_t *col_row(const MTile &t, int, int c) const {
+    return w + int64_t(min(t.n0 + c, m - 1)) * pitch;
+  }
+  __device__ float quantise(const MTile &, int r, int pt, int lane, int8_t *dst) const {
+    return in.quantise(r, pt, lane, dst);
+  }
+  __device__ void store(const MTile &t, int r, int c, int32_t v, float sr) const {
+    const int col = t.n0 + c;
+    if (col >= m) return;
+    const float o = dequant(v, sr, sw[col]);
+    put1(y + r * ldy + col, res ? Act<T>::ld(res, r * ldr + col) + o : o);
+  }
+};
+
+template <typename T>
+struct FewQkv {
+  static constexpr int CT = 2;
+  static constexpr bool GROUPED = false;
+  RowsIn<T> in;
+  const int8_t *Wq, *Wk, *Wv;
+  const float *sq, *sk, *sv;
+  T *q, *k, *v;
+  const float2 *rope;  // the rotation table, or NULL: entries are made here
+  RopeJob job;
+  int N, Hd, Kd, dh, pitch;
+  __device__ bool map(int, int by, int, int, MTile &t, const GroupScan &) const {
+    t.m0 = t.e = t.p0 = 0;
+    // 16 pairs j0 .. of one head: by counts them over the heads of q, k, v
+    const int per = dh / 32;
+    t.n0 = (by / per) * dh + (by % per) * 16;
+    t.mvalid = N;
+    return true;
+  }
+  // matrix and column within it of half `half` of pair c of the tile
+  __device__ int at(const MTile &t, int half, int c, int &which) const {
+    const int gc = t.n0 + c + half * (dh >> 1);
+    which = gc < Hd ? 0 : gc < Hd + Kd ? 1 : 2;
+    return gc - (which == 0 ? 0 : which == 1 ? Hd : Hd + Kd);
+  }
+  __device__ const int8_t *col_row(const MTile &t, int half, int c) const {
+    int which;
+    const int col = at(t, half, c, which);
+    return (which == 0 ? Wq : which == 1 ? Wk : Wv) + int64_t(col) * pitch;
+  }
+  __device__ float quantise(const MTile &, int r, int pt, int lane, int8_t *dst) const {
+    return in.quantise(r, pt, lane, dst);
+  }
+  __device__ void store(const MTile &t, int r, int c, int32_t v1, int32_t v2, float sr) const {
+    int which;
+    const int col = at(t, 0, c, which), hd = dh >> 1;
+    const float *s = which == 0 ? sq : which == 1 ? sk : sv;
+    float y1 = dequant(v1, sr, s[col]), y2 = dequant(v2, sr, s[col + hd]);
+    if (which < 2) {
+      const int j = col % dh;
+      const float2 cs = rope ? rope[int64_t(r) * hd + j] : rope_entry(job, r, j);
+      turn(y1, y2, cs.x, cs.y);
+    }
+    T *o = (which == 0 ? q : which == 1 ? k : v) + int64_t(r) * (which == 0 ? Hd : Kd) + col;
+    put1(o, y1);
+    put1(o + hd, y2);
+  }
+};
+
+// Gate/up of list rows, from the tokens: second RMSNorm (fp64, rounded once to fp32, as
+// i8_norm_kernel), codes, products, h.
+template <typename T>
+struct FewUp {
+  static constexpr int CT = 2;
+  static constexpr bool GROUPED = true;
+  const T *x, *g;
+  const int32_t *rows, *cnt;
+  int32_t *slot_of;
+  const int8_t *Wg, *Wu;
+  const float *sg, *su;
+  float *h;
+  int E, k, d, dff, pitch;
+  float eps;
+  __device__ bool map(int bx, int by, int BM, int, MTile &t, const GroupScan &gs) const {
+    t.n0 = by * 16;
+    return mmap_grouped(bx, BM, gs, t);
+  }
+  __device__ const int8_t *col_row(const MTile &t, int half, int c) const {
+    return (half ? Wu : Wg) + (int64_t(t.e - 1) * dff + t.n0 + c) * pitch;
+  }
+  __device__ float quantise(const MTile &t, int r, int pt, int lane, int8_t *dst) const {
+    const int a = rows[t.p0 + r];
+    if (t.n0 == 0 && lane == 0) slot_of[a] = t.p0 + r;
+    const T *xr = x + int64_t(a / k) * d;
+    double ss = 0.0;
+    for (int c = lane * 8; c < d; c += 512) {
+      float v[8];
+      load8(xr + c, v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) ss = fma(double(v[j]), double(v[j]), ss);
+    }
+    const double inv = 1.0 / sqrt(wave_sum(ss) / double(d) + double(eps));
+    return wave_row(
+        [&](int c, float *v) {
+          row8<T, true>(xr, c, d, v);
+          if (c < d) norm8<T>(g + c, inv, v);
+        },
+        pt, lane, dst);
+  }
+  __device__ void store(const MTile &t, int r, int c, int32_t vg, int32_t vu, float sr) const {
+    const int f = t.n0 + c;
+    const int64_t wr = int64_t(t.e - 1) * dff + f;
+    h[int64_t(t.p0 + r) * dff + f] = gated<sizeof(T) == 4>(vg, vu, sr, sg[wr], su[wr]);
+  }
+};
+
+// Down product of list rows, from h.
+struct FewDown {
+  static constexpr int CT = 1;
+  static constexpr bool GROUPED = true;
+  const float *h;
+  const int32_t *cnt;
+  const int8_t *Wd;
+  const float *sd;
+  float *Y;
+  int E, d, dff, pitch;
+  __device__ bool map(int bx, int by, int BM, int, MTile &t, const GroupScan &gs) const {
+    t.n0 = by * 16;
+    return mmap_grouped(bx, BM, gs, t);
+  }
+  __device__ const int8_t *col_row(const MTile &t, int, int c) const {
+    return Wd + (int64_t(t.e - 1) * d + t.n0 + c) * pitch;
+  }
+  __device__ float quantise(const MTile &t, int r, int pt, int lane, int8_t *dst) const {
+    const float *hr = h + int64_t(t.p0 + r) * dff;
+    return wave_row([&](int c, float *v) { row8<float, true>(hr, c, dff, v); }, pt, lane, dst);
+  }
+  __device__ void store(const MTile &t, int r, int c, int32_t v, float sr) const {
+    const int col = t.n0 + c;
+    Y[int64_t(t.p0 + r) * d + col] = dequant(v, sr, sd[int64_t(t.e - 1) * d + col]);
+  }
+};
+
+// ------------------------------------------------------------------ launchers
+template <class P>
+static hipError_t launch_few(const P &p, int rows, int pitch, int tiles, int ny, hipStream_t st) {
+  const size_t lds = size_t(rows) * (pitch + FEW_PAD);
+  // eight waves where K has as many pieces
+  if (pitch >= 8 * 128)
+    i8_few_kernel<P, 8><<<tiles * ny, 512, lds, st>>>(p, pitch, ny);
+  else
+    i8_few_kernel<P, 4><<<tiles * ny, 256, lds, st>>>(p, pitch, ny);
+  return hipGetLastError();
+}
+
+static bool few_fit(int rows, int cols) {
+  return rows <= FEW_ROWS && int64_t(rows) * i8_pitch(cols) <= FEW_PANEL;
+}
+bool i8_few_rows(int N, int cols) { return few_fit(N, cols); }
+bool i8_few_moe(const triroute_cfg &cfg, int N) {
+  return N * cfg.top_k <= FEW_ROWS && few_fit(N * cfg.top_k, std::max(cfg.d_model, cfg.d_ff));
+}
+
+template <typename T>
+static RowsIn<T> rows_in(const void *x, int64_t ldx, int cols) {
+  return RowsIn<T>{(const T *)x, ldx, cols,
+                   cols % 8 == 0 && ((uintptr_t(x) | uintptr_t(ldx * int64_t(sizeof(T)))) & 15) == 0};
+}
+
+hipError_t i8_few_linear(int act, int N, int m, int k, const void *x, int64_t ldx, const triroute_i8_w &w,
+                         const void *res, int64_t ldr, void *y, int64_t ldy, hipStream_t st) {
+  auto run = [&](auto tag) {
+    using T = decltype(tag);
+    FewLinear<T> p;
+    p.in = rows_in<T>(x, ldx, k);
+    p.w = (const int8_t *)w.codes;
+    p.sw = w.scale;
+    p.y = (T *)y;
+    p.res = (const T *)res;
+    p.ldy = ldy;
+    p.ldr = ldr;
+    p.N = N;
+    p.m = m;
+    p.pitch = i8_pitch(k);
+    return launch_few(p, N, p.pitch, 1, (m + 15) / 16, st);
+  };
+  return act == TRIROUTE_BF16 ? run(bf16{}) : run(float{});
+}
+
+hipError_t i8_few_qkv(const triroute_cfg &cfg, int N, const void *n1, const triroute_dense_i8_w &w,
+                      const RopeJob *job, const float *rope, void *q, void *k, void *v, hipStream_t st) {
+  auto run = [&](auto tag) {
+    using T = decltype(tag);
+    FewQkv<T> p;
+    p.in = rows_in<T>(n1, cfg.d_model, cfg.d_model);
+    p.Wq = (const int8_t *)w.Wq.codes;
+    p.Wk = (const int8_t *)w.Wk.codes;
+    p.Wv = (const int8_t *)w.Wv.codes;
+    p.sq = w.Wq.scale;
+    p.sk = w.Wk.scale;
+    p.sv = w.Wv.scale;
+    p.q = (T *)q;
+    p.k = (T *)k;
+    p.v = (T *)v;
+    p.rope = (const float2 *)rope;
+    if (job) p.job = *job;
+    p.N = N;
+    p.dh = cfg.head_dim;
+    p.Hd = cfg.n_heads * cfg.head_dim;
+    p.Kd = cfg.n_kv_heads * cfg.head_dim;
+    p.pitch = i8_pitch(cfg.d_model);
+    return launch_few(p, N, p.pitch, 1, (p.Hd + 2 * p.Kd) / 32, st);
+  };
+  return cfg.act == TRIROUTE_BF16 ? run(bf16{}) : run(float{});
+}
+
+hipError_t i8_few_moe_products(const triroute_cfg &cfg, int N, const void *xt, const void *g2,
+                               const triroute_moe_i8_w &w, const triroute_compaction &c,
+                               const MoeI8Ws &ws, hipStream_t st) {
+  const int Nk = N * cfg.top_k, E = cfg.n_experts, tiles = std::min(E, Nk);
+  auto up = [&](auto tag) {
+    using T = decltype(tag);
+    FewUp<T> p;
+    p.x = (const T *)xt;
+    p.g = (const T *)g2;
+    p.rows = c.exp_rows;
+    p.cnt = c.exp_cnt;
+    p.slot_of = ws.slot_of;
+    p.Wg = (const int8_t *)w.Wgate.codes;
+    p.Wu = (const int8_t *)w.Wup.codes;
+    p.sg = w.Wgate.scale;
+    p.su = w.Wup.scale;
+    p.h = ws.h;
+    p.E = E;
+    p.k = cfg.top_k;
+    p.d = cfg.d_model;
+    p.dff = cfg.d_ff;
+    p.pitch = i8_pitch(cfg.d_model);
+    p.eps = cfg.rms_eps;
+    return launch_few(p, Nk, p.pitch, tiles, cfg.d_ff / 16, st);
+  };
+  const hipError_t e = cfg.act == TRIROUTE_BF16 ? up(bf16{}) : up(float{});
+  if (e != hipSuccess) return e;
+  FewDown p;
+  p.h = ws.h;
+  p.cnt = c.exp_cnt;
+  p.Wd = (const int8_t *)w.Wdown.codes;
+  p.sd = w.Wdown.scale;
+  p.Y = ws.Y;
+  p.E = E;
+  p.d = cfg.d_model;
+  p.dff = cfg.d_ff;
+  p.pitch = i8_pitch(cfg.d_ff);
+  return launch_few(p, Nk, p.pitch, tiles, cfg.d_model / 16, st);
+}
+
+}  // namespace tr

@@ -1,105 +1,9 @@
-// Quantisation of rows to 8-bit codes with one fp32 scale a row (the tokens of an 8-bit
-// product, and weights by output channel):
-//   a = max |x|,  scale = a / 127 rounded to fp32,  c = 127 x / a rounded half to even.
-// The rounding is that of the exact quotient: near a border of two codes the sides are compared
-// as whole numbers (254 |x| against (2 k + 1) a, both exact in fp64), so a code never
-// depends on how the quotient was computed, and the same row gives the same codes on every path.
-// A row that holds a NaN or an infinity gets codes 0 and scale NaN: its outputs are
-// NaN, other rows' are not touched.  Codes lie in rows of i8_pitch() bytes, zero
-// behind the last element, so a product needs no code of its own for the end of K.
+// Passes that quantise rows to 8-bit codes (i8_rows.hpp): tokens and weights, the experts'
+// normalised tokens, hidden rows.
+#include "i8_rows.hpp"
 #include "kernels.hpp"
 
 namespace tr {
-
-constexpr uint32_t INF_BITS = 0x7F800000u;
-
-__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
-
-// Largest magnitude of a row, as the bits of |x|: as whole numbers NaN > inf > finite.
-__device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
-#define TR_ROR(n) uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x120 + (n), 0xF, 0xF, false))
-  v = max(v, TR_ROR(1));
-  v = max(v, TR_ROR(2));
-  v = max(v, TR_ROR(4));
-  v = max(v, TR_ROR(8));
-#undef TR_ROR
-  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  v = max(uint32_t(a[0]), uint32_t(a[1]));
-  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return max(uint32_t(b[0]), uint32_t(b[1]));
-}
-
-// Scale of a row and the codes of its elements.  A code is the quotient in fp32, rounded; with
-// one of 8 next to a border (4e-5; the quotient is off by at most 127 * 2^-23), the 8 are
-// compared with their borders instead.  The quotients of a row of tiny values are of values 2^64 times
-// larger (exact), so that 127 / a stays finite.
-struct RowCode {
-  float a, inv;
-  float scale;
-  bool bad, tiny;
-  __device__ __forceinline__ explicit RowCode(uint32_t amax) {
-    a = __uint_as_float(amax);
-    bad = amax >= INF_BITS;
-    tiny = a < 1e-30f;
-    scale = bad ? __uint_as_float(0x7FC00000u) : a / 127.0f;
-    if (tiny) a *= LIFT;
-    inv = a > 0.0f && !bad ? 127.0f / a : 0.0f;
-  }
-  static constexpr float LIFT = 18446744073709551616.0f;
-  // the code of v >= 0 whose quotient is about t
-  __device__ __forceinline__ int exact(float v, float t) const {
-    const int k = int(t);
-    if (fabsf(t - (float(k) + 0.5f)) > 1e-3f) return int(rintf(t));
-    const double over = 254.0 * double(v) - double(2 * k + 1) * double(a);
-    return over > 0.0 ? k + 1 : over < 0.0 ? k : k + (k & 1);
-  }
-  __device__ __forceinline__ uint2 code8(const float *x) const {
-    float v[8], r[8], far = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = x[i];
-    if (tiny) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] *= LIFT;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float t = v[i] * inv;
-      r[i] = rintf(t);
-      far = fmaxf(far, fabsf(t - r[i]));
-    }
-    if (far > 0.49996f) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) r[i] = copysignf(float(exact(fabsf(v[i]), fabsf(v[i]) * inv)), v[i]);
-    }
-    // (the byte of a whole number up to 127 is the lowest of it plus 1.5 * 2^23)
-    uint32_t w[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(r[i] + 12582912.0f);
-    // bytes 0 of two words, then of two pairs
-    uint2 o;
-    o.x = __builtin_amdgcn_perm(__builtin_amdgcn_perm(w[3], w[2], 0x0C0C0400u),
-                                __builtin_amdgcn_perm(w[1], w[0], 0x0C0C0400u), 0x05040100u);
-    o.y = __builtin_amdgcn_perm(__builtin_amdgcn_perm(w[7], w[6], 0x0C0C0400u),
-                                __builtin_amdgcn_perm(w[5], w[4], 0x0C0C0400u), 0x05040100u);
-    return bad ? make_uint2(0u, 0u) : o;
-  }
-};
-
-// 8 elements at c of a row of `cols`, zeros behind its end.  VEC: whole aligned pieces.
-template <typename T, bool VEC>
-__device__ __forceinline__ void row8(const T *row, int c, int cols, float *v) {
-  if constexpr (VEC) {
-    if (c < cols) {
-      load8(row + c, v);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 0.f;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? Act<T>::ld(row, c + i) : 0.f;
-  }
-}
 
 // W waves a row (4 / W rows a block), 8 consecutive elements per lane access; the first
 // RR accesses of a lane stay in registers between the maximum and the codes, later ones are
@@ -236,26 +140,19 @@ __global__ __launch_bounds__(256) void i8_norm_kernel(
   }
   const double r = 1.0 / sqrt(ss / double(d) + double(eps));
   uint32_t m = 0;
-  auto norm8 = [&](int c, float *w) {
+  auto normed = [&](int c, float *w) {
     if (c >= d) return;
-    float gv[8];
-    load8(g + c, gv);
+    norm8<T>(g + c, r, w);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if constexpr (sizeof(T) == 2)  // (the product of two bf16 numbers is an fp32 number)
-        w[j] = float(double(w[j] * gv[j]) * r);
-      else
-        w[j] = float((double(w[j]) * r) * double(gv[j]));
-      m = max(m, abs_bits(w[j]));
-    }
+    for (int j = 0; j < 8; ++j) m = max(m, abs_bits(w[j]));
   };
   if constexpr (KEEP) {
 #pragma unroll
-    for (int q = 0; q < RR; ++q) norm8(at + STEP * q, v[q]);
+    for (int q = 0; q < RR; ++q) normed(at + STEP * q, v[q]);
   } else {
     for (int c = at; c < d; c += STEP) {
       load8(xr + c, v[0]);
-      norm8(c, v[0]);
+      normed(c, v[0]);
     }
   }
   m = wave_umax(m);
@@ -283,7 +180,7 @@ __global__ __launch_bounds__(256) void i8_norm_kernel(
   } else {
     for (int c = at; c < pitch; c += STEP) {
       row8<T, true>(xr, c, d, v[0]);
-      norm8(c, v[0]);
+      normed(c, v[0]);
       emit(c, rc.code8(v[0]));
     }
   }
