@@ -1125,7 +1125,7 @@ static int check_act(int act) {
 static hipError_t run_linear_i8(int act, int N, int in, int out, const void *x, int64_t ldx,
                                 const triroute_i8_w &w, const void *res, int64_t ldr, void *y,
                                 int64_t ldy, const I8Rows &rows, hipStream_t st) {
-  if (tr::i8_few_rows(N, in)) return tr::i8_few_linear(act, N, out, in, x, ldx, w, res, ldr, y, ldy, st);
+  if (tr::i8_few_fit(N, in)) return tr::i8_few_linear(act, N, out, in, x, ldx, w, res, ldr, y, ldy, st);
   const hipError_t e = tr::launch_i8_rows(act, N, in, x, ldx, rows.codes, rows.scale, st);
   return e != hipSuccess ? e : tr::i8_linear(act, N, out, in, rows.codes, rows.scale, w, res, ldr, y, ldy, st);
 }
@@ -1133,7 +1133,7 @@ static hipError_t run_linear_i8(int act, int N, int in, int out, const void *x, 
 static hipError_t run_qkv_i8(const triroute_cfg &c, int N, const void *n1, const triroute_dense_i8_w &w,
                              const I8Rows &rows, const tr::RopeJob &job, float *rope, bool made, void *q,
                              void *k, void *v, hipStream_t st) {
-  if (tr::i8_few_rows(N, c.d_model))
+  if (tr::i8_few_fit(N, c.d_model))
     return tr::i8_few_qkv(c, N, n1, w, made ? nullptr : &job, made ? rope : nullptr, q, k, v, st);
   hipError_t e = made ? hipSuccess : tr::launch_rope_table(N, job, st);
   if (e == hipSuccess) e = tr::launch_i8_rows(c.act, N, c.d_model, n1, c.d_model, rows.codes, rows.scale, st);
@@ -1213,13 +1213,14 @@ static int moe_impl(const triroute_cfg *cfg, int n_tok, const void *xt, const tr
                     const triroute_moe_i8_w *w, const int32_t *eidx, const float *egate,
                     const triroute_compaction *cmp, void *x_out, Carve &cv, hipStream_t st) {
   const tr::MoeI8Ws m = carve_moe_i8(cv, *cfg, n_tok);
-  if (tr::i8_few_moe(*cfg, n_tok)) {
-    CHECK_HIP(tr::i8_few_moe_products(*cfg, n_tok, xt, dw->g2, *w, *cmp, m, st), "moe_i8 product launch");
-  } else {
-    CHECK_HIP(tr::launch_i8_norm(*cfg, n_tok, xt, dw->g2, *cmp, eidx, m.n2, m.s_n2, m.slot_of, st),
-              "moe_i8 norm launch");
-    CHECK_HIP(tr::i8_moe(*cfg, n_tok, *w, *cmp, m, st), "moe_i8 product launch");
+  if (tr::i8_few_fit_moe(*cfg, n_tok)) {
+    CHECK_HIP(tr::i8_few_moe(*cfg, n_tok, xt, dw->g2, *w, *cmp, eidx, egate, x_out, m, st),
+              "moe_i8 launch");
+    return TRIROUTE_OK;
   }
+  CHECK_HIP(tr::launch_i8_norm(*cfg, n_tok, xt, dw->g2, *cmp, eidx, m.n2, m.s_n2, m.slot_of, st),
+            "moe_i8 norm launch");
+  CHECK_HIP(tr::i8_moe(*cfg, n_tok, *w, *cmp, m, st), "moe_i8 product launch");
   CHECK_HIP(tr::launch_moe_combine(*cfg, n_tok, xt, m.Y, 1, m.slot_of, eidx, egate, x_out, st),
             "combine launch");
   return TRIROUTE_OK;

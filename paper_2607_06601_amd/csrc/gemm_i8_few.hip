@@ -18,7 +18,95 @@ constexpr int FEW_ROWS = 16;
 constexpr int FEW_PANEL = 48 << 10;  // bytes of codes of a tile's rows
 constexpr int FEW_PAD = 16;          // between rows of codes: 16 rows at one K lie in 16 bank groups
 
-// KS waves; the first WAIT pieces of a wave are asked for ahead of the quantisation.
+// A row quantised by the whole block, KS waves: up to 1024 KS elements, which stay in
+// registers.  red: KS entries for this row alone.
+template <class P, int KS>
+__device__ __forceinline__ void block_row(const P &p, const MTile &t, int r, int pitch, double *red,
+                                          uint32_t *mred, int8_t *dst, float &scale) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int STEP = 512 * KS;
+  const int at = threadIdx.x * 8;
+  const auto row = p.row(t, r);
+  float v[2][8];
+#pragma unroll
+  for (int q = 0; q < 2; ++q) p.load(row, at + STEP * q, v[q]);
+  if constexpr (P::NORM) {
+    float gv[2][8];  // (the gains on their way during the sum)
+#pragma unroll
+    for (int q = 0; q < 2; ++q) p.gains(at + STEP * q, gv[q]);
+    double ss = 0.0;
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) ss = fma(double(v[q][j]), double(v[q][j]), ss);
+    ss = wave_sum(ss);
+    if (lane == 0) red[wave] = ss;
+    __syncthreads();
+    ss = 0.0;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) ss += red[k];
+    const double inv = p.inv_norm(ss);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) norm8<typename P::elem>(gv[q], inv, v[q]);
+  }
+  uint32_t m = 0;
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[q][j]));
+  m = wave_umax(m);
+  if (lane == 0) mred[wave] = m;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < KS; ++k) m = max(m, mred[k]);
+  const RowCode rc(m);
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+    if (at + STEP * q < pitch) *(uint2 *)(dst + at + STEP * q) = rc.code8(v[q]);
+  if (threadIdx.x == 0) scale = rc.scale;
+}
+
+// The codes and scales of a tile's rows: up to two by the whole block, else a wave each.
+template <class P, int KS>
+__device__ __forceinline__ void tile_rows(const P &p, const MTile &t, int pitch, int8_t *panel,
+                                          float *srow) {
+  __shared__ double red[2][KS];
+  __shared__ uint32_t mred[2][KS];
+  if (t.mvalid <= 2 && pitch <= 1024 * KS) {
+    for (int r = 0; r < t.mvalid; ++r)
+      block_row<P, KS>(p, t, r, pitch, red[r], mred[r], panel + r * (pitch + FEW_PAD), srow[r]);
+  } else {
+    const int lane = threadIdx.x & 63;
+    for (int r = threadIdx.x >> 6; r < t.mvalid; r += KS) {
+      const auto row = p.row(t, r);
+      double inv = 0.0;
+      if constexpr (P::NORM) {
+        double ss = 0.0;
+        for (int c = lane * 8; c < pitch; c += 512) {
+          float v[8];
+          p.load(row, c, v);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) ss = fma(double(v[j]), double(v[j]), ss);
+        }
+        inv = p.inv_norm(wave_sum(ss));
+      }
+      const float s = wave_row(
+          [&](int c, float *v) {
+            p.load(row, c, v);
+            if constexpr (P::NORM) {
+              float gv[8];
+              p.gains(c, gv);
+              norm8<typename P::elem>(gv, inv, v);
+            }
+          },
+          pitch, lane, panel + r * (pitch + FEW_PAD));
+      if (lane == 0) srow[r] = s;
+    }
+  }
+  __syncthreads();
+}
+
+// KS waves; a wave's first U pieces are asked for ahead of the quantisation.
 template <class P, int KS>
 __global__ __launch_bounds__(64 * KS) void i8_few_kernel(P p, int pitch, int ny) {
   constexpr int CT = P::CT;
@@ -47,11 +135,7 @@ __global__ __launch_bounds__(64 * KS) void i8_few_kernel(P p, int pitch, int ny)
 #pragma unroll
   for (int u = 0; u < U; ++u)
     if (u < np) fetch(u, b[u]);
-  for (int r = wave; r < t.mvalid; r += KS) {
-    const float s = p.quantise(t, r, pitch, lane, panel + r * (pitch + FEW_PAD));
-    if (lane == 0) srow[r] = s;
-  }
-  __syncthreads();
+  tile_rows<P, KS>(p, t, pitch, panel, srow);
   i32x4_t acc[CT];
 #pragma unroll
   for (int c = 0; c < CT; ++c) acc[c] = i32x4_t{0, 0, 0, 0};
@@ -97,22 +181,25 @@ __global__ __launch_bounds__(64 * KS) void i8_few_kernel(P p, int pitch, int ny)
 // ---------------------------------------------------------------- problems
 template <typename T>
 struct RowsIn {  // rows of tokens, of any stride and alignment
+  typedef T elem;
+  static constexpr bool NORM = false;
   const T *x;
   int64_t ldx;
   int cols;
   bool vec;
-  __device__ float quantise(int row, int pitch, int lane, int8_t *dst) const {
-    const T *xr = x + row * ldx;
-    if (vec) return wave_row([&](int c, float *v) { row8<T, true>(xr, c, cols, v); }, pitch, lane, dst);
-    return wave_row([&](int c, float *v) { row8<T, false>(xr, c, cols, v); }, pitch, lane, dst);
+  __device__ const T *row(const MTile &, int r) const { return x + r * ldx; }
+  __device__ void load(const T *row, int c, float *v) const {
+    if (vec)
+      row8<T, true>(row, c, cols, v);
+    else
+      row8<T, false>(row, c, cols, v);
   }
 };
 
 template <typename T>
-struct FewLinear {
+struct FewLinear : RowsIn<T> {
   static constexpr int CT = 1;
   static constexpr bool GROUPED = false;
-  RowsIn<T> in;
   const int8_t *w;
   const float *sw;
   T *y;
@@ -128,9 +215,6 @@ struct FewLinear {
   __device__ const int8_t *col_row(const MTile &t, int, int c) const {
     return w + int64_t(min(t.n0 + c, m - 1)) * pitch;
   }
-  __device__ float quantise(const MTile &, int r, int pt, int lane, int8_t *dst) const {
-    return in.quantise(r, pt, lane, dst);
-  }
   __device__ void store(const MTile &t, int r, int c, int32_t v, float sr) const {
     const int col = t.n0 + c;
     if (col >= m) return;
@@ -140,10 +224,9 @@ struct FewLinear {
 };
 
 template <typename T>
-struct FewQkv {
+struct FewQkv : RowsIn<T> {
   static constexpr int CT = 2;
   static constexpr bool GROUPED = false;
-  RowsIn<T> in;
   const int8_t *Wq, *Wk, *Wv;
   const float *sq, *sk, *sv;
   T *q, *k, *v;
@@ -168,9 +251,6 @@ struct FewQkv {
     int which;
     const int col = at(t, half, c, which);
     return (which == 0 ? Wq : which == 1 ? Wk : Wv) + int64_t(col) * pitch;
-  }
-  __device__ float quantise(const MTile &, int r, int pt, int lane, int8_t *dst) const {
-    return in.quantise(r, pt, lane, dst);
   }
   __device__ void store(const MTile &t, int r, int c, int32_t v1, int32_t v2, float sr) const {
     int which;
@@ -209,25 +289,16 @@ struct FewUp {
   __device__ const int8_t *col_row(const MTile &t, int half, int c) const {
     return (half ? Wu : Wg) + (int64_t(t.e - 1) * dff + t.n0 + c) * pitch;
   }
-  __device__ float quantise(const MTile &t, int r, int pt, int lane, int8_t *dst) const {
+  typedef T elem;
+  static constexpr bool NORM = true;
+  __device__ const T *row(const MTile &t, int r) const {
     const int a = rows[t.p0 + r];
-    if (t.n0 == 0 && lane == 0) slot_of[a] = t.p0 + r;
-    const T *xr = x + int64_t(a / k) * d;
-    double ss = 0.0;
-    for (int c = lane * 8; c < d; c += 512) {
-      float v[8];
-      load8(xr + c, v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) ss = fma(double(v[j]), double(v[j]), ss);
-    }
-    const double inv = 1.0 / sqrt(wave_sum(ss) / double(d) + double(eps));
-    return wave_row(
-        [&](int c, float *v) {
-          row8<T, true>(xr, c, d, v);
-          if (c < d) norm8<T>(g + c, inv, v);
-        },
-        pt, lane, dst);
+    if (t.n0 == 0 && (threadIdx.x & 63) == 0) slot_of[a] = t.p0 + r;
+    return x + int64_t(a / k) * d;
   }
+  __device__ void load(const T *row, int c, float *v) const { row8<T, true>(row, c, d, v); }
+  __device__ void gains(int c, float *v) const { row8<T, true>(g, c, d, v); }
+  __device__ double inv_norm(double ss) const { return 1.0 / sqrt(ss / double(d) + double(eps)); }
   __device__ void store(const MTile &t, int r, int c, int32_t vg, int32_t vu, float sr) const {
     const int f = t.n0 + c;
     const int64_t wr = int64_t(t.e - 1) * dff + f;
@@ -235,32 +306,98 @@ struct FewUp {
   }
 };
 
-// Down product of list rows, from h.
-struct FewDown {
-  static constexpr int CT = 1;
-  static constexpr bool GROUPED = true;
-  const float *h;
-  const int32_t *cnt;
-  const int8_t *Wd;
-  const float *sd;
-  float *Y;
-  int E, d, dff, pitch;
-  __device__ bool map(int bx, int by, int BM, int, MTile &t, const GroupScan &gs) const {
-    t.n0 = by * 16;
-    return mmap_grouped(bx, BM, gs, t);
+// Down products of every list row and the sum over a token's slots, x_out = xt + sum gate Y.  A
+// block makes 16 columns of all rows (at most 16): the pieces of the weights of every expert
+// in use are shared by its waves, and with an expert's piece the rows of other experts are
+// zeros, so one accumulator takes them all.  Slots are added in slot order, as moe_combine
+// does.
+template <typename T, int KS>
+__global__ __launch_bounds__(64 * KS) void i8_few_down_kernel(
+    const float *__restrict__ h, const int32_t *__restrict__ cnt, const int8_t *__restrict__ Wd,
+    const float *__restrict__ sd, const int32_t *__restrict__ slot_of,
+    const int32_t *__restrict__ eidx, const float *__restrict__ egate, const T *xt, T *xout, int N,
+    int k, int E, int d, int dff, int pitch) {
+  constexpr int U = 4;
+  extern __shared__ __align__(16) int8_t panel[];
+  __shared__ i32x4_t part[KS - 1][64];
+  __shared__ float srow[FEW_ROWS], ys[FEW_ROWS][17];
+  __shared__ int ge[FEW_ROWS], gp[FEW_ROWS + 1];  // the experts in use, and their first rows
+  const GroupScan gs = group_scan(FEW_ROWS, cnt, E);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int l15 = lane & 15, kb = 16 * (lane >> 4), n0 = blockIdx.x * 16;
+  const int groups = gs.total;  // one tile an expert in use: it has 16 rows at most
+  if (wave == 0 && gs.nt) {
+    ge[gs.incl - 1] = lane + 1;
+    gp[gs.incl - 1] = gs.start;
+    if (gs.incl == groups) gp[groups] = gs.start + gs.c;
   }
-  __device__ const int8_t *col_row(const MTile &t, int, int c) const {
-    return Wd + (int64_t(t.e - 1) * d + t.n0 + c) * pitch;
+  if (groups == 0 && threadIdx.x == 0) gp[0] = 0;
+  __syncthreads();
+  const int per = pitch / 128, all = groups * per;
+  const int np = (all - wave + KS - 1) / KS;
+  const int8_t *w = Wd + int64_t(n0 + l15) * pitch + kb;
+  i32x4_t b[U][2];
+  auto fetch = [&](int i, i32x4_t (&f)[2]) {
+    const int piece = wave + KS * i, q = piece / per;
+    const int8_t *src = w + int64_t(ge[q] - 1) * d * pitch + (piece - q * per) * 128;
+#pragma unroll
+    for (int hh = 0; hh < 2; ++hh) f[hh] = *(const i32x4_t *)(src + 64 * hh);
+  };
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (u < np) fetch(u, b[u]);
+  MTile t;
+  t.mvalid = gp[groups];
+  RowsIn<float> rows{h, dff, dff, true};
+  tile_rows<RowsIn<float>, KS>(rows, t, pitch, panel, srow);
+  i32x4_t acc = {0, 0, 0, 0};
+  const int8_t *a = panel + (l15 < t.mvalid ? l15 : 0) * (pitch + FEW_PAD) + kb;
+  for (int i = 0; i < np; i += U) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i + u < np) {
+        const int piece = wave + KS * (i + u), q = piece / per;
+        const bool mine = l15 >= gp[q] && l15 < gp[q + 1];
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+          i32x4_t af = *(const i32x4_t *)(a + (piece - q * per) * 128 + 64 * hh);
+          if (!mine) af = i32x4_t{0, 0, 0, 0};
+          acc = OpI8::mma(af, b[u][hh], acc);
+        }
+        if (i + u + U < np) fetch(i + u + U, b[u]);
+      }
+    }
   }
-  __device__ float quantise(const MTile &t, int r, int pt, int lane, int8_t *dst) const {
-    const float *hr = h + int64_t(t.p0 + r) * dff;
-    return wave_row([&](int c, float *v) { row8<float, true>(hr, c, dff, v); }, pt, lane, dst);
+  if (wave > 0) part[wave - 1][lane] = acc;
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int s = 0; s < KS - 1; ++s) acc += part[s][lane];
+  int q = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = 4 * (lane >> 4) + i;
+    if (r < t.mvalid) {
+      while (r >= gp[q + 1]) ++q;
+      ys[r][l15] = dequant(acc[i], srow[r], sd[int64_t(ge[q] - 1) * d + n0 + l15]);
+    }
   }
-  __device__ void store(const MTile &t, int r, int c, int32_t v, float sr) const {
-    const int col = t.n0 + c;
-    Y[int64_t(t.p0 + r) * d + col] = dequant(v, sr, sd[int64_t(t.e - 1) * d + col]);
+  // (one wave: its LDS writes are ahead of its reads)
+  __builtin_amdgcn_wave_barrier();
+  for (int tok = lane >> 4; tok < N; tok += 4) {
+    float y = 0.f;
+    bool any = false;
+    for (int s = 0; s < k; ++s) {
+      const int at = tok * k + s;
+      if (eidx[at] == 0) continue;
+      y = fmaf(egate[at], ys[slot_of[at]][l15], y);
+      any = true;
+    }
+    const int64_t o = int64_t(tok) * d + n0 + l15;
+    const float x = Act<T>::ld(xt, o);
+    put1(xout + o, any ? x + y : x);
   }
-};
+}
 
 // ------------------------------------------------------------------ launchers
 template <class P>
@@ -274,18 +411,19 @@ static hipError_t launch_few(const P &p, int rows, int pitch, int tiles, int ny,
   return hipGetLastError();
 }
 
-static bool few_fit(int rows, int cols) {
+bool i8_few_fit(int rows, int cols) {
   return rows <= FEW_ROWS && int64_t(rows) * i8_pitch(cols) <= FEW_PANEL;
 }
-bool i8_few_rows(int N, int cols) { return few_fit(N, cols); }
-bool i8_few_moe(const triroute_cfg &cfg, int N) {
-  return N * cfg.top_k <= FEW_ROWS && few_fit(N * cfg.top_k, std::max(cfg.d_model, cfg.d_ff));
+bool i8_few_fit_moe(const triroute_cfg &cfg, int N) {
+  return N <= FEW_ROWS && i8_few_fit(N * cfg.top_k, std::max(cfg.d_model, cfg.d_ff));
 }
 
 template <typename T>
-static RowsIn<T> rows_in(const void *x, int64_t ldx, int cols) {
-  return RowsIn<T>{(const T *)x, ldx, cols,
-                   cols % 8 == 0 && ((uintptr_t(x) | uintptr_t(ldx * int64_t(sizeof(T)))) & 15) == 0};
+static void rows_in(RowsIn<T> &p, const void *x, int64_t ldx, int cols) {
+  p.x = (const T *)x;
+  p.ldx = ldx;
+  p.cols = cols;
+  p.vec = cols % 8 == 0 && ((uintptr_t(x) | uintptr_t(ldx * int64_t(sizeof(T)))) & 15) == 0;
 }
 
 hipError_t i8_few_linear(int act, int N, int m, int k, const void *x, int64_t ldx, const triroute_i8_w &w,
@@ -293,7 +431,7 @@ hipError_t i8_few_linear(int act, int N, int m, int k, const void *x, int64_t ld
   auto run = [&](auto tag) {
     using T = decltype(tag);
     FewLinear<T> p;
-    p.in = rows_in<T>(x, ldx, k);
+    rows_in<T>(p, x, ldx, k);
     p.w = (const int8_t *)w.codes;
     p.sw = w.scale;
     p.y = (T *)y;
@@ -313,7 +451,7 @@ hipError_t i8_few_qkv(const triroute_cfg &cfg, int N, const void *n1, const trir
   auto run = [&](auto tag) {
     using T = decltype(tag);
     FewQkv<T> p;
-    p.in = rows_in<T>(n1, cfg.d_model, cfg.d_model);
+    rows_in<T>(p, n1, cfg.d_model, cfg.d_model);
     p.Wq = (const int8_t *)w.Wq.codes;
     p.Wk = (const int8_t *)w.Wk.codes;
     p.Wv = (const int8_t *)w.Wv.codes;
@@ -335,11 +473,11 @@ hipError_t i8_few_qkv(const triroute_cfg &cfg, int N, const void *n1, const trir
   return cfg.act == TRIROUTE_BF16 ? run(bf16{}) : run(float{});
 }
 
-hipError_t i8_few_moe_products(const triroute_cfg &cfg, int N, const void *xt, const void *g2,
-                               const triroute_moe_i8_w &w, const triroute_compaction &c,
-                               const MoeI8Ws &ws, hipStream_t st) {
-  const int Nk = N * cfg.top_k, E = cfg.n_experts, tiles = std::min(E, Nk);
-  auto up = [&](auto tag) {
+hipError_t i8_few_moe(const triroute_cfg &cfg, int N, const void *xt, const void *g2,
+                      const triroute_moe_i8_w &w, const triroute_compaction &c, const int32_t *eidx,
+                      const float *egate, void *x_out, const MoeI8Ws &ws, hipStream_t st) {
+  const int Nk = N * cfg.top_k, E = cfg.n_experts, d = cfg.d_model, dff = cfg.d_ff;
+  auto run = [&](auto tag) {
     using T = decltype(tag);
     FewUp<T> p;
     p.x = (const T *)xt;
@@ -354,25 +492,19 @@ hipError_t i8_few_moe_products(const triroute_cfg &cfg, int N, const void *xt, c
     p.h = ws.h;
     p.E = E;
     p.k = cfg.top_k;
-    p.d = cfg.d_model;
-    p.dff = cfg.d_ff;
-    p.pitch = i8_pitch(cfg.d_model);
+    p.d = d;
+    p.dff = dff;
+    p.pitch = i8_pitch(d);
     p.eps = cfg.rms_eps;
-    return launch_few(p, Nk, p.pitch, tiles, cfg.d_ff / 16, st);
+    const hipError_t e = launch_few(p, Nk, p.pitch, std::min(E, Nk), dff / 16, st);
+    if (e != hipSuccess) return e;
+    const int pitch = i8_pitch(dff);
+    i8_few_down_kernel<T, 8><<<d / 16, 512, size_t(Nk) * (pitch + FEW_PAD), st>>>(
+        ws.h, c.exp_cnt, (const int8_t *)w.Wdown.codes, w.Wdown.scale, ws.slot_of, eidx, egate,
+        (const T *)xt, (T *)x_out, N, cfg.top_k, E, d, dff, pitch);
+    return hipGetLastError();
   };
-  const hipError_t e = cfg.act == TRIROUTE_BF16 ? up(bf16{}) : up(float{});
-  if (e != hipSuccess) return e;
-  FewDown p;
-  p.h = ws.h;
-  p.cnt = c.exp_cnt;
-  p.Wd = (const int8_t *)w.Wdown.codes;
-  p.sd = w.Wdown.scale;
-  p.Y = ws.Y;
-  p.E = E;
-  p.d = cfg.d_model;
-  p.dff = cfg.d_ff;
-  p.pitch = i8_pitch(cfg.d_ff);
-  return launch_few(p, Nk, p.pitch, tiles, cfg.d_model / 16, st);
+  return cfg.act == TRIROUTE_BF16 ? run(bf16{}) : run(float{});
 }
 
 }  // namespace tr

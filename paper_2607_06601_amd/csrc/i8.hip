@@ -142,7 +142,9 @@ __global__ __launch_bounds__(256) void i8_norm_kernel(
   uint32_t m = 0;
   auto normed = [&](int c, float *w) {
     if (c >= d) return;
-    norm8<T>(g + c, r, w);
+    float gv[8];
+    load8(g + c, gv);
+    norm8<T>(gv, r, w);
 #pragma unroll
     for (int j = 0; j < 8; ++j) m = max(m, abs_bits(w[j]));
   };

@@ -103,11 +103,9 @@ __device__ __forceinline__ void row8(const T *row, int c, int cols, float *v) {
   }
 }
 
-// v *= g / norm for 8 elements, in fp64 and rounded once to fp32 (r: the row's 1 / norm).
+// v *= g / norm for 8 elements of type T, in fp64 and rounded once to fp32 (r: the row's 1 / norm).
 template <typename T>
-__device__ __forceinline__ void norm8(const T *g, double r, float *v) {
-  float gv[8];
-  load8(g, gv);
+__device__ __forceinline__ void norm8(const float *gv, double r, float *v) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     if constexpr (sizeof(T) == 2)  // (the product of two bf16 numbers is an fp32 number)

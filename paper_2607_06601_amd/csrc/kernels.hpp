@@ -176,18 +176,18 @@ inline int i8_pitch(int cols) { return (cols + 127) / 128 * 128; }  // bytes of 
 hipError_t launch_i8_rows(int act, int64_t rows, int cols, const void *x, int64_t ldx, int8_t *codes,
                           float *scale, hipStream_t st);
 // gemm_i8_few.hip: rows quantised in the product's own launch, for up to 16 of them
-bool i8_few_rows(int N, int cols);
-bool i8_few_moe(const triroute_cfg &cfg, int N);
+bool i8_few_fit(int N, int cols);
+bool i8_few_fit_moe(const triroute_cfg &cfg, int N);
 hipError_t i8_few_linear(int act, int N, int m, int k, const void *x, int64_t ldx, const triroute_i8_w &w,
                          const void *res, int64_t ldr, void *y, int64_t ldy, hipStream_t st);
 // rope: the rotation table, or NULL and job
 hipError_t i8_few_qkv(const triroute_cfg &cfg, int N, const void *n1, const triroute_dense_i8_w &w,
                       const RopeJob *job, const float *rope, void *q, void *k, void *v, hipStream_t st);
 struct MoeI8Ws;
-// from xt to ws.Y and ws.slot_of
-hipError_t i8_few_moe_products(const triroute_cfg &cfg, int N, const void *xt, const void *g2,
-                               const triroute_moe_i8_w &w, const triroute_compaction &c,
-                               const MoeI8Ws &ws, hipStream_t st);
+// the whole block: xt to x_out
+hipError_t i8_few_moe(const triroute_cfg &cfg, int N, const void *xt, const void *g2,
+                      const triroute_moe_i8_w &w, const triroute_compaction &c, const int32_t *eidx,
+                      const float *egate, void *x_out, const MoeI8Ws &ws, hipStream_t st);
 hipError_t i8_linear(int act, int N, int m, int k, const int8_t *a, const float *sa,
                      const triroute_i8_w &w, const void *res, int64_t ldr, void *y, int64_t ldy,
                      hipStream_t st);
