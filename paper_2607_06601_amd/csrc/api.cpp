@@ -1214,13 +1214,12 @@ static int moe_impl(const triroute_cfg *cfg, int n_tok, const void *xt, const tr
                     const triroute_compaction *cmp, void *x_out, Carve &cv, hipStream_t st) {
   const tr::MoeI8Ws m = carve_moe_i8(cv, *cfg, n_tok);
   if (tr::i8_few_fit_moe(*cfg, n_tok)) {
-    CHECK_HIP(tr::i8_few_moe(*cfg, n_tok, xt, dw->g2, *w, *cmp, eidx, egate, x_out, m, st),
-              "moe_i8 launch");
-    return TRIROUTE_OK;
+    CHECK_HIP(tr::i8_few_moe(*cfg, n_tok, xt, dw->g2, *w, *cmp, m, st), "moe_i8 product launch");
+  } else {
+    CHECK_HIP(tr::launch_i8_norm(*cfg, n_tok, xt, dw->g2, *cmp, eidx, m.n2, m.s_n2, m.slot_of, st),
+              "moe_i8 norm launch");
+    CHECK_HIP(tr::i8_moe(*cfg, n_tok, *w, *cmp, m, st), "moe_i8 product launch");
   }
-  CHECK_HIP(tr::launch_i8_norm(*cfg, n_tok, xt, dw->g2, *cmp, eidx, m.n2, m.s_n2, m.slot_of, st),
-            "moe_i8 norm launch");
-  CHECK_HIP(tr::i8_moe(*cfg, n_tok, *w, *cmp, m, st), "moe_i8 product launch");
   CHECK_HIP(tr::launch_moe_combine(*cfg, n_tok, xt, m.Y, 1, m.slot_of, eidx, egate, x_out, st),
             "combine launch");
   return TRIROUTE_OK;

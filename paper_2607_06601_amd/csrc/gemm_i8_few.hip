@@ -2,7 +2,7 @@
 // in the same launch: single tokens and small decode batches, where a launch costs more
 // than the bytes it moves.
 //
-// A block makes 16 columns (16 pairs of columns for rotation and gate/up) of one 16-row MFMA
+// A block makes groups of 16 columns (16 pairs of columns for rotation and gate/up) of one 16-row MFMA
 // tile.  Its waves share K by 128-byte pieces: each loads its pieces of the weights' rows
 // straight into fragments (a fragment feeds one MFMA, so LDS would be a detour) and adds
 // their products; the waves' sums are added in LDS (whole numbers: any order).  The rows' codes
@@ -106,7 +106,9 @@ __device__ __forceinline__ void tile_rows(const P &p, const MTile &t, int pitch,
   __syncthreads();
 }
 
-// KS waves; a wave's first U pieces are asked for ahead of the quantisation.
+// KS waves.  Block (x, y) makes tile x's column groups y, y + gridDim.y, ... of ny: the rows are
+// quantised once for all of them.  A wave's first U pieces of a group are asked for ahead of the
+// quantisation, or of the sums of the group before.
 template <class P, int KS>
 __global__ __launch_bounds__(64 * KS) void i8_few_kernel(P p, int pitch, int ny) {
   constexpr int CT = P::CT;
@@ -117,14 +119,18 @@ __global__ __launch_bounds__(64 * KS) void i8_few_kernel(P p, int pitch, int ny)
   GroupScan gs;
   if constexpr (P::GROUPED) gs = group_scan(FEW_ROWS, p.cnt, p.E);
   MTile t;
-  if (!p.map(blockIdx.x / ny, blockIdx.x % ny, FEW_ROWS, 16, t, gs)) return;
+  if (!p.map(blockIdx.x, FEW_ROWS, t, gs)) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int l15 = lane & 15, kb = 16 * (lane >> 4);
+  auto group = [&](int by) {  // its first column
+    if constexpr (P::CT == 2 && !P::GROUPED)
+      return p.first_col(by);
+    else
+      return by * 16;
+  };
   // piece i of this wave: bytes 128 (wave + KS i) .. of a row, two fragments
   const int np = (pitch / 128 - wave + KS - 1) / KS;
   const int8_t *w[CT];
-#pragma unroll
-  for (int c = 0; c < CT; ++c) w[c] = p.col_row(t, c, l15) + 128 * wave + kb;
   i32x4_t b[U][CT][2];
   auto fetch = [&](int i, i32x4_t (&f)[CT][2]) {
 #pragma unroll
@@ -132,48 +138,62 @@ __global__ __launch_bounds__(64 * KS) void i8_few_kernel(P p, int pitch, int ny)
 #pragma unroll
       for (int h = 0; h < 2; ++h) f[c][h] = *(const i32x4_t *)(w[c] + int64_t(i) * (128 * KS) + 64 * h);
   };
+  auto start = [&](int by) {
+    t.n0 = group(by);
 #pragma unroll
-  for (int u = 0; u < U; ++u)
-    if (u < np) fetch(u, b[u]);
+    for (int c = 0; c < CT; ++c) w[c] = p.col_row(t, c, l15) + 128 * wave + kb;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (u < np) fetch(u, b[u]);
+  };
+  start(blockIdx.y);
   tile_rows<P, KS>(p, t, pitch, panel, srow);
-  i32x4_t acc[CT];
-#pragma unroll
-  for (int c = 0; c < CT; ++c) acc[c] = i32x4_t{0, 0, 0, 0};
   // (rows past the valid ones read row 0: their sums are not stored)
   const int8_t *a = panel + (l15 < t.mvalid ? l15 : 0) * (pitch + FEW_PAD) + 128 * wave + kb;
-  for (int i = 0; i < np; i += U) {
+  for (int by = blockIdx.y; by < ny; by += gridDim.y) {
+    i32x4_t acc[CT];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (i + u < np) {
+    for (int c = 0; c < CT; ++c) acc[c] = i32x4_t{0, 0, 0, 0};
+    for (int i = 0; i < np; i += U) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const i32x4_t af = *(const i32x4_t *)(a + (i + u) * (128 * KS) + 64 * h);
+      for (int u = 0; u < U; ++u) {
+        if (i + u < np) {
 #pragma unroll
-          for (int c = 0; c < CT; ++c) acc[c] = OpI8::mma(af, b[u][c][h], acc[c]);
+          for (int h = 0; h < 2; ++h) {
+            const i32x4_t af = *(const i32x4_t *)(a + (i + u) * (128 * KS) + 64 * h);
+#pragma unroll
+            for (int c = 0; c < CT; ++c) acc[c] = OpI8::mma(af, b[u][c][h], acc[c]);
+          }
+          if (i + u + U < np) fetch(i + u + U, b[u]);
         }
-        if (i + u + U < np) fetch(i + u + U, b[u]);
       }
     }
-  }
-  if (wave > 0) {
+    const int n0 = t.n0;
+    if (by + gridDim.y < ny) start(by + gridDim.y);
+    if (by != blockIdx.y) __syncthreads();  // the group before has been read from part
+    if (wave > 0) {
 #pragma unroll
-    for (int c = 0; c < CT; ++c) part[wave - 1][c][lane] = acc[c];
-  }
-  __syncthreads();
-  if (wave > 0) return;
+      for (int c = 0; c < CT; ++c) part[wave - 1][c][lane] = acc[c];
+    }
+    __syncthreads();
+    if (wave == 0) {
 #pragma unroll
-  for (int k = 0; k < KS - 1; ++k)
+      for (int k = 0; k < KS - 1; ++k)
 #pragma unroll
-    for (int c = 0; c < CT; ++c) acc[c] += part[k][c][lane];
-  // lane: rows 4 (lane / 16) + i, column (pair) lane % 16
+        for (int c = 0; c < CT; ++c) acc[c] += part[k][c][lane];
+      MTile o = t;
+      o.n0 = n0;
+      // lane: rows 4 (lane / 16) + i, column (pair) lane % 16
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = 4 * (lane >> 4) + i;
-    if (r < t.mvalid) {
-      if constexpr (CT == 2)
-        p.store(t, r, l15, acc[0][i], acc[1][i], srow[r]);
-      else
-        p.store(t, r, l15, acc[0][i], srow[r]);
+      for (int i = 0; i < 4; ++i) {
+        const int r = 4 * (lane >> 4) + i;
+        if (r < t.mvalid) {
+          if constexpr (CT == 2)
+            p.store(o, r, l15, acc[0][i], acc[1][i], srow[r]);
+          else
+            p.store(o, r, l15, acc[0][i], srow[r]);
+        }
+      }
     }
   }
 }
@@ -206,9 +226,8 @@ struct FewLinear : RowsIn<T> {
   const T *res;
   int64_t ldy, ldr;
   int N, m, pitch;
-  __device__ bool map(int, int by, int, int, MTile &t, const GroupScan &) const {
+  __device__ bool map(int, int, MTile &t, const GroupScan &) const {
     t.m0 = t.e = t.p0 = 0;
-    t.n0 = by * 16;
     t.mvalid = N;
     return true;
   }
@@ -233,13 +252,15 @@ struct FewQkv : RowsIn<T> {
   const float2 *rope;  // the rotation table, or NULL: entries are made here
   RopeJob job;
   int N, Hd, Kd, dh, pitch;
-  __device__ bool map(int, int by, int, int, MTile &t, const GroupScan &) const {
+  __device__ bool map(int, int, MTile &t, const GroupScan &) const {
     t.m0 = t.e = t.p0 = 0;
-    // 16 pairs j0 .. of one head: by counts them over the heads of q, k, v
-    const int per = dh / 32;
-    t.n0 = (by / per) * dh + (by % per) * 16;
     t.mvalid = N;
     return true;
+  }
+  // first column of 16 pairs of one head: by counts them over the heads of q, k, v
+  __device__ int first_col(int by) const {
+    const int per = dh / 32;
+    return (by / per) * dh + (by % per) * 16;
   }
   // matrix and column within it of half `half` of pair c of the tile
   __device__ int at(const MTile &t, int half, int c, int &which) const {
@@ -282,8 +303,7 @@ struct FewUp {
   float *h;
   int E, k, d, dff, pitch;
   float eps;
-  __device__ bool map(int bx, int by, int BM, int, MTile &t, const GroupScan &gs) const {
-    t.n0 = by * 16;
+  __device__ bool map(int bx, int BM, MTile &t, const GroupScan &gs) const {
     return mmap_grouped(bx, BM, gs, t);
   }
   __device__ const int8_t *col_row(const MTile &t, int half, int c) const {
@@ -293,7 +313,7 @@ struct FewUp {
   static constexpr bool NORM = true;
   __device__ const T *row(const MTile &t, int r) const {
     const int a = rows[t.p0 + r];
-    if (t.n0 == 0 && (threadIdx.x & 63) == 0) slot_of[a] = t.p0 + r;
+    if (blockIdx.y == 0 && (threadIdx.x & 63) == 0) slot_of[a] = t.p0 + r;
     return x + int64_t(a / k) * d;
   }
   __device__ void load(const T *row, int c, float *v) const { row8<T, true>(row, c, d, v); }
@@ -306,116 +326,59 @@ struct FewUp {
   }
 };
 
-// Down products of every list row and the sum over a token's slots, x_out = xt + sum gate Y.  A
-// block makes 16 columns of all rows (at most 16): the pieces of the weights of every expert
-// in use are shared by its waves, and with an expert's piece the rows of other experts are
-// zeros, so one accumulator takes them all.  Slots are added in slot order, as moe_combine
-// does.
-template <typename T, int KS>
-__global__ __launch_bounds__(64 * KS) void i8_few_down_kernel(
-    const float *__restrict__ h, const int32_t *__restrict__ cnt, const int8_t *__restrict__ Wd,
-    const float *__restrict__ sd, const int32_t *__restrict__ slot_of,
-    const int32_t *__restrict__ eidx, const float *__restrict__ egate, const T *xt, T *xout, int N,
-    int k, int E, int d, int dff, int pitch) {
-  constexpr int U = 4;
-  extern __shared__ __align__(16) int8_t panel[];
-  __shared__ i32x4_t part[KS - 1][64];
-  __shared__ float srow[FEW_ROWS], ys[FEW_ROWS][17];
-  __shared__ int ge[FEW_ROWS], gp[FEW_ROWS + 1];  // the experts in use, and their first rows
-  const GroupScan gs = group_scan(FEW_ROWS, cnt, E);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int l15 = lane & 15, kb = 16 * (lane >> 4), n0 = blockIdx.x * 16;
-  const int groups = gs.total;  // one tile an expert in use: it has 16 rows at most
-  if (wave == 0 && gs.nt) {
-    ge[gs.incl - 1] = lane + 1;
-    gp[gs.incl - 1] = gs.start;
-    if (gs.incl == groups) gp[groups] = gs.start + gs.c;
+// Down product of list rows, from h.
+struct FewDown {
+  typedef float elem;
+  static constexpr bool NORM = false;
+  static constexpr int CT = 1;
+  static constexpr bool GROUPED = true;
+  const float *h;
+  const int32_t *cnt;
+  const int8_t *Wd;
+  const float *sd;
+  float *Y;
+  int E, d, dff, pitch;
+  __device__ bool map(int bx, int BM, MTile &t, const GroupScan &gs) const {
+    return mmap_grouped(bx, BM, gs, t);
   }
-  if (groups == 0 && threadIdx.x == 0) gp[0] = 0;
-  __syncthreads();
-  const int per = pitch / 128, all = groups * per;
-  const int np = (all - wave + KS - 1) / KS;
-  const int8_t *w = Wd + int64_t(n0 + l15) * pitch + kb;
-  i32x4_t b[U][2];
-  auto fetch = [&](int i, i32x4_t (&f)[2]) {
-    const int piece = wave + KS * i, q = piece / per;
-    const int8_t *src = w + int64_t(ge[q] - 1) * d * pitch + (piece - q * per) * 128;
-#pragma unroll
-    for (int hh = 0; hh < 2; ++hh) f[hh] = *(const i32x4_t *)(src + 64 * hh);
-  };
-#pragma unroll
-  for (int u = 0; u < U; ++u)
-    if (u < np) fetch(u, b[u]);
-  MTile t;
-  t.mvalid = gp[groups];
-  RowsIn<float> rows{h, dff, dff, true};
-  tile_rows<RowsIn<float>, KS>(rows, t, pitch, panel, srow);
-  i32x4_t acc = {0, 0, 0, 0};
-  const int8_t *a = panel + (l15 < t.mvalid ? l15 : 0) * (pitch + FEW_PAD) + kb;
-  for (int i = 0; i < np; i += U) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (i + u < np) {
-        const int piece = wave + KS * (i + u), q = piece / per;
-        const bool mine = l15 >= gp[q] && l15 < gp[q + 1];
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-          i32x4_t af = *(const i32x4_t *)(a + (piece - q * per) * 128 + 64 * hh);
-          if (!mine) af = i32x4_t{0, 0, 0, 0};
-          acc = OpI8::mma(af, b[u][hh], acc);
-        }
-        if (i + u + U < np) fetch(i + u + U, b[u]);
-      }
-    }
+  __device__ const int8_t *col_row(const MTile &t, int, int c) const {
+    return Wd + (int64_t(t.e - 1) * d + t.n0 + c) * pitch;
   }
-  if (wave > 0) part[wave - 1][lane] = acc;
-  __syncthreads();
-  if (wave > 0) return;
-#pragma unroll
-  for (int s = 0; s < KS - 1; ++s) acc += part[s][lane];
-  int q = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = 4 * (lane >> 4) + i;
-    if (r < t.mvalid) {
-      while (r >= gp[q + 1]) ++q;
-      ys[r][l15] = dequant(acc[i], srow[r], sd[int64_t(ge[q] - 1) * d + n0 + l15]);
-    }
+  __device__ const float *row(const MTile &t, int r) const { return h + int64_t(t.p0 + r) * dff; }
+  __device__ void load(const float *row, int c, float *v) const { row8<float, true>(row, c, dff, v); }
+  __device__ void store(const MTile &t, int r, int c, int32_t v, float sr) const {
+    const int col = t.n0 + c;
+    Y[int64_t(t.p0 + r) * d + col] = dequant(v, sr, sd[int64_t(t.e - 1) * d + col]);
   }
-  // (one wave: its LDS writes are ahead of its reads)
-  __builtin_amdgcn_wave_barrier();
-  for (int tok = lane >> 4; tok < N; tok += 4) {
-    float y = 0.f;
-    bool any = false;
-    for (int s = 0; s < k; ++s) {
-      const int at = tok * k + s;
-      if (eidx[at] == 0) continue;
-      y = fmaf(egate[at], ys[slot_of[at]][l15], y);
-      any = true;
-    }
-    const int64_t o = int64_t(tok) * d + n0 + l15;
-    const float x = Act<T>::ld(xt, o);
-    put1(xout + o, any ? x + y : x);
-  }
-}
+};
 
 // ------------------------------------------------------------------ launchers
+// About two blocks a CU, one where the rows' quantisation is long (the norm; 1.3B gate/up, 1
+// token: 13.8 us, two blocks 16.8, three 19.7).
 template <class P>
 static hipError_t launch_few(const P &p, int rows, int pitch, int tiles, int ny, hipStream_t st) {
   const size_t lds = size_t(rows) * (pitch + FEW_PAD);
-  // eight waves where K has as many pieces
-  if (pitch >= 8 * 128)
-    i8_few_kernel<P, 8><<<tiles * ny, 512, lds, st>>>(p, pitch, ny);
+  const int blocks = cu_count() * (P::NORM ? 1 : 2);
+  const dim3 grid(tiles, std::max(1, std::min(ny, blocks / tiles)));
+  // eight waves where K has as many pieces, or there are rows for them
+  if (pitch >= 8 * 128 || rows > 4)
+    i8_few_kernel<P, 8><<<grid, 512, lds, st>>>(p, pitch, ny);
   else
-    i8_few_kernel<P, 4><<<tiles * ny, 256, lds, st>>>(p, pitch, ny);
+    i8_few_kernel<P, 4><<<grid, 256, lds, st>>>(p, pitch, ny);
   return hipGetLastError();
 }
 
+// Rows that gain by it (us, GPU, against the pass over the rows and the product in launches of their own):
+// 768 -> 768, 1 token 3.6 / 7.1, 16 tokens 5.9 / 7.6; 2048 -> 2048, 1 token 4.0 / 10.4, 16 tokens 9.0 /
+// 10.4; QKV 410M, 1 token 5.0 / 14.9, 16 tokens 9.0 / 15.1.
 bool i8_few_fit(int rows, int cols) {
   return rows <= FEW_ROWS && int64_t(rows) * i8_pitch(cols) <= FEW_PANEL;
 }
+// Experts: up to four assignments (160M, 1 token 14.6 / 23.7 us, 2 tokens 17.0 / 24.6; 1.3B, 1 token 26 /
+// 35, 2 tokens 42 / 45, 3 tokens 57 / 54): with more experts in use their blocks are many, and each
+// normalises its rows again.
 bool i8_few_fit_moe(const triroute_cfg &cfg, int N) {
-  return N <= FEW_ROWS && i8_few_fit(N * cfg.top_k, std::max(cfg.d_model, cfg.d_ff));
+  return N * cfg.top_k <= 4 && i8_few_fit(N * cfg.top_k, std::max(cfg.d_model, cfg.d_ff));
 }
 
 template <typename T>
@@ -474,8 +437,8 @@ hipError_t i8_few_qkv(const triroute_cfg &cfg, int N, const void *n1, const trir
 }
 
 hipError_t i8_few_moe(const triroute_cfg &cfg, int N, const void *xt, const void *g2,
-                      const triroute_moe_i8_w &w, const triroute_compaction &c, const int32_t *eidx,
-                      const float *egate, void *x_out, const MoeI8Ws &ws, hipStream_t st) {
+                      const triroute_moe_i8_w &w, const triroute_compaction &c, const MoeI8Ws &ws,
+                      hipStream_t st) {
   const int Nk = N * cfg.top_k, E = cfg.n_experts, d = cfg.d_model, dff = cfg.d_ff;
   auto run = [&](auto tag) {
     using T = decltype(tag);
@@ -498,11 +461,17 @@ hipError_t i8_few_moe(const triroute_cfg &cfg, int N, const void *xt, const void
     p.eps = cfg.rms_eps;
     const hipError_t e = launch_few(p, Nk, p.pitch, std::min(E, Nk), dff / 16, st);
     if (e != hipSuccess) return e;
-    const int pitch = i8_pitch(dff);
-    i8_few_down_kernel<T, 8><<<d / 16, 512, size_t(Nk) * (pitch + FEW_PAD), st>>>(
-        ws.h, c.exp_cnt, (const int8_t *)w.Wdown.codes, w.Wdown.scale, ws.slot_of, eidx, egate,
-        (const T *)xt, (T *)x_out, N, cfg.top_k, E, d, dff, pitch);
-    return hipGetLastError();
+    FewDown q;
+    q.h = ws.h;
+    q.cnt = c.exp_cnt;
+    q.Wd = (const int8_t *)w.Wdown.codes;
+    q.sd = w.Wdown.scale;
+    q.Y = ws.Y;
+    q.E = E;
+    q.d = d;
+    q.dff = dff;
+    q.pitch = i8_pitch(dff);
+    return launch_few(q, Nk, q.pitch, std::min(E, Nk), d / 16, st);
   };
   return cfg.act == TRIROUTE_BF16 ? run(bf16{}) : run(float{});
 }

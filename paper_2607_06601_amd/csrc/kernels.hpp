@@ -184,10 +184,10 @@ hipError_t i8_few_linear(int act, int N, int m, int k, const void *x, int64_t ld
 hipError_t i8_few_qkv(const triroute_cfg &cfg, int N, const void *n1, const triroute_dense_i8_w &w,
                       const RopeJob *job, const float *rope, void *q, void *k, void *v, hipStream_t st);
 struct MoeI8Ws;
-// the whole block: xt to x_out
+// from xt to ws.Y and ws.slot_of
 hipError_t i8_few_moe(const triroute_cfg &cfg, int N, const void *xt, const void *g2,
-                      const triroute_moe_i8_w &w, const triroute_compaction &c, const int32_t *eidx,
-                      const float *egate, void *x_out, const MoeI8Ws &ws, hipStream_t st);
+                      const triroute_moe_i8_w &w, const triroute_compaction &c, const MoeI8Ws &ws,
+                      hipStream_t st);
 hipError_t i8_linear(int act, int N, int m, int k, const int8_t *a, const float *sa,
                      const triroute_i8_w &w, const void *res, int64_t ldr, void *y, int64_t ldy,
                      hipStream_t st);
