@@ -1135,8 +1135,9 @@ static hipError_t run_qkv_i8(const triroute_cfg &c, int N, const void *n1, const
                              void *k, void *v, hipStream_t st) {
   if (tr::i8_few_fit(N, c.d_model))
     return tr::i8_few_qkv(c, N, n1, w, made ? nullptr : &job, made ? rope : nullptr, q, k, v, st);
-  hipError_t e = made ? hipSuccess : tr::launch_rope_table(N, job, st);
-  if (e == hipSuccess) e = tr::launch_i8_rows(c.act, N, c.d_model, n1, c.d_model, rows.codes, rows.scale, st);
+  const hipError_t e =
+      made ? tr::launch_i8_rows(c.act, N, c.d_model, n1, c.d_model, rows.codes, rows.scale, st)
+           : tr::launch_i8_rows_rope(c.act, N, c.d_model, n1, rows.codes, rows.scale, job, st);
   return e != hipSuccess ? e : tr::i8_qkv(c, N, rows.codes, rows.scale, w, rope, q, k, v, st);
 }
 

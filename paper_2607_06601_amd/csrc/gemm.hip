@@ -380,21 +380,15 @@ static hipError_t qkv_f32(const triroute_cfg &cfg, int B, int Tq, const void *n1
   return hipGetLastError();
 }
 
-hipError_t launch_rope_table(int N, const RopeJob &r, hipStream_t st) {
-  const int64_t n = int64_t(N) * r.hd;
-  rope_table_kernel<<<dim3(unsigned((n + 255) / 256)), 256, 0, st>>>(N, r);
-  return hipGetLastError();
-}
-
 hipError_t launch_qkv(const triroute_cfg &cfg, int B, int Tq, const void *n1,
                       const triroute_dense_w &w, const int32_t *pos_base, const int32_t *pos_idx,
                       int n_base, void *q, void *k, void *v, float *rope, bool rope_ready,
                       hipStream_t st) {
   const int N = B * Tq;
   if (!rope_ready) {
-    const hipError_t e =
-        launch_rope_table(N, make_rope_job(cfg, Tq, pos_base, pos_idx, n_base, rope), st);
-    if (e != hipSuccess) return e;
+    const RopeJob r = make_rope_job(cfg, Tq, pos_base, pos_idx, n_base, rope);
+    const int64_t n = int64_t(N) * r.hd;
+    rope_table_kernel<<<dim3(unsigned((n + 255) / 256)), 256, 0, st>>>(N, r);
   }
   return cfg.act == TRIROUTE_BF16 ? mfma_qkv(cfg, B, Tq, n1, w, rope, q, k, v, st)
                                   : qkv_f32(cfg, B, Tq, n1, w, rope, q, k, v, st);

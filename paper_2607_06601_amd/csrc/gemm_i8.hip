@@ -683,10 +683,17 @@ hipError_t i8_qkv(const triroute_cfg &cfg, int N, const int8_t *a, const float *
              span32({{p.Wq, size_t(p.Hd) * p.pitch}}, &lo) &&
              w4_rounds(p.N, c128, tile_cost(m256 * c256, COST_256X256));
       if (few_tiles(p.N, c128)) {
-        if (p.dh == 64)
-          e = launch<QkvI8<T>, 32, 64, 2, 1, 64, 4>(p, K2, (p.N + 31) / 32, c64, st);
+        // (two K groups: whole numbers, so a token's keys stay the same in every tile; QKV 410M, 64
+        // tokens 7.3 -> 6.4 us)
+        const int m32 = (p.N + 31) / 32;
+        if (p.dh == 64 && split_k(m32 * c64, K2))
+          e = launch<QkvI8<T>, 32, 64, 2, 1, 64, 4, 2>(p, K2, m32, c64, st);
+        else if (p.dh == 64)
+          e = launch<QkvI8<T>, 32, 64, 2, 1, 64, 4>(p, K2, m32, c64, st);
+        else if (split_k(m32 * c64 / 2, K2))
+          e = launch<QkvI8<T>, 32, 128, 2, 2, 64, 3, 2>(p, K2, m32, c64 / 2, st);
         else
-          e = launch<QkvI8<T>, 32, 128, 2, 2, 64, 4>(p, K2, (p.N + 31) / 32, c64 / 2, st);
+          e = launch<QkvI8<T>, 32, 128, 2, 2, 64, 4>(p, K2, m32, c64 / 2, st);
       } else if (!w4) {
         e = launch_mid(p, K2, p.N, c128, st);
       } else if constexpr (std::is_same<T, bf16>::value) {
@@ -733,9 +740,10 @@ hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
     const int c64 = (dff + 63) / 64;
     // Gate/up: as the bf16 product's rule (times of the two kernels measured alike), but 32-row tiles
     // with two K groups where they leave CUs without a tile (160M, 1 token: 5.6 -> 5.1 us).
-    if (r <= 24 && split_k(row_tiles(32) * ((dff + 31) / 32), K2)) {
+    const bool small = r <= 24 || (decltype(f64)::value && row_tiles(32) * ((dff + 31) / 32) <= 4 * cu_count());
+    if (small && split_k(row_tiles(32) * ((dff + 31) / 32), K2)) {
       e = launch<P, 32, 64, 2, 1, 64, 4, 2>(p, K2, Nk / 32 + E, (dff + 31) / 32, st);
-    } else if (r <= 24) {
+    } else if (small) {
       e = launch<P, 32, 64, 2, 1, 64, 4>(p, K2, Nk / 32 + E, (dff + 31) / 32, st);
     } else if (r <= 64) {
       e = launch<P, 64, 128, 2, 2, 64, 3>(p, K2, Nk / 64 + E, c64, st);

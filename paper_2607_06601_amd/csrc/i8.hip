@@ -9,17 +9,16 @@ namespace tr {
 // RR accesses of a lane stay in registers between the maximum and the codes, later ones are
 // read again.
 template <typename T, bool VEC, int W, int RR>
-__global__ __launch_bounds__(256) void i8_rows_kernel(const T *__restrict__ x, int64_t ldx,
-                                                      int64_t rows,
-                                                      const int32_t *__restrict__ d_rows, int cols,
-                                                      int pitch, int8_t *__restrict__ codes,
-                                                      float *__restrict__ scale) {
+__device__ __forceinline__ void rows_body(const T *__restrict__ x, int64_t ldx, int64_t rows,
+                                          const int32_t *__restrict__ d_rows, int cols, int pitch,
+                                          int8_t *__restrict__ codes, float *__restrict__ scale,
+                                          int64_t blocks) {
   if (d_rows) rows = min(rows, int64_t(*d_rows));
   constexpr int STEP = 512 * W;
   __shared__ uint32_t part[4];
   const int wave = threadIdx.x >> 6;
   const int at = (W == 4 ? threadIdx.x : threadIdx.x & 63) * 8;
-  for (int64_t row0 = int64_t(blockIdx.x) * (4 / W); row0 < rows; row0 += int64_t(gridDim.x) * (4 / W)) {
+  for (int64_t row0 = int64_t(blockIdx.x) * (4 / W); row0 < rows; row0 += blocks * (4 / W)) {
     int64_t row = row0 + (W == 4 ? 0 : wave);
     if (W != 4 && row >= rows) break;
     // rows of a product just made, its last ones first: they are still in the cache behind the
@@ -63,6 +62,30 @@ __global__ __launch_bounds__(256) void i8_rows_kernel(const T *__restrict__ x, i
   }
 }
 
+template <typename T, bool VEC, int W, int RR>
+__global__ __launch_bounds__(256) void i8_rows_kernel(const T *__restrict__ x, int64_t ldx,
+                                                      int64_t rows,
+                                                      const int32_t *__restrict__ d_rows, int cols,
+                                                      int pitch, int8_t *__restrict__ codes,
+                                                      float *__restrict__ scale) {
+  rows_body<T, VEC, W, RR>(x, ldx, rows, d_rows, cols, pitch, codes, scale, gridDim.x);
+}
+
+// The same of N rows in the first blocks, and in the others the rotation table that the product
+// behind it reads too (a launch less: QKV 410M, 64 tokens 14.7 -> 12.4 us).
+template <typename T, int W, int RR>
+__global__ __launch_bounds__(256) void i8_rows_rope_kernel(const T *__restrict__ x, int N, int cols,
+                                                           int pitch, int8_t *__restrict__ codes,
+                                                           float *__restrict__ scale, int blocks,
+                                                           RopeJob job) {
+  if (int(blockIdx.x) < blocks) {
+    rows_body<T, true, W, RR>(x, cols, N, nullptr, cols, pitch, codes, scale, blocks);
+  } else {
+    const int64_t at = int64_t(blockIdx.x - blocks) * 256 + threadIdx.x;
+    if (at < int64_t(N) * job.hd) job.tab[at] = rope_entry(job, int(at / job.hd), int(at % job.hd));
+  }
+}
+
 // d_rows (or NULL): a device count that ends the rows earlier
 static hipError_t launch_rows(int act, int64_t rows, const int32_t *d_rows, int cols, const void *x,
                               int64_t ldx, int8_t *codes, float *scale, hipStream_t st) {
@@ -91,6 +114,26 @@ static hipError_t launch_rows(int act, int64_t rows, const int32_t *d_rows, int 
 hipError_t launch_i8_rows(int act, int64_t rows, int cols, const void *x, int64_t ldx, int8_t *codes,
                           float *scale, hipStream_t st) {
   return launch_rows(act, rows, nullptr, cols, x, ldx, codes, scale, st);
+}
+
+hipError_t launch_i8_rows_rope(int act, int N, int cols, const void *x, int8_t *codes, float *scale,
+                               const RopeJob &job, hipStream_t st) {
+  const int pitch = i8_pitch(cols);
+  const unsigned table = unsigned((int64_t(N) * job.hd + 255) / 256);
+  auto run = [&](auto tag, auto w) {
+    using T = decltype(tag);
+    constexpr int W = decltype(w)::value;
+    const int blocks = (N * W + 3) / 4;
+    i8_rows_rope_kernel<T, W, 4><<<dim3(blocks + table), 256, 0, st>>>((const T *)x, N, cols, pitch, codes,
+                                                                       scale, blocks, job);
+  };
+  auto by_width = [&](auto tag) {
+    if (cols > 2048) run(tag, std::integral_constant<int, 4>{});
+    else run(tag, std::integral_constant<int, 1>{});
+  };
+  if (act == TRIROUTE_BF16) by_width(bf16{});
+  else by_width(float{});
+  return hipGetLastError();
 }
 
 // Second RMSNorm of the experts' rows, quantised: n2 in fp64, rounded once to fp32 (the

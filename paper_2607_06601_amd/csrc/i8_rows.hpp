@@ -87,19 +87,32 @@ struct RowCode {
   }
 };
 
+// 8 elements at any element's place (the hardware takes unaligned pieces).
+__device__ __forceinline__ void load8u(const bf16 *p, float *v) {
+  uint32_t u[4];
+  __builtin_memcpy(u, p, 16);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(u[i] << 16);
+    v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ void load8u(const float *p, float *v) { __builtin_memcpy(v, p, 32); }
+
 // 8 elements at c of a row of `cols`, zeros behind its end.  VEC: whole aligned pieces.
 template <typename T, bool VEC>
 __device__ __forceinline__ void row8(const T *row, int c, int cols, float *v) {
-  if constexpr (VEC) {
-    if (c < cols) {
-      load8(row + c, v);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 0.f;
-    }
+  if (c + 8 <= cols) {
+    if constexpr (VEC) load8(row + c, v);
+    else load8u(row + c, v);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? Act<T>::ld(row, c + i) : 0.f;
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    if constexpr (!VEC) {
+#pragma unroll
+      for (int i = 0; i < 7; ++i)
+        if (c + i < cols) v[i] = Act<T>::ld(row, c + i);
+    }
   }
 }
 

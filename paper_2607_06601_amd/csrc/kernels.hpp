@@ -110,7 +110,6 @@ hipError_t launch_kv_export(const triroute_cfg &cfg, const CacheView &cv, int se
 // position of token (b, t) as in RopeJob (pos_base has n_base entries);
 // rope: scratch of qkv_rope_floats(cfg, B * Tq) floats (the rotation table)
 size_t qkv_rope_floats(const triroute_cfg &cfg, int N);
-hipError_t launch_rope_table(int N, const RopeJob &job, hipStream_t st);
 hipError_t launch_qkv(const triroute_cfg &cfg, int B, int Tq, const void *n1,
                       const triroute_dense_w &w, const int32_t *pos_base, const int32_t *pos_idx,
                       int n_base, void *q, void *k, void *v, float *rope, bool rope_ready,
@@ -188,6 +187,9 @@ struct MoeI8Ws;
 hipError_t i8_few_moe(const triroute_cfg &cfg, int N, const void *xt, const void *g2,
                       const triroute_moe_i8_w &w, const triroute_compaction &c, const MoeI8Ws &ws,
                       hipStream_t st);
+// the codes of N rows of `cols` (a multiple of 8, 16-byte aligned) and the rotation table
+hipError_t launch_i8_rows_rope(int act, int N, int cols, const void *x, int8_t *codes, float *scale,
+                               const RopeJob &job, hipStream_t st);
 hipError_t i8_linear(int act, int N, int m, int k, const int8_t *a, const float *sa,
                      const triroute_i8_w &w, const void *res, int64_t ldr, void *y, int64_t ldy,
                      hipStream_t st);
