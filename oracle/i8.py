@@ -79,14 +79,15 @@ def qkv(n1, Wq, Wk, Wv, pos, dh, act):
     return out
 
 
-def _uncertain(h, rel):
-    """Codes of rows that an implementation whose h is off by up to rel |h| may set one step
-    elsewhere, and the relative error of its scales."""
+def _uncertain(h, rel, off):
+    """Codes of rows that an implementation whose h is off by up to rel |h|, and that holds it with an
+    error of up to off beside, may set one step elsewhere; and the relative error of its scales."""
     a = np.abs(h).max(axis=1, keepdims=True)
     top = np.where(np.abs(h) >= a * (1 - 2 * rel), rel, 0.0).max(axis=1, keepdims=True)
     with np.errstate(divide="ignore", invalid="ignore"):
         t = np.where(a > 0, 127.0 * np.abs(h) / np.where(a > 0, a, 1), 0.0)
-    near = np.abs(np.abs(t - np.floor(t)) - 0.5) <= 1.01 * t * (rel + top)
+        t_off = np.where(a > 0, 127.0 * off / np.where(a > 0, a, 1), 0.0)
+    near = np.abs(np.abs(t - np.floor(t)) - 0.5) <= 1.01 * (t * (rel + top) + t_off)
     return near, top[:, 0] + U
 
 
@@ -95,7 +96,9 @@ def moe(xt, g2, Wg, Wu, Wd, eidx, egate, act):
     (codes [E, d, f], scale [E, d]).  The normalised token is an fp32 value before it is
     quantised, and so is h; h of bf16 layers is formed in fp32: G and U are off by 3 U, the
     exponential's argument by 4 U |G| more, it and the quotient by a few U, so that h is
-    off by less than 4 (|G| + 8) U."""
+    off by less than 4 (|G| + 8) U; and it is held as whole numbers of 1/32767 of the largest of 32
+    units, which is off by half of one and, through an fp32 reciprocal, 32767 * 2 U of one more (0.51 in
+    all)."""
     xt = np.asarray(xt, np.float64)
     n2 = rmsnorm(xt, g2).astype(np.float32)
     # (an fp64 norm that is a last place elsewhere rounds one n2 in 2^29 to its neighbour)
@@ -113,11 +116,16 @@ def moe(xt, g2, Wg, Wu, Wd, eidx, egate, act):
             h = (G / (1.0 + np.exp(-G)) * V).astype(np.float32)
         rel = 4 * (np.abs(G) + 8) * U if act == "bf16" else np.full(h.shape, 1.01 * 2 * U)
         hq, hs = quantize(h)
-        moved, hrel = _uncertain(h.astype(np.float64), rel)
+        off = np.zeros_like(G)
+        if act == "bf16":
+            top = np.abs(h.astype(np.float64)).reshape(len(i), -1, 32).max(axis=2)
+            off = np.repeat(top * (0.51 / 32767), 32, axis=1) + 1e-33
+        moved, hrel = _uncertain(h.astype(np.float64), rel, off)
         Y, eY = product(hq, hs, Wd[0][e - 1], Wd[1][e - 1])
         wd = np.abs(matrix(Wd[0][e - 1], Wd[1][e - 1]))
         eY = eY + np.abs(Y) * hrel[:, None] + (moved * np.asarray(hs, np.float64)[:, None]) @ wd.T
         np.add.at(y, i, g * Y)
         np.add.at(err, i, g * eY + 3 * U * (eidx.shape[1] + 1) * np.abs(g * Y))
     out = xt + y
-    return out, err + (2 * U + 1.01 * HALF_STEP[act]) * np.abs(out) + 2 * U * np.abs(y)
+    # (what is rounded at the end is the sum as formed, up to err further out: half its step)
+    return out, err + (2 * U + 1.01 * HALF_STEP[act]) * (np.abs(out) + err) + 2 * U * np.abs(y)
