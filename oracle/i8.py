@@ -94,9 +94,10 @@ def _uncertain(h, rel, off):
 def moe(xt, g2, Wg, Wu, Wd, eidx, egate, act):
     """x_out of triroute_moe_i8 and its bound; Wg, Wu: (codes [E, f, d], scale [E, f]), Wd:
     (codes [E, d, f], scale [E, d]).  The normalised token is an fp32 value before it is
-    quantised, and so is h; h of bf16 layers is formed in fp32: G and U are off by 3 U, the
-    exponential's argument by 4 U |G| more, it and the quotient by a few U, so that h is
-    off by less than 4 (|G| + 8) U; and it is held as whole numbers of 1/32767 of the largest of 32
+    quantised, and so is h; h of bf16 layers is formed in fp32: the exponential's argument
+    (a sum, three products, a constant) is off by 5 U |G| and moves silu by that much at most; the sums, the
+    other products, exponential and quotient are off by 20 U together, so that h is off by less than
+    5 (|G| + 8) U; and it is held as whole numbers of 1/32767 of the largest of 32
     units, which is off by half of one and, through an fp32 reciprocal, 32767 * 2 U of one more (0.51 in
     all)."""
     xt = np.asarray(xt, np.float64)
@@ -114,7 +115,7 @@ def moe(xt, g2, Wg, Wu, Wd, eidx, egate, act):
         V, _ = product(nq[i], ns[i], Wu[0][e - 1], Wu[1][e - 1])
         with np.errstate(over="ignore"):
             h = (G / (1.0 + np.exp(-G)) * V).astype(np.float32)
-        rel = 4 * (np.abs(G) + 8) * U if act == "bf16" else np.full(h.shape, 1.01 * 2 * U)
+        rel = 5 * (np.abs(G) + 8) * U if act == "bf16" else np.full(h.shape, 1.01 * 2 * U)
         hq, hs = quantize(h)
         off = np.zeros_like(G)
         if act == "bf16":

@@ -98,7 +98,8 @@ __device__ __forceinline__ void w4_cols(const float *sc, int lane, float (&c)[NI
 // H1P3).  That is off by 2^-16 of the 32 units' largest, 1/500 of a step of the row's codes at most: about one
 // code in 3000 moves by its step, 2e-4 of the output's size where bf16 rounds by 2e-3.
 //
-// Whole numbers of v of a part whose largest |v| has the bits m, two to a word.
+// Whole numbers of v = h / row^2 (gated()) of a part whose largest |v| has the bits m, two to a word,
+// and the bits of the part's largest |h|.
 __device__ __forceinline__ float part_unit(uint32_t m) {
   return 32767.0f * __builtin_amdgcn_rcpf(fmaxf(__uint_as_float(m), 1e-33f));
 }
@@ -107,6 +108,9 @@ __device__ __forceinline__ uint32_t pack16(float a, float b, float unit) {
   const uint32_t x = __float_as_uint(fmaf(a, unit, 12582912.0f));
   const uint32_t y = __float_as_uint(fmaf(b, unit, 12582912.0f));
   return __builtin_amdgcn_perm(y, x, 0x05040100u);
+}
+__device__ __forceinline__ uint32_t part_max(uint32_t m, float row) {
+  return __float_as_uint(__uint_as_float(m) * (row * row));
 }
 // Largest of 4 or 8 lanes side by side.
 template <int LANES>
@@ -449,10 +453,11 @@ struct Moe1I8 {
   static constexpr int out_cols(int BN) { return BN / 2; }
   __device__ int tiles(int BM, int ny, const GroupScan &gs) const { return gs.total * ny; }
   __device__ bool map(int bx, int by, int BM, int BN, MTile &t, const GroupScan &gs) const {
-    if (!mmap_grouped(bx, BM, gs, t)) return false;
-    t.n0 = by * (BN / 2);  // BN/2 expert units per tile (gate + up columns)
-    return true;
+    t.n0 = first_unit(by, BN);
+    return mmap_grouped(bx, BM, gs, t);
   }
+  // BN/2 expert units per tile (gate + up columns)
+  __device__ static int first_unit(int by, int BN) { return by * (BN / 2); }
   __device__ const int8_t *a_row(const MTile &t, int r) const { return a + int64_t(t.p0 + r) * pitch; }
   __device__ const int8_t *b_row(const MTile &t, int n) const {
     int P, half;
@@ -468,8 +473,12 @@ struct Moe1I8 {
     const int f = t.n0 + P;
     return f < dff ? (half ? su : sg)[int64_t(t.e - 1) * dff + f] : 0.f;
   }
+  // F64: h; else h / row_scale^2
   __device__ float hidden(int32_t ag, int32_t au, float sr, float cg, float cu) const {
-    return gated<F64>(ag, au, sr, cg, cu);
+    if constexpr (F64)
+      return gated64(ag, au, sr, cg, cu);
+    else
+      return gated(ag, au, sr, GateScale(cg, cu));
   }
   // Four-wave kernel: in wave column wn, MFMA block ni, lane column c
   // holds expert unit (NI / 2) (16 wn + c) + ni / 2 of the tile, gate for
@@ -502,6 +511,9 @@ struct Moe1I8 {
     if (f >= dff) return;  // d_ff is a multiple of 32: a part's lanes are all in or all out
     const float *cl = scales + MI * 16 + (NI / 2) * (lane & 15);
     const float4 cg = *(const float4 *)cl, cu = *(const float4 *)(cl + NI * 8);
+    const GateScale gc[4] = {{cg.x, cu.x}, {cg.y, cu.y}, {cg.z, cu.z}, {cg.w, cu.w}};
+    // (the maximum below drops a NaN: those of the weights' scales come back with this)
+    const float nan = (gc[0].both + gc[1].both + gc[2].both + gc[3].both) * 0.0f;
     // (wave-uniform; a lane's offset fits 32 bits)
     int16_t *out = (int16_t *)h + int64_t(t.p0) * dff;
     uint32_t *pt = part + int64_t(t.p0) * (dff >> 5);
@@ -512,18 +524,16 @@ struct Moe1I8 {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float v[4];
-        uint32_t m = 0;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          v[u] = hidden(acc[mi][2 * u][i], acc[mi][2 * u + 1][i], elem(sr, i), elem(cg, u), elem(cu, u));
-          m = max(m, __float_as_uint(v[u]) & 0x7FFFFFFFu);
-        }
-        m = lanes_umax<8>(m);
+        for (int u = 0; u < 4; ++u)
+          v[u] = gated(acc[mi][2 * u][i], acc[mi][2 * u + 1][i], elem(sr, i), gc[u]);
+        const float m4 = fmaxf(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fabsf(v[2])), fabsf(v[3]));
+        const uint32_t m = lanes_umax<8>(__float_as_uint(m4 + nan));
         const float unit = part_unit(m);
         if (r0 + i < t.mvalid) {
           *(uint2 *)(out + uint32_t((r0 + i) * dff + f)) =
               make_uint2(pack16(v[0], v[1], unit), pack16(v[2], v[3], unit));
-          if ((lane & 7) == 0) pt[uint32_t((r0 + i) * (dff >> 5) + (f >> 5))] = m;
+          if ((lane & 7) == 0) pt[uint32_t((r0 + i) * (dff >> 5) + (f >> 5))] = part_max(m, elem(sr, i));
         }
       }
     }
@@ -551,12 +561,13 @@ struct Moe1I8 {
         for (int u = 0; u < 8; ++u) m = max(m, __float_as_uint(v[u]) & 0x7FFFFFFFu);
         m = lanes_umax<4>(m);  // (f < dff for all four lanes or none, r is the same)
         const float unit = part_unit(m);
+        const float sr = row_scale(t, r < t.mvalid ? r : 0);
         if (on) {
           u32x4_t w;
 #pragma unroll
           for (int u = 0; u < 4; ++u) w[u] = pack16(v[2 * u], v[2 * u + 1], unit);
           *(u32x4_t *)((int16_t *)h + row * dff + f) = w;
-          if ((c8 & 31) == 0) part[row * (dff >> 5) + (f >> 5)] = m;
+          if ((c8 & 31) == 0) part[row * (dff >> 5) + (f >> 5)] = part_max(m, sr);
         }
       }
     }
@@ -575,10 +586,10 @@ struct Moe2I8 {
   static constexpr int out_cols(int BN) { return BN; }
   __device__ int tiles(int BM, int ny, const GroupScan &gs) const { return gs.total * ny; }
   __device__ bool map(int bx, int by, int BM, int BN, MTile &t, const GroupScan &gs) const {
-    if (!mmap_grouped(bx, BM, gs, t)) return false;
-    t.n0 = by * BN;
-    return true;
+    t.n0 = first_unit(by, BN);
+    return mmap_grouped(bx, BM, gs, t);
   }
+  __device__ static int first_unit(int by, int BN) { return by * BN; }
   __device__ const int8_t *a_row(const MTile &t, int r) const { return a + int64_t(t.p0 + r) * pitch; }
   __device__ const int8_t *b_row(const MTile &t, int n) const {
     return t.n0 + n < d ? Wd + (int64_t(t.e - 1) * d + t.n0 + n) * pitch : nullptr;

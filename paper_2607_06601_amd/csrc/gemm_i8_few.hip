@@ -322,7 +322,8 @@ struct FewUp {
   __device__ void store(const MTile &t, int r, int c, int32_t vg, int32_t vu, float sr) const {
     const int f = t.n0 + c;
     const int64_t wr = int64_t(t.e - 1) * dff + f;
-    h[int64_t(t.p0 + r) * dff + f] = gated<sizeof(T) == 4>(vg, vu, sr, sg[wr], su[wr]);
+    h[int64_t(t.p0 + r) * dff + f] = sizeof(T) == 4 ? gated64(vg, vu, sr, sg[wr], su[wr])
+                                                    : gated(vg, vu, sr, GateScale(sg[wr], su[wr])) * (sr * sr);
   }
 };
 

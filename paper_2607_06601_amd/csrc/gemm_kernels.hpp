@@ -326,8 +326,47 @@ __global__ __launch_bounds__(256, 1) void gemm_w4_kernel(P p, int K, int ny) {
   const int total = __builtin_amdgcn_readfirstlane(p.tiles(BM, ny, gs));
   int L = blockIdx.x;
   if (L >= total) return;
+  // Grouped 8-bit problems: lane j holds the block's tile j of each 64 (found once, side by side;
+  // one after the other, at each tile's end, the search takes 2000 cycles of a tile's 40000 to
+  // 70000 there).
+  constexpr bool LISTED = P::GROUPED && P::Op::INT;
+  MTile mine{};
+  auto list_tiles = [&](int first) {
+    if constexpr (LISTED) {
+      const int l = first + int(gridDim.x) * (threadIdx.x & 63);
+      const int x = xcd_tile(min(l, total - 1), total);
+      int e = 0, done = 0, incl = 0, start = 0, c = 0;  // the expert whose tiles reach past x
+      for (int k = 0; k < p.E; ++k) {
+        const int ik = __builtin_amdgcn_readlane(gs.incl, k);
+        const bool here = !done && ik * ny > x;
+        const int ck = __builtin_amdgcn_readlane(gs.c, k), sk = __builtin_amdgcn_readlane(gs.start, k);
+        const int nk = __builtin_amdgcn_readlane(gs.nt, k);
+        e = here ? k + 1 : e;
+        incl = here ? ik - nk : incl;  // tiles before it
+        start = here ? sk : start;
+        c = here ? ck : c;
+        done |= here;
+      }
+      int i, j;
+      band_order(x - incl * ny, (c + BM - 1) / BM, ny, i, j);
+      mine.e = e;
+      mine.p0 = start + i * BM;
+      mine.mvalid = min(BM, c - i * BM);
+      mine.n0 = P::first_unit(j, BN);
+    }
+  };
   auto tile = [&](int l) {  // a tile's fields are wave-uniform: kept in SGPRs
     MTile t;
+    if constexpr (LISTED) {
+      const int j = (l - int(blockIdx.x)) / int(gridDim.x);
+      if ((j & 63) == 0) list_tiles(l);
+      t.m0 = 0;
+      t.n0 = __builtin_amdgcn_readlane(mine.n0, j & 63);
+      t.mvalid = __builtin_amdgcn_readlane(mine.mvalid, j & 63);
+      t.e = __builtin_amdgcn_readlane(mine.e, j & 63);
+      t.p0 = __builtin_amdgcn_readlane(mine.p0, j & 63);
+      return t;
+    }
     const int x = xcd_tile(l, total);
     int bx, by;
     if constexpr (P::GROUPED)

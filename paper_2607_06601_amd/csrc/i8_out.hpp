@@ -14,18 +14,25 @@ __device__ __forceinline__ float dequant(int32_t v, float row, float col) {
   return float(v) * row * col;
 }
 
-// silu(G) U.  F64: h of fp32 activations is computed in fp64 and rounded once: the codes of h then
-// do not hang on the last bits of an fp32 exponential (a code one step off would move the output by
-// far more than an fp32 rounding does; against bf16's rounding it does not count).
-template <bool F64>
-__device__ __forceinline__ float gated(int32_t ag, int32_t au, float row, float cg, float cu) {
-  if constexpr (F64) {
-    const double g = double(ag) * double(row) * double(cg), u = double(au) * double(row) * double(cu);
-    return float(g / (1.0 + exp(-g)) * u);
-  } else {
-    const float g = dequant(ag, row, cg), u = dequant(au, row, cu);
-    return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u;
-  }
+// h = silu(G) U of fp32 activations: computed in fp64 and rounded once, so that the codes of h do
+// not hang on the last bits of an fp32 exponential (a code one step off would move the output by far
+// more than an fp32 rounding does; against bf16's rounding it does not count).
+__device__ __forceinline__ float gated64(int32_t ag, int32_t au, float row, float cg, float cu) {
+  const double g = double(ag) * double(row) * double(cg), u = double(au) * double(row) * double(cu);
+  return float(g / (1.0 + exp(-g)) * u);
+}
+
+// h / row^2 of bf16 activations, for the sums ag, au of gate and up:
+//   silu(G) U = row^2 (cg cu) ag au / (1 + 2^(-G log2 e)).
+// row^2 is common to a token's units, so it is applied once to what they share, not to each.
+struct GateScale {
+  float exponent, both;  // -cg log2 e, cg cu
+  __device__ __forceinline__ GateScale(float cg, float cu)
+      : exponent(-1.44269504088896f * cg), both(cg * cu) {}
+};
+__device__ __forceinline__ float gated(int32_t ag, int32_t au, float row, const GateScale &c) {
+  const float g = float(ag), e = __builtin_amdgcn_exp2f(g * row * c.exponent);
+  return g * float(au) * c.both * __builtin_amdgcn_rcpf(1.0f + e);
 }
 
 // Rotation of the pair (a, b) by (cos, sin).
