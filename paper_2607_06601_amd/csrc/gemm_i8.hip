@@ -76,6 +76,12 @@ __device__ __forceinline__ void add8(const Raw8f &x, float *v) {
   }
 }
 
+// The address `off` bytes behind a wave-uniform one (32-bit offsets: no 64-bit sums a lane).
+template <class E>
+__device__ __forceinline__ E *behind(E *base, uint32_t off) {
+  return (E *)((uint8_t *)base + off);
+}
+
 // Four-wave kernel: the wave's scales in LDS, its TM rows', then its TN columns'; the
 // four rows of a lane in row block mi, and its columns' where it holds NI of them side by side.
 template <int MI>
@@ -101,7 +107,7 @@ __device__ __forceinline__ void w4_cols(const float *sc, int lane, float (&c)[NI
 // Whole numbers of v = h / row^2 (gated()) of a part whose largest |v| has the bits m, two to a word,
 // and the bits of the part's largest |h|.
 __device__ __forceinline__ float part_unit(uint32_t m) {
-  return 32767.0f * __builtin_amdgcn_rcpf(fmaxf(__uint_as_float(m), 1e-33f));
+  return 32767.0f * __builtin_amdgcn_rcpf(__uint_as_float(max(m, __float_as_uint(1e-33f))));
 }
 __device__ __forceinline__ uint32_t pack16(float a, float b, float unit) {
   // (the low half of a whole number plus 1.5 * 2^23)
@@ -115,7 +121,7 @@ __device__ __forceinline__ uint32_t part_max(uint32_t m, float row) {
 // Largest of 4 or 8 lanes side by side.
 template <int LANES>
 __device__ __forceinline__ uint32_t lanes_umax(uint32_t v) {
-#define TR_DPP(c) uint32_t(__builtin_amdgcn_update_dpp(0, int(v), c, 0xF, 0xF, false))
+#define TR_DPP(c) uint32_t(__builtin_amdgcn_update_dpp(int(v), int(v), c, 0xF, 0xF, false))
   v = max(v, TR_DPP(0xB1));                             // quad_perm 1 0 3 2
   v = max(v, TR_DPP(0x4E));                             // quad_perm 2 3 0 1
   if constexpr (LANES == 8) v = max(v, TR_DPP(0x141));  // row_half_mirror
@@ -186,12 +192,14 @@ struct LinearI8 {
     typedef std::conditional_t<sizeof(T) == 2, uint4, Raw8f> raw;
     raw x[AHEAD][4];
     const bool has = res != nullptr;
+    T *yt = y + t.m0 * ldy;  // (wave-uniform; the host checks that 256 rows lie within 4 GB)
+    const T *rt = res + t.m0 * ldr;
     auto row0 = [&](int mi) { return wm * MI * 16 + mi * 16 + 4 * (lane >> 4); };
     auto fetch = [&](int mi) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int r = row0(mi) + i;
-        x[mi % AHEAD][i] = *(const raw *)(res + (t.m0 + (r < t.mvalid ? r : 0)) * ldr + f);
+        x[mi % AHEAD][i] = *(const raw *)behind(rt, (uint32_t(r < t.mvalid ? r : 0) * uint32_t(ldr) + f) * uint32_t(sizeof(T)));
       }
     };
     if (has) {
@@ -209,7 +217,8 @@ struct LinearI8 {
 #pragma unroll
         for (int ni = 0; ni < NI; ++ni) v[ni] = dequant(acc[mi][ni][i], elem(sr, i), sc[ni]);
         if (has) add8(x[mi % AHEAD][i], v);
-        if (r0 + i < t.mvalid) put8(y + (t.m0 + r0 + i) * ldy + f, v);
+        if (r0 + i < t.mvalid)
+          put8(behind(yt, (uint32_t(r0 + i) * uint32_t(ldy) + f) * uint32_t(sizeof(T))), v);
       }
       if (has && mi + AHEAD < MI) fetch(mi + AHEAD);
       __builtin_amdgcn_sched_barrier(0);
@@ -531,9 +540,9 @@ struct Moe1I8 {
         const uint32_t m = lanes_umax<8>(__float_as_uint(m4 + nan));
         const float unit = part_unit(m);
         if (r0 + i < t.mvalid) {
-          *(uint2 *)(out + uint32_t((r0 + i) * dff + f)) =
-              make_uint2(pack16(v[0], v[1], unit), pack16(v[2], v[3], unit));
-          if ((lane & 7) == 0) pt[uint32_t((r0 + i) * (dff >> 5) + (f >> 5))] = part_max(m, elem(sr, i));
+          const uint32_t at = uint32_t((r0 + i) * dff + f);  // (of the part: at / 32, d_ff being a multiple)
+          *(uint2 *)behind(out, at * 2u) = make_uint2(pack16(v[0], v[1], unit), pack16(v[2], v[3], unit));
+          if ((lane & 7) == 0) *behind(pt, at >> 3) = part_max(m, elem(sr, i));
         }
       }
     }
@@ -633,7 +642,7 @@ struct Moe2I8 {
         float v[8];
 #pragma unroll
         for (int ni = 0; ni < NI; ++ni) v[ni] = dequant(acc[mi][ni][i], elem(sr, i), sc[ni]);
-        if (r0 + i < t.mvalid) store8(out + uint32_t((r0 + i) * d + f), v);
+        if (r0 + i < t.mvalid) store8(behind(out, uint32_t((r0 + i) * d + f) * 4u), v);
       }
     }
   }
@@ -676,7 +685,7 @@ static hipError_t linear_rows(const P &all, hipStream_t st) {
     if constexpr (P::WIDE)
       w4 = K2 >= 128 && span32({{p.a, size_t(p.N) * p.pitch}}, &lo) &&
            span32({{p.w, size_t(p.m) * p.pitch}}, &lo) &&
-           w4_rounds(p.N, c128, tile_cost(m256 * c256, COST_256X256));
+           std::max(p.ldy, p.ldr) < (1 << 22) && w4_rounds(p.N, c128, tile_cost(m256 * c256, COST_256X256));
     if (few_tiles(p.N, c128) && split_k(m32 * c64, K2))
       e = launch<P, 32, 64, 2, 1, 64, 4, 2>(p, K2, m32, c64, st);
     else if (few_tiles(p.N, c128))
