@@ -591,20 +591,6 @@ inline hipError_t launch(const P &p, int K, int m_tiles, int n_tiles, hipStream_
   return hipGetLastError();
 }
 
-// CUs of the current device (the tile-shape choice counts rounds of them).
-inline int cu_count() {
-  static int n = 0;
-  if (n == 0) {
-    int dev = 0, v = 0;
-    if (hipGetDevice(&dev) == hipSuccess &&
-        hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && v > 0)
-      n = v;
-    else
-      n = 256;
-  }
-  return n;
-}
-
 // One block per CU at most (a block holds 128 KB of LDS), each walking its
 // share of the tiles.
 template <class P, int BM, int BN>

@@ -71,6 +71,54 @@ __global__ __launch_bounds__(256) void i8_rows_kernel(const T *__restrict__ x, i
   rows_body<T, VEC, W, RR>(x, ldx, rows, d_rows, cols, pitch, codes, scale, gridDim.x);
 }
 
+// Many bf16 rows of aligned pieces, of up to 512 RR elements: a wave has its next row on the way
+// while it codes one (16384 rows of 2048, bf16: ROWS us, a row a wave 26).
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+template <int RR>
+__global__ __launch_bounds__(256) void i8_stream_kernel(const bf16 *__restrict__ x, int64_t ldx, int64_t rows,
+                                                        int cols, int pitch, int8_t *__restrict__ codes,
+                                                        float *__restrict__ scale) {
+  const int at = (threadIdx.x & 63) * 8;
+  const int64_t step = int64_t(gridDim.x) * 4;
+  uint4 next[RR];
+  auto fetch = [&](int64_t row) {
+#pragma unroll
+    for (int q = 0; q < RR; ++q) {
+      const int c = at + 512 * q;
+      if (c < cols) next[q] = *(const uint4 *)(x + row * ldx + c);
+    }
+  };
+#pragma unroll
+  for (int q = 0; q < RR; ++q) next[q] = make_uint4(0u, 0u, 0u, 0u);  // (pieces behind the row's end stay zeros)
+  int64_t row = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (row < rows) fetch(row);
+  for (; row < rows; row += step) {
+    float v[RR][8];
+    uint32_t m;
+    u16x2_t m2 = {0, 0};  // (bf16 pairs: |x| as whole numbers of 16 bits)
+#pragma unroll
+    for (int q = 0; q < RR; ++q) {
+      const uint32_t u[4] = {next[q].x, next[q].y, next[q].z, next[q].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        m2 = __builtin_elementwise_max(m2, __builtin_bit_cast(u16x2_t, u[i] & 0x7FFF7FFFu));
+        v[q][2 * i] = __uint_as_float(u[i] << 16);
+        v[q][2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+      }
+    }
+    m = uint32_t(max(m2[0], m2[1])) << 16;
+    if (row + step < rows) fetch(row + step);
+    const RowCode rc(wave_umax(m));
+    int8_t *cr = codes + row * pitch;
+#pragma unroll
+    for (int q = 0; q < RR; ++q) {
+      const int c = at + 512 * q;
+      if (c < pitch) *(uint2 *)(cr + c) = rc.code8(v[q]);
+    }
+    if (at == 0) scale[row] = rc.scale;
+  }
+}
+
 // The same of N rows in the first blocks, and in the others the rotation table that the product
 // behind it reads too (a launch less: QKV 410M, 64 tokens 14.7 -> 12.4 us).
 template <typename T, int W, int RR>
@@ -91,6 +139,19 @@ static hipError_t launch_rows(int act, int64_t rows, const int32_t *d_rows, int 
                               int64_t ldx, int8_t *codes, float *scale, hipStream_t st) {
   const int es = act == TRIROUTE_BF16 ? 2 : 4, pitch = i8_pitch(cols);
   const bool vec = cols % 8 == 0 && ((uintptr_t(x) | uintptr_t(ldx * es)) & 15) == 0;
+  // (from two rows a wave on; fp32 rows are at the memory's rate without)
+  const int waves = cu_count() * 24;
+  if (vec && act == TRIROUTE_BF16 && cols <= 2048 && rows >= 2 * waves) {
+    auto stream = [&](auto rr) {
+      i8_stream_kernel<decltype(rr)::value><<<dim3(waves / 4), 256, 0, st>>>((const bf16 *)x, ldx, rows, cols,
+                                                                             pitch, codes, scale);
+    };
+    if (pitch <= 512) stream(std::integral_constant<int, 1>{});
+    else if (pitch <= 1024) stream(std::integral_constant<int, 2>{});
+    else if (pitch <= 1536) stream(std::integral_constant<int, 3>{});
+    else stream(std::integral_constant<int, 4>{});
+    return hipGetLastError();
+  }
   auto run = [&](auto tag, auto v, auto w) {
     using T = decltype(tag);
     constexpr int W = decltype(w)::value;

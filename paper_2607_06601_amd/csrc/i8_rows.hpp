@@ -31,7 +31,7 @@ __device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
   return max(uint32_t(b[0]), uint32_t(b[1]));
 }
 
-// Scale of a row and the codes of its elements.  A code is the quotient in fp32, rounded; with
+// Scale of a row and the codes of its elements.  A code is the quotient with 1 / a in fp32, rounded; with
 // one of 8 next to a border (4e-5; the quotient is off by at most 127 * 2^-23), the 8 are
 // compared with their borders instead.  The quotients of a row of tiny values are of values 2^64 times
 // larger (exact), so that 127 / a stays finite.
@@ -39,10 +39,12 @@ struct RowCode {
   float a, inv;
   float scale;
   bool bad, tiny;
+  // amax: of the row, the same in every lane
   __device__ __forceinline__ explicit RowCode(uint32_t amax) {
+    amax = __builtin_amdgcn_readfirstlane(amax);  // (so that what hangs on it branches)
     a = __uint_as_float(amax);
     bad = amax >= INF_BITS;
-    tiny = a < 1e-30f;
+    tiny = amax < 0x0DA24260u;  // 1e-30
     scale = bad ? __uint_as_float(0x7FC00000u) : a / 127.0f;
     if (tiny) a *= LIFT;
     inv = a > 0.0f && !bad ? 127.0f / a : 0.0f;
@@ -63,20 +65,21 @@ struct RowCode {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] *= LIFT;
     }
+    // (the quotient plus 1.5 * 2^23 is rounded to a whole number, whose byte is the sum's lowest)
+    constexpr float BIG = 12582912.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float t = v[i] * inv;
-      r[i] = rintf(t);
-      far = fmaxf(far, fabsf(t - r[i]));
+      r[i] = fmaf(v[i], inv, BIG);
+      far = fmaxf(far, fabsf(fmaf(v[i], inv, BIG - r[i])));
     }
     if (far > 0.49996f) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) r[i] = copysignf(float(exact(fabsf(v[i]), fabsf(v[i]) * inv)), v[i]);
+      for (int i = 0; i < 8; ++i)
+        r[i] = BIG + copysignf(float(exact(fabsf(v[i]), fabsf(v[i]) * inv)), v[i]);
     }
-    // (the byte of a whole number up to 127 is the lowest of it plus 1.5 * 2^23)
     uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(r[i] + 12582912.0f);
+    for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(r[i]);
     // bytes 0 of two words, then of two pairs
     uint2 o;
     o.x = __builtin_amdgcn_perm(__builtin_amdgcn_perm(w[3], w[2], 0x0C0C0400u),

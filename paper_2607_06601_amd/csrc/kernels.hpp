@@ -11,6 +11,20 @@ namespace tr {
 inline int attn_groups(const triroute_cfg &c) { return c.attn_groups > 0 ? c.attn_groups : c.n_heads; }
 
 
+// CUs of the current device (the tile-shape choice counts rounds of them).
+inline int cu_count() {
+  static int n = 0;
+  if (n == 0) {
+    int dev = 0, v = 0;
+    if (hipGetDevice(&dev) == hipSuccess &&
+        hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && v > 0)
+      n = v;
+    else
+      n = 256;
+  }
+  return n;
+}
+
 // router.hip
 hipError_t router_prepare();
 // trunk K split: ks chunks of kchunk inputs; the trunk partials take

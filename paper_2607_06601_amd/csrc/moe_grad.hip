@@ -1386,16 +1386,6 @@ __global__ __launch_bounds__(1024) void moe_grad_g2_kernel(const float *__restri
 }
 
 // ------------------------------------------------------------------ launchers
-static int cu_count() {
-  static const int n = [] {
-    int dev = 0, v = 0;
-    return hipGetDevice(&dev) == hipSuccess &&
-                   hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && v > 0
-               ? v
-               : 256;
-  }();
-  return n;
-}
 
 int moe_grad_gate_parts(const triroute_cfg &cfg) { return cfg.d_ff / 64 * 2; }
 static int token_blocks(int N) { return std::min((N + 3) / 4, TOK_BLOCKS); }
