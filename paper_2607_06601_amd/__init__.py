@@ -457,7 +457,7 @@ class I8Matrix:
                 or not scale.is_contiguous() or scale.device != codes.device:
             raise ValueError("scale: one fp32 value a row, on the codes' device")
         self.codes, self.scale, self.cols = codes, scale, cols
-        self.rows = codes.shape[0]
+        self.rows, self.index = codes.shape[0], codes.get_device()
         self.w = I8W(codes.data_ptr(), scale.data_ptr())
         self.ref = C.byref(self.w)
 
@@ -478,8 +478,10 @@ class I8Matrix:
 _ACTS = {torch.float32: F32, torch.bfloat16: BF16}
 
 
-def _i8_rows(name, t, dtype, shape):
-    """Row stride of a tensor of this type and shape whose rows are contiguous."""
+def _i8_rows(name, t, dtype, shape, index):
+    """Row stride of a tensor of the GPU `index`, of this type and shape, whose rows are contiguous."""
+    if t.get_device() != index:
+        raise ValueError(f"{name}: a tensor of the current GPU wanted")
     if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name}: {list(shape)} of {dtype} wanted")
     ld, step = t.stride()
@@ -489,18 +491,31 @@ def _i8_rows(name, t, dtype, shape):
     return ld if shape[0] > 1 or ld > shape[1] else shape[1]
 
 
+def _i8_stream(stream):
+    """The stream of a call, of the current GPU."""
+    here = torch.cuda.current_stream()
+    if stream is None:
+        return here
+    if stream.device_index != here.device_index:
+        raise ValueError("stream: one of the current GPU wanted")
+    return stream
+
+
 def i8_quantize(x, codes, scale, stream=None):
     """Codes int8 [rows, i8_pitch(cols)] and scales fp32 [rows] of the rows of x."""
     if x.dim() != 2 or x.dtype not in _ACTS:
         raise ValueError("x: fp32 or bf16 rows wanted")
-    ldx = _i8_rows("x", x, x.dtype, x.shape)
+    stream = _i8_stream(stream)
+    ldx = _i8_rows("x", x, x.dtype, x.shape, stream.device_index)
     if codes.dtype != torch.int8 or codes.shape != (x.shape[0], i8_pitch(x.shape[1])) \
             or not codes.is_contiguous():
         raise ValueError("codes: contiguous int8 [rows, i8_pitch(cols)]")
     if scale.dtype != torch.float32 or scale.shape != (x.shape[0],) or not scale.is_contiguous():
         raise ValueError("scale: fp32 [rows]")
+    if codes.get_device() != stream.device_index or scale.get_device() != stream.device_index:
+        raise ValueError("codes and scale: tensors of the current GPU wanted")
     _check(lib().triroute_i8_quantize(_ACTS[x.dtype], x.shape[0], x.shape[1], _p(x), ldx, _p(codes),
-                                      _p(scale), _stream(stream)))
+                                      _p(scale), stream.cuda_stream))
 
 
 def linear_i8_workspace(n_tok: int, cols: int, device="cuda"):
@@ -517,11 +532,15 @@ def linear_i8(x, w: I8Matrix, y, ws, residual=None, stream=None):
     act = _ACTS.get(dtype)
     if act is None:
         raise ValueError(f"x: fp32 or bf16 wanted, not {dtype}")
+    stream = _i8_stream(stream)
+    index = stream.device_index
+    if w.index != index or ws.get_device() != index:
+        raise ValueError("weight and workspace: on the current GPU")
     _check(lib().triroute_linear_i8(
-        act, n, k, m, x.data_ptr(), _i8_rows("x", x, dtype, (n, k)), w.ref,
+        act, n, k, m, x.data_ptr(), _i8_rows("x", x, dtype, (n, k), index), w.ref,
         None if residual is None else residual.data_ptr(),
-        0 if residual is None else _i8_rows("residual", residual, dtype, (n, m)), y.data_ptr(),
-        _i8_rows("y", y, dtype, (n, m)), ws.data_ptr(), ws.numel(), _stream(stream)))
+        0 if residual is None else _i8_rows("residual", residual, dtype, (n, m), index), y.data_ptr(),
+        _i8_rows("y", y, dtype, (n, m), index), ws.data_ptr(), ws.numel(), stream.cuda_stream))
 
 
 def qkv_i8(cfg, B, T, n1, dw: DenseI8W, q, k, v, ws, pos0=None, stream=None):

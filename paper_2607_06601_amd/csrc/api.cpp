@@ -1179,6 +1179,7 @@ int triroute_linear_i8(int act, int n_tok, int in, int out, const void *x, int64
   TRY(check_rows(act, "x", x, ldx, in));
   TRY(check_rows(act, "y", y, ldy, out));
   if (residual) TRY(check_rows(act, "residual", residual, ldr, out));
+  REQUIRE(x != y, TRIROUTE_E_INVALID, "y in x's place");
   REQUIRE(residual != y || ldr == ldy, TRIROUTE_E_INVALID,
           "a residual in y's place needs y's row stride");
   TRY(check_i8_w({*w}));

@@ -100,9 +100,10 @@ __device__ __forceinline__ void w4_cols(const float *sc, int lane, float (&c)[NI
 // ---------------------------------------------------------------- hidden rows
 // h between the two expert products is held as whole numbers in +-32767 of each 32 units' largest
 // magnitude (fp32 rows would be written and read at twice the bytes, which is what bounds the rows'
-// pass and, for short K, the tiles' epilogue: 160M, 16384 tokens, the block 301 -> H160 us, 1.3B 1285 ->
-// H1P3).  That is off by 2^-16 of the 32 units' largest, 1/500 of a step of the row's codes at most: about one
-// code in 3000 moves by its step, 2e-4 of the output's size where bf16 rounds by 2e-3.
+// pass and, for short K, the tiles' epilogue: 16384 tokens, with gated() as it is, the block of 160M
+// 301 -> 297 us, of 1.3B 1285 -> 1213).  That is off by 2^-16 of the 32 units' largest, 1/500 of a
+// step of the row's codes at most: about one code in 3000 moves by its step, 2e-4 of the output's size
+// where bf16 rounds by 2e-3.
 //
 // Whole numbers of v = h / row^2 (gated()) of a part whose largest |v| has the bits m, two to a word,
 // and the bits of the part's largest |h|.
@@ -664,13 +665,17 @@ struct Moe2I8 {
 };
 
 // ------------------------------------------------------------------ launchers
-// Rows a launch may take: its blocks stay far below the limits of a grid.
-static int rows_a_launch(int c64) { return std::max(1, (1 << 22) / c64) * 32; }
+// Rows a launch may take: its blocks stay far below the limits of a grid, and (for the four-wave
+// kernel's 32-bit offsets) its codes within 4 GB.
+static int rows_a_launch(int c64, int pitch) {
+  const int64_t near = ((int64_t(1) << 32) - 1) / pitch / 256 * 256;
+  return int(std::min(int64_t(std::max(1, (1 << 22) / c64)) * 32, near));
+}
 
 template <class P>
 static hipError_t linear_rows(const P &all, hipStream_t st) {
   const int K2 = all.pitch / 2, c64 = (all.m + 63) / 64, c128 = (all.m + 127) / 128;
-  const int most = rows_a_launch(c64);
+  const int most = rows_a_launch(c64, all.pitch);
   for (int at = 0; at < all.N; at += most) {
     P p = all;
     p.N = std::min(most, all.N - at);
@@ -742,7 +747,7 @@ hipError_t i8_qkv(const triroute_cfg &cfg, int N, const int8_t *a, const float *
     all.Hd = cfg.n_heads * cfg.head_dim;
     all.Kd = cfg.n_kv_heads * cfg.head_dim;
     all.Ncols = all.Hd + 2 * all.Kd;
-    const int c64 = (all.Ncols + 63) / 64, most = rows_a_launch(c64), K2 = all.pitch / 2;
+    const int c64 = (all.Ncols + 63) / 64, most = rows_a_launch(c64, all.pitch), K2 = all.pitch / 2;
     for (int at = 0; at < N; at += most) {
       QkvI8<T> p = all;
       p.N = std::min(most, N - at);

@@ -575,7 +575,7 @@ __global__ __launch_bounds__(256, 1) void gemm_w4_kernel(P p, int K, int ny) {
       tn = tile(Ln);
       offsets(tn, vnx);
       bstep[0] = base_of(tn, K0) - bnow[0];
-    bstep[1] = base_of(tn, K1) - bnow[1];
+      bstep[1] = base_of(tn, K1) - bnow[1];
     }
   }
 }

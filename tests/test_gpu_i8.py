@@ -80,6 +80,18 @@ def test_codes_of_many_rows_and_one():
     check_codes(x, to_dev(x, torch.float32))
 
 
+@pytest.mark.parametrize("cols", [8, 520, 1032, 1544, 2048])
+def test_codes_of_long_batches(cols):
+    """Rows enough for several a wave; an awkward row among them."""
+    x = tokens(16, "x", 12321, cols, "bf16")
+    x[100] = 0
+    x[12320] *= np.float32(2.0 ** -120)
+    x[6000, 3] = np.nan
+    check_codes(x, to_dev(x, torch.bfloat16))
+    if cols > 8:
+        check_codes(x[:, :cols - 8], to_dev(x, torch.bfloat16)[:, :cols - 8])
+
+
 def test_matrix_of_a_weight():
     x = gen.normal(15, "w", (3, 5, 300))
     m = tr.I8Matrix.quantize(to_dev(x, torch.float32))
@@ -151,6 +163,33 @@ def test_linear_of_many_tokens(N, k, m, act):
             for lo in range(0, N, 499):
                 part = run_linear(xt[lo:lo + 40], W, act, residual=None if res is None else res[lo:lo + 40])
                 assert (torch.from_numpy(part).to(DEV).double() == got[lo:lo + 40]).all()
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+@pytest.mark.parametrize("N,k,m", [(3, 129, 9001), (8, 256, 16392), (15, 2048, 2101), (16, 2112, 8200)])
+def test_linear_of_few_tokens_and_many_columns(N, k, m, act):
+    x, (w, t) = tokens(25, "x", N, k, act), weight(25, "W", m, k)
+    r = gen.to_act(gen.normal(25, "r", (N, m)), act)
+    W, xt, rt = matrix(w, t), to_dev(x, torch_act(act)), to_dev(r, torch_act(act))
+    for guard in (3, 16):
+        within(run_linear(xt, W, act, guard=guard), *i8.linear(x, w, t, act), "y")
+        within(run_linear(xt, W, act, residual=rt, guard=guard), *i8.linear(x, w, t, act, r), "y + residual")
+
+
+def test_linear_of_codes_past_32_bits():
+    """2^24 rows of 256 codes: more than 4 GB of them.  Rows here and there, and at each end."""
+    N, k, m = 1 << 24, 256, 8
+    x0 = to_dev(tokens(26, "x", 4099, k, "bf16"), torch.bfloat16)
+    W = matrix(*weight(26, "W", m, k))
+    x = torch.empty(N, k, dtype=torch.bfloat16, device=DEV)
+    for lo in range(0, N, 4099):
+        x[lo:lo + 4099] = x0[:N - lo]
+    y = torch.full((N, m), float("nan"), dtype=torch.bfloat16, device=DEV)
+    tr.linear_i8(x, W, y, tr.linear_i8_workspace(N, k))
+    y0 = torch.empty(4099, m, dtype=torch.bfloat16, device=DEV)
+    tr.linear_i8(x0, W, y0, tr.linear_i8_workspace(4099, k))
+    at = torch.arange(N, device=DEV) % 4099
+    assert torch.equal(y, y0[at])
 
 
 def test_linear_in_place_and_strided():
@@ -251,6 +290,35 @@ def test_qkv_of_many_tokens(d, H, Hkv, dh):
             assert torch.equal(a, b[lo:lo + 40])
 
 
+def far_apart(mats):
+    """Copies of matrices more than 4 GB from each other, and the memory that holds them."""
+    step = 4352 << 20
+    mem = torch.empty(step * (len(mats) - 1) + mats[-1].codes.numel(), dtype=torch.int8, device=DEV)
+    out = []
+    for i, m in enumerate(mats):
+        codes = mem[i * step:i * step + m.codes.numel()].view(m.codes.shape)
+        codes.copy_(m.codes)
+        out.append(tr.I8Matrix(codes, m.scale, m.cols))
+    return out, mem
+
+
+@pytest.mark.parametrize("N", [7, 300, 4400])
+@pytest.mark.parametrize("d,H,Hkv,dh", [(768, 12, 3, 64), (512, 8, 2, 128)])
+def test_qkv_of_matrices_far_apart(d, H, Hkv, dh, N):
+    cfg = tr.make_cfg(d, H, Hkv, dh, 32, 4, 1, 64, 32, "bf16")
+    tok = to_dev(tokens(33, "n1", N, d, "bf16"), torch.bfloat16)
+    mats = [matrix(*weight(33, n, r * dh, d)) for n, r in (("Wq", H), ("Wk", Hkv), ("Wv", Hkv))]
+    far, mem = far_apart(mats)
+    res = []
+    for ms in (mats, far):
+        out = [torch.full((N, r * dh), 7.0, dtype=torch.bfloat16, device=DEV) for r in (H, Hkv, Hkv)]
+        tr.qkv_i8(cfg, 1, N, tok, tr.DenseI8W(*(m.w for m in ms)), *out,
+                  dirty(tr.workspace_bytes(cfg, tr.OP_QKV_I8, 1, N)))
+        res.append(out)
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
+
+
 # ------------------------------------------------------------------ experts
 def device_lists(eidx, E):
     """exp_cnt, exp_off, exp_rows (of at least one entry: an empty tensor has no address)."""
@@ -289,7 +357,8 @@ class Experts:
         within(npy(got)[rows], want, err, name)
 
 
-MOE = [(1, 64, 64, 1, 1), (1, 768, 512, 8, 2), (3, 128, 192, 4, 3), (32, 256, 512, 4, 1),
+MOE = [(2, 256, 320, 4, 2), (4, 128, 192, 3, 1), (1, 2112, 2304, 3, 4), (2, 768, 2048, 8, 2),
+       (1, 64, 64, 1, 1), (1, 768, 512, 8, 2), (3, 128, 192, 4, 3), (32, 256, 512, 4, 1),
        (33, 192, 64, 2, 2), (100, 320, 448, 6, 4), (128, 256, 512, 4, 1), (333, 512, 704, 8, 2),
        (700, 128, 128, 2, 1), (1100, 192, 320, 5, 2), (64, 2112, 192, 3, 2), (1100, 2112, 192, 3, 2)]
 
@@ -336,6 +405,21 @@ def test_experts_of_many_tokens(N, d, f, E, k):
         assert torch.equal(small.run(c.x[lo:lo + n].contiguous()), got[lo:lo + n])
 
 
+@pytest.mark.parametrize("N", [2, 200, 3000])
+def test_experts_of_matrices_far_apart(N):
+    c = Experts(51, "bf16", N, 256, 512, 3, 2)
+    want = c.run()
+    far, mem = far_apart(c.mats)
+    c.mw = tr.MoeI8W(*(m.w for m in far))
+    assert torch.equal(c.run(), want)
+
+
+def test_experts_of_very_many_tiles():
+    """More than 64 tiles of the large kernels to each CU, and hidden rows of more than 1 GB."""
+    c = Experts(52, "bf16", 34000, 256, 16448, 2, 1)
+    c.check(c.run(), np.unique(np.linspace(0, 33999, 40).astype(int)))
+
+
 @pytest.mark.parametrize("N", [50, 3000])
 def test_experts_keep_bad_tokens_apart(N):
     c = Experts(45, "bf16", N, 128, 192, 3, 2)
@@ -349,6 +433,29 @@ def test_experts_keep_bad_tokens_apart(N):
     for i in (7, N - 1):
         if (c.eidx[i] != 0).any():
             assert torch.isnan(bad[i]).all()
+
+
+@pytest.mark.parametrize("N", [1, 40, 1500])
+def test_experts_of_a_weight_that_is_not_finite(N):
+    """A gate row whose scale is NaN (it held one): every token of that expert is NaN, no other."""
+    c = Experts(49, "bf16", N, 128, 192, 3, 1, [0, N // 3, N // 3, N - N // 3 * 2])
+    good = c.run()
+    c.mats[0].scale[2 * 192 + 77] = float("nan")
+    bad = c.run()
+    at = torch.from_numpy(c.eidx[:, 0] == 3).to(DEV)
+    assert torch.isnan(bad[at]).all() and torch.equal(bad[~at], good[~at])
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [2, 30])
+def test_experts_twice_the_same(N, act):
+    """One expert in both slots of a token."""
+    c = Experts(50, act, N, 128, 192, 3, 2)
+    c.eidx[:, 1] = c.eidx[:, 0] = np.maximum(c.eidx[:, 1], 1)
+    c.t[1] = to_dev(c.eidx, torch.int32)
+    c.t[3:] = device_lists(c.eidx, 3)
+    c.cmp = tr.Compaction(exp_cnt=c.t[3].data_ptr(), exp_off=c.t[4].data_ptr(), exp_rows=c.t[5].data_ptr())
+    c.check(c.run())
 
 
 def test_experts_in_place():
@@ -418,7 +525,8 @@ def layer_i8(L):
     return D, mats, dw, tr.MoeI8W(*(mats[n].w for n in ("Wg", "Wu", "Wd")))
 
 
-@pytest.mark.parametrize("name,B,T", [("tiny_f32_prefill", 1, 128), ("160m_bf16_prefill", 2, 300)])
+@pytest.mark.parametrize("name,B,T", [("tiny_f32_prefill", 1, 128), ("160m_bf16_prefill", 2, 300),
+                                      ("160m_bf16_prefill", 40, 9)])
 @pytest.mark.parametrize("paged", [False, True])
 def test_layer_is_the_chain_of_its_stages(name, B, T, paged):
     """Prefill and decode steps of the composites equal the stage calls bit for bit, over contiguous

@@ -36,7 +36,7 @@ def test_quantize_refuses(over, code, word):
     assert word in tr.lib().triroute_last_error()
 
 
-def linear(act=tr.BF16, n=16, k=100, m=50, x=FAKE, ldx=100, wt=None, res=None, ldr=50, y=FAKE, ldy=50,
+def linear(act=tr.BF16, n=16, k=100, m=50, x=FAKE, ldx=100, wt=None, res=None, ldr=50, y=2 * FAKE, ldy=50,
            ws=FAKE, ws_bytes=1 << 40):
     wt = w() if wt is None else wt
     return tr.lib().triroute_linear_i8(act, n, k, m, x, ldx, C.byref(wt), res, ldr, y, ldy, ws,
@@ -51,7 +51,8 @@ def linear(act=tr.BF16, n=16, k=100, m=50, x=FAKE, ldx=100, wt=None, res=None, l
     (dict(wt=w(codes=None)), -1, b"codes"), (dict(wt=w(scale=None)), -1, b"codes"),
     (dict(wt=w(codes=FAKE + 4)), -1, b"aligned"), (dict(ldx=99), -1, b"x: row stride"),
     (dict(ldy=49), -1, b"y: row stride"), (dict(res=FAKE, ldr=49), -1, b"residual: row stride"),
-    (dict(res=FAKE + 1), -1, b"aligned"), (dict(res=FAKE, ldr=60), -1, b"y's row stride"),
+    (dict(res=FAKE + 1), -1, b"aligned"), (dict(y=2 * FAKE, res=2 * FAKE, ldr=60), -1, b"y's row stride"),
+    (dict(y=FAKE), -1, b"x's place"),
     (dict(ws=FAKE + 16), -1, b"aligned"), (dict(ws_bytes=2047), -3, b"workspace")])
 def test_linear_refuses(over, code, word):
     assert linear(**over) == code
@@ -137,15 +138,28 @@ def test_matrix_takes_whole_rows_of_codes():
             tr.I8Matrix(*bad)
 
 
-def test_tensors_of_other_shapes_are_refused():
+def test_tensors_of_other_shapes_are_refused(monkeypatch):
+    class Stream:  # (no GPU here: tensors of the CPU have the index -1)
+        device_index, cuda_stream = -1, 0
+
+    monkeypatch.setattr(tr, "_i8_stream", lambda s: Stream if s is None else s)
     m = tr.I8Matrix(torch.zeros(5, 128, dtype=torch.int8), torch.zeros(5), 100)
     x, y, ws = torch.zeros(3, 100), torch.zeros(3, 5), torch.zeros(4096, dtype=torch.uint8)
-    for bad in (dict(x=x[:, :99]), dict(y=y[:2]), dict(y=y.bfloat16()), dict(residual=y[:, :4]),
-                dict(x=x.double()), dict(x=torch.zeros(100, 3).T), dict(residual=y.bfloat16())):
+    for bad, word in ((dict(x=x[:, :99]), "x"), (dict(y=y[:2]), "y"), (dict(y=y.bfloat16()), "y"),
+                      (dict(residual=y[:, :4]), "residual"), (dict(x=x.double()), "x"),
+                      (dict(x=torch.zeros(100, 3).T), "contiguous"), (dict(residual=y.bfloat16()), "residual"),
+                      (dict(y=torch.zeros(5, 3).T), "contiguous")):
         a = {**dict(x=x, y=y, residual=None), **bad}
-        with pytest.raises(ValueError):
+        with pytest.raises(ValueError, match=word):
             tr.linear_i8(a["x"], m, a["y"], ws, residual=a["residual"])
-    with pytest.raises(ValueError):
-        tr.i8_quantize(x, torch.zeros(3, 100, dtype=torch.int8), torch.zeros(3))
-    with pytest.raises(ValueError):
-        tr.i8_quantize(x, torch.zeros(3, 128, dtype=torch.int8), torch.zeros(2))
+    Stream.device_index = 0                        # ... and are refused by a stream of a GPU
+    with pytest.raises(ValueError, match="current GPU"):
+        tr.linear_i8(x, m, y, ws)
+    with pytest.raises(ValueError, match="current GPU"):
+        tr.i8_quantize(x, torch.zeros(3, 128, dtype=torch.int8), torch.zeros(3))
+    Stream.device_index = -1
+    for codes, scale in ((torch.zeros(3, 100, dtype=torch.int8), torch.zeros(3)),
+                         (torch.zeros(3, 128, dtype=torch.int8), torch.zeros(2)),
+                         (torch.zeros(3, 128), torch.zeros(3))):
+        with pytest.raises(ValueError):
+            tr.i8_quantize(x, codes, scale)
