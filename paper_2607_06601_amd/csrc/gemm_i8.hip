@@ -833,6 +833,10 @@ hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
       e = launch<P, 64, 128, 2, 2, 64, 3>(p, K2, Nk / 64 + E, c64, st);
     } else if (!w4) {
       e = launch<P, 128, 128, 4, 2, 64, 3>(p, K2, Nk / 128 + E, c64, st);
+    } else if (row_tiles(128) * c64 <= 2 * cu_count()) {
+      // one round, two blocks a CU (410M, 333 tokens, 352 tiles: the block 39.5 -> 38.0 us; 160M, 1150
+      // tokens, 512: 52.4 -> 50.7; more tiles take longer here)
+      e = launch<P, 128, 128, 2, 2, 64, 2>(p, K2, Nk / 128 + E, c64, st);
     } else if constexpr (!decltype(f64)::value) {
       if (tile_cost(row_tiles(128) * ny, 1.f) < tile_cost(row_tiles(256) * ny, 1.77f))
         e = launch_w4<P, 128, 256>(p, K2, Nk / 128 + E, ny, st);
