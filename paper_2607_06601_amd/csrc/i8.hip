@@ -75,11 +75,11 @@ __global__ __launch_bounds__(256) void i8_rows_kernel(const T *__restrict__ x, i
 // while it codes one (16384 rows of 2048, bf16: 22 us, a row a wave 26).
 typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
 template <int RR>
-__global__ __launch_bounds__(256) void i8_stream_kernel(const bf16 *__restrict__ x, int64_t ldx, int64_t rows,
-                                                        int cols, int pitch, int8_t *__restrict__ codes,
-                                                        float *__restrict__ scale) {
+__device__ __forceinline__ void stream_body(const bf16 *__restrict__ x, int64_t ldx, int64_t rows,
+                                            int cols, int pitch, int8_t *__restrict__ codes,
+                                            float *__restrict__ scale, int blocks) {
   const int at = (threadIdx.x & 63) * 8;
-  const int64_t step = int64_t(gridDim.x) * 4;
+  const int64_t step = int64_t(blocks) * 4;
   uint4 next[RR];
   auto fetch = [&](int64_t row) {
 #pragma unroll
@@ -119,19 +119,42 @@ __global__ __launch_bounds__(256) void i8_stream_kernel(const bf16 *__restrict__
   }
 }
 
+template <int RR>
+__global__ __launch_bounds__(256) void i8_stream_kernel(const bf16 *__restrict__ x, int64_t ldx, int64_t rows,
+                                                        int cols, int pitch, int8_t *__restrict__ codes,
+                                                        float *__restrict__ scale) {
+  stream_body<RR>(x, ldx, rows, cols, pitch, codes, scale, gridDim.x);
+}
+
 // The same of N rows in the first blocks, and in the others the rotation table that the product
-// behind it reads too (a launch less: QKV 410M, 64 tokens 14.7 -> 12.4 us).
-template <typename T, int W, int RR>
+// behind it reads too (a launch less: QKV 410M, 64 tokens 14.7 -> 12.4 us).  STREAM: many bf16 rows, as
+// above (QKV 1.3B, 16384 tokens, this launch 27.1 -> 24.8 us).
+template <typename T, bool STREAM, int W, int RR>
 __global__ __launch_bounds__(256) void i8_rows_rope_kernel(const T *__restrict__ x, int N, int cols,
                                                            int pitch, int8_t *__restrict__ codes,
                                                            float *__restrict__ scale, int blocks,
                                                            RopeJob job) {
   if (int(blockIdx.x) < blocks) {
-    rows_body<T, true, W, RR>(x, cols, N, nullptr, cols, pitch, codes, scale, blocks);
+    if constexpr (STREAM) stream_body<RR>(x, cols, N, cols, pitch, codes, scale, blocks);
+    else rows_body<T, true, W, RR>(x, cols, N, nullptr, cols, pitch, codes, scale, blocks);
   } else {
     const int64_t at = int64_t(blockIdx.x - blocks) * 256 + threadIdx.x;
     if (at < int64_t(N) * job.hd) job.tab[at] = rope_entry(job, int(at / job.hd), int(at % job.hd));
   }
+}
+
+// Blocks of the stream of rows, 0 where there are too few (from two rows a wave on; fp32 rows are at
+// the memory's rate without).
+static int stream_blocks(int64_t rows, int cols) {
+  const int waves = cu_count() * 24;
+  return cols <= 2048 && rows >= 2 * waves ? waves / 4 : 0;
+}
+template <class F>
+static void by_pieces(int pitch, F run) {
+  if (pitch <= 512) run(std::integral_constant<int, 1>{});
+  else if (pitch <= 1024) run(std::integral_constant<int, 2>{});
+  else if (pitch <= 1536) run(std::integral_constant<int, 3>{});
+  else run(std::integral_constant<int, 4>{});
 }
 
 // d_rows (or NULL): a device count that ends the rows earlier
@@ -139,17 +162,11 @@ static hipError_t launch_rows(int act, int64_t rows, const int32_t *d_rows, int 
                               int64_t ldx, int8_t *codes, float *scale, hipStream_t st) {
   const int es = act == TRIROUTE_BF16 ? 2 : 4, pitch = i8_pitch(cols);
   const bool vec = cols % 8 == 0 && ((uintptr_t(x) | uintptr_t(ldx * es)) & 15) == 0;
-  // (from two rows a wave on; fp32 rows are at the memory's rate without)
-  const int waves = cu_count() * 24;
-  if (vec && act == TRIROUTE_BF16 && cols <= 2048 && rows >= 2 * waves) {
-    auto stream = [&](auto rr) {
-      i8_stream_kernel<decltype(rr)::value><<<dim3(waves / 4), 256, 0, st>>>((const bf16 *)x, ldx, rows, cols,
-                                                                             pitch, codes, scale);
-    };
-    if (pitch <= 512) stream(std::integral_constant<int, 1>{});
-    else if (pitch <= 1024) stream(std::integral_constant<int, 2>{});
-    else if (pitch <= 1536) stream(std::integral_constant<int, 3>{});
-    else stream(std::integral_constant<int, 4>{});
+  if (const int blocks = vec && act == TRIROUTE_BF16 ? stream_blocks(rows, cols) : 0) {
+    by_pieces(pitch, [&](auto rr) {
+      i8_stream_kernel<decltype(rr)::value><<<dim3(blocks), 256, 0, st>>>((const bf16 *)x, ldx, rows, cols,
+                                                                          pitch, codes, scale);
+    });
     return hipGetLastError();
   }
   auto run = [&](auto tag, auto v, auto w) {
@@ -181,12 +198,19 @@ hipError_t launch_i8_rows_rope(int act, int N, int cols, const void *x, int8_t *
                                const RopeJob &job, hipStream_t st) {
   const int pitch = i8_pitch(cols);
   const unsigned table = unsigned((int64_t(N) * job.hd + 255) / 256);
+  if (const int blocks = act == TRIROUTE_BF16 ? stream_blocks(N, cols) : 0) {
+    by_pieces(pitch, [&](auto rr) {
+      i8_rows_rope_kernel<bf16, true, 1, decltype(rr)::value><<<dim3(blocks + table), 256, 0, st>>>(
+          (const bf16 *)x, N, cols, pitch, codes, scale, blocks, job);
+    });
+    return hipGetLastError();
+  }
   auto run = [&](auto tag, auto w) {
     using T = decltype(tag);
     constexpr int W = decltype(w)::value;
-    const int blocks = (N * W + 3) / 4;
-    i8_rows_rope_kernel<T, W, 4><<<dim3(blocks + table), 256, 0, st>>>((const T *)x, N, cols, pitch, codes,
-                                                                       scale, blocks, job);
+    const int blocks = int(std::min<int64_t>((int64_t(N) * W + 3) / 4, 1 << 20));
+    i8_rows_rope_kernel<T, false, W, 4><<<dim3(blocks + table), 256, 0, st>>>(
+        (const T *)x, N, cols, pitch, codes, scale, blocks, job);
   };
   auto by_width = [&](auto tag) {
     if (cols > 2048) run(tag, std::integral_constant<int, 4>{});

@@ -319,6 +319,26 @@ def test_qkv_of_matrices_far_apart(d, H, Hkv, dh, N):
         assert torch.equal(a, b)
 
 
+def test_qkv_of_very_many_long_tokens():
+    """More blocks of rows than one launch has: each block takes several."""
+    N, d, many = (1 << 20) + 5, 2112, 4099
+    cfg = tr.make_cfg(d, 1, 1, 64, 32, 4, 1, 64, 32, "bf16")
+    tok0 = to_dev(tokens(34, "n1", many, d, "bf16"), torch.bfloat16)
+    tok = torch.empty(N, d, dtype=torch.bfloat16, device=DEV)
+    for lo in range(0, N, many):
+        tok[lo:lo + many] = tok0[:N - lo]
+    mats = [matrix(*weight(34, n, 64, d)) for n in ("Wq", "Wk", "Wv")]
+    res = []
+    for t in (tok, tok0):
+        out = [torch.full((len(t), 64), float("nan"), dtype=torch.bfloat16, device=DEV) for _ in range(3)]
+        tr.qkv_i8(cfg, len(t), 1, t, tr.DenseI8W(*(m.w for m in mats)), *out,
+                  tr.workspace(cfg, tr.OP_QKV_I8, len(t), 1))
+        res.append(out)
+    at = torch.arange(N, device=DEV) % many
+    for a, b in zip(*res):
+        assert torch.equal(a, b[at])
+
+
 # ------------------------------------------------------------------ experts
 def device_lists(eidx, E):
     """exp_cnt, exp_off, exp_rows (of at least one entry: an empty tensor has no address)."""
