@@ -47,7 +47,7 @@ __device__ __forceinline__ void block_row(const P &p, const MTile &t, int r, int
     for (int k = 0; k < KS; ++k) ss += red[k];
     const double inv = p.inv_norm(ss);
 #pragma unroll
-    for (int q = 0; q < 2; ++q) norm8<typename P::elem>(gv[q], inv, v[q]);
+    for (int q = 0; q < 2; ++q) norm8<typename P::elem>(gv[q], inv, norm_large(ss), v[q]);
   }
   uint32_t m = 0;
 #pragma unroll
@@ -79,16 +79,16 @@ __device__ __forceinline__ void tile_rows(const P &p, const MTile &t, int pitch,
     const int lane = threadIdx.x & 63;
     for (int r = threadIdx.x >> 6; r < t.mvalid; r += KS) {
       const auto row = p.row(t, r);
-      double inv = 0.0;
+      double inv = 0.0, ss = 0.0;
       if constexpr (P::NORM) {
-        double ss = 0.0;
         for (int c = lane * 8; c < pitch; c += 512) {
           float v[8];
           p.load(row, c, v);
 #pragma unroll
           for (int j = 0; j < 8; ++j) ss = fma(double(v[j]), double(v[j]), ss);
         }
-        inv = p.inv_norm(wave_sum(ss));
+        ss = wave_sum(ss);
+        inv = p.inv_norm(ss);
       }
       const float s = wave_row(
           [&](int c, float *v) {
@@ -96,7 +96,7 @@ __device__ __forceinline__ void tile_rows(const P &p, const MTile &t, int pitch,
             if constexpr (P::NORM) {
               float gv[8];
               p.gains(c, gv);
-              norm8<typename P::elem>(gv, inv, v);
+              norm8<typename P::elem>(gv, inv, norm_large(ss), v);
             }
           },
           pitch, lane, panel + r * (pitch + FEW_PAD));

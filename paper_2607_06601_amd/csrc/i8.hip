@@ -226,7 +226,9 @@ hipError_t launch_i8_rows_rope(int act, int N, int cols, const void *x, int8_t *
 // ENTRY: one wave per entry of the expert lists (token rows[pos] / k to row pos, and slot_of),
 // else one wave per token, to the rows slot_of names.  W waves a row; rows of up to 512 W RR
 // elements stay in registers, longer ones are read and normalised again for the codes.  (Few rows: four
-// waves on each, 1.3B, 32 tokens, 8.4 -> 4.8 us.)
+// waves on each, 1.3B, 32 tokens, 8.4 -> 4.8 us.  Many: the arithmetic bounds it, in 64 bits, then the
+// codes; the next token fetched ahead, and the gains held, gave 19.8 -> 18.8 us at 160M, 16384 tokens, and nothing
+// at 1.3B, 36.6.)
 template <typename T, bool ENTRY, int W, int RR>
 __global__ __launch_bounds__(256) void i8_norm_kernel(
     const T *__restrict__ x, const T *__restrict__ g, const int32_t *__restrict__ rows,
@@ -267,12 +269,13 @@ __global__ __launch_bounds__(256) void i8_norm_kernel(
     ss = (part[0] + part[1]) + (part[2] + part[3]);
   }
   const double r = 1.0 / sqrt(ss / double(d) + double(eps));
+  const bool large = norm_large(ss);
   uint32_t m = 0;
   auto normed = [&](int c, float *w) {
     if (c >= d) return;
     float gv[8];
     load8(g + c, gv);
-    norm8<T>(gv, r, w);
+    norm8<T>(gv, r, large, w);
 #pragma unroll
     for (int j = 0; j < 8; ++j) m = max(m, abs_bits(w[j]));
   };

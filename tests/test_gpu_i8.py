@@ -406,7 +406,9 @@ def test_experts_without_a_real_one(act):
     assert torch.equal(c.run(), c.x)
 
 
-@pytest.mark.parametrize("N,d,f,E,k", [(6000, 256, 512, 4, 2), (9000, 512, 832, 8, 2), (5000, 128, 1408, 2, 1)])
+@pytest.mark.parametrize("N,d,f,E,k", [(6000, 256, 512, 4, 2), (9000, 512, 832, 8, 2), (5000, 128, 1408, 2, 1),
+                                       (12400, 64, 64, 7, 3), (14000, 768, 256, 8, 2), (12289, 1088, 128, 3, 2),
+                                       (12300, 2048, 64, 4, 1)])
 def test_experts_of_many_tokens(N, d, f, E, k):
     """The large tiles; a token's result does not depend on the other tokens, so small batches
     give the same bits."""
@@ -476,6 +478,24 @@ def test_experts_twice_the_same(N, act):
     c.t[3:] = device_lists(c.eidx, 3)
     c.cmp = tr.Compaction(exp_cnt=c.t[3].data_ptr(), exp_off=c.t[4].data_ptr(), exp_rows=c.t[5].data_ptr())
     c.check(c.run())
+
+
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [1, 60, 2600, 13000])
+def test_experts_of_the_largest_and_smallest_tokens(N, act):
+    """Tokens whose products with the gains leave the range of fp32 on the way, or whose squares
+    are far below eps: n2 itself is an ordinary number, or 1000 times the token."""
+    if act == "f32" and N > 60:
+        N = 333
+    c = Experts(53, act, N, 128, 192, 3, 2)
+    g2 = gen.to_act(np.where(np.arange(128) % 2, 8.0, -1.5).astype(np.float32), act)
+    c.g2, c.t[0] = g2, to_dev(g2, torch_act(act))
+    c.dw = tr.DenseI8W(g2=c.t[0].data_ptr())
+    for i, f in {N - 1: 2.0 ** -100, N // 2: 2.0 ** 110, 0: 2.0 ** 122}.items():
+        c.xt[i] = gen.to_act(c.xt[i] * np.float32(f), act)
+    assert np.isfinite(c.xt).all()
+    c.x = to_dev(c.xt, torch_act(act))
+    c.check(c.run(), np.unique(np.concatenate([[0, N // 2, N - 1], np.linspace(0, N - 1, 60).astype(int)])))
 
 
 def test_experts_in_place():
