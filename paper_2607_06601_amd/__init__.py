@@ -463,8 +463,8 @@ class I8Matrix:
 
     @classmethod
     def quantize(cls, x, stream=None):
-        x = x.reshape(-1, x.shape[-1])
         with torch.cuda.stream(stream) if stream is not None else nullcontext():
+            x = x.reshape(-1, x.shape[-1])
             codes = torch.empty(x.shape[0], i8_pitch(x.shape[1]), dtype=torch.int8, device=x.device)
             scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
         i8_quantize(x, codes, scale, stream)

@@ -45,9 +45,10 @@ __device__ __forceinline__ void block_row(const P &p, const MTile &t, int r, int
     ss = 0.0;
 #pragma unroll
     for (int k = 0; k < KS; ++k) ss += red[k];
-    const double inv = p.inv_norm(ss);
+    double inv = p.inv_norm(ss);
+    norm_range(ss, inv, v);
 #pragma unroll
-    for (int q = 0; q < 2; ++q) norm8<typename P::elem>(gv[q], inv, norm_large(ss), v[q]);
+    for (int q = 0; q < 2; ++q) norm8<typename P::elem>(gv[q], inv, v[q]);
   }
   uint32_t m = 0;
 #pragma unroll
@@ -94,9 +95,15 @@ __device__ __forceinline__ void tile_rows(const P &p, const MTile &t, int pitch,
           [&](int c, float *v) {
             p.load(row, c, v);
             if constexpr (P::NORM) {
-              float gv[8];
+              float gv[8], w[1][8];
+              double r = inv;
               p.gains(c, gv);
-              norm8<typename P::elem>(gv, inv, norm_large(ss), v);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) w[0][j] = v[j];
+              norm_range(ss, r, w);
+              norm8<typename P::elem>(gv, r, w[0]);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[j] = w[0][j];
             }
           },
           pitch, lane, panel + r * (pitch + FEW_PAD));

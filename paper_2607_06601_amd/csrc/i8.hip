@@ -268,16 +268,22 @@ __global__ __launch_bounds__(256) void i8_norm_kernel(
     __syncthreads();
     ss = (part[0] + part[1]) + (part[2] + part[3]);
   }
-  const double r = 1.0 / sqrt(ss / double(d) + double(eps));
-  const bool large = norm_large(ss);
+  double r = 1.0 / sqrt(ss / double(d) + double(eps));
+  if constexpr (KEEP) norm_range(ss, r, v);
   uint32_t m = 0;
   auto normed = [&](int c, float *w) {
     if (c >= d) return;
     float gv[8];
     load8(g + c, gv);
-    norm8<T>(gv, r, large, w);
+    norm8<T>(gv, r, w);
 #pragma unroll
     for (int j = 0; j < 8; ++j) m = max(m, abs_bits(w[j]));
+  };
+  auto again = [&](int c) {  // a piece that was not kept
+    const double kept = r;
+    norm_range(ss, r, v);
+    normed(c, v[0]);
+    r = kept;
   };
   if constexpr (KEEP) {
 #pragma unroll
@@ -285,7 +291,7 @@ __global__ __launch_bounds__(256) void i8_norm_kernel(
   } else {
     for (int c = at; c < d; c += STEP) {
       load8(xr + c, v[0]);
-      normed(c, v[0]);
+      again(c);
     }
   }
   m = wave_umax(m);
@@ -313,7 +319,7 @@ __global__ __launch_bounds__(256) void i8_norm_kernel(
   } else {
     for (int c = at; c < pitch; c += STEP) {
       row8<T, true>(xr, c, d, v[0]);
-      normed(c, v[0]);
+      again(c);
       emit(c, rc.code8(v[0]));
     }
   }

@@ -119,22 +119,29 @@ __device__ __forceinline__ void row8(const T *row, int c, int cols, float *v) {
   }
 }
 
-// A row's sum of squares (the same in all lanes) from which its products with the gains may leave
-// fp32; gains are below 2^28.
-__device__ __forceinline__ bool norm_large(double ss) {
-  return __builtin_amdgcn_readfirstlane(ss > 0x1p200);
+// A row whose products with the gains (below 2^28) may leave fp32 is normalised from values 2^64
+// times smaller, in one branch for its NP pieces.  ss: its sum of squares, the same in all lanes.
+// (What that takes below fp32's range is far below half a code.)
+template <int NP>
+__device__ __forceinline__ void norm_range(double ss, double &r, float (&v)[NP][8]) {
+  if (__builtin_amdgcn_readfirstlane(ss > 0x1p200)) {
+    r *= 0x1p64;
+#pragma unroll
+    for (int q = 0; q < NP; ++q)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[q][j] *= 0x1p-64f;
+  }
 }
 
-// v *= g / norm for 8 elements of type T, in fp64 and rounded once to fp32 (r: the row's 1 / norm;
-// large: as above).
+// v *= g / norm for 8 elements of type T, in fp64 and rounded once to fp32 (r: the row's 1 / norm).
 template <typename T>
-__device__ __forceinline__ void norm8(const float *gv, double r, bool large, float *v) {
-  if (sizeof(T) == 4 || large) {
+__device__ __forceinline__ void norm8(const float *gv, double r, float *v) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = float((double(v[j]) * r) * double(gv[j]));
-  } else {  // (the product of two bf16 numbers is an fp32 number)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = float(double(v[j] * gv[j]) * r);
+  for (int j = 0; j < 8; ++j) {
+    if constexpr (sizeof(T) == 2)  // (the product of two bf16 numbers is an fp32 number)
+      v[j] = float(double(v[j] * gv[j]) * r);
+    else
+      v[j] = float((double(v[j]) * r) * double(gv[j]));
   }
 }
 

@@ -481,14 +481,15 @@ def test_experts_twice_the_same(N, act):
 
 
 @pytest.mark.parametrize("act", ["bf16", "f32"])
-@pytest.mark.parametrize("N", [1, 60, 2600, 13000])
-def test_experts_of_the_largest_and_smallest_tokens(N, act):
+@pytest.mark.parametrize("N,d", [(1, 128), (60, 128), (2600, 128), (13000, 128), (1, 8256), (2, 4224), (60, 8256),
+                                 (1100, 2112)])
+def test_experts_of_the_largest_and_smallest_tokens(N, d, act):
     """Tokens whose products with the gains leave the range of fp32 on the way, or whose squares
     are far below eps: n2 itself is an ordinary number, or 1000 times the token."""
     if act == "f32" and N > 60:
         N = 333
-    c = Experts(53, act, N, 128, 192, 3, 2)
-    g2 = gen.to_act(np.where(np.arange(128) % 2, 8.0, -1.5).astype(np.float32), act)
+    c = Experts(53, act, N, d, 192, 3, 2)
+    g2 = gen.to_act(np.where(np.arange(d) % 2, 8.0, -1.5).astype(np.float32), act)
     c.g2, c.t[0] = g2, to_dev(g2, torch_act(act))
     c.dw = tr.DenseI8W(g2=c.t[0].data_ptr())
     for i, f in {N - 1: 2.0 ** -100, N // 2: 2.0 ** 110, 0: 2.0 ** 122}.items():
