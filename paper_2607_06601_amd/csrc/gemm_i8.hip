@@ -122,7 +122,7 @@ __device__ __forceinline__ uint32_t part_max(uint32_t m, float row) {
 // Largest of 4 or 8 lanes side by side.
 template <int LANES>
 __device__ __forceinline__ uint32_t lanes_umax(uint32_t v) {
-#define TR_DPP(c) uint32_t(__builtin_amdgcn_update_dpp(int(v), int(v), c, 0xF, 0xF, false))
+#define TR_DPP(c) uint32_t(__builtin_amdgcn_update_dpp(0, int(v), c, 0xF, 0xF, true))
   v = max(v, TR_DPP(0xB1));                             // quad_perm 1 0 3 2
   v = max(v, TR_DPP(0x4E));                             // quad_perm 2 3 0 1
   if constexpr (LANES == 8) v = max(v, TR_DPP(0x141));  // row_half_mirror

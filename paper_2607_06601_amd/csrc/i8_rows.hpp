@@ -19,7 +19,7 @@ __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v
 
 // Largest magnitude of a row, as the bits of |x|: as whole numbers NaN > inf > finite.
 __device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
-#define TR_ROR(n) uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x120 + (n), 0xF, 0xF, false))
+#define TR_ROR(n) uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x120 + (n), 0xF, 0xF, true))
   v = max(v, TR_ROR(1));
   v = max(v, TR_ROR(2));
   v = max(v, TR_ROR(4));
