@@ -567,7 +567,8 @@ def layer_i8(L):
 
 
 @pytest.mark.parametrize("name,B,T", [("tiny_f32_prefill", 1, 128), ("160m_bf16_prefill", 2, 300),
-                                      ("160m_bf16_prefill", 40, 9)])
+                                      ("160m_bf16_prefill", 40, 9), ("160m_bf16_prefill", 1, 5),
+                                      ("160m_bf16_prefill", 3, 4)])
 @pytest.mark.parametrize("paged", [False, True])
 def test_layer_is_the_chain_of_its_stages(name, B, T, paged):
     """Prefill and decode steps of the composites equal the stage calls bit for bit, over contiguous
