@@ -672,6 +672,22 @@ static int rows_a_launch(int c64, int pitch) {
   return int(std::min(int64_t(std::max(1, (1 << 22) / c64)) * 32, near));
 }
 
+// K groups of a block where there is one a CU at most: the chain of K steps is that much shorter, and
+// sums of whole numbers may be split anywhere, evenly or not, so a token's result stays the same (300 x
+// 8000 -> 100: 21.2 us, two groups 23.6, one 30.7; 64 x 8192 -> 4096: 21.2, two 23.4; QKV 64 x 2112:
+// 10.9, 11.6, 12.8; 160M experts, 4 tokens: 22.9, two 23.5).
+static int k_groups(int blocks, int K2) {
+  return blocks > cu_count() || K2 < 128 ? 1 : K2 < 256 ? 2 : 4;
+}
+// 32 x 64 tiles
+template <class P>
+static hipError_t launch_32(const P &p, int K2, int m_tiles, int n_tiles, int blocks, hipStream_t st) {
+  const int groups = k_groups(blocks, K2);
+  if (groups == 4) return launch<P, 32, 64, 2, 1, 64, 3, 4>(p, K2, m_tiles, n_tiles, st);
+  if (groups == 2) return launch<P, 32, 64, 2, 1, 64, 4, 2>(p, K2, m_tiles, n_tiles, st);
+  return launch<P, 32, 64, 2, 1, 64, 4>(p, K2, m_tiles, n_tiles, st);
+}
+
 template <class P>
 static hipError_t linear_rows(const P &all, hipStream_t st) {
   const int K2 = all.pitch / 2, c64 = (all.m + 63) / 64, c128 = (all.m + 127) / 128;
@@ -691,10 +707,8 @@ static hipError_t linear_rows(const P &all, hipStream_t st) {
       w4 = K2 >= 128 && span32({{p.a, size_t(p.N) * p.pitch}}, &lo) &&
            span32({{p.w, size_t(p.m) * p.pitch}}, &lo) &&
            std::max(p.ldy, p.ldr) < (1 << 22) && w4_rounds(p.N, c128, tile_cost(m256 * c256, COST_256X256));
-    if (few_tiles(p.N, c128) && split_k(m32 * c64, K2))
-      e = launch<P, 32, 64, 2, 1, 64, 4, 2>(p, K2, m32, c64, st);
-    else if (few_tiles(p.N, c128))
-      e = launch<P, 32, 64, 2, 1, 64, 4>(p, K2, m32, c64, st);
+    if (few_tiles(p.N, c128))
+      e = launch_32(p, K2, m32, c64, m32 * c64, st);
     else if (!w4)
       e = launch_mid(p, K2, p.N, c128, st);
     else if constexpr (P::WIDE)
@@ -766,14 +780,10 @@ hipError_t i8_qkv(const triroute_cfg &cfg, int N, const int8_t *a, const float *
              span32({{p.Wq, size_t(p.Hd) * p.pitch}}, &lo) &&
              w4_rounds(p.N, c128, tile_cost(m256 * c256, COST_256X256));
       if (few_tiles(p.N, c128)) {
-        // (two K groups: whole numbers, so a token's keys stay the same in every tile; QKV 410M, 64
-        // tokens 7.3 -> 6.4 us)
         const int m32 = (p.N + 31) / 32;
-        if (p.dh == 64 && split_k(m32 * c64, K2))
-          e = launch<QkvI8<T>, 32, 64, 2, 1, 64, 4, 2>(p, K2, m32, c64, st);
-        else if (p.dh == 64)
-          e = launch<QkvI8<T>, 32, 64, 2, 1, 64, 4>(p, K2, m32, c64, st);
-        else if (split_k(m32 * c64 / 2, K2))
+        if (p.dh == 64)
+          e = launch_32(p, K2, m32, c64, m32 * c64, st);
+        else if (k_groups(m32 * c64 / 2, K2) > 1)
           e = launch<QkvI8<T>, 32, 128, 2, 2, 64, 3, 2>(p, K2, m32, c64 / 2, st);
         else
           e = launch<QkvI8<T>, 32, 128, 2, 2, 64, 4>(p, K2, m32, c64 / 2, st);
@@ -823,12 +833,11 @@ hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
     hipError_t e = hipErrorInvalidValue;
     const int c64 = (dff + 63) / 64;
     // Gate/up: as the bf16 product's rule (times of the two kernels measured alike), but 32-row tiles
-    // with two K groups where they leave CUs without a tile (160M, 1 token: 5.6 -> 5.1 us).
+    // with K groups where they leave CUs without a tile (160M, 1 token, two: 5.6 -> 5.1 us).
     const bool small = r <= 24 || (decltype(f64)::value && row_tiles(32) * ((dff + 31) / 32) <= 4 * cu_count());
-    if (small && split_k(row_tiles(32) * ((dff + 31) / 32), K2)) {
-      e = launch<P, 32, 64, 2, 1, 64, 4, 2>(p, K2, Nk / 32 + E, (dff + 31) / 32, st);
-    } else if (small) {
-      e = launch<P, 32, 64, 2, 1, 64, 4>(p, K2, Nk / 32 + E, (dff + 31) / 32, st);
+    if (small) {
+      const int c32 = (dff + 31) / 32;
+      e = launch_32(p, K2, Nk / 32 + E, c32, row_tiles(32) * c32, st);
     } else if (r <= 64) {
       e = launch<P, 64, 128, 2, 2, 64, 3>(p, K2, Nk / 64 + E, c64, st);
     } else if (!w4) {
@@ -860,15 +869,14 @@ hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
   p.pitch = i8_pitch(dff);
   const int K2 = p.pitch / 2, c64 = (d + 63) / 64, c128 = (d + 127) / 128, c256 = (d + 255) / 256;
   const int8_t *lo;
-  // Down.  Few columns and a long K: 32-row tiles up to two a CU, with two K groups up to one
-  // (160M, 1 token 8.0 -> 6.3 us, 410M, 64 tokens 10.2 -> 8.0; 410M, 333 tokens, 384 tiles: 12.4, 64-row
+  // Down.  Few columns and a long K: 32-row tiles up to two a CU, with K groups up to one (two: 160M, 1
+  // token 8.0 -> 6.3 us, 410M, 64 tokens 10.2 -> 8.0; 410M, 333 tokens, 384 tiles: 12.4, 64-row
   // tiles 14.5; 1.3B, 32 tokens, 512: 34, 64-row tiles of two stages 44), then 64-row tiles (410M, 1000
   // tokens, 256 tiles: 17.1, 32-row 25.1, 128-row 19.4), from about 400 on the four-wave
   // kernel (1.3B, 1000 tokens, 512 tiles: 60, 64-row 72; 2500 tokens 97 and, of 256 rows, 90, 128-row
   // tiles 109).
   const int t32 = row_tiles(32) * c64;
-  if (split_k(t32, K2)) return launch<Moe2I8, 32, 64, 2, 1, 64, 4, 2>(p, K2, Nk / 32 + E, c64, st);
-  if (t32 <= 2 * cu_count()) return launch<Moe2I8, 32, 64, 2, 1, 64, 4>(p, K2, Nk / 32 + E, c64, st);
+  if (t32 <= 2 * cu_count()) return launch_32(p, K2, Nk / 32 + E, c64, t32, st);
   if (row_tiles(64) * c128 <= 400) return launch<Moe2I8, 64, 128, 2, 2, 64, 3>(p, K2, Nk / 64 + E, c128, st);
   if (K2 < 128 || !span32({{p.Wd, size_t(E) * d * p.pitch}}, &lo) ||
       !span32({{p.a, size_t(Nk) * p.pitch}}, &lo))

@@ -174,7 +174,10 @@ __global__ __launch_bounds__(64 * WM * WN * KW, 1) void gemm_mfma_kernel(P p, in
   const int kg = KW > 1 ? (tid >> 6) / NW : 0, wave = KW > 1 ? (tid >> 6) % NW : tid >> 6;
   const int wm = wave / WN, wn = wave % WN;
   uint8_t *smem = smem_all + kg * S * STAGE;  // the group's stages
-  const int nk = K / BK / KW;                 // its K steps, from step kg nk on
+  // its K steps, from step kg nk on; of 8-bit operands the last groups may have fewer
+  constexpr bool UNEVEN = Op::INT && KW > 1;
+  const int nk = UNEVEN ? (K / BK + KW - 1) / KW : K / BK / KW;
+  const int own = UNEVEN ? max(min(nk, K / BK - kg * nk), 0) : nk;
   // Transfer j of this wave fills stage rows RPT g .. RPT g + RPT - 1
   // (g = wave IPW + j; A rows first, then B rows).  Lane l writes LDS chunk
   // l % CPR of row RPT g + l / CPR, which holds the source chunk that swz
@@ -208,12 +211,13 @@ __global__ __launch_bounds__(64 * WM * WN * KW, 1) void gemm_mfma_kernel(P p, in
     for (int j = 0; j < NI; ++j) acc[i][j] = typename Op::acc{0, 0, 0, 0};
 #pragma unroll
   for (int s0 = 0; s0 < S - 1; ++s0)
-    if (s0 < nk) issue(s0, s0);
+    if (s0 < own) issue(s0, s0);
   for (int kt = 0; kt < nk; ++kt) {
     // stage kt has landed once at most the later stages' transfers are out
-    wait_stages<IPW, S>(min(S - 2, nk - 1 - kt));
+    wait_stages<IPW, S>(min(S - 2, own - 1 - kt));
     __syncthreads();  // every wave's part of stage kt is in; stage kt-1 is free
-    if (kt + S - 1 < nk) issue(kt + S - 1, (kt + S - 1) % S);
+    if (kt + S - 1 < own) issue(kt + S - 1, (kt + S - 1) % S);
+    if (UNEVEN && kt >= own) continue;  // (the barriers are all groups')
     const uint8_t *As = smem + (kt % S) * STAGE;
     const uint8_t *Bs = As + BM * RB;
 #pragma unroll

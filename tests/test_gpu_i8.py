@@ -119,6 +119,7 @@ def run_linear(x, W, act, residual=None, guard=3):
 
 LINEAR = [(1, 1, 1), (1, 768, 768), (2, 3, 5), (31, 64, 63), (32, 128, 64), (33, 129, 65),
           (64, 1000, 300), (65, 256, 1024), (127, 512, 129), (128, 128, 128), (130, 1001, 517),
+          (100, 640, 300), (40, 1150, 70), (70, 1200, 64), (50, 300, 130), (60, 8000, 200),
           (200, 2048, 2048), (257, 384, 256), (300, 96, 1537), (1000, 5632, 128), (513, 640, 1280)]
 
 
@@ -235,6 +236,7 @@ def test_linear_sums_are_exact_at_the_longest_rows():
 @pytest.mark.parametrize("d,H,Hkv,dh,B,T,far", [
     (64, 1, 1, 64, 1, 1, 0), (64, 1, 1, 128, 1, 1, 7), (768, 12, 3, 64, 3, 5, 100000),
     (1024, 16, 4, 64, 64, 1, 8192), (192, 5, 1, 64, 2, 33, 50), (320, 3, 3, 128, 1, 130, 1 << 20),
+    (576, 8, 2, 64, 40, 1, 9), (1152, 2, 1, 128, 50, 1, 9), (1088, 2, 2, 64, 33, 1, 9),
     (2048, 16, 4, 128, 2, 100, 4096), (256, 6, 2, 64, 1, 700, 0), (512, 2, 1, 128, 3, 300, 3)])
 def test_qkv(d, H, Hkv, dh, B, T, far, act):
     cfg = tr.make_cfg(d, H, Hkv, dh, 32, 4, 1, 64, 32, act)
@@ -379,7 +381,7 @@ class Experts:
 
 MOE = [(2, 256, 320, 4, 2), (4, 128, 192, 3, 1), (1, 2112, 2304, 3, 4), (2, 768, 2048, 8, 2),
        (1, 64, 64, 1, 1), (1, 768, 512, 8, 2), (3, 128, 192, 4, 3), (32, 256, 512, 4, 1),
-       (33, 192, 64, 2, 2), (100, 320, 448, 6, 4), (128, 256, 512, 4, 1), (333, 512, 704, 8, 2),
+       (20, 576, 1152, 3, 1), (60, 960, 2112, 8, 2), (33, 192, 64, 2, 2), (100, 320, 448, 6, 4), (128, 256, 512, 4, 1), (333, 512, 704, 8, 2),
        (700, 128, 128, 2, 1), (1100, 192, 320, 5, 2), (64, 2112, 192, 3, 2), (1100, 2112, 192, 3, 2)]
 
 
