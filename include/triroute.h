@@ -698,9 +698,8 @@ int triroute_qkv_i8(const triroute_cfg *cfg, int B, int T, const void *n1,
 /* triroute_moe with 8-bit weights.  The normalised token (computed in fp64, rounded once to fp32)
  * and the hidden row h = silu(G) U are quantised, each with one scale; products as in
  * triroute_linear_i8, gates and the sum over slots as in triroute_moe (fp32).  Before it is quantised
- * h is held in fp32; with bf16 tokens and more than 4 assignments (n_tok * top_k) in the call, as
- * whole numbers in +-32767 of the largest magnitude of each 32 units.  But for that a token's result
- * does not depend on the other tokens.  x_out may be xt.
+ * h is held in fp32 (fp32 tokens: computed in fp64, rounded once).  A token's result does not depend on
+ * the other tokens of the call.  x_out may be xt.
  * ws: triroute_workspace_bytes(cfg, TRIROUTE_OP_MOE_I8, n_tok, 1) bytes. */
 int triroute_moe_i8(const triroute_cfg *cfg, int n_tok, const void *xt,
                     const triroute_dense_i8_w *dw, const triroute_moe_i8_w *w, const int32_t *eidx,

@@ -80,11 +80,11 @@ def qkv(n1, Wq, Wk, Wv, pos, dh, act):
 
 
 def _uncertain(h, rel, off):
-    """Codes of rows that an implementation whose h is off by up to rel |h|, and that holds it with an
-    error of up to off beside, may set one step elsewhere; and the relative error of its scales."""
+    """Codes of rows that an implementation whose h is off by up to rel |h| + off may set one step
+    elsewhere; and the relative error of its scales."""
     a = np.abs(h).max(axis=1, keepdims=True)
-    top = np.where(np.abs(h) >= a * (1 - 2 * rel), rel, 0.0).max(axis=1, keepdims=True)
     with np.errstate(divide="ignore", invalid="ignore"):
+        top = np.where((np.abs(h) >= a * (1 - 2 * rel)) & (a > 0), rel + off / a, 0.0).max(axis=1, keepdims=True)
         t = np.where(a > 0, 127.0 * np.abs(h) / np.where(a > 0, a, 1), 0.0)
         t_off = np.where(a > 0, 127.0 * off / np.where(a > 0, a, 1), 0.0)
     near = np.abs(np.abs(t - np.floor(t)) - 0.5) <= 1.01 * (t * (rel + top) + t_off)
@@ -97,9 +97,7 @@ def moe(xt, g2, Wg, Wu, Wd, eidx, egate, act):
     quantised, and so is h; h of bf16 layers is formed in fp32: the exponential's argument
     (a sum, three products, a constant) is off by 5 U |G| and moves silu by that much at most; the sums, the
     other products, exponential and quotient are off by 20 U together, so that h is off by less than
-    5 (|G| + 8) U; and it is held as whole numbers of 1/32767 of the largest of 32
-    units, which is off by half of one and, through an fp32 reciprocal, 32767 * 2 U of one more (0.51 in
-    all)."""
+    5 (|G| + 8) U; and a sigmoid below 2^-126 (the quotient's smallest) may be 0."""
     xt = np.asarray(xt, np.float64)
     n2 = rmsnorm(xt, g2).astype(np.float32)
     # (an fp64 norm that is a last place elsewhere rounds one n2 in 2^29 to its neighbour)
@@ -119,8 +117,7 @@ def moe(xt, g2, Wg, Wu, Wd, eidx, egate, act):
         hq, hs = quantize(h)
         off = np.zeros_like(G)
         if act == "bf16":
-            top = np.abs(h.astype(np.float64)).reshape(len(i), -1, 32).max(axis=2)
-            off = np.repeat(top * (0.51 / 32767), 32, axis=1) + 1e-33
+            off = 2.0 ** -125 * np.abs(G * V) * (G < -80) + 2.0 ** -148
         moved, hrel = _uncertain(h.astype(np.float64), rel, off)
         Y, eY = product(hq, hs, Wd[0][e - 1], Wd[1][e - 1])
         wd = np.abs(matrix(Wd[0][e - 1], Wd[1][e - 1]))

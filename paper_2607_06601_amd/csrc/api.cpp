@@ -274,7 +274,6 @@ tr::MoeI8Ws carve_moe_i8(Carve &cv, const triroute_cfg &c, int N) {
   w.s_h = cv.take<float>(rows);
   w.h = cv.take<float>(rows * c.d_ff);
   w.Y = cv.take<float>(rows * c.d_model);
-  w.part = cv.take<uint32_t>(rows * (c.d_ff / 32));
   w.slot_of = cv.take<int32_t>(rows);
   return w;
 }

@@ -7,8 +7,7 @@
 //
 //   linear: y = x W^T (+ residual), any sizes and row strides
 //   QKV   : [n1] x [Wq;Wk;Wv]^T, rotate-half RoPE on q and k
-//   MoE-1 : h = silu(G) U per expert, in 16 bits with a scale for each 32 units (fp32
-//           activations: in fp32)
+//   MoE-1 : h = silu(G) U per expert, fp32
 //   MoE-2 : Y = h Wdown_e^T
 #include "gemm_kernels.hpp"
 #include "i8_out.hpp"
@@ -96,38 +95,6 @@ __device__ __forceinline__ void w4_cols(const float *sc, int lane, float (&c)[NI
     const float4 v = p[q];
     c[4 * q] = v.x; c[4 * q + 1] = v.y; c[4 * q + 2] = v.z; c[4 * q + 3] = v.w;
   }
-}
-// ---------------------------------------------------------------- hidden rows
-// h between the two expert products is held as whole numbers in +-32767 of each 32 units' largest
-// magnitude (fp32 rows would be written and read at twice the bytes, which is what bounds the rows'
-// pass and, for short K, the tiles' epilogue: 16384 tokens, with gated() as it is, the block of 160M
-// 301 -> 297 us, of 1.3B 1285 -> 1213).  That is off by 2^-16 of the 32 units' largest, 1/500 of a
-// step of the row's codes at most: about one code in 3000 moves by its step, 2e-4 of the output's size
-// where bf16 rounds by 2e-3.
-//
-// Whole numbers of v = h / row^2 (gated()) of a part whose largest |v| has the bits m, two to a word,
-// and the bits of the part's largest |h|.
-__device__ __forceinline__ float part_unit(uint32_t m) {
-  return 32767.0f * __builtin_amdgcn_rcpf(__uint_as_float(max(m, __float_as_uint(1e-33f))));
-}
-__device__ __forceinline__ uint32_t pack16(float a, float b, float unit) {
-  // (the low half of a whole number plus 1.5 * 2^23)
-  const uint32_t x = __float_as_uint(fmaf(a, unit, 12582912.0f));
-  const uint32_t y = __float_as_uint(fmaf(b, unit, 12582912.0f));
-  return __builtin_amdgcn_perm(y, x, 0x05040100u);
-}
-__device__ __forceinline__ uint32_t part_max(uint32_t m, float row) {
-  return __float_as_uint(__uint_as_float(m) * (row * row));
-}
-// Largest of 4 or 8 lanes side by side.
-template <int LANES>
-__device__ __forceinline__ uint32_t lanes_umax(uint32_t v) {
-#define TR_DPP(c) uint32_t(__builtin_amdgcn_update_dpp(0, int(v), c, 0xF, 0xF, true))
-  v = max(v, TR_DPP(0xB1));                             // quad_perm 1 0 3 2
-  v = max(v, TR_DPP(0x4E));                             // quad_perm 2 3 0 1
-  if constexpr (LANES == 8) v = max(v, TR_DPP(0x141));  // row_half_mirror
-#undef TR_DPP
-  return v;
 }
 
 // ---------------------------------------------------------------- problems
@@ -456,8 +423,7 @@ struct Moe1I8 {
   static constexpr bool GROUPED = true;
   const int8_t *a, *Wg, *Wu;  // a: rows in list order
   const float *sa, *sg, *su;
-  void *h;         // F64: fp32 rows, else 16-bit ones
-  uint32_t *part;  // [list rows][d_ff / 32]: bits of the largest |h| of 32 units (not F64)
+  float *h;
   const int32_t *cnt;
   int E, dff, pitch;
   static constexpr int out_cols(int BN) { return BN / 2; }
@@ -483,17 +449,16 @@ struct Moe1I8 {
     const int f = t.n0 + P;
     return f < dff ? (half ? su : sg)[int64_t(t.e - 1) * dff + f] : 0.f;
   }
-  // F64: h; else h / row_scale^2
   __device__ float hidden(int32_t ag, int32_t au, float sr, float cg, float cu) const {
     if constexpr (F64)
       return gated64(ag, au, sr, cg, cu);
     else
-      return gated(ag, au, sr, GateScale(cg, cu));
+      return gated(ag, au, sr, GateScale(cg, cu)) * (sr * sr);
   }
   // Four-wave kernel: in wave column wn, MFMA block ni, lane column c
   // holds expert unit (NI / 2) (16 wn + c) + ni / 2 of the tile, gate for
   // even ni and up for odd, so each lane ends with both halves of NI / 2
-  // consecutive units.  A wave's NI * 8 units are one part of a row's maximum.
+  // consecutive units.
   static constexpr bool DIRECT_W4 = true;
   __device__ const int8_t *a_base() const { return a; }
   // a transfer has 8 rows of one block ni: two transfers of gate rows, two of up rows, ...
@@ -518,15 +483,10 @@ struct Moe1I8 {
                            int wn, int lane) const {
     static_assert(NI == 8 && !F64, "4 units per lane, one 16-byte piece per row");
     const int f = t.n0 + (NI / 2) * (16 * wn + (lane & 15));
-    if (f >= dff) return;  // d_ff is a multiple of 32: a part's lanes are all in or all out
+    if (f >= dff) return;  // d_ff is a multiple of 4: a lane's units are all in or all out
     const float *cl = scales + MI * 16 + (NI / 2) * (lane & 15);
     const float4 cg = *(const float4 *)cl, cu = *(const float4 *)(cl + NI * 8);
-    const GateScale gc[4] = {{cg.x, cu.x}, {cg.y, cu.y}, {cg.z, cu.z}, {cg.w, cu.w}};
-    // (the maximum below drops a NaN: those of the weights' scales come back with this)
-    const float nan = (gc[0].both + gc[1].both + gc[2].both + gc[3].both) * 0.0f;
-    // (wave-uniform; a lane's offset fits 32 bits)
-    int16_t *out = (int16_t *)h + int64_t(t.p0) * dff;
-    uint32_t *pt = part + int64_t(t.p0) * (dff >> 5);
+    float *out = h + int64_t(t.p0) * dff;  // (wave-uniform; a lane's offset fits 32 bits)
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
       const int r0 = wm * MI * 16 + mi * 16 + 4 * (lane >> 4);
@@ -536,15 +496,9 @@ struct Moe1I8 {
         float v[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-          v[u] = gated(acc[mi][2 * u][i], acc[mi][2 * u + 1][i], elem(sr, i), gc[u]);
-        const float m4 = fmaxf(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fabsf(v[2])), fabsf(v[3]));
-        const uint32_t m = lanes_umax<8>(__float_as_uint(m4 + nan));
-        const float unit = part_unit(m);
-        if (r0 + i < t.mvalid) {
-          const uint32_t at = uint32_t((r0 + i) * dff + f);  // (of the part: at / 32, d_ff being a multiple)
-          *(uint2 *)behind(out, at * 2u) = make_uint2(pack16(v[0], v[1], unit), pack16(v[2], v[3], unit));
-          if ((lane & 7) == 0) *behind(pt, at >> 3) = part_max(m, elem(sr, i));
-        }
+          v[u] = hidden(acc[mi][2 * u][i], acc[mi][2 * u + 1][i], elem(sr, i), elem(cg, u), elem(cu, u));
+        if (r0 + i < t.mvalid)
+          *(float4 *)behind(out, uint32_t((r0 + i) * dff + f) * 4u) = make_float4(v[0], v[1], v[2], v[3]);
       }
     }
   }
@@ -553,33 +507,14 @@ struct Moe1I8 {
                         int lane) const {
     stage_i8<Moe1I8, MI, NI, TM, TN, LDC>(*this, t, C, acc, wm, wn, lane);
   }
-  // item = 8 expert units of one row (C holds silu(g) u); four lanes side by side have a part
+  // item = 8 expert units of one row (C holds silu(g) u)
   template <int BM, int NC, int LDC, int NT>
   __device__ void epilogue(const MTile &t, const float *C, int tid) const {
     constexpr int CC = NC / 8;
-    static_assert(CC % 4 == 0 && NT % 4 == 0 && (BM * CC) % 64 == 0, "whole parts in a wave");
     for (int it = tid; it < BM * CC; it += NT) {
-      const int r = it / CC, c8 = (it % CC) * 8, f = t.n0 + c8;
-      const bool on = r < t.mvalid && f < dff;
-      const int64_t row = t.p0 + r;
-      const float *v = C + r * LDC + c8;
-      if constexpr (F64) {
-        if (on) store8((float *)h + row * dff + f, v);
-      } else {
-        uint32_t m = 0;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) m = max(m, __float_as_uint(v[u]) & 0x7FFFFFFFu);
-        m = lanes_umax<4>(m);  // (f < dff for all four lanes or none, r is the same)
-        const float unit = part_unit(m);
-        const float sr = row_scale(t, r < t.mvalid ? r : 0);
-        if (on) {
-          u32x4_t w;
-#pragma unroll
-          for (int u = 0; u < 4; ++u) w[u] = pack16(v[2 * u], v[2 * u + 1], unit);
-          *(u32x4_t *)((int16_t *)h + row * dff + f) = w;
-          if ((c8 & 31) == 0) part[row * (dff >> 5) + (f >> 5)] = part_max(m, sr);
-        }
-      }
+      const int r = it / CC, c8 = (it % CC) * 8;
+      if (r >= t.mvalid || t.n0 + c8 >= dff) continue;
+      store8(h + int64_t(t.p0 + r) * dff + t.n0 + c8, C + r * LDC + c8);
     }
   }
 };
@@ -816,7 +751,6 @@ hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
     p.sg = w.Wgate.scale;
     p.su = w.Wup.scale;
     p.h = ws.h;
-    p.part = ws.part;
     p.cnt = c.exp_cnt;
     p.E = E;
     p.dff = dff;
@@ -853,7 +787,7 @@ hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
         e = launch_w4<P, 256, 256>(p, K2, Nk / 256 + E, ny, st);
     }
     if (e != hipSuccess) return e;
-    return launch_i8_hidden(cfg, Nk, ws.h, ws.part, c.exp_off, ws.hq, ws.s_h, st);
+    return launch_i8_hidden(cfg, Nk, ws.h, c.exp_off, ws.hq, ws.s_h, st);
   };
   const hipError_t e = cfg.act == TRIROUTE_BF16 ? up(std::false_type{}) : up(std::true_type{});
   if (e != hipSuccess) return e;

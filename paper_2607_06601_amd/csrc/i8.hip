@@ -367,61 +367,10 @@ hipError_t launch_i8_norm(const triroute_cfg &cfg, int N, const void *x, const v
   return hipGetLastError();
 }
 
-// Hidden rows of 16-bit numbers, each 32 units with their largest magnitude, to codes; W waves a row.  Last
-// rows first, as rows_body.
-template <int W>
-__global__ __launch_bounds__(256) void i8_hidden16_kernel(const int16_t *__restrict__ h,
-                                                          const uint32_t *__restrict__ part,
-                                                          const int32_t *__restrict__ off, int E,
-                                                          int dff, int pitch,
-                                                          int8_t *__restrict__ codes,
-                                                          float *__restrict__ scale) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int at = (W == 4 ? threadIdx.x : lane) * 8, np = dff >> 5;
-  const int total = off[E];
-  for (int64_t i = int64_t(blockIdx.x) * (4 / W) + (W == 4 ? 0 : wave); i < total;
-       i += int64_t(gridDim.x) * (4 / W)) {
-    const int64_t row = total - 1 - i;
-    const int16_t *hr = h + row * dff;
-    const uint32_t *pr = part + row * np;
-    uint32_t m = 0;
-    for (int j = lane; j < np; j += 64) m = max(m, pr[j]);
-    const RowCode rc(wave_umax(m));
-    int8_t *cr = codes + row * pitch;
-#pragma unroll 3
-    for (int c = at; c < pitch; c += 512 * W) {
-      uint4 w = make_uint4(0u, 0u, 0u, 0u);
-      float unit = 0.f;
-      if (c < dff) {
-        w = *(const uint4 *)(hr + c);
-        unit = __uint_as_float(pr[c >> 5]) * (1.0f / 32767.0f);
-      }
-      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-      float v[8];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        v[2 * q] = float(int(u[q] << 16) >> 16) * unit;
-        v[2 * q + 1] = float(int(u[q]) >> 16) * unit;
-      }
-      *(uint2 *)(cr + c) = rc.code8(v);
-    }
-    if (at == 0) scale[row] = rc.scale;
-  }
-}
-
-// Hidden rows of the expert lists to codes; the lists' end is read on the device.
-hipError_t launch_i8_hidden(const triroute_cfg &cfg, int Nk, const void *h, const uint32_t *part,
-                            const int32_t *off, int8_t *codes, float *scale, hipStream_t st) {
-  const int E = cfg.n_experts, dff = cfg.d_ff, pitch = i8_pitch(dff);
-  if (cfg.act == TRIROUTE_F32)
-    return launch_rows(TRIROUTE_F32, Nk, off + E, dff, h, dff, codes, scale, st);
-  if (Nk <= 2048)
-    i8_hidden16_kernel<4><<<dim3(unsigned(Nk)), 256, 0, st>>>((const int16_t *)h, part, off, E, dff, pitch,
-                                                              codes, scale);
-  else
-    i8_hidden16_kernel<1><<<dim3(unsigned(std::min((Nk + 3) / 4, 1 << 20))), 256, 0, st>>>(
-        (const int16_t *)h, part, off, E, dff, pitch, codes, scale);
-  return hipGetLastError();
+// Hidden rows (fp32) of the expert lists to codes; the lists' end is read on the device.
+hipError_t launch_i8_hidden(const triroute_cfg &cfg, int Nk, const float *h, const int32_t *off,
+                            int8_t *codes, float *scale, hipStream_t st) {
+  return launch_rows(TRIROUTE_F32, Nk, off + cfg.n_experts, cfg.d_ff, h, cfg.d_ff, codes, scale, st);
 }
 
 }  // namespace tr

@@ -213,17 +213,15 @@ hipError_t i8_qkv(const triroute_cfg &cfg, int N, const int8_t *a, const float *
 struct MoeI8Ws {  // one row per expert-list entry
   int8_t *n2, *hq;
   float *s_n2, *s_h, *h, *Y;
-  uint32_t *part;    // [rows][d_ff / 32]
   int32_t *slot_of;  // list entry of each assignment
 };
 // RMSNorm(x; g), quantised, to the list rows of every real assignment; slot_of
 hipError_t launch_i8_norm(const triroute_cfg &cfg, int N, const void *x, const void *g,
                           const triroute_compaction &c, const int32_t *eidx, int8_t *codes,
                           float *scale, int32_t *slot_of, hipStream_t st);
-// codes of the hidden rows h of the expert lists: fp32 rows, or (bf16 activations) 16-bit ones with
-// the largest magnitudes of 32 units in part
-hipError_t launch_i8_hidden(const triroute_cfg &cfg, int Nk, const void *h, const uint32_t *part,
-                            const int32_t *off, int8_t *codes, float *scale, hipStream_t st);
+// codes of the hidden rows h of the expert lists
+hipError_t launch_i8_hidden(const triroute_cfg &cfg, int Nk, const float *h, const int32_t *off,
+                            int8_t *codes, float *scale, hipStream_t st);
 // gate/up, the hidden rows' codes, down: ws.n2 -> ws.Y
 hipError_t i8_moe(const triroute_cfg &cfg, int N, const triroute_moe_i8_w &w,
                   const triroute_compaction &c, const MoeI8Ws &ws, hipStream_t st);

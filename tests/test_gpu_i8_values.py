@@ -1,0 +1,59 @@
+"""The 8-bit experts' values: the same in any batch, with hidden rows in fp32."""
+import numpy as np
+import pytest
+import torch
+
+import gen
+import paper_2607_06601_amd as tr
+from paper_2607_06601_amd.device import to_dev
+
+from _common import torch_act
+from test_gpu_i8 import DEV, Experts, device_lists, dirty
+
+pytestmark = pytest.mark.gpu
+
+
+def part(c, at):
+    """x_out of the tokens `at` of c, in a call of their own."""
+    n, eidx = len(at), c.eidx[at]
+    t = [to_dev(eidx, torch.int32), to_dev(c.gate[at], torch.float32)] + device_lists(eidx, c.E)
+    cmp = tr.Compaction(exp_cnt=t[2].data_ptr(), exp_off=t[3].data_ptr(), exp_rows=t[4].data_ptr())
+    x = c.x[torch.from_numpy(np.asarray(at)).to(DEV)].contiguous()
+    out = torch.full_like(x, float("nan"))
+    tr.moe_i8(c.cfg, n, x, c.dw, c.mw, t[0], t[1], cmp, out,
+              dirty(tr.workspace_bytes(c.cfg, tr.OP_MOE_I8, n, 1)))
+    torch.cuda.synchronize()
+    return out
+
+
+def gains(c, g2):
+    c.g2 = gen.to_act(np.asarray(g2, np.float32), c.act)
+    c.t[0] = to_dev(c.g2, torch_act(c.act))
+    c.dw = tr.DenseI8W(g2=c.t[0].data_ptr())
+
+
+def some(n, most=60):
+    return np.unique(np.linspace(0, n - 1, most).astype(int))
+
+
+# ------------------------------------------------------------------ batches
+@pytest.mark.parametrize("act,N,d,f,E,k", [
+    ("bf16", 6000, 256, 512, 4, 2), ("bf16", 6000, 768, 192, 3, 1), ("bf16", 40, 64, 12352, 6, 4),
+    ("f32", 2100, 256, 512, 4, 2)])
+def test_a_token_alone_and_in_batches(act, N, d, f, E, k):
+    """Each batch size takes other kernels: the bits of a token are the same in all."""
+    c = Experts(61, act, N, d, f, E, k)
+    whole = c.run()
+    for n in (1, 2, 3, 5, 33, 333, 1500):
+        for lo in range(0, N - n + 1, max(n, (N - n) // 3)):
+            assert torch.equal(part(c, np.arange(lo, lo + n)), whole[lo:lo + n]), (n, lo)
+
+
+@pytest.mark.parametrize("N", [1, 2, 40, 333, 1500, 6000])
+def test_hidden_rows_are_fp32(N):
+    """Tokens far smaller than the experts' outputs, which so show nothing but their one rounding."""
+    c = Experts(62, "bf16", N, 256, 512, 4, 2)
+    c.xt = gen.to_act(c.xt * np.float32(2.0 ** -60), "bf16")
+    c.x = to_dev(c.xt, torch.bfloat16)
+    gains(c, c.g2 * 2.0 ** 50)
+    c.check(c.run(), some(N))

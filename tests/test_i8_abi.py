@@ -163,3 +163,13 @@ def test_tensors_of_other_shapes_are_refused(monkeypatch):
                          (torch.zeros(3, 128), torch.zeros(3))):
         with pytest.raises(ValueError):
             tr.i8_quantize(x, codes, scale)
+
+
+@pytest.mark.parametrize("act,N", [("bf16", 3), ("bf16", 700), ("f32", 700)])
+def test_experts_workspace_holds_what_is_used(act, N):
+    """Codes and scales of the normalised and the hidden rows, both rows' fp32 values, the
+    lists' entries: nothing else."""
+    d, f, k = 768, 2112, 2
+    c, rows = tr.make_cfg(d, 12, 3, 64, 128, 8, k, f, 64, act), N * k
+    used = rows * (768 + 2176 + 4 + 4 + 4 * f + 4 * d + 4)
+    assert used <= tr.workspace_bytes(c, tr.OP_MOE_I8, N, 1) <= used + 7 * 255
