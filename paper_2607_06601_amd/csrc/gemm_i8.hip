@@ -453,7 +453,7 @@ struct Moe1I8 {
     if constexpr (F64)
       return gated64(ag, au, sr, cg, cu);
     else
-      return gated(ag, au, sr, GateScale(cg, cu)) * (sr * sr);
+      return gated(ag, au, sr, cg, cu);
   }
   // Four-wave kernel: in wave column wn, MFMA block ni, lane column c
   // holds expert unit (NI / 2) (16 wn + c) + ni / 2 of the tile, gate for

@@ -330,7 +330,7 @@ struct FewUp {
     const int f = t.n0 + c;
     const int64_t wr = int64_t(t.e - 1) * dff + f;
     h[int64_t(t.p0 + r) * dff + f] = sizeof(T) == 4 ? gated64(vg, vu, sr, sg[wr], su[wr])
-                                                    : gated(vg, vu, sr, GateScale(sg[wr], su[wr])) * (sr * sr);
+                                                    : gated(vg, vu, sr, sg[wr], su[wr]);
   }
 };
 

@@ -22,17 +22,13 @@ __device__ __forceinline__ float gated64(int32_t ag, int32_t au, float row, floa
   return float(g / (1.0 + exp(-g)) * u);
 }
 
-// h / row^2 of bf16 activations, for the sums ag, au of gate and up:
-//   silu(G) U = row^2 (cg cu) ag au / (1 + 2^(-G log2 e)).
-// row^2 is common to a token's units, so it is applied once to what they share, not to each.
-struct GateScale {
-  float exponent, both;  // -cg log2 e, cg cu
-  __device__ __forceinline__ GateScale(float cg, float cu)
-      : exponent(-1.44269504088896f * cg), both(cg * cu) {}
-};
-__device__ __forceinline__ float gated(int32_t ag, int32_t au, float row, const GateScale &c) {
-  const float g = float(ag), e = __builtin_amdgcn_exp2f(g * row * c.exponent);
-  return g * float(au) * c.both * __builtin_amdgcn_rcpf(1.0f + e);
+// h = silu(G) U of bf16 activations, in fp32: G and U are formed each with its own scales, as
+// every other sum is.  (Products of the scales alone may leave fp32 where G and U do not; one of them
+// for a row and one for a channel would save 16 of 1270 us at 1.3B, 16384 tokens.)  An exponential that
+// overflows gives silu 0.
+__device__ __forceinline__ float gated(int32_t ag, int32_t au, float row, float cg, float cu) {
+  const float g = dequant(ag, row, cg), u = dequant(au, row, cu);
+  return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896f * g)) * u;
 }
 
 // Rotation of the pair (a, b) by (cos, sin).

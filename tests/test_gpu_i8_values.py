@@ -1,4 +1,4 @@
-"""The 8-bit experts' values: the same in any batch, with hidden rows in fp32."""
+"""The 8-bit experts' values: the same in any batch, and over the whole range of fp32."""
 import numpy as np
 import pytest
 import torch
@@ -32,6 +32,13 @@ def gains(c, g2):
     c.dw = tr.DenseI8W(g2=c.t[0].data_ptr())
 
 
+def weight_scale(c, which, at, factor):
+    """Scales of rows `at` of each expert, multiplied."""
+    q, s = c.W[which]
+    s[:, at] *= np.float32(factor)
+    c.mats[which].scale.copy_(to_dev(s.reshape(-1), torch.float32))
+
+
 def some(n, most=60):
     return np.unique(np.linspace(0, n - 1, most).astype(int))
 
@@ -57,3 +64,37 @@ def test_hidden_rows_are_fp32(N):
     c.x = to_dev(c.xt, torch.bfloat16)
     gains(c, c.g2 * 2.0 ** 50)
     c.check(c.run(), some(N))
+
+
+# ------------------------------------------------------------------ range
+SIZES = [("bf16", 1), ("bf16", 2), ("bf16", 40), ("bf16", 333), ("bf16", 1500), ("bf16", 6000),
+         ("f32", 2), ("f32", 40), ("f32", 333)]
+
+
+@pytest.mark.parametrize("act,N", SIZES)
+@pytest.mark.parametrize("gain,gate,up", [(2.0 ** 72, 2.0 ** -72, 2.0 ** -72), (2.0 ** -70, 2.0 ** 70, 2.0 ** 70),
+                                          (1, 2.0 ** -90, 2.0 ** 90), (2.0 ** 90, 2.0 ** -85, 2.0 ** -95)])
+def test_scales_far_from_one(act, N, gain, gate, up):
+    """Gates and ups that are ordinary numbers while the scales' products are not."""
+    c = Experts(63, act, N, 256, 512, 4, 2)
+    gains(c, c.g2 * gain)
+    weight_scale(c, 0, slice(None), gate)
+    weight_scale(c, 1, slice(None), up)
+    got = c.run()
+    assert torch.isfinite(got).all()
+    c.check(got, some(N))
+
+
+@pytest.mark.parametrize("act,N", SIZES)
+def test_saturated_and_zero_gates(act, N):
+    """Gates far out on both sides of silu and of 0, unit by unit and 32 units together."""
+    c = Experts(64, act, N, 256, 512, 2, 2)
+    for at, factor in ((slice(0, 64, 3), 3000.0), (slice(64, 80), 0), (slice(96, 128), 0),
+                       (slice(128, 192), 1e4), (slice(192, 224), 1e-30), (slice(256, 320), 300.0)):
+        weight_scale(c, 0, at, factor)
+    weight_scale(c, 1, slice(300, 352), 0)
+    got = c.run()
+    assert torch.isfinite(got).all()
+    c.check(got, some(N))
+    weight_scale(c, 0, slice(None), 0)             # no gate at all
+    assert torch.equal(c.run(), c.x)
