@@ -19,7 +19,7 @@ constexpr int FEW_PANEL = 48 << 10;  // bytes of codes of a tile's rows
 constexpr int FEW_PAD = 16;          // between rows of codes: 16 rows at one K lie in 16 bank groups
 
 // A row quantised by the whole block, KS waves: up to 1024 KS elements, which stay in
-// registers.  red: KS entries for this row alone.
+// registers.  red: 512 sums of squares; mred: KS entries for this row alone.
 template <class P, int KS>
 __device__ __forceinline__ void block_row(const P &p, const MTile &t, int r, int pitch, double *red,
                                           uint32_t *mred, int8_t *dst, float &scale) {
@@ -34,17 +34,14 @@ __device__ __forceinline__ void block_row(const P &p, const MTile &t, int r, int
     float gv[2][8];  // (the gains on their way during the sum)
 #pragma unroll
     for (int q = 0; q < 2; ++q) p.gains(at + STEP * q, gv[q]);
-    double ss = 0.0;
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) ss = fma(double(v[q][j]), double(v[q][j]), ss);
-    ss = wave_sum(ss);
-    if (lane == 0) red[wave] = ss;
+    // (pieces `wave` and wave + KS: of eight waves one sum, of four two)
+    double s[2] = {0.0, 0.0};
+    add_squares(v[0], s[0]);
+    add_squares(v[1], s[KS == 8 ? 0 : 1]);
+    red[threadIdx.x] = s[0];
+    if constexpr (KS == 4) red[threadIdx.x + 256] = s[1];
     __syncthreads();
-    ss = 0.0;
-#pragma unroll
-    for (int k = 0; k < KS; ++k) ss += red[k];
+    const double ss = join_shared(red, lane);
     double inv = p.inv_norm(ss);
     norm_range(ss, inv, v);
 #pragma unroll
@@ -70,25 +67,18 @@ __device__ __forceinline__ void block_row(const P &p, const MTile &t, int r, int
 // The codes and scales of a tile's rows: up to two by the whole block, else a wave each.
 template <class P, int KS>
 __device__ __forceinline__ void tile_rows(const P &p, const MTile &t, int pitch, int8_t *panel,
-                                          float *srow) {
-  __shared__ double red[2][KS];
+                                          float *srow, double *red) {
   __shared__ uint32_t mred[2][KS];
   if (t.mvalid <= 2 && pitch <= 1024 * KS) {
     for (int r = 0; r < t.mvalid; ++r)
-      block_row<P, KS>(p, t, r, pitch, red[r], mred[r], panel + r * (pitch + FEW_PAD), srow[r]);
+      block_row<P, KS>(p, t, r, pitch, red, mred[r], panel + r * (pitch + FEW_PAD), srow[r]);
   } else {
     const int lane = threadIdx.x & 63;
     for (int r = threadIdx.x >> 6; r < t.mvalid; r += KS) {
       const auto row = p.row(t, r);
       double inv = 0.0, ss = 0.0;
       if constexpr (P::NORM) {
-        for (int c = lane * 8; c < pitch; c += 512) {
-          float v[8];
-          p.load(row, c, v);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) ss = fma(double(v[j]), double(v[j]), ss);
-        }
-        ss = wave_sum(ss);
+        ss = wave_squares([&](int c, float *v) { p.load(row, c, v); }, pitch, lane);
         inv = p.inv_norm(ss);
       }
       const float s = wave_row(
@@ -154,7 +144,8 @@ __global__ __launch_bounds__(64 * KS) void i8_few_kernel(P p, int pitch, int ny)
       if (u < np) fetch(u, b[u]);
   };
   start(blockIdx.y);
-  tile_rows<P, KS>(p, t, pitch, panel, srow);
+  static_assert(!P::NORM || sizeof(part) >= 512 * sizeof(double), "the rows' sums lie where the products' will");
+  tile_rows<P, KS>(p, t, pitch, panel, srow, (double *)part);
   // (rows past the valid ones read row 0: their sums are not stored)
   const int8_t *a = panel + (l15 < t.mvalid ? l15 : 0) * (pitch + FEW_PAD) + 128 * wave + kb;
   for (int by = blockIdx.y; by < ny; by += gridDim.y) {

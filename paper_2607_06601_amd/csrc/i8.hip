@@ -236,7 +236,7 @@ __global__ __launch_bounds__(256) void i8_norm_kernel(
     int E, int k, int n, int d, int pitch, float eps, int8_t *__restrict__ codes,
     float *__restrict__ scale) {
   constexpr int STEP = 512 * W;
-  __shared__ double part[W];
+  __shared__ double part[W == 4 ? 512 : 1];
   __shared__ uint32_t mpart[W];
   const int wave = threadIdx.x >> 6;
   const int i = W == 4 ? int(blockIdx.x) : __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + wave);
@@ -246,27 +246,36 @@ __global__ __launch_bounds__(256) void i8_norm_kernel(
   const T *xr = x + int64_t(ENTRY ? a / k : i) * d;
   constexpr bool KEEP = RR > 0;
   float v[KEEP ? RR : 1][8];
-  double ss = 0.0;
-  auto square = [&](const float *w) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) ss = fma(double(w[j]), double(w[j]), ss);
-  };
+  double ss;
   if constexpr (KEEP) {
 #pragma unroll
     for (int q = 0; q < RR; ++q) row8<T, true>(xr, at + STEP * q, d, v[q]);
-#pragma unroll
-    for (int q = 0; q < RR; ++q) square(v[q]);
-  } else {
-    for (int c = at; c < d; c += STEP) {
-      load8(xr + c, v[0]);
-      square(v[0]);
-    }
   }
-  ss = wave_sum(ss);
-  if constexpr (W == 4) {
-    if ((threadIdx.x & 63) == 0) part[wave] = ss;
+  if constexpr (W == 4) {  // pieces `wave`, wave + 4, ...: sums `wave` and wave + 4 of the eight
+    double s[2] = {0.0, 0.0};
+    if constexpr (KEEP) {
+#pragma unroll
+      for (int q = 0; q < RR; ++q) add_squares(v[q], s[q & 1]);
+    } else {
+      for (int c = at; c < d; c += 2 * STEP) {
+        load8(xr + c, v[0]);
+        add_squares(v[0], s[0]);
+        if (c + STEP >= d) break;
+        load8(xr + c + STEP, v[0]);
+        add_squares(v[0], s[1]);
+      }
+    }
+    part[threadIdx.x] = s[0];
+    part[threadIdx.x + 256] = s[1];
     __syncthreads();
-    ss = (part[0] + part[1]) + (part[2] + part[3]);
+    ss = join_shared(part, threadIdx.x & 63);
+  } else if constexpr (KEEP) {
+    double s[RR] = {};
+#pragma unroll
+    for (int q = 0; q < RR; ++q) add_squares(v[q], s[q]);
+    ss = wave_sum(join_pieces(s));
+  } else {
+    ss = wave_squares([&](int c, float *w) { load8(xr + c, w); }, d, threadIdx.x & 63);
   }
   double r = 1.0 / sqrt(ss / double(d) + double(eps));
   if constexpr (KEEP) norm_range(ss, r, v);

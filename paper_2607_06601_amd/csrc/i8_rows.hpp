@@ -119,6 +119,45 @@ __device__ __forceinline__ void row8(const T *row, int c, int cols, float *v) {
   }
 }
 
+// The sum of a row's squares, in fp64 and in one order whichever waves share the row, so that a
+// token's normalised values are the same in every kernel: piece p of a row is its elements
+// 512 p .. 512 p + 511, eight a lane; a lane adds the squares of pieces p, p + 8, p + 16, ... one
+// after the other, then (join_pieces) its eight sums in pairs, and the lanes follow.
+__device__ __forceinline__ void add_squares(const float *v, double &s) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) s = fma(double(v[j]), double(v[j]), s);
+}
+// (the sums that are not there would be zeros)
+template <int N>
+__device__ __forceinline__ double join_pieces(const double (&s)[N]) {
+  static_assert(N == 2 || N == 4 || N == 8, "whole pairs");
+  if constexpr (N == 2) return s[0] + s[1];
+  if constexpr (N == 4) return (s[0] + s[1]) + (s[2] + s[3]);
+  if constexpr (N == 8) return ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+}
+// The same of sums in LDS, [8][64].
+__device__ __forceinline__ double join_shared(const double *s, int lane) {
+  double v[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = s[64 * k + lane];
+  return wave_sum(join_pieces(v));
+}
+// One wave's row of n elements, whose 8 values at c `load(c, v)` gives (zeros behind its end).
+template <class Load>
+__device__ __forceinline__ double wave_squares(const Load &load, int n, int lane) {
+  double s[8] = {};
+  for (int c = lane * 8; c < n; c += 4096) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (c + 512 * k >= n) continue;
+      float v[8];
+      load(c + 512 * k, v);
+      add_squares(v, s[k]);
+    }
+  }
+  return wave_sum(join_pieces(s));
+}
+
 // A row whose products with the gains (below 2^28) may leave fp32 is normalised from values 2^64
 // times smaller, in one branch for its NP pieces.  ss: its sum of squares, the same in all lanes.
 // (What that takes below fp32's range is far below half a code.)

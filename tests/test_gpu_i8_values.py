@@ -98,3 +98,25 @@ def test_saturated_and_zero_gates(act, N):
     c.check(got, some(N))
     weight_scale(c, 0, slice(None), 0)             # no gate at all
     assert torch.equal(c.run(), c.x)
+
+
+# ------------------------------------------------------------------ the norm
+# Tokens (fp32) for which sums of the squares in another order give another n2, found by
+# trying orders: block of rows, row, the first gain.
+@pytest.mark.parametrize("d,seed,name,row,gain", [
+    (1024, 81, "xt", 47, "0x1.04c166p+3"), (1024, 81, "xt", 182, "0x1.4e60cp+3"),
+    (2560, 82, "xt6", 72, "0x1.aa11f8p+3"), (2560, 82, "xt2", 53, "0x1.83ccb4p+3"),
+    (2560, 82, "xt9", 18, "0x1.d6e784p+3")])
+def test_sum_of_squares_in_one_order(d, seed, name, row, gain):
+    N = 2100
+    c = Experts(65, "f32", N, d, 64, 2, 1, [0, 1050, 1050])
+    x = gen.normal(seed, name, (400 if d == 1024 else 500, d))[row]
+    x[0] = 4
+    c.xt[:] = x
+    c.x = to_dev(c.xt, torch.float32)
+    g2 = np.ones(d, np.float32)
+    g2[0] = float.fromhex(gain)
+    gains(c, g2)
+    whole = c.run()
+    for n in (1, 4, 40, 333):
+        assert torch.equal(part(c, np.arange(n)), whole[:n]), n
