@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import numpy as np
 
-from .layer import ROPE_THETA, rmsnorm
+from .layer import EPS, ROPE_THETA, rmsnorm
 
 U = 2.0 ** -24
 HALF_STEP = {"bf16": 2.0 ** -8, "f32": U}
@@ -91,7 +91,7 @@ def _uncertain(h, rel, off):
     return near, top[:, 0] + U
 
 
-def moe(xt, g2, Wg, Wu, Wd, eidx, egate, act):
+def moe(xt, g2, Wg, Wu, Wd, eidx, egate, act, eps=EPS):
     """x_out of triroute_moe_i8 and its bound; Wg, Wu: (codes [E, f, d], scale [E, f]), Wd:
     (codes [E, d, f], scale [E, d]).  The normalised token is an fp32 value before it is
     quantised, and so is h; h of bf16 layers is formed in fp32: the exponential's argument
@@ -99,7 +99,7 @@ def moe(xt, g2, Wg, Wu, Wd, eidx, egate, act):
     other products, exponential and quotient are off by 20 U together, so that h is off by less than
     5 (|G| + 8) U; and a sigmoid below 2^-126 (the quotient's smallest) may be 0."""
     xt = np.asarray(xt, np.float64)
-    n2 = rmsnorm(xt, g2).astype(np.float32)
+    n2 = rmsnorm(xt, g2, eps).astype(np.float32)
     # (an fp64 norm that is a last place elsewhere rounds one n2 in 2^29 to its neighbour)
     nq, ns = quantize(n2)
     y = np.zeros_like(xt)

@@ -42,8 +42,7 @@ __device__ __forceinline__ void block_row(const P &p, const MTile &t, int r, int
     if constexpr (KS == 4) red[threadIdx.x + 256] = s[1];
     __syncthreads();
     const double ss = join_shared(red, lane);
-    double inv = p.inv_norm(ss);
-    norm_range(ss, inv, v);
+    const double inv = p.inv_norm(ss);
 #pragma unroll
     for (int q = 0; q < 2; ++q) norm8<typename P::elem>(gv[q], inv, v[q]);
   }
@@ -76,24 +75,16 @@ __device__ __forceinline__ void tile_rows(const P &p, const MTile &t, int pitch,
     const int lane = threadIdx.x & 63;
     for (int r = threadIdx.x >> 6; r < t.mvalid; r += KS) {
       const auto row = p.row(t, r);
-      double inv = 0.0, ss = 0.0;
-      if constexpr (P::NORM) {
-        ss = wave_squares([&](int c, float *v) { p.load(row, c, v); }, pitch, lane);
-        inv = p.inv_norm(ss);
-      }
+      double inv = 0.0;
+      if constexpr (P::NORM)
+        inv = p.inv_norm(wave_squares([&](int c, float *v) { p.load(row, c, v); }, pitch, lane));
       const float s = wave_row(
           [&](int c, float *v) {
             p.load(row, c, v);
             if constexpr (P::NORM) {
-              float gv[8], w[1][8];
-              double r = inv;
+              float gv[8];
               p.gains(c, gv);
-#pragma unroll
-              for (int j = 0; j < 8; ++j) w[0][j] = v[j];
-              norm_range(ss, r, w);
-              norm8<typename P::elem>(gv, r, w[0]);
-#pragma unroll
-              for (int j = 0; j < 8; ++j) v[j] = w[0][j];
+              norm8<typename P::elem>(gv, inv, v);
             }
           },
           pitch, lane, panel + r * (pitch + FEW_PAD));

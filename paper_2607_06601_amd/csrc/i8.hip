@@ -277,8 +277,7 @@ __global__ __launch_bounds__(256) void i8_norm_kernel(
   } else {
     ss = wave_squares([&](int c, float *w) { load8(xr + c, w); }, d, threadIdx.x & 63);
   }
-  double r = 1.0 / sqrt(ss / double(d) + double(eps));
-  if constexpr (KEEP) norm_range(ss, r, v);
+  const double r = 1.0 / sqrt(ss / double(d) + double(eps));
   uint32_t m = 0;
   auto normed = [&](int c, float *w) {
     if (c >= d) return;
@@ -288,19 +287,13 @@ __global__ __launch_bounds__(256) void i8_norm_kernel(
 #pragma unroll
     for (int j = 0; j < 8; ++j) m = max(m, abs_bits(w[j]));
   };
-  auto again = [&](int c) {  // a piece that was not kept
-    const double kept = r;
-    norm_range(ss, r, v);
-    normed(c, v[0]);
-    r = kept;
-  };
   if constexpr (KEEP) {
 #pragma unroll
     for (int q = 0; q < RR; ++q) normed(at + STEP * q, v[q]);
   } else {
     for (int c = at; c < d; c += STEP) {
       load8(xr + c, v[0]);
-      again(c);
+      normed(c, v[0]);
     }
   }
   m = wave_umax(m);
@@ -328,7 +321,7 @@ __global__ __launch_bounds__(256) void i8_norm_kernel(
   } else {
     for (int c = at; c < pitch; c += STEP) {
       row8<T, true>(xr, c, d, v[0]);
-      again(c);
+      normed(c, v[0]);
       emit(c, rc.code8(v[0]));
     }
   }

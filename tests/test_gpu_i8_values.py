@@ -5,10 +5,11 @@ import torch
 
 import gen
 import paper_2607_06601_amd as tr
+from oracle import i8
 from paper_2607_06601_amd.device import to_dev
 
-from _common import torch_act
-from test_gpu_i8 import DEV, Experts, device_lists, dirty
+from _common import npy, torch_act
+from test_gpu_i8 import DEV, Experts, device_lists, dirty, within
 
 pytestmark = pytest.mark.gpu
 
@@ -120,3 +121,28 @@ def test_sum_of_squares_in_one_order(d, seed, name, row, gain):
     whole = c.run()
     for n in (1, 4, 40, 333):
         assert torch.equal(part(c, np.arange(n)), whole[:n]), n
+
+
+@pytest.mark.parametrize("act,N", SIZES + [("bf16", 4), ("bf16", 2600)])
+@pytest.mark.parametrize("d", [256, 4224])
+@pytest.mark.parametrize("size,gain,eps", [(2.0 ** 50, 2.0 ** 90, 1e-6), (2.0 ** -70, 2.0 ** -75, 1e-38),
+                                           (2.0 ** 100, 2.0 ** 30, 1e-6), (1, 2.0 ** 100, 1e-6)])
+def test_gains_far_from_one(act, N, d, size, gain, eps):
+    """Products of tokens and gains that leave fp32 where the normalised token does not."""
+    if d > 256 and N > 333 and N != 2600:
+        N = 1500
+    c = Experts(66, act, N, d, 128, 1, 1, [0, N])
+    c.cfg.rms_eps = eps
+    c.xt = gen.to_act(c.xt * np.float32(size), act)
+    c.xt[N // 2] = 0
+    c.x = to_dev(c.xt, torch_act(act))
+    gains(c, c.g2 * gain)
+    norm = gain * min(1.0, size / eps ** 0.5)
+    for which in (0, 1):
+        weight_scale(c, which, slice(None), 1 / norm)
+    weight_scale(c, 2, slice(None), size)
+    rows = some(N, 40)
+    got = c.run()
+    assert torch.isfinite(got).all()
+    want, err = i8.moe(c.xt[rows], c.g2, *c.W, c.eidx[rows], c.gate[rows], act, eps=c.cfg.rms_eps)
+    within(npy(got)[rows], want, err, "x_out")
