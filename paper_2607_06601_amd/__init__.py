@@ -61,14 +61,46 @@ class MoeW(C.Structure):
 
 
 class I8W(C.Structure):
+    """Addresses of a matrix's codes and scales; an I8Matrix's knows the matrix (``known``:
+    rows, columns, GPU) and holds its tensors."""
     _fields_ = [("codes", C.c_void_p), ("scale", C.c_void_p)]
+    known = None
 
 
-class DenseI8W(C.Structure):
+class _I8Weights(C.Structure):
+    """Weights that hold the matrices they are made of, so that calls can check them."""
+
+    def __setattr__(self, name, value):
+        super().__setattr__(name, value)
+        held = self.__dict__.setdefault("held", {})
+        held.pop("fits", None)
+        if isinstance(value, I8W):
+            held[name] = value
+
+    def check(self, cfg, index, shapes):
+        """Each matrix lies on GPU `index` and has its (rows, columns) of ``shapes(cfg)``, where it
+        is known."""
+        held = self.__dict__.get("held")
+        key = (bytes(cfg), index, shapes)
+        if held is None or held.get("fits") == key:
+            return
+        for name, want in shapes(cfg).items():
+            w = held.get(name)
+            if w is None or w.known is None or getattr(self, name).codes != w.codes:
+                continue
+            if w.known[2] != index:
+                raise ValueError(f"{name}: a matrix of the current GPU wanted")
+            if w.known[:2] != want:
+                raise ValueError(f"{name}: a matrix of {want[0]} rows and {want[1]} columns wanted, "
+                                 f"not {w.known[0]} and {w.known[1]}")
+        held["fits"] = key
+
+
+class DenseI8W(_I8Weights):
     _fields_ = [(n, I8W) for n in ("Wq", "Wk", "Wv", "Wo")] + [("g2", C.c_void_p)]
 
 
-class MoeI8W(C.Structure):
+class MoeI8W(_I8Weights):
     _fields_ = [(n, I8W) for n in ("Wgate", "Wup", "Wdown")]
 
 
@@ -445,7 +477,7 @@ def i8_pitch(cols: int) -> int:
 
 class I8Matrix:
     """A matrix [rows, cols] in 8 bits: ``codes`` int8 [rows, i8_pitch(cols)], zeros from cols
-    on, and ``scale`` fp32 [rows]; ``w`` is its I8W, valid while the matrix lives.  Made of
+    on, and ``scale`` fp32 [rows]; ``w`` is its I8W, which holds both.  Made of
     these two, or by ``I8Matrix.quantize`` of a matrix (experts' weights [E, rows, cols] are
     stacked)."""
 
@@ -459,6 +491,7 @@ class I8Matrix:
         self.codes, self.scale, self.cols = codes, scale, cols
         self.rows, self.index = codes.shape[0], codes.get_device()
         self.w = I8W(codes.data_ptr(), scale.data_ptr())
+        self.w.known, self.w.held = (self.rows, cols, self.index), (codes, scale)
         self.ref = C.byref(self.w)
 
     @classmethod
@@ -543,36 +576,67 @@ def linear_i8(x, w: I8Matrix, y, ws, residual=None, stream=None):
         _i8_rows("y", y, dtype, (n, m), index), ws.data_ptr(), ws.numel(), stream.cuda_stream))
 
 
+def _qkv_shapes(cfg):
+    d, hd, kd = cfg.d_model, cfg.n_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim
+    return dict(Wq=(hd, d), Wk=(kd, d), Wv=(kd, d))
+
+
+def _dense_shapes(cfg):
+    return dict(_qkv_shapes(cfg), Wo=(cfg.d_model, cfg.n_heads * cfg.head_dim))
+
+
+def _moe_shapes(cfg):
+    d, f, E = cfg.d_model, cfg.d_ff, cfg.n_experts
+    return dict(Wgate=(E * f, d), Wup=(E * f, d), Wdown=(E * d, f))
+
+
+def _i8_call(cfg, stream, dense, dw, mw, *tensors):
+    """The stream of a call whose tensors and known matrices lie on its GPU, the latter of the layer's shapes."""
+    stream = _i8_stream(stream)
+    index = stream.device_index
+    for t in tensors:
+        if t is not None and type(t) is not int and t.get_device() != index:
+            raise ValueError("tensors of the current GPU wanted")
+    if dense is not None:
+        dw.check(cfg, index, dense)
+    if mw is not None:
+        mw.check(cfg, index, _moe_shapes)
+    return stream.cuda_stream
+
+
 def qkv_i8(cfg, B, T, n1, dw: DenseI8W, q, k, v, ws, pos0=None, stream=None):
     """triroute_qkv_i8: qkv with 8-bit weights."""
+    stream = _i8_call(cfg, stream, _qkv_shapes, dw, None, n1, q, k, v, ws, pos0)
     _check(lib().triroute_qkv_i8(C.byref(cfg), B, T, _p(n1), C.byref(dw), _p(pos0), _p(q), _p(k),
-                                 _p(v), _p(ws), ws.numel(), _stream(stream)))
+                                 _p(v), _p(ws), ws.numel(), stream))
 
 
 def moe_i8(cfg, n_tok, xt, dw: DenseI8W, mw: MoeI8W, eidx, egate, cmp: Compaction, x_out, ws,
            stream=None):
     """triroute_moe_i8: moe with 8-bit weights."""
+    stream = _i8_call(cfg, stream, None, dw, mw, xt, eidx, egate, x_out, ws)
     _check(lib().triroute_moe_i8(C.byref(cfg), n_tok, _p(xt), C.byref(dw), C.byref(mw), _p(eidx),
-                                 _p(egate), C.byref(cmp), _p(x_out), _p(ws), ws.numel(),
-                                 _stream(stream)))
+                                 _p(egate), C.byref(cmp), _p(x_out), _p(ws), ws.numel(), stream))
 
 
 def layer_prefill_i8(cfg, B, T, x, psi, rw, dw: DenseI8W, mw: MoeI8W, cache: KVCache, x_out, ws,
                      taps=None, seq_ids=None, stream=None):
     """triroute_layer_prefill_i8: layer_prefill with 8-bit weights."""
+    stream = _i8_call(cfg, stream, _dense_shapes, dw, mw, x, psi, cache.buf, x_out, ws, seq_ids)
     _check(lib().triroute_layer_prefill_i8(
         C.byref(cfg), B, T, _p(seq_ids), _p(x), _p(psi), C.byref(rw), C.byref(dw), C.byref(mw),
         cache.ref, _p(x_out), C.byref(taps) if taps is not None else None, _p(ws), ws.numel(),
-        _stream(stream)))
+        stream))
 
 
 def layer_decode_i8(cfg, B, x, psi, rw, dw: DenseI8W, mw: MoeI8W, cache: KVCache, x_out, ws,
                     taps=None, seq_ids=None, stream=None):
     """triroute_layer_decode_i8: layer_decode with 8-bit weights."""
+    stream = _i8_call(cfg, stream, _dense_shapes, dw, mw, x, psi, cache.buf, x_out, ws, seq_ids)
     _check(lib().triroute_layer_decode_i8(
         C.byref(cfg), B, _p(seq_ids), _p(x), _p(psi), C.byref(rw), C.byref(dw), C.byref(mw),
         cache.ref, _p(x_out), C.byref(taps) if taps is not None else None, _p(ws), ws.numel(),
-        _stream(stream)))
+        stream))
 
 
 # ------------------------------------------------- gradient norm and clipping

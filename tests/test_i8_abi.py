@@ -173,3 +173,92 @@ def test_experts_workspace_holds_what_is_used(act, N):
     c, rows = tr.make_cfg(d, 12, 3, 64, 128, 8, k, f, 64, act), N * k
     used = rows * (768 + 2176 + 4 + 4 + 4 * f + 4 * d + 4)
     assert used <= tr.workspace_bytes(c, tr.OP_MOE_I8, N, 1) <= used + 7 * 255
+
+
+class CpuStream:  # (no GPU here: tensors of the CPU have the index -1)
+    device_index, cuda_stream = -1, 0
+
+
+def zeros_i8(rows, cols):
+    return tr.I8Matrix(torch.zeros(rows, tr.i8_pitch(cols), dtype=torch.int8), torch.zeros(rows), cols)
+
+
+def layer_calls(cfg, dw, mw, t, cache):
+    """Each call over a layer's weights, its tensors being t (too small for a call: refused before it)."""
+    return dict(
+        qkv=lambda: tr.qkv_i8(cfg, 1, 1, t, dw, t, t, t, t),
+        moe=lambda: tr.moe_i8(cfg, 1, t, dw, mw, t, t, tr.Compaction(), t, t),
+        prefill=lambda: tr.layer_prefill_i8(cfg, 1, 1, t, t, tr.RouterW(), dw, mw, cache, t, t),
+        decode=lambda: tr.layer_decode_i8(cfg, 1, t, t, tr.RouterW(), dw, mw, cache, t, t))
+
+
+def test_matrices_of_other_shapes_are_refused(monkeypatch):
+    monkeypatch.setattr(tr, "_i8_stream", lambda s: CpuStream if s is None else s)
+    c = cfg160(n_experts=3, d_ff=128)
+    d, hd, kd, f, E = 768, 768, 192, 128, 3
+    dense = dict(Wq=(hd, d), Wk=(kd, d), Wv=(kd, d), Wo=(d, hd))
+    experts = dict(Wgate=(E * f, d), Wup=(E * f, d), Wdown=(E * d, f))
+    t = torch.zeros(16)
+
+    class Cache:
+        buf, ref = t, None
+
+    def weights(kind, shapes, **over):
+        return kind(**{n: zeros_i8(*s).w for n, s in {**shapes, **over}.items()})
+
+    good_d, good_m = weights(tr.DenseI8W, dense), weights(tr.MoeI8W, experts)
+    for name in ("qkv", "moe", "prefill", "decode"):          # these reach the library, which wants more
+        with pytest.raises(RuntimeError):
+            layer_calls(c, good_d, good_m, t, Cache)[name]()
+    for over, names in ((dict(Wq=(hd, d - 64)), ("qkv", "prefill", "decode")), (dict(Wk=(hd, d)), ("qkv", "prefill")),
+                        (dict(Wv=(kd - 64, d)), ("qkv", "decode")), (dict(Wo=(d - 1, hd)), ("prefill", "decode"))):
+        dw = weights(tr.DenseI8W, dense, **over)
+        for name in names:
+            with pytest.raises(ValueError, match=next(iter(over))):
+                layer_calls(c, dw, good_m, t, Cache)[name]()
+    for over in (dict(Wgate=(2 * f, d)), dict(Wup=(E * f, d + 64)), dict(Wdown=(E * d, f + 1)), dict(Wdown=(E * f, d))):
+        mw = weights(tr.MoeI8W, experts, **over)
+        for name in ("moe", "prefill", "decode"):
+            with pytest.raises(ValueError, match=next(iter(over))):
+                layer_calls(c, good_d, mw, t, Cache)[name]()
+    # a matrix set later counts, one set back too, and another layer's call does not remember this one's
+    good_m.Wup = zeros_i8(E * f, 64).w
+    with pytest.raises(ValueError, match="Wup"):
+        layer_calls(c, good_d, good_m, t, Cache)["moe"]()
+    good_m.Wup = zeros_i8(E * f, d).w
+    with pytest.raises(RuntimeError):
+        layer_calls(c, good_d, good_m, t, Cache)["moe"]()
+    with pytest.raises(ValueError, match="Wgate"):
+        layer_calls(cfg160(n_experts=4, d_ff=128), good_d, good_m, t, Cache)["moe"]()
+
+
+def test_weights_keep_their_matrices():
+    m = zeros_i8(5, 100)
+    at = m.codes.data_ptr()
+    held = m.codes
+    mw = tr.MoeI8W(Wgate=m.w)
+    del m
+    assert mw.Wgate.codes == at and mw.held["Wgate"].held[0] is held
+
+
+def test_tensors_and_matrices_of_another_gpu_are_refused(monkeypatch):
+    class Gpu:
+        device_index, cuda_stream = 0, 0
+
+    c, t = cfg160(n_experts=3, d_ff=128), torch.zeros(16)
+
+    class Cache:
+        buf, ref = t, None
+
+    monkeypatch.setattr(tr, "_i8_stream", lambda s: Gpu)
+    for call in layer_calls(c, tr.DenseI8W(), tr.MoeI8W(), t, Cache).values():
+        with pytest.raises(ValueError, match="current GPU"):
+            call()
+    # tensors given as addresses, matrices of the CPU
+    Cache.buf = 0
+    dw = tr.DenseI8W(Wk=zeros_i8(192, 768).w)
+    mw = tr.MoeI8W(Wdown=zeros_i8(3 * 768, 128).w)
+
+    for name, word in (("qkv", "Wk"), ("moe", "Wdown"), ("prefill", "Wk"), ("decode", "Wk")):
+        with pytest.raises(ValueError, match=word + ".*current GPU"):
+            layer_calls(c, dw, mw, FAKE, Cache)[name]()
