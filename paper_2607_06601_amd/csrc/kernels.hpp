@@ -4,26 +4,12 @@
 #include <algorithm>
 
 #include "common.hpp"
+#include "cu_count.hpp"
 
 namespace tr {
 
 // Attention decisions per token (cfg.attn_groups, 0 = one per head).
 inline int attn_groups(const triroute_cfg &c) { return c.attn_groups > 0 ? c.attn_groups : c.n_heads; }
-
-
-// CUs of the current device (the tile-shape choice counts rounds of them).
-inline int cu_count() {
-  static int n = 0;
-  if (n == 0) {
-    int dev = 0, v = 0;
-    if (hipGetDevice(&dev) == hipSuccess &&
-        hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && v > 0)
-      n = v;
-    else
-      n = 256;
-  }
-  return n;
-}
 
 // router.hip
 hipError_t router_prepare();
