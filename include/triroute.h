@@ -665,7 +665,8 @@ int triroute_linear_i8_workspace_bytes(int n_tok, int in, size_t *bytes);
 /* y = x W^T (+ residual) in 8-bit integers, for n_tok tokens, `in` input and `out` output channels:
  * the tokens are quantised as triroute_i8_quantize does, the products of codes are summed
  * exactly, and y[i, j] = sum * s_i * t_j (fp32, the token's scale, then the channel's) plus
- * residual[i, j] is rounded once to act.  The O-projection is this with residual = x.  A result does
+ * residual[i, j] is rounded once to act.  (sum * s_i may leave fp32 on the way only for a token whose
+ * largest magnitude lies outside [2^-119, 2^104].)  The O-projection is this with residual = x.  A result does
  * not depend on the other tokens of the call; a token that holds a NaN or an infinity has a
  * row of NaN.
  *   x, residual (or NULL), y: act, rows ldx, ldr, ldy elements apart, aligned to their element;

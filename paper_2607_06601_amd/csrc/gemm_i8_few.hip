@@ -358,15 +358,21 @@ static hipError_t launch_few(const P &p, int rows, int pitch, int tiles, int ny,
   return hipGetLastError();
 }
 
-// Rows that gain by it (us, GPU, against the pass over the rows and the product in launches of their own):
-// 768 -> 768, 1 token 3.6 / 7.1, 16 tokens 5.9 / 7.6; 2048 -> 2048, 1 token 4.0 / 10.4, 16 tokens 9.0 /
-// 10.4; QKV 410M, 1 token 5.0 / 14.9, 16 tokens 9.0 / 15.1.
+// Rows of one MFMA tile, as far as their codes fit; all of them gain by it (us, GPU, against the pass
+// over the rows and the product in launches of their own): 768 -> 768, 1 token 3.6 / 7.1, 16 tokens 5.9 /
+// 7.6; 2048 -> 2048, 1 token 4.0 / 10.4, 16 tokens 9.0 / 10.4; QKV 410M, 1 token 5.0 / 14.9, 16 tokens
+// 9.0 / 15.1.  More rows would need several tiles a block or a grid of them, which is not built.
 bool i8_few_fit(int rows, int cols) {
   return rows <= FEW_ROWS && int64_t(rows) * i8_pitch(cols) <= FEW_PANEL;
 }
-// Experts: up to four assignments (160M, 1 token 14.6 / 23.7 us, 2 tokens 17.0 / 24.6; 1.3B, 1 token 26 /
-// 35, 2 tokens 42 / 45, 3 tokens 57 / 54): with more experts in use their blocks are many, and each
-// normalises its rows again.
+// Experts: up to four assignments, where every layer gains; with more experts in use the blocks of a
+// wide layer are many, and each normalises its rows again (us a call of 2, 4, 6, 8, 16 assignments,
+// here / in launches of their own; narrow layers would gain by more):
+//   d 256,  d_ff 512    10.4 / 16.4  13.0 / 16.8  13.4 / 16.8  13.5 / 17.2
+//   d 512,  d_ff 1536   11.3 / 18.7  15.9 / 19.3  18.1 / 19.5  19.1 / 19.7  20.0 / 22.5
+//   d 768,  d_ff 2048   14.0 / 20.7  18.4 / 22.4  23.0 / 22.8  25.0 / 23.2  25.9 / 25.6
+//   d 1024, d_ff 2816   16.8 / 23.3  22.5 / 24.5  28.4 / 24.9  32.1 / 26.0  33.3 / 29.7
+//   d 2048, d_ff 5632   24.7 / 31.6  41.0 / 45.2  55.3 / 57.8  65.6 / 63.8  84.4 / 84.1
 bool i8_few_fit_moe(const triroute_cfg &cfg, int N) {
   return N * cfg.top_k <= 4 && i8_few_fit(N * cfg.top_k, std::max(cfg.d_model, cfg.d_ff));
 }

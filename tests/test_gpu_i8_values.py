@@ -1,4 +1,4 @@
-"""The 8-bit experts' values: the same in any batch, and over the whole range of fp32."""
+"""The 8-bit products' values: the same in any batch, and over the whole range of fp32."""
 import numpy as np
 import pytest
 import torch
@@ -9,7 +9,8 @@ from oracle import i8
 from paper_2607_06601_amd.device import to_dev
 
 from _common import npy, torch_act
-from test_gpu_i8 import DEV, Experts, device_lists, dirty, within
+from _i8 import tokens, weight
+from test_gpu_i8 import DEV, Experts, device_lists, dirty, matrix, run_linear, within
 
 pytestmark = pytest.mark.gpu
 
@@ -146,3 +147,33 @@ def test_gains_far_from_one(act, N, d, size, gain, eps):
     assert torch.isfinite(got).all()
     want, err = i8.moe(c.xt[rows], c.g2, *c.W, c.eidx[rows], c.gate[rows], act, eps=c.cfg.rms_eps)
     within(npy(got)[rows], want, err, "x_out")
+
+
+# ------------------------------------------------------------------ linear
+@pytest.mark.parametrize("act", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [3, 40, 3000])
+@pytest.mark.parametrize("size", [2.0 ** -119, 2.0 ** 104])
+def test_linear_of_the_largest_and_smallest_tokens(size, N, act):
+    k, m = 512, 264
+    x, (w, t) = tokens(67, "x", N, k, act), weight(67, "W", m, k)
+    x = gen.to_act(x / np.abs(x).max(axis=1, keepdims=True) * np.float32(size), act)
+    t = (t / np.float32(size)).astype(np.float32)
+    rows = some(N, 40)
+    for guard in (3, 16):
+        got = run_linear(to_dev(x, torch_act(act)), matrix(w, t), act, guard=guard)[rows]
+        within(got, *i8.linear(x[rows], w, t, act), "y")
+
+
+def test_linear_of_the_largest_tokens_and_longest_rows():
+    """Every code +-127 along 2^17 channels of 2^104: sum times the token's scale is next to
+    fp32's largest number."""
+    k = 131072
+    x = np.full((2, k), 2.0 ** 104, np.float32)
+    x[1, ::2] *= -1
+    w = np.full((3, k), 127, np.int8)
+    w[1, ::2], w[2] = -127, -127
+    t = np.full(3, 2.0 ** -110, np.float32)
+    y, err = i8.linear(x, w, t, "f32")
+    got = run_linear(to_dev(x, torch.float32), matrix(w, t), "f32")
+    within(got, y, err, "y")
+    assert np.abs(y).max() > 2.0 ** 17
