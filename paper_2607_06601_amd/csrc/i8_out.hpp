@@ -24,7 +24,7 @@ __device__ __forceinline__ float gated64(int32_t ag, int32_t au, float row, floa
 
 // h = silu(G) U of bf16 activations, in fp32: G and U are formed each with its own scales, as
 // every other sum is.  (Products of the scales alone may leave fp32 where G and U do not; one of them
-// for a row and one for a channel would save 16 of 1270 us at 1.3B, 16384 tokens.)  An exponential that
+// for a row and one for a channel would save at most 16 of 1270 us at 1.3B, 16384 tokens.)  An exponential that
 // overflows gives silu 0.
 __device__ __forceinline__ float gated(int32_t ag, int32_t au, float row, float cg, float cu) {
   const float g = dequant(ag, row, cg), u = dequant(au, row, cu);
